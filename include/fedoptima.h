@@ -389,6 +389,88 @@ FO_API int fo_select_split(const double* O, const double* S, int L, const double
  * ---------------------------------------------------------------------- */
 FO_API int fo_column_sums_noalloc(const void* x, int dtype, int64_t rows, int cols, float* out, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Attention with modified scores, forward and backward, for transformer
+ * blocks trained on long or packed sequences (on a device or beside the
+ * server); the paper has no counterpart.  For query i and key j of one
+ * sequence b and head h, with d = j - i:
+ *     z = scale * q_i . k_j;   softcap c > 0:  z <- c tanh(z / c)
+ *     slopes:  z <- z - slopes[h] |d|
+ *     table:   z <- z + table[h][bucket_of[clamp(d, -reach, reach) + reach]]
+ * A pair is allowed when (not causal, or j <= i, or j < prefix[b]) and, with
+ * documents, when both tokens have the same id >= 0; a negative id is
+ * padding.  P = softmax of z over the allowed keys and O = P V; a row that
+ * allows no key gives zeros and lse = -infinity.  Whatever padded tokens
+ * hold, NaN included, reaches no output of another token.
+ * Query head h reads key head h / (heads / kv_heads).  Sums, softmax
+ * statistics and gradients are held in fp32; P and dS are rounded to the
+ * tensors' type where they enter a product on the bf16 tensor-core path.
+ * All sums have a fixed order: equal calls give equal bits.
+ * ---------------------------------------------------------------------- */
+typedef struct fo_strided {  /* [batch][len][heads][head_dim], innermost stride 1 */
+  void* data;                /* device pointer                                  */
+  int64_t batch_stride, token_stride, head_stride; /* in elements               */
+} fo_strided;
+
+typedef struct fo_attention_spec {
+  int32_t batch, len;        /* sequences and tokens of each (0 allowed; len <= 2^20) */
+  int32_t heads, kv_heads;   /* heads a multiple of kv_heads                      */
+  int32_t head_dim;          /* 1..128                                            */
+  int32_t dtype;             /* FO_DTYPE_* of every tensor and of the table       */
+  int32_t causal;
+  int32_t buckets, reach;    /* with a table: 1..128 buckets, reach 1..512        */
+  float scale, softcap;      /* scale > 0; softcap 0: none                        */
+  const float* slopes;       /* device [heads] or NULL                            */
+  const void* table;         /* device [heads][buckets] or NULL (not with slopes) */
+  const uint8_t* bucket_of_host; /* host [2 reach + 1], entries below buckets; read
+                                during the call only                            */
+  const int32_t* documents;  /* device [batch][len] or NULL                       */
+  const int32_t* prefix;     /* device [batch] or NULL (causal only)              */
+} fo_attention_spec;
+
+/* Bytes of device workspace that a forward (backward = 0) or backward call
+ * with this spec needs, 0 when it needs none; -1 for a bad spec (no
+ * counterpart in the paper). */
+FO_API int64_t fo_attention_workspace(const fo_attention_spec* spec, int backward);
+/* O (o, written through its strides) and lse[b][h][i] = log sum exp z (natural
+ * log, contiguous fp32 [batch][heads][len]) on `stream` (a cudaStream_t, NULL =
+ * default).  The workspace (256-byte aligned, at least
+ * fo_attention_workspace bytes) is free again when the call's work on the
+ * stream is done.  Nothing is allocated, so a capturing stream may be
+ * passed.  FO_ERR_ARG for a bad spec, null or misaligned pointers, negative
+ * strides or overlapping output strides, or a workspace that is too small;
+ * nothing ran then (no counterpart in the paper). */
+FO_API int fo_attention_forward(const fo_attention_spec* spec, const fo_strided* q, const fo_strided* k,
+                         const fo_strided* v, const fo_strided* o, float* lse, void* workspace,
+                         int64_t workspace_bytes, void* stream);
+/* Gradients of a forward call, given its q, k, v, o and lse and dout = dL/dO:
+ * dq, dk, dv (written, not accumulated), and with a table its gradient
+ * dtable[heads][buckets] in the table's type (NULL: not wanted).  The same
+ * conventions as fo_attention_forward (no counterpart in the paper). */
+FO_API int fo_attention_backward(const fo_attention_spec* spec, const fo_strided* q, const fo_strided* k,
+                          const fo_strided* v, const fo_strided* o, const float* lse, const fo_strided* dout,
+                          const fo_strided* dq, const fo_strided* dk, const fo_strided* dv, void* dtable,
+                          void* workspace, int64_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Dropout around a residual, y = residual + keep(x), from a counter-based
+ * generator whose mask is never stored; the paper has no counterpart (its
+ * training uses none, and neither does the server's).  x, residual (NULL:
+ * none) and y are device matrices [rows][cols] of `dtype` with the given row
+ * strides in elements (innermost stride 1; residual_stride 0 broadcasts one
+ * row; y may be x or residual).  Element e = row * cols + col takes half e % 8
+ * (low half of each word first) of Philox4x32-10 with counter (e / 8, call)
+ * and key seed; it is kept when that 16-bit number is at least
+ * T = round(65536 p), and then scaled by 65536 / (65536 - T).  p in [0, 1].
+ * The gradient of x is the same call on dy, with no residual and the same
+ * (p, seed, call); the residual's gradient is dy.  Use another `call` for
+ * each layer and step.  FO_ERR_ARG for p outside [0, 1], an unknown dtype,
+ * null or misaligned pointers, negative strides or y_stride < cols.
+ * ---------------------------------------------------------------------- */
+FO_API int fo_dropout_add(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, void* y,
+                   int64_t y_stride, int dtype, int64_t rows, int64_t cols, double p, uint64_t seed,
+                   uint64_t call, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

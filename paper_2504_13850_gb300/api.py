@@ -42,6 +42,17 @@ class fo_server_cfg(C.Structure):
                  "num_classes", "dtype", "seq", "max_delay", "sched_policy")]
 
 
+class fo_strided(C.Structure):
+    _fields_ = [("data", C.c_void_p)] + [(n, C.c_int64) for n in ("batch_stride", "token_stride", "head_stride")]
+
+
+class fo_attention_spec(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("batch", "len", "heads", "kv_heads", "head_dim", "dtype", "causal",
+                                          "buckets", "reach")]
+                + [("scale", C.c_float), ("softcap", C.c_float)]
+                + [(n, C.c_void_p) for n in ("slopes", "table", "bucket_of_host", "documents", "prefix")])
+
+
 class FedOptimaError(RuntimeError):
     pass
 
@@ -101,6 +112,13 @@ _SIGS = [
     ("fo_server_store_params_device", C.c_int, [C.c_void_p, C.c_void_p, C.c_int64]),
     ("fo_select_split", C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p,
                                   C.POINTER(C.c_int), C.POINTER(C.c_double)]),
+    ("fo_attention_workspace", C.c_int64, [C.POINTER(fo_attention_spec), C.c_int]),
+    ("fo_attention_forward", C.c_int, [C.POINTER(fo_attention_spec)] + [C.POINTER(fo_strided)] * 4
+     + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    ("fo_attention_backward", C.c_int, [C.POINTER(fo_attention_spec)] + [C.POINTER(fo_strided)] * 4 + [C.c_void_p]
+     + [C.POINTER(fo_strided)] * 4 + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    ("fo_dropout_add", C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int,
+                                 C.c_int64, C.c_int64, C.c_double, C.c_uint64, C.c_uint64, C.c_void_p]),
 ]
 
 
@@ -409,3 +427,149 @@ def select_split(O, S, b, o, allowed=None):
     rc = lib().fo_select_split(O.ctypes.data, S.ctypes.data, len(O), b.ctypes.data, o.ctypes.data, len(b),
                                None if al is None else al.ctypes.data, C.byref(l), C.byref(cost))
     return rc, l.value, cost.value
+
+
+def relative_buckets(buckets, reach, bidirectional=True):
+    """The usual map from distance d = j - i to a bucket, uint8[2 * reach + 1]
+    for d = -reach..reach: half of a direction's buckets hold one small
+    distance each, the others logarithmic ranges up to `reach`.  Bidirectional
+    maps give each sign its own half; otherwise d > 0 shares bucket 0."""
+    half = buckets // 2 if bidirectional else buckets
+    if not 2 <= half <= 128 or buckets > 128 or reach < half:
+        raise ValueError("relative_buckets: 2..128 buckets per direction, reach at least that")
+    d = np.arange(-reach, reach + 1)
+    n = np.abs(d) if bidirectional else np.maximum(-d, 0)
+    near = half // 2
+    far = near + (np.log(np.maximum(n, 1) / near) / np.log(reach / near) * (half - near)).astype(np.int64)
+    b = np.where(n < near, n, np.minimum(far, half - 1))
+    return (b + np.where(d > 0, half, 0) if bidirectional else b).astype(np.uint8)
+
+
+def _rows4(t, like, name, heads=None):
+    """fo_strided of a 4-D device tensor [batch, len, heads, head_dim]."""
+    if t.dim() != 4 or not t.is_cuda or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name}: a 4-D device tensor of q's type and device is wanted")
+    if t.shape[:2] != like.shape[:2] or t.shape[3] != like.shape[3] or (heads is not None and t.shape[2] != heads):
+        raise ValueError(f"{name}: shape {tuple(t.shape)} does not fit q's {tuple(like.shape)}")
+    st = t.stride()
+    if st[3] != 1 and t.shape[3] > 1:
+        raise ValueError(f"{name}: its innermost stride must be 1")
+    return fo_strided(t.data_ptr(), st[0], st[1], st[2])
+
+
+def _small(t, shape, dtype, like, name):
+    if tuple(t.shape) != shape or t.dtype != dtype or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {shape} on q's device is wanted")
+    return t.data_ptr()
+
+
+def _attention_spec(q, k, causal, softcap, scale, slopes, table, buckets, documents, prefix):
+    import torch
+    if q.dim() != 4 or k.dim() != 4 or q.dtype not in (torch.bfloat16, torch.float32) or not q.is_cuda:
+        raise ValueError("q, k, v: 4-D bf16 or fp32 device tensors [batch, len, heads, head_dim]")
+    B, L, H, D = q.shape
+    s = fo_attention_spec(B, L, H, k.shape[2], D, DTYPE_BF16 if q.dtype == torch.bfloat16 else DTYPE_F32,
+                          1 if causal else 0, 0, 0, D ** -0.5 if scale is None and D else (scale or 0.0), softcap)
+    if slopes is not None:
+        s.slopes = _small(slopes, (H,), torch.float32, q, "slopes")
+    if table is not None:
+        if buckets is None or buckets.dtype != np.uint8 or buckets.ndim != 1 or buckets.size % 2 == 0 or table.dim() != 2:
+            raise ValueError("table: [heads, buckets] with its uint8 map of odd length (relative_buckets)")
+        s.buckets, s.reach = table.shape[1], buckets.size // 2
+        s.table = _small(table, (H, table.shape[1]), q.dtype, q, "table")
+        s.bucket_of_host = _ptr(buckets)
+    if documents is not None:
+        s.documents = _small(documents, (B, L), torch.int32, q, "documents")
+    if prefix is not None:
+        s.prefix = _small(prefix, (B,), torch.int32, q, "prefix")
+    return s
+
+
+def _stream_of(q, stream):
+    """(stream to pass on, context in which torch allocates for it)."""
+    import contextlib
+
+    import torch
+    if stream is None:
+        return torch.cuda.current_stream(q.device).cuda_stream, contextlib.nullcontext()
+    return stream, torch.cuda.stream(torch.cuda.ExternalStream(stream, device=q.device))
+
+
+def attention_forward(q, k, v, causal=False, softcap=0.0, scale=None, slopes=None, table=None, buckets=None,
+                      documents=None, prefix=None, out=None, stream=None):
+    """fo_attention_forward: (o, lse) of q [B, L, H, D], k and v [B, L, KV, D]
+    (any strides with the innermost 1).  scale defaults to D ** -0.5;
+    `buckets` is the table's host map (relative_buckets).  Runs on `stream`
+    (a cudaStream_t), by default torch's current stream."""
+    import torch
+    s = _attention_spec(q, k, causal, softcap, scale, slopes, table, buckets, documents, prefix)
+    st, ctx = _stream_of(q, stream)
+    with ctx:
+        o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+        lse = torch.empty(q.shape[0], q.shape[2], q.shape[1], dtype=torch.float32, device=q.device)
+        need = lib().fo_attention_workspace(C.byref(s), 0)
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need > 0 else None
+    args = [_rows4(q, q, "q"), _rows4(k, q, "k"), _rows4(v, q, "v", k.shape[2]), _rows4(o, q, "out", q.shape[2])]
+    _check(lib().fo_attention_forward(C.byref(s), *map(C.byref, args), lse.data_ptr(), ws.data_ptr() if need > 0 else None,
+                                      max(need, 0), st), "attention_forward")
+    return o, lse
+
+
+def attention_backward(dout, q, k, v, o, lse, causal=False, softcap=0.0, scale=None, slopes=None, table=None,
+                       buckets=None, documents=None, prefix=None, grads=None, stream=None):
+    """fo_attention_backward: (dq, dk, dv, dtable) with the arguments of the
+    forward call; dtable is None without a table.  `grads` may give the three
+    tensors to write (any strides with the innermost 1)."""
+    import torch
+    s = _attention_spec(q, k, causal, softcap, scale, slopes, table, buckets, documents, prefix)
+    if dout.stride(3) != 1:
+        dout = dout.contiguous()                 # an expanded gradient, as sum().backward() gives
+    st, ctx = _stream_of(q, stream)
+    with ctx:
+        dq, dk, dv = grads if grads is not None else (
+            torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+        dtable = None if table is None else torch.empty_like(table)
+        need = lib().fo_attention_workspace(C.byref(s), 1)
+        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need > 0 else None
+    H, KV = q.shape[2], k.shape[2]
+    args = [_rows4(t, q, n, h) for t, n, h in ((q, "q", H), (k, "k", KV), (v, "v", KV), (o, "o", H))]
+    more = [_rows4(t, q, n, h) for t, n, h in ((dout, "dout", H), (dq, "dq", H), (dk, "dk", KV), (dv, "dv", KV))]
+    _check(lib().fo_attention_backward(
+        C.byref(s), *map(C.byref, args), _small(lse, (q.shape[0], H, q.shape[1]), torch.float32, q, "lse"),
+        *map(C.byref, more), _ptr(dtable), ws.data_ptr() if need > 0 else None, max(need, 0), st), "attention_backward")
+    return dq, dk, dv, dtable
+
+
+def _matrix(t, like, name):
+    """(pointer, row stride) of `t` seen as a matrix [rows, cols of its last dimension]."""
+    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+        raise ValueError(f"{name}: x's shape, type and device are wanted")
+    if t.is_contiguous():
+        return t.data_ptr(), t.shape[-1]
+    if t.dim() == 2 and t.stride(1) == 1:
+        return t.data_ptr(), t.stride(0)
+    raise ValueError(f"{name}: contiguous, or a matrix with innermost stride 1")
+
+
+def dropout_add(x, residual, p, seed, call, out=None, stream=None):
+    """fo_dropout_add: residual + keep(x) (residual may be None) for a bf16 or
+    fp32 device tensor; (seed, call) name the mask.  Runs on `stream`, by
+    default torch's current stream."""
+    import torch
+    if not x.is_cuda or x.dtype not in (torch.bfloat16, torch.float32) or x.dim() < 1:
+        raise ValueError("x: a bf16 or fp32 device tensor")
+    st, ctx = _stream_of(x, stream)
+    with ctx:
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    cols = x.shape[-1]
+    xp, xs = _matrix(x, x, "x")
+    rp, rs = (None, 0) if residual is None else _matrix(residual, x, "residual")
+    yp, ys = _matrix(y, x, "out")
+    _check(lib().fo_dropout_add(xp, xs, rp, rs, yp, ys, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_F32,
+                                x.numel() // cols if cols else 0, cols, p, seed & (2**64 - 1), call & (2**64 - 1), st), "dropout_add")
+    return y
+
+
+def dropout_grad(dy, p, seed, call, out=None, stream=None):
+    """Gradient of dropout_add's x: keep(dy) with the mask that (seed, call) name."""
+    return dropout_add(dy, None, p, seed, call, out=out, stream=stream)

@@ -1,0 +1,693 @@
+// Scored attention (fo_scored.h): the C entry points, the preparation kernels
+// and the CUDA-core kernels, which take every type, head width and stride.
+//
+// The CUDA-core kernels work on 64 x 64 score tiles with 256 threads, each
+// thread 4 x 4 scores.  All operand tiles lie in shared memory as fp32,
+// [width][64 tokens]: both products of a tile then read 16-byte vectors along
+// the tokens, S = X U^T as one vector of each operand per width step (16 FMAs
+// per two reads) and the accumulating product (O += P V, dQ += dS K, ...) as
+// four columns of P against NC widths (16 NC FMAs per NC + 4 reads).  Vectors
+// are permuted by the width index, so that the transposing stores of a warp
+// (8 widths x 4 tokens) and the vector reads meet no bank twice.  Padding and
+// rows past the end are stored as zeros: what they hold never reaches a sum.
+// The backward pass is two kernels of one body: a tile of queries walks the
+// keys (dQ and the table gradient) and a tile of keys walks the queries
+// (dK, dV); every sum has a fixed order, at the price of forming the scores
+// twice.  Bound by the fp32 FMA rate.
+#include "fo_common.cuh"
+#include "fo_scored.h"
+#include "../../include/fedoptima.h"
+
+#include <climits>
+#include <cmath>
+#include <string>
+
+namespace fo {
+int report_error(int code, const std::string& msg);
+
+namespace {
+
+constexpr int kT = 64;             // tile of tokens
+constexpr int kThreads = 256;
+
+// ------------------------------------------------------------- preparation
+// Document ids padded to Lp (-1 past the sequence), and the summary of each
+// 64 ids; one warp per 64 ids.
+__global__ void __launch_bounds__(128) scored_docs_k(const int32_t* __restrict__ ids, int32_t* __restrict__ doc,
+                                                     int2* __restrict__ blk, int L, int Lp, int64_t n_blk) {
+  pdl_wait();
+  pdl_trigger();
+  const int64_t w = int64_t(blockIdx.x) * 4 + threadIdx.x / 32;
+  if (w >= n_blk) return;
+  const int per = Lp / kScoredBlock, lane = threadIdx.x % 32;
+  const int64_t b = w / per;
+  const int l0 = int(w % per) * kScoredBlock;
+  int2 s = make_int2(INT_MAX, -1);
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int l = l0 + lane + 32 * t;
+    int id = -1;
+    if (l < L) {
+      id = ids[b * L + l];
+      s = doc_join(s, id < 0 ? make_int2(int(0x80000000u) | INT_MAX, -1) : make_int2(id, id));
+    }
+    doc[b * Lp + l] = id;
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    s = doc_join(s, make_int2(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o)));
+  if (lane == 0) blk[w] = s;
+}
+
+// D_i = sum_d dO O and lse * log2(e), padded to Lp rows per (sequence, head).
+// VEC: 16-byte loads (8 bf16), DL lanes per row; else one warp per row.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(256) scored_delta_k(const __grid_constant__ ScoredParams p, int lanes) {
+  pdl_wait();
+  pdl_trigger();
+  const int per = 32 / lanes, lane = threadIdx.x % 32, sub = lane % lanes;
+  const int64_t row = (int64_t(blockIdx.x) * 8 + threadIdx.x / 32) * per + lane / lanes;   // (b, h, l)
+  const int64_t rows = int64_t(p.B) * p.H * p.Lp;
+  float d = 0.f;
+  bool live = false;
+  int64_t bh = 0;
+  int l = 0;
+  if (row < rows) {
+    l = int(row % p.Lp);
+    bh = row / p.Lp;
+    const int b = int(bh / p.H), h = int(bh % p.H);
+    live = l < p.L && (!p.doc || p.doc[int64_t(b) * p.Lp + l] >= 0);
+    if (live) {
+      const T* o = static_cast<const T*>(p.o.p) + b * p.o.sb + l * p.o.sl + h * p.o.sh;
+      const T* g = static_cast<const T*>(p.dout.p) + b * p.dout.sb + l * p.dout.sl + h * p.dout.sh;
+      if (VEC) {
+        if (sub * 8 < p.D) {
+          const uint4 a = reinterpret_cast<const uint4*>(o)[sub], c = reinterpret_cast<const uint4*>(g)[sub];
+          const bf16 *ab = reinterpret_cast<const bf16*>(&a), *cb = reinterpret_cast<const bf16*>(&c);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) d = fmaf(__bfloat162float(ab[e]), __bfloat162float(cb[e]), d);
+        }
+      } else {
+        for (int e = sub; e < p.D; e += lanes) d = fmaf(to_f(o[e]), to_f(g[e]), d);
+      }
+    }
+  }
+  for (int o = lanes / 2; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
+  if (row < rows && sub == 0) {
+    const float lse = live ? p.lse[bh * p.L + l] : -INFINITY;
+    p.delta[row] = live ? d : 0.f;
+    p.lse2[row] = lse == -INFINITY ? INFINITY : lse * kLog2e;
+  }
+}
+
+// dtable[h][b] = sum of its partials, one warp each, in a fixed order.
+template <typename T>
+__global__ void __launch_bounds__(128) scored_table_k(const float* __restrict__ part, T* __restrict__ out, int rows,
+                                                      int64_t n) {
+  pdl_wait();
+  pdl_trigger();
+  const int r = blockIdx.x * 4 + threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (r >= rows) return;
+  float s = 0.f;
+  for (int64_t i = lane; i < n; i += 32) s += part[r * n + i];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (lane == 0) out[r] = from_f<T>(s);
+}
+
+// ----------------------------------------------------------- shared helpers
+// Float offset of the 16-byte vector g (tokens 4 g .. 4 g + 3) of row d.
+__device__ __forceinline__ int at4(int d, int g) { return d * kT + ((g ^ (d & 7)) << 2); }
+
+// 64 tokens from l0 of one (sequence, head) -> dst[width][64], fp32, widths
+// rounded up to 8; tokens past the end and padding as zeros.
+template <typename T>
+__device__ __forceinline__ void load_tile(float* dst, const Strided& t, const ScoredParams& p, int b, int h, int l0) {
+  const T* base = static_cast<const T*>(t.p) + b * t.sb + h * t.sh;
+  const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
+  const int warp = threadIdx.x / 32, dl = (threadIdx.x % 32) >> 2, rl = threadIdx.x & 3;
+  const int n = (p.D + 7) / 8 * (kT / 4);
+  for (int e = warp; e < n; e += kThreads / 32) {
+    const int g = e % (kT / 4), d = e / (kT / 4) * 8 + dl, l = l0 + 4 * g + rl;
+    float v = 0.f;
+    if (l < p.L && d < p.D && (!doc || doc[l] >= 0)) v = to_f(base[l * t.sl + d]);
+    dst[at4(d, g) + rl] = v;
+  }
+}
+
+// s[r][c] = sum_d X[d][row r] U[d][column c].
+__device__ __forceinline__ void scores(float (&s)[4][4], const float* X, const float* U, int D8, int ty, int tx) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int c = 0; c < 4; ++c) s[r][c] = 0.f;
+#pragma unroll 4
+  for (int d = 0; d < D8; ++d) {
+    const float4 a = *reinterpret_cast<const float4*>(X + at4(d, ty));
+    const float4 u = *reinterpret_cast<const float4*>(U + at4(d, tx));
+    const float av[4] = {a.x, a.y, a.z, a.w}, uv[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[r][c] = fmaf(av[r], uv[c], s[r][c]);
+  }
+}
+
+// Offset of the vector of rows 4 ty .. 4 ty + 3 of column c of a 64 x 64 tile
+// held by columns.
+__device__ __forceinline__ int at_p(int c, int ty) { return c * kT + ((ty ^ ((c >> 2) & 15)) << 2); }
+
+__device__ __forceinline__ void put_tile(float* P, const float (&s)[4][4], int ty, int tx) {
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+    *reinterpret_cast<float4*>(P + at_p(4 * tx + c, ty)) = make_float4(s[0][c], s[1][c], s[2][c], s[3][c]);
+}
+
+// acc[r][n] += sum_c P[row r][c] W[width tx + 16 n][c].
+template <int NC>
+__device__ __forceinline__ void accumulate(float (&acc)[4][NC], const float* P, const float* W, int ty, int tx) {
+#pragma unroll 2
+  for (int g = 0; g < kT / 4; ++g) {
+    float4 w[NC];
+#pragma unroll
+    for (int n = 0; n < NC; ++n) w[n] = *reinterpret_cast<const float4*>(W + at4(tx + 16 * n, g));
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const float4 q = *reinterpret_cast<const float4*>(P + at_p(4 * g + c, ty));
+      const float qv[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+      for (int n = 0; n < NC; ++n) {
+        const float wv = c == 0 ? w[n].x : c == 1 ? w[n].y : c == 2 ? w[n].z : w[n].w;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[r][n] = fmaf(qv[r], wv, acc[r][n]);
+      }
+    }
+  }
+}
+
+// Widths [D, 16 NC) of an accumulating product read rows that load_tile does
+// not write; they are cleared once.
+__device__ __forceinline__ void clear_tail(float* W, int D, int rows) {
+  for (int e = (D + 7) / 8 * 8 * kT + threadIdx.x; e < rows * kT; e += kThreads) W[e] = 0.f;
+}
+
+template <typename T>
+__device__ __forceinline__ void load_bias(float* bias, const ScoredParams& p, int h) {
+  if (!p.table) return;
+  const T* t = static_cast<const T*>(p.table) + int64_t(h) * p.buckets;
+  for (int e = threadIdx.x; e < 2 * p.reach + 1; e += kThreads) bias[e] = to_f(t[p.map[e]]);
+}
+
+struct Pair {
+  int pf;                // the sequence's prefix
+  const int32_t* doc;    // its ids, or null
+  float slope;
+};
+
+__device__ __forceinline__ bool pair_allowed(const ScoredParams& p, const Pair& c, int i, int j) {
+  if (i >= p.L || j >= p.L) return false;
+  if (p.causal && j > i && j >= c.pf) return false;
+  return !c.doc || (c.doc[i] >= 0 && c.doc[i] == c.doc[j]);
+}
+// The biased score of raw product x, and 1 - tanh^2 of the cap (1 without).
+__device__ __forceinline__ float pair_score(const ScoredParams& p, const Pair& c, const float* bias, float x, int i,
+                                            int j, float* chain) {
+  float z = x * p.scale;
+  *chain = 1.f;
+  if (p.cap > 0.f) {
+    const float t = tanhf(z / p.cap);
+    z = p.cap * t;
+    *chain = 1.f - t * t;
+  }
+  const int d = j - i;
+  if (p.slopes) z -= c.slope * float(abs(d));
+  if (p.table) z += bias[min(max(d, -p.reach), p.reach) + p.reach];
+  return z;
+}
+
+__device__ __forceinline__ Pair pair_of(const ScoredParams& p, int b, int h) {
+  Pair c;
+  c.pf = p.prefix ? p.prefix[b] : 0;
+  c.doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
+  c.slope = p.slopes ? p.slopes[h] : 0.f;
+  return c;
+}
+__device__ __forceinline__ int tile_class(const ScoredParams& p, int pf, int b, int q0, int k0) {
+  int2 qd = make_int2(0, 0), kd = qd;
+  if (p.blk) {
+    const int2* blk = p.blk + int64_t(b) * (p.Lp / kScoredBlock);
+    qd = blk[q0 / kScoredBlock];
+    kd = blk[k0 / kScoredBlock];
+  }
+  return scored_class(p, pf, q0, q0 + kT, k0, k0 + kT, p.blk != nullptr, qd, kd);
+}
+
+template <typename T, int NC>
+__device__ __forceinline__ void store_rows(const Strided& t, const ScoredParams& p, const float (&acc)[4][NC],
+                                           const float (&mul)[4], int b, int h, int l0, int ty, int tx) {
+  T* base = static_cast<T*>(t.p) + b * t.sb + h * t.sh;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    const int l = l0 + 4 * ty + r;
+    if (l >= p.L) continue;
+#pragma unroll
+    for (int n = 0; n < NC; ++n)
+      if (tx + 16 * n < p.D) base[l * t.sl + tx + 16 * n] = from_f<T>(acc[r][n] * mul[r]);
+  }
+}
+
+// ----------------------------------------------------------------- forward
+template <typename T, int NC>
+__global__ void __launch_bounds__(kThreads) scored_fwd_k(const __grid_constant__ ScoredParams p) {
+  extern __shared__ __align__(16) float sm[];
+  constexpr int W = 16 * NC;
+  float *Q = sm, *K = Q + W * kT, *V = K + W * kT, *P = V + W * kT, *bias = P + kT * kT;
+  pdl_wait();
+  pdl_trigger();
+  const int tiles = (p.L + kT - 1) / kT, bh = blockIdx.x % (p.B * p.H);
+  const int q0 = (tiles - 1 - int(blockIdx.x / (p.B * p.H))) * kT;   // the longest causal rows first
+  const int b = bh / p.H, h = bh % p.H, kh = h / p.G, D8 = (p.D + 7) / 8 * 8;
+  const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+  const Pair pc = pair_of(p, b, h);
+  load_tile<T>(Q, p.q, p, b, h, q0);
+  load_bias<T>(bias, p, h);
+  clear_tail(V, p.D, W);
+  float acc[4][NC] = {}, m[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int r = 0; r < 4; ++r) m[r] = -INFINITY;
+  for (int k0 = 0; k0 < p.L; k0 += kT) {
+    if (tile_class(p, pc.pf, b, q0, k0) == kScoredNone) continue;
+    __syncthreads();
+    load_tile<T>(K, p.k, p, b, kh, k0);
+    load_tile<T>(V, p.v, p, b, kh, k0);
+    __syncthreads();
+    float s[4][4], chain;
+    scores(s, Q, K, D8, ty, tx);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int i = q0 + 4 * ty + r;
+      float top = m[r];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int j = k0 + 4 * tx + c;
+        s[r][c] = pair_allowed(p, pc, i, j) ? pair_score(p, pc, bias, s[r][c], i, j, &chain) : -INFINITY;
+        top = fmaxf(top, s[r][c]);
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float base = top == -INFINITY ? 0.f : top, keep = expf(m[r] - base);
+      float part = 0.f;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        s[r][c] = expf(s[r][c] - base);
+        part += s[r][c];
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+      sum[r] = sum[r] * keep + part;
+      m[r] = top;
+#pragma unroll
+      for (int n = 0; n < NC; ++n) acc[r][n] *= keep;
+    }
+    put_tile(P, s, ty, tx);
+    __syncthreads();
+    accumulate<NC>(acc, P, V, ty, tx);
+  }
+  float inv[4];
+#pragma unroll
+  for (int r = 0; r < 4; ++r) {
+    inv[r] = sum[r] > 0.f ? 1.f / sum[r] : (sum[r] == 0.f ? 0.f : sum[r]);   // a NaN row stays NaN
+    const int l = q0 + 4 * ty + r;
+    if (tx == 0 && l < p.L) p.lse[int64_t(bh) * p.L + l] = sum[r] == 0.f ? -INFINITY : m[r] + logf(sum[r]);
+  }
+  store_rows<T, NC>(p.o, p, acc, inv, b, h, q0, ty, tx);
+}
+
+// ---------------------------------------------------------------- backward
+// KV false: rows are queries (X = Q, Y = dO) walking keys (U = K, W = V):
+//   dQ = sum dS U, and the partial table gradient of this tile.
+// KV true: rows are keys (X = K, Y = V) walking the queries of every head of
+// the group (U = Q, W = dO): dV = sum P^T W, dK = sum dS^T U.
+template <typename T, int NC, bool KV>
+__global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__ ScoredParams p) {
+  extern __shared__ __align__(16) float sm[];
+  constexpr int WD = 16 * NC;
+  float *X = sm, *Y = X + WD * kT, *U = Y + WD * kT, *W = U + WD * kT, *P = W + WD * kT;
+  float* bias = P + kT * kT;
+  float* dist = bias + 2 * kMaxReach + 4;          // KV false: table gradient by distance
+  float* far = dist + 2 * kMaxReach + 4;           // [2][128] sums beyond the reach
+  pdl_wait();
+  pdl_trigger();
+  const int heads = KV ? p.KV : p.H, tiles = (p.L + kT - 1) / kT;
+  const int bh = blockIdx.x % (p.B * heads), slot = int(blockIdx.x / (p.B * heads));
+  const int tile = KV ? slot : tiles - 1 - slot, r0 = tile * kT;     // the longest causal tiles first
+  const int b = bh / heads, h0 = KV ? (bh % heads) * p.G : bh % heads, kh = h0 / p.G, D8 = (p.D + 7) / 8 * 8;
+  const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+  const bool grad = !KV && p.dtable;
+  load_tile<T>(X, KV ? p.k : p.q, p, b, KV ? kh : h0, r0);
+  load_tile<T>(Y, KV ? p.v : p.dout, p, b, KV ? kh : h0, r0);
+  clear_tail(U, p.D, WD);
+  clear_tail(W, p.D, WD);
+  if (grad)
+    for (int e = threadIdx.x; e < 2 * p.reach + 1; e += kThreads) dist[e] = 0.f;
+  float lo = 0.f, hi = 0.f;                        // sums of this thread's diagonals beyond the reach
+  float acc0[4][NC] = {}, acc1[4][NC] = {};
+  for (int g = 0; g < (KV ? p.G : 1); ++g) {
+    const int h = h0 + g;
+    const Pair pc = pair_of(p, b, h);
+    const float* lse2 = p.lse2 + (int64_t(b) * p.H + h) * p.Lp;
+    const float* delta = p.delta + (int64_t(b) * p.H + h) * p.Lp;
+    __syncthreads();
+    load_bias<T>(bias, p, h);
+    for (int c0 = 0; c0 < p.L; c0 += kT) {
+      if (tile_class(p, pc.pf, b, KV ? c0 : r0, KV ? r0 : c0) == kScoredNone) continue;
+      __syncthreads();
+      load_tile<T>(U, KV ? p.q : p.k, p, b, KV ? h : kh, c0);
+      load_tile<T>(W, KV ? p.dout : p.v, p, b, KV ? h : kh, c0);
+      __syncthreads();
+      float s[4][4], dp[4][4], chain[4][4];
+      scores(s, X, U, D8, ty, tx);
+      scores(dp, Y, W, D8, ty, tx);
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int row = r0 + 4 * ty + r, col = c0 + 4 * tx + c, i = KV ? col : row, j = KV ? row : col;
+          const bool ok = pair_allowed(p, pc, i, j);
+          const float z = pair_score(p, pc, bias, s[r][c], i, j, &chain[r][c]);
+          s[r][c] = ok ? exp2f(fmaf(z, kLog2e, -lse2[i])) : 0.f;
+          dp[r][c] = ok ? s[r][c] * (dp[r][c] - delta[i]) : 0.f;
+        }
+      if (grad) {
+        // each of 127 threads sums one diagonal of the tile in row order
+        put_tile(P, dp, ty, tx);
+        __syncthreads();
+        if (threadIdx.x < 2 * kT - 1) {
+          const int e = int(threadIdx.x) - (kT - 1);             // column - row
+          float t = 0.f;
+          for (int r = max(0, -e); r < min(kT, kT - e); ++r) t += P[at_p(r + e, r >> 2) + (r & 3)];
+          const int d = c0 - r0 + e;
+          if (d <= -p.reach) lo += t;
+          else if (d >= p.reach) hi += t;
+          else dist[d + p.reach] += t;
+        }
+        __syncthreads();
+      }
+      if (KV) {
+        put_tile(P, s, ty, tx);
+        __syncthreads();
+        accumulate<NC>(acc0, P, W, ty, tx);
+        __syncthreads();
+      }
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) dp[r][c] *= chain[r][c];
+      put_tile(P, dp, ty, tx);
+      __syncthreads();
+      accumulate<NC>(acc1, P, U, ty, tx);
+    }
+  }
+  const float one[4] = {1.f, 1.f, 1.f, 1.f}, sc[4] = {p.scale, p.scale, p.scale, p.scale};
+  if (KV) {
+    store_rows<T, NC>(p.dv, p, acc0, one, b, kh, r0, ty, tx);
+    store_rows<T, NC>(p.dk, p, acc1, sc, b, kh, r0, ty, tx);
+  } else {
+    store_rows<T, NC>(p.dq, p, acc1, sc, b, h0, r0, ty, tx);
+  }
+  if (grad) {
+    __syncthreads();
+    if (threadIdx.x < 128) {
+      far[threadIdx.x] = lo;
+      far[128 + threadIdx.x] = hi;
+    }
+    __syncthreads();
+    if (threadIdx.x < 2) {
+      float t = 0.f;
+      for (int e = 0; e < 128; ++e) t += far[128 * threadIdx.x + e];
+      dist[threadIdx.x ? 2 * p.reach : 0] += t;
+    }
+    __syncthreads();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int64_t n = int64_t(p.B) * tiles;
+    for (int k = warp; k < p.buckets; k += kThreads / 32) {
+      float t = 0.f;
+      for (int e = lane; e < 2 * p.reach + 1; e += 32)
+        if (p.map[e] == k) t += dist[e];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+      if (lane == 0) p.part[(int64_t(h0) * p.buckets + k) * n + int64_t(b) * tiles + tile] = t;
+    }
+  }
+}
+
+template <typename K>
+cudaError_t run(K kernel, int64_t blocks, size_t smem, cudaStream_t st, const ScoredParams& p) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+  if (e != cudaSuccess) return e;
+  return launch_k(kernel, dim3(unsigned(blocks)), dim3(kThreads), smem, st, p);
+}
+
+template <typename T, int NC>
+cudaError_t forward_width(const ScoredParams& p, cudaStream_t st) {
+  const int64_t tiles = ceil_div(p.L, kT);
+  const size_t smem = (size_t(3 * 16 * NC * kT) + kT * kT + 2 * kMaxReach + 4) * sizeof(float);
+  return run(scored_fwd_k<T, NC>, tiles * p.B * p.H, smem, st, p);
+}
+template <typename T, int NC>
+cudaError_t backward_width(const ScoredParams& p, cudaStream_t st) {
+  const int64_t tiles = ceil_div(p.L, kT);
+  const size_t smem =
+      (size_t(4 * 16 * NC * kT) + kT * kT + 2 * (2 * kMaxReach + 4) + 256) * sizeof(float);
+  cudaError_t e = run(scored_bwd_k<T, NC, true>, tiles * p.B * p.KV, smem, st, p);
+  if (e != cudaSuccess) return e;
+  return run(scored_bwd_k<T, NC, false>, tiles * p.B * p.H, smem, st, p);
+}
+// Accumulator columns per thread: 16 NC >= head width.
+template <typename T>
+cudaError_t forward_simt(const ScoredParams& p, cudaStream_t st) {
+  return p.D <= 32 ? forward_width<T, 2>(p, st) : p.D <= 64 ? forward_width<T, 4>(p, st) : forward_width<T, 8>(p, st);
+}
+template <typename T>
+cudaError_t backward_simt(const ScoredParams& p, cudaStream_t st) {
+  return p.D <= 32 ? backward_width<T, 2>(p, st)
+                   : p.D <= 64 ? backward_width<T, 4>(p, st) : backward_width<T, 8>(p, st);
+}
+
+// ------------------------------------------------------------- host checks
+int bad(const std::string& what) { return report_error(FO_ERR_ARG, what); }
+int cuda_error(cudaError_t e) { return report_error(FO_ERR_CUDA, cudaGetErrorString(e)); }
+
+constexpr int64_t kMaxLen = 1 << 20, kMaxTiles = 1 << 27;
+
+int check_spec(const fo_attention_spec* s) {
+  if (!s) return bad("attention: null spec");
+  if (s->batch < 0 || s->len < 0 || s->len > kMaxLen) return bad("attention: batch or len out of range");
+  if (s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads) return bad("attention: heads must be a multiple of kv_heads");
+  if (s->head_dim < 1 || s->head_dim > 128) return bad("attention: head_dim must be 1..128");
+  if (s->dtype != FO_DTYPE_F32 && s->dtype != FO_DTYPE_BF16) return bad("attention: unknown dtype");
+  if (!(s->scale > 0.f) || !std::isfinite(s->scale)) return bad("attention: scale must be positive and finite");
+  if (!(s->softcap >= 0.f) || !std::isfinite(s->softcap)) return bad("attention: softcap must be finite and not negative");
+  if (s->prefix && !s->causal) return bad("attention: a prefix needs the causal mask");
+  if (s->table && s->slopes) return bad("attention: one of slopes and table");
+  if (s->table) {
+    if (!s->bucket_of_host || s->buckets < 1 || s->buckets > 128) return bad("attention: buckets must be 1..128, with their map");
+    if (s->reach < 1 || s->reach > kMaxReach) return bad("attention: reach must be 1.." + std::to_string(kMaxReach));
+    for (int e = 0; e < 2 * s->reach + 1; ++e)
+      if (s->bucket_of_host[e] >= s->buckets) return bad("attention: bucket map entry " + std::to_string(e) + " is not below buckets");
+  }
+  // one grid dimension holds every tile of 64 tokens, and every 8 rows, of every sequence and head
+  const int64_t tiles = (int64_t(s->len) + kT - 1) / kT, bh = int64_t(s->batch) * s->heads;
+  if (tiles && bh > kMaxTiles / tiles) return bad("attention: more than 2^27 tiles of 64 tokens");
+  return FO_OK;
+}
+
+int check_tensor(const fo_strided* t, const fo_attention_spec* s, int heads, bool out, const char* name) {
+  const size_t size = s->dtype == FO_DTYPE_F32 ? 4 : 2;
+  if (!t || !t->data) return bad(std::string("attention: null ") + name);
+  if (reinterpret_cast<uintptr_t>(t->data) % size) return bad(std::string("attention: misaligned ") + name);
+  const int64_t st[3] = {t->batch_stride, t->token_stride, t->head_stride};
+  const int64_t n[3] = {s->batch, s->len, heads};
+  for (int e = 0; e < 3; ++e) {
+    if (n[e] <= 1) continue;
+    if (st[e] < 0 || (out && st[e] < s->head_dim)) return bad(std::string("attention: strides of ") + name);
+    if (st[e] > (int64_t(1) << 40)) return bad(std::string("attention: strides of ") + name);
+  }
+  return FO_OK;
+}
+
+Strided strided(const fo_strided* t) {
+  return Strided{t->data, t->batch_stride, t->token_stride, t->head_stride};
+}
+
+// The tensor-core kernels need 16-byte rows: 8-element multiples of the head
+// width, of every stride in use, and an aligned base.
+bool wide(const fo_strided* t, const fo_attention_spec* s, int heads) {
+  const int64_t st[3] = {t->batch_stride, t->token_stride, t->head_stride};
+  const int64_t n[3] = {s->batch, s->len, heads};
+  for (int e = 0; e < 3; ++e)
+    if (n[e] > 1 && (st[e] % 8 || st[e] < 8)) return false;
+  return reinterpret_cast<uintptr_t>(t->data) % 16 == 0;
+}
+
+struct Layout {
+  int64_t doc = 0, blk = 0, lse2 = 0, delta = 0, part = 0, bytes = 0;
+};
+// `part` is sized for the smaller (64-row) tiles of the CUDA-core kernels.
+Layout layout(const fo_attention_spec* s, bool backward) {
+  Layout a;
+  auto take = [&a](int64_t bytes) {
+    const int64_t at = a.bytes;
+    a.bytes += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  const int64_t Lp = (int64_t(s->len) + 127) / 128 * 128, B = s->batch, H = s->heads;
+  if (s->documents) {
+    a.doc = take(B * Lp * 4);
+    a.blk = take(B * (Lp / kScoredBlock) * 8);
+  }
+  if (backward) {
+    a.lse2 = take(B * H * Lp * 4);
+    a.delta = take(B * H * Lp * 4);
+    if (s->table) a.part = take(H * s->buckets * B * ((int64_t(s->len) + kT - 1) / kT) * 4);
+  }
+  return a;
+}
+
+ScoredParams params(const fo_attention_spec* s, const Layout& a, char* ws, bool backward) {
+  ScoredParams p = {};
+  p.B = s->batch;
+  p.L = s->len;
+  p.Lp = (s->len + 127) / 128 * 128;
+  p.H = s->heads;
+  p.KV = s->kv_heads;
+  p.G = s->heads / s->kv_heads;
+  p.D = s->head_dim;
+  p.causal = s->causal != 0;
+  p.scale = s->scale;
+  p.cap = s->softcap;
+  p.slopes = s->slopes;
+  p.table = s->table;
+  p.prefix = s->prefix;
+  if (s->table) {
+    p.buckets = s->buckets;
+    p.reach = s->reach;
+    for (int e = 0; e < 2 * s->reach + 1; ++e) p.map[e] = s->bucket_of_host[e];
+  }
+  if (s->documents) {
+    p.doc = reinterpret_cast<int32_t*>(ws + a.doc);
+    p.blk = reinterpret_cast<int2*>(ws + a.blk);
+  }
+  if (backward) {
+    p.lse2 = reinterpret_cast<float*>(ws + a.lse2);
+    p.delta = reinterpret_cast<float*>(ws + a.delta);
+    p.part = reinterpret_cast<float*>(ws + a.part);
+  }
+  return p;
+}
+
+cudaError_t prepare_docs(const fo_attention_spec* s, const ScoredParams& p, cudaStream_t st) {
+  if (!s->documents) return cudaSuccess;
+  const int64_t n = int64_t(p.B) * (p.Lp / kScoredBlock);
+  return launch_k(scored_docs_k, dim3(unsigned((n + 3) / 4)), dim3(128), 0, st, s->documents, p.doc, p.blk, p.L, p.Lp,
+                  n);
+}
+
+int check_workspace(const Layout& a, const void* ws, int64_t bytes) {
+  if (a.bytes == 0) return FO_OK;
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256) return bad("attention: null or misaligned workspace");
+  if (bytes < a.bytes) return bad("attention: workspace of " + std::to_string(bytes) + " bytes, " + std::to_string(a.bytes) + " needed");
+  return FO_OK;
+}
+
+}  // namespace
+}  // namespace fo
+
+using namespace fo;
+
+extern "C" {
+
+int64_t fo_attention_workspace(const fo_attention_spec* spec, int backward) {
+  if (check_spec(spec) != FO_OK) return -1;
+  return layout(spec, backward != 0).bytes;
+}
+
+int fo_attention_forward(const fo_attention_spec* spec, const fo_strided* q, const fo_strided* k, const fo_strided* v,
+                         const fo_strided* o, float* lse, void* workspace, int64_t workspace_bytes, void* stream) {
+  int rc = check_spec(spec);
+  if (rc != FO_OK) return rc;
+  if (spec->batch == 0 || spec->len == 0) return FO_OK;
+  if ((rc = check_tensor(q, spec, spec->heads, false, "q")) || (rc = check_tensor(k, spec, spec->kv_heads, false, "k")) ||
+      (rc = check_tensor(v, spec, spec->kv_heads, false, "v")) || (rc = check_tensor(o, spec, spec->heads, true, "o")))
+    return rc;
+  if (!lse) return bad("attention: null lse");
+  const Layout a = layout(spec, false);
+  if ((rc = check_workspace(a, workspace, workspace_bytes))) return rc;
+  ScoredParams p = params(spec, a, static_cast<char*>(workspace), false);
+  p.q = strided(q);
+  p.k = strided(k);
+  p.v = strided(v);
+  p.o = strided(o);
+  p.lse = lse;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = prepare_docs(spec, p, st);
+  if (e == cudaSuccess) e = spec->dtype == FO_DTYPE_F32 ? forward_simt<float>(p, st) : forward_simt<bf16>(p, st);
+  return e == cudaSuccess ? FO_OK : cuda_error(e);
+}
+
+int fo_attention_backward(const fo_attention_spec* spec, const fo_strided* q, const fo_strided* k, const fo_strided* v,
+                          const fo_strided* o, const float* lse, const fo_strided* dout, const fo_strided* dq,
+                          const fo_strided* dk, const fo_strided* dv, void* dtable, void* workspace,
+                          int64_t workspace_bytes, void* stream) {
+  int rc = check_spec(spec);
+  if (rc != FO_OK) return rc;
+  if (dtable && !spec->table) return bad("attention: dtable without a table");
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const bool f32 = spec->dtype == FO_DTYPE_F32;
+  if (spec->batch == 0 || spec->len == 0) {
+    if (!dtable) return FO_OK;
+    cudaError_t e = cudaMemsetAsync(dtable, 0, size_t(spec->heads) * spec->buckets * (f32 ? 4 : 2), st);
+    return e == cudaSuccess ? FO_OK : cuda_error(e);
+  }
+  if ((rc = check_tensor(q, spec, spec->heads, false, "q")) || (rc = check_tensor(k, spec, spec->kv_heads, false, "k")) ||
+      (rc = check_tensor(v, spec, spec->kv_heads, false, "v")) || (rc = check_tensor(o, spec, spec->heads, false, "o")) ||
+      (rc = check_tensor(dout, spec, spec->heads, false, "dout")) ||
+      (rc = check_tensor(dq, spec, spec->heads, true, "dq")) ||
+      (rc = check_tensor(dk, spec, spec->kv_heads, true, "dk")) ||
+      (rc = check_tensor(dv, spec, spec->kv_heads, true, "dv")))
+    return rc;
+  if (!lse) return bad("attention: null lse");
+  const Layout a = layout(spec, true);
+  if ((rc = check_workspace(a, workspace, workspace_bytes))) return rc;
+  ScoredParams p = params(spec, a, static_cast<char*>(workspace), true);
+  p.q = strided(q);
+  p.k = strided(k);
+  p.v = strided(v);
+  p.o = strided(o);
+  p.dout = strided(dout);
+  p.dq = strided(dq);
+  p.dk = strided(dk);
+  p.dv = strided(dv);
+  p.lse = const_cast<float*>(lse);
+  p.dtable = dtable;
+  cudaError_t e = prepare_docs(spec, p, st);
+  if (e != cudaSuccess) return cuda_error(e);
+  const int64_t rows = int64_t(p.B) * p.H * p.Lp;
+  const bool vec = !f32 && p.D % 8 == 0 && wide(o, spec, spec->heads) && wide(dout, spec, spec->heads);
+  const int lanes = vec ? (p.D <= 64 ? 8 : 16) : 32;
+  const unsigned blocks = unsigned((rows + 8 * (32 / lanes) - 1) / (8 * (32 / lanes)));
+  auto delta = f32 ? scored_delta_k<float, false> : vec ? scored_delta_k<bf16, true> : scored_delta_k<bf16, false>;
+  e = launch_k(delta, dim3(blocks), dim3(256), 0, st, p, lanes);
+  if (e == cudaSuccess) e = f32 ? backward_simt<float>(p, st) : backward_simt<bf16>(p, st);
+  if (e == cudaSuccess && dtable) {
+    const int n = p.H * p.buckets;
+    const int64_t parts = int64_t(p.B) * ((p.L + kT - 1) / kT);
+    e = f32 ? launch_k(scored_table_k<float>, dim3((n + 3) / 4), dim3(128), 0, st, p.part, static_cast<float*>(dtable),
+                       n, parts)
+            : launch_k(scored_table_k<bf16>, dim3((n + 3) / 4), dim3(128), 0, st, p.part, static_cast<bf16*>(dtable),
+                       n, parts);
+  }
+  return e == cudaSuccess ? FO_OK : cuda_error(e);
+}
+
+}  // extern "C"
