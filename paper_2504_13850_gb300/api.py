@@ -117,6 +117,7 @@ _SIGS = [
      + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
     ("fo_attention_backward", C.c_int, [C.POINTER(fo_attention_spec)] + [C.POINTER(fo_strided)] * 4 + [C.c_void_p]
      + [C.POINTER(fo_strided)] * 4 + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    ("fo_attention_error", C.c_int, [C.c_void_p]),
     ("fo_dropout_add", C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int,
                                  C.c_int64, C.c_int64, C.c_double, C.c_uint64, C.c_uint64, C.c_void_p]),
 ]
@@ -538,6 +539,14 @@ def attention_backward(dout, q, k, v, o, lse, causal=False, softcap=0.0, scale=N
         C.byref(s), *map(C.byref, args), _small(lse, (q.shape[0], H, q.shape[1]), torch.float32, q, "lse"),
         *map(C.byref, more), _ptr(dtable), ws.data_ptr() if need > 0 else None, max(need, 0), st), "attention_backward")
     return dq, dk, dv, dtable
+
+
+def attention_error(stream=None):
+    """Waits for `stream` (default: torch's current stream) and raises if a
+    tensor-core attention kernel gave up a bounded wait."""
+    import torch
+    st = torch.cuda.current_stream().cuda_stream if stream is None else stream
+    _check(lib().fo_attention_error(st), "attention_error")
 
 
 def _matrix(t, like, name):

@@ -70,6 +70,10 @@ int* tc_error_word(TcContext* c);
 // Tensor map of a row-major bf16 matrix [rows][cols] with 128-byte-swizzled
 // boxes of 64 columns x box_rows rows.
 bool tc_encode_2d(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, int box_rows);
+// The general form: a tiled bf16 map with 128-byte swizzle, dims and box
+// innermost first, strides in bytes of dims 1 and up.
+bool tc_encode(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
+               const uint32_t* box);
 
 // Tensor-core attention (k_attention_tc.cu): sequences of at most 128 tokens,
 // head width 64, bf16.  A plan holds the tensor maps of the packed q|k|v

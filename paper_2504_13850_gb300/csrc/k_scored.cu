@@ -631,7 +631,10 @@ int fo_attention_forward(const fo_attention_spec* spec, const fo_strided* q, con
   p.lse = lse;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = prepare_docs(spec, p, st);
-  if (e == cudaSuccess) e = spec->dtype == FO_DTYPE_F32 ? forward_simt<float>(p, st) : forward_simt<bf16>(p, st);
+  bool tc = spec->dtype == FO_DTYPE_BF16 && p.D % 8 == 0 && wide(q, spec, p.H) && wide(k, spec, p.KV) &&
+            wide(v, spec, p.KV) && wide(o, spec, p.H);
+  if (e == cudaSuccess && tc) e = scored_fwd_tc(p, st, &tc);
+  if (e == cudaSuccess && !tc) e = spec->dtype == FO_DTYPE_F32 ? forward_simt<float>(p, st) : forward_simt<bf16>(p, st);
   return e == cudaSuccess ? FO_OK : cuda_error(e);
 }
 
@@ -688,6 +691,14 @@ int fo_attention_backward(const fo_attention_spec* spec, const fo_strided* q, co
                        n, parts);
   }
   return e == cudaSuccess ? FO_OK : cuda_error(e);
+}
+
+int fo_attention_error(void* stream) {
+  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
+  int word = 0;
+  if (e == cudaSuccess) e = scored_fwd_error(&word);
+  if (e != cudaSuccess) return cuda_error(e);
+  return word ? report_error(FO_ERR_TIMEOUT, "an attention kernel timed out waiting (code " + std::to_string(word) + ")") : FO_OK;
 }
 
 }  // extern "C"

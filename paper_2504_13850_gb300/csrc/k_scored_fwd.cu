@@ -1,0 +1,414 @@
+// Scored attention forward on the tensor cores (fo_scored.h): bf16, head width
+// a multiple of 8 up to 128.
+//
+// A CTA owns NT tiles of 128 queries of one (sequence, head) and walks the
+// allowed blocks of 128 keys once, with the running maximum and sum of an
+// online softmax.  Warp roles: 4 NT softmax warps (one thread per query row),
+// one TMA warp, one MMA warp.  Per tile and block:
+//   S = Q K^T into 128 TMEM columns -> cap, bias and mask in registers ->
+//   P~ = 2^(c x - M) as bf16 into the first half of the same columns, the A
+//   operand of O += P~ V (P never touches shared memory).
+// The two tiles take turns: one's softmax runs while the other's products do,
+// and each K and V block is read once for 256 queries.  K and V share one ring
+// of TMA-filled stages.  O is rescaled in TMEM only when a row's maximum has
+// grown by more than 2^8, so a step normally touches O not at all; P~ is then
+// at most 2^8, which fp32 sums and bf16's exponent hold without loss.
+// Scores stay in raw units x with exponent factor c (scale * log2(e), or
+// log2(e) after a cap), so an uncapped, unbiased score costs one FMA and one
+// exponential.  tanh(y) = 1 - 2 / (1 + e^2y) has an absolute error of a few
+// 2^-24, against the 2^-11 relative error of the hardware's tanh.
+// Rounding: P~ to bf16 before its product, O once when stored.
+#include "fo_scored_tc.cuh"
+
+namespace fo {
+
+namespace {
+
+__device__ int g_err;     // set by a wait that gave up
+
+struct FwdParams {
+  ScoredParams s;
+  CUtensorMap q, k, v;
+};
+
+template <int DP, int NT>
+struct Fwd {
+  static constexpr int kSub = 16384;                       // 128 rows x 64 bf16
+  static constexpr int kTileBytes = DP / 64 * kSub;
+  static constexpr int kStages = NT == 2 ? (DP == 64 ? 6 : 4) : (DP == 64 ? 4 : 2);
+  static constexpr int kThreads = 128 * NT + 64;
+  static constexpr int kCols = NT == 2 ? 512 : 256;         // TMEM columns
+  static constexpr int kBars = 1 + 2 * kStages + 3 * NT;
+  static constexpr int kOps = (NT + kStages) * kTileBytes;
+  // operands, barriers (and the TMEM slot), bias by distance, bitmaps
+  static size_t smem(int L) {
+    const int words = (L + 4095) / 4096;
+    return 1024 + kOps + 8 * (kBars + 1) + 4 * (2 * kMaxReach + 4) + size_t(4) * words * (2 * NT + 1);
+  }
+};
+
+// x[32] of columns j0 .. j0 + 31: cap, bias and mask (units as above).
+struct Shape {
+  float cap, cap_in, slope;       // cap (0: none), its exponent factor, slope in score units (negated)
+  const float* bias;              // by distance + reach, in score units, or null
+  int reach, i, lim, id;          // query row, first key not allowed by position, document id
+  const int32_t* doc;             // the sequence's ids, or null
+};
+
+__device__ __forceinline__ void shape_scores(uint32_t (&r)[32], const Shape& a, int j0, int i0, bool some) {
+  if (a.cap > 0.f) {
+    const float two = 2.f * a.cap;
+#pragma unroll
+    for (int e = 0; e < 32; ++e) {
+      const float t = rcp(1.f + ex2(__uint_as_float(r[e]) * a.cap_in));
+      r[e] = __float_as_uint(fmaf(-two, t, a.cap));
+    }
+  }
+  if (a.bias) {
+    // i0: the warp's first row; distances of the warp's 32 x 32 patch
+    const int lo = j0 - i0 - 31, hi = j0 + 31 - i0;
+    if (lo >= a.reach || hi <= -a.reach) {
+      const float c = a.bias[lo >= a.reach ? 2 * a.reach : 0];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) + c);
+    } else if (lo >= -a.reach && hi <= a.reach) {
+      const float* c = a.bias + (j0 - a.i + a.reach);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) + c[e]);
+    } else {
+      const int d = j0 - a.i;
+#pragma unroll
+      for (int e = 0; e < 32; ++e)
+        r[e] = __float_as_uint(__uint_as_float(r[e]) + a.bias[min(max(d + e, -a.reach), a.reach) + a.reach]);
+    }
+  } else if (a.slope != 0.f) {
+    const float d = float(j0 - a.i);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(fmaf(a.slope, fabsf(d + float(e)), __uint_as_float(r[e])));
+  }
+  if (some) {
+    const int n = a.lim - j0;
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+      if (e >= n) r[e] = 0xff800000u;
+    if (a.doc) {
+      const int4* d = reinterpret_cast<const int4*>(a.doc + j0);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int4 v = __ldg(d + e);
+        if (v.x != a.id) r[4 * e] = 0xff800000u;
+        if (v.y != a.id) r[4 * e + 1] = 0xff800000u;
+        if (v.z != a.id) r[4 * e + 2] = 0xff800000u;
+        if (v.w != a.id) r[4 * e + 3] = 0xff800000u;
+      }
+    }
+  }
+}
+
+template <int DP, int NT>
+__global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 1) scored_fwd_tc_k(const __grid_constant__ FwdParams fp) {
+  using F = Fwd<DP, NT>;
+  const ScoredParams& p = fp.s;
+  extern __shared__ __align__(1024) char smem_raw[];
+  char* sm = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  char* sQ = sm;
+  char* ring = sm + NT * F::kTileBytes;
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sm + F::kOps);
+  uint64_t *qfull = bars, *full = bars + 1, *empty = full + F::kStages, *sfull = empty + F::kStages,
+           *pfull = sfull + NT, *ofull = pfull + NT;
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + F::kBars);
+  float* bias = reinterpret_cast<float*>(bars + F::kBars + 1);
+  const int words = (p.L + 4095) / 4096;
+  uint32_t* act = reinterpret_cast<uint32_t*>(bias + 2 * kMaxReach + 4);   // [NT][words]: blocks of the tile
+  uint32_t* some = act + NT * words;                                        // [NT][words]: blocks that need the mask
+  uint32_t* padded = some + NT * words;                                     // [words]: blocks that hold padding
+
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int tiles = (p.L + 128 * NT - 1) / (128 * NT), bh = blockIdx.x % (p.B * p.H);
+  const int q0 = (tiles - 1 - int(blockIdx.x / (p.B * p.H))) * 128 * NT;   // the longest causal rows first
+  const int b = bh / p.H, h = bh % p.H, kh = h / p.G;
+  if (threadIdx.x == 0) {
+    mbar_init(qfull, 1);
+    for (int e = 0; e < F::kStages; ++e) {
+      mbar_init(&full[e], 1);
+      mbar_init(&empty[e], 1);
+    }
+    for (int e = 0; e < NT; ++e) {
+      mbar_init(&sfull[e], 1);
+      mbar_init(&pfull[e], 128);
+      mbar_init(&ofull[e], 1);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  constexpr int kTma = 4 * NT, kMma = 4 * NT + 1;
+  if (warp == kMma) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tslot)),
+                 "r"(F::kCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (warp == kTma && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&fp.q)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&fp.k)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&fp.v)) : "memory");
+  }
+  pdl_wait();
+  // score units: raw products without a cap, natural ones after it
+  const float unit = p.cap > 0.f ? 1.f : p.scale, c = unit * kLog2e;
+  const int pf = p.prefix ? p.prefix[b] : 0;
+  if (p.table)
+    for (int e = threadIdx.x; e < 2 * p.reach + 1; e += F::kThreads)
+      bias[e] = __bfloat162float(static_cast<const bf16*>(p.table)[int64_t(h) * p.buckets + p.map[e]]) / unit;
+  for (int w = warp; w < words; w += F::kThreads / 32) {
+    const int k0 = (32 * w + lane) * 128;
+    const int2* blk = p.blk ? p.blk + int64_t(b) * (p.Lp / kScoredBlock) : nullptr;
+    int2 kd = make_int2(0, 0);
+    if (blk && k0 < p.L) kd = doc_join(blk[k0 / 64], blk[k0 / 64 + 1]);
+    bool any = false;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int i0 = q0 + 128 * t;
+      int cls = kScoredNone;
+      if (k0 < p.L && i0 < p.L) {
+        int2 qd = make_int2(0, 0);
+        if (blk) qd = doc_join(blk[i0 / 64], blk[i0 / 64 + 1]);
+        cls = scored_class(p, pf, i0, i0 + 128, k0, k0 + 128, blk != nullptr, qd, kd);
+        if (cls == kScoredAll && k0 + 128 > p.L) cls = kScoredSome;
+      }
+      const uint32_t on = __ballot_sync(0xffffffffu, cls != kScoredNone);
+      const uint32_t mask = __ballot_sync(0xffffffffu, cls == kScoredSome);
+      any = any || cls != kScoredNone;
+      if (lane == 0) {
+        act[t * words + w] = on;
+        some[t * words + w] = mask;
+      }
+    }
+    const uint32_t pad = __ballot_sync(0xffffffffu, any && kd.x < 0);
+    if (lane == 0) padded[w] = pad;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tslot;     // S / P of tile t: columns 128 t; O: 128 NT + DP t
+  pdl_trigger();                    // this block holds its tensor memory
+  Waits wait(&g_err);
+  const uint32_t* act1 = act + (NT - 1) * words;
+
+  if (warp == kTma) {
+    if (lane == 0) {
+      mbar_expect_tx(qfull, NT * F::kTileBytes);
+      for (int t = 0; t < NT; ++t)
+        for (int s = 0; s < DP / 64; ++s)
+          tma_4d(sQ + t * F::kTileBytes + s * F::kSub, &fp.q, qfull, 64 * s, q0 + 128 * t, h, b);
+      Bits list(act, act1, words);
+      int it = 0;
+      for (int jb = list.next(); jb >= 0 && !wait.dead; jb = list.next())
+        for (int kv = 0; kv < 2; ++kv, ++it) {
+          const int slot = it % F::kStages;
+          if (it >= F::kStages) wait.on(&empty[slot], (it / F::kStages - 1) & 1, 21);
+          if (wait.dead) break;
+          mbar_expect_tx(&full[slot], F::kTileBytes);
+          for (int s = 0; s < DP / 64; ++s)
+            tma_4d(ring + slot * F::kTileBytes + s * F::kSub, kv ? &fp.v : &fp.k, &full[slot], 64 * s, jb * 128, kh, b);
+        }
+      if (wait.dead) {   // let the copies in flight land before the block ends
+        mbar_wait(qfull, 0);
+        for (int e = max(0, it - F::kStages); e < it; ++e) mbar_wait(&full[e % F::kStages], (e / F::kStages) & 1);
+      }
+    }
+  } else if (warp == kMma) {
+    constexpr uint32_t id_s = instr_desc(128, false, false), id_o = instr_desc(DP, false, true);
+    auto issue_s = [&](int t, int slot) {
+      const uint32_t a = smem_u32(sQ + t * F::kTileBytes), k = smem_u32(ring + slot * F::kTileBytes);
+#pragma unroll
+      for (int e = 0; e < DP / 16; ++e) {
+        const uint32_t off = (e >> 2) * F::kSub + 32 * (e & 3);
+        mma_f16(tmem + 128 * t, smem_desc(a + off, 16, 1024), smem_desc(k + off, 16, 1024), id_s, e > 0 ? 1u : 0u);
+      }
+      mma_commit(&sfull[t]);
+    };
+    Bits list(act, act1, words);
+    int cur = list.next(), it = 0, step[2] = {0, 0};
+    wait.on_warp(qfull, 0, 22);
+    if (cur >= 0) {
+      wait.on_warp(&full[0], 0, 23);
+      tc_fence_after();
+      if (lane == 0 && !wait.dead) {
+        for (int t = 0; t < NT; ++t)
+          if (bit_of(act + t * words, cur)) issue_s(t, 0);
+        mma_commit(&empty[0]);
+      }
+      ++it;
+    }
+    while (cur >= 0 && !wait.dead) {
+      const int nxt = list.next(), vs = it % F::kStages, ks = (it + 1) % F::kStages;
+      wait.on_warp(&full[vs], (it / F::kStages) & 1, 24);
+      if (bit_of(padded, cur)) clear_padding(ring + vs * F::kTileBytes, 128, DP / 64, p.doc + int64_t(b) * p.Lp, cur * 128, p.L);
+      if (nxt >= 0) wait.on_warp(&full[ks], ((it + 1) / F::kStages) & 1, 25);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const uint32_t* at = act + t * words;
+        if (bit_of(at, cur)) {
+          wait.on_warp(&pfull[t], step[t] & 1, 26);
+          tc_fence_after();
+          if (lane == 0 && !wait.dead) {
+            const uint32_t v = smem_u32(ring + vs * F::kTileBytes);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              mma_f16_ta(tmem + 128 * NT + DP * t, tmem + 128 * t + 8 * e, smem_desc(v + 2048 * e, F::kSub, 1024), id_o,
+                         step[t] > 0 || e > 0 ? 1u : 0u);
+            mma_commit(&ofull[t]);
+          }
+          ++step[t];
+        }
+        if (nxt >= 0 && bit_of(at, nxt) && lane == 0 && !wait.dead) issue_s(t, ks);
+      }
+      if (lane == 0 && !wait.dead) {
+        mma_commit(&empty[vs]);
+        if (nxt >= 0) mma_commit(&empty[ks]);
+      }
+      it += 2;
+      cur = nxt;
+    }
+  } else {
+    const int t = warp / 4, quarter = warp % 4, i0 = q0 + 128 * t + 32 * quarter, i = i0 + lane;
+    const uint32_t lanes = uint32_t(32 * quarter) << 16;
+    const uint32_t s_col = tmem + lanes + 128 * t, o_col = tmem + lanes + 128 * NT + DP * t;
+    const uint32_t *mine = act + t * words, *masked = some + t * words;
+    Shape a;
+    a.cap = p.cap;
+    a.cap_in = p.cap > 0.f ? 2.f * kLog2e * p.scale / p.cap : 0.f;
+    a.slope = p.slopes ? -p.slopes[h] / unit : 0.f;
+    a.bias = p.table ? bias : nullptr;
+    a.reach = p.reach;
+    a.i = i;
+    a.lim = min(p.causal ? max(i + 1, pf) : p.L, p.L);
+    a.doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
+    a.id = a.doc && i < p.L ? a.doc[i] : 0;
+    if (a.id < 0) a.id = INT32_MIN;           // padding equals nothing, itself included
+    float m = -INFINITY, sum = 0.f;
+    int step = 0;
+    Bits list(mine, mine, words);
+    for (int jb = list.next(); jb >= 0; jb = list.next(), ++step) {
+      const bool mask = bit_of(masked, jb);
+      wait.on_warp(&sfull[t], step & 1, 27);
+      tc_fence_after();
+      uint32_t r[4][32];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) tmem_ld32_issue(s_col + 32 * g, r[g]);
+      float top[4];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        tmem_ld32_wait(r[g]);
+        shape_scores(r[g], a, jb * 128 + 32 * g, i0, mask);
+        top[g] = __uint_as_float(r[g][0]);
+#pragma unroll
+        for (int e = 1; e < 32; ++e) top[g] = fmaxf(top[g], __uint_as_float(r[g][e]));
+      }
+      const float now = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+      if (step == 0) {
+        m = now;
+      } else {
+        const bool need = (now - m) * c > 8.f;
+        if (__any_sync(0xffffffffu, need)) {
+          const float keep = need ? ex2((m - now) * c) : 1.f;
+          wait.on_warp(&ofull[t], (step - 1) & 1, 28);
+          tc_fence_after();
+#pragma unroll 1
+          for (int g = 0; g < DP / 32; ++g) {
+            uint32_t o[32];
+            tmem_ld32(o_col + 32 * g, o);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+            tmem_st32(o_col + 32 * g, o);
+          }
+          sum *= keep;
+          if (need) m = now;
+        }
+      }
+      const float base = m == -INFINITY ? 0.f : m * c;
+      float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        uint32_t w[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const float x = ex2(fmaf(__uint_as_float(r[2 * g + e / 16][2 * (e % 16)]), c, -base));
+          const float y = ex2(fmaf(__uint_as_float(r[2 * g + e / 16][2 * (e % 16) + 1]), c, -base));
+          part[e & 1] += x;
+          part[2 + (e & 1)] += y;
+          w[e] = bf16_pair(x, y);
+        }
+        tmem_st32(s_col + 32 * g, w);
+      }
+      sum += (part[0] + part[1]) + (part[2] + part[3]);
+      tmem_st_wait();
+      tc_fence_before();
+      mbar_arrive(&pfull[t]);
+    }
+    const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);     // a NaN row stays NaN
+    if (step > 0) {
+      wait.on_warp(&ofull[t], (step - 1) & 1, 29);
+      tc_fence_after();
+    }
+    if (i < p.L) p.lse[int64_t(bh) * p.L + i] = sum == 0.f ? -INFINITY : m * c * kLn2 + logf(sum);
+    bf16* row = static_cast<bf16*>(p.o.p) + b * p.o.sb + int64_t(i) * p.o.sl + h * p.o.sh;
+#pragma unroll 1
+    for (int g = 0; g < DP / 32; ++g) {
+      uint32_t o[32];
+      if (step > 0) {
+        tmem_ld32(o_col + 32 * g, o);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) o[e] = 0u;
+      }
+      if (i >= p.L) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (32 * g + 8 * e >= p.D) break;
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          w[k] = bf16_pair(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv);
+        reinterpret_cast<uint4*>(row + 32 * g)[e] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMma) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(F::kCols) : "memory");
+  }
+}
+
+template <int DP, int NT>
+cudaError_t launch(const FwdParams& fp, cudaStream_t st) {
+  using F = Fwd<DP, NT>;
+  const size_t smem = F::smem(fp.s.L);
+  auto k = scored_fwd_tc_k<DP, NT>;
+  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+  if (e != cudaSuccess) return e;
+  e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, int(cudaSharedmemCarveoutMaxShared));
+  if (e != cudaSuccess) return e;
+  const int64_t tiles = ceil_div(fp.s.L, 128 * NT);
+  return launch_k(k, dim3(unsigned(tiles * fp.s.B * fp.s.H)), dim3(F::kThreads), smem, st, fp);
+}
+
+}  // namespace
+
+cudaError_t scored_fwd_tc(const ScoredParams& p, cudaStream_t st, bool* ok) {
+  FwdParams fp;
+  fp.s = p;
+  *ok = scored_map(&fp.q, p.q, p, p.H, 128) && scored_map(&fp.k, p.k, p, p.KV, 128) &&
+        scored_map(&fp.v, p.v, p, p.KV, 128);
+  if (!*ok) return cudaSuccess;
+  // Two query tiles per CTA share each K and V block and overlap softmax with
+  // products; a sequence of one tile would leave the second one empty.
+  if (p.L <= 128) return p.D <= 64 ? launch<64, 1>(fp, st) : launch<128, 1>(fp, st);
+  return p.D <= 64 ? launch<64, 2>(fp, st) : launch<128, 2>(fp, st);
+}
+
+cudaError_t scored_fwd_error(int* word) { return cudaMemcpyFromSymbol(word, g_err, sizeof(int)); }
+
+}  // namespace fo

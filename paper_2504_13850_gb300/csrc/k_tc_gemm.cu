@@ -354,6 +354,11 @@ bool tc_encode_2d(CUtensorMap* m, const void* base, int64_t rows, int64_t cols, 
   return map_2d(m, base, rows, cols, box_rows);
 }
 
+bool tc_encode(CUtensorMap* m, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
+               const uint32_t* box) {
+  return make_map(m, base, rank, dims, strides, box);
+}
+
 int* tc_error_word(TcContext* c) { return c ? c->err : nullptr; }
 
 void tc_set_lane(TcGemm* g, int lane) {

@@ -54,7 +54,7 @@ def check(x, how, grads=None, out=None):
     ref, err = R.attention(x["q"], x["k"], x["v"], x["dout"], **how)
     o, lse = api.attention_forward(x["q"], x["k"], x["v"], out=out, **how)
     dq, dk, dv, dtable = api.attention_backward(x["dout"], x["q"], x["k"], x["v"], o, lse, grads=grads, **how)
-    torch.cuda.synchronize()
+    api.attention_error()
     got = {"o": o, "lse": lse, "dq": dq, "dk": dk, "dv": dv, "dtable": dtable}
     for name, want in ref.items():
         g = got[name].double()
