@@ -86,7 +86,5 @@ cudaError_t scored_bwd_tc(const ScoredParams& p, cudaStream_t st, bool* ok);
 // The word the tensor-core kernels set when a bounded wait gives up (0: none).
 cudaError_t scored_fwd_error(int* word);
 cudaError_t scored_bwd_error(int* word);
-// Query tiles per sequence whose table gradients are partial sums.
-int scored_part_tiles(int L, bool tc);
 
 }  // namespace fo

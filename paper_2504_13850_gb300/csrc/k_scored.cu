@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(128) scored_docs_k(const int32_t* __restrict__
     const int l = l0 + lane + 32 * t;
     int id = -1;
     if (l < L) {
-      id = ids[b * L + l];
+      id = max(ids[b * L + l], -1);      // one id for all padding
       s = doc_join(s, id < 0 ? make_int2(int(0x80000000u) | INT_MAX, -1) : make_int2(id, id));
     }
     doc[b * Lp + l] = id;
@@ -681,10 +681,13 @@ int fo_attention_backward(const fo_attention_spec* spec, const fo_strided* q, co
   const unsigned blocks = unsigned((rows + 8 * (32 / lanes) - 1) / (8 * (32 / lanes)));
   auto delta = f32 ? scored_delta_k<float, false> : vec ? scored_delta_k<bf16, true> : scored_delta_k<bf16, false>;
   e = launch_k(delta, dim3(blocks), dim3(256), 0, st, p, lanes);
-  if (e == cudaSuccess) e = f32 ? backward_simt<float>(p, st) : backward_simt<bf16>(p, st);
+  bool tc = vec && wide(q, spec, p.H) && wide(k, spec, p.KV) && wide(v, spec, p.KV) && wide(dq, spec, p.H) &&
+            wide(dk, spec, p.KV) && wide(dv, spec, p.KV);
+  if (e == cudaSuccess && tc) e = scored_bwd_tc(p, st, &tc);
+  if (e == cudaSuccess && !tc) e = f32 ? backward_simt<float>(p, st) : backward_simt<bf16>(p, st);
   if (e == cudaSuccess && dtable) {
     const int n = p.H * p.buckets;
-    const int64_t parts = int64_t(p.B) * ((p.L + kT - 1) / kT);
+    const int64_t parts = int64_t(p.B) * ceil_div(p.L, tc ? 128 : kT);     // query tiles of the kernel that ran
     e = f32 ? launch_k(scored_table_k<float>, dim3((n + 3) / 4), dim3(128), 0, st, p.part, static_cast<float*>(dtable),
                        n, parts)
             : launch_k(scored_table_k<bf16>, dim3((n + 3) / 4), dim3(128), 0, st, p.part, static_cast<bf16*>(dtable),
@@ -697,6 +700,7 @@ int fo_attention_error(void* stream) {
   cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
   int word = 0;
   if (e == cudaSuccess) e = scored_fwd_error(&word);
+  if (e == cudaSuccess && !word) e = scored_bwd_error(&word);
   if (e != cudaSuccess) return cuda_error(e);
   return word ? report_error(FO_ERR_TIMEOUT, "an attention kernel timed out waiting (code " + std::to_string(word) + ")") : FO_OK;
 }
