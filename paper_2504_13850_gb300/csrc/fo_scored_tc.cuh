@@ -20,6 +20,50 @@ __device__ __forceinline__ float rcp(float x) {
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Pairs of fp32 in one instruction (two independent roundings).
+struct F2 {
+  uint64_t v;
+};
+__device__ __forceinline__ F2 f2(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ F2 f2u(uint32_t a, uint32_t b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ void split(F2 p, float& a, float& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p.v));
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+// x <- x + y for two neighbours of a register array of fp32 bits.
+__device__ __forceinline__ void add_to(uint32_t& a, uint32_t& b, F2 y) {
+  float u, v;
+  split(add2(f2u(a, b), y), u, v);
+  a = __float_as_uint(u);
+  b = __float_as_uint(v);
+}
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&h);
@@ -66,6 +110,68 @@ struct Bits {
 };
 __device__ __forceinline__ bool bit_of(const uint32_t* map, int i) { return (map[i >> 5] >> (i & 31)) & 1u; }
 
+// Bias kinds, compile-time in the kernels.
+enum { kBiasNone = 0, kBiasSlope = 1, kBiasTable = 2 };
+
+// The table's biases by distance, extended by kExt on both sides with the
+// outermost values: a patch of up to 32 x 64 scores that is not entirely
+// beyond the reach then reads it directly.
+constexpr int kExt = 96;
+constexpr int kBiasFloats = 2 * kMaxReach + 2 * kExt + 4;
+__device__ __forceinline__ void load_bias(float* bias, const ScoredParams& p, int h, float inv_unit, int tid, int n) {
+  const bf16* t = static_cast<const bf16*>(p.table) + int64_t(h) * p.buckets;
+  for (int e = tid; e < 2 * p.reach + 1 + 2 * kExt; e += n)
+    bias[e] = __bfloat162float(t[p.map[min(max(e - kExt, 0), 2 * p.reach)]]) * inv_unit;
+}
+
+// N scores (fp32 bits) of one query row, keys j0 .. j0 + N - 1 -> score units:
+// the cap (q, when asked for, receives 1 / (1 + e^2y), from which tanh y =
+// 1 - 2 q and its derivative 4 q (1 - q) follow) and the bias.  DIR is +1 when
+// the columns are keys and -1 when they are queries (the row then is the key);
+// d = distance of column 0, lo and hi the bounds of the warp's distances.
+struct Shape {
+  float cap, cap_in, slope;     // cap; its exponent factor; the slope, negated, in score units
+  const float* bias;
+  int reach;
+};
+template <int N, int BIAS, bool CAP, int DIR, bool KEEP>
+__device__ __forceinline__ void shape_scores(uint32_t (&r)[N], uint32_t (&q)[N], const Shape& a, int d, int lo, int hi) {
+  if (CAP) {
+    const float two = -2.f * a.cap;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float t = rcp(1.f + ex2(__uint_as_float(r[e]) * a.cap_in));
+      if (KEEP) q[e] = __float_as_uint(t);
+      r[e] = __float_as_uint(fmaf(two, t, a.cap));
+    }
+  }
+  if (BIAS == kBiasTable) {
+    if (lo >= a.reach || hi <= -a.reach) {
+      const float c = a.bias[kExt + (lo >= a.reach ? 2 * a.reach : 0)];
+#pragma unroll
+      for (int e = 0; e < N; e += 2) add_to(r[e], r[e + 1], f2(c, c));
+    } else {
+      const float* c = a.bias + (d + a.reach + kExt);
+#pragma unroll
+      for (int e = 0; e < N; e += 2) add_to(r[e], r[e + 1], f2(c[DIR * e], c[DIR * (e + 1)]));
+    }
+  }
+  if (BIAS == kBiasSlope) {
+    const float f = float(d);
+#pragma unroll
+    for (int e = 0; e < N; ++e) r[e] = __float_as_uint(fmaf(a.slope, fabsf(f + float(DIR * e)), __uint_as_float(r[e])));
+  }
+}
+__device__ __forceinline__ Shape shape_of(const ScoredParams& p, int h, float unit, const float* bias) {
+  Shape a;
+  a.cap = p.cap;
+  a.cap_in = p.cap > 0.f ? 2.f * kLog2e * p.scale / p.cap : 0.f;
+  a.slope = p.slopes ? -p.slopes[h] / unit : 0.f;
+  a.bias = bias;
+  a.reach = p.reach;
+  return a;
+}
+
 // Clears the rows of padded tokens of a swizzled tile of `rows` rows and
 // `subs` 64-column sub-tiles (a whole warp; a row's swizzled units stay within
 // its 128 bytes), so that what they hold meets no product as an operand summed
@@ -79,6 +185,16 @@ __device__ __forceinline__ void clear_padding(char* tile, int rows, int subs, co
         for (int u = 0; u < 8; ++u) st_shared4(smem_u32(tile) + s * rows * 128 + r * 128 + u * 16, 0u, 0u, 0u, 0u);
   fence_proxy_async_smem();
   __syncwarp();
+}
+
+// Calls f.template operator()<BIAS, CAP>() for the bias and cap of p.
+template <typename Fn>
+cudaError_t with_shape(const ScoredParams& p, Fn f) {
+  if (p.cap > 0.f)
+    return p.table ? f.template operator()<kBiasTable, true>()
+                   : p.slopes ? f.template operator()<kBiasSlope, true>() : f.template operator()<kBiasNone, true>();
+  return p.table ? f.template operator()<kBiasTable, false>()
+                 : p.slopes ? f.template operator()<kBiasSlope, false>() : f.template operator()<kBiasNone, false>();
 }
 
 // Tensor map of [batch][len][heads][head_dim] as {head_dim, len, heads, batch}

@@ -3,20 +3,26 @@
 //
 // A CTA owns NT tiles of 128 queries of one (sequence, head) and walks the
 // allowed blocks of 128 keys once, with the running maximum and sum of an
-// online softmax.  Warp roles: 4 NT softmax warps (one thread per query row),
-// one TMA warp, one MMA warp.  Per tile and block:
+// online softmax.  Warp roles: 8 NT softmax warps, one TMA warp, one MMA warp.
+// Per tile and block:
 //   S = Q K^T into 128 TMEM columns -> cap, bias and mask in registers ->
-//   P~ = 2^(c x - M) as bf16 into the first half of the same columns, the A
+//   P~ = 2^(c x - M) as bf16 back into the columns it came from, the A
 //   operand of O += P~ V (P never touches shared memory).
 // The two tiles take turns: one's softmax runs while the other's products do,
 // and each K and V block is read once for 256 queries.  K and V share one ring
-// of TMA-filled stages.  O is rescaled in TMEM only when a row's maximum has
-// grown by more than 2^8, so a step normally touches O not at all; P~ is then
-// at most 2^8, which fp32 sums and bf16's exponent hold without loss.
+// of TMA-filled stages.  A query row is shared by two threads, 64 keys each,
+// which exchange their maxima through shared memory once per block: sixteen
+// warps hide the TMEM and barrier latencies that eight (one thread per row)
+// left exposed, at half of the registers.
+// O is rescaled in TMEM only when a row's maximum has grown by more than 2^8,
+// so a step normally touches O not at all; P~ is then at most 2^8, which fp32
+// sums and bf16's exponent hold without loss.
 // Scores stay in raw units x with exponent factor c (scale * log2(e), or
-// log2(e) after a cap), so an uncapped, unbiased score costs one FMA and one
-// exponential.  tanh(y) = 1 - 2 / (1 + e^2y) has an absolute error of a few
-// 2^-24, against the 2^-11 relative error of the hardware's tanh.
+// log2(e) after a cap), so an uncapped, unbiased score costs half a packed FMA
+// and one exponential.  tanh(y) = 1 - 2 / (1 + e^2y) has an absolute error of a
+// few 2^-24, against the 2^-11 relative error of the hardware's tanh.
+// The bias kind and the cap are template parameters: the branches cost
+// instruction fetches even when not taken.
 // Rounding: P~ to bf16 before its product, O once when stored.
 #include "fo_scored_tc.cuh"
 
@@ -36,77 +42,53 @@ struct Fwd {
   static constexpr int kSub = 16384;                       // 128 rows x 64 bf16
   static constexpr int kTileBytes = DP / 64 * kSub;
   static constexpr int kStages = NT == 2 ? (DP == 64 ? 6 : 4) : (DP == 64 ? 4 : 2);
-  static constexpr int kThreads = 128 * NT + 64;
+  static constexpr int kThreads = 256 * NT + 64;
   static constexpr int kCols = NT == 2 ? 512 : 256;         // TMEM columns
   static constexpr int kBars = 1 + 2 * kStages + 3 * NT;
   static constexpr int kOps = (NT + kStages) * kTileBytes;
-  // operands, barriers (and the TMEM slot), bias by distance, bitmaps
-  static size_t smem(int L) {
+  static constexpr int kXch = 2 * NT * 256;                 // floats: [step parity][tile][half][row]
+  // operands, barriers (and the TMEM slot), exchanged maxima, bias, bitmaps
+  static size_t smem(int L, bool table) {
     const int words = (L + 4095) / 4096;
-    return 1024 + kOps + 8 * (kBars + 1) + 4 * (2 * kMaxReach + 4) + size_t(4) * words * (2 * NT + 1);
+    return 1024 + kOps + 8 * (kBars + 1) + 4 * kXch + (table ? 4 * kBiasFloats : 0) + size_t(4) * words * (2 * NT + 1);
   }
 };
 
-// x[32] of columns j0 .. j0 + 31: cap, bias and mask (units as above).
-struct Shape {
-  float cap, cap_in, slope;       // cap (0: none), its exponent factor, slope in score units (negated)
-  const float* bias;              // by distance + reach, in score units, or null
-  int reach, i, lim, id;          // query row, first key not allowed by position, document id
-  const int32_t* doc;             // the sequence's ids, or null
-};
-
-__device__ __forceinline__ void shape_scores(uint32_t (&r)[32], const Shape& a, int j0, int i0, bool some) {
-  if (a.cap > 0.f) {
-    const float two = 2.f * a.cap;
+// Minus infinity where key j0 + e is not allowed: from `lim` on by position,
+// or of another document than `id`.
+__device__ __forceinline__ void mask_keys(uint32_t (&r)[32], int j0, int lim, const int32_t* doc, int id) {
+  const int n = lim - j0;
 #pragma unroll
-    for (int e = 0; e < 32; ++e) {
-      const float t = rcp(1.f + ex2(__uint_as_float(r[e]) * a.cap_in));
-      r[e] = __float_as_uint(fmaf(-two, t, a.cap));
-    }
-  }
-  if (a.bias) {
-    // i0: the warp's first row; distances of the warp's 32 x 32 patch
-    const int lo = j0 - i0 - 31, hi = j0 + 31 - i0;
-    if (lo >= a.reach || hi <= -a.reach) {
-      const float c = a.bias[lo >= a.reach ? 2 * a.reach : 0];
+  for (int e = 0; e < 32; ++e)
+    if (e >= n) r[e] = 0xff800000u;
+  if (doc) {
+    const int4* d = reinterpret_cast<const int4*>(doc + j0);
 #pragma unroll
-      for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) + c);
-    } else if (lo >= -a.reach && hi <= a.reach) {
-      const float* c = a.bias + (j0 - a.i + a.reach);
-#pragma unroll
-      for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) + c[e]);
-    } else {
-      const int d = j0 - a.i;
-#pragma unroll
-      for (int e = 0; e < 32; ++e)
-        r[e] = __float_as_uint(__uint_as_float(r[e]) + a.bias[min(max(d + e, -a.reach), a.reach) + a.reach]);
-    }
-  } else if (a.slope != 0.f) {
-    const float d = float(j0 - a.i);
-#pragma unroll
-    for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(fmaf(a.slope, fabsf(d + float(e)), __uint_as_float(r[e])));
-  }
-  if (some) {
-    const int n = a.lim - j0;
-#pragma unroll
-    for (int e = 0; e < 32; ++e)
-      if (e >= n) r[e] = 0xff800000u;
-    if (a.doc) {
-      const int4* d = reinterpret_cast<const int4*>(a.doc + j0);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int4 v = __ldg(d + e);
-        if (v.x != a.id) r[4 * e] = 0xff800000u;
-        if (v.y != a.id) r[4 * e + 1] = 0xff800000u;
-        if (v.z != a.id) r[4 * e + 2] = 0xff800000u;
-        if (v.w != a.id) r[4 * e + 3] = 0xff800000u;
-      }
+    for (int e = 0; e < 8; ++e) {
+      const int4 v = __ldg(d + e);
+      if (v.x != id) r[4 * e] = 0xff800000u;
+      if (v.y != id) r[4 * e + 1] = 0xff800000u;
+      if (v.z != id) r[4 * e + 2] = 0xff800000u;
+      if (v.w != id) r[4 * e + 3] = 0xff800000u;
     }
   }
 }
 
-template <int DP, int NT>
-__global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 1) scored_fwd_tc_k(const __grid_constant__ FwdParams fp) {
+__device__ __forceinline__ float max_of(const uint32_t (&r)[32]) {
+  float m[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    m[k] = __uint_as_float(r[8 * k]);
+#pragma unroll
+    for (int e = 1; e < 7; e += 2)
+      m[k] = max3(m[k], __uint_as_float(r[8 * k + e]), __uint_as_float(r[8 * k + e + 1]));
+    m[k] = fmaxf(m[k], __uint_as_float(r[8 * k + 7]));
+  }
+  return fmaxf(max3(m[0], m[1], m[2]), m[3]);
+}
+
+template <int DP, int NT, int BIAS, bool CAP>
+__global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k(const __grid_constant__ FwdParams fp) {
   using F = Fwd<DP, NT>;
   const ScoredParams& p = fp.s;
   extern __shared__ __align__(1024) char smem_raw[];
@@ -117,9 +99,10 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 1) scored_fwd_tc_k(cons
   uint64_t *qfull = bars, *full = bars + 1, *empty = full + F::kStages, *sfull = empty + F::kStages,
            *pfull = sfull + NT, *ofull = pfull + NT;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + F::kBars);
-  float* bias = reinterpret_cast<float*>(bars + F::kBars + 1);
+  float* xch = reinterpret_cast<float*>(bars + F::kBars + 1);
+  float* bias = xch + F::kXch;
   const int words = (p.L + 4095) / 4096;
-  uint32_t* act = reinterpret_cast<uint32_t*>(bias + 2 * kMaxReach + 4);   // [NT][words]: blocks of the tile
+  uint32_t* act = reinterpret_cast<uint32_t*>(bias + (BIAS == kBiasTable ? kBiasFloats : 0));   // [NT][words]: blocks of the tile
   uint32_t* some = act + NT * words;                                        // [NT][words]: blocks that need the mask
   uint32_t* padded = some + NT * words;                                     // [words]: blocks that hold padding
 
@@ -135,12 +118,12 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 1) scored_fwd_tc_k(cons
     }
     for (int e = 0; e < NT; ++e) {
       mbar_init(&sfull[e], 1);
-      mbar_init(&pfull[e], 128);
+      mbar_init(&pfull[e], 256);
       mbar_init(&ofull[e], 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  constexpr int kTma = 4 * NT, kMma = 4 * NT + 1;
+  constexpr int kTma = 8 * NT, kMma = 8 * NT + 1;
   if (warp == kMma) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tslot)),
                  "r"(F::kCols)
@@ -154,11 +137,9 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 1) scored_fwd_tc_k(cons
   }
   pdl_wait();
   // score units: raw products without a cap, natural ones after it
-  const float unit = p.cap > 0.f ? 1.f : p.scale, c = unit * kLog2e;
+  const float unit = CAP ? 1.f : p.scale, c = unit * kLog2e;
   const int pf = p.prefix ? p.prefix[b] : 0;
-  if (p.table)
-    for (int e = threadIdx.x; e < 2 * p.reach + 1; e += F::kThreads)
-      bias[e] = __bfloat162float(static_cast<const bf16*>(p.table)[int64_t(h) * p.buckets + p.map[e]]) / unit;
+  if (BIAS == kBiasTable) load_bias(bias, p, h, 1.f / unit, threadIdx.x, F::kThreads);
   for (int w = warp; w < words; w += F::kThreads / 32) {
     const int k0 = (32 * w + lane) * 128;
     const int2* blk = p.blk ? p.blk + int64_t(b) * (p.Lp / kScoredBlock) : nullptr;
@@ -255,7 +236,7 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 1) scored_fwd_tc_k(cons
             const uint32_t v = smem_u32(ring + vs * F::kTileBytes);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              mma_f16_ta(tmem + 128 * NT + DP * t, tmem + 128 * t + 8 * e, smem_desc(v + 2048 * e, F::kSub, 1024), id_o,
+              mma_f16_ta(tmem + 128 * NT + DP * t, tmem + 128 * t + 64 * (e >> 2) + 8 * (e & 3), smem_desc(v + 2048 * e, F::kSub, 1024), id_o,
                          step[t] > 0 || e > 0 ? 1u : 0u);
             mma_commit(&ofull[t]);
           }
@@ -271,41 +252,42 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 1) scored_fwd_tc_k(cons
       cur = nxt;
     }
   } else {
-    const int t = warp / 4, quarter = warp % 4, i0 = q0 + 128 * t + 32 * quarter, i = i0 + lane;
+    const int t = warp / 8, half = warp / 4 % 2, quarter = warp % 4, row = 32 * quarter + lane;
+    const int i0 = q0 + 128 * t + 32 * quarter, i = i0 + lane;
     const uint32_t lanes = uint32_t(32 * quarter) << 16;
-    const uint32_t s_col = tmem + lanes + 128 * t, o_col = tmem + lanes + 128 * NT + DP * t;
+    const uint32_t s_col = tmem + lanes + 128 * t + 64 * half, o_col = tmem + lanes + 128 * NT + DP * t + DP / 2 * half;
     const uint32_t *mine = act + t * words, *masked = some + t * words;
-    Shape a;
-    a.cap = p.cap;
-    a.cap_in = p.cap > 0.f ? 2.f * kLog2e * p.scale / p.cap : 0.f;
-    a.slope = p.slopes ? -p.slopes[h] / unit : 0.f;
-    a.bias = p.table ? bias : nullptr;
-    a.reach = p.reach;
-    a.i = i;
-    a.lim = min(p.causal ? max(i + 1, pf) : p.L, p.L);
-    a.doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
-    a.id = a.doc && i < p.L ? a.doc[i] : 0;
-    if (a.id < 0) a.id = INT32_MIN;           // padding equals nothing, itself included
-    float m = -INFINITY, sum = 0.f;
+    const Shape a = shape_of(p, h, unit, bias);
+    const int lim = min(p.causal ? max(i + 1, pf) : p.L, p.L);
+    const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
+    int id = doc && i < p.L ? doc[i] : 0;
+    if (id < 0) id = INT32_MIN;               // padding equals nothing, itself included
+    float* my_max = xch + 256 * t + 128 * half + row;          // + 256 NT on odd steps
+    const float* other_max = xch + 256 * t + 128 * (1 - half) + row;
+    const int pair = 1 + 4 * t + quarter;     // the named barrier of the two warps of these rows
+    float m = -INFINITY;
+    F2 sum2 = f2(0.f, 0.f);
     int step = 0;
     Bits list(mine, mine, words);
     for (int jb = list.next(); jb >= 0; jb = list.next(), ++step) {
-      const bool mask = bit_of(masked, jb);
+      const int j0 = jb * 128 + 64 * half, flip = (step & 1) * 256 * NT;
       wait.on_warp(&sfull[t], step & 1, 27);
       tc_fence_after();
-      uint32_t r[4][32];
-#pragma unroll
-      for (int g = 0; g < 4; ++g) tmem_ld32_issue(s_col + 32 * g, r[g]);
-      float top[4];
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        tmem_ld32_wait(r[g]);
-        shape_scores(r[g], a, jb * 128 + 32 * g, i0, mask);
-        top[g] = __uint_as_float(r[g][0]);
-#pragma unroll
-        for (int e = 1; e < 32; ++e) top[g] = fmaxf(top[g], __uint_as_float(r[g][e]));
+      uint32_t r0[32], r1[32];
+      tmem_ld32_issue(s_col, r0);
+      tmem_ld32_issue(s_col + 32, r1);
+      tmem_ld32_wait(r0);
+      tmem_ld32_wait(r1);
+      shape_scores<32, BIAS, CAP, 1, false>(r0, r0, a, j0 - i, j0 - i0 - 31, j0 - i0 + 31);
+      shape_scores<32, BIAS, CAP, 1, false>(r1, r1, a, j0 + 32 - i, j0 - i0 + 1, j0 - i0 + 63);
+      if (bit_of(masked, jb)) {
+        mask_keys(r0, j0, lim, doc, id);
+        mask_keys(r1, j0 + 32, lim, doc, id);
       }
-      const float now = fmaxf(m, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
+      const float top = fmaxf(max_of(r0), max_of(r1));
+      my_max[flip] = top;
+      asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory");
+      const float now = max3(m, top, other_max[flip]);
       if (step == 0) {
         m = now;
       } else {
@@ -316,45 +298,64 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 1) scored_fwd_tc_k(cons
           tc_fence_after();
 #pragma unroll 1
           for (int g = 0; g < DP / 32; ++g) {
-            uint32_t o[32];
-            tmem_ld32(o_col + 32 * g, o);
+            uint32_t o[16];
+            tmem_ld16_issue(o_col + 16 * g, o);
+            tmem_ld16_wait(o);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
-            tmem_st32(o_col + 32 * g, o);
+            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * keep);
+            tmem_st16(o_col + 16 * g, o);
           }
-          sum *= keep;
+          sum2 = mul2(sum2, f2(keep, keep));
           if (need) m = now;
         }
       }
-      const float base = m == -INFINITY ? 0.f : m * c;
-      float part[4] = {0.f, 0.f, 0.f, 0.f};
+      const float base = m == -INFINITY ? 0.f : -m * c;
+      const F2 c2 = f2(c, c), base2 = f2(base, base);
+      F2 part = f2(0.f, 0.f);
+      // columns 0..31 -> words 0..15 of r0, then 32..63 -> words 16..31
 #pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        uint32_t w[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const float x = ex2(fmaf(__uint_as_float(r[2 * g + e / 16][2 * (e % 16)]), c, -base));
-          const float y = ex2(fmaf(__uint_as_float(r[2 * g + e / 16][2 * (e % 16) + 1]), c, -base));
-          part[e & 1] += x;
-          part[2 + (e & 1)] += y;
-          w[e] = bf16_pair(x, y);
-        }
-        tmem_st32(s_col + 32 * g, w);
+      for (int e = 0; e < 16; ++e) {
+        float x, y;
+        split(fma2(f2u(r0[2 * e], r0[2 * e + 1]), c2, base2), x, y);
+        x = ex2(x);
+        y = ex2(y);
+        sum2 = add2(sum2, f2(x, y));
+        r0[e] = bf16_pair(x, y);
       }
-      sum += (part[0] + part[1]) + (part[2] + part[3]);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        float x, y;
+        split(fma2(f2u(r1[2 * e], r1[2 * e + 1]), c2, base2), x, y);
+        x = ex2(x);
+        y = ex2(y);
+        part = add2(part, f2(x, y));
+        r0[16 + e] = bf16_pair(x, y);
+      }
+      sum2 = add2(sum2, part);
+      tmem_st32(s_col, r0);
       tmem_st_wait();
       tc_fence_before();
       mbar_arrive(&pfull[t]);
     }
+    // the row's sum over both halves (the last step's maxima have been read:
+    // this is the other buffer)
+    float sum, other;
+    split(sum2, sum, other);
+    sum += other;
+    my_max[(step & 1) * 256 * NT] = sum;
+    asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory");
+    const float theirs = other_max[(step & 1) * 256 * NT];
+    sum = half ? theirs + sum : sum + theirs;
     const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);     // a NaN row stays NaN
     if (step > 0) {
       wait.on_warp(&ofull[t], (step - 1) & 1, 29);
       tc_fence_after();
     }
-    if (i < p.L) p.lse[int64_t(bh) * p.L + i] = sum == 0.f ? -INFINITY : m * c * kLn2 + logf(sum);
-    bf16* row = static_cast<bf16*>(p.o.p) + b * p.o.sb + int64_t(i) * p.o.sl + h * p.o.sh;
+    if (half == 0 && i < p.L) p.lse[int64_t(bh) * p.L + i] = sum == 0.f ? -INFINITY : m * c * kLn2 + logf(sum);
+    bf16* out = static_cast<bf16*>(p.o.p) + b * p.o.sb + int64_t(i) * p.o.sl + h * p.o.sh;
 #pragma unroll 1
-    for (int g = 0; g < DP / 32; ++g) {
+    for (int g = 0; g < DP / 64; ++g) {
+      const int col = DP / 2 * half + 32 * g;
       uint32_t o[32];
       if (step > 0) {
         tmem_ld32(o_col + 32 * g, o);
@@ -365,12 +366,12 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 1) scored_fwd_tc_k(cons
       if (i >= p.L) continue;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (32 * g + 8 * e >= p.D) break;
+        if (col + 8 * e >= p.D) break;
         uint32_t w[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           w[k] = bf16_pair(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv);
-        reinterpret_cast<uint4*>(row + 32 * g)[e] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(out + col)[e] = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
   }
@@ -383,17 +384,22 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 1) scored_fwd_tc_k(cons
 }
 
 template <int DP, int NT>
-cudaError_t launch(const FwdParams& fp, cudaStream_t st) {
-  using F = Fwd<DP, NT>;
-  const size_t smem = F::smem(fp.s.L);
-  auto k = scored_fwd_tc_k<DP, NT>;
-  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
-  if (e != cudaSuccess) return e;
-  e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, int(cudaSharedmemCarveoutMaxShared));
-  if (e != cudaSuccess) return e;
-  const int64_t tiles = ceil_div(fp.s.L, 128 * NT);
-  return launch_k(k, dim3(unsigned(tiles * fp.s.B * fp.s.H)), dim3(F::kThreads), smem, st, fp);
-}
+struct Launch {
+  const FwdParams& fp;
+  cudaStream_t st;
+  template <int BIAS, bool CAP>
+  cudaError_t operator()() const {
+    using F = Fwd<DP, NT>;
+    const size_t smem = F::smem(fp.s.L, BIAS == kBiasTable);
+    auto k = scored_fwd_tc_k<DP, NT, BIAS, CAP>;
+    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    if (e != cudaSuccess) return e;
+    e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, int(cudaSharedmemCarveoutMaxShared));
+    if (e != cudaSuccess) return e;
+    const int64_t tiles = ceil_div(fp.s.L, 128 * NT);
+    return launch_k(k, dim3(unsigned(tiles * fp.s.B * fp.s.H)), dim3(F::kThreads), smem, st, fp);
+  }
+};
 
 }  // namespace
 
@@ -405,8 +411,9 @@ cudaError_t scored_fwd_tc(const ScoredParams& p, cudaStream_t st, bool* ok) {
   if (!*ok) return cudaSuccess;
   // Two query tiles per CTA share each K and V block and overlap softmax with
   // products; a sequence of one tile would leave the second one empty.
-  if (p.L <= 128) return p.D <= 64 ? launch<64, 1>(fp, st) : launch<128, 1>(fp, st);
-  return p.D <= 64 ? launch<64, 2>(fp, st) : launch<128, 2>(fp, st);
+  if (p.L <= 128)
+    return p.D <= 64 ? with_shape(p, Launch<64, 1>{fp, st}) : with_shape(p, Launch<128, 1>{fp, st});
+  return p.D <= 64 ? with_shape(p, Launch<64, 2>{fp, st}) : with_shape(p, Launch<128, 2>{fp, st});
 }
 
 cudaError_t scored_fwd_error(int* word) { return cudaMemcpyFromSymbol(word, g_err, sizeof(int)); }
