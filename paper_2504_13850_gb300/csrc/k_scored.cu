@@ -11,9 +11,10 @@
 // (8 widths x 4 tokens) and the vector reads meet no bank twice.  Padding and
 // rows past the end are stored as zeros: what they hold never reaches a sum.
 // The backward pass is two kernels of one body: a tile of queries walks the
-// keys (dQ and the table gradient) and a tile of keys walks the queries
-// (dK, dV); every sum has a fixed order, at the price of forming the scores
-// twice.  Bound by the fp32 FMA rate.
+// keys (dQ), then a tile of keys walks the queries (dK, dV and the table
+// gradient); every sum has a fixed order, at the price of forming the scores
+// twice.  The first one adds each row's sum of dS, which the rounding of O
+// keeps from being zero, to D for the second.  Bound by the fp32 FMA rate.
 #include "fo_common.cuh"
 #include "fo_scored.h"
 #include "../../include/fedoptima.h"
@@ -325,16 +326,17 @@ __global__ void __launch_bounds__(kThreads) scored_fwd_k(const __grid_constant__
 
 // ---------------------------------------------------------------- backward
 // KV false: rows are queries (X = Q, Y = dO) walking keys (U = K, W = V):
-//   dQ = sum dS U, and the partial table gradient of this tile.
+//   dQ = sum dS U, and D += sum dS.
 // KV true: rows are keys (X = K, Y = V) walking the queries of every head of
-// the group (U = Q, W = dO): dV = sum P^T W, dK = sum dS^T U.
+// the group (U = Q, W = dO): dV = sum P^T W, dK = sum dS^T U, and the partial
+// table gradients of this tile.
 template <typename T, int NC, bool KV>
 __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__ ScoredParams p) {
   extern __shared__ __align__(16) float sm[];
   constexpr int WD = 16 * NC;
   float *X = sm, *Y = X + WD * kT, *U = Y + WD * kT, *W = U + WD * kT, *P = W + WD * kT;
   float* bias = P + kT * kT;
-  float* dist = bias + 2 * kMaxReach + 4;          // KV false: table gradient by distance
+  float* dist = bias + 2 * kMaxReach + 4;          // KV true: table gradient by distance
   float* far = dist + 2 * kMaxReach + 4;           // [2][128] sums beyond the reach
   pdl_wait();
   pdl_trigger();
@@ -343,14 +345,13 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
   const int tile = KV ? slot : tiles - 1 - slot, r0 = tile * kT;     // the longest causal tiles first
   const int b = bh / heads, h0 = KV ? (bh % heads) * p.G : bh % heads, kh = h0 / p.G, D8 = (p.D + 7) / 8 * 8;
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-  const bool grad = !KV && p.dtable;
+  const bool grad = KV && p.dtable;
   load_tile<T>(X, KV ? p.k : p.q, p, b, KV ? kh : h0, r0);
   load_tile<T>(Y, KV ? p.v : p.dout, p, b, KV ? kh : h0, r0);
   clear_tail(U, p.D, WD);
   clear_tail(W, p.D, WD);
-  if (grad)
-    for (int e = threadIdx.x; e < 2 * p.reach + 1; e += kThreads) dist[e] = 0.f;
   float lo = 0.f, hi = 0.f;                        // sums of this thread's diagonals beyond the reach
+  float eps[4] = {0.f, 0.f, 0.f, 0.f};             // row sums of dS
   float acc0[4][NC] = {}, acc1[4][NC] = {};
   for (int g = 0; g < (KV ? p.G : 1); ++g) {
     const int h = h0 + g;
@@ -359,6 +360,10 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
     const float* delta = p.delta + (int64_t(b) * p.H + h) * p.Lp;
     __syncthreads();
     load_bias<T>(bias, p, h);
+    if (grad) {
+      for (int e = threadIdx.x; e < 2 * p.reach + 1; e += kThreads) dist[e] = 0.f;
+      lo = hi = 0.f;
+    }
     for (int c0 = 0; c0 < p.L; c0 += kT) {
       if (tile_class(p, pc.pf, b, KV ? c0 : r0, KV ? r0 : c0) == kScoredNone) continue;
       __syncthreads();
@@ -377,16 +382,17 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
           const float z = pair_score(p, pc, bias, s[r][c], i, j, &chain[r][c]);
           s[r][c] = ok ? exp2f(fmaf(z, kLog2e, -lse2[i])) : 0.f;
           dp[r][c] = ok ? s[r][c] * (dp[r][c] - delta[i]) : 0.f;
+          eps[r] += dp[r][c];
         }
       if (grad) {
         // each of 127 threads sums one diagonal of the tile in row order
         put_tile(P, dp, ty, tx);
         __syncthreads();
         if (threadIdx.x < 2 * kT - 1) {
-          const int e = int(threadIdx.x) - (kT - 1);             // column - row
+          const int e = int(threadIdx.x) - (kT - 1);             // row - column
           float t = 0.f;
-          for (int r = max(0, -e); r < min(kT, kT - e); ++r) t += P[at_p(r + e, r >> 2) + (r & 3)];
-          const int d = c0 - r0 + e;
+          for (int r = max(0, e); r < min(kT, kT + e); ++r) t += P[at_p(r - e, r >> 2) + (r & 3)];
+          const int d = r0 - c0 + e;
           if (d <= -p.reach) lo += t;
           else if (d >= p.reach) hi += t;
           else dist[d + p.reach] += t;
@@ -407,6 +413,30 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
       __syncthreads();
       accumulate<NC>(acc1, P, U, ty, tx);
     }
+    if (grad) {
+      __syncthreads();
+      if (threadIdx.x < 128) {
+        far[threadIdx.x] = lo;
+        far[128 + threadIdx.x] = hi;
+      }
+      __syncthreads();
+      if (threadIdx.x < 2) {
+        float t = 0.f;
+        for (int e = 0; e < 128; ++e) t += far[128 * threadIdx.x + e];
+        dist[threadIdx.x ? 2 * p.reach : 0] += t;
+      }
+      __syncthreads();
+      const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+      const int64_t n = int64_t(p.B) * tiles;
+      for (int k = warp; k < p.buckets; k += kThreads / 32) {
+        float t = 0.f;
+        for (int e = lane; e < 2 * p.reach + 1; e += 32)
+          if (p.map[e] == k) t += dist[e];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+        if (lane == 0) p.part[(int64_t(h) * p.buckets + k) * n + int64_t(b) * tiles + tile] = t;
+      }
+    }
   }
   const float one[4] = {1.f, 1.f, 1.f, 1.f}, sc[4] = {p.scale, p.scale, p.scale, p.scale};
   if (KV) {
@@ -414,29 +444,12 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
     store_rows<T, NC>(p.dk, p, acc1, sc, b, kh, r0, ty, tx);
   } else {
     store_rows<T, NC>(p.dq, p, acc1, sc, b, h0, r0, ty, tx);
-  }
-  if (grad) {
-    __syncthreads();
-    if (threadIdx.x < 128) {
-      far[threadIdx.x] = lo;
-      far[128 + threadIdx.x] = hi;
-    }
-    __syncthreads();
-    if (threadIdx.x < 2) {
-      float t = 0.f;
-      for (int e = 0; e < 128; ++e) t += far[128 * threadIdx.x + e];
-      dist[threadIdx.x ? 2 * p.reach : 0] += t;
-    }
-    __syncthreads();
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int64_t n = int64_t(p.B) * tiles;
-    for (int k = warp; k < p.buckets; k += kThreads / 32) {
-      float t = 0.f;
-      for (int e = lane; e < 2 * p.reach + 1; e += 32)
-        if (p.map[e] == k) t += dist[e];
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-      if (lane == 0) p.part[(int64_t(h0) * p.buckets + k) * n + int64_t(b) * tiles + tile] = t;
+    for (int r = 0; r < 4; ++r) {
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) eps[r] += __shfl_xor_sync(0xffffffffu, eps[r], o);
+      const int l = r0 + 4 * ty + r;
+      if (tx == 0 && l < p.L) p.delta[(int64_t(b) * p.H + h0) * p.Lp + l] += eps[r];
     }
   }
 }
@@ -459,9 +472,9 @@ cudaError_t backward_width(const ScoredParams& p, cudaStream_t st) {
   const int64_t tiles = ceil_div(p.L, kT);
   const size_t smem =
       (size_t(4 * 16 * NC * kT) + kT * kT + 2 * (2 * kMaxReach + 4) + 256) * sizeof(float);
-  cudaError_t e = run(scored_bwd_k<T, NC, true>, tiles * p.B * p.KV, smem, st, p);
+  cudaError_t e = run(scored_bwd_k<T, NC, false>, tiles * p.B * p.H, smem, st, p);
   if (e != cudaSuccess) return e;
-  return run(scored_bwd_k<T, NC, false>, tiles * p.B * p.H, smem, st, p);
+  return run(scored_bwd_k<T, NC, true>, tiles * p.B * p.KV, smem, st, p);
 }
 // Accumulator columns per thread: 16 NC >= head width.
 template <typename T>
@@ -687,7 +700,7 @@ int fo_attention_backward(const fo_attention_spec* spec, const fo_strided* q, co
   if (e == cudaSuccess && !tc) e = f32 ? backward_simt<float>(p, st) : backward_simt<bf16>(p, st);
   if (e == cudaSuccess && dtable) {
     const int n = p.H * p.buckets;
-    const int64_t parts = int64_t(p.B) * ceil_div(p.L, tc ? 128 : kT);     // query tiles of the kernel that ran
+    const int64_t parts = int64_t(p.B) * ceil_div(p.L, tc ? 128 : kT);     // key tiles of the kernel that ran
     e = f32 ? launch_k(scored_table_k<float>, dim3((n + 3) / 4), dim3(128), 0, st, p.part, static_cast<float*>(dtable),
                        n, parts)
             : launch_k(scored_table_k<bf16>, dim3((n + 3) / 4), dim3(128), 0, st, p.part, static_cast<bf16*>(dtable),

@@ -4,26 +4,32 @@
 // One kernel body, launched twice.  A CTA keeps a tile of 128 rows of X and Y
 // in shared memory and walks blocks of 64 rows of U and W:
 //   KV = false  rows are queries:  X = Q, Y = dO, U = K, W = V
-//               S = X U^T, dP = Y W^T,  dQ += dS U, table gradient
+//               S = X U^T, dP = Y W^T,  dQ += dS U
 //   KV = true   rows are keys:     X = K, Y = V, U = Q, W = dO, over every
 //               query head of the group
-//               S^T = X U^T, dP^T = Y W^T,  dV += P^T W, dK += dS^T U
+//               S^T = X U^T, dP^T = Y W^T,  dV += P^T W, dK += dS^T U, and the
+//               table gradient
 // so each gradient is a sum in one CTA, in a fixed order, without atomics; the
 // price is that S and dP are formed twice (7 products instead of 5).  An
 // alternative that adds dQ in global memory would save two products and lose
 // reproducibility.
-// S and dP take 64 TMEM columns each, twice: two warpgroups of 128 threads (one
-// row each) process alternate blocks, so that one's arithmetic runs while the
-// other's products do.  P and dS go back to TMEM as bf16 over the scores they
-// came from, as A operands of the accumulating products; no score touches
-// shared memory.  Row statistics come from scored_delta_k; for KV = true they
-// are per column and ride along in each stage.
-// The table gradient sums dS in fp32 by distance: each warp turns 32 x 32
-// patches through shared memory so that a lane sums a diagonal, in arrays of
-// its own by distance; patches beyond the reach are one sum per thread.  It is
-// stored in the table's type: D comes from the rounded O, so further bits would
-// carry no information.
-// Rounding: P and dS to bf16 before their products, each gradient once.
+// S and dP take 64 TMEM columns each, twice: two groups of 256 threads process
+// alternate blocks, so that one's arithmetic runs while the other's products
+// do; a row is shared by two threads, 32 columns each, in two passes of 16.  P
+// and dS go back to TMEM as bf16 over the scores they came from, as A operands
+// of the accumulating products; no score touches shared memory.  Row
+// statistics (scored_delta_k) are per column where rows are keys and ride
+// along in each stage.
+// D = dO . O carries the rounding of O, which would leave each row's dS with a
+// sum of -dD instead of 0, most of it in whichever bucket holds most keys: the
+// query pass, launched first, sums its dS rows in fp32 and adds the sum to D,
+// so that dK and the table gradient come from the exact D.
+// The table gradient sums dS in fp32 by distance: each warp turns 32 x 16
+// patches through shared memory so that a lane sums a diagonal, into arrays by
+// distance shared by the two warps of a row group, one after the other;
+// patches beyond the reach are one sum per thread.
+// Rounding: P and dS to bf16 before their products, each gradient once (the
+// table's in the table's type).
 #include "fo_scored_tc.cuh"
 
 namespace fo {
@@ -37,10 +43,10 @@ struct BwdParams {
   CUtensorMap x, y, u, w;
 };
 
-constexpr int kThreads = 320;           // two warpgroups, the TMA warp, the MMA warp
-constexpr int kTma = 8, kMma = 9;
+constexpr int kThreads = 576;           // sixteen warps of arithmetic, the TMA warp, the MMA warp
+constexpr int kTma = 16, kMma = 17;
 constexpr int kMaxStages = 4;
-constexpr int kPatch = 32 * 33;         // floats of a warp's 32 x 32 patch, rows 33 apart
+constexpr int kPatch = 32 * 17;         // floats of a warp's 32 x 16 patch, rows 17 apart
 
 template <int DP, bool KV>
 struct Bwd {
@@ -49,20 +55,20 @@ struct Bwd {
   static constexpr int kStats = KV ? 512 : 0;       // lse and D of 64 queries
   static constexpr int kStage = 2 * kU + (KV ? 1024 : 0);
   static constexpr int kBars = 1 + 2 * kMaxStages + 2 * 2 + 1;
-  static constexpr int kBias = 2 * kMaxReach + 4;
-  // X, Y, stages, barriers (and the TMEM slot), bias (one per warpgroup when
-  // heads change along the walk), bitmaps, table-gradient arrays
+  // X, Y, stages, barriers (and the TMEM slot), bitmaps, row sums of dS, bias,
+  // table-gradient arrays
   static size_t smem(int L, int stages, bool table, bool grad, int reach) {
     const int words = (L + 2047) / 2048;
     size_t n = 1024 + 2 * kX + size_t(stages) * kStage + 8 * (kBars + 1) + size_t(4) * words * 3;
-    if (table) n += 4 * kBias * (KV ? 2 : 1);
-    if (grad) n += 4 * (8 * kPatch + 8 * dist_floats(reach)) + 2 * kMaxReach + 4;
+    if (!KV) n += 4 * 4 * 128;
+    if (table) n += 4 * kBiasFloats;
+    if (grad) n += 4 * (16 * kPatch + 8 * dist_floats(reach)) + 2 * kMaxReach + 4;
     return n;
   }
   __host__ __device__ static int dist_floats(int reach) { return (2 * reach + 1 + 3) / 4 * 4; }
 };
 
-template <int DP, bool KV>
+template <int DP, bool KV, int BIAS, bool CAP>
 __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_constant__ BwdParams bp) {
   using F = Bwd<DP, KV>;
   const ScoredParams& p = bp.s;
@@ -76,10 +82,11 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + F::kBars);
   uint32_t* act = reinterpret_cast<uint32_t*>(bars + F::kBars + 1);
   uint32_t *some = act + words, *padded = some + words;
-  float* bias = reinterpret_cast<float*>(padded + words);
-  const bool grad = !KV && p.dtable;
-  float* patch = bias + (p.table ? F::kBias * (KV ? 2 : 1) : 0);
-  float* dist = patch + 8 * kPatch;
+  float* rowsum = reinterpret_cast<float*>(padded + words);            // KV false: [4][128]
+  float* bias = rowsum + (KV ? 0 : 512);
+  const bool grad = KV && BIAS == kBiasTable && p.dtable;
+  float* patch = bias + (BIAS == kBiasTable ? kBiasFloats : 0);
+  float* dist = patch + 16 * kPatch;
   const int nd = F::dist_floats(p.reach);
   uint8_t* map = reinterpret_cast<uint8_t*>(dist + 8 * nd);
 
@@ -96,7 +103,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     }
     for (int e = 0; e < 2; ++e) {
       mbar_init(&sfull[e], 1);
-      mbar_init(&pfull[e], 128);
+      mbar_init(&pfull[e], 256);
     }
     mbar_init(afull, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -113,12 +120,10 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&bp.w)) : "memory");
   }
   pdl_wait();
-  const float unit = p.cap > 0.f ? 1.f : p.scale, c = unit * kLog2e;
+  const float unit = CAP ? 1.f : p.scale, c = unit * kLog2e;
   const int pf = p.prefix ? p.prefix[b] : 0;
   const int2* blk = p.blk ? p.blk + int64_t(b) * (p.Lp / kScoredBlock) : nullptr;
-  if (p.table && !KV)
-    for (int e = threadIdx.x; e < 2 * p.reach + 1; e += kThreads)
-      bias[e] = __bfloat162float(static_cast<const bf16*>(p.table)[int64_t(h0) * p.buckets + p.map[e]]) / unit;
+  if (BIAS == kBiasTable && !KV) load_bias(bias, p, h0, 1.f / unit, threadIdx.x, kThreads);
   if (grad) {
     for (int e = threadIdx.x; e < 8 * nd; e += kThreads) dist[e] = 0.f;
     for (int e = threadIdx.x; e < 2 * p.reach + 1; e += kThreads) map[e] = p.map[e];
@@ -135,9 +140,10 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         if (blk) cd = blk[c0 / 64];
         cls = KV ? scored_class(p, pf, c0, c0 + 64, r0, r0 + 128, blk != nullptr, cd, rd)
                  : scored_class(p, pf, r0, r0 + 128, c0, c0 + 64, blk != nullptr, rd, cd);
-        // keys past the end are zeros in shared memory, not absent; queries
-        // past the end have lse = +infinity
-        if (!KV && cls == kScoredAll && c0 + 64 > p.L) cls = kScoredSome;
+        // keys past the end are zeros in shared memory, not absent: as columns
+        // they would enter dQ, as rows the table gradient; queries past the
+        // end have lse = +infinity
+        if (cls == kScoredAll && (KV ? grad && r0 + 128 > p.L : c0 + 64 > p.L)) cls = kScoredSome;
         pad = cd.x < 0 && cls != kScoredNone;
       }
       const uint32_t on = __ballot_sync(0xffffffffu, cls != kScoredNone);
@@ -238,198 +244,215 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         if (KV) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            mma_f16_ta(tmem + 256, a + 8 * e, smem_desc(w + 2048 * e, 8192, 1024), id_a, n > 0 || e > 0 ? 1u : 0u);
+            mma_f16_ta(tmem + 256, a + 32 * (e >> 1) + 8 * (e & 1), smem_desc(w + 2048 * e, 8192, 1024), id_a, n > 0 || e > 0 ? 1u : 0u);
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          mma_f16_ta(tmem + 256 + (KV ? DP : 0), a + 64 + 8 * e, smem_desc(u + 2048 * e, 8192, 1024), id_a,
-                     n > 0 || e > 0 ? 1u : 0u);
+          mma_f16_ta(tmem + 256 + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1),
+                     smem_desc(u + 2048 * e, 8192, 1024), id_a, n > 0 || e > 0 ? 1u : 0u);
         mma_commit(&empty[n % stages]);
         if (n + 1 == total) mma_commit(afull);
       }
       if (n + 2 < total) scores(n + 2);
     }
   } else {
-    const int wg = warp / 4, quarter = warp % 4, i0 = r0 + 32 * quarter, i = i0 + lane;
+    const int side = warp / 8, half = warp / 4 % 2, quarter = warp % 4, i0 = r0 + 32 * quarter, i = i0 + lane;
     const uint32_t lanes = uint32_t(32 * quarter) << 16;
-    const uint32_t s_col = tmem + lanes + 128 * wg, d_col = s_col + 64;
+    const uint32_t s_col = tmem + lanes + 128 * side + 32 * half, d_col = s_col + 64;
     const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
     int id = doc && i < p.L ? doc[i] : 0;
     if (id < 0) id = INT32_MIN;            // padding equals nothing, itself included
-    const float cap = p.cap, cap_in = cap > 0.f ? 2.f * kLog2e * p.scale / cap : 0.f;
-    const int reach = p.reach;
-    float row_lse = 0.f, row_d = 0.f;
-    if (!KV) {
-      const int64_t at = (int64_t(b) * p.H + h0) * p.Lp + i;
-      row_lse = p.lse2[at];
-      row_d = p.delta[at];
-    }
+    // position mask: rows that are queries allow columns below `edge`, rows
+    // that are keys allow columns from `edge` on (none past the end)
+    const int edge = KV ? (i >= p.L ? INT32_MAX : p.causal && i >= pf ? i : 0) : min(p.causal ? max(i + 1, pf) : p.L, p.L);
+    const int64_t stat = (int64_t(b) * p.H + h0) * p.Lp + i;
+    const float row_lse = KV ? 0.f : -p.lse2[stat], row_d = KV ? 0.f : -p.delta[stat];
+    const F2 c2 = f2(c, c);
+    F2 eps = f2(0.f, 0.f);                 // KV false: sum of this thread's dS
     float lo_sum = 0.f, hi_sum = 0.f;      // table gradient beyond the reach
     float* my_patch = patch + warp * kPatch;
-    float* my_dist = dist + warp * nd;
-    float* my_bias = bias + (KV ? wg * F::kBias : 0);
+    float* my_dist = dist + (4 * side + quarter) * nd;
+    const int pair = 1 + 4 * side + quarter;
     int n = 0;
     for (int g = 0; g < groups; ++g) {
-      const float slope = p.slopes ? -p.slopes[h0 + g] / unit : 0.f;
-      if (KV && p.table) {
-        asm volatile("bar.sync %0, 128;" ::"r"(1 + wg) : "memory");
-        for (int e = threadIdx.x % 128; e < 2 * reach + 1; e += 128)
-          my_bias[e] = __bfloat162float(static_cast<const bf16*>(p.table)[int64_t(h0 + g) * p.buckets + p.map[e]]) / unit;
-        asm volatile("bar.sync %0, 128;" ::"r"(1 + wg) : "memory");
+      const Shape a = shape_of(p, h0 + g, unit, bias);
+      if (KV && BIAS == kBiasTable) {
+        asm volatile("bar.sync 9, 512;" ::: "memory");
+        load_bias(bias, p, h0 + g, 1.f / unit, threadIdx.x, 512);
+        asm volatile("bar.sync 9, 512;" ::: "memory");
       }
       Bits list(act, act, words);
       for (int cb = list.next(); cb >= 0; cb = list.next(), ++n) {
-        if ((n & 1) != wg) continue;
+        if ((n & 1) != side) continue;
         const bool mask = bit_of(some, cb);
         const int slot = n % stages;
         if (KV) wait.on_warp(&full[slot], (n / stages) & 1, 35);   // its statistics
-        wait.on_warp(&sfull[wg], (n >> 1) & 1, 36);
+        wait.on_warp(&sfull[side], (n >> 1) & 1, 36);
         tc_fence_after();
-        const uint32_t stats = smem_u32(ring + slot * F::kStage + 2 * F::kU);
+        const uint32_t stats = smem_u32(ring + slot * F::kStage + 2 * F::kU) + 128 * half;
 #pragma unroll 1
-        for (int half = 0; half < 2; ++half) {
-          const int c0 = cb * 64 + 32 * half;
-          uint32_t s[32], t[32];
-          tmem_ld32_issue(s_col + 32 * half, s);
-          tmem_ld32_issue(d_col + 32 * half, t);
-          tmem_ld32_wait(s);
-          tmem_ld32_wait(t);
-          // scores: cap (its derivative goes to `chain` below), then bias.
-          // For rows i and columns c0 + e the distance j - i is
-          // c0 + e - i (rows are queries) or i - c0 - e (rows are keys).
-          uint32_t pr[32];
-          if (cap > 0.f) {
+        for (int pass = 0; pass < 2; ++pass) {
+          const int c0 = cb * 64 + 32 * half + 16 * pass;
+          uint32_t s[16], t[16], q[16];
+          tmem_ld16_issue(s_col + 16 * pass, s);
+          tmem_ld16_issue(d_col + 16 * pass, t);
+          tmem_ld16_wait(s);
+          tmem_ld16_wait(t);
+          // distance j - i: c0 + e - i (rows are queries) or i - c0 - e
+          const int lo = KV ? i0 - c0 - 15 : c0 - i0 - 31;
+          shape_scores<16, BIAS, CAP, KV ? -1 : 1, true>(s, q, a, KV ? i - c0 : c0 - i, lo, lo + 46);
+          // P = 2^(c x - lse) -> s, dS = P (dP - D) -> t
 #pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float q = rcp(1.f + ex2(__uint_as_float(s[e]) * cap_in));
-              s[e] = __float_as_uint(q);
-              pr[e] = __float_as_uint(fmaf(-2.f * cap, q, cap));
-            }
-          } else {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) pr[e] = s[e];
-          }
-          if (p.table) {
-            const int lo = KV ? i0 - c0 - 31 : c0 - i0 - 31, hi = lo + 62, d = KV ? i - c0 : c0 - i;
-            if (lo >= reach || hi <= -reach) {
-              const float z = my_bias[lo >= reach ? 2 * reach : 0];
-#pragma unroll
-              for (int e = 0; e < 32; ++e) pr[e] = __float_as_uint(__uint_as_float(pr[e]) + z);
-            } else if (lo >= -reach && hi <= reach) {
-              const float* z = my_bias + d + reach;
-#pragma unroll
-              for (int e = 0; e < 32; ++e) pr[e] = __float_as_uint(__uint_as_float(pr[e]) + z[KV ? -e : e]);
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                pr[e] = __float_as_uint(__uint_as_float(pr[e]) +
-                                        my_bias[min(max(KV ? d - e : d + e, -reach), reach) + reach]);
-            }
-          } else if (slope != 0.f) {
-            const float d = float(c0 - i);
-#pragma unroll
-            for (int e = 0; e < 32; ++e)
-              pr[e] = __float_as_uint(fmaf(slope, fabsf(d + float(e)), __uint_as_float(pr[e])));
-          }
-          // P = 2^(c x - lse), dS = P (dP - D)
-#pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            float4 l4 = make_float4(row_lse, row_lse, row_lse, row_lse), d4 = make_float4(row_d, row_d, row_d, row_d);
+          for (int e = 0; e < 16; e += 4) {
+            F2 l0 = f2(row_lse, row_lse), l1 = l0, d0 = f2(row_d, row_d), d1 = d0;
             if (KV) {
-              l4 = ld_shared4(stats + 128 * half + 16 * q);
-              d4 = ld_shared4(stats + 256 + 128 * half + 16 * q);
+              const float4 l4 = ld_shared4(stats + 64 * pass + 4 * e), d4 = ld_shared4(stats + 256 + 64 * pass + 4 * e);
+              l0 = f2(-l4.x, -l4.y), l1 = f2(-l4.z, -l4.w), d0 = f2(-d4.x, -d4.y), d1 = f2(-d4.z, -d4.w);
             }
-            const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dv[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float x = ex2(fmaf(__uint_as_float(pr[4 * q + e]), c, -lv[e]));
-              pr[4 * q + e] = __float_as_uint(x);
-              t[4 * q + e] = __float_as_uint(x * (__uint_as_float(t[4 * q + e]) - dv[e]));
+            for (int k = 0; k < 2; ++k) {
+              const int at = e + 2 * k;
+              float x, y;
+              split(fma2(f2u(s[at], s[at + 1]), c2, k ? l1 : l0), x, y);
+              const F2 w = f2(ex2(x), ex2(y));
+              split(w, x, y);
+              s[at] = __float_as_uint(x), s[at + 1] = __float_as_uint(y);
+              split(mul2(w, add2(f2u(t[at], t[at + 1]), k ? d1 : d0)), x, y);
+              t[at] = __float_as_uint(x), t[at + 1] = __float_as_uint(y);
             }
           }
           if (mask) {
-            // KV: the row is the key; its queries are allowed from `first` on
-            const int n_ok = (KV ? 0 : min(p.causal ? max(i + 1, pf) : p.L, p.L)) - c0;
-            const int first = (KV && p.causal && i >= pf ? i : 0) - c0;
+            const int first = edge - c0;
 #pragma unroll
-            for (int e = 0; e < 32; ++e)
-              if (KV ? e < first : e >= n_ok) pr[e] = t[e] = 0u;
+            for (int e = 0; e < 16; ++e)
+              if (KV ? e < first : e >= first) s[e] = t[e] = 0u;
             if (doc) {
               const int4* dd = reinterpret_cast<const int4*>(doc + c0);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) {
+              for (int e = 0; e < 4; ++e) {
                 const int4 v = __ldg(dd + e);
-                if (v.x != id) pr[4 * e] = t[4 * e] = 0u;
-                if (v.y != id) pr[4 * e + 1] = t[4 * e + 1] = 0u;
-                if (v.z != id) pr[4 * e + 2] = t[4 * e + 2] = 0u;
-                if (v.w != id) pr[4 * e + 3] = t[4 * e + 3] = 0u;
+                if (v.x != id) s[4 * e] = t[4 * e] = 0u;
+                if (v.y != id) s[4 * e + 1] = t[4 * e + 1] = 0u;
+                if (v.z != id) s[4 * e + 2] = t[4 * e + 2] = 0u;
+                if (v.w != id) s[4 * e + 3] = t[4 * e + 3] = 0u;
               }
             }
           }
-          if (grad) {
-            const int base = c0 - i0;                    // distance of the patch's corner
-            if (base - 31 >= reach || base + 31 <= -reach) {
-              float z = 0.f;
+          if (!KV) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) z += __uint_as_float(t[e]);
-              if (base > 0) hi_sum += z;
-              else lo_sum += z;
+            for (int e = 0; e < 16; e += 2) eps = add2(eps, f2u(t[e], t[e + 1]));
+          }
+          if (KV && BIAS == kBiasTable && grad) {
+            // the patch's distances: base + row - column; whether any of the
+            // block's is within the reach is the same for the warps of a row
+            // group, which meet at barriers below
+            const int base = i0 - c0, corner = i0 - cb * 64;
+            if (corner - 63 >= a.reach || corner + 31 <= -a.reach) {
+              F2 z = f2u(t[0], t[1]);
+#pragma unroll
+              for (int e = 2; e < 16; e += 2) z = add2(z, f2u(t[e], t[e + 1]));
+              float x, y;
+              split(z, x, y);
+              if (corner > 0) hi_sum += x + y;
+              else lo_sum += x + y;
             } else {
               __syncwarp();
 #pragma unroll
-              for (int e = 0; e < 32; ++e) my_patch[lane * 33 + e] = __uint_as_float(t[e]);
+              for (int e = 0; e < 16; ++e) my_patch[lane * 17 + e] = __uint_as_float(t[e]);
               __syncwarp();
-              // lane: the diagonals of distance base + lane (columns from
-              // `lane` on) and base + lane - 32 (the wrapped rest)
+              // lane: distance base + lane (rows lane + e) and, where the rows
+              // wrap, base + lane - 32
               float up = 0.f, down = 0.f;
-#pragma unroll 8
-              for (int e = 0; e < 32; ++e) {
-                const float z = my_patch[e * 33 + ((e + lane) & 31)];
-                if (e + lane < 32) up += z;
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const float z = my_patch[((lane + e) & 31) * 17 + e];
+                if (lane + e < 32) up += z;
                 else down += z;
               }
+              // the two warps of these rows write one after the other
               const int du = base + lane, dn = du - 32;
-              if (du >= reach) hi_sum += up;
-              else if (du <= -reach) lo_sum += up;
-              else my_dist[du + reach] += up;
+              auto put = [&](int d, float z) {
+                if (d >= a.reach) hi_sum += z;
+                else if (d <= -a.reach) lo_sum += z;
+                else my_dist[d + a.reach] += z;
+              };
+              if (half) asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory");
+              put(du, up);
               __syncwarp();
-              if (dn >= reach) hi_sum += down;
-              else if (dn <= -reach) lo_sum += down;
-              else my_dist[dn + reach] += down;
+              if (lane >= 17) put(dn, down);
+              if (!half) asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory");
+              asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory");
             }
           }
-          if (cap > 0.f) {     // 1 - tanh^2 = 4 q (1 - q)
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float q = __uint_as_float(s[e]);
-              t[e] = __float_as_uint(__uint_as_float(t[e]) * (4.f * q * (1.f - q)));
-            }
-            if (mask) {        // a masked score may have been NaN
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (pr[e] == 0u) t[e] = 0u;
-            }
-          }
-          uint32_t w[16];
+          uint32_t w[8];
           if (KV) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] = bf16_pair(__uint_as_float(pr[2 * e]), __uint_as_float(pr[2 * e + 1]));
-            tmem_st16(s_col + 16 * half, w);
+            for (int e = 0; e < 8; ++e) w[e] = bf16_pair(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
+            tmem_st8(s_col + 8 * pass, w);
+          }
+          if (CAP) {           // 1 - tanh^2 = 4 q (1 - q); a masked score may have been NaN
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float z = __uint_as_float(q[e]), y = __uint_as_float(t[e]) * (4.f * z * (1.f - z));
+              t[e] = s[e] == 0u ? 0u : __float_as_uint(y);
+            }
           }
 #pragma unroll
-          for (int e = 0; e < 16; ++e) w[e] = bf16_pair(__uint_as_float(t[2 * e]), __uint_as_float(t[2 * e + 1]));
-          tmem_st16(d_col + 16 * half, w);
+          for (int e = 0; e < 8; ++e) w[e] = bf16_pair(__uint_as_float(t[2 * e]), __uint_as_float(t[2 * e + 1]));
+          tmem_st8(d_col + 8 * pass, w);
         }
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(&pfull[wg]);
+        mbar_arrive(&pfull[side]);
+      }
+      if (grad) {
+        // this head's sums by distance -> buckets -> its partial gradient
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+          lo_sum += __shfl_xor_sync(0xffffffffu, lo_sum, o);
+          hi_sum += __shfl_xor_sync(0xffffffffu, hi_sum, o);
+        }
+        for (int turn = 0; turn < 2; ++turn) {
+          __syncwarp();
+          if (turn == half && lane == 0) {
+            my_dist[0] += lo_sum;
+            my_dist[2 * a.reach] += hi_sum;
+          }
+          asm volatile("bar.sync 9, 512;" ::: "memory");
+        }
+        const int64_t parts = int64_t(p.B) * tiles;
+        for (int k = warp; k < p.buckets; k += 16) {
+          float z = 0.f;
+          for (int e = lane; e < 2 * a.reach + 1; e += 32)
+            if (map[e] == k)
+#pragma unroll
+              for (int w = 0; w < 8; ++w) z += dist[w * nd + e];
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+          if (lane == 0) p.part[(int64_t(h0 + g) * p.buckets + k) * parts + int64_t(b) * tiles + tile] = z;
+        }
+        if (g + 1 < groups) {
+          asm volatile("bar.sync 9, 512;" ::: "memory");
+          for (int e = threadIdx.x; e < 8 * nd; e += 512) dist[e] = 0.f;
+          lo_sum = hi_sum = 0.f;       // the next head's bias load synchronises
+        }
+      }
+    }
+    if (!KV) {
+      float x, y;
+      split(eps, x, y);
+      rowsum[(2 * side + half) * 128 + 32 * quarter + lane] = x + y;
+      asm volatile("bar.sync 9, 512;" ::: "memory");
+      if (warp < 4 && i < p.L) {
+        const float* z = rowsum + 32 * quarter + lane;
+        p.delta[stat] = (z[0] + z[128]) + (z[256] + z[384]) - row_d;
       }
     }
     if (n > 0) {
       wait.on_warp(afull, 0, 37);
       tc_fence_after();
     }
-    // each warpgroup stores half of the columns of each sum
+    // each of the four warps of a row group stores a quarter of the columns
 #pragma unroll 1
     for (int o = 0; o < (KV ? 2 : 1); ++o) {
       const Strided& out = !KV ? p.dq : o ? p.dk : p.dv;
@@ -437,17 +460,18 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       bf16* row = static_cast<bf16*>(out.p) + b * out.sb + int64_t(i) * out.sl + (KV ? kh : h0) * out.sh;
 #pragma unroll 1
       for (int g = 0; g < DP / 64; ++g) {
-        const int col = 32 * (wg * (DP / 64) + g);
-        uint32_t a[32];
+        const int col = DP / 4 * (2 * side + half) + 16 * g;
+        uint32_t a[16];
         if (n > 0) {
-          tmem_ld32(tmem + lanes + 256 + o * DP + col, a);
+          tmem_ld16_issue(tmem + lanes + 256 + o * DP + col, a);
+          tmem_ld16_wait(a);
         } else {
 #pragma unroll
-          for (int e = 0; e < 32; ++e) a[e] = 0u;
+          for (int e = 0; e < 16; ++e) a[e] = 0u;
         }
         if (i >= p.L) continue;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < 2; ++e) {
           if (col + 8 * e >= p.D) break;
           uint32_t w[4];
 #pragma unroll
@@ -455,30 +479,6 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
             w[k] = bf16_pair(__uint_as_float(a[8 * e + 2 * k]) * mul, __uint_as_float(a[8 * e + 2 * k + 1]) * mul);
           reinterpret_cast<uint4*>(row + col)[e] = make_uint4(w[0], w[1], w[2], w[3]);
         }
-      }
-    }
-    if (grad) {
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) {
-        lo_sum += __shfl_xor_sync(0xffffffffu, lo_sum, o);
-        hi_sum += __shfl_xor_sync(0xffffffffu, hi_sum, o);
-      }
-      __syncwarp();
-      if (lane == 0) {
-        my_dist[0] += lo_sum;
-        my_dist[2 * reach] += hi_sum;
-      }
-      asm volatile("bar.sync 3, 256;" ::: "memory");
-      const int64_t parts = int64_t(p.B) * tiles;
-      for (int k = warp; k < p.buckets; k += 8) {
-        float z = 0.f;
-        for (int e = lane; e < 2 * reach + 1; e += 32)
-          if (map[e] == k)
-#pragma unroll
-            for (int w = 0; w < 8; ++w) z += dist[w * nd + e];
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-        if (lane == 0) p.part[(int64_t(h0) * p.buckets + k) * parts + int64_t(b) * tiles + tile] = z;
       }
     }
   }
@@ -493,20 +493,25 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
 constexpr size_t kSmemLimit = 232448;
 
 template <int DP, bool KV>
-cudaError_t launch(BwdParams bp, cudaStream_t st) {
-  using F = Bwd<DP, KV>;
-  const bool grad = !KV && bp.s.dtable;
-  int stages = kMaxStages;
-  auto need = [&](int n) { return F::smem(bp.s.L, n, bp.s.table != nullptr, grad, bp.s.reach); };
-  while (stages > 2 && need(stages) > kSmemLimit) --stages;
-  bp.s.stages = stages;
-  const size_t smem = need(stages);
-  auto k = scored_bwd_tc_k<DP, KV>;
-  cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
-  if (e != cudaSuccess) return e;
-  const int64_t tiles = ceil_div(bp.s.L, 128);
-  return launch_k(k, dim3(unsigned(tiles * bp.s.B * (KV ? bp.s.KV : bp.s.H))), dim3(kThreads), smem, st, bp);
-}
+struct Launch {
+  BwdParams& bp;
+  cudaStream_t st;
+  template <int BIAS, bool CAP>
+  cudaError_t operator()() const {
+    using F = Bwd<DP, KV>;
+    const bool grad = KV && bp.s.dtable;
+    int stages = kMaxStages;
+    auto need = [&](int n) { return F::smem(bp.s.L, n, BIAS == kBiasTable, grad, bp.s.reach); };
+    while (stages > 2 && need(stages) > kSmemLimit) --stages;
+    bp.s.stages = stages;
+    const size_t smem = need(stages);
+    auto k = scored_bwd_tc_k<DP, KV, BIAS, CAP>;
+    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    if (e != cudaSuccess) return e;
+    const int64_t tiles = ceil_div(bp.s.L, 128);
+    return launch_k(k, dim3(unsigned(tiles * bp.s.B * (KV ? bp.s.KV : bp.s.H))), dim3(kThreads), smem, st, bp);
+  }
+};
 
 }  // namespace
 
@@ -518,9 +523,9 @@ cudaError_t scored_bwd_tc(const ScoredParams& p, cudaStream_t st, bool* ok) {
         scored_map(&k.x, p.k, p, p.KV, 128) && scored_map(&k.y, p.v, p, p.KV, 128) &&
         scored_map(&k.u, p.q, p, p.H, 64) && scored_map(&k.w, p.dout, p, p.H, 64);
   if (!*ok) return cudaSuccess;
-  cudaError_t e = p.D <= 64 ? launch<64, true>(k, st) : launch<128, true>(k, st);
+  cudaError_t e = p.D <= 64 ? with_shape(p, Launch<64, false>{q, st}) : with_shape(p, Launch<128, false>{q, st});
   if (e != cudaSuccess) return e;
-  return p.D <= 64 ? launch<64, false>(q, st) : launch<128, false>(q, st);
+  return p.D <= 64 ? with_shape(p, Launch<64, true>{k, st}) : with_shape(p, Launch<128, true>{k, st});
 }
 
 cudaError_t scored_bwd_error(int* word) { return cudaMemcpyFromSymbol(word, g_err, sizeof(int)); }
