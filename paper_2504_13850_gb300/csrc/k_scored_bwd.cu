@@ -198,62 +198,68 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     }
   } else if (warp == kMma) {
     constexpr uint32_t id_s = instr_desc(64, false, false), id_a = instr_desc(DP, false, true);
+    const uint32_t tm = uni(tmem), x_at = uni(smem_u32(sX)), y_at = uni(smem_u32(sY)), ring_at = uni(smem_u32(ring));
+    const uint32_t one = elect_one();
     int blocks = 0;
     for (int w = 0; w < words; ++w) blocks += __popc(act[w]);
-    const int total = blocks * groups;
+    const int total = uni(blocks * groups), nst = uni(stages);
     const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
     Bits list(act, act, words);
-    // wait for the operands of step n, then S and dP into TMEM stage n % 2
-    auto scores = [&](int n) {
-      int cb = list.next();
+    int in = 0, in_slot = 0, in_phase = 0;           // the next step whose operands are waited for
+    // wait for the operands of step `in`, then S and dP into TMEM stage in % 2
+    auto scores = [&]() {
+      int cb = uni(list.next());
       if (cb < 0) {              // the next head of the group walks the same blocks
         list = Bits(act, act, words);
-        cb = list.next();
+        cb = uni(list.next());
       }
-      const int slot = n % stages;
-      char* st = ring + slot * F::kStage;
-      wait.on_warp(&full[slot], (n / stages) & 1, 32);
-      if (bit_of(padded, cb)) {
+      char* st = ring + in_slot * F::kStage;
+      wait.on_warp(&full[in_slot], in_phase, 32);
+      if (uni(int(bit_of(padded, cb)))) {
         clear_padding(st, 64, DP / 64, doc, cb * 64, p.L);
         if (KV) clear_padding(st + F::kU, 64, DP / 64, doc, cb * 64, p.L);
       }
       tc_fence_after();
-      if (lane == 0 && !wait.dead) {
-        const uint32_t x = smem_u32(sX), y = smem_u32(sY), u = smem_u32(st), w = u + F::kU, d = tmem + 128 * (n & 1);
+      const uint32_t on = wait.dead ? 0u : one, d = tm + 128 * (in & 1);
+      const uint64_t x = smem_desc(x_at, 16, 1024), y = smem_desc(y_at, 16, 1024);
+      const uint64_t u = smem_desc(ring_at + in_slot * F::kStage, 16, 1024), w = u + (F::kU >> 4);
 #pragma unroll
-        for (int e = 0; e < DP / 16; ++e) {
-          const uint32_t rx = (e >> 2) * 16384 + 32 * (e & 3), ru = (e >> 2) * 8192 + 32 * (e & 3);
-          mma_f16(d, smem_desc(x + rx, 16, 1024), smem_desc(u + ru, 16, 1024), id_s, e > 0 ? 1u : 0u);
-        }
+      for (int e = 0; e < DP / 16; ++e)
+        mma_ss(d, x + (((e >> 2) * 16384 + 32 * (e & 3)) >> 4), u + (((e >> 2) * 8192 + 32 * (e & 3)) >> 4), id_s,
+               e > 0 ? 1u : 0u, on);
 #pragma unroll
-        for (int e = 0; e < DP / 16; ++e) {
-          const uint32_t rx = (e >> 2) * 16384 + 32 * (e & 3), ru = (e >> 2) * 8192 + 32 * (e & 3);
-          mma_f16(d + 64, smem_desc(y + rx, 16, 1024), smem_desc(w + ru, 16, 1024), id_s, e > 0 ? 1u : 0u);
-        }
-        mma_commit(&sfull[n & 1]);
+      for (int e = 0; e < DP / 16; ++e)
+        mma_ss(d + 64, y + (((e >> 2) * 16384 + 32 * (e & 3)) >> 4), w + (((e >> 2) * 8192 + 32 * (e & 3)) >> 4), id_s,
+               e > 0 ? 1u : 0u, on);
+      commit_to(&sfull[in & 1], on);
+      ++in;
+      if (++in_slot == nst) {
+        in_slot = 0;
+        in_phase ^= 1;
       }
     };
     wait.on_warp(xfull, 0, 33);
-    if (total > 0) scores(0);
-    if (total > 1) scores(1);
+    if (total > 0) scores();
+    if (total > 1) scores();
+    int slot = 0;
     for (int n = 0; n < total && !wait.dead; ++n) {
       wait.on_warp(&pfull[n & 1], (n >> 1) & 1, 34);
       tc_fence_after();
-      if (lane == 0 && !wait.dead) {
-        const uint32_t u = smem_u32(ring + (n % stages) * F::kStage), w = u + F::kU, a = tmem + 128 * (n & 1);
-        if (KV) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            mma_f16_ta(tmem + 256, a + 32 * (e >> 1) + 8 * (e & 1), smem_desc(w + 2048 * e, 8192, 1024), id_a, n > 0 || e > 0 ? 1u : 0u);
-        }
+      const uint32_t on = wait.dead ? 0u : one, a = tm + 128 * (n & 1);
+      const uint64_t u = smem_desc(ring_at + slot * F::kStage, 8192, 1024), w = u + (F::kU >> 4);
+      if (KV) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          mma_f16_ta(tmem + 256 + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1),
-                     smem_desc(u + 2048 * e, 8192, 1024), id_a, n > 0 || e > 0 ? 1u : 0u);
-        mma_commit(&empty[n % stages]);
-        if (n + 1 == total) mma_commit(afull);
+          mma_ts(tm + 256, a + 32 * (e >> 1) + 8 * (e & 1), w + 128 * e, id_a, n > 0 || e > 0 ? 1u : 0u, on);
       }
-      if (n + 2 < total) scores(n + 2);
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        mma_ts(tm + 256 + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1), u + 128 * e, id_a,
+               n > 0 || e > 0 ? 1u : 0u, on);
+      commit_to(&empty[slot], on);
+      if (n + 1 == total) commit_to(afull, on);
+      if (++slot == nst) slot = 0;
+      if (n + 2 < total) scores();
     }
   } else {
     const int side = warp / 8, half = warp / 4 % 2, quarter = warp % 4, i0 = r0 + 32 * quarter, i = i0 + lane;

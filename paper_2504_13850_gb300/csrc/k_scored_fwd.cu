@@ -199,55 +199,56 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
     }
   } else if (warp == kMma) {
     constexpr uint32_t id_s = instr_desc(128, false, false), id_o = instr_desc(DP, false, true);
-    auto issue_s = [&](int t, int slot) {
-      const uint32_t a = smem_u32(sQ + t * F::kTileBytes), k = smem_u32(ring + slot * F::kTileBytes);
+    const uint32_t tm = uni(tmem), q_at = uni(smem_u32(sQ)), ring_at = uni(smem_u32(ring));
+    const uint32_t one = elect_one();
+    auto issue_s = [&](int t, int slot, uint32_t on) {
+      const uint64_t a = smem_desc(q_at + t * F::kTileBytes, 16, 1024), k = smem_desc(ring_at + slot * F::kTileBytes, 16, 1024);
 #pragma unroll
       for (int e = 0; e < DP / 16; ++e) {
-        const uint32_t off = (e >> 2) * F::kSub + 32 * (e & 3);
-        mma_f16(tmem + 128 * t, smem_desc(a + off, 16, 1024), smem_desc(k + off, 16, 1024), id_s, e > 0 ? 1u : 0u);
+        const uint32_t off = ((e >> 2) * F::kSub + 32 * (e & 3)) >> 4;
+        mma_ss(tm + 128 * t, a + off, k + off, id_s, e > 0 ? 1u : 0u, on);
       }
-      mma_commit(&sfull[t]);
+      commit_to(&sfull[t], on);
     };
     Bits list(act, act1, words);
-    int cur = list.next(), it = 0, step[2] = {0, 0};
+    int cur = uni(list.next()), it = 0, step[2] = {0, 0};
     wait.on_warp(qfull, 0, 22);
     if (cur >= 0) {
       wait.on_warp(&full[0], 0, 23);
       tc_fence_after();
-      if (lane == 0 && !wait.dead) {
-        for (int t = 0; t < NT; ++t)
-          if (bit_of(act + t * words, cur)) issue_s(t, 0);
-        mma_commit(&empty[0]);
-      }
+      const uint32_t on = wait.dead ? 0u : one;
+#pragma unroll
+      for (int t = 0; t < NT; ++t)
+        if (uni(int(bit_of(act + t * words, cur)))) issue_s(t, 0, on);
+      commit_to(&empty[0], on);
       ++it;
     }
     while (cur >= 0 && !wait.dead) {
-      const int nxt = list.next(), vs = it % F::kStages, ks = (it + 1) % F::kStages;
+      const int nxt = uni(list.next()), vs = it % F::kStages, ks = (it + 1) % F::kStages;
       wait.on_warp(&full[vs], (it / F::kStages) & 1, 24);
-      if (bit_of(padded, cur)) clear_padding(ring + vs * F::kTileBytes, 128, DP / 64, p.doc + int64_t(b) * p.Lp, cur * 128, p.L);
+      if (uni(int(bit_of(padded, cur))))
+        clear_padding(ring + vs * F::kTileBytes, 128, DP / 64, p.doc + int64_t(b) * p.Lp, cur * 128, p.L);
       if (nxt >= 0) wait.on_warp(&full[ks], ((it + 1) / F::kStages) & 1, 25);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const uint32_t* at = act + t * words;
-        if (bit_of(at, cur)) {
+        if (uni(int(bit_of(at, cur)))) {
           wait.on_warp(&pfull[t], step[t] & 1, 26);
           tc_fence_after();
-          if (lane == 0 && !wait.dead) {
-            const uint32_t v = smem_u32(ring + vs * F::kTileBytes);
+          const uint32_t on = wait.dead ? 0u : one;
+          const uint64_t v = smem_desc(ring_at + vs * F::kTileBytes, F::kSub, 1024);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              mma_f16_ta(tmem + 128 * NT + DP * t, tmem + 128 * t + 64 * (e >> 2) + 8 * (e & 3), smem_desc(v + 2048 * e, F::kSub, 1024), id_o,
-                         step[t] > 0 || e > 0 ? 1u : 0u);
-            mma_commit(&ofull[t]);
-          }
+          for (int e = 0; e < 8; ++e)
+            mma_ts(tm + 128 * NT + DP * t, tm + 128 * t + 64 * (e >> 2) + 8 * (e & 3), v + 128 * e, id_o,
+                   step[t] > 0 || e > 0 ? 1u : 0u, on);
+          commit_to(&ofull[t], on);
           ++step[t];
         }
-        if (nxt >= 0 && bit_of(at, nxt) && lane == 0 && !wait.dead) issue_s(t, ks);
+        if (nxt >= 0 && uni(int(bit_of(at, nxt)))) issue_s(t, ks, wait.dead ? 0u : one);
       }
-      if (lane == 0 && !wait.dead) {
-        mma_commit(&empty[vs]);
-        if (nxt >= 0) mma_commit(&empty[ks]);
-      }
+      const uint32_t on = wait.dead ? 0u : one;
+      commit_to(&empty[vs], on);
+      if (nxt >= 0) commit_to(&empty[ks], on);
       it += 2;
       cur = nxt;
     }
