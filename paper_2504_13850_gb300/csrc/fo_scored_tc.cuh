@@ -69,40 +69,25 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// The MMA warp runs converged and one elected lane issues: operands stay in
-// uniform registers.  (Issued from a branch of one lane, every MMA took ~170
-// cycles whatever its size, as each operand was moved to a uniform register in
-// divergent code.)
-__device__ __forceinline__ uint32_t elect_one() {
-  uint32_t e;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(e));
-  return e;
+// The MMA warp runs converged and issues from regions that elect.sync guards:
+// the compiler then knows that one lane issues and keeps the operands in
+// uniform registers.  (From a branch on the lane index, or under a predicate,
+// every tcgen05.mma took 90 to 170 cycles whatever its size.)
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e = 0;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n @p mov.u32 %0, 1;\n}\n" : "+r"(e));
+  return e != 0;
 }
 template <typename T>
 __device__ __forceinline__ T uni(T x) {
   return __shfl_sync(0xffffffffu, x, 0);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t on) {
+// tcgen05.mma with A in tensor memory: lane = row, each 32-bit column two
+// consecutive K elements (16 elements of K are 8 columns).
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
-      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(on)
-      : "memory");
-}
-// A in tensor memory: lane = row, each 32-bit column two consecutive K
-// elements (16 elements of K are 8 columns).
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc, uint32_t on) {
-  asm volatile(
-      "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n setp.ne.b32 q, %5, 0;\n"
-      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(on)
-      : "memory");
-}
-__device__ __forceinline__ void commit_to(uint64_t* bar, uint32_t on) {
-  asm volatile(
-      "{\n .reg .pred q;\n setp.ne.b32 q, %1, 0;\n"
-      " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(smem_u32(bar)),
-      "r"(on)
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(acc)
       : "memory");
 }
 

@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   const int nd = F::dist_floats(p.reach);
   uint8_t* map = reinterpret_cast<uint8_t*>(dist + 8 * nd);
 
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = __shfl_sync(0xffffffffu, int(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
   const int heads = KV ? p.KV : p.H, tiles = (p.L + 127) / 128, bh = blockIdx.x % (p.B * heads);
   const int slot0 = int(blockIdx.x / (p.B * heads)), tile = KV ? slot0 : tiles - 1 - slot0;   // longest causal first
   const int r0 = tile * 128, b = bh / heads, h0 = KV ? (bh % heads) * p.G : bh % heads, kh = h0 / p.G;
@@ -198,40 +198,44 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     }
   } else if (warp == kMma) {
     constexpr uint32_t id_s = instr_desc(64, false, false), id_a = instr_desc(DP, false, true);
-    const uint32_t tm = uni(tmem), x_at = uni(smem_u32(sX)), y_at = uni(smem_u32(sY)), ring_at = uni(smem_u32(ring));
-    const uint32_t one = elect_one();
+    const uint32_t x_at = smem_u32(sX), y_at = smem_u32(sY), ring_at = smem_u32(ring);
     int blocks = 0;
     for (int w = 0; w < words; ++w) blocks += __popc(act[w]);
     const int total = uni(blocks * groups), nst = uni(stages);
     const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
     Bits list(act, act, words);
     int in = 0, in_slot = 0, in_phase = 0;           // the next step whose operands are waited for
-    // wait for the operands of step `in`, then S and dP into TMEM stage in % 2
-    auto scores = [&]() {
+    // the operands of step `in` have landed, without padding
+    auto arrive = [&]() {
       int cb = uni(list.next());
       if (cb < 0) {              // the next head of the group walks the same blocks
         list = Bits(act, act, words);
         cb = uni(list.next());
       }
-      char* st = ring + in_slot * F::kStage;
       wait.on_warp(&full[in_slot], in_phase, 32);
       if (uni(int(bit_of(padded, cb)))) {
+        char* st = ring + in_slot * F::kStage;
         clear_padding(st, 64, DP / 64, doc, cb * 64, p.L);
         if (KV) clear_padding(st + F::kU, 64, DP / 64, doc, cb * 64, p.L);
       }
       tc_fence_after();
-      const uint32_t on = wait.dead ? 0u : one, d = tm + 128 * (in & 1);
+    };
+    // S and dP of step `in` into TMEM stage in % 2, by the elected lane
+    auto scores = [&]() {
+      const uint32_t d = tmem + 128 * (in & 1);
       const uint64_t x = smem_desc(x_at, 16, 1024), y = smem_desc(y_at, 16, 1024);
       const uint64_t u = smem_desc(ring_at + in_slot * F::kStage, 16, 1024), w = u + (F::kU >> 4);
 #pragma unroll
       for (int e = 0; e < DP / 16; ++e)
-        mma_ss(d, x + (((e >> 2) * 16384 + 32 * (e & 3)) >> 4), u + (((e >> 2) * 8192 + 32 * (e & 3)) >> 4), id_s,
-               e > 0 ? 1u : 0u, on);
+        mma_f16(d, x + (((e >> 2) * 16384 + 32 * (e & 3)) >> 4), u + (((e >> 2) * 8192 + 32 * (e & 3)) >> 4), id_s,
+                e > 0 ? 1u : 0u);
 #pragma unroll
       for (int e = 0; e < DP / 16; ++e)
-        mma_ss(d + 64, y + (((e >> 2) * 16384 + 32 * (e & 3)) >> 4), w + (((e >> 2) * 8192 + 32 * (e & 3)) >> 4), id_s,
-               e > 0 ? 1u : 0u, on);
-      commit_to(&sfull[in & 1], on);
+        mma_f16(d + 64, y + (((e >> 2) * 16384 + 32 * (e & 3)) >> 4), w + (((e >> 2) * 8192 + 32 * (e & 3)) >> 4), id_s,
+                e > 0 ? 1u : 0u);
+      mma_commit(&sfull[in & 1]);
+    };
+    auto advance = [&]() {
       ++in;
       if (++in_slot == nst) {
         in_slot = 0;
@@ -239,27 +243,35 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       }
     };
     wait.on_warp(xfull, 0, 33);
-    if (total > 0) scores();
-    if (total > 1) scores();
+    for (int n = 0; n < 2 && n < total; ++n) {
+      arrive();
+      if (!wait.dead && elect_one()) scores();
+      advance();
+    }
     int slot = 0;
     for (int n = 0; n < total && !wait.dead; ++n) {
+      const bool more = n + 2 < total;
+      if (more) arrive();
       wait.on_warp(&pfull[n & 1], (n >> 1) & 1, 34);
       tc_fence_after();
-      const uint32_t on = wait.dead ? 0u : one, a = tm + 128 * (n & 1);
-      const uint64_t u = smem_desc(ring_at + slot * F::kStage, 8192, 1024), w = u + (F::kU >> 4);
-      if (KV) {
+      if (!wait.dead && elect_one()) {
+        const uint32_t a = tmem + 128 * (n & 1);
+        const uint64_t u = smem_desc(ring_at + slot * F::kStage, 8192, 1024), w = u + (F::kU >> 4);
+        if (KV) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            mma_ts(tmem + 256, a + 32 * (e >> 1) + 8 * (e & 1), w + 128 * e, id_a, n > 0 || e > 0 ? 1u : 0u);
+        }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          mma_ts(tm + 256, a + 32 * (e >> 1) + 8 * (e & 1), w + 128 * e, id_a, n > 0 || e > 0 ? 1u : 0u, on);
+          mma_ts(tmem + 256 + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1), u + 128 * e, id_a,
+                 n > 0 || e > 0 ? 1u : 0u);
+        mma_commit(&empty[slot]);
+        if (more) scores();
+        else if (n + 1 == total) mma_commit(afull);
       }
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        mma_ts(tm + 256 + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1), u + 128 * e, id_a,
-               n > 0 || e > 0 ? 1u : 0u, on);
-      commit_to(&empty[slot], on);
-      if (n + 1 == total) commit_to(afull, on);
+      if (more) advance();
       if (++slot == nst) slot = 0;
-      if (n + 2 < total) scores();
     }
   } else {
     const int side = warp / 8, half = warp / 4 % 2, quarter = warp % 4, i0 = r0 + 32 * quarter, i = i0 + lane;

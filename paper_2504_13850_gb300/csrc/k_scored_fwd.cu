@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
   uint32_t* some = act + NT * words;                                        // [NT][words]: blocks that need the mask
   uint32_t* padded = some + NT * words;                                     // [words]: blocks that hold padding
 
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int warp = __shfl_sync(0xffffffffu, int(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
   const int tiles = (p.L + 128 * NT - 1) / (128 * NT), bh = blockIdx.x % (p.B * p.H);
   const int q0 = (tiles - 1 - int(blockIdx.x / (p.B * p.H))) * 128 * NT;   // the longest causal rows first
   const int b = bh / p.H, h = bh % p.H, kh = h / p.G;
@@ -199,16 +199,15 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
     }
   } else if (warp == kMma) {
     constexpr uint32_t id_s = instr_desc(128, false, false), id_o = instr_desc(DP, false, true);
-    const uint32_t tm = uni(tmem), q_at = uni(smem_u32(sQ)), ring_at = uni(smem_u32(ring));
-    const uint32_t one = elect_one();
-    auto issue_s = [&](int t, int slot, uint32_t on) {
+    const uint32_t q_at = smem_u32(sQ), ring_at = smem_u32(ring);
+    auto issue_s = [&](int t, int slot) {       // by the elected lane
       const uint64_t a = smem_desc(q_at + t * F::kTileBytes, 16, 1024), k = smem_desc(ring_at + slot * F::kTileBytes, 16, 1024);
 #pragma unroll
       for (int e = 0; e < DP / 16; ++e) {
         const uint32_t off = ((e >> 2) * F::kSub + 32 * (e & 3)) >> 4;
-        mma_ss(tm + 128 * t, a + off, k + off, id_s, e > 0 ? 1u : 0u, on);
+        mma_f16(tmem + 128 * t, a + off, k + off, id_s, e > 0 ? 1u : 0u);
       }
-      commit_to(&sfull[t], on);
+      mma_commit(&sfull[t]);
     };
     Bits list(act, act1, words);
     int cur = uni(list.next()), it = 0, step[2] = {0, 0};
@@ -216,11 +215,12 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
     if (cur >= 0) {
       wait.on_warp(&full[0], 0, 23);
       tc_fence_after();
-      const uint32_t on = wait.dead ? 0u : one;
-#pragma unroll
-      for (int t = 0; t < NT; ++t)
-        if (uni(int(bit_of(act + t * words, cur)))) issue_s(t, 0, on);
-      commit_to(&empty[0], on);
+      const bool on0 = uni(int(bit_of(act, cur))), on1 = uni(int(bit_of(act1, cur)));
+      if (!wait.dead && elect_one()) {
+        if (on0) issue_s(0, 0);
+        if (NT == 2 && on1) issue_s(1, 0);
+        mma_commit(&empty[0]);
+      }
       ++it;
     }
     while (cur >= 0 && !wait.dead) {
@@ -232,23 +232,28 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const uint32_t* at = act + t * words;
-        if (uni(int(bit_of(at, cur)))) {
+        const bool now = uni(int(bit_of(at, cur))), then = nxt >= 0 && uni(int(bit_of(at, nxt)));
+        if (now) {
           wait.on_warp(&pfull[t], step[t] & 1, 26);
           tc_fence_after();
-          const uint32_t on = wait.dead ? 0u : one;
-          const uint64_t v = smem_desc(ring_at + vs * F::kTileBytes, F::kSub, 1024);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            mma_ts(tm + 128 * NT + DP * t, tm + 128 * t + 64 * (e >> 2) + 8 * (e & 3), v + 128 * e, id_o,
-                   step[t] > 0 || e > 0 ? 1u : 0u, on);
-          commit_to(&ofull[t], on);
-          ++step[t];
         }
-        if (nxt >= 0 && uni(int(bit_of(at, nxt)))) issue_s(t, ks, wait.dead ? 0u : one);
+        if (!wait.dead && elect_one()) {
+          if (now) {
+            const uint64_t v = smem_desc(ring_at + vs * F::kTileBytes, F::kSub, 1024);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              mma_ts(tmem + 128 * NT + DP * t, tmem + 128 * t + 64 * (e >> 2) + 8 * (e & 3), v + 128 * e, id_o,
+                     step[t] > 0 || e > 0 ? 1u : 0u);
+            mma_commit(&ofull[t]);
+          }
+          if (then) issue_s(t, ks);
+          if (t == NT - 1) {
+            mma_commit(&empty[vs]);
+            if (nxt >= 0) mma_commit(&empty[ks]);
+          }
+        }
+        if (now) ++step[t];
       }
-      const uint32_t on = wait.dead ? 0u : one;
-      commit_to(&empty[vs], on);
-      if (nxt >= 0) commit_to(&empty[ks], on);
       it += 2;
       cur = nxt;
     }
