@@ -69,18 +69,15 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// The MMA warp runs converged and issues from regions that elect.sync guards:
-// the compiler then knows that one lane issues and keeps the operands in
-// uniform registers.  (From a branch on the lane index, or under a predicate,
-// every tcgen05.mma took 90 to 170 cycles whatever its size.)
+// The MMA warp's whole loop runs in a region that elect.sync guards: the
+// compiler then knows that one lane issues and keeps the operands in uniform
+// registers.  (From a branch on the lane index, or under a predicate, every
+// tcgen05.mma took 90 to 170 cycles whatever its size; a converged warp that
+// votes on its waits spent more time between the products than in them.)
 __device__ __forceinline__ bool elect_one() {
   uint32_t e = 0;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n @p mov.u32 %0, 1;\n}\n" : "+r"(e));
   return e != 0;
-}
-template <typename T>
-__device__ __forceinline__ T uni(T x) {
-  return __shfl_sync(0xffffffffu, x, 0);
 }
 // tcgen05.mma with A in tensor memory: lane = row, each 32-bit column two
 // consecutive K elements (16 elements of K are 8 columns).
@@ -194,19 +191,29 @@ __device__ __forceinline__ Shape shape_of(const ScoredParams& p, int h, float un
   return a;
 }
 
-// Clears the rows of padded tokens of a swizzled tile of `rows` rows and
-// `subs` 64-column sub-tiles (a whole warp; a row's swizzled units stay within
-// its 128 bytes), so that what they hold meets no product as an operand summed
-// over tokens.
-__device__ __forceinline__ void clear_padding(char* tile, int rows, int subs, const int32_t* doc, int l0, int L) {
-  const int lane = threadIdx.x % 32;
-  for (int r = lane; r < rows; r += 32)
-    if (l0 + r < L && doc[l0 + r] < 0)
-      for (int s = 0; s < subs; ++s)
+// Clears the rows of padded tokens of a swizzled tile of ROWS rows and SUBS
+// 64-column sub-tiles (one thread; a row's swizzled units stay within its 128
+// bytes), so that what they hold meets no product as an operand summed over
+// tokens.  doc: the ids of the tile's tokens, 16-byte aligned, -1 past the end
+// (rows past the end are zero-filled copies, clearing them changes nothing).
+template <int ROWS, int SUBS>
+__device__ __forceinline__ void clear_padding(uint32_t tile, const int32_t* doc) {
+#pragma unroll 1
+  for (int r = 0; r < ROWS; r += 16) {
+    int4 id[4];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) st_shared4(smem_u32(tile) + s * rows * 128 + r * 128 + u * 16, 0u, 0u, 0u, 0u);
+    for (int e = 0; e < 4; ++e) id[e] = __ldg(reinterpret_cast<const int4*>(doc + r) + e);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int4 v = id[e / 4];
+      const int one = e % 4 == 0 ? v.x : e % 4 == 1 ? v.y : e % 4 == 2 ? v.z : v.w;
+      if (one < 0)
+#pragma unroll 1
+        for (int u = 0; u < 8 * SUBS; ++u)
+          st_shared4(tile + (u >> 3) * ROWS * 128 + (r + e) * 128 + (u & 7) * 16, 0u, 0u, 0u, 0u);
+    }
+  }
   fence_proxy_async_smem();
-  __syncwarp();
 }
 
 // Calls f.template operator()<BIAS, CAP>() for the bias and cap of p.

@@ -197,64 +197,60 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       }
     }
   } else if (warp == kMma) {
-    constexpr uint32_t id_s = instr_desc(64, false, false), id_a = instr_desc(DP, false, true);
-    const uint32_t x_at = smem_u32(sX), y_at = smem_u32(sY), ring_at = smem_u32(ring);
-    int blocks = 0;
-    for (int w = 0; w < words; ++w) blocks += __popc(act[w]);
-    const int total = uni(blocks * groups), nst = uni(stages);
-    const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
-    Bits list(act, act, words);
-    int in = 0, in_slot = 0, in_phase = 0;           // the next step whose operands are waited for
-    // the operands of step `in` have landed, without padding
-    auto arrive = [&]() {
-      int cb = uni(list.next());
-      if (cb < 0) {              // the next head of the group walks the same blocks
-        list = Bits(act, act, words);
-        cb = uni(list.next());
-      }
-      wait.on_warp(&full[in_slot], in_phase, 32);
-      if (uni(int(bit_of(padded, cb)))) {
-        char* st = ring + in_slot * F::kStage;
-        clear_padding(st, 64, DP / 64, doc, cb * 64, p.L);
-        if (KV) clear_padding(st + F::kU, 64, DP / 64, doc, cb * 64, p.L);
-      }
-      tc_fence_after();
-    };
-    // S and dP of step `in` into TMEM stage in % 2, by the elected lane
-    auto scores = [&]() {
-      const uint32_t d = tmem + 128 * (in & 1);
-      const uint64_t x = smem_desc(x_at, 16, 1024), y = smem_desc(y_at, 16, 1024);
-      const uint64_t u = smem_desc(ring_at + in_slot * F::kStage, 16, 1024), w = u + (F::kU >> 4);
+    if (elect_one()) {
+      constexpr uint32_t id_s = instr_desc(64, false, false), id_a = instr_desc(DP, false, true);
+      const uint32_t x_at = smem_u32(sX), y_at = smem_u32(sY), ring_at = smem_u32(ring);
+      const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
+      int total = 0;
+      for (int w = 0; w < words; ++w) total += __popc(act[w]);
+      total *= groups;
+      Bits list(act, act, words);
+      int in = 0, in_slot = 0, in_phase = 0;           // the next step whose scores are formed
+      // its operands have landed, without padding
+      auto arrive = [&]() {
+        wait.on(&full[in_slot], in_phase, 32);
+        if (doc) {
+          int cb = list.next();
+          if (cb < 0) {              // the next head of the group walks the same blocks
+            list = Bits(act, act, words);
+            cb = list.next();
+          }
+          if (bit_of(padded, cb)) {
+            clear_padding<64, DP / 64>(ring_at + in_slot * F::kStage, doc + cb * 64);
+            if (KV) clear_padding<64, DP / 64>(ring_at + in_slot * F::kStage + F::kU, doc + cb * 64);
+          }
+        }
+        tc_fence_after();
+      };
+      // S and dP into TMEM stage in % 2
+      auto scores = [&]() {
+        const uint32_t d = tmem + 128 * (in & 1);
+        const uint64_t x = smem_desc(x_at, 16, 1024), y = smem_desc(y_at, 16, 1024);
+        const uint64_t u = smem_desc(ring_at + in_slot * F::kStage, 16, 1024), w = u + (F::kU >> 4);
 #pragma unroll
-      for (int e = 0; e < DP / 16; ++e)
-        mma_f16(d, x + (((e >> 2) * 16384 + 32 * (e & 3)) >> 4), u + (((e >> 2) * 8192 + 32 * (e & 3)) >> 4), id_s,
-                e > 0 ? 1u : 0u);
+        for (int e = 0; e < DP / 16; ++e)
+          mma_f16(d, x + (((e >> 2) * 16384 + 32 * (e & 3)) >> 4), u + (((e >> 2) * 8192 + 32 * (e & 3)) >> 4), id_s,
+                  e > 0 ? 1u : 0u);
 #pragma unroll
-      for (int e = 0; e < DP / 16; ++e)
-        mma_f16(d + 64, y + (((e >> 2) * 16384 + 32 * (e & 3)) >> 4), w + (((e >> 2) * 8192 + 32 * (e & 3)) >> 4), id_s,
-                e > 0 ? 1u : 0u);
-      mma_commit(&sfull[in & 1]);
-    };
-    auto advance = [&]() {
-      ++in;
-      if (++in_slot == nst) {
-        in_slot = 0;
-        in_phase ^= 1;
+        for (int e = 0; e < DP / 16; ++e)
+          mma_f16(d + 64, y + (((e >> 2) * 16384 + 32 * (e & 3)) >> 4), w + (((e >> 2) * 8192 + 32 * (e & 3)) >> 4),
+                  id_s, e > 0 ? 1u : 0u);
+        mma_commit(&sfull[in & 1]);
+        ++in;
+        if (++in_slot == stages) in_slot = 0, in_phase ^= 1;
+      };
+      wait.on(xfull, 0, 33);
+      for (int n = 0; n < 2 && n < total; ++n) {
+        arrive();
+        if (!wait.dead) scores();
       }
-    };
-    wait.on_warp(xfull, 0, 33);
-    for (int n = 0; n < 2 && n < total; ++n) {
-      arrive();
-      if (!wait.dead && elect_one()) scores();
-      advance();
-    }
-    int slot = 0;
-    for (int n = 0; n < total && !wait.dead; ++n) {
-      const bool more = n + 2 < total;
-      if (more) arrive();
-      wait.on_warp(&pfull[n & 1], (n >> 1) & 1, 34);
-      tc_fence_after();
-      if (!wait.dead && elect_one()) {
+      int slot = 0;
+      for (int n = 0; n < total && !wait.dead; ++n) {
+        const bool more = n + 2 < total;
+        if (more) arrive();
+        wait.on(&pfull[n & 1], (n >> 1) & 1, 34);
+        tc_fence_after();
+        if (wait.dead) break;
         const uint32_t a = tmem + 128 * (n & 1);
         const uint64_t u = smem_desc(ring_at + slot * F::kStage, 8192, 1024), w = u + (F::kU >> 4);
         if (KV) {
@@ -269,10 +265,10 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         mma_commit(&empty[slot]);
         if (more) scores();
         else if (n + 1 == total) mma_commit(afull);
+        if (++slot == stages) slot = 0;
       }
-      if (more) advance();
-      if (++slot == nst) slot = 0;
     }
+    __syncwarp();
   } else {
     const int side = warp / 8, half = warp / 4 % 2, quarter = warp % 4, i0 = r0 + 32 * quarter, i = i0 + lane;
     const uint32_t lanes = uint32_t(32 * quarter) << 16;

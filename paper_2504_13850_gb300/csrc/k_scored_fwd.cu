@@ -198,65 +198,66 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
       }
     }
   } else if (warp == kMma) {
-    constexpr uint32_t id_s = instr_desc(128, false, false), id_o = instr_desc(DP, false, true);
-    const uint32_t q_at = smem_u32(sQ), ring_at = smem_u32(ring);
-    auto issue_s = [&](int t, int slot) {       // by the elected lane
-      const uint64_t a = smem_desc(q_at + t * F::kTileBytes, 16, 1024), k = smem_desc(ring_at + slot * F::kTileBytes, 16, 1024);
+    if (elect_one()) {
+      constexpr uint32_t id_s = instr_desc(128, false, false), id_o = instr_desc(DP, false, true);
+      const uint32_t q_at = smem_u32(sQ), ring_at = smem_u32(ring);
+      const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
+      auto issue_s = [&](int t, int slot) {
+        const uint64_t a = smem_desc(q_at + t * F::kTileBytes, 16, 1024),
+                       k = smem_desc(ring_at + slot * F::kTileBytes, 16, 1024);
 #pragma unroll
-      for (int e = 0; e < DP / 16; ++e) {
-        const uint32_t off = ((e >> 2) * F::kSub + 32 * (e & 3)) >> 4;
-        mma_f16(tmem + 128 * t, a + off, k + off, id_s, e > 0 ? 1u : 0u);
-      }
-      mma_commit(&sfull[t]);
-    };
-    Bits list(act, act1, words);
-    int cur = uni(list.next()), it = 0, step[2] = {0, 0};
-    wait.on_warp(qfull, 0, 22);
-    if (cur >= 0) {
-      wait.on_warp(&full[0], 0, 23);
-      tc_fence_after();
-      const bool on0 = uni(int(bit_of(act, cur))), on1 = uni(int(bit_of(act1, cur)));
-      if (!wait.dead && elect_one()) {
-        if (on0) issue_s(0, 0);
-        if (NT == 2 && on1) issue_s(1, 0);
-        mma_commit(&empty[0]);
-      }
-      ++it;
-    }
-    while (cur >= 0 && !wait.dead) {
-      const int nxt = uni(list.next()), vs = it % F::kStages, ks = (it + 1) % F::kStages;
-      wait.on_warp(&full[vs], (it / F::kStages) & 1, 24);
-      if (uni(int(bit_of(padded, cur))))
-        clear_padding(ring + vs * F::kTileBytes, 128, DP / 64, p.doc + int64_t(b) * p.Lp, cur * 128, p.L);
-      if (nxt >= 0) wait.on_warp(&full[ks], ((it + 1) / F::kStages) & 1, 25);
-#pragma unroll
-      for (int t = 0; t < NT; ++t) {
-        const uint32_t* at = act + t * words;
-        const bool now = uni(int(bit_of(at, cur))), then = nxt >= 0 && uni(int(bit_of(at, nxt)));
-        if (now) {
-          wait.on_warp(&pfull[t], step[t] & 1, 26);
-          tc_fence_after();
+        for (int e = 0; e < DP / 16; ++e) {
+          const uint32_t off = ((e >> 2) * F::kSub + 32 * (e & 3)) >> 4;
+          mma_f16(tmem + 128 * t, a + off, k + off, id_s, e > 0 ? 1u : 0u);
         }
-        if (!wait.dead && elect_one()) {
-          if (now) {
+        mma_commit(&sfull[t]);
+      };
+      Bits list(act, act1, words);
+      int cur = list.next(), slot = 0, phase = 0, step[2] = {0, 0};
+      wait.on(qfull, 0, 22);
+      if (cur >= 0) {
+        wait.on(&full[0], 0, 23);
+        tc_fence_after();
+        if (!wait.dead) {
+          if (bit_of(act, cur)) issue_s(0, 0);
+          if (NT == 2 && bit_of(act1, cur)) issue_s(1, 0);
+          mma_commit(&empty[0]);
+        }
+        slot = 1;
+      }
+      while (cur >= 0 && !wait.dead) {
+        const int nxt = list.next(), vs = slot, vphase = phase;
+        if (++slot == F::kStages) slot = 0, phase ^= 1;
+        const int ks = slot, kphase = phase;
+        if (++slot == F::kStages) slot = 0, phase ^= 1;
+        wait.on(&full[vs], vphase, 24);
+        if (doc && bit_of(padded, cur)) clear_padding<128, DP / 64>(ring_at + vs * F::kTileBytes, doc + cur * 128);
+        if (nxt >= 0) wait.on(&full[ks], kphase, 25);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          const uint32_t* at = act + t * words;
+          if (bit_of(at, cur)) {
+            wait.on(&pfull[t], step[t] & 1, 26);
+            tc_fence_after();
+            if (wait.dead) break;
             const uint64_t v = smem_desc(ring_at + vs * F::kTileBytes, F::kSub, 1024);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               mma_ts(tmem + 128 * NT + DP * t, tmem + 128 * t + 64 * (e >> 2) + 8 * (e & 3), v + 128 * e, id_o,
                      step[t] > 0 || e > 0 ? 1u : 0u);
             mma_commit(&ofull[t]);
+            ++step[t];
           }
-          if (then) issue_s(t, ks);
-          if (t == NT - 1) {
-            mma_commit(&empty[vs]);
-            if (nxt >= 0) mma_commit(&empty[ks]);
-          }
+          if (nxt >= 0 && bit_of(at, nxt) && !wait.dead) issue_s(t, ks);
         }
-        if (now) ++step[t];
+        if (!wait.dead) {
+          mma_commit(&empty[vs]);
+          if (nxt >= 0) mma_commit(&empty[ks]);
+        }
+        cur = nxt;
       }
-      it += 2;
-      cur = nxt;
     }
+    __syncwarp();
   } else {
     const int t = warp / 8, half = warp / 4 % 2, quarter = warp % 4, row = 32 * quarter + lane;
     const int i0 = q0 + 128 * t + 32 * quarter, i = i0 + lane;
