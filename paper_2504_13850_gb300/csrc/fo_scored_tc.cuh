@@ -88,6 +88,18 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
       : "memory");
 }
 
+// A K- or MN-major operand descriptor whose high word is a constant, so that
+// moving it by `off` bytes within shared memory is a 32-bit addition.
+template <uint32_t LBO>
+struct Operand {
+  uint32_t lo;
+  __device__ __forceinline__ explicit Operand(uint32_t addr) : lo((addr >> 4) | (LBO >> 4) << 16) {}
+  __device__ __forceinline__ uint64_t at(uint32_t off) const {
+    constexpr uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);      // stride 1024, version 1, 128-byte swizzle
+    return uint64_t(lo + (off >> 4)) | uint64_t(hi) << 32;
+  }
+};
+
 // A role's waits: after one has given up (about two seconds) the rest return
 // at once, so the kernel ends soon and its error word is set.
 struct Waits {
@@ -99,28 +111,60 @@ struct Waits {
     atomicExch(err, code);
     dead = true;
   }
-  // The same for a whole warp, which stays converged and agrees on the outcome.
+  // The same for a whole warp, converged afterwards.
   __device__ __forceinline__ void on_warp(uint64_t* bar, uint32_t parity, int code) {
-    if (!dead && !mbar_wait(bar, parity)) {
-      atomicExch(err, code);
-      dead = true;
-    }
-    dead = __any_sync(0xffffffffu, dead);
+    on(bar, parity, code);
+    __syncwarp();
   }
 };
 
-// Walks the set bits of a bitmap in shared memory in ascending order.
+// One arrival for a warp whose lanes have all written what it announces.
+__device__ __forceinline__ void arrive_warp(uint64_t* bar) {
+  __syncwarp();
+  if (threadIdx.x % 32 == 0) mbar_arrive(bar);
+}
+
+// Walks the blocks set in either of two bitmaps in shared memory, in ascending
+// order; on[k] tells whether map k has the current one.
 struct Bits {
-  const uint32_t *a, *b;    // the union of two maps (b may equal a)
+  const uint32_t *a, *b;
   int words, w;
-  uint32_t left;
+  uint32_t wa, wb, left;
+  bool on[2];
   __device__ __forceinline__ Bits(const uint32_t* a_, const uint32_t* b_, int words_)
-      : a(a_), b(b_), words(words_), w(0), left(words_ > 0 ? a_[0] | b_[0] : 0u) {}
+      : a(a_), b(b_), words(words_), w(0), wa(a_[0]), wb(b_[0]), left(wa | wb) {}
   // The next block, or -1.
   __device__ __forceinline__ int next() {
     while (!left) {
       if (++w >= words) return -1;
-      left = a[w] | b[w];
+      wa = a[w];
+      wb = b[w];
+      left = wa | wb;
+    }
+    const int bit = __ffs(int(left)) - 1;
+    left &= left - 1;
+    on[0] = (wa >> bit) & 1u;
+    on[1] = (wb >> bit) & 1u;
+    return 32 * w + bit;
+  }
+};
+// The same for one bitmap, with few registers for the warps of arithmetic.
+struct BitList {
+  uint32_t map;             // shared-memory address
+  int words, w;
+  uint32_t left;
+  __device__ __forceinline__ static uint32_t word(uint32_t map, int w) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(map + 4 * w));
+    return v;
+  }
+  __device__ __forceinline__ BitList(const uint32_t* m, int words_) : map(smem_u32(m)), words(words_), w(0) {
+    left = word(map, 0);
+  }
+  __device__ __forceinline__ int next() {
+    while (!left) {
+      if (++w >= words) return -1;
+      left = word(map, w);
     }
     const int bit = __ffs(int(left)) - 1;
     left &= left - 1;
@@ -128,6 +172,23 @@ struct Bits {
   }
 };
 __device__ __forceinline__ bool bit_of(const uint32_t* map, int i) { return (map[i >> 5] >> (i & 31)) & 1u; }
+__device__ __forceinline__ bool any_bit(const uint32_t* map, int words) {
+  uint32_t o = 0;
+  for (int w = 0; w < words; ++w) o |= map[w];
+  return o != 0;
+}
+
+// A position in a ring of N stages that moves S at a time, and the parity of
+// its barrier's phase.
+template <int N, int S = 1>
+struct Ring {
+  int at, phase;
+  __device__ __forceinline__ explicit Ring(int first = 0) : at(first), phase(0) {}
+  __device__ __forceinline__ void step() {
+    at += S;
+    if (at >= N) at -= N, phase ^= 1;
+  }
+};
 
 // Bias kinds, compile-time in the kernels.
 enum { kBiasNone = 0, kBiasSlope = 1, kBiasTable = 2 };
@@ -191,28 +252,18 @@ __device__ __forceinline__ Shape shape_of(const ScoredParams& p, int h, float un
   return a;
 }
 
-// Clears the rows of padded tokens of a swizzled tile of ROWS rows and SUBS
-// 64-column sub-tiles (one thread; a row's swizzled units stay within its 128
-// bytes), so that what they hold meets no product as an operand summed over
-// tokens.  doc: the ids of the tile's tokens, 16-byte aligned, -1 past the end
-// (rows past the end are zero-filled copies, clearing them changes nothing).
-template <int ROWS, int SUBS>
-__device__ __forceinline__ void clear_padding(uint32_t tile, const int32_t* doc) {
-#pragma unroll 1
-  for (int r = 0; r < ROWS; r += 16) {
-    int4 id[4];
+// Clears the rows of padded tokens of a swizzled tile of `rows` rows and
+// `subs` 64-column sub-tiles (a whole warp; a row's swizzled units stay within
+// its 128 bytes), so that what they hold meets no product as an operand summed
+// over tokens.  doc: the ids of the tile's tokens (-1 past the end, where the
+// copy has filled in zeros).
+__device__ __forceinline__ void clear_padding(char* tile, int rows, int subs, const int32_t* doc) {
+  const int lane = threadIdx.x % 32;
+  for (int r = lane; r < rows; r += 32)
+    if (doc[r] < 0)
+      for (int s = 0; s < subs; ++s)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) id[e] = __ldg(reinterpret_cast<const int4*>(doc + r) + e);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int4 v = id[e / 4];
-      const int one = e % 4 == 0 ? v.x : e % 4 == 1 ? v.y : e % 4 == 2 ? v.z : v.w;
-      if (one < 0)
-#pragma unroll 1
-        for (int u = 0; u < 8 * SUBS; ++u)
-          st_shared4(tile + (u >> 3) * ROWS * 128 + (r + e) * 128 + (u & 7) * 16, 0u, 0u, 0u, 0u);
-    }
-  }
+        for (int u = 0; u < 8; ++u) st_shared4(smem_u32(tile) + s * rows * 128 + r * 128 + u * 16, 0u, 0u, 0u, 0u);
   fence_proxy_async_smem();
 }
 

@@ -13,9 +13,10 @@
 // price is that S and dP are formed twice (7 products instead of 5).  An
 // alternative that adds dQ in global memory would save two products and lose
 // reproducibility.
-// S and dP take 64 TMEM columns each, twice: two groups of 256 threads process
-// alternate blocks, so that one's arithmetic runs while the other's products
-// do; a row is shared by two threads, 32 columns each, in two passes of 16.  P
+// S and dP take 64 TMEM columns each, in three buffers where the sums leave
+// room (two for keys of a head width above 64): two groups of 256 threads
+// process alternate blocks, so that one's arithmetic runs while the other's
+// products do, and a third buffer keeps the scores one block ahead; a row is shared by two threads, 32 columns each, in two passes of 16.  P
 // and dS go back to TMEM as bf16 over the scores they came from, as A operands
 // of the accumulating products; no score touches shared memory.  Row
 // statistics (scored_delta_k) are per column where rows are keys and ride
@@ -43,9 +44,9 @@ struct BwdParams {
   CUtensorMap x, y, u, w;
 };
 
-constexpr int kThreads = 576;           // sixteen warps of arithmetic, the TMA warp, the MMA warp
-constexpr int kTma = 16, kMma = 17;
-constexpr int kMaxStages = 4;
+constexpr int kThreads = 608;           // sixteen warps of arithmetic; TMA, MMA and padding warps
+constexpr int kTma = 16, kMma = 17, kClean = 18;
+constexpr int kMaxStages = 6;
 constexpr int kPatch = 32 * 17;         // floats of a warp's 32 x 16 patch, rows 17 apart
 
 template <int DP, bool KV>
@@ -54,7 +55,8 @@ struct Bwd {
   static constexpr int kU = DP / 64 * 8192;         // 64 rows
   static constexpr int kStats = KV ? 512 : 0;       // lse and D of 64 queries
   static constexpr int kStage = 2 * kU + (KV ? 1024 : 0);
-  static constexpr int kBars = 1 + 2 * kMaxStages + 2 * 2 + 1;
+  static constexpr int kBufs = KV && DP == 128 ? 2 : 3;     // TMEM buffers of S and dP; the sums follow
+  static constexpr int kBars = 1 + 3 * kMaxStages + 2 * kBufs + 1;
   // X, Y, stages, barriers (and the TMEM slot), bitmaps, row sums of dS, bias,
   // table-gradient arrays
   static size_t smem(int L, int stages, bool table, bool grad, int reach) {
@@ -77,8 +79,8 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   char *sX = sm, *sY = sm + F::kX, *ring = sm + 2 * F::kX;
   const int stages = p.stages, words = (p.L + 2047) / 2048;
   uint64_t* bars = reinterpret_cast<uint64_t*>(ring + stages * F::kStage);
-  uint64_t *xfull = bars, *full = bars + 1, *empty = full + kMaxStages, *sfull = empty + kMaxStages, *pfull = sfull + 2,
-           *afull = pfull + 2;
+  uint64_t *xfull = bars, *full = bars + 1, *empty = full + kMaxStages, *clean = empty + kMaxStages,
+           *sfull = clean + kMaxStages, *pfull = sfull + F::kBufs, *afull = pfull + F::kBufs;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + F::kBars);
   uint32_t* act = reinterpret_cast<uint32_t*>(bars + F::kBars + 1);
   uint32_t *some = act + words, *padded = some + words;
@@ -100,10 +102,11 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     for (int e = 0; e < stages; ++e) {
       mbar_init(&full[e], 1);
       mbar_init(&empty[e], 1);
+      mbar_init(&clean[e], 1);
     }
-    for (int e = 0; e < 2; ++e) {
+    for (int e = 0; e < F::kBufs; ++e) {
       mbar_init(&sfull[e], 1);
-      mbar_init(&pfull[e], 256);
+      mbar_init(&pfull[e], 8);           // one arrival per warp
     }
     mbar_init(afull, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -159,8 +162,8 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  // S and dP of stage s: columns 128 s and 128 s + 64; sums at 256 and 256 + DP
-  const uint32_t tmem = *tslot;
+  // S and dP of buffer k: columns 128 k and 128 k + 64; sums at `acc` and acc + DP
+  const uint32_t tmem = *tslot, acc = tmem + 128 * F::kBufs;
   pdl_trigger();
   Waits wait(&g_err);
 
@@ -200,79 +203,76 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     if (elect_one()) {
       constexpr uint32_t id_s = instr_desc(64, false, false), id_a = instr_desc(DP, false, true);
       const uint32_t x_at = smem_u32(sX), y_at = smem_u32(sY), ring_at = smem_u32(ring);
-      const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
+      uint64_t* landed = any_bit(padded, words) ? clean : full;      // U and W have landed, without padding
       int total = 0;
       for (int w = 0; w < words; ++w) total += __popc(act[w]);
       total *= groups;
-      Bits list(act, act, words);
       int in = 0, in_slot = 0, in_phase = 0;           // the next step whose scores are formed
-      // its operands have landed, without padding
-      auto arrive = [&]() {
-        wait.on(&full[in_slot], in_phase, 32);
-        if (doc) {
-          int cb = list.next();
-          if (cb < 0) {              // the next head of the group walks the same blocks
-            list = Bits(act, act, words);
-            cb = list.next();
-          }
-          if (bit_of(padded, cb)) {
-            clear_padding<64, DP / 64>(ring_at + in_slot * F::kStage, doc + cb * 64);
-            if (KV) clear_padding<64, DP / 64>(ring_at + in_slot * F::kStage + F::kU, doc + cb * 64);
-          }
-        }
-        tc_fence_after();
-      };
-      // S and dP into TMEM stage in % 2
+      Ring<F::kBufs> in_buf, buf;
       auto scores = [&]() {
-        const uint32_t d = tmem + 128 * (in & 1);
-        const uint64_t x = smem_desc(x_at, 16, 1024), y = smem_desc(y_at, 16, 1024);
-        const uint64_t u = smem_desc(ring_at + in_slot * F::kStage, 16, 1024), w = u + (F::kU >> 4);
+        wait.on(&landed[in_slot], in_phase, 32);
+        tc_fence_after();
+        if (wait.dead) return;
+        const uint32_t d = tmem + 128 * in_buf.at;
+        const Operand<16> x(x_at), y(y_at), u(ring_at + in_slot * F::kStage), w(ring_at + in_slot * F::kStage + F::kU);
 #pragma unroll
         for (int e = 0; e < DP / 16; ++e)
-          mma_f16(d, x + (((e >> 2) * 16384 + 32 * (e & 3)) >> 4), u + (((e >> 2) * 8192 + 32 * (e & 3)) >> 4), id_s,
+          mma_f16(d, x.at((e >> 2) * 16384 + 32 * (e & 3)), u.at((e >> 2) * 8192 + 32 * (e & 3)), id_s, e > 0 ? 1u : 0u);
+#pragma unroll
+        for (int e = 0; e < DP / 16; ++e)
+          mma_f16(d + 64, y.at((e >> 2) * 16384 + 32 * (e & 3)), w.at((e >> 2) * 8192 + 32 * (e & 3)), id_s,
                   e > 0 ? 1u : 0u);
-#pragma unroll
-        for (int e = 0; e < DP / 16; ++e)
-          mma_f16(d + 64, y + (((e >> 2) * 16384 + 32 * (e & 3)) >> 4), w + (((e >> 2) * 8192 + 32 * (e & 3)) >> 4),
-                  id_s, e > 0 ? 1u : 0u);
-        mma_commit(&sfull[in & 1]);
+        mma_commit(&sfull[in_buf.at]);
+        in_buf.step();
         ++in;
         if (++in_slot == stages) in_slot = 0, in_phase ^= 1;
       };
       wait.on(xfull, 0, 33);
-      for (int n = 0; n < 2 && n < total; ++n) {
-        arrive();
-        if (!wait.dead) scores();
-      }
+      while (in < F::kBufs && in < total && !wait.dead) scores();
       int slot = 0;
       for (int n = 0; n < total && !wait.dead; ++n) {
-        const bool more = n + 2 < total;
-        if (more) arrive();
-        wait.on(&pfull[n & 1], (n >> 1) & 1, 34);
+        wait.on(&pfull[buf.at], buf.phase, 34);
         tc_fence_after();
         if (wait.dead) break;
-        const uint32_t a = tmem + 128 * (n & 1);
-        const uint64_t u = smem_desc(ring_at + slot * F::kStage, 8192, 1024), w = u + (F::kU >> 4);
+        const uint32_t a = tmem + 128 * buf.at;
+        const Operand<8192> u(ring_at + slot * F::kStage), w(ring_at + slot * F::kStage + F::kU);
         if (KV) {
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            mma_ts(tmem + 256, a + 32 * (e >> 1) + 8 * (e & 1), w + 128 * e, id_a, n > 0 || e > 0 ? 1u : 0u);
+            mma_ts(acc, a + 32 * (e >> 1) + 8 * (e & 1), w.at(2048 * e), id_a, e > 0 ? 1u : uint32_t(n));
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          mma_ts(tmem + 256 + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1), u + 128 * e, id_a,
-                 n > 0 || e > 0 ? 1u : 0u);
+          mma_ts(acc + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1), u.at(2048 * e), id_a,
+                 e > 0 ? 1u : uint32_t(n));
         mma_commit(&empty[slot]);
-        if (more) scores();
+        if (in < total) scores();
         else if (n + 1 == total) mma_commit(afull);
         if (++slot == stages) slot = 0;
+        buf.step();
       }
     }
     __syncwarp();
+  } else if (warp == kClean) {
+    if (any_bit(padded, words)) {
+      const int32_t* doc = p.doc + int64_t(b) * p.Lp;
+      int slot = 0, phase = 0;
+      for (int g = 0; g < groups; ++g) {
+        Bits list(act, act, words);
+        for (int cb = list.next(); cb >= 0 && !wait.dead; cb = list.next()) {
+          wait.on_warp(&full[slot], phase, 38);
+          if (bit_of(padded, cb)) {
+            clear_padding(ring + slot * F::kStage, 64, DP / 64, doc + cb * 64);
+            if (KV) clear_padding(ring + slot * F::kStage + F::kU, 64, DP / 64, doc + cb * 64);
+          }
+          arrive_warp(&clean[slot]);
+          if (++slot == stages) slot = 0, phase ^= 1;
+        }
+      }
+    }
   } else {
     const int side = warp / 8, half = warp / 4 % 2, quarter = warp % 4, i0 = r0 + 32 * quarter, i = i0 + lane;
     const uint32_t lanes = uint32_t(32 * quarter) << 16;
-    const uint32_t s_col = tmem + lanes + 128 * side + 32 * half, d_col = s_col + 64;
     const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
     int id = doc && i < p.L ? doc[i] : 0;
     if (id < 0) id = INT32_MIN;            // padding equals nothing, itself included
@@ -287,7 +287,8 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     float* my_patch = patch + warp * kPatch;
     float* my_dist = dist + (4 * side + quarter) * nd;
     const int pair = 1 + 4 * side + quarter;
-    int n = 0;
+    int n = 0, slot = 0, phase = 0;          // step, its stage in shared memory
+    Ring<F::kBufs, 2> buf(side);             // this side's buffer
     for (int g = 0; g < groups; ++g) {
       const Shape a = shape_of(p, h0 + g, unit, bias);
       if (KV && BIAS == kBiasTable) {
@@ -295,15 +296,17 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         load_bias(bias, p, h0 + g, 1.f / unit, threadIdx.x, 512);
         asm volatile("bar.sync 9, 512;" ::: "memory");
       }
-      Bits list(act, act, words);
-      for (int cb = list.next(); cb >= 0; cb = list.next(), ++n) {
-        if ((n & 1) != side) continue;
+      BitList list(act, words);
+      for (int cb = list.next(); cb >= 0; cb = list.next()) {
+        const int my_slot = slot, my_phase = phase;
+        if (++slot == stages) slot = 0, phase ^= 1;
+        if ((n++ & 1) != side) continue;
         const bool mask = bit_of(some, cb);
-        const int slot = n % stages;
-        if (KV) wait.on_warp(&full[slot], (n / stages) & 1, 35);   // its statistics
-        wait.on_warp(&sfull[side], (n >> 1) & 1, 36);
+        const uint32_t s_col = tmem + lanes + 128 * buf.at + 32 * half, d_col = s_col + 64;
+        if (KV) wait.on_warp(&full[my_slot], my_phase, 35);        // its statistics
+        wait.on_warp(&sfull[buf.at], buf.phase, 36);
         tc_fence_after();
-        const uint32_t stats = smem_u32(ring + slot * F::kStage + 2 * F::kU) + 128 * half;
+        const uint32_t stats = smem_u32(ring + my_slot * F::kStage + 2 * F::kU) + 128 * half;
 #pragma unroll 1
         for (int pass = 0; pass < 2; ++pass) {
           const int c0 = cb * 64 + 32 * half + 16 * pass;
@@ -417,7 +420,8 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         }
         tmem_st_wait();
         tc_fence_before();
-        mbar_arrive(&pfull[side]);
+        arrive_warp(&pfull[buf.at]);
+        buf.step();
       }
       if (grad) {
         // this head's sums by distance -> buckets -> its partial gradient
@@ -477,7 +481,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         const int col = DP / 4 * (2 * side + half) + 16 * g;
         uint32_t a[16];
         if (n > 0) {
-          tmem_ld16_issue(tmem + lanes + 256 + o * DP + col, a);
+          tmem_ld16_issue(acc + lanes + o * DP + col, a);
           tmem_ld16_wait(a);
         } else {
 #pragma unroll
@@ -516,7 +520,7 @@ struct Launch {
     const bool grad = KV && bp.s.dtable;
     int stages = kMaxStages;
     auto need = [&](int n) { return F::smem(bp.s.L, n, BIAS == kBiasTable, grad, bp.s.reach); };
-    while (stages > 2 && need(stages) > kSmemLimit) --stages;
+    while (stages > F::kBufs && need(stages) > kSmemLimit) --stages;   // kBufs steps are in flight: fewer would not do
     bp.s.stages = stages;
     const size_t smem = need(stages);
     auto k = scored_bwd_tc_k<DP, KV, BIAS, CAP>;

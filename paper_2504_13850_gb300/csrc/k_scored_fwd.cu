@@ -3,7 +3,8 @@
 //
 // A CTA owns NT tiles of 128 queries of one (sequence, head) and walks the
 // allowed blocks of 128 keys once, with the running maximum and sum of an
-// online softmax.  Warp roles: 8 NT softmax warps, one TMA warp, one MMA warp.
+// online softmax.  Warp roles: 8 NT softmax warps, one TMA warp, one MMA warp,
+// and one that clears padded tokens out of V where there are any.
 // Per tile and block:
 //   S = Q K^T into 128 TMEM columns -> cap, bias and mask in registers ->
 //   P~ = 2^(c x - M) as bf16 back into the columns it came from, the A
@@ -42,9 +43,9 @@ struct Fwd {
   static constexpr int kSub = 16384;                       // 128 rows x 64 bf16
   static constexpr int kTileBytes = DP / 64 * kSub;
   static constexpr int kStages = NT == 2 ? (DP == 64 ? 6 : 4) : (DP == 64 ? 4 : 2);
-  static constexpr int kThreads = 256 * NT + 64;
+  static constexpr int kThreads = 256 * NT + (NT == 2 ? 96 : 64);
   static constexpr int kCols = NT == 2 ? 512 : 256;         // TMEM columns
-  static constexpr int kBars = 1 + 2 * kStages + 3 * NT;
+  static constexpr int kBars = 1 + 3 * kStages + 3 * NT;
   static constexpr int kOps = (NT + kStages) * kTileBytes;
   static constexpr int kXch = 2 * NT * 256;                 // floats: [step parity][tile][half][row]
   // operands, barriers (and the TMEM slot), exchanged maxima, bias, bitmaps
@@ -96,8 +97,8 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
   char* sQ = sm;
   char* ring = sm + NT * F::kTileBytes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(sm + F::kOps);
-  uint64_t *qfull = bars, *full = bars + 1, *empty = full + F::kStages, *sfull = empty + F::kStages,
-           *pfull = sfull + NT, *ofull = pfull + NT;
+  uint64_t *qfull = bars, *full = bars + 1, *empty = full + F::kStages, *clean = empty + F::kStages,
+           *sfull = clean + F::kStages, *pfull = sfull + NT, *ofull = pfull + NT;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + F::kBars);
   float* xch = reinterpret_cast<float*>(bars + F::kBars + 1);
   float* bias = xch + F::kXch;
@@ -115,15 +116,17 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
     for (int e = 0; e < F::kStages; ++e) {
       mbar_init(&full[e], 1);
       mbar_init(&empty[e], 1);
+      mbar_init(&clean[e], 1);
     }
     for (int e = 0; e < NT; ++e) {
       mbar_init(&sfull[e], 1);
-      mbar_init(&pfull[e], 256);
+      mbar_init(&pfull[e], 8);         // one arrival per warp
       mbar_init(&ofull[e], 1);
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  constexpr int kTma = 8 * NT, kMma = 8 * NT + 1;
+  // one tile walks at most one block, which the TMA warp can clear itself
+  constexpr int kTma = 8 * NT, kMma = 8 * NT + 1, kClean = NT == 2 ? kMma + 1 : kTma;
   if (warp == kMma) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tslot)),
                  "r"(F::kCols)
@@ -182,15 +185,16 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
         for (int s = 0; s < DP / 64; ++s)
           tma_4d(sQ + t * F::kTileBytes + s * F::kSub, &fp.q, qfull, 64 * s, q0 + 128 * t, h, b);
       Bits list(act, act1, words);
+      Ring<F::kStages> at;
       int it = 0;
       for (int jb = list.next(); jb >= 0 && !wait.dead; jb = list.next())
         for (int kv = 0; kv < 2; ++kv, ++it) {
-          const int slot = it % F::kStages;
-          if (it >= F::kStages) wait.on(&empty[slot], (it / F::kStages - 1) & 1, 21);
+          if (it >= F::kStages) wait.on(&empty[at.at], at.phase ^ 1, 21);
           if (wait.dead) break;
-          mbar_expect_tx(&full[slot], F::kTileBytes);
+          mbar_expect_tx(&full[at.at], F::kTileBytes);
           for (int s = 0; s < DP / 64; ++s)
-            tma_4d(ring + slot * F::kTileBytes + s * F::kSub, kv ? &fp.v : &fp.k, &full[slot], 64 * s, jb * 128, kh, b);
+            tma_4d(ring + at.at * F::kTileBytes + s * F::kSub, kv ? &fp.v : &fp.k, &full[at.at], 64 * s, jb * 128, kh, b);
+          at.step();
         }
       if (wait.dead) {   // let the copies in flight land before the block ends
         mbar_wait(qfull, 0);
@@ -200,70 +204,71 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
   } else if (warp == kMma) {
     if (elect_one()) {
       constexpr uint32_t id_s = instr_desc(128, false, false), id_o = instr_desc(DP, false, true);
-      const uint32_t q_at = smem_u32(sQ), ring_at = smem_u32(ring);
-      const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
+      const uint32_t ring_at = smem_u32(ring);
       auto issue_s = [&](int t, int slot) {
-        const uint64_t a = smem_desc(q_at + t * F::kTileBytes, 16, 1024),
-                       k = smem_desc(ring_at + slot * F::kTileBytes, 16, 1024);
+        const Operand<16> q(smem_u32(sQ) + t * F::kTileBytes), k(ring_at + slot * F::kTileBytes);
 #pragma unroll
         for (int e = 0; e < DP / 16; ++e) {
-          const uint32_t off = ((e >> 2) * F::kSub + 32 * (e & 3)) >> 4;
-          mma_f16(tmem + 128 * t, a + off, k + off, id_s, e > 0 ? 1u : 0u);
+          const uint32_t off = (e >> 2) * F::kSub + 32 * (e & 3);
+          mma_f16(tmem + 128 * t, q.at(off), k.at(off), id_s, e > 0 ? 1u : 0u);
         }
         mma_commit(&sfull[t]);
       };
       Bits list(act, act1, words);
-      int cur = list.next(), slot = 0, phase = 0, step[2] = {0, 0};
+      uint64_t* landed = any_bit(padded, words) ? clean : full;      // V has landed, without padding
+      int cur = list.next();
+      bool on[2] = {list.on[0], list.on[1]};
+      uint32_t step[2] = {0, 0};
+      Ring<F::kStages, 2> k_at(0), v_at(1);
       wait.on(qfull, 0, 22);
       if (cur >= 0) {
         wait.on(&full[0], 0, 23);
         tc_fence_after();
         if (!wait.dead) {
-          if (bit_of(act, cur)) issue_s(0, 0);
-          if (NT == 2 && bit_of(act1, cur)) issue_s(1, 0);
+          if (on[0]) issue_s(0, 0);
+          if (NT == 2 && on[1]) issue_s(1, 0);
           mma_commit(&empty[0]);
         }
-        slot = 1;
+        k_at.step();
       }
       while (cur >= 0 && !wait.dead) {
-        const int nxt = list.next(), vs = slot, vphase = phase;
-        if (++slot == F::kStages) slot = 0, phase ^= 1;
-        const int ks = slot, kphase = phase;
-        if (++slot == F::kStages) slot = 0, phase ^= 1;
-        wait.on(&full[vs], vphase, 24);
-        if (doc && bit_of(padded, cur)) clear_padding<128, DP / 64>(ring_at + vs * F::kTileBytes, doc + cur * 128);
-        if (nxt >= 0) wait.on(&full[ks], kphase, 25);
+        const int nxt = list.next();
+        wait.on(&landed[v_at.at], v_at.phase, 24);
+        if (nxt >= 0) wait.on(&full[k_at.at], k_at.phase, 25);
+        const Operand<F::kSub> v(ring_at + v_at.at * F::kTileBytes);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-          const uint32_t* at = act + t * words;
-          if (bit_of(at, cur)) {
+          if (on[t]) {
             wait.on(&pfull[t], step[t] & 1, 26);
             tc_fence_after();
             if (wait.dead) break;
-            const uint64_t v = smem_desc(ring_at + vs * F::kTileBytes, F::kSub, 1024);
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-              mma_ts(tmem + 128 * NT + DP * t, tmem + 128 * t + 64 * (e >> 2) + 8 * (e & 3), v + 128 * e, id_o,
-                     step[t] > 0 || e > 0 ? 1u : 0u);
+              mma_ts(tmem + 128 * NT + DP * t, tmem + 128 * t + 64 * (e >> 2) + 8 * (e & 3), v.at(2048 * e), id_o,
+                     e > 0 ? 1u : step[t]);
             mma_commit(&ofull[t]);
             ++step[t];
           }
-          if (nxt >= 0 && bit_of(at, nxt) && !wait.dead) issue_s(t, ks);
+          if (nxt >= 0 && list.on[t] && !wait.dead) issue_s(t, k_at.at);
         }
         if (!wait.dead) {
-          mma_commit(&empty[vs]);
-          if (nxt >= 0) mma_commit(&empty[ks]);
+          mma_commit(&empty[v_at.at]);
+          if (nxt >= 0) mma_commit(&empty[k_at.at]);
         }
+        v_at.step();
+        k_at.step();
+        on[0] = list.on[0];
+        on[1] = list.on[1];
         cur = nxt;
       }
     }
     __syncwarp();
-  } else {
+  } else if (warp < kTma) {
     const int t = warp / 8, half = warp / 4 % 2, quarter = warp % 4, row = 32 * quarter + lane;
     const int i0 = q0 + 128 * t + 32 * quarter, i = i0 + lane;
     const uint32_t lanes = uint32_t(32 * quarter) << 16;
     const uint32_t s_col = tmem + lanes + 128 * t + 64 * half, o_col = tmem + lanes + 128 * NT + DP * t + DP / 2 * half;
-    const uint32_t *mine = act + t * words, *masked = some + t * words;
+    const uint32_t masked = smem_u32(some + t * words);
     const Shape a = shape_of(p, h, unit, bias);
     const int lim = min(p.causal ? max(i + 1, pf) : p.L, p.L);
     const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
@@ -275,7 +280,7 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
     float m = -INFINITY;
     F2 sum2 = f2(0.f, 0.f);
     int step = 0;
-    Bits list(mine, mine, words);
+    BitList list(act + t * words, words);
     for (int jb = list.next(); jb >= 0; jb = list.next(), ++step) {
       const int j0 = jb * 128 + 64 * half, flip = (step & 1) * 256 * NT;
       wait.on_warp(&sfull[t], step & 1, 27);
@@ -287,7 +292,7 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
       tmem_ld32_wait(r1);
       shape_scores<32, BIAS, CAP, 1, false>(r0, r0, a, j0 - i, j0 - i0 - 31, j0 - i0 + 31);
       shape_scores<32, BIAS, CAP, 1, false>(r1, r1, a, j0 + 32 - i, j0 - i0 + 1, j0 - i0 + 63);
-      if (bit_of(masked, jb)) {
+      if ((BitList::word(masked, jb >> 5) >> (jb & 31)) & 1u) {
         mask_keys(r0, j0, lim, doc, id);
         mask_keys(r1, j0 + 32, lim, doc, id);
       }
@@ -342,7 +347,7 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
       tmem_st32(s_col, r0);
       tmem_st_wait();
       tc_fence_before();
-      mbar_arrive(&pfull[t]);
+      arrive_warp(&pfull[t]);
     }
     // the row's sum over both halves (the last step's maxima have been read:
     // this is the other buffer)
@@ -380,6 +385,18 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
           w[k] = bf16_pair(__uint_as_float(o[8 * e + 2 * k]) * inv, __uint_as_float(o[8 * e + 2 * k + 1]) * inv);
         reinterpret_cast<uint4*>(out + col)[e] = make_uint4(w[0], w[1], w[2], w[3]);
       }
+    }
+  }
+  if (warp == kClean && any_bit(padded, words)) {
+    __syncwarp();
+    Bits list(act, act1, words);
+    Ring<F::kStages, 2> v_at(1);
+    for (int jb = list.next(); jb >= 0 && !wait.dead; jb = list.next()) {
+      wait.on_warp(&full[v_at.at], v_at.phase, 25);
+      if (bit_of(padded, jb))
+        clear_padding(ring + v_at.at * F::kTileBytes, 128, DP / 64, p.doc + int64_t(b) * p.Lp + jb * 128);
+      arrive_warp(&clean[v_at.at]);
+      v_at.step();
     }
   }
   tc_fence_before();
