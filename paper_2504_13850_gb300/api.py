@@ -113,10 +113,8 @@ _SIGS = [
     ("fo_select_split", C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p,
                                   C.POINTER(C.c_int), C.POINTER(C.c_double)]),
     ("fo_attention_workspace", C.c_int64, [C.POINTER(fo_attention_spec), C.c_int]),
-    ("fo_attention_forward", C.c_int, [C.POINTER(fo_attention_spec)] + [C.POINTER(fo_strided)] * 4
-     + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
-    ("fo_attention_backward", C.c_int, [C.POINTER(fo_attention_spec)] + [C.POINTER(fo_strided)] * 4 + [C.c_void_p]
-     + [C.POINTER(fo_strided)] * 4 + [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p]),
+    ("fo_attention_forward", C.c_int, [C.POINTER(fo_attention_spec)] + [C.c_void_p] * 6 + [C.c_int64, C.c_void_p]),
+    ("fo_attention_backward", C.c_int, [C.POINTER(fo_attention_spec)] + [C.c_void_p] * 11 + [C.c_int64, C.c_void_p]),
     ("fo_attention_error", C.c_int, [C.c_void_p]),
     ("fo_dropout_add", C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int,
                                  C.c_int64, C.c_int64, C.c_double, C.c_uint64, C.c_uint64, C.c_void_p]),
@@ -446,31 +444,43 @@ def relative_buckets(buckets, reach, bidirectional=True):
     return (b + np.where(d > 0, half, 0) if bidirectional else b).astype(np.uint8)
 
 
-def _rows4(t, like, name, heads=None):
-    """fo_strided of a 4-D device tensor [batch, len, heads, head_dim]."""
-    if t.dim() != 4 or not t.is_cuda or t.dtype != like.dtype or t.device != like.device:
-        raise ValueError(f"{name}: a 4-D device tensor of q's type and device is wanted")
-    if t.shape[:2] != like.shape[:2] or t.shape[3] != like.shape[3] or (heads is not None and t.shape[2] != heads):
-        raise ValueError(f"{name}: shape {tuple(t.shape)} does not fit q's {tuple(like.shape)}")
-    st = t.stride()
-    if st[3] != 1 and t.shape[3] > 1:
-        raise ValueError(f"{name}: its innermost stride must be 1")
-    return fo_strided(t.data_ptr(), st[0], st[1], st[2])
+_fo_strided_bytes = C.sizeof(fo_strided)
+
+
+def _strided(q, keys, *tensors):
+    """An array of fo_strided for tensors like q, or like `keys` = (batch, len,
+    kv_heads, head_dim) where a (tensor, True, name) triple says so."""
+    wide, dtype, device, flat = q.shape, q.dtype, q.get_device(), []
+    for t, key_heads, name in tensors:
+        want = keys if key_heads else wide
+        if t.shape != want or t.dtype != dtype or t.get_device() != device:
+            raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}; wanted {tuple(want)} {dtype} on {q.device}")
+        st = t.stride()
+        if st[3] != 1 and want[3] > 1:
+            raise ValueError(f"{name}: its innermost stride must be 1")
+        flat.append(t.data_ptr())
+        flat += st[:3]
+    return (C.c_int64 * len(flat))(*flat)
 
 
 def _small(t, shape, dtype, like, name):
-    if tuple(t.shape) != shape or t.dtype != dtype or t.device != like.device or not t.is_contiguous():
+    if t.shape != shape or t.dtype != dtype or t.get_device() != like.get_device() or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {shape} on q's device is wanted")
     return t.data_ptr()
 
 
-def _attention_spec(q, k, causal, softcap, scale, slopes, table, buckets, documents, prefix):
-    import torch
-    if q.dim() != 4 or k.dim() != 4 or q.dtype not in (torch.bfloat16, torch.float32) or not q.is_cuda:
-        raise ValueError("q, k, v: 4-D bf16 or fp32 device tensors [batch, len, heads, head_dim]")
+def _attention_spec(torch, q, k, causal, softcap, scale, slopes, table, buckets, documents, prefix):
+    if q.dim() != 4 or k.dim() != 4 or not q.is_cuda:
+        raise ValueError("q, k, v: 4-D device tensors [batch, len, heads, head_dim]")
+    if q.dtype == torch.bfloat16:
+        dtype = DTYPE_BF16
+    elif q.dtype == torch.float32:
+        dtype = DTYPE_F32
+    else:
+        raise ValueError("q, k, v: bf16 or fp32")
     B, L, H, D = q.shape
-    s = fo_attention_spec(B, L, H, k.shape[2], D, DTYPE_BF16 if q.dtype == torch.bfloat16 else DTYPE_F32,
-                          1 if causal else 0, 0, 0, D ** -0.5 if scale is None and D else (scale or 0.0), softcap)
+    s = fo_attention_spec(B, L, H, k.shape[2], D, dtype, 1 if causal else 0, 0, 0,
+                          (D ** -0.5 if D else 0.0) if scale is None else scale, softcap)
     if slopes is not None:
         s.slopes = _small(slopes, (H,), torch.float32, q, "slopes")
     if table is not None:
@@ -486,14 +496,12 @@ def _attention_spec(q, k, causal, softcap, scale, slopes, table, buckets, docume
     return s
 
 
-def _stream_of(q, stream):
-    """(stream to pass on, context in which torch allocates for it)."""
-    import contextlib
-
-    import torch
+def _on_stream(torch, q, stream, make):
+    """(make(), stream to pass on): what a call allocates belongs to its stream."""
     if stream is None:
-        return torch.cuda.current_stream(q.device).cuda_stream, contextlib.nullcontext()
-    return stream, torch.cuda.stream(torch.cuda.ExternalStream(stream, device=q.device))
+        return make(), torch.cuda.current_stream(q.get_device()).cuda_stream
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=q.device)):
+        return make(), stream
 
 
 def attention_forward(q, k, v, causal=False, softcap=0.0, scale=None, slopes=None, table=None, buckets=None,
@@ -503,16 +511,23 @@ def attention_forward(q, k, v, causal=False, softcap=0.0, scale=None, slopes=Non
     `buckets` is the table's host map (relative_buckets).  Runs on `stream`
     (a cudaStream_t), by default torch's current stream."""
     import torch
-    s = _attention_spec(q, k, causal, softcap, scale, slopes, table, buckets, documents, prefix)
-    st, ctx = _stream_of(q, stream)
-    with ctx:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
-        lse = torch.empty(q.shape[0], q.shape[2], q.shape[1], dtype=torch.float32, device=q.device)
-        need = lib().fo_attention_workspace(C.byref(s), 0)
-        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need > 0 else None
-    args = [_rows4(q, q, "q"), _rows4(k, q, "k"), _rows4(v, q, "v", k.shape[2]), _rows4(o, q, "out", q.shape[2])]
-    _check(lib().fo_attention_forward(C.byref(s), *map(C.byref, args), lse.data_ptr(), ws.data_ptr() if need > 0 else None,
-                                      max(need, 0), st), "attention_forward")
+    L_ = lib()
+    s = _attention_spec(torch, q, k, causal, softcap, scale, slopes, table, buckets, documents, prefix)
+    B, L, H, D = shape = q.shape
+    device = q.device
+
+    def make():
+        o = torch.empty(shape, dtype=q.dtype, device=device) if out is None else out
+        lse = torch.empty((B, H, L), dtype=torch.float32, device=device)
+        # without documents a forward call needs no workspace
+        need = L_.fo_attention_workspace(s, 0) if documents is not None else 0
+        return o, lse, torch.empty(need, dtype=torch.uint8, device=device) if need > 0 else None, need
+
+    (o, lse, ws, need), st = _on_stream(torch, q, stream, make)
+    args = _strided(q, (B, L, s.kv_heads, D), (q, False, "q"), (k, True, "k"), (v, True, "v"), (o, False, "out"))
+    at, n = C.addressof(args), _fo_strided_bytes
+    _check(L_.fo_attention_forward(s, at, at + n, at + 2 * n, at + 3 * n, lse.data_ptr(),
+                                   ws.data_ptr() if need > 0 else None, need, st), "attention_forward")
     return o, lse
 
 
@@ -522,22 +537,28 @@ def attention_backward(dout, q, k, v, o, lse, causal=False, softcap=0.0, scale=N
     forward call; dtable is None without a table.  `grads` may give the three
     tensors to write (any strides with the innermost 1)."""
     import torch
-    s = _attention_spec(q, k, causal, softcap, scale, slopes, table, buckets, documents, prefix)
-    if dout.stride(3) != 1:
-        dout = dout.contiguous()                 # an expanded gradient, as sum().backward() gives
-    st, ctx = _stream_of(q, stream)
-    with ctx:
+    L_ = lib()
+    s = _attention_spec(torch, q, k, causal, softcap, scale, slopes, table, buckets, documents, prefix)
+    B, L, H, D = shape = q.shape
+    keys, device, dtype = (B, L, s.kv_heads, D), q.device, q.dtype
+    need = L_.fo_attention_workspace(s, 1)
+
+    def make():
+        g = dout.contiguous() if dout.dim() == 4 and dout.stride(3) != 1 else dout    # as sum().backward() gives it
         dq, dk, dv = grads if grads is not None else (
-            torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+            torch.empty(shape, dtype=dtype, device=device), torch.empty(keys, dtype=dtype, device=device),
+            torch.empty(keys, dtype=dtype, device=device))
         dtable = None if table is None else torch.empty_like(table)
-        need = lib().fo_attention_workspace(C.byref(s), 1)
-        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need > 0 else None
-    H, KV = q.shape[2], k.shape[2]
-    args = [_rows4(t, q, n, h) for t, n, h in ((q, "q", H), (k, "k", KV), (v, "v", KV), (o, "o", H))]
-    more = [_rows4(t, q, n, h) for t, n, h in ((dout, "dout", H), (dq, "dq", H), (dk, "dk", KV), (dv, "dv", KV))]
-    _check(lib().fo_attention_backward(
-        C.byref(s), *map(C.byref, args), _small(lse, (q.shape[0], H, q.shape[1]), torch.float32, q, "lse"),
-        *map(C.byref, more), _ptr(dtable), ws.data_ptr() if need > 0 else None, max(need, 0), st), "attention_backward")
+        return g, dq, dk, dv, dtable, torch.empty(need, dtype=torch.uint8, device=device) if need > 0 else None
+
+    (dout, dq, dk, dv, dtable, ws), st = _on_stream(torch, q, stream, make)
+    args = _strided(q, keys, (q, False, "q"), (k, True, "k"), (v, True, "v"), (o, False, "o"), (dout, False, "dout"),
+                    (dq, False, "dq"), (dk, True, "dk"), (dv, True, "dv"))
+    at, n = C.addressof(args), _fo_strided_bytes
+    _check(L_.fo_attention_backward(
+        s, at, at + n, at + 2 * n, at + 3 * n, _small(lse, (B, H, L), torch.float32, q, "lse"), at + 4 * n, at + 5 * n,
+        at + 6 * n, at + 7 * n, None if dtable is None else dtable.data_ptr(), ws.data_ptr() if need > 0 else None,
+        max(need, 0), st), "attention_backward")
     return dq, dk, dv, dtable
 
 
@@ -551,7 +572,7 @@ def attention_error(stream=None):
 
 def _matrix(t, like, name):
     """(pointer, row stride) of `t` seen as a matrix [rows, cols of its last dimension]."""
-    if t.shape != like.shape or t.dtype != like.dtype or t.device != like.device:
+    if t.shape != like.shape or t.dtype != like.dtype or t.get_device() != like.get_device():
         raise ValueError(f"{name}: x's shape, type and device are wanted")
     if t.is_contiguous():
         return t.data_ptr(), t.shape[-1]
@@ -567,16 +588,16 @@ def dropout_add(x, residual, p, seed, call, out=None, stream=None):
     import torch
     if not x.is_cuda or x.dtype not in (torch.bfloat16, torch.float32) or x.dim() < 1:
         raise ValueError("x: a bf16 or fp32 device tensor")
-    st, ctx = _stream_of(x, stream)
-    with ctx:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out
+    out, st = _on_stream(torch, x, stream,
+                         lambda: torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out)
     cols = x.shape[-1]
     xp, xs = _matrix(x, x, "x")
     rp, rs = (None, 0) if residual is None else _matrix(residual, x, "residual")
-    yp, ys = _matrix(y, x, "out")
+    yp, ys = _matrix(out, x, "out")
     _check(lib().fo_dropout_add(xp, xs, rp, rs, yp, ys, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_F32,
-                                x.numel() // cols if cols else 0, cols, p, seed & (2**64 - 1), call & (2**64 - 1), st), "dropout_add")
-    return y
+                                x.numel() // cols if cols else 0, cols, p, seed & (2**64 - 1), call & (2**64 - 1), st),
+           "dropout_add")
+    return out
 
 
 def dropout_grad(dy, p, seed, call, out=None, stream=None):

@@ -16,6 +16,7 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 
@@ -55,6 +56,23 @@ struct ScoredParams {
 enum { kScoredNone = 0, kScoredAll = 1, kScoredSome = 2 };
 
 #ifdef __CUDACC__
+// Sets a kernel's shared-memory limits the first time it is launched on the
+// current device (`done`: one flag per device, static in the launcher).
+constexpr int kMaxDevices = 64;
+constexpr int kSmemLimit = 232448;      // 227 KB per block
+template <typename K>
+cudaError_t allow_smem(K kernel, std::atomic<bool> (&done)[kMaxDevices]) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 0 && dev < kMaxDevices && done[dev]) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemLimit);
+  if (e == cudaSuccess)
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, int(cudaSharedmemCarveoutMaxShared));
+  if (e == cudaSuccess && dev >= 0 && dev < kMaxDevices) done[dev] = true;
+  return e;
+}
+
 // Summary of a run of document ids: x the smallest id >= 0 (INT_MAX when there
 // is none) with its sign bit set when the run holds padding, y the largest id.
 __device__ __forceinline__ int2 doc_join(int2 a, int2 b) {

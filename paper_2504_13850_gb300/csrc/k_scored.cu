@@ -7,9 +7,13 @@
 // the tokens, S = X U^T as one vector of each operand per width step (16 FMAs
 // per two reads) and the accumulating product (O += P V, dQ += dS K, ...) as
 // four columns of P against NC widths (16 NC FMAs per NC + 4 reads).  Vectors
-// are permuted by the width index, so that the transposing stores of a warp
-// (8 widths x 4 tokens) and the vector reads meet no bank twice.  Padding and
-// rows past the end are stored as zeros: what they hold never reaches a sum.
+// are permuted by the width index, so that the transposing copies of a warp
+// (8 x 4 widths x 4 tokens) and the vector reads meet no bank twice.  The next
+// tile's copies run while the current one is worked on: fp32 elements go to
+// their transposed place by 4-byte asynchronous copies, which need no
+// registers (loading them with the threads took five times the FMAs' time).
+// Padding and rows past the end are stored as zeros: what they hold never
+// reaches a sum.
 // The backward pass is two kernels of one body: a tile of queries walks the
 // keys (dQ), then a tile of keys walks the queries (dK, dV and the table
 // gradient); every sum has a fixed order, at the price of forming the scores
@@ -118,21 +122,49 @@ __global__ void __launch_bounds__(128) scored_table_k(const float* __restrict__ 
 
 // ----------------------------------------------------------- shared helpers
 // Float offset of the 16-byte vector g (tokens 4 g .. 4 g + 3) of row d.
-__device__ __forceinline__ int at4(int d, int g) { return d * kT + ((g ^ (d & 7)) << 2); }
+__device__ __forceinline__ int at4(int d, int g) { return d * kT + ((g ^ ((d >> 2) & 7)) << 2); }
+
+// Width n of this thread's NC accumulator columns.
+template <int NC>
+__device__ __forceinline__ int width_of(int tx, int n) {
+  return NC == 2 ? 2 * tx + n : 4 * tx + (n & 3) + 64 * (n >> 2);
+}
+
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Until at most N of this thread's groups of copies are in flight.
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
 
 // 64 tokens from l0 of one (sequence, head) -> dst[width][64], fp32, widths
-// rounded up to 8; tokens past the end and padding as zeros.
+// rounded up to 32; tokens past the end and padding as zeros.  Asynchronous
+// for fp32 (copies_commit / copies_wait).
 template <typename T>
 __device__ __forceinline__ void load_tile(float* dst, const Strided& t, const ScoredParams& p, int b, int h, int l0) {
   const T* base = static_cast<const T*>(t.p) + b * t.sb + h * t.sh;
   const int32_t* doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
   const int warp = threadIdx.x / 32, dl = (threadIdx.x % 32) >> 2, rl = threadIdx.x & 3;
-  const int n = (p.D + 7) / 8 * (kT / 4);
+  const int n = (p.D + 31) / 32 * (kT / 4);
+#pragma unroll 4
   for (int e = warp; e < n; e += kThreads / 32) {
-    const int g = e % (kT / 4), d = e / (kT / 4) * 8 + dl, l = l0 + 4 * g + rl;
-    float v = 0.f;
-    if (l < p.L && d < p.D && (!doc || doc[l] >= 0)) v = to_f(base[l * t.sl + d]);
-    dst[at4(d, g) + rl] = v;
+    const int g = e % (kT / 4), d0 = e / (kT / 4) * 32 + 4 * dl, l = l0 + 4 * g + rl;
+    const bool live = l < p.L && (!doc || doc[l] >= 0);
+    const T* src = base + (live ? l * t.sl : 0);
+    float* to = dst + at4(d0, g) + rl;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const bool in = live && d0 + c < p.D;
+      if (sizeof(T) == 4) {
+        const int bytes = in ? 4 : 0;      // 0: the copy writes a zero
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(
+                         static_cast<uint32_t>(__cvta_generic_to_shared(to + c * kT))),
+                     "l"(in ? src + d0 + c : base), "r"(bytes)
+                     : "memory");
+      } else {
+        to[c * kT] = in ? to_f(src[d0 + c]) : 0.f;
+      }
+    }
   }
 }
 
@@ -164,14 +196,14 @@ __device__ __forceinline__ void put_tile(float* P, const float (&s)[4][4], int t
     *reinterpret_cast<float4*>(P + at_p(4 * tx + c, ty)) = make_float4(s[0][c], s[1][c], s[2][c], s[3][c]);
 }
 
-// acc[r][n] += sum_c P[row r][c] W[width tx + 16 n][c].
+// acc[r][n] += sum_c P[row r][c] W[width n of this thread][c].
 template <int NC>
 __device__ __forceinline__ void accumulate(float (&acc)[4][NC], const float* P, const float* W, int ty, int tx) {
 #pragma unroll 2
   for (int g = 0; g < kT / 4; ++g) {
     float4 w[NC];
 #pragma unroll
-    for (int n = 0; n < NC; ++n) w[n] = *reinterpret_cast<const float4*>(W + at4(tx + 16 * n, g));
+    for (int n = 0; n < NC; ++n) w[n] = *reinterpret_cast<const float4*>(W + at4(width_of<NC>(tx, n), g));
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
       const float4 q = *reinterpret_cast<const float4*>(P + at_p(4 * g + c, ty));
@@ -186,10 +218,10 @@ __device__ __forceinline__ void accumulate(float (&acc)[4][NC], const float* P, 
   }
 }
 
-// Widths [D, 16 NC) of an accumulating product read rows that load_tile does
-// not write; they are cleared once.
+// An accumulating product reads all 16 NC rows of widths, also those that
+// load_tile does not write; they are cleared once.
 __device__ __forceinline__ void clear_tail(float* W, int D, int rows) {
-  for (int e = (D + 7) / 8 * 8 * kT + threadIdx.x; e < rows * kT; e += kThreads) W[e] = 0.f;
+  for (int e = (D + 31) / 32 * 32 * kT + threadIdx.x; e < rows * kT; e += kThreads) W[e] = 0.f;
 }
 
 template <typename T>
@@ -199,16 +231,23 @@ __device__ __forceinline__ void load_bias(float* bias, const ScoredParams& p, in
   for (int e = threadIdx.x; e < 2 * p.reach + 1; e += kThreads) bias[e] = to_f(t[p.map[e]]);
 }
 
+// What decides on a pair besides its positions.
 struct Pair {
   int pf;                // the sequence's prefix
   const int32_t* doc;    // its ids, or null
   float slope;
+  int row_id[4], col_id[4];
 };
 
-__device__ __forceinline__ bool pair_allowed(const ScoredParams& p, const Pair& c, int i, int j) {
+__device__ __forceinline__ void ids_of(int (&id)[4], const Pair& c, int l0) {
+  if (!c.doc) return;
+  const int4 v = *reinterpret_cast<const int4*>(c.doc + l0);
+  id[0] = v.x, id[1] = v.y, id[2] = v.z, id[3] = v.w;
+}
+__device__ __forceinline__ bool pair_allowed(const ScoredParams& p, const Pair& c, int i, int j, int r, int col) {
   if (i >= p.L || j >= p.L) return false;
   if (p.causal && j > i && j >= c.pf) return false;
-  return !c.doc || (c.doc[i] >= 0 && c.doc[i] == c.doc[j]);
+  return !c.doc || (c.row_id[r] >= 0 && c.row_id[r] == c.col_id[col]);
 }
 // The biased score of raw product x, and 1 - tanh^2 of the cap (1 without).
 __device__ __forceinline__ float pair_score(const ScoredParams& p, const Pair& c, const float* bias, float x, int i,
@@ -227,7 +266,7 @@ __device__ __forceinline__ float pair_score(const ScoredParams& p, const Pair& c
 }
 
 __device__ __forceinline__ Pair pair_of(const ScoredParams& p, int b, int h) {
-  Pair c;
+  Pair c = {};
   c.pf = p.prefix ? p.prefix[b] : 0;
   c.doc = p.doc ? p.doc + int64_t(b) * p.Lp : nullptr;
   c.slope = p.slopes ? p.slopes[h] : 0.f;
@@ -240,7 +279,18 @@ __device__ __forceinline__ int tile_class(const ScoredParams& p, int pf, int b, 
     qd = blk[q0 / kScoredBlock];
     kd = blk[k0 / kScoredBlock];
   }
-  return scored_class(p, pf, q0, q0 + kT, k0, k0 + kT, p.blk != nullptr, qd, kd);
+  const int cls = scored_class(p, pf, q0, q0 + kT, k0, k0 + kT, p.blk != nullptr, qd, kd);
+  return cls == kScoredAll && max(q0, k0) + kT > p.L ? kScoredSome : cls;
+}
+// The first tile from c0 on of which pairs with the tile at r0 are allowed
+// (p.L or more: none); *cls receives its class.
+template <bool KEYS_ARE_ROWS>
+__device__ __forceinline__ int next_tile(const ScoredParams& p, int pf, int b, int r0, int c0, int* cls) {
+  for (; c0 < p.L; c0 += kT) {
+    *cls = tile_class(p, pf, b, KEYS_ARE_ROWS ? c0 : r0, KEYS_ARE_ROWS ? r0 : c0);
+    if (*cls != kScoredNone) break;
+  }
+  return c0;
 }
 
 template <typename T, int NC>
@@ -253,7 +303,7 @@ __device__ __forceinline__ void store_rows(const Strided& t, const ScoredParams&
     if (l >= p.L) continue;
 #pragma unroll
     for (int n = 0; n < NC; ++n)
-      if (tx + 16 * n < p.D) base[l * t.sl + tx + 16 * n] = from_f<T>(acc[r][n] * mul[r]);
+      if (width_of<NC>(tx, n) < p.D) base[l * t.sl + width_of<NC>(tx, n)] = from_f<T>(acc[r][n] * mul[r]);
   }
 }
 
@@ -262,28 +312,43 @@ template <typename T, int NC>
 __global__ void __launch_bounds__(kThreads) scored_fwd_k(const __grid_constant__ ScoredParams p) {
   extern __shared__ __align__(16) float sm[];
   constexpr int W = 16 * NC;
-  float *Q = sm, *K = Q + W * kT, *V = K + W * kT, *P = V + W * kT, *bias = P + kT * kT;
+  constexpr int kTile = W * kT;
+  float *Q = sm, *KVs = Q + kTile, *P = KVs + 4 * kTile, *bias = P + kT * kT;    // KVs: two pairs of K and V
   pdl_wait();
   pdl_trigger();
   const int tiles = (p.L + kT - 1) / kT, bh = blockIdx.x % (p.B * p.H);
   const int q0 = (tiles - 1 - int(blockIdx.x / (p.B * p.H))) * kT;   // the longest causal rows first
   const int b = bh / p.H, h = bh % p.H, kh = h / p.G, D8 = (p.D + 7) / 8 * 8;
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
-  const Pair pc = pair_of(p, b, h);
+  Pair pc = pair_of(p, b, h);
+  int cls = 0, cls_next = 0, buf = 0;
+  int k0 = next_tile<false>(p, pc.pf, b, q0, 0, &cls);
   load_tile<T>(Q, p.q, p, b, h, q0);
+  if (k0 < p.L) {
+    load_tile<T>(KVs, p.k, p, b, kh, k0);
+    load_tile<T>(KVs + kTile, p.v, p, b, kh, k0);
+  }
+  copies_commit();
   load_bias<T>(bias, p, h);
-  clear_tail(V, p.D, W);
-  float acc[4][NC] = {}, m[4], sum[4] = {0.f, 0.f, 0.f, 0.f};
+  clear_tail(KVs + kTile, p.D, W);
+  clear_tail(KVs + 3 * kTile, p.D, W);
+  ids_of(pc.row_id, pc, q0 + 4 * ty);
+  float acc[4][NC] = {}, m[4], sum[4] = {0.f, 0.f, 0.f, 0.f};     // m in units of log2
 #pragma unroll
   for (int r = 0; r < 4; ++r) m[r] = -INFINITY;
-  for (int k0 = 0; k0 < p.L; k0 += kT) {
-    if (tile_class(p, pc.pf, b, q0, k0) == kScoredNone) continue;
+  while (k0 < p.L) {
+    const int k1 = next_tile<false>(p, pc.pf, b, q0, k0 + kT, &cls_next);
+    if (k1 < p.L) {
+      load_tile<T>(KVs + 2 * (buf ^ 1) * kTile, p.k, p, b, kh, k1);
+      load_tile<T>(KVs + (2 * (buf ^ 1) + 1) * kTile, p.v, p, b, kh, k1);
+    }
+    copies_commit();
+    copies_wait<1>();
     __syncthreads();
-    load_tile<T>(K, p.k, p, b, kh, k0);
-    load_tile<T>(V, p.v, p, b, kh, k0);
-    __syncthreads();
+    const float *K = KVs + 2 * buf * kTile, *V = K + kTile;
     float s[4][4], chain;
     scores(s, Q, K, D8, ty, tx);
+    if (cls == kScoredSome) ids_of(pc.col_id, pc, k0 + 4 * tx);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int i = q0 + 4 * ty + r;
@@ -291,16 +356,17 @@ __global__ void __launch_bounds__(kThreads) scored_fwd_k(const __grid_constant__
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         const int j = k0 + 4 * tx + c;
-        s[r][c] = pair_allowed(p, pc, i, j) ? pair_score(p, pc, bias, s[r][c], i, j, &chain) : -INFINITY;
+        s[r][c] = pair_score(p, pc, bias, s[r][c], i, j, &chain) * kLog2e;
+        if (cls == kScoredSome && !pair_allowed(p, pc, i, j, r, c)) s[r][c] = -INFINITY;
         top = fmaxf(top, s[r][c]);
       }
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const float base = top == -INFINITY ? 0.f : top, keep = expf(m[r] - base);
+      const float base = top == -INFINITY ? 0.f : top, keep = exp2f(m[r] - base);
       float part = 0.f;
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
-        s[r][c] = expf(s[r][c] - base);
+        s[r][c] = exp2f(s[r][c] - base);
         part += s[r][c];
       }
 #pragma unroll
@@ -313,13 +379,18 @@ __global__ void __launch_bounds__(kThreads) scored_fwd_k(const __grid_constant__
     put_tile(P, s, ty, tx);
     __syncthreads();
     accumulate<NC>(acc, P, V, ty, tx);
+    __syncthreads();
+    k0 = k1;
+    cls = cls_next;
+    buf ^= 1;
   }
+  copies_wait<0>();
   float inv[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     inv[r] = sum[r] > 0.f ? 1.f / sum[r] : (sum[r] == 0.f ? 0.f : sum[r]);   // a NaN row stays NaN
     const int l = q0 + 4 * ty + r;
-    if (tx == 0 && l < p.L) p.lse[int64_t(bh) * p.L + l] = sum[r] == 0.f ? -INFINITY : m[r] + logf(sum[r]);
+    if (tx == 0 && l < p.L) p.lse[int64_t(bh) * p.L + l] = sum[r] == 0.f ? -INFINITY : m[r] * kLn2 + logf(sum[r]);
   }
   store_rows<T, NC>(p.o, p, acc, inv, b, h, q0, ty, tx);
 }
@@ -334,7 +405,8 @@ template <typename T, int NC, bool KV>
 __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__ ScoredParams p) {
   extern __shared__ __align__(16) float sm[];
   constexpr int WD = 16 * NC;
-  float *X = sm, *Y = X + WD * kT, *U = Y + WD * kT, *W = U + WD * kT, *P = W + WD * kT;
+  constexpr int kTile = WD * kT;
+  float *X = sm, *Y = X + kTile, *UWs = Y + kTile, *P = UWs + 4 * kTile;        // UWs: two pairs of U and W
   float* bias = P + kT * kT;
   float* dist = bias + 2 * kMaxReach + 4;          // KV true: table gradient by distance
   float* far = dist + 2 * kMaxReach + 4;           // [2][128] sums beyond the reach
@@ -348,37 +420,47 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
   const bool grad = KV && p.dtable;
   load_tile<T>(X, KV ? p.k : p.q, p, b, KV ? kh : h0, r0);
   load_tile<T>(Y, KV ? p.v : p.dout, p, b, KV ? kh : h0, r0);
-  clear_tail(U, p.D, WD);
-  clear_tail(W, p.D, WD);
+  for (int e = 0; e < 4; ++e) clear_tail(UWs + e * kTile, p.D, WD);
   float lo = 0.f, hi = 0.f;                        // sums of this thread's diagonals beyond the reach
   float eps[4] = {0.f, 0.f, 0.f, 0.f};             // row sums of dS
   float acc0[4][NC] = {}, acc1[4][NC] = {};
   for (int g = 0; g < (KV ? p.G : 1); ++g) {
     const int h = h0 + g;
-    const Pair pc = pair_of(p, b, h);
+    Pair pc = pair_of(p, b, h);
+    ids_of(pc.row_id, pc, r0 + 4 * ty);
     const float* lse2 = p.lse2 + (int64_t(b) * p.H + h) * p.Lp;
     const float* delta = p.delta + (int64_t(b) * p.H + h) * p.Lp;
+    auto load = [&](int buf, int c0) {
+      load_tile<T>(UWs + 2 * buf * kTile, KV ? p.q : p.k, p, b, KV ? h : kh, c0);
+      load_tile<T>(UWs + (2 * buf + 1) * kTile, KV ? p.dout : p.v, p, b, KV ? h : kh, c0);
+    };
+    int cls = 0, cls_next = 0, buf = 0;
+    int c0 = next_tile<KV>(p, pc.pf, b, r0, 0, &cls);
     __syncthreads();
+    if (c0 < p.L) load(0, c0);
+    copies_commit();
     load_bias<T>(bias, p, h);
     if (grad) {
       for (int e = threadIdx.x; e < 2 * p.reach + 1; e += kThreads) dist[e] = 0.f;
       lo = hi = 0.f;
     }
-    for (int c0 = 0; c0 < p.L; c0 += kT) {
-      if (tile_class(p, pc.pf, b, KV ? c0 : r0, KV ? r0 : c0) == kScoredNone) continue;
+    for (; c0 < p.L;) {
+      const int c1 = next_tile<KV>(p, pc.pf, b, r0, c0 + kT, &cls_next);
+      if (c1 < p.L) load(buf ^ 1, c1);
+      copies_commit();
+      copies_wait<1>();
       __syncthreads();
-      load_tile<T>(U, KV ? p.q : p.k, p, b, KV ? h : kh, c0);
-      load_tile<T>(W, KV ? p.dout : p.v, p, b, KV ? h : kh, c0);
-      __syncthreads();
+      const float *U = UWs + 2 * buf * kTile, *W = U + kTile;
       float s[4][4], dp[4][4], chain[4][4];
       scores(s, X, U, D8, ty, tx);
       scores(dp, Y, W, D8, ty, tx);
+      if (cls == kScoredSome) ids_of(pc.col_id, pc, c0 + 4 * tx);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const int row = r0 + 4 * ty + r, col = c0 + 4 * tx + c, i = KV ? col : row, j = KV ? row : col;
-          const bool ok = pair_allowed(p, pc, i, j);
+          const bool ok = cls == kScoredAll || pair_allowed(p, pc, i, j, r, c);
           const float z = pair_score(p, pc, bias, s[r][c], i, j, &chain[r][c]);
           s[r][c] = ok ? exp2f(fmaf(z, kLog2e, -lse2[i])) : 0.f;
           dp[r][c] = ok ? s[r][c] * (dp[r][c] - delta[i]) : 0.f;
@@ -412,7 +494,12 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
       put_tile(P, dp, ty, tx);
       __syncthreads();
       accumulate<NC>(acc1, P, U, ty, tx);
+      __syncthreads();
+      c0 = c1;
+      cls = cls_next;
+      buf ^= 1;
     }
+    copies_wait<0>();
     if (grad) {
       __syncthreads();
       if (threadIdx.x < 128) {
@@ -454,27 +541,27 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
   }
 }
 
-template <typename K>
-cudaError_t run(K kernel, int64_t blocks, size_t smem, cudaStream_t st, const ScoredParams& p) {
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
-  if (e != cudaSuccess) return e;
-  return launch_k(kernel, dim3(unsigned(blocks)), dim3(kThreads), smem, st, p);
-}
-
 template <typename T, int NC>
 cudaError_t forward_width(const ScoredParams& p, cudaStream_t st) {
   const int64_t tiles = ceil_div(p.L, kT);
-  const size_t smem = (size_t(3 * 16 * NC * kT) + kT * kT + 2 * kMaxReach + 4) * sizeof(float);
-  return run(scored_fwd_k<T, NC>, tiles * p.B * p.H, smem, st, p);
+  const size_t smem = (size_t(5 * 16 * NC * kT) + kT * kT + (p.table ? 2 * kMaxReach + 4 : 0)) * sizeof(float);
+  static std::atomic<bool> allowed[kMaxDevices];
+  const cudaError_t e = allow_smem(scored_fwd_k<T, NC>, allowed);
+  if (e != cudaSuccess) return e;
+  return launch_k(scored_fwd_k<T, NC>, dim3(unsigned(tiles * p.B * p.H)), dim3(kThreads), smem, st, p);
 }
 template <typename T, int NC>
 cudaError_t backward_width(const ScoredParams& p, cudaStream_t st) {
   const int64_t tiles = ceil_div(p.L, kT);
   const size_t smem =
-      (size_t(4 * 16 * NC * kT) + kT * kT + 2 * (2 * kMaxReach + 4) + 256) * sizeof(float);
-  cudaError_t e = run(scored_bwd_k<T, NC, false>, tiles * p.B * p.H, smem, st, p);
+      (size_t(6 * 16 * NC * kT) + kT * kT + (p.table ? 2 * (2 * kMaxReach + 4) + 256 : 0)) * sizeof(float);
+  static std::atomic<bool> allowed[2][kMaxDevices];
+  cudaError_t e = allow_smem(scored_bwd_k<T, NC, false>, allowed[0]);
+  if (e == cudaSuccess) e = allow_smem(scored_bwd_k<T, NC, true>, allowed[1]);
+  if (e == cudaSuccess)
+    e = launch_k(scored_bwd_k<T, NC, false>, dim3(unsigned(tiles * p.B * p.H)), dim3(kThreads), smem, st, p);
   if (e != cudaSuccess) return e;
-  return run(scored_bwd_k<T, NC, true>, tiles * p.B * p.KV, smem, st, p);
+  return launch_k(scored_bwd_k<T, NC, true>, dim3(unsigned(tiles * p.B * p.KV)), dim3(kThreads), smem, st, p);
 }
 // Accumulator columns per thread: 16 NC >= head width.
 template <typename T>

@@ -508,8 +508,6 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   }
 }
 
-constexpr size_t kSmemLimit = 232448;
-
 template <int DP, bool KV>
 struct Launch {
   BwdParams& bp;
@@ -524,7 +522,8 @@ struct Launch {
     bp.s.stages = stages;
     const size_t smem = need(stages);
     auto k = scored_bwd_tc_k<DP, KV, BIAS, CAP>;
-    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    static std::atomic<bool> allowed[kMaxDevices];
+    const cudaError_t e = allow_smem(k, allowed);
     if (e != cudaSuccess) return e;
     const int64_t tiles = ceil_div(bp.s.L, 128);
     return launch_k(k, dim3(unsigned(tiles * bp.s.B * (KV ? bp.s.KV : bp.s.H))), dim3(kThreads), smem, st, bp);

@@ -416,9 +416,8 @@ struct Launch {
     using F = Fwd<DP, NT>;
     const size_t smem = F::smem(fp.s.L, BIAS == kBiasTable);
     auto k = scored_fwd_tc_k<DP, NT, BIAS, CAP>;
-    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
-    if (e != cudaSuccess) return e;
-    e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, int(cudaSharedmemCarveoutMaxShared));
+    static std::atomic<bool> allowed[kMaxDevices];
+    const cudaError_t e = allow_smem(k, allowed);
     if (e != cudaSuccess) return e;
     const int64_t tiles = ceil_div(fp.s.L, 128 * NT);
     return launch_k(k, dim3(unsigned(tiles * fp.s.B * fp.s.H)), dim3(F::kThreads), smem, st, fp);
