@@ -168,21 +168,31 @@ __device__ __forceinline__ void load_tile(float* dst, const Strided& t, const Sc
   }
 }
 
-// s[r][c] = sum_d X[d][row r] U[d][column c].
-__device__ __forceinline__ void scores(float (&s)[4][4], const float* X, const float* U, int D8, int ty, int tx) {
+// s[r][c] = sum_d X[d][row r] U[d][column c], widths rounded up to 4.  The
+// permutation repeats every 32 widths: unrolled over them its offsets are
+// constants xor the thread's vector.
+__device__ __forceinline__ void scores(float (&s)[4][4], const float* X, const float* U, int D, int ty, int tx) {
 #pragma unroll
   for (int r = 0; r < 4; ++r)
 #pragma unroll
     for (int c = 0; c < 4; ++c) s[r][c] = 0.f;
-#pragma unroll 4
-  for (int d = 0; d < D8; ++d) {
-    const float4 a = *reinterpret_cast<const float4*>(X + at4(d, ty));
-    const float4 u = *reinterpret_cast<const float4*>(U + at4(d, tx));
-    const float av[4] = {a.x, a.y, a.z, a.w}, uv[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll 1
+  for (int d0 = 0; d0 < D; d0 += 32, X += 32 * kT, U += 32 * kT) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int k = 0; k < 8; ++k) {
+      if (d0 + 4 * k >= D) break;
+      const float *x = X + 4 * k * kT + ((ty ^ k) << 2), *u = U + 4 * k * kT + ((tx ^ k) << 2);
 #pragma unroll
-      for (int c = 0; c < 4; ++c) s[r][c] = fmaf(av[r], uv[c], s[r][c]);
+      for (int e = 0; e < 4; ++e) {
+        const float4 a = *reinterpret_cast<const float4*>(x + e * kT);
+        const float4 w = *reinterpret_cast<const float4*>(u + e * kT);
+        const float av[4] = {a.x, a.y, a.z, a.w}, wv[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) s[r][c] = fmaf(av[r], wv[c], s[r][c]);
+      }
+    }
   }
 }
 
@@ -199,20 +209,28 @@ __device__ __forceinline__ void put_tile(float* P, const float (&s)[4][4], int t
 // acc[r][n] += sum_c P[row r][c] W[width n of this thread][c].
 template <int NC>
 __device__ __forceinline__ void accumulate(float (&acc)[4][NC], const float* P, const float* W, int ty, int tx) {
-#pragma unroll 2
-  for (int g = 0; g < kT / 4; ++g) {
-    float4 w[NC];
+  // rows of W this thread reads share one permutation (see width_of)
+  const int first = width_of<NC>(tx, 0), turn = (first >> 2) & 7;
+  W += first * kT;
+#pragma unroll 1
+  for (int g0 = 0; g0 < kT / 4; g0 += 4, P += 16 * kT) {
 #pragma unroll
-    for (int n = 0; n < NC; ++n) w[n] = *reinterpret_cast<const float4*>(W + at4(width_of<NC>(tx, n), g));
+    for (int k = 0; k < 4; ++k) {
+      const float *w_at = W + (((g0 + k) ^ turn) << 2), *p_at = P + 4 * k * kT + ((ty ^ (g0 + k)) << 2);
+      float4 w[NC];
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      const float4 q = *reinterpret_cast<const float4*>(P + at_p(4 * g + c, ty));
-      const float qv[4] = {q.x, q.y, q.z, q.w};
+      for (int n = 0; n < NC; ++n)
+        w[n] = *reinterpret_cast<const float4*>(w_at + (NC == 2 ? n : (n & 3) + 64 * (n >> 2)) * kT);
 #pragma unroll
-      for (int n = 0; n < NC; ++n) {
-        const float wv = c == 0 ? w[n].x : c == 1 ? w[n].y : c == 2 ? w[n].z : w[n].w;
+      for (int c = 0; c < 4; ++c) {
+        const float4 q = *reinterpret_cast<const float4*>(p_at + c * kT);
+        const float qv[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[r][n] = fmaf(qv[r], wv, acc[r][n]);
+        for (int n = 0; n < NC; ++n) {
+          const float wv = c == 0 ? w[n].x : c == 1 ? w[n].y : c == 2 ? w[n].z : w[n].w;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[r][n] = fmaf(qv[r], wv, acc[r][n]);
+        }
       }
     }
   }
@@ -318,7 +336,7 @@ __global__ void __launch_bounds__(kThreads) scored_fwd_k(const __grid_constant__
   pdl_trigger();
   const int tiles = (p.L + kT - 1) / kT, bh = blockIdx.x % (p.B * p.H);
   const int q0 = (tiles - 1 - int(blockIdx.x / (p.B * p.H))) * kT;   // the longest causal rows first
-  const int b = bh / p.H, h = bh % p.H, kh = h / p.G, D8 = (p.D + 7) / 8 * 8;
+  const int b = bh / p.H, h = bh % p.H, kh = h / p.G;
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
   Pair pc = pair_of(p, b, h);
   int cls = 0, cls_next = 0, buf = 0;
@@ -347,7 +365,7 @@ __global__ void __launch_bounds__(kThreads) scored_fwd_k(const __grid_constant__
     __syncthreads();
     const float *K = KVs + 2 * buf * kTile, *V = K + kTile;
     float s[4][4], chain;
-    scores(s, Q, K, D8, ty, tx);
+    scores(s, Q, K, p.D, ty, tx);
     if (cls == kScoredSome) ids_of(pc.col_id, pc, k0 + 4 * tx);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -415,7 +433,7 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
   const int heads = KV ? p.KV : p.H, tiles = (p.L + kT - 1) / kT;
   const int bh = blockIdx.x % (p.B * heads), slot = int(blockIdx.x / (p.B * heads));
   const int tile = KV ? slot : tiles - 1 - slot, r0 = tile * kT;     // the longest causal tiles first
-  const int b = bh / heads, h0 = KV ? (bh % heads) * p.G : bh % heads, kh = h0 / p.G, D8 = (p.D + 7) / 8 * 8;
+  const int b = bh / heads, h0 = KV ? (bh % heads) * p.G : bh % heads, kh = h0 / p.G;
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
   const bool grad = KV && p.dtable;
   load_tile<T>(X, KV ? p.k : p.q, p, b, KV ? kh : h0, r0);
@@ -452,8 +470,8 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
       __syncthreads();
       const float *U = UWs + 2 * buf * kTile, *W = U + kTile;
       float s[4][4], dp[4][4], chain[4][4];
-      scores(s, X, U, D8, ty, tx);
-      scores(dp, Y, W, D8, ty, tx);
+      scores(s, X, U, p.D, ty, tx);
+      scores(dp, Y, W, p.D, ty, tx);
       if (cls == kScoredSome) ids_of(pc.col_id, pc, c0 + 4 * tx);
 #pragma unroll
       for (int r = 0; r < 4; ++r)
