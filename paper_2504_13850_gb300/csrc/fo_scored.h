@@ -39,8 +39,8 @@ struct ScoredParams {
   // workspace
   int32_t* doc;            // [B][Lp] document ids, -1 past the sequence; null without documents
   int2* blk;               // [B][Lp / 64] summary of each 64 ids (see doc_summary)
-  float* lse2;             // [B][H][Lp] lse * log2(e), +inf where P is zero
-  float* delta;            // [B][H][Lp] D
+  float* lse2;             // [B][H][Lp] -lse * log2(e), -inf where P is zero
+  float* delta;            // [B][H][Lp] -D
   float* part;             // [H][buckets][B * query tiles] partial table gradients
   const float* slopes;     // [H] or null
   const void* table;       // [H][buckets] in the tensors' type, or null

@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(128) scored_docs_k(const int32_t* __restrict__
   if (lane == 0) blk[w] = s;
 }
 
-// D_i = sum_d dO O and lse * log2(e), padded to Lp rows per (sequence, head).
+// -D_i = -sum_d dO O and -lse * log2(e), padded to Lp rows per (sequence, head).
 // VEC: 16-byte loads (8 bf16), DL lanes per row; else one warp per row.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) scored_delta_k(const __grid_constant__ ScoredParams p, int lanes) {
@@ -100,8 +100,8 @@ __global__ void __launch_bounds__(256) scored_delta_k(const __grid_constant__ Sc
   for (int o = lanes / 2; o > 0; o >>= 1) d += __shfl_xor_sync(0xffffffffu, d, o);
   if (row < rows && sub == 0) {
     const float lse = live ? p.lse[bh * p.L + l] : -INFINITY;
-    p.delta[row] = live ? d : 0.f;
-    p.lse2[row] = lse == -INFINITY ? INFINITY : lse * kLog2e;
+    p.delta[row] = live ? -d : 0.f;
+    p.lse2[row] = lse == -INFINITY ? -INFINITY : -lse * kLog2e;
   }
 }
 
@@ -480,8 +480,8 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
           const int row = r0 + 4 * ty + r, col = c0 + 4 * tx + c, i = KV ? col : row, j = KV ? row : col;
           const bool ok = cls == kScoredAll || pair_allowed(p, pc, i, j, r, c);
           const float z = pair_score(p, pc, bias, s[r][c], i, j, &chain[r][c]);
-          s[r][c] = ok ? exp2f(fmaf(z, kLog2e, -lse2[i])) : 0.f;
-          dp[r][c] = ok ? s[r][c] * (dp[r][c] - delta[i]) : 0.f;
+          s[r][c] = ok ? exp2f(fmaf(z, kLog2e, lse2[i])) : 0.f;
+          dp[r][c] = ok ? s[r][c] * (dp[r][c] + delta[i]) : 0.f;
           eps[r] += dp[r][c];
         }
       if (grad) {
@@ -554,7 +554,7 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) eps[r] += __shfl_xor_sync(0xffffffffu, eps[r], o);
       const int l = r0 + 4 * ty + r;
-      if (tx == 0 && l < p.L) p.delta[(int64_t(b) * p.H + h0) * p.Lp + l] += eps[r];
+      if (tx == 0 && l < p.L) p.delta[(int64_t(b) * p.H + h0) * p.Lp + l] -= eps[r];
     }
   }
 }

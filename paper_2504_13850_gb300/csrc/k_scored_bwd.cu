@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   using F = Bwd<DP, KV>;
   const ScoredParams& p = bp.s;
   extern __shared__ __align__(1024) char smem_raw[];
-  char* sm = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  char* sm = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);    // 1024-byte aligned
   char *sX = sm, *sY = sm + F::kX, *ring = sm + 2 * F::kX;
   const int stages = p.stages, words = (p.L + 2047) / 2048;
   uint64_t* bars = reinterpret_cast<uint64_t*>(ring + stages * F::kStage);
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
                  : scored_class(p, pf, r0, r0 + 128, c0, c0 + 64, blk != nullptr, rd, cd);
         // keys past the end are zeros in shared memory, not absent: as columns
         // they would enter dQ, as rows the table gradient; queries past the
-        // end have lse = +infinity
+        // end have P = 0
         if (cls == kScoredAll && (KV ? grad && r0 + 128 > p.L : c0 + 64 > p.L)) cls = kScoredSome;
         pad = cd.x < 0 && cls != kScoredNone;
       }
@@ -209,47 +209,48 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       total *= groups;
       int in = 0, in_slot = 0, in_phase = 0;           // the next step whose scores are formed
       Ring<F::kBufs> in_buf, buf;
-      auto scores = [&]() {
-        wait.on(&landed[in_slot], in_phase, 32);
-        tc_fence_after();
-        if (wait.dead) return;
-        const uint32_t d = tmem + 128 * in_buf.at;
-        const Operand<16> x(x_at), y(y_at), u(ring_at + in_slot * F::kStage), w(ring_at + in_slot * F::kStage + F::kU);
-#pragma unroll
-        for (int e = 0; e < DP / 16; ++e)
-          mma_f16(d, x.at((e >> 2) * 16384 + 32 * (e & 3)), u.at((e >> 2) * 8192 + 32 * (e & 3)), id_s, e > 0 ? 1u : 0u);
-#pragma unroll
-        for (int e = 0; e < DP / 16; ++e)
-          mma_f16(d + 64, y.at((e >> 2) * 16384 + 32 * (e & 3)), w.at((e >> 2) * 8192 + 32 * (e & 3)), id_s,
-                  e > 0 ? 1u : 0u);
-        mma_commit(&sfull[in_buf.at]);
-        in_buf.step();
-        ++in;
-        if (++in_slot == stages) in_slot = 0, in_phase ^= 1;
-      };
       wait.on(xfull, 0, 33);
-      while (in < F::kBufs && in < total && !wait.dead) scores();
       int slot = 0;
-      for (int n = 0; n < total && !wait.dead; ++n) {
-        wait.on(&pfull[buf.at], buf.phase, 34);
-        tc_fence_after();
-        if (wait.dead) break;
-        const uint32_t a = tmem + 128 * buf.at;
-        const Operand<8192> u(ring_at + slot * F::kStage), w(ring_at + slot * F::kStage + F::kU);
-        if (KV) {
+      // one loop with one place for each product: kBufs steps of scores ahead
+      for (int n = -F::kBufs; n < total && !wait.dead; ++n) {
+        if (n >= 0) {
+          wait.on(&pfull[buf.at], buf.phase, 34);
+          tc_fence_after();
+          if (wait.dead) break;
+          const uint32_t a = tmem + 128 * buf.at;
+          const Operand<8192> u(ring_at + slot * F::kStage), w(ring_at + slot * F::kStage + F::kU);
+          if (KV) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              mma_ts(acc, a + 32 * (e >> 1) + 8 * (e & 1), w.at(2048 * e), id_a, e > 0 ? 1u : uint32_t(n));
+          }
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            mma_ts(acc, a + 32 * (e >> 1) + 8 * (e & 1), w.at(2048 * e), id_a, e > 0 ? 1u : uint32_t(n));
+            mma_ts(acc + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1), u.at(2048 * e), id_a,
+                   e > 0 ? 1u : uint32_t(n));
+          mma_commit(&empty[slot]);
+          if (n + 1 == total) mma_commit(afull);
+          if (++slot == stages) slot = 0;
+          buf.step();
         }
+        if (in < total) {
+          wait.on(&landed[in_slot], in_phase, 32);
+          tc_fence_after();
+          if (wait.dead) break;
+          const uint32_t d = tmem + 128 * in_buf.at;
+          const Operand<16> x(x_at), y(y_at), u(ring_at + in_slot * F::kStage), w(ring_at + in_slot * F::kStage + F::kU);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          mma_ts(acc + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1), u.at(2048 * e), id_a,
-                 e > 0 ? 1u : uint32_t(n));
-        mma_commit(&empty[slot]);
-        if (in < total) scores();
-        else if (n + 1 == total) mma_commit(afull);
-        if (++slot == stages) slot = 0;
-        buf.step();
+          for (int e = 0; e < DP / 16; ++e)
+            mma_f16(d, x.at((e >> 2) * 16384 + 32 * (e & 3)), u.at((e >> 2) * 8192 + 32 * (e & 3)), id_s, e > 0 ? 1u : 0u);
+#pragma unroll
+          for (int e = 0; e < DP / 16; ++e)
+            mma_f16(d + 64, y.at((e >> 2) * 16384 + 32 * (e & 3)), w.at((e >> 2) * 8192 + 32 * (e & 3)), id_s,
+                    e > 0 ? 1u : 0u);
+          mma_commit(&sfull[in_buf.at]);
+          in_buf.step();
+          ++in;
+          if (++in_slot == stages) in_slot = 0, in_phase ^= 1;
+        }
       }
     }
     __syncwarp();
@@ -280,7 +281,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     // that are keys allow columns from `edge` on (none past the end)
     const int edge = KV ? (i >= p.L ? INT32_MAX : p.causal && i >= pf ? i : 0) : min(p.causal ? max(i + 1, pf) : p.L, p.L);
     const int64_t stat = (int64_t(b) * p.H + h0) * p.Lp + i;
-    const float row_lse = KV ? 0.f : -p.lse2[stat], row_d = KV ? 0.f : -p.delta[stat];
+    const float row_lse = KV ? 0.f : p.lse2[stat], row_d = KV ? 0.f : p.delta[stat];
     const F2 c2 = f2(c, c);
     F2 eps = f2(0.f, 0.f);                 // KV false: sum of this thread's dS
     float lo_sum = 0.f, hi_sum = 0.f;      // table gradient beyond the reach
@@ -323,8 +324,8 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
           for (int e = 0; e < 16; e += 4) {
             F2 l0 = f2(row_lse, row_lse), l1 = l0, d0 = f2(row_d, row_d), d1 = d0;
             if (KV) {
-              const float4 l4 = ld_shared4(stats + 64 * pass + 4 * e), d4 = ld_shared4(stats + 256 + 64 * pass + 4 * e);
-              l0 = f2(-l4.x, -l4.y), l1 = f2(-l4.z, -l4.w), d0 = f2(-d4.x, -d4.y), d1 = f2(-d4.z, -d4.w);
+              ld_pairs(stats + 64 * pass + 4 * e, l0, l1);
+              ld_pairs(stats + 256 + 64 * pass + 4 * e, d0, d1);
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
@@ -463,7 +464,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       asm volatile("bar.sync 9, 512;" ::: "memory");
       if (warp < 4 && i < p.L) {
         const float* z = rowsum + 32 * quarter + lane;
-        p.delta[stat] = (z[0] + z[128]) + (z[256] + z[384]) - row_d;
+        p.delta[stat] = row_d - ((z[0] + z[128]) + (z[256] + z[384]));
       }
     }
     if (n > 0) {

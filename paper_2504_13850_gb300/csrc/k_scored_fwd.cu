@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
   using F = Fwd<DP, NT>;
   const ScoredParams& p = fp.s;
   extern __shared__ __align__(1024) char smem_raw[];
-  char* sm = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  char* sm = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);    // 1024-byte aligned
   char* sQ = sm;
   char* ring = sm + NT * F::kTileBytes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(sm + F::kOps);
