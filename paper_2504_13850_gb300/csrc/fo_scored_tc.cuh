@@ -7,6 +7,8 @@
 #include "fo_scored.h"
 #include "fo_tc.h"
 
+#include <cuda_fp16.h>
+
 namespace fo {
 namespace {
 
@@ -209,8 +211,10 @@ __device__ __forceinline__ void load_bias(float* bias, const ScoredParams& p, in
 }
 
 // N scores (fp32 bits) of one query row, keys j0 .. j0 + N - 1 -> score units:
-// the cap (q, when asked for, receives 1 / (1 + e^2y), from which tanh y =
-// 1 - 2 q and its derivative 4 q (1 - q) follow) and the bias.  DIR is +1 when
+// the cap (ch, when given, receives its derivative 1 - tanh^2 as pairs of
+// fp16: a factor in [0, 1] of a product that is itself rounded to bf16; with
+// q = 1 / (1 + e^2y), tanh y = 1 - 2 q and the derivative is 4 q (1 - q)) and
+// the bias.  DIR is +1 when
 // the columns are keys and -1 when they are queries (the row then is the key);
 // d = distance of column 0, lo and hi the bounds of the warp's distances.
 struct Shape {
@@ -218,15 +222,24 @@ struct Shape {
   const float* bias;
   int reach;
 };
-template <int N, int BIAS, bool CAP, int DIR, bool KEEP>
-__device__ __forceinline__ void shape_scores(uint32_t (&r)[N], uint32_t (&q)[N], const Shape& a, int d, int lo, int hi) {
+template <int N, int BIAS, bool CAP, int DIR>
+__device__ __forceinline__ void shape_scores(uint32_t (&r)[N], uint32_t* ch, const Shape& a, int d, int lo, int hi) {
   if (CAP) {
-    const float two = -2.f * a.cap;
+    const F2 in = f2(a.cap_in, a.cap_in), one = f2(1.f, 1.f), two = f2(-2.f * a.cap, -2.f * a.cap), cap = f2(a.cap, a.cap);
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float t = rcp(1.f + ex2(__uint_as_float(r[e]) * a.cap_in));
-      if (KEEP) q[e] = __float_as_uint(t);
-      r[e] = __float_as_uint(fmaf(two, t, a.cap));
+    for (int e = 0; e < N; e += 2) {
+      float x, y;
+      split(mul2(f2u(r[e], r[e + 1]), in), x, y);
+      split(add2(f2(ex2(x), ex2(y)), one), x, y);
+      const F2 q = f2(rcp(x), rcp(y));
+      if (ch) {
+        split(mul2(mul2(f2(4.f, 4.f), q), fma2(q, f2(-1.f, -1.f), one)), x, y);
+        const __half2 h = __floats2half2_rn(x, y);
+        ch[e / 2] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+      split(fma2(two, q, cap), x, y);
+      r[e] = __float_as_uint(x);
+      r[e + 1] = __float_as_uint(y);
     }
   }
   if (BIAS == kBiasTable) {

@@ -311,14 +311,14 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
 #pragma unroll 1
         for (int pass = 0; pass < 2; ++pass) {
           const int c0 = cb * 64 + 32 * half + 16 * pass;
-          uint32_t s[16], t[16], q[16];
+          uint32_t s[16], t[16], ch[8];       // ch: 1 - tanh^2 of the cap, pairs of fp16
           tmem_ld16_issue(s_col + 16 * pass, s);
           tmem_ld16_issue(d_col + 16 * pass, t);
           tmem_ld16_wait(s);
           tmem_ld16_wait(t);
           // distance j - i: c0 + e - i (rows are queries) or i - c0 - e
           const int lo = KV ? i0 - c0 - 15 : c0 - i0 - 31;
-          shape_scores<16, BIAS, CAP, KV ? -1 : 1, true>(s, q, a, KV ? i - c0 : c0 - i, lo, lo + 46);
+          shape_scores<16, BIAS, CAP, KV ? -1 : 1>(s, ch, a, KV ? i - c0 : c0 - i, lo, lo + 46);
           // P = 2^(c x - lse) -> s, dS = P (dP - D) -> t
 #pragma unroll
           for (int e = 0; e < 16; e += 4) {
@@ -408,11 +408,14 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
             for (int e = 0; e < 8; ++e) w[e] = bf16_pair(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
             tmem_st8(s_col + 8 * pass, w);
           }
-          if (CAP) {           // 1 - tanh^2 = 4 q (1 - q); a masked score may have been NaN
+          if (CAP) {           // a masked score may have been NaN
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float z = __uint_as_float(q[e]), y = __uint_as_float(t[e]) * (4.f * z * (1.f - z));
-              t[e] = s[e] == 0u ? 0u : __float_as_uint(y);
+            for (int e = 0; e < 8; ++e) {
+              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&ch[e]));
+              float x, y;
+              split(mul2(f2u(t[2 * e], t[2 * e + 1]), f2(f.x, f.y)), x, y);
+              t[2 * e] = s[2 * e] == 0u ? 0u : __float_as_uint(x);
+              t[2 * e + 1] = s[2 * e + 1] == 0u ? 0u : __float_as_uint(y);
             }
           }
 #pragma unroll

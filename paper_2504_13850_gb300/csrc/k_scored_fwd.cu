@@ -290,8 +290,8 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
       tmem_ld32_issue(s_col + 32, r1);
       tmem_ld32_wait(r0);
       tmem_ld32_wait(r1);
-      shape_scores<32, BIAS, CAP, 1, false>(r0, r0, a, j0 - i, j0 - i0 - 31, j0 - i0 + 31);
-      shape_scores<32, BIAS, CAP, 1, false>(r1, r1, a, j0 + 32 - i, j0 - i0 + 1, j0 - i0 + 63);
+      shape_scores<32, BIAS, CAP, 1>(r0, nullptr, a, j0 - i, j0 - i0 - 31, j0 - i0 + 31);
+      shape_scores<32, BIAS, CAP, 1>(r1, nullptr, a, j0 + 32 - i, j0 - i0 + 1, j0 - i0 + 63);
       if ((BitList::word(masked, jb >> 5) >> (jb & 31)) & 1u) {
         mask_keys(r0, j0, lim, doc, id);
         mask_keys(r1, j0 + 32, lim, doc, id);
