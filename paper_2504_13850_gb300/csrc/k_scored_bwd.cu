@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
           tmem_ld16_wait(t);
           // distance j - i: c0 + e - i (rows are queries) or i - c0 - e
           const int lo = KV ? i0 - c0 - 15 : c0 - i0 - 31;
-          shape_scores<16, BIAS, CAP, KV ? -1 : 1>(s, ch, a, KV ? i - c0 : c0 - i, lo, lo + 46);
+          shape_scores<16, BIAS, CAP, KV ? -1 : 1, true>(s, ch, a, KV ? i - c0 : c0 - i, lo, lo + 46);
           // P = 2^(c x - lse) -> s, dS = P (dP - D) -> t
 #pragma unroll
           for (int e = 0; e < 16; e += 4) {

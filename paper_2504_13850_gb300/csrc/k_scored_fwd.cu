@@ -20,8 +20,8 @@
 // sums and bf16's exponent hold without loss.
 // Scores stay in raw units x with exponent factor c (scale * log2(e), or
 // log2(e) after a cap), so an uncapped, unbiased score costs half a packed FMA
-// and one exponential.  tanh(y) = 1 - 2 / (1 + e^2y) has an absolute error of a
-// few 2^-24, against the 2^-11 relative error of the hardware's tanh.
+// and one exponential.  The cap's tanh (shape_scores) has an absolute error of
+// a few 2^-24, against the 2^-11 relative error of the hardware's tanh.
 // The bias kind and the cap are template parameters: the branches cost
 // instruction fetches even when not taken.
 // Rounding: P~ to bf16 before its product, O once when stored.
@@ -290,8 +290,8 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
       tmem_ld32_issue(s_col + 32, r1);
       tmem_ld32_wait(r0);
       tmem_ld32_wait(r1);
-      shape_scores<32, BIAS, CAP, 1>(r0, nullptr, a, j0 - i, j0 - i0 - 31, j0 - i0 + 31);
-      shape_scores<32, BIAS, CAP, 1>(r1, nullptr, a, j0 + 32 - i, j0 - i0 + 1, j0 - i0 + 63);
+      shape_scores<32, BIAS, CAP, 1, false>(r0, nullptr, a, j0 - i, j0 - i0 - 31, j0 - i0 + 31);
+      shape_scores<32, BIAS, CAP, 1, false>(r1, nullptr, a, j0 + 32 - i, j0 - i0 + 1, j0 - i0 + 63);
       if ((BitList::word(masked, jb >> 5) >> (jb & 31)) & 1u) {
         mask_keys(r0, j0, lim, doc, id);
         mask_keys(r1, j0 + 32, lim, doc, id);
