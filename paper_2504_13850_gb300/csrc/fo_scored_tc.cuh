@@ -75,22 +75,38 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// The MMA warp's whole loop runs in a region that elect.sync guards: the
-// compiler then knows that one lane issues and keeps the operands in uniform
-// registers.  (From a branch on the lane index, or under a predicate, every
-// tcgen05.mma took 90 to 170 cycles whatever its size; a converged warp that
-// votes on its waits spent more time between the products than in them.)
+// The MMA warp runs converged and issues each run of products from a region
+// that elect.sync guards: the compiler then knows that one lane issues, and a
+// product costs one instruction besides its descriptors.  (From a branch on
+// the lane index every tcgen05.mma took 170 cycles whatever its size, and
+// inside a loop of the elected lane about 36 instructions: other lanes might
+// have been active there.)
 __device__ __forceinline__ bool elect_one() {
   uint32_t e = 0;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n @p mov.u32 %0, 1;\n}\n" : "+r"(e));
   return e != 0;
 }
-// tcgen05.mma with A in tensor memory: lane = row, each 32-bit column two
-// consecutive K elements (16 elements of K are 8 columns).
+// tcgen05.mma issued by one elected lane of a converged warp: both operands in
+// shared memory, or A in tensor memory (lane = row, each 32-bit column two
+// consecutive K elements, so 16 elements of K are 8 columns); and the commit.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n elect.sync _|q, 0xffffffff;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
+}
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
+      "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n elect.sync _|q, 0xffffffff;\n"
+      " @q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
       "r"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void commit_to(uint64_t* bar) {
+  asm volatile(
+      "{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n"
+      " @q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(smem_u32(bar))
       : "memory");
 }
 
@@ -117,10 +133,17 @@ struct Waits {
     atomicExch(err, code);
     dead = true;
   }
-  // The same for a whole warp, converged afterwards.
+  // The same for a whole converged warp, whose lanes agree on the outcome.
   __device__ __forceinline__ void on_warp(uint64_t* bar, uint32_t parity, int code) {
-    on(bar, parity, code);
-    __syncwarp();
+    if (dead || __all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;
+    const uint64_t t0 = global_ns();
+    while (true) {
+      for (int i = 0; i < 64; ++i)
+        if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;
+      if (__any_sync(0xffffffffu, global_ns() - t0 > 2000000000ull)) break;
+    }
+    atomicExch(err, code);
+    dead = true;
   }
 };
 

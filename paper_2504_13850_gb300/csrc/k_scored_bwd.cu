@@ -200,23 +200,23 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       }
     }
   } else if (warp == kMma) {
-    if (elect_one()) {
-      constexpr uint32_t id_s = instr_desc(64, false, false), id_a = instr_desc(DP, false, true);
-      const uint32_t x_at = smem_u32(sX), y_at = smem_u32(sY), ring_at = smem_u32(ring);
-      uint64_t* landed = any_bit(padded, words) ? clean : full;      // U and W have landed, without padding
-      int total = 0;
-      for (int w = 0; w < words; ++w) total += __popc(act[w]);
-      total *= groups;
-      int in = 0, in_slot = 0, in_phase = 0;           // the next step whose scores are formed
-      Ring<F::kBufs> in_buf, buf;
-      wait.on(xfull, 0, 33);
-      int slot = 0;
-      // one loop with one place for each product: kBufs steps of scores ahead
-      for (int n = -F::kBufs; n < total && !wait.dead; ++n) {
-        if (n >= 0) {
-          wait.on(&pfull[buf.at], buf.phase, 34);
-          tc_fence_after();
-          if (wait.dead) break;
+    constexpr uint32_t id_s = instr_desc(64, false, false), id_a = instr_desc(DP, false, true);
+    const uint32_t ring_at = smem_u32(ring);
+    const Operand<16> x(smem_u32(sX)), y(smem_u32(sY));
+    uint64_t* landed = any_bit(padded, words) ? clean : full;      // U and W have landed, without padding
+    int total = 0;
+    for (int w = 0; w < words; ++w) total += __popc(act[w]);
+    total *= groups;
+    int in = 0, in_slot = 0, in_phase = 0;           // the next step whose scores are formed
+    Ring<F::kBufs> in_buf, buf;
+    wait.on_warp(xfull, 0, 33);
+    int slot = 0;
+    // one loop with one place for each product: kBufs steps of scores ahead
+    for (int n = -F::kBufs; n < total && !wait.dead; ++n) {
+      if (n >= 0) {
+        wait.on_warp(&pfull[buf.at], buf.phase, 34);
+        tc_fence_after();
+        if (!wait.dead) {
           const uint32_t a = tmem + 128 * buf.at;
           const Operand<8192> u(ring_at + slot * F::kStage), w(ring_at + slot * F::kStage + F::kU);
           if (KV) {
@@ -228,32 +228,35 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
           for (int e = 0; e < 4; ++e)
             mma_ts(acc + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1), u.at(2048 * e), id_a,
                    e > 0 ? 1u : uint32_t(n));
-          mma_commit(&empty[slot]);
-          if (n + 1 == total) mma_commit(afull);
-          if (++slot == stages) slot = 0;
-          buf.step();
+          commit_to(&empty[slot]);
+          if (n + 1 == total) commit_to(afull);
         }
-        if (in < total) {
-          wait.on(&landed[in_slot], in_phase, 32);
-          tc_fence_after();
-          if (wait.dead) break;
+        __syncwarp();
+        if (++slot == stages) slot = 0;
+        buf.step();
+      }
+      if (in < total) {
+        // after the commit above: with kBufs stages, this is the one it frees
+        wait.on_warp(&landed[in_slot], in_phase, 32);
+        tc_fence_after();
+        if (!wait.dead) {
           const uint32_t d = tmem + 128 * in_buf.at;
-          const Operand<16> x(x_at), y(y_at), u(ring_at + in_slot * F::kStage), w(ring_at + in_slot * F::kStage + F::kU);
+          const Operand<16> u(ring_at + in_slot * F::kStage), w(ring_at + in_slot * F::kStage + F::kU);
 #pragma unroll
           for (int e = 0; e < DP / 16; ++e)
-            mma_f16(d, x.at((e >> 2) * 16384 + 32 * (e & 3)), u.at((e >> 2) * 8192 + 32 * (e & 3)), id_s, e > 0 ? 1u : 0u);
+            mma_ss(d, x.at((e >> 2) * 16384 + 32 * (e & 3)), u.at((e >> 2) * 8192 + 32 * (e & 3)), id_s, e > 0 ? 1u : 0u);
 #pragma unroll
           for (int e = 0; e < DP / 16; ++e)
-            mma_f16(d + 64, y.at((e >> 2) * 16384 + 32 * (e & 3)), w.at((e >> 2) * 8192 + 32 * (e & 3)), id_s,
+            mma_ss(d + 64, y.at((e >> 2) * 16384 + 32 * (e & 3)), w.at((e >> 2) * 8192 + 32 * (e & 3)), id_s,
                     e > 0 ? 1u : 0u);
-          mma_commit(&sfull[in_buf.at]);
-          in_buf.step();
-          ++in;
-          if (++in_slot == stages) in_slot = 0, in_phase ^= 1;
+          commit_to(&sfull[in_buf.at]);
         }
+        __syncwarp();
+        ++in;
+        in_buf.step();
+        if (++in_slot == stages) in_slot = 0, in_phase ^= 1;
       }
     }
-    __syncwarp();
   } else if (warp == kClean) {
     if (any_bit(padded, words)) {
       const int32_t* doc = p.doc + int64_t(b) * p.Lp;

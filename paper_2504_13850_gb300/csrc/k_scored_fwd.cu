@@ -202,67 +202,70 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
       }
     }
   } else if (warp == kMma) {
-    if (elect_one()) {
-      constexpr uint32_t id_s = instr_desc(128, false, false), id_o = instr_desc(DP, false, true);
-      const uint32_t ring_at = smem_u32(ring);
-      auto issue_s = [&](int t, int slot) {
-        const Operand<16> q(smem_u32(sQ) + t * F::kTileBytes), k(ring_at + slot * F::kTileBytes);
+    constexpr uint32_t id_s = instr_desc(128, false, false), id_o = instr_desc(DP, false, true);
+    const uint32_t ring_at = smem_u32(ring);
+    auto issue_s = [&](int t, int slot) {       // in an elected region
+      const Operand<16> q(smem_u32(sQ) + t * F::kTileBytes), k(ring_at + slot * F::kTileBytes);
 #pragma unroll
-        for (int e = 0; e < DP / 16; ++e) {
-          const uint32_t off = (e >> 2) * F::kSub + 32 * (e & 3);
-          mma_f16(tmem + 128 * t, q.at(off), k.at(off), id_s, e > 0 ? 1u : 0u);
-        }
-        mma_commit(&sfull[t]);
-      };
-      Bits list(act, act1, words);
-      uint64_t* landed = any_bit(padded, words) ? clean : full;      // V has landed, without padding
-      int cur = list.next();
-      bool on[2] = {list.on[0], list.on[1]};
-      uint32_t step[2] = {0, 0};
-      Ring<F::kStages, 2> k_at(0), v_at(1);
-      wait.on(qfull, 0, 22);
-      if (cur >= 0) {
-        wait.on(&full[0], 0, 23);
-        tc_fence_after();
-        if (!wait.dead) {
-          if (on[0]) issue_s(0, 0);
-          if (NT == 2 && on[1]) issue_s(1, 0);
-          mma_commit(&empty[0]);
-        }
-        k_at.step();
+      for (int e = 0; e < DP / 16; ++e) {
+        const uint32_t off = (e >> 2) * F::kSub + 32 * (e & 3);
+        mma_ss(tmem + 128 * t, q.at(off), k.at(off), id_s, e > 0 ? 1u : 0u);
       }
-      while (cur >= 0 && !wait.dead) {
-        const int nxt = list.next();
-        wait.on(&landed[v_at.at], v_at.phase, 24);
-        if (nxt >= 0) wait.on(&full[k_at.at], k_at.phase, 25);
-        const Operand<F::kSub> v(ring_at + v_at.at * F::kTileBytes);
+      commit_to(&sfull[t]);
+    };
+    Bits list(act, act1, words);
+    uint64_t* landed = any_bit(padded, words) ? clean : full;      // V has landed, without padding
+    int cur = list.next();
+    bool on[2] = {list.on[0], list.on[1]};
+    uint32_t step[2] = {0, 0};
+    Ring<F::kStages, 2> k_at(0), v_at(1);
+    wait.on_warp(qfull, 0, 22);
+    if (cur >= 0) {
+      wait.on_warp(&full[0], 0, 23);
+      tc_fence_after();
+      if (!wait.dead) {
+        if (on[0]) issue_s(0, 0);
+        if (NT == 2 && on[1]) issue_s(1, 0);
+        commit_to(&empty[0]);
+      }
+      __syncwarp();
+      k_at.step();
+    }
+    while (cur >= 0 && !wait.dead) {
+      const int nxt = list.next();
+      wait.on_warp(&landed[v_at.at], v_at.phase, 24);
+      if (nxt >= 0) wait.on_warp(&full[k_at.at], k_at.phase, 25);
+      const Operand<F::kSub> v(ring_at + v_at.at * F::kTileBytes);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+      for (int t = 0; t < NT; ++t) {
+        const bool then = nxt >= 0 && list.on[t];
+        if (on[t]) {
+          wait.on_warp(&pfull[t], step[t] & 1, 26);
+          tc_fence_after();
+        }
+        if (!wait.dead) {
           if (on[t]) {
-            wait.on(&pfull[t], step[t] & 1, 26);
-            tc_fence_after();
-            if (wait.dead) break;
 #pragma unroll
             for (int e = 0; e < 8; ++e)
               mma_ts(tmem + 128 * NT + DP * t, tmem + 128 * t + 64 * (e >> 2) + 8 * (e & 3), v.at(2048 * e), id_o,
                      e > 0 ? 1u : step[t]);
-            mma_commit(&ofull[t]);
-            ++step[t];
+            commit_to(&ofull[t]);
           }
-          if (nxt >= 0 && list.on[t] && !wait.dead) issue_s(t, k_at.at);
+          if (then) issue_s(t, k_at.at);
+          if (t == NT - 1) {
+            commit_to(&empty[v_at.at]);
+            if (nxt >= 0) commit_to(&empty[k_at.at]);
+          }
         }
-        if (!wait.dead) {
-          mma_commit(&empty[v_at.at]);
-          if (nxt >= 0) mma_commit(&empty[k_at.at]);
-        }
-        v_at.step();
-        k_at.step();
-        on[0] = list.on[0];
-        on[1] = list.on[1];
-        cur = nxt;
+        __syncwarp();
+        if (on[t]) ++step[t];
       }
+      v_at.step();
+      k_at.step();
+      on[0] = list.on[0];
+      on[1] = list.on[1];
+      cur = nxt;
     }
-    __syncwarp();
   } else if (warp < kTma) {
     const int t = warp / 8, half = warp / 4 % 2, quarter = warp % 4, row = 32 * quarter + lane;
     const int i0 = q0 + 128 * t + 32 * quarter, i = i0 + lane;
