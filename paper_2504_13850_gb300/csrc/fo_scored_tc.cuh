@@ -133,6 +133,11 @@ struct Waits {
     atomicExch(err, code);
     dead = true;
   }
+  // The same for the lanes of a warp of arithmetic, converged afterwards.
+  __device__ __forceinline__ void on_lanes(uint64_t* bar, uint32_t parity, int code) {
+    on(bar, parity, code);
+    __syncwarp();
+  }
   // The same for a whole converged warp, whose lanes agree on the outcome.
   __device__ __forceinline__ void on_warp(uint64_t* bar, uint32_t parity, int code) {
     if (dead || __all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;

@@ -47,6 +47,7 @@ struct BwdParams {
 constexpr int kThreads = 608;           // sixteen warps of arithmetic; TMA, MMA and padding warps
 constexpr int kTma = 16, kMma = 17, kClean = 18;
 constexpr int kMaxStages = 6;
+constexpr int kBlock = 0x3fff, kMasked = 0x4000, kPadded = 0x8000;   // entries of the list of blocks: kMaxLen / 64 = 2^14
 constexpr int kPatch = 32 * 17;         // floats of a warp's 32 x 16 patch, rows 17 apart
 
 template <int DP, bool KV>
@@ -57,11 +58,11 @@ struct Bwd {
   static constexpr int kStage = 2 * kU + (KV ? 1024 : 0);
   static constexpr int kBufs = KV && DP == 128 ? 2 : 3;     // TMEM buffers of S and dP; the sums follow
   static constexpr int kBars = 1 + 3 * kMaxStages + 2 * kBufs + 1;
-  // X, Y, stages, barriers (and the TMEM slot), bitmaps, row sums of dS, bias,
-  // table-gradient arrays
+  // X, Y, stages, barriers (and the TMEM slot and the number of blocks), the
+  // list of blocks, row sums of dS, bias, table-gradient arrays
+  __host__ __device__ static int list_bytes(int L) { return (L + 511) / 512 * 16; }
   static size_t smem(int L, int stages, bool table, bool grad, int reach) {
-    const int words = (L + 2047) / 2048;
-    size_t n = 1024 + 2 * kX + size_t(stages) * kStage + 8 * (kBars + 1) + size_t(4) * words * 3;
+    size_t n = 1024 + 2 * kX + size_t(stages) * kStage + 8 * (kBars + 1) + list_bytes(L);
     if (!KV) n += 4 * 4 * 128;
     if (table) n += 4 * kBiasFloats;
     if (grad) n += 4 * (16 * kPatch + 8 * dist_floats(reach)) + 2 * kMaxReach + 4;
@@ -77,14 +78,16 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   extern __shared__ __align__(1024) char smem_raw[];
   char* sm = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);    // 1024-byte aligned
   char *sX = sm, *sY = sm + F::kX, *ring = sm + 2 * F::kX;
-  const int stages = p.stages, words = (p.L + 2047) / 2048;
+  const int stages = p.stages;
   uint64_t* bars = reinterpret_cast<uint64_t*>(ring + stages * F::kStage);
   uint64_t *xfull = bars, *full = bars + 1, *empty = full + kMaxStages, *clean = empty + kMaxStages,
            *sfull = clean + kMaxStages, *pfull = sfull + F::kBufs, *afull = pfull + F::kBufs;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + F::kBars);
-  uint32_t* act = reinterpret_cast<uint32_t*>(bars + F::kBars + 1);
-  uint32_t *some = act + words, *padded = some + words;
-  float* rowsum = reinterpret_cast<float*>(padded + words);            // KV false: [4][128]
+  // blocks of 64 columns with allowed pairs, in ascending order: the index,
+  // with kMasked where some pairs are not allowed and kPadded where there is
+  // padding
+  uint16_t* list = reinterpret_cast<uint16_t*>(bars + F::kBars + 1);
+  float* rowsum = reinterpret_cast<float*>(reinterpret_cast<char*>(list) + F::list_bytes(p.L));   // KV false: [4][128]
   float* bias = rowsum + (KV ? 0 : 512);
   const bool grad = KV && BIAS == kBiasTable && p.dtable;
   float* patch = bias + (BIAS == kBiasTable ? kBiasFloats : 0);
@@ -131,11 +134,12 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     for (int e = threadIdx.x; e < 8 * nd; e += kThreads) dist[e] = 0.f;
     for (int e = threadIdx.x; e < 2 * p.reach + 1; e += kThreads) map[e] = p.map[e];
   }
-  {
+  if (warp == kClean) {
     int2 rd = make_int2(0, 0);
     if (blk) rd = doc_join(blk[r0 / 64], blk[r0 / 64 + 1]);
-    for (int w = warp; w < words; w += kThreads / 32) {
-      const int c0 = (32 * w + lane) * 64;
+    uint32_t n = 0, pads = 0;
+    for (int first = 0; first * 64 < p.L; first += 32) {
+      const int c0 = (first + lane) * 64;
       int cls = kScoredNone;
       bool pad = false;
       if (c0 < p.L) {
@@ -150,20 +154,21 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         pad = cd.x < 0 && cls != kScoredNone;
       }
       const uint32_t on = __ballot_sync(0xffffffffu, cls != kScoredNone);
-      const uint32_t mask = __ballot_sync(0xffffffffu, cls == kScoredSome);
-      const uint32_t pads = __ballot_sync(0xffffffffu, pad);
-      if (lane == 0) {
-        act[w] = on;
-        some[w] = mask;
-        padded[w] = pads;
-      }
+      pads |= __ballot_sync(0xffffffffu, pad);
+      if (cls != kScoredNone)
+        list[n + __popc(on & ((1u << lane) - 1))] =
+            uint16_t((first + lane) | (cls == kScoredSome ? kMasked : 0) | (pad ? kPadded : 0));
+      n += __popc(on);
     }
+    if (lane == 0) tslot[1] = n | (pads ? 0x80000000u : 0u);
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   // S and dP of buffer k: columns 128 k and 128 k + 64; sums at `acc` and acc + DP
   const uint32_t tmem = *tslot, acc = tmem + 128 * F::kBufs;
+  const int count = int(tslot[1] & 0x7fffffffu);
+  const bool any_padding = tslot[1] >> 31;
   pdl_trigger();
   Waits wait(&g_err);
 
@@ -176,9 +181,9 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       }
       int it = 0;
       for (int g = 0; g < groups && !wait.dead; ++g) {
-        Bits list(act, act, words);
         const int64_t stat = (int64_t(b) * p.H + h0 + g) * p.Lp;
-        for (int cb = list.next(); cb >= 0; cb = list.next(), ++it) {
+        for (int k = 0; k < count; ++k, ++it) {
+          const int cb = list[k] & kBlock;
           const int slot = it % stages;
           if (it >= stages) wait.on(&empty[slot], (it / stages - 1) & 1, 31);
           if (wait.dead) break;
@@ -203,10 +208,8 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     constexpr uint32_t id_s = instr_desc(64, false, false), id_a = instr_desc(DP, false, true);
     const uint32_t ring_at = smem_u32(ring);
     const Operand<16> x(smem_u32(sX)), y(smem_u32(sY));
-    uint64_t* landed = any_bit(padded, words) ? clean : full;      // U and W have landed, without padding
-    int total = 0;
-    for (int w = 0; w < words; ++w) total += __popc(act[w]);
-    total *= groups;
+    uint64_t* landed = any_padding ? clean : full;      // U and W have landed, without padding
+    const int total = count * groups;
     int in = 0, in_slot = 0, in_phase = 0;           // the next step whose scores are formed
     Ring<F::kBufs> in_buf, buf;
     wait.on_warp(xfull, 0, 33);
@@ -258,14 +261,14 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       }
     }
   } else if (warp == kClean) {
-    if (any_bit(padded, words)) {
+    if (any_padding) {
       const int32_t* doc = p.doc + int64_t(b) * p.Lp;
       int slot = 0, phase = 0;
       for (int g = 0; g < groups; ++g) {
-        Bits list(act, act, words);
-        for (int cb = list.next(); cb >= 0 && !wait.dead; cb = list.next()) {
+        for (int k = 0; k < count && !wait.dead; ++k) {
+          const int cb = list[k] & kBlock;
           wait.on_warp(&full[slot], phase, 38);
-          if (bit_of(padded, cb)) {
+          if (list[k] & kPadded) {
             clear_padding(ring + slot * F::kStage, 64, DP / 64, doc + cb * 64);
             if (KV) clear_padding(ring + slot * F::kStage + F::kU, 64, DP / 64, doc + cb * 64);
           }
@@ -291,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     float* my_patch = patch + warp * kPatch;
     float* my_dist = dist + (4 * side + quarter) * nd;
     const int pair = 1 + 4 * side + quarter;
-    int n = 0, slot = 0, phase = 0;          // step, its stage in shared memory
+    int slot = side, phase = 0;              // this side's stage in shared memory
     Ring<F::kBufs, 2> buf(side);             // this side's buffer
     for (int g = 0; g < groups; ++g) {
       const Shape a = shape_of(p, h0 + g, unit, bias);
@@ -300,17 +303,15 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         load_bias(bias, p, h0 + g, 1.f / unit, threadIdx.x, 512);
         asm volatile("bar.sync 9, 512;" ::: "memory");
       }
-      BitList list(act, words);
-      for (int cb = list.next(); cb >= 0; cb = list.next()) {
-        const int my_slot = slot, my_phase = phase;
-        if (++slot == stages) slot = 0, phase ^= 1;
-        if ((n++ & 1) != side) continue;
-        const bool mask = bit_of(some, cb);
+      for (int k = (side + g * count) & 1; k < count; k += 2) {      // every other step of the whole walk
+        const uint32_t entry = list[k];
+        const int cb = entry & kBlock;
+        const bool mask = entry & kMasked;
         const uint32_t s_col = tmem + lanes + 128 * buf.at + 32 * half, d_col = s_col + 64;
-        if (KV) wait.on_warp(&full[my_slot], my_phase, 35);        // its statistics
-        wait.on_warp(&sfull[buf.at], buf.phase, 36);
+        if (KV) wait.on_lanes(&full[slot], phase, 35);              // its statistics
+        wait.on_lanes(&sfull[buf.at], buf.phase, 36);
         tc_fence_after();
-        const uint32_t stats = smem_u32(ring + my_slot * F::kStage + 2 * F::kU) + 128 * half;
+        const uint32_t stats = smem_u32(ring + slot * F::kStage + 2 * F::kU) + 128 * half;
 #pragma unroll 1
         for (int pass = 0; pass < 2; ++pass) {
           const int c0 = cb * 64 + 32 * half + 16 * pass;
@@ -429,6 +430,8 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         tc_fence_before();
         arrive_warp(&pfull[buf.at]);
         buf.step();
+        slot += 2;
+        if (slot >= stages) slot -= stages, phase ^= 1;
       }
       if (grad) {
         // this head's sums by distance -> buckets -> its partial gradient
@@ -473,8 +476,8 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         p.delta[stat] = row_d - ((z[0] + z[128]) + (z[256] + z[384]));
       }
     }
-    if (n > 0) {
-      wait.on_warp(afull, 0, 37);
+    if (count > 0) {
+      wait.on_lanes(afull, 0, 37);
       tc_fence_after();
     }
     // each of the four warps of a row group stores a quarter of the columns
@@ -487,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       for (int g = 0; g < DP / 64; ++g) {
         const int col = DP / 4 * (2 * side + half) + 16 * g;
         uint32_t a[16];
-        if (n > 0) {
+        if (count > 0) {
           tmem_ld16_issue(acc + lanes + o * DP + col, a);
           tmem_ld16_wait(a);
         } else {
@@ -519,6 +522,7 @@ template <int DP, bool KV>
 struct Launch {
   BwdParams& bp;
   cudaStream_t st;
+  bool* ok;
   template <int BIAS, bool CAP>
   cudaError_t operator()() const {
     using F = Bwd<DP, KV>;
@@ -526,6 +530,10 @@ struct Launch {
     int stages = kMaxStages;
     auto need = [&](int n) { return F::smem(bp.s.L, n, BIAS == kBiasTable, grad, bp.s.reach); };
     while (stages > F::kBufs && need(stages) > kSmemLimit) --stages;   // kBufs steps are in flight: fewer would not do
+    if (need(stages) > kSmemLimit) {      // the list of a sequence of half a million tokens and more
+      *ok = false;
+      return cudaSuccess;
+    }
     bp.s.stages = stages;
     const size_t smem = need(stages);
     auto k = scored_bwd_tc_k<DP, KV, BIAS, CAP>;
@@ -547,9 +555,9 @@ cudaError_t scored_bwd_tc(const ScoredParams& p, cudaStream_t st, bool* ok) {
         scored_map(&k.x, p.k, p, p.KV, 128) && scored_map(&k.y, p.v, p, p.KV, 128) &&
         scored_map(&k.u, p.q, p, p.H, 64) && scored_map(&k.w, p.dout, p, p.H, 64);
   if (!*ok) return cudaSuccess;
-  cudaError_t e = p.D <= 64 ? with_shape(p, Launch<64, false>{q, st}) : with_shape(p, Launch<128, false>{q, st});
-  if (e != cudaSuccess) return e;
-  return p.D <= 64 ? with_shape(p, Launch<64, true>{k, st}) : with_shape(p, Launch<128, true>{k, st});
+  cudaError_t e = p.D <= 64 ? with_shape(p, Launch<64, false>{q, st, ok}) : with_shape(p, Launch<128, false>{q, st, ok});
+  if (e != cudaSuccess || !*ok) return e;
+  return p.D <= 64 ? with_shape(p, Launch<64, true>{k, st, ok}) : with_shape(p, Launch<128, true>{k, st, ok});
 }
 
 cudaError_t scored_bwd_error(int* word) { return cudaMemcpyFromSymbol(word, g_err, sizeof(int)); }

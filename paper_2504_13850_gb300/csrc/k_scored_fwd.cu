@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
     BitList list(act + t * words, words);
     for (int jb = list.next(); jb >= 0; jb = list.next(), ++step) {
       const int j0 = jb * 128 + 64 * half, flip = (step & 1) * 256 * NT;
-      wait.on_warp(&sfull[t], step & 1, 27);
+      wait.on_lanes(&sfull[t], step & 1, 27);
       tc_fence_after();
       uint32_t r0[32], r1[32];
       tmem_ld32_issue(s_col, r0);
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
         const bool need = (now - m) * c > 8.f;
         if (__any_sync(0xffffffffu, need)) {
           const float keep = need ? ex2((m - now) * c) : 1.f;
-          wait.on_warp(&ofull[t], (step - 1) & 1, 28);
+          wait.on_lanes(&ofull[t], (step - 1) & 1, 28);
           tc_fence_after();
 #pragma unroll 1
           for (int g = 0; g < DP / 32; ++g) {
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
     sum = half ? theirs + sum : sum + theirs;
     const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);     // a NaN row stays NaN
     if (step > 0) {
-      wait.on_warp(&ofull[t], (step - 1) & 1, 29);
+      wait.on_lanes(&ofull[t], (step - 1) & 1, 29);
       tc_fence_after();
     }
     if (half == 0 && i < p.L) p.lse[int64_t(bh) * p.L + i] = sum == 0.f ? -INFINITY : m * c * kLn2 + logf(sum);
