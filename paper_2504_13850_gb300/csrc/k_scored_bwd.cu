@@ -212,14 +212,14 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     const int total = count * groups;
     int in = 0, in_slot = 0, in_phase = 0;           // the next step whose scores are formed
     Ring<F::kBufs> in_buf, buf;
-    wait.on_warp(xfull, 0, 33);
+    wait.on_lanes(xfull, 0, 33);
     int slot = 0;
     // one loop with one place for each product: kBufs steps of scores ahead
-    for (int n = -F::kBufs; n < total && !wait.dead; ++n) {
+    for (int n = -F::kBufs; n < total; ++n) {
       if (n >= 0) {
-        wait.on_warp(&pfull[buf.at], buf.phase, 34);
+        wait.on_lanes(&pfull[buf.at], buf.phase, 34);
         tc_fence_after();
-        if (!wait.dead) {
+        {
           const uint32_t a = tmem + 128 * buf.at;
           const Operand<8192> u(ring_at + slot * F::kStage), w(ring_at + slot * F::kStage + F::kU);
           if (KV) {
@@ -234,15 +234,14 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
           commit_to(&empty[slot]);
           if (n + 1 == total) commit_to(afull);
         }
-        __syncwarp();
         if (++slot == stages) slot = 0;
         buf.step();
       }
       if (in < total) {
         // after the commit above: with kBufs stages, this is the one it frees
-        wait.on_warp(&landed[in_slot], in_phase, 32);
+        wait.on_lanes(&landed[in_slot], in_phase, 32);
         tc_fence_after();
-        if (!wait.dead) {
+        {
           const uint32_t d = tmem + 128 * in_buf.at;
           const Operand<16> u(ring_at + in_slot * F::kStage), w(ring_at + in_slot * F::kStage + F::kU);
 #pragma unroll
@@ -254,11 +253,12 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
                     e > 0 ? 1u : 0u);
           commit_to(&sfull[in_buf.at]);
         }
-        __syncwarp();
         ++in;
         in_buf.step();
         if (++in_slot == stages) in_slot = 0, in_phase ^= 1;
       }
+      // off the waits' path; what was issued after one gave up is void anyway
+      if (__any_sync(0xffffffffu, wait.dead)) break;
     }
   } else if (warp == kClean) {
     if (any_padding) {

@@ -219,31 +219,28 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
     bool on[2] = {list.on[0], list.on[1]};
     uint32_t step[2] = {0, 0};
     Ring<F::kStages, 2> k_at(0), v_at(1);
-    wait.on_warp(qfull, 0, 22);
+    wait.on_lanes(qfull, 0, 22);
     if (cur >= 0) {
-      wait.on_warp(&full[0], 0, 23);
+      wait.on_lanes(&full[0], 0, 23);
       tc_fence_after();
-      if (!wait.dead) {
-        if (on[0]) issue_s(0, 0);
-        if (NT == 2 && on[1]) issue_s(1, 0);
-        commit_to(&empty[0]);
-      }
-      __syncwarp();
+      if (on[0]) issue_s(0, 0);
+      if (NT == 2 && on[1]) issue_s(1, 0);
+      commit_to(&empty[0]);
       k_at.step();
     }
-    while (cur >= 0 && !wait.dead) {
+    while (cur >= 0) {
       const int nxt = list.next();
-      wait.on_warp(&landed[v_at.at], v_at.phase, 24);
-      if (nxt >= 0) wait.on_warp(&full[k_at.at], k_at.phase, 25);
+      wait.on_lanes(&landed[v_at.at], v_at.phase, 24);
+      if (nxt >= 0) wait.on_lanes(&full[k_at.at], k_at.phase, 25);
       const Operand<F::kSub> v(ring_at + v_at.at * F::kTileBytes);
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const bool then = nxt >= 0 && list.on[t];
         if (on[t]) {
-          wait.on_warp(&pfull[t], step[t] & 1, 26);
+          wait.on_lanes(&pfull[t], step[t] & 1, 26);
           tc_fence_after();
         }
-        if (!wait.dead) {
+        {
           if (on[t]) {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
@@ -257,7 +254,6 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
             if (nxt >= 0) commit_to(&empty[k_at.at]);
           }
         }
-        __syncwarp();
         if (on[t]) ++step[t];
       }
       v_at.step();
@@ -265,6 +261,8 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
       on[0] = list.on[0];
       on[1] = list.on[1];
       cur = nxt;
+      // off the waits' path; what was issued after one gave up is void anyway
+      if (__any_sync(0xffffffffu, wait.dead)) break;
     }
   } else if (warp < kTma) {
     const int t = warp / 8, half = warp / 4 % 2, quarter = warp % 4, row = 32 * quarter + lane;
