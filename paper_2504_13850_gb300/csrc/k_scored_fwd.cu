@@ -111,7 +111,18 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
   const int tiles = (p.L + 128 * NT - 1) / (128 * NT), bh = blockIdx.x % (p.B * p.H);
   const int q0 = (tiles - 1 - int(blockIdx.x / (p.B * p.H))) * 128 * NT;   // the longest causal rows first
   const int b = bh / p.H, h = bh % p.H, kh = h / p.G;
-  if (threadIdx.x == 0) {
+  // one tile walks at most one block, which the TMA warp can clear itself
+  constexpr int kTma = 8 * NT, kMma = 8 * NT + 1, kClean = NT == 2 ? kMma + 1 : kTma;
+  if (warp == kMma) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tslot)),
+                 "r"(F::kCols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  if (warp == kTma && lane == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&fp.q)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&fp.k)) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&fp.v)) : "memory");
     mbar_init(qfull, 1);
     for (int e = 0; e < F::kStages; ++e) {
       mbar_init(&full[e], 1);
@@ -125,20 +136,14 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  // one tile walks at most one block, which the TMA warp can clear itself
-  constexpr int kTma = 8 * NT, kMma = 8 * NT + 1, kClean = NT == 2 ? kMma + 1 : kTma;
-  if (warp == kMma) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tslot)),
-                 "r"(F::kCols)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  if (warp == kTma && lane == 0) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&fp.q)) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&fp.k)) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&fp.v)) : "memory");
-  }
+  __syncwarp();
   pdl_wait();
+  if (warp == kTma && lane == 0) {       // the queries, while the rest is prepared
+    mbar_expect_tx(qfull, NT * F::kTileBytes);
+    for (int t = 0; t < NT; ++t)
+      for (int s = 0; s < DP / 64; ++s)
+        tma_4d(sQ + t * F::kTileBytes + s * F::kSub, &fp.q, qfull, 64 * s, q0 + 128 * t, h, b);
+  }
   // score units: raw products without a cap, natural ones after it
   const float unit = CAP ? 1.f : p.scale, c = unit * kLog2e;
   const int pf = p.prefix ? p.prefix[b] : 0;
@@ -180,10 +185,6 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
 
   if (warp == kTma) {
     if (lane == 0) {
-      mbar_expect_tx(qfull, NT * F::kTileBytes);
-      for (int t = 0; t < NT; ++t)
-        for (int s = 0; s < DP / 64; ++s)
-          tma_4d(sQ + t * F::kTileBytes + s * F::kSub, &fp.q, qfull, 64 * s, q0 + 128 * t, h, b);
       Bits list(act, act1, words);
       Ring<F::kStages> at;
       int it = 0;
