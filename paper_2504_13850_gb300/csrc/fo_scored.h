@@ -48,7 +48,7 @@ struct ScoredParams {
   void* dtable;
   int B, L, Lp, H, KV, G, D;
   int causal, buckets, reach;
-  int stages;              // shared-memory stages of the backward tensor-core kernels
+  int stages;              // shared-memory stages of the backward tensor-core kernels; see work_of_block for the others
   float scale, cap;
   uint8_t map[2 * kMaxReach + 1];
 };

@@ -325,17 +325,28 @@ __device__ __forceinline__ void store_rows(const Strided& t, const ScoredParams&
   }
 }
 
+// Which (tile, sequence and head) a block works on: the longest causal tiles
+// first, so that the hardware's order of dispatch balances them.  When two
+// blocks per SM hold the whole grid there is no later dispatch, and the second
+// block of each SM comes in the opposite order, a short one to the longest
+// (2 x 1000 causal tokens, 8 heads of 64: forward 143 -> 127 us).
+__device__ __forceinline__ unsigned work_of_block(int sms) {
+  const unsigned n = gridDim.x, x = blockIdx.x;
+  return sms > 0 && x >= unsigned(sms) ? n - 1 - (x - unsigned(sms)) : x;
+}
+
 // ----------------------------------------------------------------- forward
 template <typename T, int NC>
-__global__ void __launch_bounds__(kThreads) scored_fwd_k(const __grid_constant__ ScoredParams p) {
+__global__ void __launch_bounds__(kThreads, NC <= 4 ? 2 : 1) scored_fwd_k(const __grid_constant__ ScoredParams p) {
   extern __shared__ __align__(16) float sm[];
   constexpr int W = 16 * NC;
   constexpr int kTile = W * kT;
   float *Q = sm, *KVs = Q + kTile, *P = KVs + 4 * kTile, *bias = P + kT * kT;    // KVs: two pairs of K and V
   pdl_wait();
   pdl_trigger();
-  const int tiles = (p.L + kT - 1) / kT, bh = blockIdx.x % (p.B * p.H);
-  const int q0 = (tiles - 1 - int(blockIdx.x / (p.B * p.H))) * kT;   // the longest causal rows first
+  const unsigned work = work_of_block(p.stages);
+  const int tiles = (p.L + kT - 1) / kT, bh = work % (p.B * p.H);
+  const int q0 = (tiles - 1 - int(work / (p.B * p.H))) * kT;
   const int b = bh / p.H, h = bh % p.H, kh = h / p.G;
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
   Pair pc = pair_of(p, b, h);
@@ -420,7 +431,7 @@ __global__ void __launch_bounds__(kThreads) scored_fwd_k(const __grid_constant__
 // the group (U = Q, W = dO): dV = sum P^T W, dK = sum dS^T U, and the partial
 // table gradients of this tile.
 template <typename T, int NC, bool KV>
-__global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__ ScoredParams p) {
+__global__ void __launch_bounds__(kThreads, NC <= (KV ? 2 : 4) ? 2 : 1) scored_bwd_k(const __grid_constant__ ScoredParams p) {
   extern __shared__ __align__(16) float sm[];
   constexpr int WD = 16 * NC;
   constexpr int kTile = WD * kT;
@@ -431,8 +442,9 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
   pdl_wait();
   pdl_trigger();
   const int heads = KV ? p.KV : p.H, tiles = (p.L + kT - 1) / kT;
-  const int bh = blockIdx.x % (p.B * heads), slot = int(blockIdx.x / (p.B * heads));
-  const int tile = KV ? slot : tiles - 1 - slot, r0 = tile * kT;     // the longest causal tiles first
+  const unsigned work = work_of_block(p.stages);
+  const int bh = work % (p.B * heads), slot = int(work / (p.B * heads));
+  const int tile = KV ? slot : tiles - 1 - slot, r0 = tile * kT;
   const int b = bh / heads, h0 = KV ? (bh % heads) * p.G : bh % heads, kh = h0 / p.G;
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
   const bool grad = KV && p.dtable;
@@ -559,26 +571,36 @@ __global__ void __launch_bounds__(kThreads) scored_bwd_k(const __grid_constant__
   }
 }
 
+// The argument of work_of_block: the number of SMs when all `blocks` are
+// resident two to an SM, else 0.
+int paired(int64_t blocks, int NC) {
+  const int sms = elementwise_blocks(INT64_MAX / 2, kThreads) / 8;
+  return NC <= 4 && blocks > sms && blocks <= 2 * sms ? sms : 0;
+}
+
 template <typename T, int NC>
-cudaError_t forward_width(const ScoredParams& p, cudaStream_t st) {
+cudaError_t forward_width(ScoredParams p, cudaStream_t st) {
   const int64_t tiles = ceil_div(p.L, kT);
   const size_t smem = (size_t(5 * 16 * NC * kT) + kT * kT + (p.table ? 2 * kMaxReach + 4 : 0)) * sizeof(float);
   static std::atomic<bool> allowed[kMaxDevices];
   const cudaError_t e = allow_smem(scored_fwd_k<T, NC>, allowed);
   if (e != cudaSuccess) return e;
+  p.stages = paired(tiles * p.B * p.H, NC);
   return launch_k(scored_fwd_k<T, NC>, dim3(unsigned(tiles * p.B * p.H)), dim3(kThreads), smem, st, p);
 }
 template <typename T, int NC>
-cudaError_t backward_width(const ScoredParams& p, cudaStream_t st) {
+cudaError_t backward_width(ScoredParams p, cudaStream_t st) {
   const int64_t tiles = ceil_div(p.L, kT);
   const size_t smem =
       (size_t(6 * 16 * NC * kT) + kT * kT + (p.table ? 2 * (2 * kMaxReach + 4) + 256 : 0)) * sizeof(float);
   static std::atomic<bool> allowed[2][kMaxDevices];
   cudaError_t e = allow_smem(scored_bwd_k<T, NC, false>, allowed[0]);
   if (e == cudaSuccess) e = allow_smem(scored_bwd_k<T, NC, true>, allowed[1]);
-  if (e == cudaSuccess)
-    e = launch_k(scored_bwd_k<T, NC, false>, dim3(unsigned(tiles * p.B * p.H)), dim3(kThreads), smem, st, p);
   if (e != cudaSuccess) return e;
+  p.stages = paired(tiles * p.B * p.H, NC);
+  e = launch_k(scored_bwd_k<T, NC, false>, dim3(unsigned(tiles * p.B * p.H)), dim3(kThreads), smem, st, p);
+  if (e != cudaSuccess) return e;
+  p.stages = paired(tiles * p.B * p.KV, NC <= 2 ? NC : 8);      // wider ones take an SM each
   return launch_k(scored_bwd_k<T, NC, true>, dim3(unsigned(tiles * p.B * p.KV)), dim3(kThreads), smem, st, p);
 }
 // Accumulator columns per thread: 16 NC >= head width.
