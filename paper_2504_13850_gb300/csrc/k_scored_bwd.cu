@@ -24,7 +24,10 @@
 // D = dO . O carries the rounding of O, which would leave each row's dS with a
 // sum of -dD instead of 0, most of it in whichever bucket holds most keys: the
 // query pass, launched first, sums its dS rows in fp32 and adds the sum to D,
-// so that dK and the table gradient come from the exact D.
+// so that dK and the table gradient come from the exact D.  Where two blocks
+// are all that a tile walks, as in sequences of up to 128 tokens, whose few
+// keys feel the error most, it sums P dP over the row first and dQ has the
+// exact D too.
 // The table gradient sums dS in fp32 by distance: each warp turns 32 x 16
 // patches through shared memory so that a lane sums a diagonal, into arrays by
 // distance shared by the two warps of a row group, one after the other;
@@ -56,14 +59,15 @@ struct Bwd {
   static constexpr int kU = DP / 64 * 8192;         // 64 rows
   static constexpr int kStats = KV ? 512 : 0;       // lse and D of 64 queries
   static constexpr int kStage = 2 * kU + (KV ? 1024 : 0);
+  static constexpr bool kSplit = KV && DP == 128;          // P handed over before dS
   static constexpr int kBufs = KV && DP == 128 ? 2 : 3;     // TMEM buffers of S and dP; the sums follow
-  static constexpr int kBars = 1 + 3 * kMaxStages + 2 * kBufs + 1;
+  static constexpr int kBars = 1 + 3 * kMaxStages + 4 * kBufs + 1;
   // X, Y, stages, barriers (and the TMEM slot and the number of blocks), the
   // list of blocks, row sums of dS, bias, table-gradient arrays
   __host__ __device__ static int list_bytes(int L) { return (L + 511) / 512 * 16; }
   static size_t smem(int L, int stages, bool table, bool grad, int reach) {
     size_t n = 1024 + 2 * kX + size_t(stages) * kStage + 8 * (kBars + 1) + list_bytes(L);
-    if (!KV) n += 4 * 4 * 128;
+    if (!KV) n += 4 * 8 * 128;
     if (table) n += 4 * kBiasFloats;
     if (grad) n += 4 * (16 * kPatch + 8 * dist_floats(reach)) + 2 * kMaxReach + 4;
     return n;
@@ -81,14 +85,15 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   const int stages = p.stages;
   uint64_t* bars = reinterpret_cast<uint64_t*>(ring + stages * F::kStage);
   uint64_t *xfull = bars, *full = bars + 1, *empty = full + kMaxStages, *clean = empty + kMaxStages,
-           *sfull = clean + kMaxStages, *pfull = sfull + F::kBufs, *afull = pfull + F::kBufs;
+           *sfull = clean + kMaxStages, *pfull = sfull + F::kBufs, *dfull = pfull + F::kBufs,
+           *tfull = dfull + F::kBufs, *afull = tfull + F::kBufs;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + F::kBars);
   // blocks of 64 columns with allowed pairs, in ascending order: the index,
   // with kMasked where some pairs are not allowed and kPadded where there is
   // padding
   uint16_t* list = reinterpret_cast<uint16_t*>(bars + F::kBars + 1);
-  float* rowsum = reinterpret_cast<float*>(reinterpret_cast<char*>(list) + F::list_bytes(p.L));   // KV false: [4][128]
-  float* bias = rowsum + (KV ? 0 : 512);
+  float* rowsum = reinterpret_cast<float*>(reinterpret_cast<char*>(list) + F::list_bytes(p.L));   // KV false: [2][4][128]
+  float* bias = rowsum + (KV ? 0 : 1024);
   const bool grad = KV && BIAS == kBiasTable && p.dtable;
   float* patch = bias + (BIAS == kBiasTable ? kBiasFloats : 0);
   float* dist = patch + 16 * kPatch;
@@ -109,7 +114,9 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     }
     for (int e = 0; e < F::kBufs; ++e) {
       mbar_init(&sfull[e], 1);
-      mbar_init(&pfull[e], 8);           // one arrival per warp
+      mbar_init(&pfull[e], 8);           // P written (one arrival per warp)
+      mbar_init(&dfull[e], 1);
+      mbar_init(&tfull[e], 8);           // dS written
     }
     mbar_init(afull, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -217,23 +224,25 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     // one loop with one place for each product: kBufs steps of scores ahead
     for (int n = -F::kBufs; n < total; ++n) {
       if (n >= 0) {
-        wait.on_lanes(&pfull[buf.at], buf.phase, 34);
-        tc_fence_after();
-        {
-          const uint32_t a = tmem + 128 * buf.at;
-          const Operand<8192> u(ring_at + slot * F::kStage), w(ring_at + slot * F::kStage + F::kU);
-          if (KV) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              mma_ts(acc, a + 32 * (e >> 1) + 8 * (e & 1), w.at(2048 * e), id_a, e > 0 ? 1u : uint32_t(n));
-          }
+        const uint32_t a = tmem + 128 * buf.at;
+        const Operand<8192> u(ring_at + slot * F::kStage), w(ring_at + slot * F::kStage + F::kU);
+        if (KV) {
+          wait.on_lanes(F::kSplit ? &pfull[buf.at] : &tfull[buf.at], buf.phase, 34);
+          tc_fence_after();
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            mma_ts(acc + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1), u.at(2048 * e), id_a,
-                   e > 0 ? 1u : uint32_t(n));
-          commit_to(&empty[slot]);
-          if (n + 1 == total) commit_to(afull);
+            mma_ts(acc, a + 32 * (e >> 1) + 8 * (e & 1), w.at(2048 * e), id_a, e > 0 ? 1u : uint32_t(n));
         }
+        if (!KV || F::kSplit) {
+          wait.on_lanes(&tfull[buf.at], buf.phase, 39);
+          tc_fence_after();
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          mma_ts(acc + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1), u.at(2048 * e), id_a,
+                 e > 0 ? 1u : uint32_t(n));
+        commit_to(&empty[slot]);
+        if (n + 1 == total) commit_to(afull);
         if (++slot == stages) slot = 0;
         buf.step();
       }
@@ -241,18 +250,17 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         // after the commit above: with kBufs stages, this is the one it frees
         wait.on_lanes(&landed[in_slot], in_phase, 32);
         tc_fence_after();
-        {
-          const uint32_t d = tmem + 128 * in_buf.at;
-          const Operand<16> u(ring_at + in_slot * F::kStage), w(ring_at + in_slot * F::kStage + F::kU);
+        const uint32_t d = tmem + 128 * in_buf.at;
+        const Operand<16> u(ring_at + in_slot * F::kStage), w(ring_at + in_slot * F::kStage + F::kU);
 #pragma unroll
-          for (int e = 0; e < DP / 16; ++e)
-            mma_ss(d, x.at((e >> 2) * 16384 + 32 * (e & 3)), u.at((e >> 2) * 8192 + 32 * (e & 3)), id_s, e > 0 ? 1u : 0u);
+        for (int e = 0; e < DP / 16; ++e)
+          mma_ss(d, x.at((e >> 2) * 16384 + 32 * (e & 3)), u.at((e >> 2) * 8192 + 32 * (e & 3)), id_s, e > 0 ? 1u : 0u);
+        commit_to(&sfull[in_buf.at]);
 #pragma unroll
-          for (int e = 0; e < DP / 16; ++e)
-            mma_ss(d + 64, y.at((e >> 2) * 16384 + 32 * (e & 3)), w.at((e >> 2) * 8192 + 32 * (e & 3)), id_s,
-                    e > 0 ? 1u : 0u);
-          commit_to(&sfull[in_buf.at]);
-        }
+        for (int e = 0; e < DP / 16; ++e)
+          mma_ss(d + 64, y.at((e >> 2) * 16384 + 32 * (e & 3)), w.at((e >> 2) * 8192 + 32 * (e & 3)), id_s,
+                 e > 0 ? 1u : 0u);
+        commit_to(&dfull[in_buf.at]);
         ++in;
         in_buf.step();
         if (++in_slot == stages) in_slot = 0, in_phase ^= 1;
@@ -287,7 +295,8 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     // that are keys allow columns from `edge` on (none past the end)
     const int edge = KV ? (i >= p.L ? INT32_MAX : p.causal && i >= pf ? i : 0) : min(p.causal ? max(i + 1, pf) : p.L, p.L);
     const int64_t stat = (int64_t(b) * p.H + h0) * p.Lp + i;
-    const float row_lse = KV ? 0.f : p.lse2[stat], row_d = KV ? 0.f : p.delta[stat];
+    const float row_lse = KV ? 0.f : p.lse2[stat];
+    float row_d = KV ? 0.f : p.delta[stat];
     const F2 c2 = f2(c, c);
     F2 eps = f2(0.f, 0.f);                 // KV false: sum of this thread's dS
     float lo_sum = 0.f, hi_sum = 0.f;      // table gradient beyond the reach
@@ -295,6 +304,13 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     float* my_dist = dist + (4 * side + quarter) * nd;
     const int pair = 1 + 4 * side + quarter;
     int slot = side, phase = 0;              // this side's stage in shared memory
+    // the sum of a value over the four threads of a row (all warps of arithmetic)
+    auto row_total = [&](float d) {
+      float* z = rowsum + 512 + 32 * quarter + lane;
+      z[128 * (2 * side + half)] = d;
+      asm volatile("bar.sync 9, 512;" ::: "memory");
+      return (z[0] + z[128]) + (z[256] + z[384]);
+    };
     Ring<F::kBufs, 2> buf(side);             // this side's buffer
     for (int g = 0; g < groups; ++g) {
       const Shape a = shape_of(p, h0 + g, unit, bias);
@@ -312,53 +328,92 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         wait.on_lanes(&sfull[buf.at], buf.phase, 36);
         tc_fence_after();
         const uint32_t stats = smem_u32(ring + slot * F::kStage + 2 * F::kU) + 128 * half;
-#pragma unroll 1
-        for (int pass = 0; pass < 2; ++pass) {
-          const int c0 = cb * 64 + 32 * half + 16 * pass;
-          uint32_t s[16], t[16], ch[8];       // ch: 1 - tanh^2 of the cap, pairs of fp16
-          tmem_ld16_issue(s_col + 16 * pass, s);
-          tmem_ld16_issue(d_col + 16 * pass, t);
-          tmem_ld16_wait(s);
-          tmem_ld16_wait(t);
+        const int c0 = cb * 64 + 32 * half;
+        // P = 2^(c x - lse)
+        uint32_t s[32], ch[16];                 // ch: 1 - tanh^2 of the cap, pairs of fp16
+        tmem_ld32_issue(s_col, s);
+        tmem_ld32_wait(s);
+        {
           // distance j - i: c0 + e - i (rows are queries) or i - c0 - e
-          const int lo = KV ? i0 - c0 - 15 : c0 - i0 - 31;
-          shape_scores<16, BIAS, CAP, KV ? -1 : 1, true>(s, ch, a, KV ? i - c0 : c0 - i, lo, lo + 46);
-          // P = 2^(c x - lse) -> s, dS = P (dP - D) -> t
+          const int lo = KV ? i0 - c0 - 31 : c0 - i0 - 31;
+          shape_scores<32, BIAS, CAP, KV ? -1 : 1, true>(s, ch, a, KV ? i - c0 : c0 - i, lo, lo + 62);
+        }
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) {
+          F2 l0 = f2(row_lse, row_lse), l1 = l0;
+          if (KV) ld_pairs(stats + 4 * e, l0, l1);
+          float x, y;
+          split(fma2(f2u(s[e], s[e + 1]), c2, l0), x, y);
+          s[e] = __float_as_uint(ex2(x)), s[e + 1] = __float_as_uint(ex2(y));
+          split(fma2(f2u(s[e + 2], s[e + 3]), c2, l1), x, y);
+          s[e + 2] = __float_as_uint(ex2(x)), s[e + 3] = __float_as_uint(ex2(y));
+        }
+        if (mask) {
+          const int first = edge - c0;
+#pragma unroll
+          for (int e = 0; e < 32; ++e)
+            if (KV ? e < first : e >= first) s[e] = 0u;
+          if (doc) {
+            const int4* dd = reinterpret_cast<const int4*>(doc + c0);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int4 v = __ldg(dd + e);
+              if (v.x != id) s[4 * e] = 0u;
+              if (v.y != id) s[4 * e + 1] = 0u;
+              if (v.z != id) s[4 * e + 2] = 0u;
+              if (v.w != id) s[4 * e + 3] = 0u;
+            }
+          }
+        }
+        if (KV) {
+          uint32_t w[16];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) w[e] = bf16_pair(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
+          tmem_st16(s_col, w);
+          if (F::kSplit) {
+            tmem_st_wait();
+            tc_fence_before();
+            arrive_warp(&pfull[buf.at]);
+          }
+        }
+        // dS = P (dP - D)
+        wait.on_lanes(&dfull[buf.at], buf.phase, 40);
+        tc_fence_after();
+        if (!KV && count <= 2) {
+          // the whole row is at hand: D = sum P dP, exactly
+          float d = 0.f;
+#pragma unroll
+          for (int pass = 0; pass < 2; ++pass) {
+            uint32_t t[16];
+            tmem_ld16_issue(d_col + 16 * pass, t);
+            tmem_ld16_wait(t);
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+              if (s[16 * pass + e] != 0u) d = fmaf(__uint_as_float(s[16 * pass + e]), __uint_as_float(t[e]), d);
+          }
+          row_d = -row_total(d);
+        }
+#pragma unroll
+        for (int pass = 0; pass < 2; ++pass) {
+          uint32_t t[16];
+          tmem_ld16_issue(d_col + 16 * pass, t);
+          tmem_ld16_wait(t);
 #pragma unroll
           for (int e = 0; e < 16; e += 4) {
-            F2 l0 = f2(row_lse, row_lse), l1 = l0, d0 = f2(row_d, row_d), d1 = d0;
-            if (KV) {
-              ld_pairs(stats + 64 * pass + 4 * e, l0, l1);
-              ld_pairs(stats + 256 + 64 * pass + 4 * e, d0, d1);
-            }
+            F2 d0 = f2(row_d, row_d), d1 = d0;
+            if (KV) ld_pairs(stats + 256 + 64 * pass + 4 * e, d0, d1);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              const int at = e + 2 * k;
+              const int at = e + 2 * k, sat = 16 * pass + at;
               float x, y;
-              split(fma2(f2u(s[at], s[at + 1]), c2, k ? l1 : l0), x, y);
-              const F2 w = f2(ex2(x), ex2(y));
-              split(w, x, y);
-              s[at] = __float_as_uint(x), s[at + 1] = __float_as_uint(y);
-              split(mul2(w, add2(f2u(t[at], t[at + 1]), k ? d1 : d0)), x, y);
+              split(mul2(f2u(s[sat], s[sat + 1]), add2(f2u(t[at], t[at + 1]), k ? d1 : d0)), x, y);
               t[at] = __float_as_uint(x), t[at + 1] = __float_as_uint(y);
             }
           }
-          if (mask) {
-            const int first = edge - c0;
+          if (mask) {                          // what stands in a masked place may have been NaN
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              if (KV ? e < first : e >= first) s[e] = t[e] = 0u;
-            if (doc) {
-              const int4* dd = reinterpret_cast<const int4*>(doc + c0);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const int4 v = __ldg(dd + e);
-                if (v.x != id) s[4 * e] = t[4 * e] = 0u;
-                if (v.y != id) s[4 * e + 1] = t[4 * e + 1] = 0u;
-                if (v.z != id) s[4 * e + 2] = t[4 * e + 2] = 0u;
-                if (v.w != id) s[4 * e + 3] = t[4 * e + 3] = 0u;
-              }
-            }
+              if (s[16 * pass + e] == 0u) t[e] = 0u;
           }
           if (!KV) {
 #pragma unroll
@@ -368,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
             // the patch's distances: base + row - column; whether any of the
             // block's is within the reach is the same for the warps of a row
             // group, which meet at barriers below
-            const int base = i0 - c0, corner = i0 - cb * 64;
+            const int base = i0 - c0 - 16 * pass, corner = i0 - cb * 64;
             if (corner - 63 >= a.reach || corner + 31 <= -a.reach) {
               F2 z = f2u(t[0], t[1]);
 #pragma unroll
@@ -406,29 +461,28 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
               asm volatile("bar.sync %0, 64;" ::"r"(pair) : "memory");
             }
           }
-          uint32_t w[8];
-          if (KV) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = bf16_pair(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
-            tmem_st8(s_col + 8 * pass, w);
-          }
-          if (CAP) {           // a masked score may have been NaN
+          if (CAP) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&ch[e]));
+              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&ch[8 * pass + e]));
               float x, y;
               split(mul2(f2u(t[2 * e], t[2 * e + 1]), f2(f.x, f.y)), x, y);
-              t[2 * e] = s[2 * e] == 0u ? 0u : __float_as_uint(x);
-              t[2 * e + 1] = s[2 * e + 1] == 0u ? 0u : __float_as_uint(y);
+              t[2 * e] = __float_as_uint(x), t[2 * e + 1] = __float_as_uint(y);
+            }
+            if (mask) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (s[16 * pass + e] == 0u) t[e] = 0u;
             }
           }
+          uint32_t w[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) w[e] = bf16_pair(__uint_as_float(t[2 * e]), __uint_as_float(t[2 * e + 1]));
           tmem_st8(d_col + 8 * pass, w);
         }
         tmem_st_wait();
         tc_fence_before();
-        arrive_warp(&pfull[buf.at]);
+        arrive_warp(&tfull[buf.at]);
         buf.step();
         slot += 2;
         if (slot >= stages) slot -= stages, phase ^= 1;
@@ -467,6 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       }
     }
     if (!KV) {
+      if (count == 1 && side == 1) row_d = -row_total(0.f);       // the other side has the only block
       float x, y;
       split(eps, x, y);
       rowsum[(2 * side + half) * 128 + 32 * quarter + lane] = x + y;
