@@ -448,19 +448,25 @@ _fo_strided_bytes = C.sizeof(fo_strided)
 
 
 def _strided(q, keys, *tensors):
-    """An array of fo_strided for tensors like q, or like `keys` = (batch, len,
-    kv_heads, head_dim) where a (tensor, True, name) triple says so."""
+    """The fields of fo_strided, one after another, for (tensor, name) pairs
+    like q, or like `keys` = (batch, len, kv_heads, head_dim) for triples with
+    True."""
     wide, dtype, device, flat = q.shape, q.dtype, q.get_device(), []
-    for t, key_heads, name in tensors:
+    for t, name, *key_heads in tensors:
         want = keys if key_heads else wide
         if t.shape != want or t.dtype != dtype or t.get_device() != device:
             raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype} on {t.device}; wanted {tuple(want)} {dtype} on {q.device}")
-        st = t.stride()
-        if st[3] != 1 and want[3] > 1:
+        sb, sl, sh, sd = t.stride()
+        if sd != 1 and want[3] > 1:
             raise ValueError(f"{name}: its innermost stride must be 1")
-        flat.append(t.data_ptr())
-        flat += st[:3]
-    return (C.c_int64 * len(flat))(*flat)
+        flat += (t.data_ptr(), sb, sl, sh)
+    return flat
+
+
+def _contiguous(t, shape):
+    """The same for a contiguous tensor that the binding has allocated."""
+    _, L, H, D = shape
+    return [t.data_ptr(), L * H * D, H * D, D]
 
 
 def _small(t, shape, dtype, like, name):
@@ -524,7 +530,9 @@ def attention_forward(q, k, v, causal=False, softcap=0.0, scale=None, slopes=Non
         return o, lse, torch.empty(need, dtype=torch.uint8, device=device) if need > 0 else None, need
 
     (o, lse, ws, need), st = _on_stream(torch, q, stream, make)
-    args = _strided(q, (B, L, s.kv_heads, D), (q, False, "q"), (k, True, "k"), (v, True, "v"), (o, False, "out"))
+    flat = _strided(q, (B, L, s.kv_heads, D), (q, "q"), (k, "k", True), (v, "v", True))
+    flat += _contiguous(o, shape) if out is None else _strided(q, None, (o, "out"))
+    args = (C.c_int64 * 16)(*flat)
     at, n = C.addressof(args), _fo_strided_bytes
     _check(L_.fo_attention_forward(s, at, at + n, at + 2 * n, at + 3 * n, lse.data_ptr(),
                                    ws.data_ptr() if need > 0 else None, need, st), "attention_forward")
@@ -552,8 +560,12 @@ def attention_backward(dout, q, k, v, o, lse, causal=False, softcap=0.0, scale=N
         return g, dq, dk, dv, dtable, torch.empty(need, dtype=torch.uint8, device=device) if need > 0 else None
 
     (dout, dq, dk, dv, dtable, ws), st = _on_stream(torch, q, stream, make)
-    args = _strided(q, keys, (q, False, "q"), (k, True, "k"), (v, True, "v"), (o, False, "o"), (dout, False, "dout"),
-                    (dq, False, "dq"), (dk, True, "dk"), (dv, True, "dv"))
+    flat = _strided(q, keys, (q, "q"), (k, "k", True), (v, "v", True), (o, "o"), (dout, "dout"))
+    if grads is None:
+        flat += _contiguous(dq, shape) + _contiguous(dk, keys) + _contiguous(dv, keys)
+    else:
+        flat += _strided(q, keys, (dq, "dq"), (dk, "dk", True), (dv, "dv", True))
+    args = (C.c_int64 * 32)(*flat)
     at, n = C.addressof(args), _fo_strided_bytes
     _check(L_.fo_attention_backward(
         s, at, at + n, at + 2 * n, at + 3 * n, _small(lse, (B, H, L), torch.float32, q, "lse"), at + 4 * n, at + 5 * n,
@@ -586,18 +598,31 @@ def dropout_add(x, residual, p, seed, call, out=None, stream=None):
     fp32 device tensor; (seed, call) name the mask.  Runs on `stream`, by
     default torch's current stream."""
     import torch
-    if not x.is_cuda or x.dtype not in (torch.bfloat16, torch.float32) or x.dim() < 1:
-        raise ValueError("x: a bf16 or fp32 device tensor")
-    out, st = _on_stream(torch, x, stream,
-                         lambda: torch.empty(x.shape, dtype=x.dtype, device=x.device) if out is None else out)
-    cols = x.shape[-1]
+    if x.dtype == torch.bfloat16:
+        dtype = DTYPE_BF16
+    elif x.dtype == torch.float32:
+        dtype = DTYPE_F32
+    else:
+        raise ValueError("x: bf16 or fp32")
+    if not x.is_cuda or x.dim() < 1:
+        raise ValueError("x: a device tensor of one dimension at least")
+    shape = x.shape
+    cols = shape[-1]
+
+    def make():
+        return torch.empty(shape, dtype=x.dtype, device=x.device)
+
+    if out is None:
+        y, st = _on_stream(torch, x, stream, make)
+        yp, ys = y.data_ptr(), cols
+    else:
+        y, st = out, torch.cuda.current_stream(x.get_device()).cuda_stream if stream is None else stream
+        yp, ys = _matrix(y, x, "out")
     xp, xs = _matrix(x, x, "x")
     rp, rs = (None, 0) if residual is None else _matrix(residual, x, "residual")
-    yp, ys = _matrix(out, x, "out")
-    _check(lib().fo_dropout_add(xp, xs, rp, rs, yp, ys, DTYPE_BF16 if x.dtype == torch.bfloat16 else DTYPE_F32,
-                                x.numel() // cols if cols else 0, cols, p, seed & (2**64 - 1), call & (2**64 - 1), st),
-           "dropout_add")
-    return out
+    _check(lib().fo_dropout_add(xp, xs, rp, rs, yp, ys, dtype, x.numel() // cols if cols else 0, cols, p,
+                                seed & (2**64 - 1), call & (2**64 - 1), st), "dropout_add")
+    return y
 
 
 def dropout_grad(dy, p, seed, call, out=None, stream=None):

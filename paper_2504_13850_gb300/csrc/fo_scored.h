@@ -45,6 +45,7 @@ struct ScoredParams {
   const float* slopes;     // [H] or null
   const void* table;       // [H][buckets] in the tensors' type, or null
   const int32_t* prefix;   // [B] or null
+  const int32_t* ids;      // [B][L] document ids as given, or null
   void* dtable;
   int B, L, Lp, H, KV, G, D;
   int causal, buckets, reach;

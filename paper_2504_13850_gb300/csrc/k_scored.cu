@@ -37,14 +37,10 @@ constexpr int kThreads = 256;
 
 // ------------------------------------------------------------- preparation
 // Document ids padded to Lp (-1 past the sequence), and the summary of each
-// 64 ids; one warp per 64 ids.
-__global__ void __launch_bounds__(128) scored_docs_k(const int32_t* __restrict__ ids, int32_t* __restrict__ doc,
-                                                     int2* __restrict__ blk, int L, int Lp, int64_t n_blk) {
-  pdl_wait();
-  pdl_trigger();
-  const int64_t w = int64_t(blockIdx.x) * 4 + threadIdx.x / 32;
-  if (w >= n_blk) return;
-  const int per = Lp / kScoredBlock, lane = threadIdx.x % 32;
+// 64 ids: one warp per 64 ids, w of them.
+__device__ __forceinline__ void summarise_docs(const ScoredParams& p, int64_t w) {
+  const int per = p.Lp / kScoredBlock, lane = threadIdx.x % 32;
+  if (w >= int64_t(p.B) * per) return;
   const int64_t b = w / per;
   const int l0 = int(w % per) * kScoredBlock;
   int2 s = make_int2(INT_MAX, -1);
@@ -52,24 +48,36 @@ __global__ void __launch_bounds__(128) scored_docs_k(const int32_t* __restrict__
   for (int t = 0; t < 2; ++t) {
     const int l = l0 + lane + 32 * t;
     int id = -1;
-    if (l < L) {
-      id = max(ids[b * L + l], -1);      // one id for all padding
+    if (l < p.L) {
+      id = max(p.ids[b * p.L + l], -1);      // one id for all padding
       s = doc_join(s, id < 0 ? make_int2(int(0x80000000u) | INT_MAX, -1) : make_int2(id, id));
     }
-    doc[b * Lp + l] = id;
+    p.doc[b * p.Lp + l] = id;
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1)
     s = doc_join(s, make_int2(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o)));
-  if (lane == 0) blk[w] = s;
+  if (lane == 0) p.blk[w] = s;
+}
+
+__global__ void __launch_bounds__(128) scored_docs_k(const __grid_constant__ ScoredParams p) {
+  pdl_wait();
+  pdl_trigger();
+  summarise_docs(p, int64_t(blockIdx.x) * 4 + threadIdx.x / 32);
 }
 
 // -D_i = -sum_d dO O and -lse * log2(e), padded to Lp rows per (sequence, head).
-// VEC: 16-byte loads (8 bf16), DL lanes per row; else one warp per row.
+// VEC: 16-byte loads (8 bf16), `lanes` lanes per row; else one warp per row.
+// The blocks from row_blocks on summarise the document ids.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) scored_delta_k(const __grid_constant__ ScoredParams p, int lanes) {
+__global__ void __launch_bounds__(256) scored_delta_k(const __grid_constant__ ScoredParams p, int lanes,
+                                                      unsigned row_blocks) {
   pdl_wait();
   pdl_trigger();
+  if (blockIdx.x >= row_blocks) {
+    summarise_docs(p, int64_t(blockIdx.x - row_blocks) * 8 + threadIdx.x / 32);
+    return;
+  }
   const int per = 32 / lanes, lane = threadIdx.x % 32, sub = lane % lanes;
   const int64_t row = (int64_t(blockIdx.x) * 8 + threadIdx.x / 32) * per + lane / lanes;   // (b, h, l)
   const int64_t rows = int64_t(p.B) * p.H * p.Lp;
@@ -81,7 +89,7 @@ __global__ void __launch_bounds__(256) scored_delta_k(const __grid_constant__ Sc
     l = int(row % p.Lp);
     bh = row / p.Lp;
     const int b = int(bh / p.H), h = int(bh % p.H);
-    live = l < p.L && (!p.doc || p.doc[int64_t(b) * p.Lp + l] >= 0);
+    live = l < p.L && (!p.ids || p.ids[int64_t(b) * p.L + l] >= 0);
     if (live) {
       const T* o = static_cast<const T*>(p.o.p) + b * p.o.sb + l * p.o.sl + h * p.o.sh;
       const T* g = static_cast<const T*>(p.dout.p) + b * p.dout.sb + l * p.dout.sl + h * p.dout.sh;
@@ -715,6 +723,7 @@ ScoredParams params(const fo_attention_spec* s, const Layout& a, char* ws, bool 
     for (int e = 0; e < 2 * s->reach + 1; ++e) p.map[e] = s->bucket_of_host[e];
   }
   if (s->documents) {
+    p.ids = s->documents;
     p.doc = reinterpret_cast<int32_t*>(ws + a.doc);
     p.blk = reinterpret_cast<int2*>(ws + a.blk);
   }
@@ -724,13 +733,6 @@ ScoredParams params(const fo_attention_spec* s, const Layout& a, char* ws, bool 
     p.part = reinterpret_cast<float*>(ws + a.part);
   }
   return p;
-}
-
-cudaError_t prepare_docs(const fo_attention_spec* s, const ScoredParams& p, cudaStream_t st) {
-  if (!s->documents) return cudaSuccess;
-  const int64_t n = int64_t(p.B) * (p.Lp / kScoredBlock);
-  return launch_k(scored_docs_k, dim3(unsigned((n + 3) / 4)), dim3(128), 0, st, s->documents, p.doc, p.blk, p.L, p.Lp,
-                  n);
 }
 
 int check_workspace(const Layout& a, const void* ws, int64_t bytes) {
@@ -770,7 +772,9 @@ int fo_attention_forward(const fo_attention_spec* spec, const fo_strided* q, con
   p.o = strided(o);
   p.lse = lse;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = prepare_docs(spec, p, st);
+  cudaError_t e = cudaSuccess;
+  const int64_t runs = int64_t(p.B) * (p.Lp / kScoredBlock);
+  if (p.ids) e = launch_k(scored_docs_k, dim3(unsigned((runs + 3) / 4)), dim3(128), 0, st, p);
   bool tc = spec->dtype == FO_DTYPE_BF16 && p.D % 8 == 0 && wide(q, spec, p.H) && wide(k, spec, p.KV) &&
             wide(v, spec, p.KV) && wide(o, spec, p.H);
   if (e == cudaSuccess && tc) e = scored_fwd_tc(p, st, &tc);
@@ -813,14 +817,13 @@ int fo_attention_backward(const fo_attention_spec* spec, const fo_strided* q, co
   p.dv = strided(dv);
   p.lse = const_cast<float*>(lse);
   p.dtable = dtable;
-  cudaError_t e = prepare_docs(spec, p, st);
-  if (e != cudaSuccess) return cuda_error(e);
   const int64_t rows = int64_t(p.B) * p.H * p.Lp;
   const bool vec = !f32 && p.D % 8 == 0 && wide(o, spec, spec->heads) && wide(dout, spec, spec->heads);
   const int lanes = vec ? (p.D <= 64 ? 8 : 16) : 32;
   const unsigned blocks = unsigned((rows + 8 * (32 / lanes) - 1) / (8 * (32 / lanes)));
+  const int64_t runs = p.ids ? int64_t(p.B) * (p.Lp / kScoredBlock) : 0;
   auto delta = f32 ? scored_delta_k<float, false> : vec ? scored_delta_k<bf16, true> : scored_delta_k<bf16, false>;
-  e = launch_k(delta, dim3(blocks), dim3(256), 0, st, p, lanes);
+  cudaError_t e = launch_k(delta, dim3(blocks + unsigned((runs + 7) / 8)), dim3(256), 0, st, p, lanes, blocks);
   bool tc = vec && wide(q, spec, p.H) && wide(k, spec, p.KV) && wide(v, spec, p.KV) && wide(dq, spec, p.H) &&
             wide(dk, spec, p.KV) && wide(dv, spec, p.KV);
   if (e == cudaSuccess && tc) e = scored_bwd_tc(p, st, &tc);
