@@ -438,8 +438,9 @@ FO_API int64_t fo_attention_workspace(const fo_attention_spec* spec, int backwar
  * fo_attention_workspace bytes) is free again when the call's work on the
  * stream is done.  Nothing is allocated, so a capturing stream may be
  * passed.  FO_ERR_ARG for a bad spec, null or misaligned pointers, negative
- * strides or overlapping output strides, or a workspace that is too small;
- * nothing ran then (no counterpart in the paper). */
+ * strides, output strides of which one does not step over all smaller
+ * dimensions, or a workspace that is too small; nothing ran then (no
+ * counterpart in the paper). */
 FO_API int fo_attention_forward(const fo_attention_spec* spec, const fo_strided* q, const fo_strided* k,
                          const fo_strided* v, const fo_strided* o, float* lse, void* workspace,
                          int64_t workspace_bytes, void* stream);

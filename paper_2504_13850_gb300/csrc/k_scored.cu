@@ -23,6 +23,7 @@
 #include "fo_scored.h"
 #include "../../include/fedoptima.h"
 
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <string>
@@ -656,10 +657,15 @@ int check_tensor(const fo_strided* t, const fo_attention_spec* s, int heads, boo
   if (reinterpret_cast<uintptr_t>(t->data) % size) return bad(std::string("attention: misaligned ") + name);
   const int64_t st[3] = {t->batch_stride, t->token_stride, t->head_stride};
   const int64_t n[3] = {s->batch, s->len, heads};
-  for (int e = 0; e < 3; ++e) {
+  int64_t extent = s->head_dim;        // elements that the dimensions seen so far span
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + 3, [&](int x, int y) { return st[x] < st[y]; });
+  for (int e : order) {
     if (n[e] <= 1) continue;
-    if (st[e] < 0 || (out && st[e] < s->head_dim)) return bad(std::string("attention: strides of ") + name);
-    if (st[e] > (int64_t(1) << 40)) return bad(std::string("attention: strides of ") + name);
+    // what is written: each dimension steps over all of the smaller ones
+    if (st[e] < 0 || st[e] > (int64_t(1) << 40) || (out && st[e] < extent))
+      return bad(std::string("attention: strides of ") + name);
+    extent += (n[e] - 1) * st[e];
   }
   return FO_OK;
 }

@@ -71,7 +71,9 @@ def test_bad_tensors_and_workspaces_are_refused():
         return L.fo_attention_forward(C.byref(s), q, t(), t(), o, lse, ws, n, None)
 
     for kw, what in (({"q": None}, "null q"), ({"q": t(p=0)}, "null q"), ({"q": t(p=4097)}, "misaligned q"),
-                     ({"q": t(l=-1)}, "strides of q"), ({"o": t(l=0)}, "strides of o"), ({"lse": None}, "lse"),
+                     ({"q": t(l=-1)}, "strides of q"), ({"o": t(l=0)}, "strides of o"),
+                     ({"o": t(l=255)}, "strides of o"), ({"o": t(b=200 * 256 - 1)}, "strides of o"),
+                     ({"o": t(h=63)}, "strides of o"), ({"lse": None}, "lse"),
                      ({"ws": None}, "workspace"), ({"ws": 4100}, "workspace"), ({"n": 100}, "needed")):
         assert forward(**kw) == api.ERR_ARG and what in api.last_error(), kw
     bare = spec()
