@@ -75,20 +75,12 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// The MMA warp runs converged and issues each run of products from a region
-// that elect.sync guards: the compiler then knows that one lane issues, and a
-// product costs one instruction besides its descriptors.  (From a branch on
-// the lane index every tcgen05.mma took 170 cycles whatever its size, and
-// inside a loop of the elected lane about 36 instructions: other lanes might
-// have been active there.)
-__device__ __forceinline__ bool elect_one() {
-  uint32_t e = 0;
-  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n @p mov.u32 %0, 1;\n}\n" : "+r"(e));
-  return e != 0;
-}
-// tcgen05.mma issued by one elected lane of a converged warp: both operands in
-// shared memory, or A in tensor memory (lane = row, each 32-bit column two
-// consecutive K elements, so 16 elements of K are 8 columns); and the commit.
+// tcgen05.mma and its commit, issued by one elected lane of a converged warp:
+// both operands in shared memory, or A in tensor memory (lane = row, each
+// 32-bit column two consecutive K elements, so 16 elements of K are 8
+// columns).  elect.sync stands beside each product, which tells the compiler
+// that one lane issues: from a branch on the lane index every product took 170
+// cycles whatever its size, and under a predicate computed once 90.
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
       "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n elect.sync _|q, 0xffffffff;\n"

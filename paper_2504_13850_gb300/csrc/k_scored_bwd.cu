@@ -16,18 +16,22 @@
 // S and dP take 64 TMEM columns each, in three buffers where the sums leave
 // room (two for keys of a head width above 64): two groups of 256 threads
 // process alternate blocks, so that one's arithmetic runs while the other's
-// products do, and a third buffer keeps the scores one block ahead; a row is shared by two threads, 32 columns each, in two passes of 16.  P
-// and dS go back to TMEM as bf16 over the scores they came from, as A operands
-// of the accumulating products; no score touches shared memory.  Row
-// statistics (scored_delta_k) are per column where rows are keys and ride
-// along in each stage.
+// products do, and a third buffer keeps the scores one block ahead.  A row is
+// shared by two threads, 32 columns each, which form P from all 32 at once and
+// dS in two passes of 16.  S is handed over before dP, whose products run
+// while P is formed; P is handed over before dS where there are only two
+// buffers (capped 2048: 294 -> 275 us, causal 16384 of width 128: 1510 ->
+// 1400; with three the extra wait cost what it gained).  P and dS go back to
+// TMEM as bf16 over the scores they came from, as A operands of the
+// accumulating products; no score touches shared memory.  Row statistics
+// (scored_delta_k) are per column where rows are keys and ride along in each
+// stage.
 // D = dO . O carries the rounding of O, which would leave each row's dS with a
 // sum of -dD instead of 0, most of it in whichever bucket holds most keys: the
 // query pass, launched first, sums its dS rows in fp32 and adds the sum to D,
-// so that dK and the table gradient come from the exact D.  Where two blocks
-// are all that a tile walks, as in sequences of up to 128 tokens, whose few
-// keys feel the error most, it sums P dP over the row first and dQ has the
-// exact D too.
+// so that dK and the table gradient come from the exact D.  Where a tile walks
+// at most two blocks, as in sequences of up to 128 tokens, whose few keys feel
+// the error most, it sums P dP over the row first and dQ has the exact D too.
 // The table gradient sums dS in fp32 by distance: each warp turns 32 x 16
 // patches through shared memory so that a lane sums a diagonal, into arrays by
 // distance shared by the two warps of a row group, one after the other;

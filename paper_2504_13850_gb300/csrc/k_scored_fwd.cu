@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
   } else if (warp == kMma) {
     constexpr uint32_t id_s = instr_desc(128, false, false), id_o = instr_desc(DP, false, true);
     const uint32_t ring_at = smem_u32(ring);
-    auto issue_s = [&](int t, int slot) {       // in an elected region
+    auto issue_s = [&](int t, int slot) {
       const Operand<16> q(smem_u32(sQ) + t * F::kTileBytes), k(ring_at + slot * F::kTileBytes);
 #pragma unroll
       for (int e = 0; e < DP / 16; ++e) {
@@ -241,19 +241,17 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
           wait.on_lanes(&pfull[t], step[t] & 1, 26);
           tc_fence_after();
         }
-        {
-          if (on[t]) {
+        if (on[t]) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              mma_ts(tmem + 128 * NT + DP * t, tmem + 128 * t + 64 * (e >> 2) + 8 * (e & 3), v.at(2048 * e), id_o,
-                     e > 0 ? 1u : step[t]);
-            commit_to(&ofull[t]);
-          }
-          if (then) issue_s(t, k_at.at);
-          if (t == NT - 1) {
-            commit_to(&empty[v_at.at]);
-            if (nxt >= 0) commit_to(&empty[k_at.at]);
-          }
+          for (int e = 0; e < 8; ++e)
+            mma_ts(tmem + 128 * NT + DP * t, tmem + 128 * t + 64 * (e >> 2) + 8 * (e & 3), v.at(2048 * e), id_o,
+                   e > 0 ? 1u : step[t]);
+          commit_to(&ofull[t]);
+        }
+        if (then) issue_s(t, k_at.at);
+        if (t == NT - 1) {
+          commit_to(&empty[v_at.at]);
+          if (nxt >= 0) commit_to(&empty[k_at.at]);
         }
         if (on[t]) ++step[t];
       }
