@@ -49,7 +49,8 @@ struct ScoredParams {
   void* dtable;
   int B, L, Lp, H, KV, G, D;
   int causal, buckets, reach;
-  int stages;              // shared-memory stages of the backward tensor-core kernels; see work_of_block for the others
+  int stages;              // shared-memory stages of the backward tensor-core kernels
+  int share;               // CUDA-core kernels: blocks that share a tile of rows
   float scale, cap;
   uint8_t map[2 * kMaxReach + 1];
 };

@@ -18,7 +18,11 @@
 // keys (dQ), then a tile of keys walks the queries (dK, dV and the table
 // gradient); every sum has a fixed order, at the price of forming the scores
 // twice.  The first one adds each row's sum of dS, which the rounding of O
-// keeps from being zero, to D for the second.  Bound by the fp32 FMA rate.
+// keeps from being zero, to D for the second.
+// Bound by instruction issue: FMAs are a little over half of the instructions
+// and 16 warps per SM fill a little over half of the slots.  2 x 2048 tokens,
+// 8 heads of 64, fp32: forward 667 us (25.8 TFLOP/s), backward 2.04 ms (21.0,
+// counting 5 products).
 #include "fo_common.cuh"
 #include "fo_scored.h"
 #include "../../include/fedoptima.h"
@@ -35,6 +39,7 @@ namespace {
 
 constexpr int kT = 64;             // tile of tokens
 constexpr int kThreads = 256;
+constexpr int kMaxShare = 8;       // blocks that share a tile of rows: the portable cluster size
 
 // ------------------------------------------------------------- preparation
 // Document ids padded to Lp (-1 past the sequence), and the summary of each
@@ -334,15 +339,34 @@ __device__ __forceinline__ void store_rows(const Strided& t, const ScoredParams&
   }
 }
 
-// Which (tile, sequence and head) a block works on: the longest causal tiles
-// first, so that the hardware's order of dispatch balances them.  When two
-// blocks per SM hold the whole grid there is no later dispatch, and the second
-// block of each SM comes in the opposite order, a short one to the longest
-// (2 x 1000 causal tokens, 8 heads of 64: forward 143 -> 127 us).
-__device__ __forceinline__ unsigned work_of_block(int sms) {
-  const unsigned n = gridDim.x, x = blockIdx.x;
-  return sms > 0 && x >= unsigned(sms) ? n - 1 - (x - unsigned(sms)) : x;
-}
+// A cluster of blocks may share a tile of rows: block `rank` of `n` takes every
+// n-th allowed tile of columns, and the first one adds up.
+struct Share {
+  int n, rank;
+  __device__ __forceinline__ explicit Share(int n_) : n(n_), rank(int(blockIdx.x) % n_) {}
+  // Skips the other blocks' tiles: next_tile of the one after `count` more.
+  template <bool KEYS_ARE_ROWS>
+  __device__ __forceinline__ int skip(const ScoredParams& p, int pf, int b, int r0, int c0, int* cls, int count) const {
+    c0 = next_tile<KEYS_ARE_ROWS>(p, pf, b, r0, c0, cls);
+    for (; count > 0 && c0 < p.L; --count) c0 = next_tile<KEYS_ARE_ROWS>(p, pf, b, r0, c0 + kT, cls);
+    return c0;
+  }
+  // Every thread of the cluster has come here, and sees what the others wrote.
+  __device__ __forceinline__ static void sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  // This thread's value e of block r's buffer x (a shared-memory array at the
+  // same place in every block).
+  __device__ __forceinline__ static float of(const float* x, int e, int r) {
+    uint32_t at;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;"
+                 : "=r"(at)
+                 : "r"(static_cast<uint32_t>(__cvta_generic_to_shared(x + e * kThreads + threadIdx.x))), "r"(r));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+  }
+};
 
 // ----------------------------------------------------------------- forward
 template <typename T, int NC>
@@ -353,14 +377,15 @@ __global__ void __launch_bounds__(kThreads, NC <= 4 ? 2 : 1) scored_fwd_k(const 
   float *Q = sm, *KVs = Q + kTile, *P = KVs + 4 * kTile, *bias = P + kT * kT;    // KVs: two pairs of K and V
   pdl_wait();
   pdl_trigger();
-  const unsigned work = work_of_block(p.stages);
-  const int tiles = (p.L + kT - 1) / kT, bh = work % (p.B * p.H);
+  const Share share(p.share);
+  const unsigned work = blockIdx.x / unsigned(share.n);
+  const int tiles = (p.L + kT - 1) / kT, bh = work % (p.B * p.H);      // the longest causal tiles first
   const int q0 = (tiles - 1 - int(work / (p.B * p.H))) * kT;
   const int b = bh / p.H, h = bh % p.H, kh = h / p.G;
   const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
   Pair pc = pair_of(p, b, h);
   int cls = 0, cls_next = 0, buf = 0;
-  int k0 = next_tile<false>(p, pc.pf, b, q0, 0, &cls);
+  int k0 = share.skip<false>(p, pc.pf, b, q0, 0, &cls, share.rank);
   load_tile<T>(Q, p.q, p, b, h, q0);
   if (k0 < p.L) {
     load_tile<T>(KVs, p.k, p, b, kh, k0);
@@ -375,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, NC <= 4 ? 2 : 1) scored_fwd_k(const 
 #pragma unroll
   for (int r = 0; r < 4; ++r) m[r] = -INFINITY;
   while (k0 < p.L) {
-    const int k1 = next_tile<false>(p, pc.pf, b, q0, k0 + kT, &cls_next);
+    const int k1 = share.skip<false>(p, pc.pf, b, q0, k0 + kT, &cls_next, share.n - 1);
     if (k1 < p.L) {
       load_tile<T>(KVs + 2 * (buf ^ 1) * kTile, p.k, p, b, kh, k1);
       load_tile<T>(KVs + (2 * (buf ^ 1) + 1) * kTile, p.v, p, b, kh, k1);
@@ -423,6 +448,35 @@ __global__ void __launch_bounds__(kThreads, NC <= 4 ? 2 : 1) scored_fwd_k(const 
     buf ^= 1;
   }
   copies_wait<0>();
+  if (share.n > 1) {
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float* x = KVs + r * (NC + 2) * kThreads + threadIdx.x;
+      x[0] = m[r];
+      x[kThreads] = sum[r];
+#pragma unroll
+      for (int n = 0; n < NC; ++n) x[(2 + n) * kThreads] = acc[r][n];
+    }
+    Share::sync();
+    if (share.rank == 0) {
+#pragma unroll 1
+      for (int o = 1; o < share.n; ++o) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float* x = KVs + r * (NC + 2) * kThreads;
+          const float mo = Share::of(x, 0, o), top = fmaxf(m[r], mo), base = top == -INFINITY ? 0.f : top;
+          const float keep = exp2f(m[r] - base), add = exp2f(mo - base);
+          sum[r] = sum[r] * keep + Share::of(x, 1, o) * add;
+          m[r] = top;
+#pragma unroll
+          for (int n = 0; n < NC; ++n) acc[r][n] = acc[r][n] * keep + Share::of(x, 2 + n, o) * add;
+        }
+      }
+    }
+    Share::sync();                     // the others' memory has been read
+    if (share.rank > 0) return;
+  }
   float inv[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
@@ -440,7 +494,7 @@ __global__ void __launch_bounds__(kThreads, NC <= 4 ? 2 : 1) scored_fwd_k(const 
 // the group (U = Q, W = dO): dV = sum P^T W, dK = sum dS^T U, and the partial
 // table gradients of this tile.
 template <typename T, int NC, bool KV>
-__global__ void __launch_bounds__(kThreads, NC <= (KV ? 2 : 4) ? 2 : 1) scored_bwd_k(const __grid_constant__ ScoredParams p) {
+__global__ void __launch_bounds__(kThreads, NC <= 4 ? 2 : 1) scored_bwd_k(const __grid_constant__ ScoredParams p) {
   extern __shared__ __align__(16) float sm[];
   constexpr int WD = 16 * NC;
   constexpr int kTile = WD * kT;
@@ -451,7 +505,8 @@ __global__ void __launch_bounds__(kThreads, NC <= (KV ? 2 : 4) ? 2 : 1) scored_b
   pdl_wait();
   pdl_trigger();
   const int heads = KV ? p.KV : p.H, tiles = (p.L + kT - 1) / kT;
-  const unsigned work = work_of_block(p.stages);
+  const Share share(p.share);
+  const unsigned work = blockIdx.x / unsigned(share.n);
   const int bh = work % (p.B * heads), slot = int(work / (p.B * heads));
   const int tile = KV ? slot : tiles - 1 - slot, r0 = tile * kT;
   const int b = bh / heads, h0 = KV ? (bh % heads) * p.G : bh % heads, kh = h0 / p.G;
@@ -474,7 +529,7 @@ __global__ void __launch_bounds__(kThreads, NC <= (KV ? 2 : 4) ? 2 : 1) scored_b
       load_tile<T>(UWs + (2 * buf + 1) * kTile, KV ? p.dout : p.v, p, b, KV ? h : kh, c0);
     };
     int cls = 0, cls_next = 0, buf = 0;
-    int c0 = next_tile<KV>(p, pc.pf, b, r0, 0, &cls);
+    int c0 = share.skip<KV>(p, pc.pf, b, r0, 0, &cls, (share.rank + g) % share.n);
     __syncthreads();
     if (c0 < p.L) load(0, c0);
     copies_commit();
@@ -484,34 +539,39 @@ __global__ void __launch_bounds__(kThreads, NC <= (KV ? 2 : 4) ? 2 : 1) scored_b
       lo = hi = 0.f;
     }
     for (; c0 < p.L;) {
-      const int c1 = next_tile<KV>(p, pc.pf, b, r0, c0 + kT, &cls_next);
+      const int c1 = share.skip<KV>(p, pc.pf, b, r0, c0 + kT, &cls_next, share.n - 1);
       if (c1 < p.L) load(buf ^ 1, c1);
       copies_commit();
       copies_wait<1>();
       __syncthreads();
       const float *U = UWs + 2 * buf * kTile, *W = U + kTile;
-      float s[4][4], dp[4][4], chain[4][4];
+      float s[4][4], dp[4][4];
       scores(s, X, U, p.D, ty, tx);
       scores(dp, Y, W, p.D, ty, tx);
       if (cls == kScoredSome) ids_of(pc.col_id, pc, c0 + 4 * tx);
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+      for (int c = 0; c < 4; ++c) {
+        float ds[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+        for (int r = 0; r < 4; ++r) {
           const int row = r0 + 4 * ty + r, col = c0 + 4 * tx + c, i = KV ? col : row, j = KV ? row : col;
           const bool ok = cls == kScoredAll || pair_allowed(p, pc, i, j, r, c);
-          const float z = pair_score(p, pc, bias, s[r][c], i, j, &chain[r][c]);
+          float chain;
+          const float z = pair_score(p, pc, bias, s[r][c], i, j, &chain);
           s[r][c] = ok ? exp2f(fmaf(z, kLog2e, lse2[i])) : 0.f;
-          dp[r][c] = ok ? s[r][c] * (dp[r][c] + delta[i]) : 0.f;
-          eps[r] += dp[r][c];
+          ds[r] = ok ? s[r][c] * (dp[r][c] + delta[i]) : 0.f;
+          eps[r] += ds[r];
+          dp[r][c] = ds[r] * chain;
         }
+        if (grad) *reinterpret_cast<float4*>(P + at_p(4 * tx + c, ty)) = make_float4(ds[0], ds[1], ds[2], ds[3]);
+      }
       if (grad) {
-        // each of 127 threads sums one diagonal of the tile in row order
-        put_tile(P, dp, ty, tx);
+        // each of 127 threads sums one diagonal of the tile of dS in row order
         __syncthreads();
         if (threadIdx.x < 2 * kT - 1) {
           const int e = int(threadIdx.x) - (kT - 1);             // row - column
           float t = 0.f;
+#pragma unroll 8
           for (int r = max(0, e); r < min(kT, kT + e); ++r) t += P[at_p(r - e, r >> 2) + (r & 3)];
           const int d = r0 - c0 + e;
           if (d <= -p.reach) lo += t;
@@ -526,10 +586,6 @@ __global__ void __launch_bounds__(kThreads, NC <= (KV ? 2 : 4) ? 2 : 1) scored_b
         accumulate<NC>(acc0, P, W, ty, tx);
         __syncthreads();
       }
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int c = 0; c < 4; ++c) dp[r][c] *= chain[r][c];
       put_tile(P, dp, ty, tx);
       __syncthreads();
       accumulate<NC>(acc1, P, U, ty, tx);
@@ -553,16 +609,48 @@ __global__ void __launch_bounds__(kThreads, NC <= (KV ? 2 : 4) ? 2 : 1) scored_b
       }
       __syncthreads();
       const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-      const int64_t n = int64_t(p.B) * tiles;
+      const int64_t n = int64_t(p.B) * tiles * share.n;
       for (int k = warp; k < p.buckets; k += kThreads / 32) {
         float t = 0.f;
         for (int e = lane; e < 2 * p.reach + 1; e += 32)
           if (p.map[e] == k) t += dist[e];
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-        if (lane == 0) p.part[(int64_t(h) * p.buckets + k) * n + int64_t(b) * tiles + tile] = t;
+        if (lane == 0) p.part[(int64_t(h) * p.buckets + k) * n + (int64_t(b) * tiles + tile) * share.n + share.rank] = t;
       }
     }
+  }
+  if (share.n > 1) {
+    __syncthreads();
+    constexpr int kEach = KV ? 2 * NC : NC + 1;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float* x = UWs + r * kEach * kThreads + threadIdx.x;
+#pragma unroll
+      for (int n = 0; n < NC; ++n) {
+        x[n * kThreads] = acc1[r][n];
+        if (KV) x[(NC + n) * kThreads] = acc0[r][n];
+      }
+      if (!KV) x[NC * kThreads] = eps[r];
+    }
+    Share::sync();
+    if (share.rank == 0) {
+#pragma unroll 1
+      for (int o = 1; o < share.n; ++o) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float* x = UWs + r * kEach * kThreads;
+#pragma unroll
+          for (int n = 0; n < NC; ++n) {
+            acc1[r][n] += Share::of(x, n, o);
+            if (KV) acc0[r][n] += Share::of(x, NC + n, o);
+          }
+          if (!KV) eps[r] += Share::of(x, NC, o);
+        }
+      }
+    }
+    Share::sync();                     // the others' memory has been read
+    if (share.rank > 0) return;
   }
   const float one[4] = {1.f, 1.f, 1.f, 1.f}, sc[4] = {p.scale, p.scale, p.scale, p.scale};
   if (KV) {
@@ -580,11 +668,37 @@ __global__ void __launch_bounds__(kThreads, NC <= (KV ? 2 : 4) ? 2 : 1) scored_b
   }
 }
 
-// The argument of work_of_block: the number of SMs when all `blocks` are
-// resident two to an SM, else 0.
-int paired(int64_t blocks, int NC) {
-  const int sms = elementwise_blocks(INT64_MAX / 2, kThreads) / 8;
-  return NC <= 4 && blocks > sms && blocks <= 2 * sms ? sms : 0;
+// How many blocks share a tile of rows (Share): twice as many while the grid
+// still fits the SMs, each of which holds two blocks up to head width 64 and
+// one above.  4 sequences of 200 tokens, 4 heads of 32, took 25.6 / 93.9 us
+// forward / backward with a block each and take 23.5 / 73.7.  With a causal
+// mask, whose tiles of rows differ in length, up to twice what fits: the
+// longest are half as long and start first (2 x 1000 causal tokens, 8 heads of
+// 64: 145 / 544 us -> 102 / 314); equal tiles only pay for it (16 x 128
+// tokens, 8 heads of 64: 32.8 / 175 us against 38.9 / 235).
+int shared_by(const ScoredParams& p, int64_t blocks, int64_t tiles, int NC) {
+  const int64_t sms = elementwise_blocks(INT64_MAX / 2, kThreads) / 8, room = sms * (NC <= 4 ? 2 : 1) * (p.causal ? 2 : 1);
+  int n = 1;
+  while (n < kMaxShare && 2 * n <= tiles && 2 * n * blocks <= room) n *= 2;
+  return n;
+}
+
+template <typename K>
+cudaError_t launch_shared(K kernel, int64_t blocks, size_t smem, cudaStream_t st, const ScoredParams& p) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(blocks * p.share));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = unsigned(p.share);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
 template <typename T, int NC>
@@ -594,11 +708,11 @@ cudaError_t forward_width(ScoredParams p, cudaStream_t st) {
   static std::atomic<bool> allowed[kMaxDevices];
   const cudaError_t e = allow_smem(scored_fwd_k<T, NC>, allowed);
   if (e != cudaSuccess) return e;
-  p.stages = paired(tiles * p.B * p.H, NC);
-  return launch_k(scored_fwd_k<T, NC>, dim3(unsigned(tiles * p.B * p.H)), dim3(kThreads), smem, st, p);
+  p.share = shared_by(p, tiles * p.B * p.H, tiles, NC);
+  return launch_shared(scored_fwd_k<T, NC>, tiles * p.B * p.H, smem, st, p);
 }
 template <typename T, int NC>
-cudaError_t backward_width(ScoredParams p, cudaStream_t st) {
+cudaError_t backward_width(ScoredParams& p, cudaStream_t st) {
   const int64_t tiles = ceil_div(p.L, kT);
   const size_t smem =
       (size_t(6 * 16 * NC * kT) + kT * kT + (p.table ? 2 * (2 * kMaxReach + 4) + 256 : 0)) * sizeof(float);
@@ -606,11 +720,11 @@ cudaError_t backward_width(ScoredParams p, cudaStream_t st) {
   cudaError_t e = allow_smem(scored_bwd_k<T, NC, false>, allowed[0]);
   if (e == cudaSuccess) e = allow_smem(scored_bwd_k<T, NC, true>, allowed[1]);
   if (e != cudaSuccess) return e;
-  p.stages = paired(tiles * p.B * p.H, NC);
-  e = launch_k(scored_bwd_k<T, NC, false>, dim3(unsigned(tiles * p.B * p.H)), dim3(kThreads), smem, st, p);
+  p.share = shared_by(p, tiles * p.B * p.H, tiles, NC);
+  e = launch_shared(scored_bwd_k<T, NC, false>, tiles * p.B * p.H, smem, st, p);
   if (e != cudaSuccess) return e;
-  p.stages = paired(tiles * p.B * p.KV, NC <= 2 ? NC : 8);      // wider ones take an SM each
-  return launch_k(scored_bwd_k<T, NC, true>, dim3(unsigned(tiles * p.B * p.KV)), dim3(kThreads), smem, st, p);
+  p.share = shared_by(p, tiles * p.B * p.KV, tiles, NC);
+  return launch_shared(scored_bwd_k<T, NC, true>, tiles * p.B * p.KV, smem, st, p);
 }
 // Accumulator columns per thread: 16 NC >= head width.
 template <typename T>
@@ -618,7 +732,7 @@ cudaError_t forward_simt(const ScoredParams& p, cudaStream_t st) {
   return p.D <= 32 ? forward_width<T, 2>(p, st) : p.D <= 64 ? forward_width<T, 4>(p, st) : forward_width<T, 8>(p, st);
 }
 template <typename T>
-cudaError_t backward_simt(const ScoredParams& p, cudaStream_t st) {
+cudaError_t backward_simt(ScoredParams& p, cudaStream_t st) {
   return p.D <= 32 ? backward_width<T, 2>(p, st)
                    : p.D <= 64 ? backward_width<T, 4>(p, st) : backward_width<T, 8>(p, st);
 }
@@ -687,7 +801,8 @@ bool wide(const fo_strided* t, const fo_attention_spec* s, int heads) {
 struct Layout {
   int64_t doc = 0, blk = 0, lse2 = 0, delta = 0, part = 0, bytes = 0;
 };
-// `part` is sized for the smaller (64-row) tiles of the CUDA-core kernels.
+// `part` is sized for the smaller (64-row) tiles of the CUDA-core kernels and
+// the blocks that may share one.
 Layout layout(const fo_attention_spec* s, bool backward) {
   Layout a;
   auto take = [&a](int64_t bytes) {
@@ -703,7 +818,8 @@ Layout layout(const fo_attention_spec* s, bool backward) {
   if (backward) {
     a.lse2 = take(B * H * Lp * 4);
     a.delta = take(B * H * Lp * 4);
-    if (s->table) a.part = take(H * s->buckets * B * ((int64_t(s->len) + kT - 1) / kT) * 4);
+    const int64_t tiles = (int64_t(s->len) + kT - 1) / kT;
+    if (s->table) a.part = take(H * s->buckets * B * tiles * std::min<int64_t>(tiles, kMaxShare) * 4);
   }
   return a;
 }
@@ -836,7 +952,7 @@ int fo_attention_backward(const fo_attention_spec* spec, const fo_strided* q, co
   if (e == cudaSuccess && !tc) e = f32 ? backward_simt<float>(p, st) : backward_simt<bf16>(p, st);
   if (e == cudaSuccess && dtable) {
     const int n = p.H * p.buckets;
-    const int64_t parts = int64_t(p.B) * ceil_div(p.L, tc ? 128 : kT);     // key tiles of the kernel that ran
+    const int64_t parts = int64_t(p.B) * (tc ? ceil_div(p.L, 128) : ceil_div(p.L, kT) * p.share);     // of the kernel that ran
     e = f32 ? launch_k(scored_table_k<float>, dim3((n + 3) / 4), dim3(128), 0, st, p.part, static_cast<float*>(dtable),
                        n, parts)
             : launch_k(scored_table_k<bf16>, dim3((n + 3) / 4), dim3(128), 0, st, p.part, static_cast<bf16*>(dtable),

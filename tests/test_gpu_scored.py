@@ -113,6 +113,13 @@ def test_longer_sequences():
     check(*make(1, 1000, 2, 1, 64, F32, seed=3, bias="bucket", causal=True))
 
 
+@pytest.mark.parametrize("dtype,D", [(F32, 32), (F32, 72), (BF, 20), (BF, 64)])
+@pytest.mark.parametrize("B,causal", [(1, False), (7, True), (16, False), (24, True)])
+def test_small_and_full_grids(B, causal, dtype, D):
+    """Few tiles, which several blocks may share, and more tiles than the GPU holds at once."""
+    check(*make(B, 330, 6, 3, D, dtype, seed=B, bias="bucket", causal=causal, docs="padded"))
+
+
 def test_large_scores():
     """Scores far apart, so that the running maximum moves by more than any threshold."""
     for dtype, D in ((BF, 64), (BF, 128), (F32, 64)):
