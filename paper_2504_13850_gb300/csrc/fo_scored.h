@@ -41,7 +41,7 @@ struct ScoredParams {
   int2* blk;               // [B][Lp / 64] summary of each 64 ids (see doc_summary)
   float* lse2;             // [B][H][Lp] -lse * log2(e), -inf where P is zero
   float* delta;            // [B][H][Lp] -D
-  float* part;             // [H][buckets][B * query tiles] partial table gradients
+  float* part;             // [H][buckets][B * key tiles * share] partial table gradients
   const float* slopes;     // [H] or null
   const void* table;       // [H][buckets] in the tensors' type, or null
   const int32_t* prefix;   // [B] or null
@@ -50,10 +50,12 @@ struct ScoredParams {
   int B, L, Lp, H, KV, G, D;
   int causal, buckets, reach;
   int stages;              // shared-memory stages of the backward tensor-core kernels
-  int share;               // CUDA-core kernels: blocks that share a tile of rows
+  int share;               // blocks (a cluster) that share a tile of rows
   float scale, cap;
   uint8_t map[2 * kMaxReach + 1];
 };
+
+constexpr int kMaxShare = 8;      // the portable cluster size
 
 enum { kScoredNone = 0, kScoredAll = 1, kScoredSome = 2 };
 
@@ -73,6 +75,29 @@ cudaError_t allow_smem(K kernel, std::atomic<bool> (&done)[kMaxDevices]) {
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributePreferredSharedMemoryCarveout, int(cudaSharedmemCarveoutMaxShared));
   if (e == cudaSuccess && dev >= 0 && dev < kMaxDevices) done[dev] = true;
   return e;
+}
+
+// Launches `blocks` clusters of `share` blocks.
+template <typename K, typename P>
+cudaError_t launch_cluster(K kernel, int64_t blocks, int threads, size_t smem, int share, cudaStream_t st, const P& p) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(blocks * share));
+  cfg.blockDim = dim3(unsigned(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = unsigned(share);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+// Every thread of the cluster has come here, and sees what the others wrote.
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // Summary of a run of document ids: x the smallest id >= 0 (INT_MAX when there
@@ -102,7 +127,7 @@ __device__ __forceinline__ int scored_class(const ScoredParams& p, int pf, int q
 // Tensor-core paths (bf16, head width a multiple of 8, 16-byte aligned rows).
 // Each returns a cudaError_t; `ok` tells whether a tensor map was refused.
 cudaError_t scored_fwd_tc(const ScoredParams& p, cudaStream_t st, bool* ok);
-cudaError_t scored_bwd_tc(const ScoredParams& p, cudaStream_t st, bool* ok);
+cudaError_t scored_bwd_tc(ScoredParams& p, cudaStream_t st, bool* ok);    // sets p.share
 // The word the tensor-core kernels set when a bounded wait gives up (0: none).
 cudaError_t scored_fwd_error(int* word);
 cudaError_t scored_bwd_error(int* word);

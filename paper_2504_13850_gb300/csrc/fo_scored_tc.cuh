@@ -104,10 +104,12 @@ __device__ __forceinline__ void commit_to(uint64_t* bar) {
 
 // A K- or MN-major operand descriptor whose high word is a constant, so that
 // moving it by `off` bytes within shared memory is a 32-bit addition.
+// (In a cluster the upper bits of a shared-memory address hold the block's
+// rank, which is no part of a descriptor.)
 template <uint32_t LBO>
 struct Operand {
   uint32_t lo;
-  __device__ __forceinline__ explicit Operand(uint32_t addr) : lo((addr >> 4) | (LBO >> 4) << 16) {}
+  __device__ __forceinline__ explicit Operand(uint32_t addr) : lo((addr & 0x3ffff) >> 4 | (LBO >> 4) << 16) {}
   __device__ __forceinline__ uint64_t at(uint32_t off) const {
     constexpr uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);      // stride 1024, version 1, 128-byte swizzle
     return uint64_t(lo + (off >> 4)) | uint64_t(hi) << 32;

@@ -39,7 +39,6 @@ namespace {
 
 constexpr int kT = 64;             // tile of tokens
 constexpr int kThreads = 256;
-constexpr int kMaxShare = 8;       // blocks that share a tile of rows: the portable cluster size
 
 // ------------------------------------------------------------- preparation
 // Document ids padded to Lp (-1 past the sequence), and the summary of each
@@ -351,10 +350,6 @@ struct Share {
     for (; count > 0 && c0 < p.L; --count) c0 = next_tile<KEYS_ARE_ROWS>(p, pf, b, r0, c0 + kT, cls);
     return c0;
   }
-  // Every thread of the cluster has come here, and sees what the others wrote.
-  __device__ __forceinline__ static void sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-  }
   // This thread's value e of block r's buffer x (a shared-memory array at the
   // same place in every block).
   __device__ __forceinline__ static float of(const float* x, int e, int r) {
@@ -458,7 +453,7 @@ __global__ void __launch_bounds__(kThreads, NC <= 4 ? 2 : 1) scored_fwd_k(const 
 #pragma unroll
       for (int n = 0; n < NC; ++n) x[(2 + n) * kThreads] = acc[r][n];
     }
-    Share::sync();
+    cluster_sync();
     if (share.rank == 0) {
 #pragma unroll 1
       for (int o = 1; o < share.n; ++o) {
@@ -474,7 +469,7 @@ __global__ void __launch_bounds__(kThreads, NC <= 4 ? 2 : 1) scored_fwd_k(const 
         }
       }
     }
-    Share::sync();                     // the others' memory has been read
+    cluster_sync();                     // the others' memory has been read
     if (share.rank > 0) return;
   }
   float inv[4];
@@ -633,7 +628,7 @@ __global__ void __launch_bounds__(kThreads, NC <= 4 ? 2 : 1) scored_bwd_k(const 
       }
       if (!KV) x[NC * kThreads] = eps[r];
     }
-    Share::sync();
+    cluster_sync();
     if (share.rank == 0) {
 #pragma unroll 1
       for (int o = 1; o < share.n; ++o) {
@@ -649,7 +644,7 @@ __global__ void __launch_bounds__(kThreads, NC <= 4 ? 2 : 1) scored_bwd_k(const 
         }
       }
     }
-    Share::sync();                     // the others' memory has been read
+    cluster_sync();                     // the others' memory has been read
     if (share.rank > 0) return;
   }
   const float one[4] = {1.f, 1.f, 1.f, 1.f}, sc[4] = {p.scale, p.scale, p.scale, p.scale};
@@ -683,24 +678,6 @@ int shared_by(const ScoredParams& p, int64_t blocks, int64_t tiles, int NC) {
   return n;
 }
 
-template <typename K>
-cudaError_t launch_shared(K kernel, int64_t blocks, size_t smem, cudaStream_t st, const ScoredParams& p) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(blocks * p.share));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = unsigned(p.share);
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[1].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = pdl_enabled() ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, p);
-}
-
 template <typename T, int NC>
 cudaError_t forward_width(ScoredParams p, cudaStream_t st) {
   const int64_t tiles = ceil_div(p.L, kT);
@@ -709,7 +686,7 @@ cudaError_t forward_width(ScoredParams p, cudaStream_t st) {
   const cudaError_t e = allow_smem(scored_fwd_k<T, NC>, allowed);
   if (e != cudaSuccess) return e;
   p.share = shared_by(p, tiles * p.B * p.H, tiles, NC);
-  return launch_shared(scored_fwd_k<T, NC>, tiles * p.B * p.H, smem, st, p);
+  return launch_cluster(scored_fwd_k<T, NC>, tiles * p.B * p.H, kThreads, smem, p.share, st, p);
 }
 template <typename T, int NC>
 cudaError_t backward_width(ScoredParams& p, cudaStream_t st) {
@@ -721,10 +698,10 @@ cudaError_t backward_width(ScoredParams& p, cudaStream_t st) {
   if (e == cudaSuccess) e = allow_smem(scored_bwd_k<T, NC, true>, allowed[1]);
   if (e != cudaSuccess) return e;
   p.share = shared_by(p, tiles * p.B * p.H, tiles, NC);
-  e = launch_shared(scored_bwd_k<T, NC, false>, tiles * p.B * p.H, smem, st, p);
+  e = launch_cluster(scored_bwd_k<T, NC, false>, tiles * p.B * p.H, kThreads, smem, p.share, st, p);
   if (e != cudaSuccess) return e;
   p.share = shared_by(p, tiles * p.B * p.KV, tiles, NC);
-  return launch_shared(scored_bwd_k<T, NC, true>, tiles * p.B * p.KV, smem, st, p);
+  return launch_cluster(scored_bwd_k<T, NC, true>, tiles * p.B * p.KV, kThreads, smem, p.share, st, p);
 }
 // Accumulator columns per thread: 16 NC >= head width.
 template <typename T>
@@ -952,7 +929,7 @@ int fo_attention_backward(const fo_attention_spec* spec, const fo_strided* q, co
   if (e == cudaSuccess && !tc) e = f32 ? backward_simt<float>(p, st) : backward_simt<bf16>(p, st);
   if (e == cudaSuccess && dtable) {
     const int n = p.H * p.buckets;
-    const int64_t parts = int64_t(p.B) * (tc ? ceil_div(p.L, 128) : ceil_div(p.L, kT) * p.share);     // of the kernel that ran
+    const int64_t parts = int64_t(p.B) * ceil_div(p.L, tc ? 128 : kT) * p.share;     // of the kernel that ran
     e = f32 ? launch_k(scored_table_k<float>, dim3((n + 3) / 4), dim3(128), 0, st, p.part, static_cast<float*>(dtable),
                        n, parts)
             : launch_k(scored_table_k<bf16>, dim3((n + 3) / 4), dim3(128), 0, st, p.part, static_cast<bf16*>(dtable),

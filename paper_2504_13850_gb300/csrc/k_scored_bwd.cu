@@ -36,6 +36,9 @@
 // patches through shared memory so that a lane sums a diagonal, into arrays by
 // distance shared by the two warps of a row group, one after the other;
 // patches beyond the reach are one sum per thread.
+// Where the key tiles are fewer than the SMs can take, a cluster of blocks
+// shares one: each walks every n-th block of queries, and the first two add up
+// dV and dK through distributed shared memory, in the order of the ranks.
 // Rounding: P and dS to bf16 before their products, each gradient once (the
 // table's in the table's type).
 #include "fo_scored_tc.cuh"
@@ -105,8 +108,9 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   uint8_t* map = reinterpret_cast<uint8_t*>(dist + 8 * nd);
 
   const int warp = __shfl_sync(0xffffffffu, int(threadIdx.x) / 32, 0), lane = threadIdx.x % 32;
-  const int heads = KV ? p.KV : p.H, tiles = (p.L + 127) / 128, bh = blockIdx.x % (p.B * heads);
-  const int slot0 = int(blockIdx.x / (p.B * heads)), tile = KV ? slot0 : tiles - 1 - slot0;   // longest causal first
+  const int heads = KV ? p.KV : p.H, tiles = (p.L + 127) / 128, share = KV ? p.share : 1,
+            rank = KV ? int(blockIdx.x) % share : 0, work = int(blockIdx.x) / share, bh = work % (p.B * heads);
+  const int slot0 = work / (p.B * heads), tile = KV ? slot0 : tiles - 1 - slot0;   // longest causal first
   const int r0 = tile * 128, b = bh / heads, h0 = KV ? (bh % heads) * p.G : bh % heads, kh = h0 / p.G;
   const int groups = KV ? p.G : 1;
   if (threadIdx.x == 0) {
@@ -166,11 +170,12 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       }
       const uint32_t on = __ballot_sync(0xffffffffu, cls != kScoredNone);
       pads |= __ballot_sync(0xffffffffu, pad);
-      if (cls != kScoredNone)
-        list[n + __popc(on & ((1u << lane) - 1))] =
-            uint16_t((first + lane) | (cls == kScoredSome ? kMasked : 0) | (pad ? kPadded : 0));
+      const uint32_t at = n + __popc(on & ((1u << lane) - 1));
+      if (cls != kScoredNone && int(at) % share == rank)
+        list[int(at) / share] = uint16_t((first + lane) | (cls == kScoredSome ? kMasked : 0) | (pad ? kPadded : 0));
       n += __popc(on);
     }
+    n = (n + uint32_t(share - 1 - rank)) / uint32_t(share);          // of this block
     if (lane == 0) tslot[1] = n | (pads ? 0x80000000u : 0u);
   }
   tc_fence_before();
@@ -182,6 +187,38 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   const bool any_padding = tslot[1] >> 31;
   pdl_trigger();
   Waits wait(&g_err);
+  // Warps of arithmetic: 16 columns g of output o, of the sums of this
+  // thread's row that it stores (each of the four warps of a row group has a
+  // quarter of the columns).
+  auto sums_of = [&](int o, int g, uint32_t (&a)[16]) {
+    if (count > 0) {
+      tmem_ld16_issue(acc + (uint32_t(32 * (warp % 4)) << 16) + o * DP + DP / 4 * (warp / 4) + 16 * g, a);
+      tmem_ld16_wait(a);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) a[e] = 0u;
+    }
+  };
+  auto store = [&](int o, int g, const uint32_t (&a)[16]) {
+    const Strided& out = !KV ? p.dq : o ? p.dk : p.dv;
+    const float mul = KV && !o ? 1.f : p.scale;
+    const int i = r0 + 32 * (warp % 4) + lane, col = DP / 4 * (warp / 4) + 16 * g;
+    if (i >= p.L) return;
+    bf16* row = static_cast<bf16*>(out.p) + b * out.sb + int64_t(i) * out.sl + (KV ? kh : h0) * out.sh;
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      if (col + 8 * e >= p.D) break;
+      uint32_t w[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        w[k] = bf16_pair(__uint_as_float(a[8 * e + 2 * k]) * mul, __uint_as_float(a[8 * e + 2 * k + 1]) * mul);
+      reinterpret_cast<uint4*>(row + col)[e] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  };
+  // Where blocks share a tile: output o is added up by block o; the others
+  // leave theirs where X, Y and the stages were, four values of each thread
+  // together (16 DP / 64 vectors of 512 threads: 64 KB per 64 columns).
+  auto left = [&](int o, int g, int e) { return sm + ((o * (DP / 64) + g) * 4 + e) * 8192 + 16 * int(threadIdx.x); };
 
   if (warp == kTma) {
     if (lane == 0) {
@@ -506,7 +543,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
           }
           asm volatile("bar.sync 9, 512;" ::: "memory");
         }
-        const int64_t parts = int64_t(p.B) * tiles;
+        const int64_t parts = int64_t(p.B) * tiles * share;
         for (int k = warp; k < p.buckets; k += 16) {
           float z = 0.f;
           for (int e = lane; e < 2 * a.reach + 1; e += 32)
@@ -515,7 +552,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
               for (int w = 0; w < 8; ++w) z += dist[w * nd + e];
 #pragma unroll
           for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
-          if (lane == 0) p.part[(int64_t(h0 + g) * p.buckets + k) * parts + int64_t(b) * tiles + tile] = z;
+          if (lane == 0) p.part[(int64_t(h0 + g) * p.buckets + k) * parts + (int64_t(b) * tiles + tile) * share + rank] = z;
         }
         if (g + 1 < groups) {
           asm volatile("bar.sync 9, 512;" ::: "memory");
@@ -539,35 +576,52 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       wait.on_lanes(afull, 0, 37);
       tc_fence_after();
     }
-    // each of the four warps of a row group stores a quarter of the columns
+    if (share > 1 && count == 0) wait.on_lanes(xfull, 0, 41);     // before X and Y are written over
 #pragma unroll 1
-    for (int o = 0; o < (KV ? 2 : 1); ++o) {
-      const Strided& out = !KV ? p.dq : o ? p.dk : p.dv;
-      const float mul = KV && !o ? 1.f : p.scale;
-      bf16* row = static_cast<bf16*>(out.p) + b * out.sb + int64_t(i) * out.sl + (KV ? kh : h0) * out.sh;
+    for (int o = 0; o < (KV ? 2 : 1); ++o)
 #pragma unroll 1
       for (int g = 0; g < DP / 64; ++g) {
-        const int col = DP / 4 * (2 * side + half) + 16 * g;
         uint32_t a[16];
-        if (count > 0) {
-          tmem_ld16_issue(acc + lanes + o * DP + col, a);
-          tmem_ld16_wait(a);
+        if (share > 1 && o == rank) break;
+        sums_of(o, g, a);
+        if (share == 1) {
+          store(o, g, a);
         } else {
 #pragma unroll
-          for (int e = 0; e < 16; ++e) a[e] = 0u;
-        }
-        if (i >= p.L) continue;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          if (col + 8 * e >= p.D) break;
-          uint32_t w[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            w[k] = bf16_pair(__uint_as_float(a[8 * e + 2 * k]) * mul, __uint_as_float(a[8 * e + 2 * k + 1]) * mul);
-          reinterpret_cast<uint4*>(row + col)[e] = make_uint4(w[0], w[1], w[2], w[3]);
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<uint4*>(left(o, g, e)) = make_uint4(a[4 * e], a[4 * e + 1], a[4 * e + 2], a[4 * e + 3]);
         }
       }
+  }
+  if (KV && share > 1) {
+    __syncwarp();
+    cluster_sync();
+    if (warp < kTma && rank < 2) {
+#pragma unroll 1
+      for (int g = 0; g < DP / 64; ++g) {
+        uint32_t a[16];
+        sums_of(rank, g, a);
+#pragma unroll 1
+        for (int r = 0; r < share; ++r) {
+          if (r == rank) continue;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t at, v[4];
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(left(rank, g, e))), "r"(r));
+            asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                         : "r"(at)
+                         : "memory");
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              a[4 * e + k] = __float_as_uint(__uint_as_float(a[4 * e + k]) + __uint_as_float(v[k]));
+          }
+        }
+        store(rank, g, a);
+      }
     }
+    __syncwarp();
+    cluster_sync();                    // the others' memory has been read
   }
   tc_fence_before();
   __syncthreads();
@@ -600,13 +654,37 @@ struct Launch {
     const cudaError_t e = allow_smem(k, allowed);
     if (e != cudaSuccess) return e;
     const int64_t tiles = ceil_div(bp.s.L, 128);
-    return launch_k(k, dim3(unsigned(tiles * bp.s.B * (KV ? bp.s.KV : bp.s.H))), dim3(kThreads), smem, st, bp);
+    if (KV) return launch_cluster(k, tiles * bp.s.B * bp.s.KV, kThreads, smem, bp.s.share, st, bp);
+    return launch_k(k, dim3(unsigned(tiles * bp.s.B * bp.s.H)), dim3(kThreads), smem, st, bp);
   }
 };
 
 }  // namespace
 
-cudaError_t scored_bwd_tc(const ScoredParams& p, cudaStream_t st, bool* ok) {
+// How many blocks (a cluster) share a tile of keys: twice as many while each
+// keeps enough steps of 64 queries to pay for its start and for adding up.
+// Eight will do while every block has an SM of its own (8192 causal tokens, 4
+// heads of 128 on 1: 495 -> 302 us; four did not, 2048 tokens of one head of
+// 64: 44 -> 46 us).  With a causal mask a second block per SM
+// evens out the tiles' lengths from 32 steps on (the same 302 -> 212; 8 steps,
+// 2 x 1024 tokens, 8 heads of 64 on 2, took 56 us against 36), and up to four
+// from 512 on (16384 tokens, 16 heads of 128 on 2: 2.71 -> 2.57 ms; 64 steps,
+// 4 x 2048 tokens, 16 heads of 128 on 4, 293 us against 274).
+int shared_by(const ScoredParams& p) {
+  const int64_t sms = elementwise_blocks(INT64_MAX / 2, kThreads) / 8, blocks = ceil_div(p.L, 128) * p.B * p.KV;
+  const int64_t steps = ceil_div(p.L, 64);
+  int n = 1;
+  while (n < kMaxShare && 2 * n <= steps) {
+    const int64_t grid = 2 * n * blocks, each = steps * p.G / (2 * n);
+    const int64_t room = !p.causal || each < 32 ? sms : each < 512 ? 2 * sms : 4 * sms;
+    if (each < 8 || grid > room) break;
+    n *= 2;
+  }
+  return n;
+}
+
+cudaError_t scored_bwd_tc(ScoredParams& p, cudaStream_t st, bool* ok) {
+  p.share = shared_by(p);
   BwdParams q, k;
   q.s = k.s = p;
   *ok = scored_map(&q.x, p.q, p, p.H, 128) && scored_map(&q.y, p.dout, p, p.H, 128) &&

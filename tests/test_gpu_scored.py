@@ -120,6 +120,14 @@ def test_small_and_full_grids(B, causal, dtype, D):
     check(*make(B, 330, 6, 3, D, dtype, seed=B, bias="bucket", causal=causal, docs="padded"))
 
 
+@pytest.mark.parametrize("H,KV,D", [(2, 1, 64), (4, 1, 128), (3, 1, 40), (2, 2, 128)])
+@pytest.mark.parametrize("docs,bias", [("none", "none"), ("packed", "bucket"), ("mixed", "distance")])
+def test_key_tiles_shared_by_clusters(docs, bias, H, KV, D):
+    """Long sequences with few key heads; documents leave some of a cluster's blocks without work."""
+    for causal in (False, True):
+        check(*make(1, 1100, H, KV, D, BF, seed=H + D, bias=bias, causal=causal, docs=docs))
+
+
 def test_large_scores():
     """Scores far apart, so that the running maximum moves by more than any threshold."""
     for dtype, D in ((BF, 64), (BF, 128), (F32, 64)):
