@@ -18,7 +18,8 @@
 // keys (dQ), then a tile of keys walks the queries (dK, dV and the table
 // gradient); every sum has a fixed order, at the price of forming the scores
 // twice.  The first one adds each row's sum of dS, which the rounding of O
-// keeps from being zero, to D for the second.
+// keeps from being zero, to D for the second.  Where tiles of rows are few, or
+// differ in length under a causal mask, a cluster of blocks shares one (Share).
 // Bound by instruction issue: FMAs are a little over half of the instructions
 // and 16 warps per SM fill a little over half of the slots.  2 x 2048 tokens,
 // 8 heads of 64, fp32: forward 667 us (25.8 TFLOP/s), backward 2.04 ms (21.0,

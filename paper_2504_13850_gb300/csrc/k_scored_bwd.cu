@@ -9,7 +9,7 @@
 //               query head of the group
 //               S^T = X U^T, dP^T = Y W^T,  dV += P^T W, dK += dS^T U, and the
 //               table gradient
-// so each gradient is a sum in one CTA, in a fixed order, without atomics; the
+// so each gradient is a sum in one CTA (or cluster), in a fixed order, without atomics; the
 // price is that S and dP are formed twice (7 products instead of 5).  An
 // alternative that adds dQ in global memory would save two products and lose
 // reproducibility.
@@ -664,8 +664,8 @@ struct Launch {
 // How many blocks (a cluster) share a tile of keys: twice as many while each
 // keeps enough steps of 64 queries to pay for its start and for adding up.
 // Eight will do while every block has an SM of its own (8192 causal tokens, 4
-// heads of 128 on 1: 495 -> 302 us; four did not, 2048 tokens of one head of
-// 64: 44 -> 46 us).  With a causal mask a second block per SM
+// heads of 128 on 1: 495 -> 302 us; 2048 tokens of one head of 64: 44 -> 36,
+// and 46 with four steps each).  With a causal mask a second block per SM
 // evens out the tiles' lengths from 32 steps on (the same 302 -> 212; 8 steps,
 // 2 x 1024 tokens, 8 heads of 64 on 2, took 56 us against 36), and up to four
 // from 512 on (16384 tokens, 16 heads of 128 on 2: 2.71 -> 2.57 ms; 64 steps,
