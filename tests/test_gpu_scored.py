@@ -128,6 +128,13 @@ def test_key_tiles_shared_by_clusters(docs, bias, H, KV, D):
         check(*make(1, 1100, H, KV, D, BF, seed=H + D, bias=bias, causal=causal, docs=docs))
 
 
+@pytest.mark.parametrize("dtype,D", [(BF, 64), (BF, 128), (F32, 64), (F32, 128)])
+def test_largest_clusters(dtype, D):
+    """One head, long enough for clusters of eight blocks."""
+    check(*make(1, 4200, 1, 1, D, dtype, seed=D, bias="bucket", docs="packed"))
+    check(*make(1, 2300, 3, 1, D, dtype, seed=D, cap=20.0, causal=True, prefix=True))
+
+
 def test_large_scores():
     """Scores far apart, so that the running maximum moves by more than any threshold."""
     for dtype, D in ((BF, 64), (BF, 128), (F32, 64)):
