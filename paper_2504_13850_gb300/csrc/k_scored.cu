@@ -73,7 +73,7 @@ __global__ void __launch_bounds__(128) scored_docs_k(const __grid_constant__ Sco
 }
 
 // -D_i = -sum_d dO O and -lse * log2(e), padded to Lp rows per (sequence, head).
-// VEC: 16-byte loads (8 bf16), `lanes` lanes per row; else one warp per row.
+// `lanes` lanes per row, VEC: 16-byte loads (8 bf16).
 // The blocks from row_blocks on summarise the document ids.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) scored_delta_k(const __grid_constant__ ScoredParams p, int lanes,
@@ -919,7 +919,7 @@ int fo_attention_backward(const fo_attention_spec* spec, const fo_strided* q, co
   p.dtable = dtable;
   const int64_t rows = int64_t(p.B) * p.H * p.Lp;
   const bool vec = !f32 && p.D % 8 == 0 && wide(o, spec, spec->heads) && wide(dout, spec, spec->heads);
-  const int lanes = vec ? (p.D <= 64 ? 8 : 16) : 32;
+  const int lanes = p.D <= 32 ? 8 : p.D <= 64 ? (vec ? 8 : 16) : vec ? 16 : 32;
   const unsigned blocks = unsigned((rows + 8 * (32 / lanes) - 1) / (8 * (32 / lanes)));
   const int64_t runs = p.ids ? int64_t(p.B) * (p.Lp / kScoredBlock) : 0;
   auto delta = f32 ? scored_delta_k<float, false> : vec ? scored_delta_k<bf16, true> : scored_delta_k<bf16, false>;
