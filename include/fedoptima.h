@@ -402,6 +402,7 @@ FO_API int fo_column_sums_noalloc(const void* x, int dtype, int64_t rows, int co
  * padding.  P = softmax of z over the allowed keys and O = P V; a row that
  * allows no key gives zeros and lse = -infinity.  Whatever padded tokens
  * hold, NaN included, reaches no output of another token.
+ * The tensors and the stream belong to the current device.
  * Query head h reads key head h / (heads / kv_heads).  Sums, softmax
  * statistics and gradients are held in fp32; P and dS are rounded to the
  * tensors' type where they enter a product on the bf16 tensor-core path.
@@ -470,7 +471,8 @@ FO_API int fo_attention_error(void* stream);
  * The gradient of x is the same call on dy, with no residual and the same
  * (p, seed, call); the residual's gradient is dy.  Use another `call` for
  * each layer and step.  FO_ERR_ARG for p outside [0, 1], an unknown dtype,
- * null or misaligned pointers, negative strides or y_stride < cols.
+ * null or misaligned pointers, negative strides or y_stride < cols.  The
+ * matrices and the stream belong to the current device.
  * ---------------------------------------------------------------------- */
 FO_API int fo_dropout_add(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, void* y,
                    int64_t y_stride, int dtype, int64_t rows, int64_t cols, double p, uint64_t seed,

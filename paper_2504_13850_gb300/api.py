@@ -7,6 +7,7 @@ not been built: there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from array import array
@@ -503,6 +504,15 @@ def _attention_spec(torch, q, k, causal, softcap, scale, slopes, table, buckets,
     return s
 
 
+_here = contextlib.nullcontext()
+
+
+def _device_of(torch, t):
+    """Makes t's device current: launches and default streams go by the current one."""
+    index = t.get_device()
+    return _here if index < 0 or index == torch.cuda.current_device() else torch.cuda.device(index)
+
+
 def _on_stream(torch, q, stream, make):
     """(make(), stream to pass on): what a call allocates belongs to its stream."""
     if stream is None:
@@ -530,13 +540,14 @@ def attention_forward(q, k, v, causal=False, softcap=0.0, scale=None, slopes=Non
         need = L_.fo_attention_workspace(s, 0) if documents is not None else 0
         return o, lse, torch.empty(need, dtype=torch.uint8, device=device) if need > 0 else None, need
 
-    (o, lse, ws, need), st = _on_stream(torch, q, stream, make)
-    flat = _strided(q, (B, L, s.kv_heads, D), (q, "q"), (k, "k", True), (v, "v", True))
-    flat += _contiguous(o, shape) if out is None else _strided(q, None, (o, "out"))
-    args = array("q", flat)             # a third of the time of a ctypes array
-    at, n = args.buffer_info()[0], _fo_strided_bytes
-    _check(L_.fo_attention_forward(s, at, at + n, at + 2 * n, at + 3 * n, lse.data_ptr(),
-                                   ws.data_ptr() if need > 0 else None, need, st), "attention_forward")
+    with _device_of(torch, q):
+        (o, lse, ws, need), st = _on_stream(torch, q, stream, make)
+        flat = _strided(q, (B, L, s.kv_heads, D), (q, "q"), (k, "k", True), (v, "v", True))
+        flat += _contiguous(o, shape) if out is None else _strided(q, None, (o, "out"))
+        args = array("q", flat)             # a third of the time of a ctypes array
+        at, n = args.buffer_info()[0], _fo_strided_bytes
+        _check(L_.fo_attention_forward(s, at, at + n, at + 2 * n, at + 3 * n, lse.data_ptr(),
+                                       ws.data_ptr() if need > 0 else None, need, st), "attention_forward")
     return o, lse
 
 
@@ -560,27 +571,30 @@ def attention_backward(dout, q, k, v, o, lse, causal=False, softcap=0.0, scale=N
         dtable = None if table is None else torch.empty_like(table)
         return g, dq, dk, dv, dtable, torch.empty(need, dtype=torch.uint8, device=device) if need > 0 else None
 
-    (dout, dq, dk, dv, dtable, ws), st = _on_stream(torch, q, stream, make)
-    flat = _strided(q, keys, (q, "q"), (k, "k", True), (v, "v", True), (o, "o"), (dout, "dout"))
-    if grads is None:
-        flat += _contiguous(dq, shape) + _contiguous(dk, keys) + _contiguous(dv, keys)
-    else:
-        flat += _strided(q, keys, (dq, "dq"), (dk, "dk", True), (dv, "dv", True))
-    args = array("q", flat)
-    at, n = args.buffer_info()[0], _fo_strided_bytes
-    _check(L_.fo_attention_backward(
-        s, at, at + n, at + 2 * n, at + 3 * n, _small(lse, (B, H, L), torch.float32, q, "lse"), at + 4 * n, at + 5 * n,
-        at + 6 * n, at + 7 * n, None if dtable is None else dtable.data_ptr(), ws.data_ptr() if need > 0 else None,
-        max(need, 0), st), "attention_backward")
+    with _device_of(torch, q):
+        (dout, dq, dk, dv, dtable, ws), st = _on_stream(torch, q, stream, make)
+        flat = _strided(q, keys, (q, "q"), (k, "k", True), (v, "v", True), (o, "o"), (dout, "dout"))
+        if grads is None:
+            flat += _contiguous(dq, shape) + _contiguous(dk, keys) + _contiguous(dv, keys)
+        else:
+            flat += _strided(q, keys, (dq, "dq"), (dk, "dk", True), (dv, "dv", True))
+        args = array("q", flat)
+        at, n = args.buffer_info()[0], _fo_strided_bytes
+        _check(L_.fo_attention_backward(
+            s, at, at + n, at + 2 * n, at + 3 * n, _small(lse, (B, H, L), torch.float32, q, "lse"), at + 4 * n,
+            at + 5 * n, at + 6 * n, at + 7 * n, None if dtable is None else dtable.data_ptr(),
+            ws.data_ptr() if need > 0 else None, max(need, 0), st), "attention_backward")
     return dq, dk, dv, dtable
 
 
-def attention_error(stream=None):
-    """Waits for `stream` (default: torch's current stream) and raises if a
-    tensor-core attention kernel gave up a bounded wait."""
+def attention_error(stream=None, device=None):
+    """Waits for `stream` (default: torch's current stream) of `device`
+    (default: the current one) and raises if a tensor-core attention kernel
+    gave up a bounded wait there."""
     import torch
-    st = torch.cuda.current_stream().cuda_stream if stream is None else stream
-    _check(lib().fo_attention_error(st), "attention_error")
+    with _here if device is None else torch.cuda.device(device):
+        st = torch.cuda.current_stream().cuda_stream if stream is None else stream
+        _check(lib().fo_attention_error(st), "attention_error")
 
 
 def _matrix(t, like, name):
@@ -613,16 +627,17 @@ def dropout_add(x, residual, p, seed, call, out=None, stream=None):
     def make():
         return torch.empty(shape, dtype=x.dtype, device=x.device)
 
-    if out is None:
-        y, st = _on_stream(torch, x, stream, make)
-        yp, ys = y.data_ptr(), cols
-    else:
-        y, st = out, torch.cuda.current_stream(x.get_device()).cuda_stream if stream is None else stream
-        yp, ys = _matrix(y, x, "out")
-    xp, xs = _matrix(x, x, "x")
-    rp, rs = (None, 0) if residual is None else _matrix(residual, x, "residual")
-    _check(lib().fo_dropout_add(xp, xs, rp, rs, yp, ys, dtype, x.numel() // cols if cols else 0, cols, p,
-                                seed & (2**64 - 1), call & (2**64 - 1), st), "dropout_add")
+    with _device_of(torch, x):
+        if out is None:
+            y, st = _on_stream(torch, x, stream, make)
+            yp, ys = y.data_ptr(), cols
+        else:
+            y, st = out, torch.cuda.current_stream(x.get_device()).cuda_stream if stream is None else stream
+            yp, ys = _matrix(y, x, "out")
+        xp, xs = _matrix(x, x, "x")
+        rp, rs = (None, 0) if residual is None else _matrix(residual, x, "residual")
+        _check(lib().fo_dropout_add(xp, xs, rp, rs, yp, ys, dtype, x.numel() // cols if cols else 0, cols, p,
+                                    seed & (2**64 - 1), call & (2**64 - 1), st), "dropout_add")
     return y
 
 
