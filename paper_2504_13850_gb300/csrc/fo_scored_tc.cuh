@@ -218,8 +218,9 @@ struct Ring {
   }
 };
 
-// Bias kinds, compile-time in the kernels.
+// Bias kinds and caps, compile-time in the kernels.
 enum { kBiasNone = 0, kBiasSlope = 1, kBiasTable = 2 };
+enum { kCapNone = 0, kCapPlain = 1, kCapLarge = 2 };
 
 // The table's biases by distance, extended by kExt on both sides with the
 // outermost values: a patch of up to 32 x 64 scores that is not entirely
@@ -234,64 +235,91 @@ __device__ __forceinline__ void load_bias(float* bias, const ScoredParams& p, in
 
 // N scores (fp32 bits) of one query row, keys j0 .. j0 + N - 1 -> score units:
 // the cap (KEEP: ch receives its derivative 1 - tanh^2 as pairs of fp16, a
-// factor in [0, 1] of a product that is itself rounded to bf16) and the bias.  DIR is +1 when the columns are keys and -1 when they are queries
-// (the row then is the key); d = distance of column 0, lo and hi the bounds of
-// the warp's distances.
-// tanh y = 1 - 2 q with q = 1 / (1 + e^2y), whose derivative is 4 q (1 - q).
-// In the forward pass, where every |y| of the warp's patch is at most 1/2, as
-// scores well below the cap are, its Taylor series to y^11 instead (the next
-// term is below 4.5e-7 there), which takes no special-function operation
-// against two per score: scoring 2 x 4095 tokens, 16 heads of 128, with a
-// prefix took 203 us against 223.  The backward pass, whose special-function
-// unit is less busy, ran 3% slower with it.
+// factor in [0, 1] of a product that is itself rounded to bf16; below 6e-5
+// its spacing is 2^-24, what 1 - t^2 in fp32 leaves as well) and the bias.
+// DIR is +1 when the columns are keys and -1 when they are queries (the row
+// then is the key); d = distance of column 0, lo and hi the bounds of the
+// warp's distances.
+// Two forms of tanh y: 1 - 2 q with q = 1 / (1 + e^2y), whose derivative is
+// 4 q (1 - q), and up to |y| = kSeriesEnd the Taylor series to y^11 (the next
+// term is below 6e-8 of the sum there).  The first has an absolute error of
+// about 1.7e-7 (q to 2 units in the last place), so a score is off by 1.7e-7
+// of the cap however small it is: up to caps of kPlainCap 1.1e-5, which P's
+// rounding to bf16 hides 300 times over.  Above it (kCapLarge) each score takes
+// the form that is exact for it, the same one forward and backward; as a branch
+// at run time instead of a kernel of its own it cost the backward pass of 4 x
+// 2048 tokens, 16 heads of 128 on 4, 6% (274 -> 292 us) at a cap of 50.
+// In the forward pass a warp whose patch has only |y| up to kSeriesEnd, as
+// scores well below the cap have, takes the series alone, which needs no
+// special-function operation against two per score: scoring 2 x 4095 tokens,
+// 16 heads of 128, with a prefix took 203 us against 223.  The backward pass,
+// whose special-function unit is less busy, ran 3% slower with it.
+constexpr float kSeriesEnd = 0.4f, kPlainCap = 64.f;
 struct Shape {
   float cap, cap_in, y_in;      // the cap; scale to 2 y log2(e) and to y
   float slope;                  // negated, in score units
   const float* bias;
   int reach;
 };
-template <int N, int BIAS, bool CAP, int DIR, bool KEEP>
+__device__ __forceinline__ F2 tanh_series(F2 y) {
+  const F2 z = mul2(y, y);
+  F2 t = fma2(z, f2(-1382.f / 155925.f, -1382.f / 155925.f), f2(62.f / 2835.f, 62.f / 2835.f));
+  t = fma2(z, t, f2(-17.f / 315.f, -17.f / 315.f));
+  t = fma2(z, t, f2(2.f / 15.f, 2.f / 15.f));
+  t = fma2(z, t, f2(-1.f / 3.f, -1.f / 3.f));
+  return fma2(mul2(z, t), y, y);
+}
+template <int N, int BIAS, int CAP, int DIR, bool KEEP>
 __device__ __forceinline__ void shape_scores(uint32_t (&r)[N], uint32_t* ch, const Shape& a, int d, int lo, int hi) {
   if (CAP) {
-    const F2 one = f2(1.f, 1.f), cap = f2(a.cap, a.cap);
+    const F2 one = f2(1.f, 1.f), cap = f2(a.cap, a.cap), in = f2(a.cap_in, a.cap_in), y_in = f2(a.y_in, a.y_in),
+             two = f2(-2.f * a.cap, -2.f * a.cap);
+    // scores e and e + 1 by the exponential; the second form (and ch)
+    auto by_exponential = [&](int e, float& u, float& v) {
+      float x, y;
+      split(mul2(f2u(r[e], r[e + 1]), in), x, y);
+      split(add2(f2(ex2(x), ex2(y)), one), x, y);
+      const F2 q = f2(rcp(x), rcp(y));
+      if (KEEP) {
+        split(mul2(mul2(f2(4.f, 4.f), q), fma2(q, f2(-1.f, -1.f), one)), x, y);
+        const __half2 h = __floats2half2_rn(x, y);
+        ch[e / 2] = *reinterpret_cast<const uint32_t*>(&h);
+      }
+      split(fma2(two, q, cap), u, v);
+    };
     bool small = false;
     if (!KEEP) {
       float top = 0.f;
 #pragma unroll
       for (int e = 0; e < N; e += 2) top = max3(top, fabsf(__uint_as_float(r[e])), fabsf(__uint_as_float(r[e + 1])));
-      small = __all_sync(0xffffffffu, top * a.y_in <= 0.5f);
+      small = __all_sync(0xffffffffu, top * a.y_in <= kSeriesEnd);
     }
     if (small) {
-      const F2 in = f2(a.y_in, a.y_in);
 #pragma unroll
       for (int e = 0; e < N; e += 2) {
-        const F2 y = mul2(f2u(r[e], r[e + 1]), in), z = mul2(y, y);
-        F2 t = fma2(z, f2(-1382.f / 155925.f, -1382.f / 155925.f), f2(62.f / 2835.f, 62.f / 2835.f));
-        t = fma2(z, t, f2(-17.f / 315.f, -17.f / 315.f));
-        t = fma2(z, t, f2(2.f / 15.f, 2.f / 15.f));
-        t = fma2(z, t, f2(-1.f / 3.f, -1.f / 3.f));
-        t = fma2(mul2(z, t), y, y);                       // tanh y
         float u, v;
-        split(mul2(t, cap), u, v);
+        split(mul2(tanh_series(mul2(f2u(r[e], r[e + 1]), y_in)), cap), u, v);
+        r[e] = __float_as_uint(u);
+        r[e + 1] = __float_as_uint(v);
+      }
+    } else if (CAP == kCapPlain) {
+#pragma unroll
+      for (int e = 0; e < N; e += 2) {
+        float u, v;
+        by_exponential(e, u, v);
         r[e] = __float_as_uint(u);
         r[e + 1] = __float_as_uint(v);
       }
     } else {
-      const F2 in = f2(a.cap_in, a.cap_in), two = f2(-2.f * a.cap, -2.f * a.cap);
 #pragma unroll
       for (int e = 0; e < N; e += 2) {
-        float x, y;
-        split(mul2(f2u(r[e], r[e + 1]), in), x, y);
-        split(add2(f2(ex2(x), ex2(y)), one), x, y);
-        const F2 q = f2(rcp(x), rcp(y));
-        if (KEEP) {
-          split(mul2(mul2(f2(4.f, 4.f), q), fma2(q, f2(-1.f, -1.f), one)), x, y);
-          const __half2 h = __floats2half2_rn(x, y);
-          ch[e / 2] = *reinterpret_cast<const uint32_t*>(&h);
-        }
-        split(fma2(two, q, cap), x, y);
-        r[e] = __float_as_uint(x);
-        r[e + 1] = __float_as_uint(y);
+        float u, v, x, y, s, t;
+        by_exponential(e, u, v);
+        const F2 at = mul2(f2u(r[e], r[e + 1]), y_in);
+        split(at, x, y);
+        split(mul2(tanh_series(at), cap), s, t);
+        r[e] = __float_as_uint(fabsf(x) <= kSeriesEnd ? s : u);
+        r[e + 1] = __float_as_uint(fabsf(y) <= kSeriesEnd ? t : v);
       }
     }
   }
@@ -339,13 +367,15 @@ __device__ __forceinline__ void clear_padding(char* tile, int rows, int subs, co
 }
 
 // Calls f.template operator()<BIAS, CAP>() for the bias and cap of p.
+template <int CAP, typename Fn>
+cudaError_t with_bias(const ScoredParams& p, Fn f) {
+  return p.table ? f.template operator()<kBiasTable, CAP>()
+                 : p.slopes ? f.template operator()<kBiasSlope, CAP>() : f.template operator()<kBiasNone, CAP>();
+}
 template <typename Fn>
 cudaError_t with_shape(const ScoredParams& p, Fn f) {
-  if (p.cap > 0.f)
-    return p.table ? f.template operator()<kBiasTable, true>()
-                   : p.slopes ? f.template operator()<kBiasSlope, true>() : f.template operator()<kBiasNone, true>();
-  return p.table ? f.template operator()<kBiasTable, false>()
-                 : p.slopes ? f.template operator()<kBiasSlope, false>() : f.template operator()<kBiasNone, false>();
+  return p.cap > kPlainCap ? with_bias<kCapLarge>(p, f)
+                           : p.cap > 0.f ? with_bias<kCapPlain>(p, f) : with_bias<kCapNone>(p, f);
 }
 
 // Tensor map of [batch][len][heads][head_dim] as {head_dim, len, heads, batch}

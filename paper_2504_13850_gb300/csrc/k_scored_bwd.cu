@@ -82,7 +82,7 @@ struct Bwd {
   __host__ __device__ static int dist_floats(int reach) { return (2 * reach + 1 + 3) / 4 * 4; }
 };
 
-template <int DP, bool KV, int BIAS, bool CAP>
+template <int DP, bool KV, int BIAS, int CAP>
 __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_constant__ BwdParams bp) {
   using F = Bwd<DP, KV>;
   const ScoredParams& p = bp.s;
@@ -636,7 +636,7 @@ struct Launch {
   BwdParams& bp;
   cudaStream_t st;
   bool* ok;
-  template <int BIAS, bool CAP>
+  template <int BIAS, int CAP>
   cudaError_t operator()() const {
     using F = Bwd<DP, KV>;
     const bool grad = KV && bp.s.dtable;

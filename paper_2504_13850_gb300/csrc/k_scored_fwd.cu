@@ -20,8 +20,8 @@
 // sums and bf16's exponent hold without loss.
 // Scores stay in raw units x with exponent factor c (scale * log2(e), or
 // log2(e) after a cap), so an uncapped, unbiased score costs half a packed FMA
-// and one exponential.  The cap's tanh (shape_scores) has an absolute error of
-// a few 2^-24, against the 2^-11 relative error of the hardware's tanh.
+// and one exponential.  The cap's tanh (shape_scores) is off by 2e-7 of one at
+// most, against the 2^-11 relative error of the hardware's tanh.
 // The bias kind and the cap are template parameters: the branches cost
 // instruction fetches even when not taken.
 // Rounding: P~ to bf16 before its product, O once when stored.
@@ -88,7 +88,7 @@ __device__ __forceinline__ float max_of(const uint32_t (&r)[32]) {
   return fmaxf(max3(m[0], m[1], m[2]), m[3]);
 }
 
-template <int DP, int NT, int BIAS, bool CAP>
+template <int DP, int NT, int BIAS, int CAP>
 __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k(const __grid_constant__ FwdParams fp) {
   using F = Fwd<DP, NT>;
   const ScoredParams& p = fp.s;
@@ -411,7 +411,7 @@ template <int DP, int NT>
 struct Launch {
   const FwdParams& fp;
   cudaStream_t st;
-  template <int BIAS, bool CAP>
+  template <int BIAS, int CAP>
   cudaError_t operator()() const {
     using F = Fwd<DP, NT>;
     const size_t smem = F::smem(fp.s.L, BIAS == kBiasTable);
