@@ -776,6 +776,13 @@ bool wide(const fo_strided* t, const fo_attention_spec* s, int heads) {
   return reinterpret_cast<uintptr_t>(t->data) % 16 == 0;
 }
 
+// They also hold biases in units of the scale and the scale in units of the
+// cap, which has to stay within fp32's range.
+bool ordinary(const fo_attention_spec* s) {
+  auto within = [](float x) { return x >= 0x1p-60f && x <= 0x1p60f; };
+  return within(s->scale) && (s->softcap == 0.f || within(s->softcap));
+}
+
 struct Layout {
   int64_t doc = 0, blk = 0, lse2 = 0, delta = 0, part = 0, bytes = 0;
 };
@@ -875,8 +882,8 @@ int fo_attention_forward(const fo_attention_spec* spec, const fo_strided* q, con
   cudaError_t e = cudaSuccess;
   const int64_t runs = int64_t(p.B) * (p.Lp / kScoredBlock);
   if (p.ids) e = launch_k(scored_docs_k, dim3(unsigned((runs + 3) / 4)), dim3(128), 0, st, p);
-  bool tc = spec->dtype == FO_DTYPE_BF16 && p.D % 8 == 0 && wide(q, spec, p.H) && wide(k, spec, p.KV) &&
-            wide(v, spec, p.KV) && wide(o, spec, p.H);
+  bool tc = spec->dtype == FO_DTYPE_BF16 && p.D % 8 == 0 && ordinary(spec) && wide(q, spec, p.H) &&
+            wide(k, spec, p.KV) && wide(v, spec, p.KV) && wide(o, spec, p.H);
   if (e == cudaSuccess && tc) e = scored_fwd_tc(p, st, &tc);
   if (e == cudaSuccess && !tc) e = spec->dtype == FO_DTYPE_F32 ? forward_simt<float>(p, st) : forward_simt<bf16>(p, st);
   return e == cudaSuccess ? FO_OK : cuda_error(e);
@@ -924,8 +931,8 @@ int fo_attention_backward(const fo_attention_spec* spec, const fo_strided* q, co
   const int64_t runs = p.ids ? int64_t(p.B) * (p.Lp / kScoredBlock) : 0;
   auto delta = f32 ? scored_delta_k<float, false> : vec ? scored_delta_k<bf16, true> : scored_delta_k<bf16, false>;
   cudaError_t e = launch_k(delta, dim3(blocks + unsigned((runs + 7) / 8)), dim3(256), 0, st, p, lanes, blocks);
-  bool tc = vec && wide(q, spec, p.H) && wide(k, spec, p.KV) && wide(v, spec, p.KV) && wide(dq, spec, p.H) &&
-            wide(dk, spec, p.KV) && wide(dv, spec, p.KV);
+  bool tc = vec && ordinary(spec) && wide(q, spec, p.H) && wide(k, spec, p.KV) && wide(v, spec, p.KV) &&
+            wide(dq, spec, p.H) && wide(dk, spec, p.KV) && wide(dv, spec, p.KV);
   if (e == cudaSuccess && tc) e = scored_bwd_tc(p, st, &tc);
   if (e == cudaSuccess && !tc) e = f32 ? backward_simt<float>(p, st) : backward_simt<bf16>(p, st);
   if (e == cudaSuccess && dtable) {
