@@ -402,6 +402,11 @@ FO_API int fo_column_sums_noalloc(const void* x, int dtype, int64_t rows, int co
  * padding.  P = softmax of z over the allowed keys and O = P V; a row that
  * allows no key gives zeros and lse = -infinity.  Whatever padded tokens
  * hold, NaN included, reaches no output of another token.
+ * A finite table entry beyond +-2^15 counts as +-2^15, so that a row of
+ * nothing but keys masked that way (-1e9, the type's lowest value) keeps a
+ * softmax over them in both passes; an infinite one counts as it is.  The
+ * backward pass forms P from lse, whose rounding leaves it a relative error
+ * of 2e-7 |lse|: scores in the tens of thousands are beyond it.
  * The tensors and the stream belong to the current device.
  * Query head h reads key head h / (heads / kv_heads).  Sums, softmax
  * statistics and gradients are held in fp32; P and dS are rounded to the

@@ -60,6 +60,16 @@ constexpr int kMaxShare = 8;      // the portable cluster size
 enum { kScoredNone = 0, kScoredAll = 1, kScoredSome = 2 };
 
 #ifdef __CUDACC__
+// A table's entry as a bias: finite ones end at +-2^15.  Beside a key of
+// ordinary score the probability is 0 (or 1) all the same; but a row of nothing
+// but keys masked by -1e9 or the type's lowest value would lose its scores in
+// the bias's rounding forward, and backward, where P comes from lse, give
+// anything from 0 to infinity.
+__device__ __forceinline__ float bias_of(float t) {
+  constexpr float kEnd = 32768.f;
+  return fabsf(t) > kEnd && !isinf(t) ? copysignf(kEnd, t) : t;
+}
+
 // Sets a kernel's shared-memory limits the first time it is launched on the
 // current device (`done`: one flag per device, static in the launcher).
 constexpr int kMaxDevices = 64;

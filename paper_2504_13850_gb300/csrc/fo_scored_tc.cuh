@@ -230,7 +230,7 @@ constexpr int kBiasFloats = 2 * kMaxReach + 2 * kExt + 4;
 __device__ __forceinline__ void load_bias(float* bias, const ScoredParams& p, int h, float inv_unit, int tid, int n) {
   const bf16* t = static_cast<const bf16*>(p.table) + int64_t(h) * p.buckets;
   for (int e = tid; e < 2 * p.reach + 1 + 2 * kExt; e += n)
-    bias[e] = __bfloat162float(t[p.map[min(max(e - kExt, 0), 2 * p.reach)]]) * inv_unit;
+    bias[e] = bias_of(__bfloat162float(t[p.map[min(max(e - kExt, 0), 2 * p.reach)]])) * inv_unit;
 }
 
 // N scores (fp32 bits) of one query row, keys j0 .. j0 + N - 1 -> score units:

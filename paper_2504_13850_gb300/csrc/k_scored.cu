@@ -260,7 +260,7 @@ template <typename T>
 __device__ __forceinline__ void load_bias(float* bias, const ScoredParams& p, int h) {
   if (!p.table) return;
   const T* t = static_cast<const T*>(p.table) + int64_t(h) * p.buckets;
-  for (int e = threadIdx.x; e < 2 * p.reach + 1; e += kThreads) bias[e] = to_f(t[p.map[e]]);
+  for (int e = threadIdx.x; e < 2 * p.reach + 1; e += kThreads) bias[e] = bias_of(to_f(t[p.map[e]]));
 }
 
 // What decides on a pair besides its positions.
