@@ -459,8 +459,9 @@ FO_API int fo_attention_backward(const fo_attention_spec* spec, const fo_strided
                           const fo_strided* dq, const fo_strided* dk, const fo_strided* dv, void* dtable,
                           void* workspace, int64_t workspace_bytes, void* stream);
 /* Waits for `stream` and reports FO_ERR_TIMEOUT if a tensor-core attention
- * kernel of this process gave up a bounded wait on the current device, whose
- * outputs are then void (FO_OK otherwise; no counterpart in the paper). */
+ * kernel of this process gave up a bounded wait on the current device, on any
+ * stream, since the calling thread last asked; outputs of calls in between may
+ * then be void (FO_OK otherwise; no counterpart in the paper). */
 FO_API int fo_attention_error(void* stream);
 
 /* ------------------------------------------------------------------------

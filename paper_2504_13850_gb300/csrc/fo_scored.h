@@ -138,8 +138,9 @@ __device__ __forceinline__ int scored_class(const ScoredParams& p, int pf, int q
 // Each returns a cudaError_t; `ok` tells whether a tensor map was refused.
 cudaError_t scored_fwd_tc(const ScoredParams& p, cudaStream_t st, bool* ok);
 cudaError_t scored_bwd_tc(ScoredParams& p, cudaStream_t st, bool* ok);    // sets p.share
-// The word the tensor-core kernels set when a bounded wait gives up (0: none).
-cudaError_t scored_fwd_error(int* word);
-cudaError_t scored_bwd_error(int* word);
+// The code of a bounded wait that gave up on the current device since `told`
+// (which is brought up to date), 0 for none.
+cudaError_t scored_fwd_error(unsigned* told, int* code);
+cudaError_t scored_bwd_error(unsigned* told, int* code);
 
 }  // namespace fo

@@ -116,16 +116,40 @@ struct Operand {
   }
 };
 
+// What a kernel's waits that gave up leave on a device: the last one's code and
+// how many threads did.  The count only grows: each host thread holds what it
+// has been told of.
+struct GaveUp {
+  int code;
+  unsigned count;
+};
+// The code of a wait that gave up since this thread last asked (`told`), or 0.
+template <typename Symbol>
+cudaError_t gave_up_since(const Symbol& symbol, unsigned* told, int* code) {
+  GaveUp now;
+  const cudaError_t e = cudaMemcpyFromSymbol(&now, symbol, sizeof(now));
+  *code = 0;
+  if (e != cudaSuccess || now.count == *told) return e;
+  *told = now.count;
+  *code = now.code;
+  return e;
+}
+
 // A role's waits: after one has given up (about two seconds) the rest return
-// at once, so the kernel ends soon and its error word is set.
+// at once, so the kernel ends soon and says so in `err`.
 struct Waits {
-  int* err;
+  GaveUp* err;
+  uint64_t limit;
   bool dead = false;
-  __device__ __forceinline__ explicit Waits(int* e) : err(e) {}
-  __device__ __forceinline__ void on(uint64_t* bar, uint32_t parity, int code) {
-    if (dead || mbar_wait(bar, parity)) return;
-    atomicExch(err, code);
+  __device__ __forceinline__ explicit Waits(GaveUp* e, uint64_t ns = kWaitLimit) : err(e), limit(ns) {}
+  __device__ __forceinline__ void give_up(int code) {
+    atomicExch(&err->code, code);
+    atomicAdd(&err->count, 1u);
     dead = true;
+  }
+  __device__ __forceinline__ void on(uint64_t* bar, uint32_t parity, int code) {
+    if (dead || mbar_wait(bar, parity, limit)) return;
+    give_up(code);
   }
   // The same for the lanes of a warp of arithmetic, converged afterwards.
   __device__ __forceinline__ void on_lanes(uint64_t* bar, uint32_t parity, int code) {
@@ -139,10 +163,9 @@ struct Waits {
     while (true) {
       for (int i = 0; i < 64; ++i)
         if (__all_sync(0xffffffffu, mbar_try_wait(bar, parity))) return;
-      if (__any_sync(0xffffffffu, global_ns() - t0 > 2000000000ull)) break;
+      if (__any_sync(0xffffffffu, global_ns() - t0 > limit)) break;
     }
-    atomicExch(err, code);
-    dead = true;
+    give_up(code);
   }
 };
 

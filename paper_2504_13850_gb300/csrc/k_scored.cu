@@ -947,12 +947,15 @@ int fo_attention_backward(const fo_attention_spec* spec, const fo_strided* q, co
 }
 
 int fo_attention_error(void* stream) {
+  static thread_local unsigned told[kMaxDevices][2];     // what this thread has reported
+  int dev = 0, fwd = 0, bwd = 0;
   cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
-  int word = 0;
-  if (e == cudaSuccess) e = scored_fwd_error(&word);
-  if (e == cudaSuccess && !word) e = scored_bwd_error(&word);
+  if (e == cudaSuccess) e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = scored_fwd_error(&told[dev % kMaxDevices][0], &fwd);
+  if (e == cudaSuccess) e = scored_bwd_error(&told[dev % kMaxDevices][1], &bwd);
   if (e != cudaSuccess) return cuda_error(e);
-  return word ? report_error(FO_ERR_TIMEOUT, "an attention kernel timed out waiting (code " + std::to_string(word) + ")") : FO_OK;
+  if (!fwd && !bwd) return FO_OK;
+  return report_error(FO_ERR_TIMEOUT, "an attention kernel timed out waiting (code " + std::to_string(fwd ? fwd : bwd) + ")");
 }
 
 }  // extern "C"

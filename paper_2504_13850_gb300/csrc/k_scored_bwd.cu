@@ -47,7 +47,7 @@ namespace fo {
 
 namespace {
 
-__device__ int g_err;     // set by a wait that gave up
+__device__ GaveUp g_err;
 
 struct BwdParams {
   ScoredParams s;
@@ -697,6 +697,6 @@ cudaError_t scored_bwd_tc(ScoredParams& p, cudaStream_t st, bool* ok) {
   return p.D <= 64 ? with_shape(p, Launch<64, true>{k, st, ok}) : with_shape(p, Launch<128, true>{k, st, ok});
 }
 
-cudaError_t scored_bwd_error(int* word) { return cudaMemcpyFromSymbol(word, g_err, sizeof(int)); }
+cudaError_t scored_bwd_error(unsigned* told, int* code) { return gave_up_since(g_err, told, code); }
 
 }  // namespace fo

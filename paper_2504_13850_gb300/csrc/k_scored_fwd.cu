@@ -31,7 +31,7 @@ namespace fo {
 
 namespace {
 
-__device__ int g_err;     // set by a wait that gave up
+__device__ GaveUp g_err;
 
 struct FwdParams {
   ScoredParams s;
@@ -439,6 +439,6 @@ cudaError_t scored_fwd_tc(const ScoredParams& p, cudaStream_t st, bool* ok) {
   return p.D <= 64 ? with_shape(p, Launch<64, 2>{fp, st}) : with_shape(p, Launch<128, 2>{fp, st});
 }
 
-cudaError_t scored_fwd_error(int* word) { return cudaMemcpyFromSymbol(word, g_err, sizeof(int)); }
+cudaError_t scored_fwd_error(unsigned* told, int* code) { return gave_up_since(g_err, told, code); }
 
 }  // namespace fo
