@@ -13,6 +13,7 @@ f_d, then the upload of its split-point activations, which the server trains on
     python -m paper_2504_13850_gb300.sequence
 """
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import api
 from . import workloads as W
@@ -33,6 +34,7 @@ class PackedAttention(torch.autograd.Function):
         return o
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do):
         qkv, table, documents, o, lse = ctx.saved_tensors
         q, k, v = qkv.unbind(2)
@@ -51,6 +53,7 @@ class ResidualDropout(torch.autograd.Function):
         return api.dropout_add(x, residual, p, seed, call)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         dy = dy.contiguous()
         return api.dropout_grad(dy, *ctx.mask), dy, None, None, None
