@@ -68,7 +68,7 @@ struct Bwd {
   static constexpr int kStage = 2 * kU + (KV ? 1024 : 0);
   static constexpr bool kSplit = KV && DP == 128;          // P handed over before dS
   static constexpr int kBufs = KV && DP == 128 ? 2 : 3;     // TMEM buffers of S and dP; the sums follow
-  static constexpr int kBars = 1 + 3 * kMaxStages + 4 * kBufs + 1;
+  static constexpr int kBars = 1 + 3 * kMaxStages + 4 * kBufs + 2;
   // X, Y, stages, barriers (and the TMEM slot and the number of blocks), the
   // list of blocks, row sums of dS, bias, table-gradient arrays
   __host__ __device__ static int list_bytes(int L) { return (L + 511) / 512 * 16; }
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   uint64_t* bars = reinterpret_cast<uint64_t*>(ring + stages * F::kStage);
   uint64_t *xfull = bars, *full = bars + 1, *empty = full + kMaxStages, *clean = empty + kMaxStages,
            *sfull = clean + kMaxStages, *pfull = sfull + F::kBufs, *dfull = pfull + F::kBufs,
-           *tfull = dfull + F::kBufs, *afull = tfull + F::kBufs;
+           *tfull = dfull + F::kBufs, *afull = tfull + F::kBufs, *done = afull + 1;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + F::kBars);
   // blocks of 64 columns with allowed pairs, in ascending order: the index,
   // with kMasked where some pairs are not allowed and kPadded where there is
@@ -127,6 +127,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       mbar_init(&tfull[e], 8);           // dS written
     }
     mbar_init(afull, 1);
+    mbar_init(done, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kMma) {
@@ -247,10 +248,9 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
           }
         }
       }
-      if (wait.dead) {   // let the copies in flight land before the block ends
-        mbar_wait(xfull, 0);
-        for (int e = max(0, it - stages); e < it; ++e) mbar_wait(&full[e % stages], (e / stages) & 1);
-      }
+      // every copy has landed before the block ends, whichever role gave up
+      mbar_wait(xfull, 0);
+      for (int e = max(0, it - stages); e < it; ++e) mbar_wait(&full[e % stages], (e / stages) & 1);
     }
   } else if (warp == kMma) {
     constexpr uint32_t id_s = instr_desc(64, false, false), id_a = instr_desc(DP, false, true);
@@ -309,6 +309,10 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       // off the waits' path; what was issued after one gave up is void anyway
       if (__any_sync(0xffffffffu, wait.dead)) break;
     }
+    // no product is in flight when the block ends and its memory is another's
+    commit_to(done);
+    mbar_wait(done, 0);
+    __syncwarp();
   } else if (warp == kClean) {
     if (any_padding) {
       const int32_t* doc = p.doc + int64_t(b) * p.Lp;

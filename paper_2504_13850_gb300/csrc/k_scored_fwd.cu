@@ -45,7 +45,7 @@ struct Fwd {
   static constexpr int kStages = NT == 2 ? (DP == 64 ? 6 : 4) : (DP == 64 ? 4 : 2);
   static constexpr int kThreads = 256 * NT + (NT == 2 ? 96 : 64);
   static constexpr int kCols = NT == 2 ? 512 : 256;         // TMEM columns
-  static constexpr int kBars = 1 + 3 * kStages + 3 * NT;
+  static constexpr int kBars = 2 + 3 * kStages + 3 * NT;
   static constexpr int kOps = (NT + kStages) * kTileBytes;
   static constexpr int kXch = 2 * NT * 256;                 // floats: [step parity][tile][half][row]
   // operands, barriers (and the TMEM slot), exchanged maxima, bias, bitmaps
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
   char* ring = sm + NT * F::kTileBytes;
   uint64_t* bars = reinterpret_cast<uint64_t*>(sm + F::kOps);
   uint64_t *qfull = bars, *full = bars + 1, *empty = full + F::kStages, *clean = empty + F::kStages,
-           *sfull = clean + F::kStages, *pfull = sfull + NT, *ofull = pfull + NT;
+           *sfull = clean + F::kStages, *pfull = sfull + NT, *ofull = pfull + NT, *done = ofull + NT;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(bars + F::kBars);
   float* xch = reinterpret_cast<float*>(bars + F::kBars + 1);
   float* bias = xch + F::kXch;
@@ -134,6 +134,7 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
       mbar_init(&pfull[e], 8);         // one arrival per warp
       mbar_init(&ofull[e], 1);
     }
+    mbar_init(done, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   __syncwarp();
@@ -197,10 +198,9 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
             tma_4d(ring + at.at * F::kTileBytes + s * F::kSub, kv ? &fp.v : &fp.k, &full[at.at], 64 * s, jb * 128, kh, b);
           at.step();
         }
-      if (wait.dead) {   // let the copies in flight land before the block ends
-        mbar_wait(qfull, 0);
-        for (int e = max(0, it - F::kStages); e < it; ++e) mbar_wait(&full[e % F::kStages], (e / F::kStages) & 1);
-      }
+      // every copy has landed before the block ends, whichever role gave up
+      mbar_wait(qfull, 0);
+      for (int e = max(0, it - F::kStages); e < it; ++e) mbar_wait(&full[e % F::kStages], (e / F::kStages) & 1);
     }
   } else if (warp == kMma) {
     constexpr uint32_t id_s = instr_desc(128, false, false), id_o = instr_desc(DP, false, true);
@@ -263,6 +263,10 @@ __global__ void __launch_bounds__(Fwd<DP, NT>::kThreads, 3 - NT) scored_fwd_tc_k
       // off the waits' path; what was issued after one gave up is void anyway
       if (__any_sync(0xffffffffu, wait.dead)) break;
     }
+    // no product is in flight when the block ends and its memory is another's
+    commit_to(done);
+    mbar_wait(done, 0);
+    __syncwarp();
   } else if (warp < kTma) {
     const int t = warp / 8, half = warp / 4 % 2, quarter = warp % 4, row = 32 * quarter + lane;
     const int i0 = q0 + 128 * t + 32 * quarter, i = i0 + lane;
