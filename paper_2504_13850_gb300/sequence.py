@@ -109,6 +109,10 @@ class SequenceDevice:
         pooled = (x.float() * valid).sum(1) / lengths[:, None]
         loss = torch.nn.functional.cross_entropy(pooled @ self.head.t(), labels.long())
         loss.backward()
+        # waits for the step's work, so that x may be uploaded from another
+        # stream; a kernel that gave up a wait ends the step before it changes
+        # a parameter
+        api.attention_error()
         self.opt.step()
         self.steps += 1
         return x.detach(), loss.detach()
@@ -131,10 +135,8 @@ def run(events=32, devices=4, seed=0, vocab=30522):
         tokens, lengths, labels = data[k]
         x, loss = parts[k].step(tokens, lengths, labels)
         local.append(loss)
-        torch.cuda.current_stream().synchronize()        # the upload runs on the server's copy stream
         if server.enqueue_activations(k, x, labels, lengths)[0] == api.OK:
             server.server_step()
-    api.attention_error()
     server.synchronize()
     server.check_error()
     losses = server.read_losses(0, events)
