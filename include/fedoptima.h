@@ -412,6 +412,10 @@ FO_API int fo_column_sums_noalloc(const void* x, int dtype, int64_t rows, int co
  * statistics and gradients are held in fp32; P and dS are rounded to the
  * tensors' type where they enter a product on the bf16 tensor-core path.
  * All sums have a fixed order: equal calls give equal bits.
+ * bf16 calls run on the tensor cores where head_dim is a multiple of 8, every
+ * tensor starts on a 16-byte boundary and every stride of a dimension longer
+ * than one is a positive multiple of 8 elements; any other bf16 call runs like
+ * fp32, 10 to 100 times slower.
  * ---------------------------------------------------------------------- */
 typedef struct fo_strided {  /* [batch][len][heads][head_dim], innermost stride 1 */
   void* data;                /* device pointer                                  */

@@ -521,10 +521,27 @@ def _on_stream(torch, q, stream, make):
         return make(), stream
 
 
+def _dense_gradient(torch, g):
+    """`g`, or a contiguous copy where its strides would refuse it (an innermost
+    one other than 1) or keep bf16 from the tensor cores: autograd hands over
+    gradients broadcast by a sum or a mean, which the caller never chose."""
+    if g.dim() != 4 or g.is_contiguous() and g.data_ptr() % 16 == 0:
+        return g
+    *outer, inner = g.stride()
+    if inner == 1 or g.shape[3] == 1:
+        if g.dtype != torch.bfloat16 or g.shape[3] % 8:
+            return g
+        if g.data_ptr() % 16 == 0 and all(n == 1 or s >= 8 and s % 8 == 0 for n, s in zip(g.shape, outer)):
+            return g
+    return g.clone(memory_format=torch.contiguous_format)
+
+
 def attention_forward(q, k, v, causal=False, softcap=0.0, scale=None, slopes=None, table=None, buckets=None,
                       documents=None, prefix=None, out=None, stream=None):
     """fo_attention_forward: (o, lse) of q [B, L, H, D], k and v [B, L, KV, D]
-    (any strides with the innermost 1).  scale defaults to D ** -0.5;
+    (any strides with the innermost 1; bf16 runs on the tensor cores where D,
+    the strides and the addresses are multiples of 8 elements, and 10 to 100
+    times slower elsewhere).  scale defaults to D ** -0.5;
     `buckets` is the table's host map (relative_buckets).  Runs on `stream`
     (a cudaStream_t), by default torch's current stream."""
     import torch
@@ -564,7 +581,7 @@ def attention_backward(dout, q, k, v, o, lse, causal=False, softcap=0.0, scale=N
     need = L_.fo_attention_workspace(s, 1)
 
     def make():
-        g = dout.contiguous() if dout.dim() == 4 and dout.stride(3) != 1 else dout    # as sum().backward() gives it
+        g = _dense_gradient(torch, dout)
         dq, dk, dv = grads if grads is not None else (
             torch.empty(shape, dtype=dtype, device=device), torch.empty(keys, dtype=dtype, device=device),
             torch.empty(keys, dtype=dtype, device=device))
