@@ -40,6 +40,8 @@ namespace {
 
 constexpr int kT = 64;             // tile of tokens
 constexpr int kThreads = 256;
+constexpr int kBiasPart = 2 * kMaxReach + 4;              // floats in shared memory of a head's biases
+constexpr int kGradPart = kBiasPart + 256;                // and of its table gradient: by distance, and beyond the reach
 
 // ------------------------------------------------------------- preparation
 // Document ids padded to Lp (-1 past the sequence), and the summary of each
@@ -496,8 +498,8 @@ __global__ void __launch_bounds__(kThreads, NC <= 4 ? 2 : 1) scored_bwd_k(const 
   constexpr int kTile = WD * kT;
   float *X = sm, *Y = X + kTile, *UWs = Y + kTile, *P = UWs + 4 * kTile;        // UWs: two pairs of U and W
   float* bias = P + kT * kT;
-  float* dist = bias + 2 * kMaxReach + 4;          // KV true: table gradient by distance
-  float* far = dist + 2 * kMaxReach + 4;           // [2][128] sums beyond the reach
+  float* dist = bias + kBiasPart;                  // KV true: table gradient by distance
+  float* far = dist + kBiasPart;                   // [2][128] sums beyond the reach
   pdl_wait();
   pdl_trigger();
   const int heads = KV ? p.KV : p.H, tiles = (p.L + kT - 1) / kT;
@@ -664,16 +666,22 @@ __global__ void __launch_bounds__(kThreads, NC <= 4 ? 2 : 1) scored_bwd_k(const 
   }
 }
 
+// Blocks of `smem` bytes that an SM holds (228 KB with 1 KB reserved for each);
+// registers allow two up to head width 64 and one above.  The backward passes
+// with a table at widths 33 to 64 do not fit twice: taken for two, 2 x 200
+// tokens, 8 heads of 64, took 134 us instead of 107, and 1000 causal ones 337
+// instead of 260.
+int per_sm(size_t smem, int NC) { return NC <= 4 && 2 * (smem + 1024) <= 233472 ? 2 : 1; }
+
 // How many blocks share a tile of rows (Share): twice as many while the grid
-// still fits the SMs, each of which holds two blocks up to head width 64 and
-// one above.  4 sequences of 200 tokens, 4 heads of 32, took 25.6 / 93.9 us
-// forward / backward with a block each and take 23.5 / 73.7.  With a causal
-// mask, whose tiles of rows differ in length, up to twice what fits: the
+// still fits the SMs.  4 sequences of 200 tokens, 4 heads of 32, took 25.6 /
+// 93.9 us forward / backward with a block each and take 23.5 / 73.7.  With a
+// causal mask, whose tiles of rows differ in length, up to twice what fits: the
 // longest are half as long and start first (2 x 1000 causal tokens, 8 heads of
 // 64: 145 / 544 us -> 102 / 314); equal tiles only pay for it (16 x 128
 // tokens, 8 heads of 64: 32.8 / 175 us against 38.9 / 235).
-int shared_by(const ScoredParams& p, int64_t blocks, int64_t tiles, int NC) {
-  const int64_t sms = elementwise_blocks(INT64_MAX / 2, kThreads) / 8, room = sms * (NC <= 4 ? 2 : 1) * (p.causal ? 2 : 1);
+int shared_by(const ScoredParams& p, int64_t blocks, int64_t tiles, int per) {
+  const int64_t sms = elementwise_blocks(INT64_MAX / 2, kThreads) / 8, room = sms * per * (p.causal ? 2 : 1);
   int n = 1;
   while (n < kMaxShare && 2 * n <= tiles && 2 * n * blocks <= room) n *= 2;
   return n;
@@ -682,27 +690,29 @@ int shared_by(const ScoredParams& p, int64_t blocks, int64_t tiles, int NC) {
 template <typename T, int NC>
 cudaError_t forward_width(ScoredParams p, cudaStream_t st) {
   const int64_t tiles = ceil_div(p.L, kT);
-  const size_t smem = (size_t(5 * 16 * NC * kT) + kT * kT + (p.table ? 2 * kMaxReach + 4 : 0)) * sizeof(float);
+  const size_t smem = (size_t(5 * 16 * NC * kT) + kT * kT + (p.table ? kBiasPart : 0)) * sizeof(float);
   static std::atomic<bool> allowed[kMaxDevices];
   const cudaError_t e = allow_smem(scored_fwd_k<T, NC>, allowed);
   if (e != cudaSuccess) return e;
-  p.share = shared_by(p, tiles * p.B * p.H, tiles, NC);
+  p.share = shared_by(p, tiles * p.B * p.H, tiles, per_sm(smem, NC));
   return launch_cluster(scored_fwd_k<T, NC>, tiles * p.B * p.H, kThreads, smem, p.share, st, p);
 }
 template <typename T, int NC>
 cudaError_t backward_width(ScoredParams& p, cudaStream_t st) {
   const int64_t tiles = ceil_div(p.L, kT);
-  const size_t smem =
-      (size_t(6 * 16 * NC * kT) + kT * kT + (p.table ? 2 * (2 * kMaxReach + 4) + 256 : 0)) * sizeof(float);
+  // the query pass needs the bias, the key pass the table gradient as well
+  const size_t tile_bytes = (size_t(6 * 16 * NC * kT) + kT * kT) * sizeof(float);
+  const size_t queries = tile_bytes + (p.table ? kBiasPart * sizeof(float) : 0);
+  const size_t keys = tile_bytes + (p.table ? (kBiasPart + (p.dtable ? kGradPart : 0)) * sizeof(float) : 0);
   static std::atomic<bool> allowed[2][kMaxDevices];
   cudaError_t e = allow_smem(scored_bwd_k<T, NC, false>, allowed[0]);
   if (e == cudaSuccess) e = allow_smem(scored_bwd_k<T, NC, true>, allowed[1]);
   if (e != cudaSuccess) return e;
-  p.share = shared_by(p, tiles * p.B * p.H, tiles, NC);
-  e = launch_cluster(scored_bwd_k<T, NC, false>, tiles * p.B * p.H, kThreads, smem, p.share, st, p);
+  p.share = shared_by(p, tiles * p.B * p.H, tiles, per_sm(queries, NC));
+  e = launch_cluster(scored_bwd_k<T, NC, false>, tiles * p.B * p.H, kThreads, queries, p.share, st, p);
   if (e != cudaSuccess) return e;
-  p.share = shared_by(p, tiles * p.B * p.KV, tiles, NC);
-  return launch_cluster(scored_bwd_k<T, NC, true>, tiles * p.B * p.KV, kThreads, smem, p.share, st, p);
+  p.share = shared_by(p, tiles * p.B * p.KV, tiles, per_sm(keys, NC));
+  return launch_cluster(scored_bwd_k<T, NC, true>, tiles * p.B * p.KV, kThreads, keys, p.share, st, p);
 }
 // Accumulator columns per thread: 16 NC >= head width.
 template <typename T>
