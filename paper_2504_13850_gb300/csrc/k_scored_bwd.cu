@@ -71,13 +71,27 @@ struct Bwd {
   static constexpr int kBars = 1 + 3 * kMaxStages + 4 * kBufs + 2;
   // X, Y, stages, barriers (and the TMEM slot and the number of blocks), the
   // list of blocks, row sums of dS, bias, table-gradient arrays
-  __host__ __device__ static int list_bytes(int L) { return (L + 511) / 512 * 16; }
-  static size_t smem(int L, int stages, bool table, bool grad, int reach) {
-    size_t n = 1024 + 2 * kX + size_t(stages) * kStage + 8 * (kBars + 1) + list_bytes(L);
+  // (of one of `share` blocks that divide the list)
+  __host__ __device__ static int list_bytes(int L, int share) {
+    const int steps = (L + 63) / 64;
+    return ((steps + share - 1) / share + 7) / 8 * 16;
+  }
+  static size_t smem(int L, int share, int stages, bool table, bool grad, int reach) {
+    size_t n = 1024 + 2 * kX + size_t(stages) * kStage + 8 * (kBars + 1) + list_bytes(L, share);
     if (!KV) n += 4 * 8 * 128;
     if (table) n += 4 * kBiasFloats;
     if (grad) n += 4 * (16 * kPatch + 8 * dist_floats(reach)) + 2 * kMaxReach + 4;
     return n;
+  }
+  // Stages that fit in shared memory, 0 where too few do: kBufs steps are in
+  // flight.  Only the keys of widths above 64 with the gradient of a table whose
+  // reach is above about 380 can be too large, because of the list of a sequence
+  // of 780,000 tokens (reach 512) and more.
+  static int stages(const ScoredParams& p) {
+    const int share = KV ? p.share : 1;
+    int n = kMaxStages;
+    while (n >= kBufs && smem(p.L, share, n, p.table, KV && p.dtable, p.reach) > kSmemLimit) --n;
+    return n < kBufs ? 0 : n;
   }
   __host__ __device__ static int dist_floats(int reach) { return (2 * reach + 1 + 3) / 4 * 4; }
 };
@@ -99,7 +113,8 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   // with kMasked where some pairs are not allowed and kPadded where there is
   // padding
   uint16_t* list = reinterpret_cast<uint16_t*>(bars + F::kBars + 1);
-  float* rowsum = reinterpret_cast<float*>(reinterpret_cast<char*>(list) + F::list_bytes(p.L));   // KV false: [2][4][128]
+  float* rowsum = reinterpret_cast<float*>(reinterpret_cast<char*>(list) +
+                                             F::list_bytes(p.L, KV ? p.share : 1));   // KV false: [2][4][128]
   float* bias = rowsum + (KV ? 0 : 1024);
   const bool grad = KV && BIAS == kBiasTable && p.dtable;
   float* patch = bias + (BIAS == kBiasTable ? kBiasFloats : 0);
@@ -639,29 +654,30 @@ template <int DP, bool KV>
 struct Launch {
   BwdParams& bp;
   cudaStream_t st;
-  bool* ok;
   template <int BIAS, int CAP>
   cudaError_t operator()() const {
     using F = Bwd<DP, KV>;
-    const bool grad = KV && bp.s.dtable;
-    int stages = kMaxStages;
-    auto need = [&](int n) { return F::smem(bp.s.L, n, BIAS == kBiasTable, grad, bp.s.reach); };
-    while (stages > F::kBufs && need(stages) > kSmemLimit) --stages;   // kBufs steps are in flight: fewer would not do
-    if (need(stages) > kSmemLimit) {      // the list of a sequence of half a million tokens and more
-      *ok = false;
-      return cudaSuccess;
-    }
-    bp.s.stages = stages;
-    const size_t smem = need(stages);
+    const ScoredParams& s = bp.s;
+    const size_t smem = F::smem(s.L, KV ? s.share : 1, s.stages, BIAS == kBiasTable, KV && s.dtable, s.reach);
     auto k = scored_bwd_tc_k<DP, KV, BIAS, CAP>;
     static std::atomic<bool> allowed[kMaxDevices];
     const cudaError_t e = allow_smem(k, allowed);
     if (e != cudaSuccess) return e;
-    const int64_t tiles = ceil_div(bp.s.L, 128);
-    if (KV) return launch_cluster(k, tiles * bp.s.B * bp.s.KV, kThreads, smem, bp.s.share, st, bp);
-    return launch_k(k, dim3(unsigned(tiles * bp.s.B * bp.s.H)), dim3(kThreads), smem, st, bp);
+    const int64_t tiles = ceil_div(s.L, 128);
+    if (KV) return launch_cluster(k, tiles * s.B * s.KV, kThreads, smem, s.share, st, bp);
+    return launch_k(k, dim3(unsigned(tiles * s.B * s.H)), dim3(kThreads), smem, st, bp);
   }
 };
+// Both launches, or none where one does not fit.
+template <int DP>
+cudaError_t launch_both(BwdParams& queries, BwdParams& keys, cudaStream_t st, bool* ok) {
+  queries.s.stages = Bwd<DP, false>::stages(queries.s);
+  keys.s.stages = Bwd<DP, true>::stages(keys.s);
+  *ok = queries.s.stages > 0 && keys.s.stages > 0;
+  if (!*ok) return cudaSuccess;
+  const cudaError_t e = with_shape(queries.s, Launch<DP, false>{queries, st});
+  return e != cudaSuccess ? e : with_shape(keys.s, Launch<DP, true>{keys, st});
+}
 
 }  // namespace
 
@@ -696,9 +712,7 @@ cudaError_t scored_bwd_tc(ScoredParams& p, cudaStream_t st, bool* ok) {
         scored_map(&k.x, p.k, p, p.KV, 128) && scored_map(&k.y, p.v, p, p.KV, 128) &&
         scored_map(&k.u, p.q, p, p.H, 64) && scored_map(&k.w, p.dout, p, p.H, 64);
   if (!*ok) return cudaSuccess;
-  cudaError_t e = p.D <= 64 ? with_shape(p, Launch<64, false>{q, st, ok}) : with_shape(p, Launch<128, false>{q, st, ok});
-  if (e != cudaSuccess || !*ok) return e;
-  return p.D <= 64 ? with_shape(p, Launch<64, true>{k, st, ok}) : with_shape(p, Launch<128, true>{k, st, ok});
+  return p.D <= 64 ? launch_both<64>(q, k, st, ok) : launch_both<128>(q, k, st, ok);
 }
 
 cudaError_t scored_bwd_error(unsigned* told, int* code) { return gave_up_since(g_err, told, code); }
