@@ -487,6 +487,8 @@ def _attention_spec(torch, q, k, causal, softcap, scale, slopes, table, buckets,
     else:
         raise ValueError("q, k, v: bf16 or fp32")
     B, L, H, D = q.shape
+    if max(B, L, H, k.shape[2], D) >= 1 << 31:
+        raise ValueError("q, k, v: sizes below 2^31")
     s = fo_attention_spec(B, L, H, k.shape[2], D, dtype, 1 if causal else 0, 0, 0,
                           (D ** -0.5 if D else 0.0) if scale is None else scale, softcap)
     if slopes is not None:
