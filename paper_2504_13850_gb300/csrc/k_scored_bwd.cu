@@ -31,7 +31,8 @@
 // query pass, launched first, sums its dS rows in fp32 and adds the sum to D,
 // so that dK and the table gradient come from the exact D.  Where a tile walks
 // at most two blocks, as in sequences of up to 128 tokens, whose few keys feel
-// the error most, it sums P dP over the row first and dQ has the exact D too.
+// the error most, it sums P dP over the row first and dQ has the exact D too
+// (which of the two a tile takes goes by its mask: documents and prefixes too).
 // The table gradient sums dS in fp32 by distance: each warp turns 32 x 16
 // patches through shared memory so that a lane sums a diagonal, into arrays by
 // distance shared by the two warps of a row group, one after the other;
@@ -679,8 +680,6 @@ cudaError_t launch_both(BwdParams& queries, BwdParams& keys, cudaStream_t st, bo
   return e != cudaSuccess ? e : with_shape(keys.s, Launch<DP, true>{keys, st});
 }
 
-}  // namespace
-
 // How many blocks (a cluster) share a tile of keys: twice as many while each
 // keeps enough steps of 64 queries to pay for its start and for adding up.
 // Eight will do while every block has an SM of its own (8192 causal tokens, 4
@@ -702,6 +701,8 @@ int shared_by(const ScoredParams& p) {
   }
   return n;
 }
+
+}  // namespace
 
 cudaError_t scored_bwd_tc(ScoredParams& p, cudaStream_t st, bool* ok) {
   p.share = shared_by(p);
