@@ -4,17 +4,17 @@
 // One kernel body, launched twice.  A CTA keeps a tile of 128 rows of X and Y
 // in shared memory and walks blocks of 64 rows of U and W:
 //   KV = false  rows are queries:  X = Q, Y = dO, U = K, W = V
-//               S = X U^T, dP = Y W^T,  dQ += dS U
+//               S = X U^T, dP = Y W^T,  dQ += dS U, and P U
 //   KV = true   rows are keys:     X = K, Y = V, U = Q, W = dO, over every
 //               query head of the group
 //               S^T = X U^T, dP^T = Y W^T,  dV += P^T W, dK += dS^T U, and the
 //               table gradient
 // so each gradient is a sum in one CTA (or cluster), in a fixed order, without atomics; the
-// price is that S and dP are formed twice (7 products instead of 5).  An
-// alternative that adds dQ in global memory would save two products and lose
+// price is that S and dP are formed twice, and P U (8 products instead of 5).  An
+// alternative that adds dQ in global memory would save three products and lose
 // reproducibility.
 // S and dP take 64 TMEM columns each, in three buffers where the sums leave
-// room (two for keys of a head width above 64): two groups of 256 threads
+// room (two for head widths above 64): two groups of 256 threads
 // process alternate blocks, so that one's arithmetic runs while the other's
 // products do, and a third buffer keeps the scores one block ahead.  A row is
 // shared by two threads, 32 columns each, which form P from all 32 at once and
@@ -26,13 +26,17 @@
 // accumulating products; no score touches shared memory.  Row statistics
 // (scored_delta_k) are per column where rows are keys and ride along in each
 // stage.
-// D = dO . O carries the rounding of O, which would leave each row's dS with a
-// sum of -dD instead of 0, most of it in whichever bucket holds most keys: the
-// query pass, launched first, sums its dS rows in fp32 and adds the sum to D,
-// so that dK and the table gradient come from the exact D.  Where a tile walks
-// at most two blocks, as in sequences of up to 128 tokens, whose few keys feel
-// the error most, it sums P dP over the row first and dQ has the exact D too
-// (which of the two a tile takes goes by its mask: documents and prefixes too).
+// D = dO . O carries the rounding of O (and the truncating sums of the tensor
+// cores that formed it), which would leave each row's dS with a sum of -dD
+// instead of 0, most of it in whichever bucket holds most keys, and dQ with
+// -dD P K.  The query pass, launched first, sums its dS rows in fp32.  The sum
+// goes into D for the second launch, so that dK and the table gradient come
+// from the exact D, and sum * P K is taken off dQ at the end, which costs the
+// product P U.  Without it dQ was off by 0.3% beside the roundings' 0.24% with
+// values of mean 0, and with values of mean 1 by 1.6% at 16384 keys and 13% at
+// 131072, where the gradients that are left are small beside D; it takes 2 to
+// 7% of the backward pass (4 x 2048 capped tokens 275 -> 286 us, 16384 tokens
+// 1369 -> 1462).
 // The table gradient sums dS in fp32 by distance: each warp turns 32 x 16
 // patches through shared memory so that a lane sums a diagonal, into arrays by
 // distance shared by the two warps of a row group, one after the other;
@@ -67,8 +71,8 @@ struct Bwd {
   static constexpr int kU = DP / 64 * 8192;         // 64 rows
   static constexpr int kStats = KV ? 512 : 0;       // lse and D of 64 queries
   static constexpr int kStage = 2 * kU + (KV ? 1024 : 0);
-  static constexpr bool kSplit = KV && DP == 128;          // P handed over before dS
-  static constexpr int kBufs = KV && DP == 128 ? 2 : 3;     // TMEM buffers of S and dP; the sums follow
+  static constexpr bool kSplit = DP == 128;                // P handed over before dS
+  static constexpr int kBufs = DP == 128 ? 2 : 3;          // TMEM buffers of S and dP; the sums follow
   static constexpr int kBars = 1 + 3 * kMaxStages + 4 * kBufs + 2;
   // X, Y, stages, barriers (and the TMEM slot and the number of blocks), the
   // list of blocks, row sums of dS, bias, table-gradient arrays
@@ -79,7 +83,7 @@ struct Bwd {
   }
   static size_t smem(int L, int share, int stages, bool table, bool grad, int reach) {
     size_t n = 1024 + 2 * kX + size_t(stages) * kStage + 8 * (kBars + 1) + list_bytes(L, share);
-    if (!KV) n += 4 * 8 * 128;
+    if (!KV) n += 4 * 4 * 128;
     if (table) n += 4 * kBiasFloats;
     if (grad) n += 4 * (16 * kPatch + 8 * dist_floats(reach)) + 2 * kMaxReach + 4;
     return n;
@@ -115,8 +119,8 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   // padding
   uint16_t* list = reinterpret_cast<uint16_t*>(bars + F::kBars + 1);
   float* rowsum = reinterpret_cast<float*>(reinterpret_cast<char*>(list) +
-                                             F::list_bytes(p.L, KV ? p.share : 1));   // KV false: [2][4][128]
-  float* bias = rowsum + (KV ? 0 : 1024);
+                                             F::list_bytes(p.L, KV ? p.share : 1));   // KV false: [4][128]
+  float* bias = rowsum + (KV ? 0 : 512);
   const bool grad = KV && BIAS == kBiasTable && p.dtable;
   float* patch = bias + (BIAS == kBiasTable ? kBiasFloats : 0);
   float* dist = patch + 16 * kPatch;
@@ -283,20 +287,18 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       if (n >= 0) {
         const uint32_t a = tmem + 128 * buf.at;
         const Operand<8192> u(ring_at + slot * F::kStage), w(ring_at + slot * F::kStage + F::kU);
-        if (KV) {
-          wait.on_lanes(F::kSplit ? &pfull[buf.at] : &tfull[buf.at], buf.phase, 34);
-          tc_fence_after();
+        wait.on_lanes(F::kSplit ? &pfull[buf.at] : &tfull[buf.at], buf.phase, 34);
+        tc_fence_after();
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            mma_ts(acc, a + 32 * (e >> 1) + 8 * (e & 1), w.at(2048 * e), id_a, e > 0 ? 1u : uint32_t(n));
-        }
-        if (!KV || F::kSplit) {
+        for (int e = 0; e < 4; ++e)
+          mma_ts(acc, a + 32 * (e >> 1) + 8 * (e & 1), (KV ? w : u).at(2048 * e), id_a, e > 0 ? 1u : uint32_t(n));
+        if (F::kSplit) {
           wait.on_lanes(&tfull[buf.at], buf.phase, 39);
           tc_fence_after();
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          mma_ts(acc + (KV ? DP : 0), a + 64 + 32 * (e >> 1) + 8 * (e & 1), u.at(2048 * e), id_a,
+          mma_ts(acc + DP, a + 64 + 32 * (e >> 1) + 8 * (e & 1), u.at(2048 * e), id_a,
                  e > 0 ? 1u : uint32_t(n));
         commit_to(&empty[slot]);
         if (n + 1 == total) commit_to(afull);
@@ -357,7 +359,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     const int edge = KV ? (i >= p.L ? INT32_MAX : p.causal && i >= pf ? i : 0) : min(p.causal ? max(i + 1, pf) : p.L, p.L);
     const int64_t stat = (int64_t(b) * p.H + h0) * p.Lp + i;
     const float row_lse = KV ? 0.f : p.lse2[stat];
-    float row_d = KV ? 0.f : p.delta[stat];
+    const float row_d = KV ? 0.f : p.delta[stat];
     const F2 c2 = f2(c, c);
     F2 eps = f2(0.f, 0.f);                 // KV false: sum of this thread's dS
     float lo_sum = 0.f, hi_sum = 0.f;      // table gradient beyond the reach
@@ -365,13 +367,6 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
     float* my_dist = dist + (4 * side + quarter) * nd;
     const int pair = 1 + 4 * side + quarter;
     int slot = side, phase = 0;              // this side's stage in shared memory
-    // the sum of a value over the four threads of a row (all warps of arithmetic)
-    auto row_total = [&](float d) {
-      float* z = rowsum + 512 + 32 * quarter + lane;
-      z[128 * (2 * side + half)] = d;
-      asm volatile("bar.sync 9, 512;" ::: "memory");
-      return (z[0] + z[128]) + (z[256] + z[384]);
-    };
     Ring<F::kBufs, 2> buf(side);             // this side's buffer
     for (int g = 0; g < groups; ++g) {
       const Shape a = shape_of(p, h0 + g, unit, bias);
@@ -426,7 +421,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
             }
           }
         }
-        if (KV) {
+        {
           uint32_t w[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) w[e] = bf16_pair(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
@@ -440,20 +435,6 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         // dS = P (dP - D)
         wait.on_lanes(&dfull[buf.at], buf.phase, 40);
         tc_fence_after();
-        if (!KV && count <= 2) {
-          // the whole row is at hand: D = sum P dP, exactly
-          float d = 0.f;
-#pragma unroll
-          for (int pass = 0; pass < 2; ++pass) {
-            uint32_t t[16];
-            tmem_ld16_issue(d_col + 16 * pass, t);
-            tmem_ld16_wait(t);
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (s[16 * pass + e] != 0u) d = fmaf(__uint_as_float(s[16 * pass + e]), __uint_as_float(t[e]), d);
-          }
-          row_d = -row_total(d);
-        }
 #pragma unroll
         for (int pass = 0; pass < 2; ++pass) {
           uint32_t t[16];
@@ -581,24 +562,35 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         }
       }
     }
+    float off = 0.f;                       // KV false: the row's sum of dS, what D is off by
     if (!KV) {
-      if (count == 1 && side == 1) row_d = -row_total(0.f);       // the other side has the only block
       float x, y;
       split(eps, x, y);
-      rowsum[(2 * side + half) * 128 + 32 * quarter + lane] = x + y;
+      float* z = rowsum + 32 * quarter + lane;
+      z[(2 * side + half) * 128] = x + y;
       asm volatile("bar.sync 9, 512;" ::: "memory");
-      if (warp < 4 && i < p.L) {
-        const float* z = rowsum + 32 * quarter + lane;
-        p.delta[stat] = row_d - ((z[0] + z[128]) + (z[256] + z[384]));
-      }
+      off = (z[0] + z[128]) + (z[256] + z[384]);
+      if (warp < 4 && i < p.L) p.delta[stat] = row_d - off;
     }
     if (count > 0) {
       wait.on_lanes(afull, 0, 37);
       tc_fence_after();
     }
     if (share > 1 && count == 0) wait.on_lanes(xfull, 0, 41);     // before X and Y are written over
+    if (!KV) {
 #pragma unroll 1
-    for (int o = 0; o < (KV ? 2 : 1); ++o)
+      for (int g = 0; g < DP / 64; ++g) {
+        uint32_t a[16], pu[16];
+        sums_of(1, g, a);
+        sums_of(0, g, pu);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          a[e] = __float_as_uint(fmaf(-off, __uint_as_float(pu[e]), __uint_as_float(a[e])));
+        store(1, g, a);
+      }
+    }
+#pragma unroll 1
+    for (int o = 0; o < (KV ? 2 : 0); ++o)
 #pragma unroll 1
       for (int g = 0; g < DP / 64; ++g) {
         uint32_t a[16];
@@ -683,12 +675,12 @@ cudaError_t launch_both(BwdParams& queries, BwdParams& keys, cudaStream_t st, bo
 // How many blocks (a cluster) share a tile of keys: twice as many while each
 // keeps enough steps of 64 queries to pay for its start and for adding up.
 // Eight will do while every block has an SM of its own (8192 causal tokens, 4
-// heads of 128 on 1: 495 -> 302 us; 2048 tokens of one head of 64: 44 -> 36,
-// and 46 with four steps each).  With a causal mask a second block per SM
-// evens out the tiles' lengths from 32 steps on (the same 302 -> 212; 8 steps,
+// heads of 128 on 1: 488 -> 305 us; 2048 tokens of one head of 64: 46 -> 36,
+// and 48 with four steps each).  With a causal mask a second block per SM
+// evens out the tiles' lengths from 32 steps on (the same 305 -> 216; 8 steps,
 // 2 x 1024 tokens, 8 heads of 64 on 2, took 56 us against 36), and up to four
-// from 512 on (16384 tokens, 16 heads of 128 on 2: 2.71 -> 2.57 ms; 64 steps,
-// 4 x 2048 tokens, 16 heads of 128 on 4, 293 us against 274).
+// from 512 on (16384 tokens, 16 heads of 128 on 2: 2.87 -> 2.75 ms; 64 steps,
+// 4 x 2048 tokens, 16 heads of 128 on 4, 308 us against 289).
 int shared_by(const ScoredParams& p) {
   const int64_t sms = elementwise_blocks(INT64_MAX / 2, kThreads) / 8, blocks = ceil_div(p.L, 128) * p.B * p.KV;
   const int64_t steps = ceil_div(p.L, 64);
