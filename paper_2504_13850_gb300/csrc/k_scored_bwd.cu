@@ -21,7 +21,8 @@
 // dS in two passes of 16.  S is handed over before dP, whose products run
 // while P is formed; P is handed over before dS where there are only two
 // buffers (capped 2048: 294 -> 275 us, causal 16384 of width 128: 1510 ->
-// 1400; with three the extra wait cost what it gained).  P and dS go back to
+// 1400; with three the extra wait cost what it gained; so it did for queries
+// under a cap, whose P is formed with dS).  P and dS go back to
 // TMEM as bf16 over the scores they came from, as A operands of the
 // accumulating products; no score touches shared memory.  Row statistics
 // (scored_delta_k) are per column where rows are keys and ride along in each
@@ -31,12 +32,12 @@
 // instead of 0, most of it in whichever bucket holds most keys, and dQ with
 // -dD P K.  The query pass, launched first, sums its dS rows in fp32.  The sum
 // goes into D for the second launch, so that dK and the table gradient come
-// from the exact D, and sum * P K is taken off dQ at the end, which costs the
-// product P U.  Without it dQ was off by 0.3% beside the roundings' 0.24% with
-// values of mean 0, and with values of mean 1 by 1.6% at 16384 keys and 13% at
-// 131072, where the gradients that are left are small beside D; it takes 2 to
-// 7% of the backward pass (4 x 2048 capped tokens 275 -> 286 us, 16384 tokens
-// 1369 -> 1462).
+// from the exact D, and sum * P K (under a cap each pair with its derivative,
+// like dS) is taken off dQ at the end, which costs the product P U.  Without it
+// dQ was off by 0.3% beside the roundings' 0.24% with values of mean 0, and with
+// values of mean 1 by 1.6% at 16384 keys and 13% at 131072, where the gradients
+// that are left are small beside D; it takes 2 to 8% of the backward pass (16384
+// tokens 1369 -> 1455 us, 4 x 2048 capped tokens 275 -> 297).
 // The table gradient sums dS in fp32 by distance: each warp turns 32 x 16
 // patches through shared memory so that a lane sums a diagonal, into arrays by
 // distance shared by the two warps of a row group, one after the other;
@@ -71,7 +72,6 @@ struct Bwd {
   static constexpr int kU = DP / 64 * 8192;         // 64 rows
   static constexpr int kStats = KV ? 512 : 0;       // lse and D of 64 queries
   static constexpr int kStage = 2 * kU + (KV ? 1024 : 0);
-  static constexpr bool kSplit = DP == 128;                // P handed over before dS
   static constexpr int kBufs = DP == 128 ? 2 : 3;          // TMEM buffers of S and dP; the sums follow
   static constexpr int kBars = 1 + 3 * kMaxStages + 4 * kBufs + 2;
   // X, Y, stages, barriers (and the TMEM slot and the number of blocks), the
@@ -104,6 +104,9 @@ struct Bwd {
 template <int DP, bool KV, int BIAS, int CAP>
 __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_constant__ BwdParams bp) {
   using F = Bwd<DP, KV>;
+  // the cap's derivative multiplies P as well (rows are queries)
+  constexpr bool kChained = !KV && CAP;
+  constexpr bool kSplit = DP == 128 && !kChained;            // P handed over before dS
   const ScoredParams& p = bp.s;
   extern __shared__ __align__(1024) char smem_raw[];
   char* sm = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);    // 1024-byte aligned
@@ -287,12 +290,12 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
       if (n >= 0) {
         const uint32_t a = tmem + 128 * buf.at;
         const Operand<8192> u(ring_at + slot * F::kStage), w(ring_at + slot * F::kStage + F::kU);
-        wait.on_lanes(F::kSplit ? &pfull[buf.at] : &tfull[buf.at], buf.phase, 34);
+        wait.on_lanes(kSplit ? &pfull[buf.at] : &tfull[buf.at], buf.phase, 34);
         tc_fence_after();
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           mma_ts(acc, a + 32 * (e >> 1) + 8 * (e & 1), (KV ? w : u).at(2048 * e), id_a, e > 0 ? 1u : uint32_t(n));
-        if (F::kSplit) {
+        if (kSplit) {
           wait.on_lanes(&tfull[buf.at], buf.phase, 39);
           tc_fence_after();
         }
@@ -421,12 +424,12 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
             }
           }
         }
-        {
+        if (!kChained) {
           uint32_t w[16];
 #pragma unroll
           for (int e = 0; e < 16; ++e) w[e] = bf16_pair(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
           tmem_st16(s_col, w);
-          if (F::kSplit) {
+          if (kSplit) {
             tmem_st_wait();
             tc_fence_before();
             arrive_warp(&pfull[buf.at]);
@@ -504,18 +507,27 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
             }
           }
           if (CAP) {
+            uint32_t pc[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&ch[8 * pass + e]));
               float x, y;
               split(mul2(f2u(t[2 * e], t[2 * e + 1]), f2(f.x, f.y)), x, y);
               t[2 * e] = __float_as_uint(x), t[2 * e + 1] = __float_as_uint(y);
+              if (kChained) {
+                split(mul2(f2u(s[16 * pass + 2 * e], s[16 * pass + 2 * e + 1]), f2(f.x, f.y)), x, y);
+                pc[e] = bf16_pair(x, y);
+              }
             }
             if (mask) {
 #pragma unroll
               for (int e = 0; e < 16; ++e)
-                if (s[16 * pass + e] == 0u) t[e] = 0u;
+                if (s[16 * pass + e] == 0u) {
+                  t[e] = 0u;
+                  if (kChained) pc[e / 2] &= e & 1 ? 0x0000ffffu : 0xffff0000u;
+                }
             }
+            if (kChained) tmem_st8(s_col + 8 * pass, pc);
           }
           uint32_t w[8];
 #pragma unroll

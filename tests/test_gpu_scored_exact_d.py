@@ -144,3 +144,35 @@ def test_backward_on_another_stream():
     api.attention_error(stream=s.cuda_stream)
     for name, g in zip(("dq", "dk", "dv", "dtable"), grads):
         assert bool(((g.double() - ref[name]).abs() <= err[name]).all()), name
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("L", [100, 512])
+@pytest.mark.parametrize("cap", [1.0, 100.0])
+def test_queries_under_a_cap(cap, L, D):
+    """Under a cap each pair of dS carries the cap's derivative, and so does what D
+    was off by: scores of a few units under a cap of 1, and under one of 100."""
+    x, how = inputs(L, D, seed=L)
+    x["q"] = 2 * x["q"]
+    how["softcap"] = cap
+    got = run(x, how)
+    Q, K, V, dO, O = (t[0].double().transpose(0, 1) for t in (x["q"], x["k"], x["v"], x["dout"], got["o"]))
+    pos, reach, s = torch.arange(L, device="cuda"), how["buckets"].size // 2, D ** -0.5
+    which = torch.from_numpy(how["buckets"].astype(np.int64)).cuda()[(pos[None] - pos[:, None]).clamp(-reach, reach) + reach]
+    t = torch.tanh(s * Q @ K.mT / cap)
+    P, chain = torch.softmax(cap * t + how["table"].double()[:, which], -1), 1 - t * t
+    dP, dP_abs = dO @ V.mT, dO.abs() @ V.abs().mT
+    exact, stored = (P * dP).sum(-1, keepdim=True), (dO * O).sum(-1, keepdim=True)
+    dS, off = P * (dP - exact), (exact - stored).abs()
+    want = s * (dS * chain) @ K
+
+    def norm(a):
+        return a.flatten(1).norm(dim=1)
+
+    # the derivative is held as fp16 (2^-11 of it), then the products' operands as bf16
+    operands = [(dS.abs() + P * off) * chain, off * P * chain]
+    bound = s * (sum((U + 2.0 ** -11) * norm((a ** 2 @ K ** 2).sqrt()) for a in operands)
+                 + norm((chain * (F * dS.abs() + ACC * P * (dP_abs + exact.abs()))) @ K.abs())) + U * norm(want)
+    assert bool((error("dq", got["dq"], want) <= bound).all())
+    for wrong in (s * (P * (dP - stored) * chain) @ K, want + s * ((exact - stored) * P * (1 - chain)) @ K):
+        assert cap > 1 or bool((norm(wrong - want) > bound).any())          # D from the stored O; a correction without the derivative
