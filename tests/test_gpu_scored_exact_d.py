@@ -176,3 +176,33 @@ def test_queries_under_a_cap(cap, L, D):
     assert bool((error("dq", got["dq"], want) <= bound).all())
     for wrong in (s * (P * (dP - stored) * chain) @ K, want + s * ((exact - stored) * P * (1 - chain)) @ K):
         assert cap > 1 or bool((norm(wrong - want) > bound).any())          # D from the stored O; a correction without the derivative
+
+
+@pytest.mark.parametrize("D", [20, 36, 100])
+@pytest.mark.parametrize("L,cap", [(60, 0.0), (300, 0.0), (300, 1.0), (700, 0.0)])
+def test_queries_on_the_cuda_cores(L, cap, D):
+    """bf16 widths that the tensor cores do not take: P and dS are not rounded there,
+    so only fp32 sums and the last rounding are granted.  Few tiles, which several
+    blocks share, and a single one."""
+    x, how = inputs(L, D, seed=L + D)
+    x["q"] = 2 * x["q"]
+    how["softcap"] = cap
+    got = run(x, how)
+    Q, K, V, dO, O = (t[0].double().transpose(0, 1) for t in (x["q"], x["k"], x["v"], x["dout"], got["o"]))
+    pos, reach, s = torch.arange(L, device="cuda"), how["buckets"].size // 2, D ** -0.5
+    which = torch.from_numpy(how["buckets"].astype(np.int64)).cuda()[(pos[None] - pos[:, None]).clamp(-reach, reach) + reach]
+    z = s * Q @ K.mT
+    t = torch.tanh(z / cap) if cap else torch.zeros_like(z)
+    P, chain = torch.softmax((cap * t if cap else z) + how["table"].double()[:, which], -1), 1 - t * t
+    dP, dP_abs = dO @ V.mT, dO.abs() @ V.abs().mT
+    exact, stored = (P * dP).sum(-1, keepdim=True), (dO * O).sum(-1, keepdim=True)
+    dS = P * (dP - exact)
+    want = s * (dS * chain) @ K
+
+    def norm(a):
+        return a.flatten(1).norm(dim=1)
+
+    # 1 - t^2 in fp32 is off by 2^-23 beside its own size
+    bound = s * norm((chain * (F * dS.abs() + ACC * P * (dP_abs + exact.abs())) + 2.0 ** -23 * dS.abs()) @ K.abs()) + U * norm(want)
+    assert bool((error("dq", got["dq"], want) <= bound).all())
+    assert bool((norm(s * (P * (dP - stored) * chain) @ K - want) > bound).any())
