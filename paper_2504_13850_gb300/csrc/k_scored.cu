@@ -289,9 +289,11 @@ __device__ __forceinline__ float pair_score(const ScoredParams& p, const Pair& c
   float z = x * p.scale;
   *chain = 1.f;
   if (p.cap > 0.f) {
-    const float t = tanhf(z / p.cap);
-    z = p.cap * t;
-    *chain = 1.f - t * t;
+    // the derivative as 4 e / (1 + e)^2, e = exp(-2 |y|): 1 - tanh^2 would keep
+    // nothing but tanh's rounding where the score is at the cap
+    const float y = z / p.cap, e = exp2f(-2.f * kLog2e * fabsf(y)), q = 1.f / (1.f + e);
+    z = p.cap * tanhf(y);
+    *chain = 4.f * e * q * q;
   }
   const int d = j - i;
   if (p.slopes) z -= c.slope * float(abs(d));

@@ -39,3 +39,10 @@ def test_one_row_near_the_cap_among_ordinary_ones(dtype, D, cap):
         x["q"][0, i, h] = (k * (0.8 * cap / (scale * (k * k).sum()))).to(dtype)
     x["dout"][0, i] = 0
     check(x, how)
+
+
+@pytest.mark.parametrize("seed", range(6))
+@pytest.mark.parametrize("D", [64, 96])
+def test_scores_beyond_the_cap_in_fp32(D, seed):
+    """Scores of several times the cap, where the cap's derivative is small and has to be as exact as the rest."""
+    check(*make(6, 112, 4, 2, D, F32, seed=100 + seed, bias="distance", causal=True, cap=2.0, scale=1.0, docs="mixed"))
