@@ -257,9 +257,10 @@ __device__ __forceinline__ void load_bias(float* bias, const ScoredParams& p, in
 }
 
 // N scores (fp32 bits) of one query row, keys j0 .. j0 + N - 1 -> score units:
-// the cap (KEEP: ch receives its derivative 1 - tanh^2 as pairs of fp16, a
-// factor in [0, 1] of a product that is itself rounded to bf16; below 6e-5
-// its spacing is 2^-24, what 1 - t^2 in fp32 leaves as well) and the bias.
+// the cap (KEEP: ch receives kChainUp times its derivative 1 - tanh^2 as pairs
+// of fp16, a factor of a product that is itself rounded to bf16; times kChainUp
+// it keeps its 11 bits down to 2e-9, the derivative at ten times the cap) and
+// the bias.
 // DIR is +1 when the columns are keys and -1 when they are queries (the row
 // then is the key); d = distance of column 0, lo and hi the bounds of the
 // warp's distances.
@@ -277,7 +278,7 @@ __device__ __forceinline__ void load_bias(float* bias, const ScoredParams& p, in
 // special-function operation against two per score: scoring 2 x 4095 tokens,
 // 16 heads of 128, with a prefix took 203 us against 223.  The backward pass,
 // whose special-function unit is less busy, ran 3% slower with it.
-constexpr float kSeriesEnd = 0.4f, kPlainCap = 64.f;
+constexpr float kSeriesEnd = 0.4f, kPlainCap = 64.f, kChainUp = 32768.f;
 struct Shape {
   float cap, cap_in, y_in;      // the cap; scale to 2 y log2(e) and to y
   float slope;                  // negated, in score units
@@ -304,7 +305,7 @@ __device__ __forceinline__ void shape_scores(uint32_t (&r)[N], uint32_t* ch, con
       split(add2(f2(ex2(x), ex2(y)), one), x, y);
       const F2 q = f2(rcp(x), rcp(y));
       if (KEEP) {
-        split(mul2(mul2(f2(4.f, 4.f), q), fma2(q, f2(-1.f, -1.f), one)), x, y);
+        split(mul2(mul2(f2(4.f * kChainUp, 4.f * kChainUp), q), fma2(q, f2(-1.f, -1.f), one)), x, y);
         const __half2 h = __floats2half2_rn(x, y);
         ch[e / 2] = *reinterpret_cast<const uint32_t*>(&h);
       }

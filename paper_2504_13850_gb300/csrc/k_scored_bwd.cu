@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
   };
   auto store = [&](int o, int g, const uint32_t (&a)[16]) {
     const Strided& out = !KV ? p.dq : o ? p.dk : p.dv;
-    const float mul = KV && !o ? 1.f : p.scale;
+    const float mul = KV && !o ? 1.f : CAP ? p.scale / kChainUp : p.scale;      // ch holds kChainUp derivatives
     const int i = r0 + 32 * (warp % 4) + lane, col = DP / 4 * (warp / 4) + 16 * g;
     if (i >= p.L) return;
     bf16* row = static_cast<bf16*>(out.p) + b * out.sb + int64_t(i) * out.sl + (KV ? kh : h0) * out.sh;
@@ -389,7 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) scored_bwd_tc_k(const __grid_cons
         const uint32_t stats = smem_u32(ring + slot * F::kStage + 2 * F::kU) + 128 * half;
         const int c0 = cb * 64 + 32 * half;
         // P = 2^(c x - lse)
-        uint32_t s[32], ch[16];                 // ch: 1 - tanh^2 of the cap, pairs of fp16
+        uint32_t s[32], ch[16];                 // ch: kChainUp (1 - tanh^2) of the cap, pairs of fp16
         tmem_ld32_issue(s_col, s);
         tmem_ld32_wait(s);
         {

@@ -46,3 +46,40 @@ def test_one_row_near_the_cap_among_ordinary_ones(dtype, D, cap):
 def test_scores_beyond_the_cap_in_fp32(D, seed):
     """Scores of several times the cap, where the cap's derivative is small and has to be as exact as the rest."""
     check(*make(6, 112, 4, 2, D, F32, seed=100 + seed, bias="distance", causal=True, cap=2.0, scale=1.0, docs="mixed"))
+
+
+@pytest.mark.parametrize("y", [3.0, 7.0, 9.0])
+@pytest.mark.parametrize("L,D", [(100, 64), (100, 128), (400, 64), (400, 128)])
+def test_every_score_beyond_the_cap_in_bf16(L, D, y):
+    """All scores are about y times the cap, so that the derivative (down to 6e-8) is all
+    that scales dQ and dK.  2-norms per head: P and dS (and what the correction of D
+    takes off) are rounded to bf16 and the derivative to fp16, independently of each
+    other; the derivative, exp(-2 y) in its exponent, takes the scores' fp32 rounding
+    of 8 y 2^-24 at most, and fp32 sums as everywhere."""
+    g = torch.Generator(device="cuda").manual_seed(int(10 * y) + L + D)
+
+    def rnd(mean, size):
+        return (mean + size * torch.randn(1, L, 2, D, device="cuda", generator=g)).to(BF)
+
+    s = D ** -0.5
+    q, k, v, dout = rnd(y / (D * s), 0.0), rnd(1.0, 0.1), rnd(0.0, 1.0), rnd(0.0, 1.0)
+    o, lse = api.attention_forward(q, k, v, softcap=1.0)
+    dq, dk, _, _ = api.attention_backward(dout, q, k, v, o, lse, softcap=1.0)
+    api.attention_error()
+    Q, K, V, dO, O = (t[0].double().transpose(0, 1) for t in (q, k, v, dout, o))
+    t = torch.tanh(s * Q @ K.mT)
+    P, chain = torch.softmax(t, -1), 1 / torch.cosh(s * Q @ K.mT) ** 2
+    dP, dP_abs = dO @ V.mT, dO.abs() @ V.abs().mT
+    exact = (P * dP).sum(-1, keepdim=True)
+    dS, off = P * (dP - exact), (exact - (dO * O).sum(-1, keepdim=True)).abs()
+    U, F, u = 2.0 ** -8, 4e-5, 8 * y * 2.0 ** -24
+
+    def norm(a):
+        return a.flatten(1).norm(dim=1)
+
+    for got, X, turn in ((dq, K, lambda a: a), (dk, Q, lambda a: a.mT)):
+        want = s * turn(dS * chain) @ X
+        operands = [(dS.abs() + P * off) * chain] + ([off * P * chain] if turn(dS) is dS else [])
+        bound = s * (sum((U + 2.0 ** -11) * norm((turn(a) ** 2 @ X ** 2).sqrt()) for a in operands)
+                     + norm(turn(chain * ((F + u) * dS.abs() + 2.0 ** -20 * P * (dP_abs + exact.abs()))) @ X.abs())) + U * norm(want)
+        assert bool((norm(got[0].double().transpose(0, 1) - want) <= bound).all())
