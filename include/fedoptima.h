@@ -491,6 +491,72 @@ FO_API int fo_dropout_add(const void* x, int64_t x_stride, const void* residual,
                    int64_t y_stride, int dtype, int64_t rows, int64_t cols, double p, uint64_t seed,
                    uint64_t call, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Embedding lookup with scaling, and the gradient of its table, for the tokens
+ * of transformer blocks trained on a device; the paper has no counterpart.
+ *     out[t] = scale * table[id_t];   dtable[v] = scale * sum over id_t = v of dout[t]
+ * An id outside of 0 .. vocab - 1 (padding) gives a row of zeros, and what dout
+ * holds there, NaN included, reaches no gradient.  ids: device, `tokens` of 32
+ * or 64 bits (ids_bits); table, dtable: contiguous device matrices
+ * [vocab][width] of table_dtype; out, dout: device matrices [tokens][width] of
+ * dtype with a row stride in elements (dout_stride 0 broadcasts one row).  fp32
+ * tables take fp32 or bf16 activations, bf16 tables bf16.  Products and sums
+ * are fp32 and rounded once; each sum is taken in a fixed order (equal calls
+ * give equal bits).  tokens <= 2^30, vocab <= 2^30, width <= 2^20.
+ * ---------------------------------------------------------------------- */
+FO_API int fo_embedding(const void* ids, int ids_bits, int64_t tokens, const void* table, int table_dtype, int64_t vocab,
+                 int64_t width, double scale, void* out, int64_t out_stride, int dtype, void* stream);
+/* Bytes of device workspace of a gradient, -1 for bad sizes (no counterpart
+ * in the paper). */
+FO_API int64_t fo_embedding_workspace(int64_t tokens, int64_t width);
+/* Writes all of dtable (rows without a token are zeros), or adds to what it
+ * holds (accumulate).  The workspace (256-byte aligned, at least
+ * fo_embedding_workspace bytes) is free again when the call's work on the
+ * stream is done; nothing is allocated, so a capturing stream may be passed (no
+ * counterpart in the paper). */
+FO_API int fo_embedding_grad(const void* dout, int64_t dout_stride, int dtype, const void* ids, int ids_bits, int64_t tokens,
+                      void* dtable, int table_dtype, int64_t vocab, int64_t width, double scale, int accumulate,
+                      void* workspace, int64_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Root-mean-square norm of a residual's addition over the last dimension, its
+ * gradient, and its output as 8-bit floats, in which a device can upload its
+ * split-point activations in half the bytes; the paper has no counterpart (its
+ * transformer uses layer norms).
+ *     s = x + residual, rounded to dtype;   r = (mean s^2 + eps)^(-1/2);   y = s r w
+ * x, residual (NULL: none, s is x), sum (may be NULL without a residual) and y
+ * are device matrices [rows][cols] of dtype with row strides in elements (0
+ * broadcasts an input's row); weight is a device vector of dtype or fp32; rstd
+ * (NULL: not wanted) receives r, fp32 [rows].  y or sum may be x or residual.
+ * Sums are fp32: magnitudes above 1e19 / sqrt(cols) overflow them.
+ * 8-bit form (q and scales, both or neither; y may then be NULL): each 32
+ * columns share the smallest power of two 2^e, -127 <= e <= 127, for which
+ * max|y| / 2^e <= 448; scales [rows][ceil(cols / 32)] holds e + 127, q
+ * [rows][cols] y / 2^e rounded to 4 exponent and 3 mantissa bits (e4m3).  Its y
+ * is not rounded to dtype before.  A group that holds an infinity or NaN has
+ * scale 255 and decodes to NaN.
+ * rows < 2^31, cols <= 2^20.
+ * ---------------------------------------------------------------------- */
+FO_API int fo_rms_norm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,
+                int weight_dtype, void* sum, int64_t sum_stride, void* y, int64_t y_stride, uint8_t* q, uint8_t* scales,
+                float* rstd, int dtype, int64_t rows, int64_t cols, double eps, void* stream);
+/* Bytes of device workspace of a gradient, -1 for bad sizes (no counterpart
+ * in the paper). */
+FO_API int64_t fo_rms_norm_workspace(int64_t rows, int64_t cols);
+/* Gradients of a call whose sum and rstd are s and rstd, from dy = dL/dy and
+ * the gradient ds that reaches s by the residual stream (NULL: none):
+ *     dx = r (w dy - s r^2 mean(w dy s)) + ds (also the residual's);   dweight = sum over rows of dy s r
+ * dx may be dy or ds.  dweight has the weight's type.  Fixed order of sums;
+ * the workspace as in fo_embedding_grad (no counterpart in the paper). */
+FO_API int fo_rms_norm_grad(const void* dy, int64_t dy_stride, const void* ds, int64_t ds_stride, const void* s, int64_t s_stride,
+                     const void* weight, int weight_dtype, const float* rstd, void* dx, int64_t dx_stride, void* dweight,
+                     int dtype, int64_t rows, int64_t cols, void* workspace, int64_t workspace_bytes, void* stream);
+/* The values that an 8-bit form stands for, y = q 2^(scale - 127), in dtype
+ * (exact in fp32, and in bf16 down to its smallest normal number; no counterpart
+ * in the paper). */
+FO_API int fo_decode_8bit(const uint8_t* q, const uint8_t* scales, void* y, int64_t y_stride, int dtype, int64_t rows, int64_t cols,
+                   void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -120,6 +120,18 @@ _SIGS = [
     ("fo_attention_error", C.c_int, [C.c_void_p]),
     ("fo_dropout_add", C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_int,
                                  C.c_int64, C.c_int64, C.c_double, C.c_uint64, C.c_uint64, C.c_void_p]),
+    ("fo_embedding", C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_double,
+                               C.c_void_p, C.c_int64, C.c_int, C.c_void_p]),
+    ("fo_embedding_workspace", C.c_int64, [C.c_int64, C.c_int64]),
+    ("fo_embedding_grad", C.c_int, [C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int,
+                                    C.c_int64, C.c_int64, C.c_double, C.c_int, C.c_void_p, C.c_int64, C.c_void_p]),
+    ("fo_rms_norm", C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_void_p, C.c_int64,
+                              C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64,
+                              C.c_double, C.c_void_p]),
+    ("fo_rms_norm_workspace", C.c_int64, [C.c_int64, C.c_int64]),
+    ("fo_rms_norm_grad", C.c_int, [C.c_void_p, C.c_int64] * 3 + [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int64,
+                                   C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]),
+    ("fo_decode_8bit", C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_void_p]),
 ]
 
 
@@ -663,3 +675,200 @@ def dropout_add(x, residual, p, seed, call, out=None, stream=None):
 def dropout_grad(dy, p, seed, call, out=None, stream=None):
     """Gradient of dropout_add's x: keep(dy) with the mask that (seed, call) name."""
     return dropout_add(dy, None, p, seed, call, out=out, stream=stream)
+
+
+def _dtype_of(torch, t, name):
+    if t.dtype == torch.bfloat16:
+        return DTYPE_BF16
+    if t.dtype == torch.float32:
+        return DTYPE_F32
+    raise ValueError(f"{name}: bf16 or fp32")
+
+
+def _dense_rows(torch, g):
+    """`g`, or a contiguous copy where its strides would refuse it: autograd
+    hands over gradients broadcast by a sum or a mean."""
+    if g.is_contiguous() or g.dim() == 2 and g.stride(1) == 1:
+        return g
+    return g.clone(memory_format=torch.contiguous_format)
+
+
+def _ids(torch, ids):
+    if not ids.is_cuda or ids.dtype not in (torch.int32, torch.int64) or not ids.is_contiguous():
+        raise ValueError("ids: a contiguous int32 or int64 device tensor")
+    return ids.data_ptr(), 32 if ids.dtype == torch.int32 else 64
+
+
+def _of_tokens(t, ids, width, dtype, name):
+    """(pointer, row stride) of `t`, [*ids.shape, width] of `dtype`."""
+    if t.shape[:-1] != ids.shape or t.shape[-1] != width or t.dtype != dtype or t.get_device() != ids.get_device():
+        raise ValueError(f"{name}: {tuple(ids.shape)} x {width} {dtype} on the ids' device is wanted")
+    return _matrix(t, t, name)
+
+
+def embedding(ids, table, scale=1.0, dtype=None, out=None, stream=None):
+    """fo_embedding: scale * table[ids] of int32 or int64 ids (any shape) and a
+    contiguous table [vocab, width]; ids outside of the table (padding) give
+    zeros.  `dtype` of the output defaults to the table's (bf16 of an fp32 table
+    is the other choice).  Runs on `stream`, by default torch's current stream."""
+    import torch
+    if table.dim() != 2 or not table.is_contiguous() or table.get_device() != ids.get_device():
+        raise ValueError("table: a contiguous matrix [vocab, width] on the ids' device")
+    ip, bits = _ids(torch, ids)
+    vocab, width = table.shape
+    dtype = table.dtype if dtype is None else dtype
+
+    def make():
+        return torch.empty((*ids.shape, width), dtype=dtype, device=ids.device)
+
+    with _device_of(torch, ids):
+        if out is None:
+            y, st = _on_stream(torch, ids, stream, make)
+            yp, ys = y.data_ptr(), width
+        else:
+            y, st = out, torch.cuda.current_stream(ids.get_device()).cuda_stream if stream is None else stream
+            yp, ys = _of_tokens(y, ids, width, dtype, "out")
+        _check(lib().fo_embedding(ip, bits, ids.numel(), table.data_ptr(), _dtype_of(torch, table, "table"), vocab, width,
+                                  scale, yp, ys, _dtype_of(torch, y, "out"), st), "embedding")
+    return y
+
+
+def embedding_grad(dout, ids, vocab, scale=1.0, dtype=None, out=None, accumulate=False, stream=None):
+    """fo_embedding_grad: the gradient [vocab, width] of embedding's table, of
+    `dtype` (default: dout's), from dout = [*ids.shape, width].  `out` may give
+    the tensor to write, or with `accumulate` to add to."""
+    import torch
+    ip, bits = _ids(torch, ids)
+    if accumulate and out is None:
+        raise ValueError("accumulate: out holds what is added to")
+    width = dout.shape[-1]
+    dtype = out.dtype if out is not None else dout.dtype if dtype is None else dtype
+    L_ = lib()
+    need = L_.fo_embedding_workspace(ids.numel(), width)
+
+    def make():
+        d = torch.empty((vocab, width), dtype=dtype, device=ids.device) if out is None else out
+        return _dense_rows(torch, dout), d, torch.empty(need, dtype=torch.uint8, device=ids.device) if need > 0 else None
+
+    with _device_of(torch, ids):
+        (g, d, ws), st = _on_stream(torch, ids, stream, make)
+        gp, gs = _of_tokens(g, ids, width, g.dtype, "dout")
+        if out is not None and (d.shape != (vocab, width) or not d.is_contiguous() or d.get_device() != ids.get_device()):
+            raise ValueError("out: a contiguous matrix [vocab, width] on the ids' device")
+        _check(L_.fo_embedding_grad(gp, gs, _dtype_of(torch, g, "dout"), ip, bits, ids.numel(), d.data_ptr(),
+                                    _dtype_of(torch, d, "out"), vocab, width, scale, 1 if accumulate else 0,
+                                    None if ws is None else ws.data_ptr(), max(need, 0), st), "embedding_grad")
+    return d
+
+
+def _norm_weight(torch, x, weight):
+    if weight.shape != x.shape[-1:] or weight.get_device() != x.get_device() or not weight.is_contiguous():
+        raise ValueError("weight: a contiguous vector as long as x's last dimension, on x's device")
+    return weight.data_ptr(), _dtype_of(torch, weight, "weight")
+
+
+def _norm(x, residual, weight, eps, out, sum_out, eight, with_y, stream):
+    import torch
+    dtype = _dtype_of(torch, x, "x")
+    if not x.is_cuda or x.dim() < 1:
+        raise ValueError("x: a device tensor of one dimension at least")
+    shape, device = x.shape, x.device
+    cols = shape[-1]
+    rows = x.numel() // cols if cols else 0
+
+    def make():
+        q = scales = y = r = None
+        s = x
+        if residual is not None:
+            s = torch.empty(shape, dtype=x.dtype, device=device) if sum_out is None else sum_out
+        if with_y:
+            y = torch.empty(shape, dtype=x.dtype, device=device) if out is None else out
+            r = torch.empty(shape[:-1], dtype=torch.float32, device=device)
+        if eight:
+            q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device)
+            scales = torch.empty((*shape[:-1], (cols + 31) // 32), dtype=torch.uint8, device=device)
+        return q, scales, s, y, r
+
+    with _device_of(torch, x):
+        (q, scales, s, y, r), st = _on_stream(torch, x, stream, make)
+        xp, xs = _matrix(x, x, "x")
+        rp, rs = (None, 0) if residual is None else _matrix(residual, x, "residual")
+        sp, ss = (None, 0) if residual is None else _matrix(s, x, "sum_out")
+        yp, ys = (None, 0) if y is None else _matrix(y, x, "out")
+        wp, wt = _norm_weight(torch, x, weight)
+        _check(lib().fo_rms_norm(xp, xs, rp, rs, wp, wt, sp, ss, yp, ys, None if q is None else q.data_ptr(),
+                                 None if q is None else scales.data_ptr(), None if r is None else r.data_ptr(), dtype, rows,
+                                 cols, eps, st), "rms_norm")
+    return q, scales, s, y, r
+
+
+def rms_norm(x, residual, weight, eps=1e-6, out=None, sum_out=None, stream=None):
+    """fo_rms_norm: (y, s, r) with s = x + residual (x itself where residual is
+    None), r = (mean s^2 + eps)^(-1/2) in fp32 and y = s r weight, over the last
+    dimension of a bf16 or fp32 device tensor.  weight: x's type or fp32.  `out`
+    and `sum_out` may give y and s.  Runs on `stream`, by default torch's
+    current stream."""
+    s, y, r = _norm(x, residual, weight, eps, out, sum_out, False, True, stream)[2:]
+    return y, s, r
+
+
+def rms_norm_8bit(x, residual, weight, eps=1e-6, with_y=False, stream=None):
+    """The norm as 8-bit floats: (q, scales, s), q float8_e4m3fn like x, scales
+    uint8 [..., ceil(cols / 32)] (fo_rms_norm has the format), or with `with_y`
+    (q, scales, s, y, r) from the same pass."""
+    q, scales, s, y, r = _norm(x, residual, weight, eps, None, None, True, with_y, stream)
+    return (q, scales, s, y, r) if with_y else (q, scales, s)
+
+
+def rms_norm_grad(dy, ds, s, weight, r, out=None, stream=None):
+    """fo_rms_norm_grad: (dx, dweight) of rms_norm, from the gradients dy of y and
+    ds of s (None: none), and the call's s, weight and r.  dx is also the
+    residual's gradient."""
+    import torch
+    L_ = lib()
+    dtype = _dtype_of(torch, s, "s")
+    shape, device = s.shape, s.device
+    cols = shape[-1]
+    rows = s.numel() // cols if cols else 0
+    need = L_.fo_rms_norm_workspace(rows, cols)
+
+    def make():
+        return (_dense_rows(torch, dy), None if ds is None else _dense_rows(torch, ds),
+                torch.empty(shape, dtype=s.dtype, device=device) if out is None else out,
+                torch.empty(weight.shape, dtype=weight.dtype, device=device),
+                torch.empty(need, dtype=torch.uint8, device=device) if need > 0 else None)
+
+    with _device_of(torch, s):
+        (g, h, dx, dw, ws), st = _on_stream(torch, s, stream, make)
+        gp, gs = _matrix(g, s, "dy")
+        hp, hs = (None, 0) if h is None else _matrix(h, s, "ds")
+        sp, ss = _matrix(s, s, "s")
+        wp, wt = _norm_weight(torch, s, weight)
+        xp, xs = _matrix(dx, s, "out")
+        _check(L_.fo_rms_norm_grad(gp, gs, hp, hs, sp, ss, wp, wt, _small(r, shape[:-1], torch.float32, s, "r"), xp, xs,
+                                   dw.data_ptr(), dtype, rows, cols, None if ws is None else ws.data_ptr(), max(need, 0), st),
+               "rms_norm_grad")
+    return dx, dw
+
+
+def decode_8bit(q, scales, dtype=None, out=None, stream=None):
+    """fo_decode_8bit: the values of rms_norm_8bit's (q, scales), in `dtype`
+    (default: bf16)."""
+    import torch
+    shape, device = q.shape, q.device
+    if not q.is_cuda or q.dtype != torch.float8_e4m3fn or not q.is_contiguous() or q.dim() < 1:
+        raise ValueError("q: a contiguous float8_e4m3fn device tensor")
+    cols = shape[-1]
+    sp = _small(scales, (*shape[:-1], (cols + 31) // 32), torch.uint8, q, "scales")
+
+    def make():
+        return torch.empty(shape, dtype=torch.bfloat16 if dtype is None else dtype, device=device) if out is None else out
+
+    with _device_of(torch, q):
+        y, st = _on_stream(torch, q, stream, make)
+        if y.shape != shape or y.get_device() != q.get_device():
+            raise ValueError("out: q's shape and device are wanted")
+        yp, ys = _matrix(y, y, "out")
+        _check(lib().fo_decode_8bit(q.data_ptr(), sp, yp, ys, _dtype_of(torch, y, "out"), q.numel() // cols if cols else 0, cols,
+                                    st), "decode_8bit")
+    return y
