@@ -557,6 +557,47 @@ FO_API int fo_rms_norm_grad(const void* dy, int64_t dy_stride, const void* ds, i
 FO_API int fo_decode_8bit(const uint8_t* q, const uint8_t* scales, void* y, int64_t y_stride, int dtype, int64_t rows, int64_t cols,
                    void* stream);
 
+/* ------------------------------------------------------------------------
+ * Orthogonalised updates of weight matrices (for devices that train with
+ * momentum whose matrices are made orthogonal before a step); the paper has no
+ * counterpart (its updates are SGD with momentum).  For each matrix,
+ *     momentum <- mu momentum + grad;  U = grad + mu momentum (nesterov) or momentum
+ *     (U = grad without a momentum);   X = U / (|U|_F + eps)
+ *     `steps` times, on X or its transpose, whichever has rows <= columns:
+ *         A = X X^T;  X <- c0 X + (c1 A + c2 A A) X
+ *     out = X;  param <- decay param - step X
+ * Coefficients such as (3.4445, -4.7750, 2.0315) bring the singular values into
+ * 0.7 .. 1.2 in five steps.  The products run on the tensor cores, on fp16
+ * operands for bf16 matrices (roundings of 2^-12) and on pairs of them for fp32
+ * ones (2^-22), with fp32 sums; singular values that exceed 64 on the way
+ * overflow.  An infinity or NaN in U makes all of X NaN.  The order of all sums
+ * is fixed.  Sides of 0 to 32768 (the smaller) and 2^20.
+ * ---------------------------------------------------------------------- */
+typedef struct fo_matrix_update {
+  int64_t rows, cols;
+  const void* grad;         /* device [rows][cols] of dtype                     */
+  float* momentum;          /* device [rows][cols] fp32, or NULL                */
+  void* out;                /* device [rows][cols] of dtype, or NULL; may be grad */
+  float* param;             /* device [rows][cols] fp32, or NULL (one of the two) */
+  int64_t grad_stride, momentum_stride, out_stride, param_stride; /* of rows, in elements */
+  float step;
+} fo_matrix_update;
+/* Bytes of device workspace, -1 for bad sizes (no counterpart in the paper). */
+FO_API int64_t fo_orthogonalize_workspace(const fo_matrix_update* items, int count, int dtype);
+/* All matrices in launches shared by up to 32 of them, on `stream`.  items and
+ * coefficients (3) are host memory read during the call.  1 to 64 steps,
+ * coefficients within +-64, eps of 1e-30 to 1e30, mu of 0 to 1.  The workspace
+ * (256-byte aligned) is free again when the call's work on the stream is done;
+ * nothing is allocated, so a capturing stream may be passed (no counterpart in
+ * the paper). */
+FO_API int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int steps, const double* coefficients, double eps,
+                     double mu, int nesterov, double decay, void* workspace, int64_t workspace_bytes, void* stream);
+/* Waits for `stream` and reports FO_ERR_TIMEOUT if a kernel of
+ * fo_orthogonalize gave up a bounded wait on the current device, on any stream,
+ * since the calling thread last asked; outputs of calls in between may then be
+ * void (no counterpart in the paper). */
+FO_API int fo_orthogonalize_error(void* stream);
+
 #ifdef __cplusplus
 }
 #endif

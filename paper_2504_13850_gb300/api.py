@@ -55,6 +55,11 @@ class fo_attention_spec(C.Structure):
                 + [(n, C.c_void_p) for n in ("slopes", "table", "bucket_of_host", "documents", "prefix")])
 
 
+class fo_matrix_update(C.Structure):
+    _fields_ = ([(n, C.c_int64) for n in ("rows", "cols")] + [(n, C.c_void_p) for n in ("grad", "momentum", "out", "param")]
+                + [(n, C.c_int64) for n in ("grad_stride", "momentum_stride", "out_stride", "param_stride")] + [("step", C.c_float)])
+
+
 class FedOptimaError(RuntimeError):
     pass
 
@@ -131,6 +136,10 @@ _SIGS = [
     ("fo_rms_norm_workspace", C.c_int64, [C.c_int64, C.c_int64]),
     ("fo_rms_norm_grad", C.c_int, [C.c_void_p, C.c_int64] * 3 + [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p, C.c_int64,
                                    C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]),
+    ("fo_orthogonalize_workspace", C.c_int64, [C.c_void_p, C.c_int, C.c_int]),
+    ("fo_orthogonalize", C.c_int, [C.c_void_p, C.c_int, C.c_int, C.c_int, C.c_void_p, C.c_double, C.c_double, C.c_int, C.c_double,
+                                   C.c_void_p, C.c_int64, C.c_void_p]),
+    ("fo_orthogonalize_error", C.c_int, [C.c_void_p]),
     ("fo_decode_8bit", C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64, C.c_int, C.c_int64, C.c_int64, C.c_void_p]),
 ]
 
@@ -872,3 +881,94 @@ def decode_8bit(q, scales, dtype=None, out=None, stream=None):
         _check(lib().fo_decode_8bit(q.data_ptr(), sp, yp, ys, _dtype_of(torch, y, "out"), q.numel() // cols if cols else 0, cols,
                                     st), "decode_8bit")
     return y
+
+
+# Coefficients that bring singular values into 0.7 .. 1.2 in five steps.
+QUINTIC = (3.4445, -4.7750, 2.0315)
+
+
+def _matrices(torch, tensors, like, dtype, name):
+    """(pointer, row stride) of each matrix, shaped and placed like `like`'s."""
+    flat = []
+    for t, g in zip(tensors, like, strict=True):
+        if t.dim() != 2 or t.shape != g.shape or t.dtype != dtype or t.get_device() != like[0].get_device() or not t.is_cuda:
+            raise ValueError(f"{name}: {dtype} matrices with the gradients' shapes, on one device")
+        flat.append(_matrix(t, t, name))
+    return flat
+
+
+def _orthogonalize(torch, grads, momenta, outs, params, steps_of, steps, coefficients, eps, mu, nesterov, decay, stream):
+    """fo_orthogonalize on lists of tensors (each of the last three may be None);
+    returns outs, made here where it is True."""
+    L_ = lib()
+    n, first = len(grads), grads[0]
+    dtype = _dtype_of(torch, first, "updates")
+    items = (fo_matrix_update * n)()
+
+    def make():
+        dense = [_dense_rows(torch, g) for g in grads]
+        made = [torch.empty(g.shape, dtype=g.dtype, device=g.device) for g in grads] if outs is True else outs
+        for it, g in zip(items, dense):
+            if g.dim() != 2:
+                raise ValueError("updates: matrices")
+            it.rows, it.cols = g.shape
+        need = L_.fo_orthogonalize_workspace(items, n, dtype)
+        if need < 0:
+            _check(ERR_ARG, "orthogonalize")
+        return dense, made, torch.empty(need, dtype=torch.uint8, device=first.device) if need > 0 else None, need
+
+    with _device_of(torch, first):
+        (dense, outs, ws, need), st = _on_stream(torch, first, stream, make)
+        for name, tensors, t in (("grad", dense, first.dtype), ("momentum", momenta, torch.float32), ("out", outs, first.dtype),
+                                 ("param", params, torch.float32)):
+            if tensors is None:
+                continue
+            for it, (p, ld) in zip(items, _matrices(torch, tensors, dense, t, name)):
+                setattr(it, name, p)
+                setattr(it, name + "_stride", ld)
+        if steps_of is not None:
+            for it, v in zip(items, steps_of, strict=True):
+                it.step = v
+        _check(L_.fo_orthogonalize(items, n, dtype, steps, (C.c_double * 3)(*coefficients), eps, mu, 1 if nesterov else 0, decay,
+                                   None if ws is None else ws.data_ptr(), need, st), "orthogonalize")
+    return outs
+
+
+def orthogonalize(updates, steps=5, coefficients=QUINTIC, eps=1e-7, out=None, stream=None):
+    """fo_orthogonalize without momentum: X of a matrix, or of each of a list of
+    matrices, bf16 or fp32 (all of one type), U / (|U| + eps) followed by `steps`
+    of X <- c0 X + (c1 A + c2 A A) X with A = X X^T.  One call for a list shares
+    its launches.  `out` may give the tensors to write (the updates too).  Runs
+    on `stream`, by default torch's current stream."""
+    import torch
+    if isinstance(updates, torch.Tensor):
+        return orthogonalize([updates], steps, coefficients, eps, None if out is None else [out], stream)[0]
+    if len(updates) == 0:
+        return []
+    return _orthogonalize(torch, updates, None, True if out is None else out, None, None, steps, coefficients, eps, 0.0, False, 1.0,
+                          stream)
+
+
+def muon_step(params, grads, momenta, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scales=None, steps=5,
+              coefficients=QUINTIC, eps=1e-7, stream=None):
+    """One optimiser step on weight matrices with orthogonalised momentum, in
+    place: m <- momentum m + g; X = orthogonalize(g + momentum m, or m without
+    nesterov); p <- (1 - lr weight_decay) p - lr scale X.  params and momenta are
+    fp32, grads fp32 or bf16; scales default to sqrt(max(1, rows / cols))."""
+    import torch
+    if len(params) == 0:
+        return
+    if scales is None:
+        scales = [max(1.0, p.shape[0] / max(1, p.shape[1])) ** 0.5 for p in params]
+    _orthogonalize(torch, grads, momenta, None, params, [lr * s for s in scales], steps, coefficients, eps, momentum, nesterov,
+                   1.0 - lr * weight_decay, stream)
+
+
+def orthogonalize_error(stream=None, device=None):
+    """Waits for `stream` (default: torch's current stream) of `device`
+    (default: the current one) and raises if a kernel of orthogonalize or
+    muon_step gave up a bounded wait there."""
+    import torch
+    with _here if device is None else torch.cuda.device(device):
+        st = torch.cuda.current_stream().cuda_stream if stream is None else stream
+        _check(lib().fo_orthogonalize_error(st), "orthogonalize_error")
