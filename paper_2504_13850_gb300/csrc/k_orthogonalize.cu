@@ -3,7 +3,7 @@
 // after them.
 //
 //   X = U / (|U|_F + eps), of U or its transpose so that m <= n;  then `steps` times
-//   A = X X^T (m x m);  B = a I + b A + c A A;  X <- B X
+//   A = X X^T (m x m);  C = b A + c A A;  X <- a X + C X
 //
 // A and A A are symmetric: only tiles on and above the diagonal are formed and
 // stored, 3 m^2 n + m^3 multiplications and additions per step instead of
@@ -13,18 +13,27 @@
 //
 // Operands are fp16, not bf16: singular values stay below about 1.3, so the
 // range is known and held in the middle of fp16's by powers of two, and each
-// rounding costs 2^-12 instead of 2^-9.  For fp32 matrices each operand is a sum
-// of two fp16 numbers (22 bits) and each product three (hi hi, hi lo, lo hi);
-// the fourth is below fp32's rounding.  Sums are fp32 in tensor memory; because
-// the tensor cores truncate, those of fp32 matrices are moved to registers and
-// added there, rounded, every 512 terms, and the two small products have a sum
-// of their own.
+// rounding costs 2^-12 instead of 2^-9.  X itself is kept as the sum of two fp16
+// numbers (22 bits), and a X is added from both: what the roundings of the
+// products' operands leave in the weak directions, which each step multiplies by
+// up to a, is then proportional to C, which is small there (off by 0.5 to 0.8e-3
+// for bf16 matrices instead of 2e-3 with a in the product).  For fp32 matrices
+// all operands are such pairs, and each product three (hi lo, lo hi, hi hi, in
+// this order; the fourth is below fp32's rounding).  Sums are fp32 in tensor
+// memory; because the tensor cores truncate, those of fp32 matrices are moved to
+// registers and added there, rounded, every 64 terms (512: 7e-6 off instead of
+// 1.5e-6 on matrices of width 512, torch's fp32 products 2.3e-6).
 //
-// X, A and B lie in the workspace as blocks of 64 x 64 elements of 8 KB in the
+// X, A and C lie in the workspace as blocks of 64 x 64 elements of 8 KB in the
 // image that a 128-byte-swizzled operand has in shared memory, block rows
-// fastest: every operand tile is one or two contiguous copies without a tensor
-// map, whatever the number and sizes of the matrices, and the padding of odd
-// sizes to 128 is zeros.
+// fastest: every operand tile is a few contiguous copies without a tensor map,
+// whatever the number and sizes of the matrices, and the padding of odd sizes to
+// 128 is zeros.
+//
+// A pair of CTAs (cta_group::2) works on a tile of 256 x 256 or 256 x 128: each
+// loads its 128 rows and half of the columns' operand.  A single CTA's tile of
+// 128 x 128 loads twice to four times the bytes per product, and 64 bytes per
+// clock and SM is what L2 gives: it ran 4096 x 4096 at 1.0 PFLOP/s.
 #include "fo_scored_tc.cuh"
 #include "fo_vec8.cuh"
 #include "../../include/fedoptima.h"
@@ -42,47 +51,76 @@ __device__ GaveUp g_err;
 
 constexpr int kItems = 32;                    // matrices per launch
 constexpr int kBlock = 8192;                  // bytes of a 64 x 64 block
-constexpr int kMaxSums = 1024;                // partial sums of squares per matrix
-constexpr float kUpX = 1024.f, kUpA = 256.f;  // what X, and A and B, are multiplied by as fp16
+constexpr int kMaxSums = 256;                 // partial sums of squares per matrix
+constexpr float kUpX = 1024.f, kUpA = 256.f;  // what X, and A and C, are multiplied by as fp16
 
 struct Item {
   const void* g;            // [rows][cols] gradient
   float *mom, *param;
   void* out;
   int64_t ldg, ldm, ldp, ldo;
-  int64_t x[2], a, b;       // byte offsets in the workspace
-  int64_t sums;             // index of its partial sums
+  int64_t x[2], a, c;       // byte offsets in the workspace
   int rows, cols, mt, nt;   // mt, nt: tiles of 128 of the smaller and the larger side
-  int nsums, transposed;
+  int nsums;                // partial sums of squares, at kMaxSums times its index
+  bool transposed, vec_in, vec_out;
   float step;
 };
 struct OrthoParams {
   Item item[kItems];
   int start[kItems + 1];    // first unit of work of each matrix in this launch
+  uint8_t order[kItems];    // the matrices in the order of their units
   char* ws;
   double* sums;
   int count, from, last;    // from: which X is read; last: X goes to the caller
   float ca, cb, cc, mu, decay;
-  int nesterov;
+  bool nesterov;
   double eps;
 };
 
-__device__ __forceinline__ int item_of(const OrthoParams& p, int unit) {
+__device__ __forceinline__ int slot_of(const OrthoParams& p, int unit) {
   int n = 0;
   while (n + 1 < p.count && unit >= p.start[n + 1]) ++n;
   return n;
 }
 
 // ------------------------------------------------------------- before the steps
-// U of one element; FIRST updates the momentum, afterwards it is read.
+// U of eight neighbouring elements, zeros outside of the matrix; FIRST updates
+// the momentum, afterwards it is read.
 template <typename T, bool FIRST>
-__device__ __forceinline__ float update_at(const OrthoParams& p, const Item& it, int64_t r, int64_t c) {
-  const float g = to_f(static_cast<const T*>(it.g)[r * it.ldg + c]);
-  if (!it.mom) return g;
-  float* m = it.mom + r * it.ldm + c;
-  float v = *m;
-  if (FIRST) *m = v = fmaf(p.mu, v, g);
-  return p.nesterov ? fmaf(p.mu, v, g) : v;
+__device__ __forceinline__ void update8(const OrthoParams& p, const Item& it, int64_t r, int c, float (&v)[8]) {
+  const T* g = static_cast<const T*>(it.g) + r * it.ldg + c;
+  float* m = it.mom ? it.mom + r * it.ldm + c : nullptr;
+  const int left = r < it.rows ? it.cols - c : 0;
+  if (it.vec_in && left >= 8) {
+    Raw8<T> raw;
+    raw.load(g);
+    raw.get(v);
+    if (m) {
+      Raw8<float> old;
+      old.load(m);
+      float z[8];
+      old.get(z);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (FIRST) z[e] = fmaf(p.mu, z[e], v[e]);
+        v[e] = p.nesterov ? fmaf(p.mu, z[e], v[e]) : z[e];
+      }
+      if (FIRST) store8(m, z);
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    v[e] = 0.f;
+    if (e < left) {
+      v[e] = to_f(g[e]);
+      if (m) {
+        float z = m[e];
+        if (FIRST) m[e] = z = fmaf(p.mu, z, v[e]);
+        v[e] = p.nesterov ? fmaf(p.mu, z, v[e]) : z;
+      }
+    }
+  }
 }
 
 // Sums of squares.  fp32 squares leave its range beyond 2^+-64; elements far
@@ -92,17 +130,34 @@ __global__ void __launch_bounds__(256) ortho_sums_k(const __grid_constant__ Orth
   __shared__ double box[8];
   pdl_wait();
   pdl_trigger();
-  const int n = item_of(p, blockIdx.x), part = int(blockIdx.x) - p.start[n];
+  const int n = slot_of(p, blockIdx.x), part = int(blockIdx.x) - p.start[n];
   const Item& it = p.item[n];
-  const int64_t total = int64_t(it.rows) * it.cols, per = (total + it.nsums - 1) / it.nsums;
-  const int64_t end = min(total, (part + 1) * per);
+  const uint32_t per_row = uint32_t(it.cols + 7) / 8;               // vectors of eight
+  const int64_t total = int64_t(it.rows) * per_row, stride = int64_t(it.nsums) * 256;
+  int64_t e = int64_t(part) * 256 + threadIdx.x, row = e / per_row;
+  uint32_t col = uint32_t(e - row * per_row);
+  const int64_t down = stride / per_row;
+  const uint32_t right = uint32_t(stride - down * per_row);
   float mid = 0.f, big = 0.f, small = 0.f;
-  for (int64_t e = part * per + threadIdx.x; e < end; e += 256) {
-    const int64_t r = e / it.cols;
-    const float v = update_at<T, true>(p, it, r, e - r * it.cols), a = fabsf(v);
-    if (a > 0x1p40f) big = fmaf(v * 0x1p-80f, v * 0x1p-80f, big);
-    else if (a < 0x1p-40f) small = fmaf(v * 0x1p80f, v * 0x1p80f, small);
-    else mid = fmaf(v, v, mid);         // NaN too
+  constexpr int U = 4;                                              // in flight
+  for (; e < total; e += U * stride) {
+    float v[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      update8<T, true>(p, it, row, 8 * int(col), v[u]);             // zeros below the last row
+      row += down;
+      col += right;
+      if (col >= per_row) col -= per_row, ++row;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float x = v[u][k], a = fabsf(x);
+        if (a > 0x1p40f) big = fmaf(x * 0x1p-80f, x * 0x1p-80f, big);
+        else if (a < 0x1p-40f) small = fmaf(x * 0x1p80f, x * 0x1p80f, small);
+        else mid = fmaf(x, x, mid);     // NaN too
+      }
   }
   double s = double(mid) + double(big) * 0x1p160 + double(small) * 0x1p-160;
 #pragma unroll
@@ -111,7 +166,7 @@ __global__ void __launch_bounds__(256) ortho_sums_k(const __grid_constant__ Orth
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < 8; ++w) s += box[w];
-    p.sums[it.sums + part] = s;
+    p.sums[n * kMaxSums + part] = s;
   }
 }
 
@@ -122,145 +177,285 @@ __device__ __forceinline__ uint32_t half_pair(float a, float b) {
 __device__ __forceinline__ float2 of_pair(uint32_t w) {
   return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
+// Eight values as fp16; v keeps what they leave.
+__device__ __forceinline__ uint4 take_half8(float* v) {
+  uint32_t w[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    w[e] = half_pair(v[2 * e], v[2 * e + 1]);
+    const float2 f = of_pair(w[e]);
+    v[2 * e] -= f.x;
+    v[2 * e + 1] -= f.y;
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
 
 // X = U / (|U| + eps) as an image: one 64 x 64 block per block of threads.
-template <typename T, int PARTS>
+template <typename T>
 __global__ void __launch_bounds__(256) ortho_pack_k(const __grid_constant__ OrthoParams p) {
   __shared__ float tile[64][65];
   __shared__ double box[8];
+  __shared__ float scale[2];
+  static_assert(kMaxSums == 256, "one partial sum per thread");
   pdl_wait();
   pdl_trigger();
-  const int n = item_of(p, blockIdx.x);
+  const int n = slot_of(p, blockIdx.x);
   const Item& it = p.item[n];
   const int blk = int(blockIdx.x) - p.start[n], rows = 2 * it.mt;
-  const int rb = blk % rows, cb = blk / rows, t = threadIdx.x;
-  double s = 0.0;
-  for (int i = t; i < it.nsums; i += 256) s += p.sums[it.sums + i];
+  const int rb = blk % rows, cb = blk / rows, t = threadIdx.x, row = t / 4;
+  double s = t < it.nsums ? p.sums[n * kMaxSums + t] : 0.0;
+  // the user's matrix: two groups of eight of one row
+  const int r0 = 64 * (it.transposed ? cb : rb), c0 = 64 * (it.transposed ? rb : cb);
+  float v[2][8];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) update8<T, false>(p, it, r0 + row, c0 + 8 * (t % 4 * 2 + h), v[h]);
 #pragma unroll
   for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if (t % 32 == 0) box[t / 32] = s;
-  // the user's matrix, rows along its rows
-  const int r0 = 64 * (it.transposed ? cb : rb), c0 = 64 * (it.transposed ? rb : cb);
-  for (int e = t; e < 4096; e += 256) {
-    const int r = r0 + e / 64, c = c0 + e % 64;
-    tile[e / 64][e % 64] = r < it.rows && c < it.cols ? update_at<T, false>(p, it, r, c) : 0.f;
+  if (it.transposed)
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) tile[row][8 * (t % 4 * 2 + h) + e] = v[h][e];
+  __syncthreads();
+  if (t == 0) {
+    for (int w = 1; w < 8; ++w) s += box[w];
+    const double norm = sqrt(s) + p.eps;
+    // a power of two first, so that neither factor leaves fp32's range
+    int k = 0;
+    const double part = frexp(norm, &k);        // norm = part 2^k
+    const bool fine = isfinite(norm);
+    scale[0] = fine ? ldexpf(1.f, min(127, -k)) : float(1.0 / norm);
+    scale[1] = fine ? float(double(kUpX) / part) : 1.f;
   }
   __syncthreads();
-  s = 0.0;
-  for (int w = 0; w < 8; ++w) s += box[w];
-  const double norm = sqrt(s) + p.eps;
-  // a power of two first, so that neither factor leaves fp32's range
-  int k = 0;
-  const double part = frexp(norm, &k);          // norm = part 2^k
-  const bool fine = isfinite(norm);
-  const float s1 = fine ? ldexpf(1.f, min(127, -k)) : float(1.0 / norm), s2 = fine ? float(double(kUpX) / part) : 1.f;
-  const int row = t / 4;
-  char* img = p.ws + it.x[0] + int64_t(cb * int64_t(rows) + rb) * kBlock + row * 128;
+  const float s1 = scale[0], s2 = scale[1];
+  char* img = p.ws + it.x[0] + (cb * int64_t(rows) + rb) * kBlock + row * 128;
   const int64_t image = int64_t(it.mt) * it.nt * 4 * kBlock;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int u = t % 4 * 2 + h;
-    float v[8];
+    const int u = t % 4 * 2 + h, at = (u ^ (row & 7)) * 16;
+    float z[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (it.transposed ? tile[8 * u + e][row] : tile[row][8 * u + e]) * s1 * s2;
-    uint32_t w[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = half_pair(v[2 * e], v[2 * e + 1]);
-    const int at = (u ^ (row & 7)) * 16;
-    *reinterpret_cast<uint4*>(img + at) = make_uint4(w[0], w[1], w[2], w[3]);
-    if (PARTS == 2) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 f = of_pair(w[e]);
-        w[e] = half_pair(v[2 * e] - f.x, v[2 * e + 1] - f.y);
-      }
-      *reinterpret_cast<uint4*>(img + image + at) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    for (int e = 0; e < 8; ++e) z[e] = (it.transposed ? tile[8 * u + e][row] : v[h][e]) * s1 * s2;
+    *reinterpret_cast<uint4*>(img + at) = take_half8(z);
+    *reinterpret_cast<uint4*>(img + image + at) = take_half8(z);
   }
 }
 
 // ------------------------------------------------------------------ products
 enum { kGram = 0, kPoly = 1, kApply = 2 };
 constexpr int kThreads = 320;                 // copies, products, eight warps of arithmetic
-constexpr int kOperand = 2 * kBlock;          // 128 x 64
-constexpr int kSums = 8;                      // blocks of 64 terms between sums in registers (fp32 matrices)
 
-template <int PARTS>
+// Per CTA of a pair, for tiles of 256 x BN: 128 rows of A's operand and BN / 2 of
+// B's by 64 terms, in PARTS parts each.
+template <int PARTS, int BN>
 struct Tiles {
-  static constexpr int kStage = 2 * PARTS * kOperand, kStages = PARTS == 2 ? 3 : 6;
+  static constexpr int kA = 2 * kBlock, kB = BN / 128 * kBlock;
+  static constexpr int kStage = PARTS * (kA + kB), kStages = 196608 / kStage;
   static constexpr int kOut = 8 * 4096;       // 4 KB per warp of arithmetic
-  static constexpr int kBars = 2 * kStages + 5;
+  static constexpr int kBars = 3 * kStages + 5;
   static constexpr int kSmem = 1024 + kStages * kStage + kOut + 8 * kBars + 16;
-  static constexpr uint32_t kCols = PARTS * 256;
+  static constexpr uint32_t kCols = 2 * BN;   // two tiles' sums
 };
-static_assert(Tiles<2>::kSmem <= 232448 && Tiles<1>::kSmem <= 232448, "shared memory per CTA");
+static_assert(Tiles<1, 256>::kSmem <= 232448 && Tiles<1, 128>::kSmem <= 232448 && Tiles<2, 128>::kSmem <= 232448, "shared memory per CTA");
 
 struct Place {
-  int item, i, j, kb;       // tile and its blocks of 64 terms
+  int item, i, j, kb;       // rows 256 i, columns BN j, blocks of 64 terms (none: nothing to do)
 };
-template <int PHASE>
+template <int PHASE, int BN>
 __device__ __forceinline__ Place place_of(const OrthoParams& p, int unit) {
   Place a;
-  a.item = item_of(p, unit);
+  const int n = slot_of(p, unit);
+  a.item = p.order[n];
   const Item& it = p.item[a.item];
-  const int t = unit - p.start[a.item];
+  const int t = unit - p.start[n];
+  const int h = (it.mt + 1) / 2, cols = PHASE == kApply ? it.nt : it.mt;
   if (PHASE == kApply) {
-    a.i = t % it.mt;
-    a.j = t / it.mt;
-  } else {                  // i <= j, column by column
-    int j = int((sqrtf(8.f * float(t) + 1.f) - 1.f) * 0.5f);
-    while ((j + 1) * (j + 2) / 2 <= t) ++j;
-    while (j * (j + 1) / 2 > t) --j;
-    a.j = j;
-    a.i = t - j * (j + 1) / 2;
+    a.i = t % h;
+    a.j = t / h;
+  } else {                  // 256 x 256 on and above the diagonal, column by column
+    const int u = BN == 256 ? t : t / 2;
+    int j = int((sqrtf(8.f * float(u) + 1.f) - 1.f) * 0.5f);
+    while ((j + 1) * (j + 2) / 2 <= u) ++j;
+    while (j * (j + 1) / 2 > u) --j;
+    a.i = u - j * (j + 1) / 2;
+    a.j = BN == 256 ? j : 2 * j + t % 2;
   }
-  a.kb = 2 * (PHASE == kGram ? it.nt : it.mt);
+  a.kb = a.j * (BN / 128) < cols ? 2 * (PHASE == kGram ? it.nt : it.mt) : 0;
   return a;
 }
+// A symmetric matrix holds its 128 x 128 tiles (i, j) with i / 2 <= j / 2.  Rows
+// 128 i .. of block column kb lie there as rows, or mirrored, as columns of block
+// row kb.
+__device__ __forceinline__ bool mirrored(int i, int kb) { return i / 2 > kb / 4; }
 
-// 128 rows 128 i .. of block column kb, or the columns 128 i .. of block row kb.
-__device__ __forceinline__ void copy_rows(char* dst, const char* img, int mt, int i, int kb, uint64_t* bar) {
-  bulk_g2s(dst, img + (int64_t(kb) * 2 * mt + 2 * i) * kBlock, kOperand, bar);
+// Arrivals, products and commits of the two CTAs.  Arrivals and waits keep the
+// default scope: with release and acquire at cluster scope each block of terms
+// took 1 us (4096 x 4096: 2361 us).
+__device__ __forceinline__ void arrive_leader(uint64_t* bar) {
+  asm volatile(
+      "{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, 0;\n mbarrier.arrive.shared::cluster.b64 _, [r];\n}\n" ::"r"(
+          smem_u32(bar))
+      : "memory");
 }
-__device__ __forceinline__ void copy_cols(char* dst, const char* img, int mt, int i, int kb, uint64_t* bar) {
-  const char* src = img + (int64_t(2 * i) * 2 * mt + kb) * kBlock;
-  bulk_g2s(dst, src, kBlock, bar);
-  bulk_g2s(dst + kBlock, src + int64_t(2 * mt) * kBlock, kBlock, bar);
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n .reg .pred p, q;\n setp.ne.b32 p, %4, 0;\n elect.sync _|q, 0xffffffff;\n"
+      " @q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint64_t* bar) {     // the barrier of both CTAs
+  asm volatile(
+      "{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n"
+      " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}\n" ::"r"(smem_u32(bar)),
+      "h"(uint16_t(3))
+      : "memory");
 }
 
+// 64 sums of one row, columns 64 cblk .., become elements of A, C or X.
 template <int PARTS, int PHASE, typename T>
-__global__ void __launch_bounds__(kThreads, 1) ortho_product_k(const __grid_constant__ OrthoParams p) {
-  using S = Tiles<PARTS>;
+__device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int tile, int cblk, int q, int lane, uint32_t buf, float (&v)[64]) {
+  const int row = 128 * tile + 32 * q + lane, c0 = 64 * cblk;       // of the smaller and the larger side
+  const int64_t block = int64_t(cblk) * 2 * m.mt + 2 * tile + q / 2;
+  const int64_t half_block = block * kBlock + (q & 1) * 4096;       // this warp's 32 rows
+  const int64_t xi = int64_t(m.mt) * m.nt * 4 * kBlock, si = int64_t(m.mt) * m.mt * 4 * kBlock;
+  if (PHASE == kGram) {
+#pragma unroll
+    for (int e = 0; e < 64; ++e) v[e] *= kUpA / (kUpX * kUpX);
+  } else {
+    // C = b A + c A A, or a X + C X
+    const float linear = PHASE == kPoly ? p.cb : p.ca, other = (PHASE == kPoly ? p.cc : 1.f) / kUpA;
+    const char* src = p.ws + (PHASE == kPoly ? m.a : m.x[p.from]) + half_block + lane * 128;
+    constexpr int kParts = PHASE == kPoly ? PARTS : 2;
+    const int64_t image = PHASE == kPoly ? si : xi;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int off = (k ^ (lane & 7)) * 16;
+#pragma unroll
+      for (int part = kParts - 1; part >= 0; --part) {
+        const uint4 w = *reinterpret_cast<const uint4*>(src + part * image + off);
+        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 f = of_pair(ww[e]);
+          float &x = v[8 * k + 2 * e], &y = v[8 * k + 2 * e + 1];
+          x = fmaf(linear, f.x, part == kParts - 1 ? x * other : x);
+          y = fmaf(linear, f.y, part == kParts - 1 ? y * other : y);
+        }
+      }
+    }
+  }
+  if (PHASE == kApply && p.last) {
+    constexpr float down = 1.f / kUpX;
+    const int side = m.transposed ? m.cols : m.rows, wide = m.transposed ? m.rows : m.cols;
+    if (m.transposed) {       // a row here is a column there: lanes are neighbours
+      if (row < side)
+#pragma unroll
+        for (int e = 0; e < 64; ++e)
+          if (c0 + e < wide) {
+            const float x = v[e] * down;
+            if (m.out) static_cast<T*>(m.out)[(c0 + e) * m.ldo + row] = from_f<T>(x);
+            if (m.param) {
+              float* w = m.param + (c0 + e) * m.ldp + row;
+              *w = fmaf(-m.step, x, *w * p.decay);
+            }
+          }
+      return;
+    }
+    // 32 columns at a time through shared memory: eight lanes then hold a row's
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        st_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16, __float_as_uint(v[32 * h + 4 * k] * down), __float_as_uint(v[32 * h + 4 * k + 1] * down),
+                   __float_as_uint(v[32 * h + 4 * k + 2] * down), __float_as_uint(v[32 * h + 4 * k + 3] * down));
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int rr = 4 * i + lane / 8, r = 128 * tile + 32 * q + rr, c = c0 + 32 * h + 4 * (lane % 8);
+        const float4 x = ld_shared4(buf + rr * 128 + ((lane % 8) ^ (rr & 7)) * 16);
+        if (r >= side || c >= wide) continue;
+        const float z[4] = {x.x, x.y, x.z, x.w};
+        if (m.out) {
+          T* o = static_cast<T*>(m.out) + r * m.ldo + c;
+          if (m.vec_out && c + 4 <= wide) {
+            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(o) = x;
+            else *reinterpret_cast<uint2*>(o) = make_uint2(bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3]));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (c + e < wide) o[e] = from_f<T>(z[e]);
+          }
+        }
+        if (m.param) {
+          float* w = m.param + r * m.ldp + c;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (c + e < wide) w[e] = fmaf(-m.step, z[e], w[e] * p.decay);
+        }
+      }
+    }
+    return;
+  }
+  char* dst = p.ws + (PHASE == kGram ? m.a : PHASE == kPoly ? m.c : m.x[p.from ^ 1]) + half_block;
+  const int64_t image = PHASE == kApply ? xi : si;
+#pragma unroll
+  for (int part = 0; part < (PHASE == kApply ? 2 : PARTS); ++part) {
+    if (lane == 0) bulk_wait_read<0>();       // the last store has read the buffer
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint4 w = take_half8(v + 8 * k);
+      st_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16, w.x, w.y, w.z, w.w);
+    }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 4096;" ::"l"(dst + part * image), "r"(buf) : "memory");
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+  }
+}
+
+template <int PARTS, int BN, int PHASE, typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_product_k(const __grid_constant__ OrthoParams p) {
+  using S = Tiles<PARTS, BN>;
   extern __shared__ char smem_raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   char* stage_out = smem + S::kStages * S::kStage;
   uint64_t* full = reinterpret_cast<uint64_t*>(stage_out + S::kOut);
-  uint64_t *empty = full + S::kStages, *acc_full = empty + S::kStages, *acc_empty = acc_full + 2, *done = acc_empty + 2;
+  uint64_t *peer = full + S::kStages, *empty = peer + S::kStages, *acc_full = empty + S::kStages, *acc_empty = acc_full + 2,
+           *done = acc_empty + 2;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(done + 1);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int units = p.start[p.count];
+  const int units = p.start[p.count], pair = int(blockIdx.x) / 2, pairs = int(gridDim.x) / 2, me = int(blockIdx.x) % 2;
 
   if (threadIdx.x == 0) {
     for (int e = 0; e < S::kStages; ++e) {
       mbar_init(&full[e], 1);
+      mbar_init(&peer[e], 1);
       mbar_init(&empty[e], 1);
     }
     for (int e = 0; e < 2; ++e) {
       mbar_init(&acc_full[e], 1);
-      mbar_init(&acc_empty[e], 8);         // one arrival per warp
+      mbar_init(&acc_empty[e], 16);        // one arrival per warp of arithmetic, of both CTAs
     }
     mbar_init(done, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tslot)), "r"(S::kCols)
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tslot)), "r"(S::kCols)
                  : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
+  cluster_sync_all();                // both CTAs' barriers are there
   tc_fence_after();
-  const uint32_t tmem = *tslot;      // sum s: columns 128 PARTS s (and + 128 for the small products)
+  const uint32_t tmem = *tslot;      // sum s: columns BN s
   pdl_trigger();                     // this block holds its tensor memory
   pdl_wait();
   Waits wait(&g_err);
@@ -269,30 +464,47 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_k(const __grid_cons
     if (lane == 0) {
       Ring<S::kStages> at;
       int it = 0;
-      for (int u = blockIdx.x; u < units && !wait.dead; u += gridDim.x) {
-        const Place a = place_of<PHASE>(p, u);
+      for (int u = pair; u < units && !wait.dead; u += pairs) {
+        const Place a = place_of<PHASE, BN>(p, u);
         const Item& m = p.item[a.item];
         const char* x = p.ws + m.x[p.from];
-        const char* sym = p.ws + (PHASE == kPoly ? m.a : m.b);
+        const char* sym = p.ws + (PHASE == kPoly ? m.a : m.c);
         const int64_t xi = int64_t(m.mt) * m.nt * 4 * kBlock, si = int64_t(m.mt) * m.mt * 4 * kBlock;
+        const int cols = PHASE == kApply ? m.nt : m.mt;       // tiles of 128
+        const int ta = 2 * a.i + me, tb = BN == 256 ? 2 * a.j + me : a.j;
+        const bool has_a = ta < m.mt, has_b = tb < cols;
+        const uint32_t bytes = PARTS * ((has_a ? S::kA : 0) + (has_b ? S::kB : 0));
+        const int64_t wide = int64_t(2 * m.mt) * kBlock;      // from one block column to the next
         for (int kb = 0; kb < a.kb; ++kb, ++it) {
           if (it >= S::kStages) wait.on(&empty[at.at], at.phase ^ 1, 61);
           if (wait.dead) break;
           char* s = smem + at.at * S::kStage;
           uint64_t* bar = &full[at.at];
-          mbar_expect_tx(bar, S::kStage);
+          mbar_expect_tx(bar, bytes);
 #pragma unroll
           for (int q = 0; q < PARTS; ++q) {
-            char *da = s + q * kOperand, *db = s + (PARTS + q) * kOperand;
-            if (PHASE == kGram) {
-              copy_rows(da, x + q * xi, m.mt, a.i, kb, bar);
-              copy_rows(db, x + q * xi, m.mt, a.j, kb, bar);
-            } else {
-              if (a.i <= kb / 2) copy_rows(da, sym + q * si, m.mt, a.i, kb, bar);
-              else copy_cols(da, sym + q * si, m.mt, a.i, kb, bar);
-              if (PHASE == kApply) copy_cols(db, x + q * xi, m.mt, a.j, kb, bar);
-              else if (a.j <= kb / 2) copy_rows(db, sym + q * si, m.mt, a.j, kb, bar);
-              else copy_cols(db, sym + q * si, m.mt, a.j, kb, bar);
+            if (has_a) {
+              char* d = s + q * S::kA;
+              const char* src = PHASE == kGram ? x + q * xi : sym + q * si;
+              if (PHASE == kGram || !mirrored(ta, kb)) {
+                bulk_g2s(d, src + kb * wide + int64_t(2 * ta) * kBlock, 2 * kBlock, bar);
+              } else {
+                src += 2 * ta * wide + int64_t(kb) * kBlock;
+                bulk_g2s(d, src, kBlock, bar);
+                bulk_g2s(d + kBlock, src + wide, kBlock, bar);
+              }
+            }
+            if (has_b) {
+              char* d = s + PARTS * S::kA + q * S::kB;
+              const char* src = PHASE == kPoly ? sym + q * si : x + q * xi;
+              const int b0 = BN == 256 ? 2 * tb : 2 * tb + me;          // this CTA's first block
+              if (PHASE == kGram || (PHASE == kPoly && !mirrored(tb, kb))) {
+                bulk_g2s(d, src + kb * wide + int64_t(b0) * kBlock, S::kB, bar);
+              } else {
+                src += b0 * wide + int64_t(kb) * kBlock;
+                bulk_g2s(d, src, kBlock, bar);
+                if (BN == 256) bulk_g2s(d + kBlock, src + wide, kBlock, bar);
+              }
             }
           }
           at.step();
@@ -301,159 +513,133 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_k(const __grid_cons
       // every copy has landed before the block ends, whichever role gave up
       for (int e = max(0, it - S::kStages); e < it; ++e) mbar_wait(&full[e % S::kStages], (e / S::kStages) & 1);
     }
+  } else if (warp == 1 && me == 1) {
+    // tells the leader what has landed here
+    if (lane == 0) {
+      Ring<S::kStages> at;
+      for (int u = pair; u < units && !wait.dead; u += pairs) {
+        const Place a = place_of<PHASE, BN>(p, u);
+        for (int kb = 0; kb < a.kb; ++kb) {
+          wait.on(&full[at.at], at.phase, 65);
+          if (wait.dead) break;
+          arrive_leader(&peer[at.at]);
+          at.step();
+        }
+      }
+    }
+    __syncwarp();
   } else if (warp == 1) {
-    // kind::f16 with fp16 operands, fp32 sums, M = N = 128
-    constexpr uint32_t id = (1u << 4) | (128u >> 3) << 17 | (128u >> 4) << 24;
+    // kind::f16 with fp16 operands, fp32 sums, M = 256, N = BN
+    constexpr uint32_t id = (1u << 4) | uint32_t(BN >> 3) << 17 | (256u >> 4) << 24;
     Ring<S::kStages> at;
     uint32_t pass = 0;
     const uint32_t ring = smem_u32(smem);
-    for (int u = blockIdx.x; u < units; u += gridDim.x) {
-      const Place a = place_of<PHASE>(p, u);
+    bool dead = false;
+    for (int u = pair; u < units && !dead; u += pairs) {
+      const Place a = place_of<PHASE, BN>(p, u);
+      const int tb = BN == 256 ? 2 * a.j : a.j;
       for (int kb = 0; kb < a.kb; ++kb) {
-        const int in = PARTS == 2 ? kb % kSums : kb;
-        const uint32_t d = tmem + (pass & 1) * 128 * PARTS;
-        if (in == 0) wait.on_lanes(&acc_empty[pass & 1], ((pass >> 1) & 1) ^ 1, 62);
-        wait.on_lanes(&full[at.at], at.phase, 63);
+        const uint32_t d = tmem + (pass & 1) * BN;
+        const bool fresh = PARTS == 2 || kb == 0;
+        if (fresh) wait.on(&acc_empty[pass & 1], ((pass >> 1) & 1) ^ 1, 62);
+        wait.on(&full[at.at], at.phase, 63);
+        wait.on(&peer[at.at], at.phase, 66);
+        __syncwarp();
         tc_fence_after();
         const uint32_t s = ring + at.at * S::kStage;
         // mirrored operands have their rows along the terms
-        const uint32_t am = PHASE != kGram && a.i > kb / 2, bm = PHASE == kApply || (PHASE == kPoly && a.j > kb / 2);
+        const uint32_t am = PHASE != kGram && mirrored(2 * a.i, kb), bm = PHASE == kApply || (PHASE == kPoly && mirrored(tb, kb));
         const uint32_t idesc = id | am << 15 | bm << 16;
         const uint32_t as = am ? 2048u : 32u, bs = bm ? 2048u : 32u;
         const uint32_t al = (am ? uint32_t(kBlock) : 16u) >> 4 << 16, bl = (bm ? uint32_t(kBlock) : 16u) >> 4 << 16;
         constexpr uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);      // stride 1024, version 1, 128-byte swizzle
         auto desc = [&](uint32_t off, uint32_t lbo) { return uint64_t(((s + off) & 0x3ffff) >> 4 | lbo) | uint64_t(hi) << 32; };
+        constexpr uint32_t b0 = PARTS * S::kA;
+        if (PARTS == 2) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t first = in > 0 || k > 0 ? 1u : 0u;
-          const uint64_t ah = desc(k * as, al), bh = desc(PARTS * kOperand + k * bs, bl);
-          mma_ss(d, ah, bh, idesc, first);
-          if (PARTS == 2) {
-            mma_ss(d + 128, ah, desc(3 * kOperand + k * bs, bl), idesc, first);
-            mma_ss(d + 128, desc(kOperand + k * as, al), bh, idesc, 1u);
+          for (int k = 0; k < 4; ++k) {
+            mma_pair(d, desc(k * as, al), desc(b0 + S::kB + k * bs, bl), idesc, k > 0 ? 1u : 0u);
+            mma_pair(d, desc(S::kA + k * as, al), desc(b0 + k * bs, bl), idesc, 1u);
           }
         }
-        commit_to(&empty[at.at]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          mma_pair(d, desc(k * as, al), desc(b0 + k * bs, bl), idesc, PARTS == 2 || kb > 0 || k > 0 ? 1u : 0u);
+        commit_pair(&empty[at.at]);
         at.step();
-        if (kb + 1 == a.kb || (PARTS == 2 && in + 1 == kSums)) commit_to(&acc_full[pass++ & 1]);
+        if (PARTS == 2 || kb + 1 == a.kb) commit_pair(&acc_full[pass++ & 1]);
         // off the waits' path; what was issued after one gave up is void anyway
-        if (__any_sync(0xffffffffu, wait.dead)) break;
+        dead = __any_sync(0xffffffffu, wait.dead);
+        if (dead) break;
       }
-      if (__any_sync(0xffffffffu, wait.dead)) break;
     }
-    // no product is in flight when the block ends and its memory is another's
-    commit_to(done);
+    // no product is in flight when the blocks end and their memory is another's
+    asm volatile(
+        "{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n"
+        " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(smem_u32(done))
+        : "memory");
     mbar_wait(done, 0);
     __syncwarp();
   } else {
-    // warp: 32 rows 32 q .. and 64 columns, half a block
+    // warp: 32 rows 32 q .. and half of the columns, in blocks of 64
     const int q = warp % 4, half = (warp - 2) / 4;
-    const uint32_t col = tmem + (uint32_t(32 * q) << 16) + 64 * half;
+    constexpr int NB = BN / 128;
+    const uint32_t col = tmem + (uint32_t(32 * q) << 16) + (BN / 2) * half;
     const uint32_t buf = smem_u32(stage_out) + uint32_t(warp - 2) * 4096u;
     uint32_t pass = 0;
-    for (int u = blockIdx.x; u < units; u += gridDim.x) {
-      const Place a = place_of<PHASE>(p, u);
+    bool dead = false;
+    for (int u = pair; u < units && !dead; u += pairs) {
+      const Place a = place_of<PHASE, BN>(p, u);
+      if (a.kb == 0) continue;
       const Item& m = p.item[a.item];
-      float v[64];
-      for (int kb = 0; kb < a.kb; kb += PARTS == 2 ? kSums : a.kb, ++pass) {
-        wait.on_lanes(&acc_full[pass & 1], (pass >> 1) & 1, 64);
-        tc_fence_after();
+      const int tile = 2 * a.i + me, cblk = a.j * (BN / 64) + half * NB, cols = 2 * (PHASE == kApply ? m.nt : m.mt);
+      float v[PARTS == 2 ? NB : 1][64];
+      if (PARTS == 2) {
+        for (int kb = 0; kb < a.kb; ++kb, ++pass) {
+          wait.on(&acc_full[pass & 1], (pass >> 1) & 1, 64);
+          __syncwarp();
+          tc_fence_after();
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t from = col + (pass & 1) * 128 * PARTS + 32 * h;
-          uint32_t r[32];
-          tmem_ld32(from, r);
+          for (int h = 0; h < 2 * NB; ++h) {
+            uint32_t r[32];
+            tmem_ld32(col + (pass & 1) * BN + 32 * h, r);
 #pragma unroll
-          for (int e = 0; e < 32; ++e) v[32 * h + e] = (PARTS == 2 && kb > 0 ? v[32 * h + e] : 0.f) + __uint_as_float(r[e]);
-          if (PARTS == 2) {
-            tmem_ld32(from + 128, r);
-#pragma unroll
-            for (int e = 0; e < 32; ++e) v[32 * h + e] += __uint_as_float(r[e]);
-          }
-        }
-        tc_fence_before();
-        arrive_warp(&acc_empty[pass & 1]);
-      }
-      if (__any_sync(0xffffffffu, wait.dead)) break;
-      const int row = 128 * a.i + 32 * q + lane, c0 = 128 * a.j + 64 * half;     // of the smaller and the larger side
-      const int64_t block = int64_t(2 * a.j + half) * 2 * m.mt + 2 * a.i + q / 2;
-      const int in_block = (q & 1) * 4096 + lane * 128;
-      const int64_t si = int64_t(m.mt) * m.mt * 4 * kBlock;
-      if (PHASE == kApply && p.last) {
-        constexpr float down = 1.f / (kUpX * kUpA);
-        const int side = m.transposed ? m.cols : m.rows, other = m.transposed ? m.rows : m.cols;
-        if (row < side) {
-          const int64_t so = m.transposed ? m.ldo : 1, sp = m.transposed ? m.ldp : 1;
-          const int64_t fo = m.transposed ? int64_t(row) : row * m.ldo, fp = m.transposed ? int64_t(row) : row * m.ldp;
-#pragma unroll
-          for (int e = 0; e < 64; ++e) {
-            const int c = c0 + e;
-            if (c < other) {
-              const float x = v[e] * down;
-              if (m.out) static_cast<T*>(m.out)[fo + c * so] = from_f<T>(x);
-              if (m.param) {
-                float* w = m.param + fp + c * sp;
-                *w = fmaf(-m.step, x, *w * p.decay);
-              }
+            for (int e = 0; e < 32; ++e) {
+              float& x = v[h / 2][32 * (h % 2) + e];
+              x = (kb > 0 ? x : 0.f) + __uint_as_float(r[e]);
             }
           }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) arrive_leader(&acc_empty[pass & 1]);
         }
-        continue;
-      }
-      if (PHASE == kPoly) {
-        const char* src = p.ws + m.a + block * kBlock + in_block;
+        dead = __any_sync(0xffffffffu, wait.dead);
+        if (dead) break;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int off = (k ^ (lane & 7)) * 16;
-          float z[8];
-#pragma unroll
-          for (int part = 0; part < PARTS; ++part) {
-            const uint4 w = *reinterpret_cast<const uint4*>(src + part * si + off);
-            const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 f = of_pair(ww[e]);
-              z[2 * e] = (part ? z[2 * e] : 0.f) + f.x;
-              z[2 * e + 1] = (part ? z[2 * e + 1] : 0.f) + f.y;
-            }
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int c = 8 * k + e;
-            const float diagonal = row == c0 + c ? p.ca * kUpA : 0.f;
-            v[c] = fmaf(p.cc / kUpA, v[c], fmaf(p.cb, z[e], diagonal));
-          }
-        }
+        for (int b = 0; b < NB; ++b)
+          if (tile < m.mt && cblk + b < cols) finish<PARTS, PHASE, T>(p, m, tile, cblk + b, q, lane, buf, v[b]);
       } else {
-        constexpr float down = PHASE == kGram ? kUpA / (kUpX * kUpX) : 1.f / kUpA;
-#pragma unroll
-        for (int e = 0; e < 64; ++e) v[e] *= down;
-      }
-      char* dst = p.ws + (PHASE == kGram ? m.a : PHASE == kPoly ? m.b : m.x[p.from ^ 1]) + block * kBlock + (q & 1) * 4096;
-      const int64_t image = PHASE == kApply ? int64_t(m.mt) * m.nt * 4 * kBlock : si;
-#pragma unroll
-      for (int part = 0; part < PARTS; ++part) {
-        if (lane == 0) bulk_wait_read<0>();       // the last store has read the buffer
+        wait.on(&acc_full[pass & 1], (pass >> 1) & 1, 64);
         __syncwarp();
+        tc_fence_after();
+        dead = __any_sync(0xffffffffu, wait.dead);
+#pragma unroll 1
+        for (int b = 0; b < NB; ++b) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          uint32_t w[4];
+          for (int h = 0; h < 2; ++h) {
+            uint32_t r[32];
+            tmem_ld32(col + (pass & 1) * BN + 64 * b + 32 * h, r);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float &x = v[8 * k + 2 * e], &y = v[8 * k + 2 * e + 1];
-            w[e] = half_pair(x, y);
-            const float2 f = of_pair(w[e]);
-            x -= f.x;
-            y -= f.y;
+            for (int e = 0; e < 32; ++e) v[0][32 * h + e] = __uint_as_float(r[e]);
           }
-          st_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16, w[0], w[1], w[2], w[3]);
+          if (b == NB - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_leader(&acc_empty[pass & 1]);
+          }
+          if (!dead && tile < m.mt && cblk + b < cols) finish<PARTS, PHASE, T>(p, m, tile, cblk + b, q, lane, buf, v[0]);
         }
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 4096;" ::"l"(dst + part * image), "r"(buf) : "memory");
-          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-        }
+        ++pass;
       }
     }
     if (lane == 0) bulk_wait_all();
@@ -461,9 +647,10 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_product_k(const __grid_cons
   }
   tc_fence_before();
   __syncthreads();
+  cluster_sync_all();                // neither CTA is needed by the other any more
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kCols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kCols) : "memory");
   }
 }
 
@@ -483,22 +670,56 @@ int check_items(const fo_matrix_update* m, int count, int dtype) {
 int64_t item_bytes(const fo_matrix_update& m, int parts) {
   if (m.rows == 0 || m.cols == 0) return 0;
   const int64_t r = (m.rows + 127) / 128, c = (m.cols + 127) / 128, mt = r < c ? r : c, nt = r < c ? c : r;
-  return (2 * mt * nt + 2 * mt * mt) * 4 * kBlock * parts + kMaxSums * 8;
+  return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + kMaxSums * 8;
 }
 
-template <int PARTS, int PHASE, typename T>
-cudaError_t product(OrthoParams& p, int sms, cudaStream_t st) {
-  auto k = ortho_product_k<PARTS, PHASE, T>;
+template <int PARTS, int BN, int PHASE, typename T>
+cudaError_t launch_product(const OrthoParams& p, int pairs, cudaStream_t st) {
+  auto k = ortho_product_k<PARTS, BN, PHASE, T>;
   static std::atomic<bool> allowed[kMaxDevices];
   const cudaError_t e = allow_smem(k, allowed);
   if (e != cudaSuccess) return e;
+  const int units = p.start[p.count];
+  return launch_k(k, dim3(2 * unsigned(units < pairs ? units : pairs)), dim3(kThreads), Tiles<PARTS, BN>::kSmem, st, p);
+}
+
+// Units of each matrix, those with the longest sums first.
+template <int PHASE, int BN>
+int64_t plan(OrthoParams& p) {
+  auto length = [&p](int i) { return PHASE == kGram ? p.item[i].nt : p.item[i].mt; };
+  for (int i = 0; i < p.count; ++i) {
+    int at = i;
+    for (; at > 0 && length(p.order[at - 1]) < length(i); --at) p.order[at] = p.order[at - 1];
+    p.order[at] = uint8_t(i);
+  }
   int64_t units = 0;
   for (int i = 0; i < p.count; ++i) {
     p.start[i] = int(units);
-    units += PHASE == kApply ? int64_t(p.item[i].mt) * p.item[i].nt : int64_t(p.item[i].mt) * (p.item[i].mt + 1) / 2;
+    const Item& m = p.item[p.order[i]];
+    const int64_t h = (m.mt + 1) / 2;
+    if (PHASE == kApply) units += h * (BN == 256 ? (m.nt + 1) / 2 : m.nt);
+    else units += h * (h + 1) / 2 * (256 / BN);
   }
   p.start[p.count] = int(units);
-  return launch_k(k, dim3(unsigned(units < sms ? units : sms)), dim3(kThreads), Tiles<PARTS>::kSmem, st, p);
+  return units;
+}
+
+template <int PARTS, int PHASE, typename T>
+cudaError_t product(OrthoParams& p, int pairs, cudaStream_t st) {
+  // Wide tiles load fewer bytes per product and take 1.7 times as long as narrow
+  // ones; narrow ones divide the work into twice as many.  fp32 matrices, whose
+  // products are three, load few enough with narrow ones, and a wide tile's sums
+  // would not fit into the registers.
+  if constexpr (PARTS == 1) {
+    const int64_t wide = plan<PHASE, 256>(p), narrow = plan<PHASE, 128>(p);
+    if (17 * ((wide + pairs - 1) / pairs) <= 10 * ((narrow + pairs - 1) / pairs)) {
+      plan<PHASE, 256>(p);
+      return launch_product<PARTS, 256, PHASE, T>(p, pairs, st);
+    }
+  } else {
+    plan<PHASE, 128>(p);
+  }
+  return launch_product<PARTS, 128, PHASE, T>(p, pairs, st);
 }
 
 template <typename T>
@@ -508,6 +729,7 @@ cudaError_t orthogonalize(OrthoParams& p, int steps, cudaStream_t st) {
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
+  const int pairs = sms > 1 ? sms / 2 : 1;
   int64_t units = 0;
   for (int i = 0; i < p.count; ++i) {
     p.start[i] = int(units);
@@ -521,13 +743,13 @@ cudaError_t orthogonalize(OrthoParams& p, int steps, cudaStream_t st) {
     units += 4 * int64_t(p.item[i].mt) * p.item[i].nt;
   }
   p.start[p.count] = int(units);
-  if ((e = launch_k(ortho_pack_k<T, PARTS>, dim3(unsigned(units)), dim3(256), 0, st, p)) != cudaSuccess) return e;
+  if ((e = launch_k(ortho_pack_k<T>, dim3(unsigned(units)), dim3(256), 0, st, p)) != cudaSuccess) return e;
   for (int s = 0; s < steps; ++s) {
     p.from = s & 1;
     p.last = s + 1 == steps;
-    if ((e = product<PARTS, kGram, T>(p, sms, st)) != cudaSuccess) return e;
-    if ((e = product<PARTS, kPoly, T>(p, sms, st)) != cudaSuccess) return e;
-    if ((e = product<PARTS, kApply, T>(p, sms, st)) != cudaSuccess) return e;
+    if ((e = product<PARTS, kGram, T>(p, pairs, st)) != cudaSuccess) return e;
+    if ((e = product<PARTS, kPoly, T>(p, pairs, st)) != cudaSuccess) return e;
+    if ((e = product<PARTS, kApply, T>(p, pairs, st)) != cudaSuccess) return e;
   }
   return cudaSuccess;
 }
@@ -613,16 +835,19 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
       const int64_t r = (m.rows + 127) / 128, c = (m.cols + 127) / 128;
       it.mt = int(r < c ? r : c);
       it.nt = int(r < c ? c : r);
-      for (int k = 0; k < 2; ++k) it.x[k] = take(int64_t(it.mt) * it.nt * 4 * kBlock * parts);
+      for (int k = 0; k < 2; ++k) it.x[k] = take(int64_t(it.mt) * it.nt * 4 * kBlock * 2);
       it.a = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
-      it.b = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
-      const int64_t sums = (m.rows * m.cols + 16383) / 16384;
+      it.c = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
+      const int64_t per = dtype == FO_DTYPE_F32 ? 4 : 8;
+      it.vec_in = aligned16(m.grad) && (m.rows == 1 || m.grad_stride % per == 0) &&
+                  (!m.momentum || (aligned16(m.momentum) && (m.rows == 1 || m.momentum_stride % 4 == 0)));
+      it.vec_out = aligned16(m.out) && (m.rows == 1 || m.out_stride % per == 0);
+      const int64_t sums = (m.rows * ((m.cols + 7) / 8) + 1023) / 1024;       // four groups of eight per thread
       it.nsums = int(sums < kMaxSums ? sums : kMaxSums);
       it.step = m.step;
     }
     if (p.count == 0) continue;
     p.sums = reinterpret_cast<double*>(p.ws + at);
-    for (int i = 0; i < p.count; ++i) p.item[i].sums = int64_t(i) * kMaxSums;
     const cudaError_t e = dtype == FO_DTYPE_F32 ? orthogonalize<float>(p, steps, st) : orthogonalize<bf16>(p, steps, st);
     if (e != cudaSuccess) return done(e);
   }
