@@ -51,7 +51,7 @@ __device__ GaveUp g_err;
 
 constexpr int kItems = 32;                    // matrices per launch
 constexpr int kBlock = 8192;                  // bytes of a 64 x 64 block
-constexpr int kMaxSums = 256;                 // partial sums of squares per matrix
+constexpr int kMaxSums = 1024;                // partial sums of squares per matrix
 constexpr float kUpX = 1024.f, kUpA = 256.f;  // what X, and A and C, are multiplied by as fp16
 
 struct Item {
@@ -71,6 +71,7 @@ struct OrthoParams {
   uint8_t order[kItems];    // the matrices in the order of their units
   char* ws;
   double* sums;
+  float2* scale;            // of each matrix: the two factors that make X of U
   int count, from, last;    // from: which X is read; last: X goes to the caller
   float ca, cb, cc, mu, decay;
   bool nesterov;
@@ -127,7 +128,7 @@ __device__ __forceinline__ void update8(const OrthoParams& p, const Item& it, in
 // from 1 are squared in units of 2^80 or 2^-80 and summed apart.
 template <typename T>
 __global__ void __launch_bounds__(256) ortho_sums_k(const __grid_constant__ OrthoParams p) {
-  __shared__ double box[8];
+  __shared__ float4 box[8];
   pdl_wait();
   pdl_trigger();
   const int n = slot_of(p, blockIdx.x), part = int(blockIdx.x) - p.start[n];
@@ -139,35 +140,81 @@ __global__ void __launch_bounds__(256) ortho_sums_k(const __grid_constant__ Orth
   const int64_t down = stride / per_row;
   const uint32_t right = uint32_t(stride - down * per_row);
   float mid = 0.f, big = 0.f, small = 0.f;
+  auto add = [&](float x) {
+    const float a = fabsf(x);
+    if (a > 0x1p40f) big = fmaf(x * 0x1p-80f, x * 0x1p-80f, big);
+    else if (a < 0x1p-40f) small = fmaf(x * 0x1p80f, x * 0x1p80f, small);
+    else mid = fmaf(x, x, mid);         // NaN too
+  };
+  auto next = [&] {
+    row += down;
+    col += right;
+    if (col >= per_row) col -= per_row, ++row;
+  };
   constexpr int U = 4;                                              // in flight
-  for (; e < total; e += U * stride) {
-    float v[U][8];
+  if (it.vec_in && !it.mom && it.cols % 8 == 0) {
+    for (; e < total; e += U * stride) {
+      Raw8<T> raw[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      update8<T, true>(p, it, row, 8 * int(col), v[u]);             // zeros below the last row
-      row += down;
-      col += right;
-      if (col >= per_row) col -= per_row, ++row;
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float x = v[u][k], a = fabsf(x);
-        if (a > 0x1p40f) big = fmaf(x * 0x1p-80f, x * 0x1p-80f, big);
-        else if (a < 0x1p-40f) small = fmaf(x * 0x1p80f, x * 0x1p80f, small);
-        else mid = fmaf(x, x, mid);     // NaN too
+      for (int u = 0; u < U; ++u) {
+        raw[u].zero();
+        if (row < it.rows) raw[u].load(static_cast<const T*>(it.g) + row * it.ldg + 8 * col);
+        next();
       }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float v[8];
+        raw[u].get(v);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) add(v[k]);
+      }
+    }
+  } else {
+    for (; e < total; e += stride) {
+      float v[8];
+      update8<T, true>(p, it, row, 8 * int(col), v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) add(v[k]);
+      next();
+    }
   }
-  double s = double(mid) + double(big) * 0x1p160 + double(small) * 0x1p-160;
+  mid = warp_sum(mid);
+  big = warp_sum(big);
+  small = warp_sum(small);
+  if (threadIdx.x % 32 == 0) box[threadIdx.x / 32] = make_float4(mid, big, small, 0.f);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < 8; ++w) {
+      mid += box[w].x;
+      big += box[w].y;
+      small += box[w].z;
+    }
+    p.sums[n * kMaxSums + part] = double(mid) + double(big) * 0x1p160 + double(small) * 0x1p-160;
+  }
+}
+
+// X = U (kUpX / (|U| + eps)): the factor as a power of two, which goes first, and
+// a rest near kUpX, so that neither leaves fp32's range.  A kernel of its own:
+// double arithmetic in every block of the next one cost more than a launch.
+__global__ void __launch_bounds__(128) ortho_scale_k(const __grid_constant__ OrthoParams p) {
+  __shared__ double box[4];
+  pdl_wait();
+  pdl_trigger();
+  const int n = blockIdx.x;
+  const double* from = p.sums + n * kMaxSums;
+  double s = 0.0;
+#pragma unroll
+  for (int i = 0; i < kMaxSums / 128; ++i) s += int(threadIdx.x) + 128 * i < p.item[n].nsums ? from[threadIdx.x + 128 * i] : 0.0;
 #pragma unroll
   for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if (threadIdx.x % 32 == 0) box[threadIdx.x / 32] = s;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < 8; ++w) s += box[w];
-    p.sums[n * kMaxSums + part] = s;
-  }
+  if (threadIdx.x) return;
+  for (int w = 1; w < 4; ++w) s += box[w];
+  const double norm = sqrt(s) + p.eps;
+  int k = 0;
+  const double part = frexp(norm, &k);        // norm = part 2^k
+  p.scale[n] = isfinite(norm) ? make_float2(ldexpf(1.f, min(127, -k)), float(double(kUpX) / part)) : make_float2(float(1.0 / norm), 1.f);
 }
 
 __device__ __forceinline__ uint32_t half_pair(float a, float b) {
@@ -194,42 +241,24 @@ __device__ __forceinline__ uint4 take_half8(float* v) {
 template <typename T>
 __global__ void __launch_bounds__(256) ortho_pack_k(const __grid_constant__ OrthoParams p) {
   __shared__ float tile[64][65];
-  __shared__ double box[8];
-  __shared__ float scale[2];
-  static_assert(kMaxSums == 256, "one partial sum per thread");
   pdl_wait();
   pdl_trigger();
   const int n = slot_of(p, blockIdx.x);
   const Item& it = p.item[n];
   const int blk = int(blockIdx.x) - p.start[n], rows = 2 * it.mt;
   const int rb = blk % rows, cb = blk / rows, t = threadIdx.x, row = t / 4;
-  double s = t < it.nsums ? p.sums[n * kMaxSums + t] : 0.0;
   // the user's matrix: two groups of eight of one row
   const int r0 = 64 * (it.transposed ? cb : rb), c0 = 64 * (it.transposed ? rb : cb);
   float v[2][8];
 #pragma unroll
   for (int h = 0; h < 2; ++h) update8<T, false>(p, it, r0 + row, c0 + 8 * (t % 4 * 2 + h), v[h]);
-#pragma unroll
-  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if (t % 32 == 0) box[t / 32] = s;
+  const float2 scale = p.scale[n];
   if (it.transposed)
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int e = 0; e < 8; ++e) tile[row][8 * (t % 4 * 2 + h) + e] = v[h][e];
-  __syncthreads();
-  if (t == 0) {
-    for (int w = 1; w < 8; ++w) s += box[w];
-    const double norm = sqrt(s) + p.eps;
-    // a power of two first, so that neither factor leaves fp32's range
-    int k = 0;
-    const double part = frexp(norm, &k);        // norm = part 2^k
-    const bool fine = isfinite(norm);
-    scale[0] = fine ? ldexpf(1.f, min(127, -k)) : float(1.0 / norm);
-    scale[1] = fine ? float(double(kUpX) / part) : 1.f;
-  }
-  __syncthreads();
-  const float s1 = scale[0], s2 = scale[1];
+  if (it.transposed) __syncthreads();
   char* img = p.ws + it.x[0] + (cb * int64_t(rows) + rb) * kBlock + row * 128;
   const int64_t image = int64_t(it.mt) * it.nt * 4 * kBlock;
 #pragma unroll
@@ -237,7 +266,7 @@ __global__ void __launch_bounds__(256) ortho_pack_k(const __grid_constant__ Orth
     const int u = t % 4 * 2 + h, at = (u ^ (row & 7)) * 16;
     float z[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) z[e] = (it.transposed ? tile[8 * u + e][row] : v[h][e]) * s1 * s2;
+    for (int e = 0; e < 8; ++e) z[e] = (it.transposed ? tile[8 * u + e][row] : v[h][e]) * scale.x * scale.y;
     *reinterpret_cast<uint4*>(img + at) = take_half8(z);
     *reinterpret_cast<uint4*>(img + image + at) = take_half8(z);
   }
@@ -254,9 +283,9 @@ struct Tiles {
   static constexpr int kA = 2 * kBlock, kB = BN / 128 * kBlock;
   static constexpr int kStage = PARTS * (kA + kB), kStages = 196608 / kStage;
   static constexpr int kOut = 8 * 4096;       // 4 KB per warp of arithmetic
-  static constexpr int kBars = 3 * kStages + 5;
+  static constexpr int kSumsAt = 512 / BN;    // tiles' sums in tensor memory
+  static constexpr int kBars = 3 * kStages + 2 * kSumsAt + 1;
   static constexpr int kSmem = 1024 + kStages * kStage + kOut + 8 * kBars + 16;
-  static constexpr uint32_t kCols = 2 * BN;   // two tiles' sums
 };
 static_assert(Tiles<1, 256>::kSmem <= 232448 && Tiles<1, 128>::kSmem <= 232448 && Tiles<2, 128>::kSmem <= 232448, "shared memory per CTA");
 
@@ -292,7 +321,9 @@ __device__ __forceinline__ bool mirrored(int i, int kb) { return i / 2 > kb / 4;
 
 // Arrivals, products and commits of the two CTAs.  Arrivals and waits keep the
 // default scope: with release and acquire at cluster scope each block of terms
-// took 1 us (4096 x 4096: 2361 us).
+// took 1 us (4096 x 4096: 2361 us).  Copies are plain ones to this CTA's barrier,
+// of which a warp tells the leader; tensor copies that complete on the leader's
+// barrier themselves were 10% slower on 256 x 256 tiles (rows of 128 bytes).
 __device__ __forceinline__ void arrive_leader(uint64_t* bar) {
   asm volatile(
       "{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, 0;\n mbarrier.arrive.shared::cluster.b64 _, [r];\n}\n" ::"r"(
@@ -327,25 +358,36 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
   } else {
     // C = b A + c A A, or a X + C X
     const float linear = PHASE == kPoly ? p.cb : p.ca, other = (PHASE == kPoly ? p.cc : 1.f) / kUpA;
-    const char* src = p.ws + (PHASE == kPoly ? m.a : m.x[p.from]) + half_block + lane * 128;
+    // the warp's 4 KB are read as they lie, and handed out by rows through shared memory
+    const uint4* src = reinterpret_cast<const uint4*>(p.ws + (PHASE == kPoly ? m.a : m.x[p.from]) + half_block) + lane;
     constexpr int kParts = PHASE == kPoly ? PARTS : 2;
-    const int64_t image = PHASE == kPoly ? si : xi;
+    const int64_t image = (PHASE == kPoly ? si : xi) / 16;
+    uint4 w[kParts][8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int off = (k ^ (lane & 7)) * 16;
+    for (int part = 0; part < kParts; ++part)
 #pragma unroll
-      for (int part = kParts - 1; part >= 0; --part) {
-        const uint4 w = *reinterpret_cast<const uint4*>(src + part * image + off);
-        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+      for (int k = 0; k < 8; ++k) w[part][k] = src[part * image + 32 * k];
+    if (lane == 0) bulk_wait_read<0>();       // the last store has read the buffer
+#pragma unroll
+    for (int part = kParts - 1; part >= 0; --part) {
+      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < 8; ++k) st_shared4(buf + (32 * k + lane) * 16, w[part][k].x, w[part][k].y, w[part][k].z, w[part][k].w);
+      __syncwarp();
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float4 u = ld_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16);
+        const float z[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const float2 f = of_pair(ww[e]);
+          const float2 f = of_pair(__float_as_uint(z[e]));
           float &x = v[8 * k + 2 * e], &y = v[8 * k + 2 * e + 1];
           x = fmaf(linear, f.x, part == kParts - 1 ? x * other : x);
           y = fmaf(linear, f.y, part == kParts - 1 ? y * other : y);
         }
       }
     }
+    __syncwarp();
   }
   if (PHASE == kApply && p.last) {
     constexpr float down = 1.f / kUpX;
@@ -427,8 +469,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   char* stage_out = smem + S::kStages * S::kStage;
   uint64_t* full = reinterpret_cast<uint64_t*>(stage_out + S::kOut);
-  uint64_t *peer = full + S::kStages, *empty = peer + S::kStages, *acc_full = empty + S::kStages, *acc_empty = acc_full + 2,
-           *done = acc_empty + 2;
+  uint64_t *peer = full + S::kStages, *empty = peer + S::kStages, *acc_full = empty + S::kStages, *acc_empty = acc_full + S::kSumsAt,
+           *done = acc_empty + S::kSumsAt;
   uint32_t* tslot = reinterpret_cast<uint32_t*>(done + 1);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int units = p.start[p.count], pair = int(blockIdx.x) / 2, pairs = int(gridDim.x) / 2, me = int(blockIdx.x) % 2;
@@ -439,7 +481,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
       mbar_init(&peer[e], 1);
       mbar_init(&empty[e], 1);
     }
-    for (int e = 0; e < 2; ++e) {
+    for (int e = 0; e < S::kSumsAt; ++e) {
       mbar_init(&acc_full[e], 1);
       mbar_init(&acc_empty[e], 16);        // one arrival per warp of arithmetic, of both CTAs
     }
@@ -447,7 +489,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tslot)), "r"(S::kCols)
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tslot)), "r"(512)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
@@ -532,16 +574,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
     // kind::f16 with fp16 operands, fp32 sums, M = 256, N = BN
     constexpr uint32_t id = (1u << 4) | uint32_t(BN >> 3) << 17 | (256u >> 4) << 24;
     Ring<S::kStages> at;
-    uint32_t pass = 0;
+    Ring<S::kSumsAt> sum;
     const uint32_t ring = smem_u32(smem);
     bool dead = false;
     for (int u = pair; u < units && !dead; u += pairs) {
       const Place a = place_of<PHASE, BN>(p, u);
       const int tb = BN == 256 ? 2 * a.j : a.j;
       for (int kb = 0; kb < a.kb; ++kb) {
-        const uint32_t d = tmem + (pass & 1) * BN;
+        const uint32_t d = tmem + sum.at * BN;
         const bool fresh = PARTS == 2 || kb == 0;
-        if (fresh) wait.on(&acc_empty[pass & 1], ((pass >> 1) & 1) ^ 1, 62);
+        if (fresh) wait.on(&acc_empty[sum.at], sum.phase ^ 1, 62);
         wait.on(&full[at.at], at.phase, 63);
         wait.on(&peer[at.at], at.phase, 66);
         __syncwarp();
@@ -567,7 +609,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
           mma_pair(d, desc(k * as, al), desc(b0 + k * bs, bl), idesc, PARTS == 2 || kb > 0 || k > 0 ? 1u : 0u);
         commit_pair(&empty[at.at]);
         at.step();
-        if (PARTS == 2 || kb + 1 == a.kb) commit_pair(&acc_full[pass++ & 1]);
+        if (PARTS == 2 || kb + 1 == a.kb) {
+          commit_pair(&acc_full[sum.at]);
+          sum.step();
+        }
         // off the waits' path; what was issued after one gave up is void anyway
         dead = __any_sync(0xffffffffu, wait.dead);
         if (dead) break;
@@ -586,7 +631,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
     constexpr int NB = BN / 128;
     const uint32_t col = tmem + (uint32_t(32 * q) << 16) + (BN / 2) * half;
     const uint32_t buf = smem_u32(stage_out) + uint32_t(warp - 2) * 4096u;
-    uint32_t pass = 0;
+    Ring<S::kSumsAt> sum;
     bool dead = false;
     for (int u = pair; u < units && !dead; u += pairs) {
       const Place a = place_of<PHASE, BN>(p, u);
@@ -595,14 +640,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
       const int tile = 2 * a.i + me, cblk = a.j * (BN / 64) + half * NB, cols = 2 * (PHASE == kApply ? m.nt : m.mt);
       float v[PARTS == 2 ? NB : 1][64];
       if (PARTS == 2) {
-        for (int kb = 0; kb < a.kb; ++kb, ++pass) {
-          wait.on(&acc_full[pass & 1], (pass >> 1) & 1, 64);
+        for (int kb = 0; kb < a.kb; ++kb) {
+          wait.on(&acc_full[sum.at], sum.phase, 64);
           __syncwarp();
           tc_fence_after();
 #pragma unroll
           for (int h = 0; h < 2 * NB; ++h) {
             uint32_t r[32];
-            tmem_ld32(col + (pass & 1) * BN + 32 * h, r);
+            tmem_ld32(col + sum.at * BN + 32 * h, r);
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
               float& x = v[h / 2][32 * (h % 2) + e];
@@ -611,7 +656,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
           }
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) arrive_leader(&acc_empty[pass & 1]);
+          if (lane == 0) arrive_leader(&acc_empty[sum.at]);
+          sum.step();
         }
         dead = __any_sync(0xffffffffu, wait.dead);
         if (dead) break;
@@ -619,7 +665,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
         for (int b = 0; b < NB; ++b)
           if (tile < m.mt && cblk + b < cols) finish<PARTS, PHASE, T>(p, m, tile, cblk + b, q, lane, buf, v[b]);
       } else {
-        wait.on(&acc_full[pass & 1], (pass >> 1) & 1, 64);
+        wait.on(&acc_full[sum.at], sum.phase, 64);
         __syncwarp();
         tc_fence_after();
         dead = __any_sync(0xffffffffu, wait.dead);
@@ -628,18 +674,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             uint32_t r[32];
-            tmem_ld32(col + (pass & 1) * BN + 64 * b + 32 * h, r);
+            tmem_ld32(col + sum.at * BN + 64 * b + 32 * h, r);
 #pragma unroll
             for (int e = 0; e < 32; ++e) v[0][32 * h + e] = __uint_as_float(r[e]);
           }
           if (b == NB - 1) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) arrive_leader(&acc_empty[pass & 1]);
+            if (lane == 0) arrive_leader(&acc_empty[sum.at]);
           }
           if (!dead && tile < m.mt && cblk + b < cols) finish<PARTS, PHASE, T>(p, m, tile, cblk + b, q, lane, buf, v[0]);
         }
-        ++pass;
+        sum.step();
       }
     }
     if (lane == 0) bulk_wait_all();
@@ -650,7 +696,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
   cluster_sync_all();                // neither CTA is needed by the other any more
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::kCols) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
 }
 
@@ -670,7 +716,7 @@ int check_items(const fo_matrix_update* m, int count, int dtype) {
 int64_t item_bytes(const fo_matrix_update& m, int parts) {
   if (m.rows == 0 || m.cols == 0) return 0;
   const int64_t r = (m.rows + 127) / 128, c = (m.cols + 127) / 128, mt = r < c ? r : c, nt = r < c ? c : r;
-  return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + kMaxSums * 8;
+  return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + (kMaxSums + 1) * 8;
 }
 
 template <int PARTS, int BN, int PHASE, typename T>
@@ -737,6 +783,7 @@ cudaError_t orthogonalize(OrthoParams& p, int steps, cudaStream_t st) {
   }
   p.start[p.count] = int(units);
   if ((e = launch_k(ortho_sums_k<T>, dim3(unsigned(units)), dim3(256), 0, st, p)) != cudaSuccess) return e;
+  if ((e = launch_k(ortho_scale_k, dim3(unsigned(p.count)), dim3(128), 0, st, p)) != cudaSuccess) return e;
   units = 0;
   for (int i = 0; i < p.count; ++i) {
     p.start[i] = int(units);
@@ -796,8 +843,8 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
       return bad("bad row stride");
     if (!(std::fabs(m.step) <= 1e30f)) return bad("bad step");
   }
-  if (fo_orthogonalize_workspace(items, count, dtype) > 0 &&
-      (!workspace || odd(workspace, 256) || workspace_bytes < fo_orthogonalize_workspace(items, count, dtype)))
+  const int64_t need = fo_orthogonalize_workspace(items, count, dtype);
+  if (need > 0 && (!workspace || odd(workspace, 256) || workspace_bytes < need))
     return bad("the workspace is missing, misaligned or too small");
   const int parts = dtype == FO_DTYPE_F32 ? 2 : 1;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -848,6 +895,7 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
     }
     if (p.count == 0) continue;
     p.sums = reinterpret_cast<double*>(p.ws + at);
+    p.scale = reinterpret_cast<float2*>(p.sums + p.count * kMaxSums);
     const cudaError_t e = dtype == FO_DTYPE_F32 ? orthogonalize<float>(p, steps, st) : orthogonalize<bf16>(p, steps, st);
     if (e != cudaSuccess) return done(e);
   }
