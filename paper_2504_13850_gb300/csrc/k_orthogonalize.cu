@@ -193,9 +193,16 @@ __global__ void __launch_bounds__(256) ortho_sums_k(const __grid_constant__ Orth
   }
 }
 
-// X = U (kUpX / (|U| + eps)): the factor as a power of two, which goes first, and
-// a rest near kUpX, so that neither leaves fp32's range.  A kernel of its own:
-// double arithmetic in every block of the next one cost more than a launch.
+// X = U (kUpX / (|U| + eps)), |U|^2 = s: the factor as a power of two, which goes
+// first, and a rest near kUpX, so that neither leaves fp32's range.
+__device__ __forceinline__ float2 scale_of(double s, double eps) {
+  const double norm = sqrt(s) + eps;
+  int k = 0;
+  const double part = frexp(norm, &k);        // norm = part 2^k
+  return isfinite(norm) ? make_float2(ldexpf(1.f, min(127, -k)), float(double(kUpX) / part)) : make_float2(float(1.0 / norm), 1.f);
+}
+// A kernel of its own: double arithmetic in every block of the next one cost more
+// than a launch.
 __global__ void __launch_bounds__(128) ortho_scale_k(const __grid_constant__ OrthoParams p) {
   __shared__ double box[4];
   pdl_wait();
@@ -211,10 +218,7 @@ __global__ void __launch_bounds__(128) ortho_scale_k(const __grid_constant__ Ort
   __syncthreads();
   if (threadIdx.x) return;
   for (int w = 1; w < 4; ++w) s += box[w];
-  const double norm = sqrt(s) + p.eps;
-  int k = 0;
-  const double part = frexp(norm, &k);        // norm = part 2^k
-  p.scale[n] = isfinite(norm) ? make_float2(ldexpf(1.f, min(127, -k)), float(double(kUpX) / part)) : make_float2(float(1.0 / norm), 1.f);
+  p.scale[n] = scale_of(s, p.eps);
 }
 
 __device__ __forceinline__ uint32_t half_pair(float a, float b) {
@@ -345,10 +349,70 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar) {     // the barrier 
       : "memory");
 }
 
+// 64 elements of kUpX X, row 128 tile + 32 q + lane and columns 64 cblk .., to the caller.
+template <typename T>
+__device__ __forceinline__ void deliver(const OrthoParams& p, const Item& m, int tile, int cblk, int q, int lane, uint32_t buf, float (&v)[64]) {
+  const int row = 128 * tile + 32 * q + lane, c0 = 64 * cblk;
+  constexpr float down = 1.f / kUpX;
+  const int side = m.transposed ? m.cols : m.rows, wide = m.transposed ? m.rows : m.cols;
+#pragma unroll
+  for (int e = 0; e < 64; ++e) v[e] *= down;
+  if (m.transposed) {       // a row here is a column there: lanes are neighbours
+    if (row >= side) return;
+    if (m.out) {
+      T* o = static_cast<T*>(m.out) + c0 * m.ldo + row;
+#pragma unroll
+      for (int e = 0; e < 64; ++e, o += m.ldo)
+        if (c0 + e < wide) *o = from_f<T>(v[e]);
+    }
+    if (m.param) {
+      float* w = m.param + c0 * m.ldp + row;
+#pragma unroll
+      for (int e = 0; e < 64; ++e, w += m.ldp)
+        if (c0 + e < wide) *w = fmaf(-m.step, v[e], *w * p.decay);
+    }
+    return;
+  }
+  // 32 columns at a time through shared memory: eight lanes then hold a row's
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      st_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16, __float_as_uint(v[32 * h + 4 * k]), __float_as_uint(v[32 * h + 4 * k + 1]),
+                 __float_as_uint(v[32 * h + 4 * k + 2]), __float_as_uint(v[32 * h + 4 * k + 3]));
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int rr = 4 * i + lane / 8, r = 128 * tile + 32 * q + rr, c = c0 + 32 * h + 4 * (lane % 8);
+      const float4 x = ld_shared4(buf + rr * 128 + ((lane % 8) ^ (rr & 7)) * 16);
+      if (r >= side || c >= wide) continue;
+      const float z[4] = {x.x, x.y, x.z, x.w};
+      if (m.out) {
+        T* o = static_cast<T*>(m.out) + r * m.ldo + c;
+        if (m.vec_out && c + 4 <= wide) {
+          if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(o) = x;
+          else *reinterpret_cast<uint2*>(o) = make_uint2(bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (c + e < wide) o[e] = from_f<T>(z[e]);
+        }
+      }
+      if (m.param) {
+        float* w = m.param + r * m.ldp + c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (c + e < wide) w[e] = fmaf(-m.step, z[e], w[e] * p.decay);
+      }
+    }
+  }
+  __syncwarp();
+}
+
 // 64 sums of one row, columns 64 cblk .., become elements of A, C or X.
 template <int PARTS, int PHASE, typename T>
 __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int tile, int cblk, int q, int lane, uint32_t buf, float (&v)[64]) {
-  const int row = 128 * tile + 32 * q + lane, c0 = 64 * cblk;       // of the smaller and the larger side
   const int64_t block = int64_t(cblk) * 2 * m.mt + 2 * tile + q / 2;
   const int64_t half_block = block * kBlock + (q & 1) * 4096;       // this warp's 32 rows
   const int64_t xi = int64_t(m.mt) * m.nt * 4 * kBlock, si = int64_t(m.mt) * m.mt * 4 * kBlock;
@@ -390,56 +454,7 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
     __syncwarp();
   }
   if (PHASE == kApply && p.last) {
-    constexpr float down = 1.f / kUpX;
-    const int side = m.transposed ? m.cols : m.rows, wide = m.transposed ? m.rows : m.cols;
-    if (m.transposed) {       // a row here is a column there: lanes are neighbours
-      if (row < side)
-#pragma unroll
-        for (int e = 0; e < 64; ++e)
-          if (c0 + e < wide) {
-            const float x = v[e] * down;
-            if (m.out) static_cast<T*>(m.out)[(c0 + e) * m.ldo + row] = from_f<T>(x);
-            if (m.param) {
-              float* w = m.param + (c0 + e) * m.ldp + row;
-              *w = fmaf(-m.step, x, *w * p.decay);
-            }
-          }
-      return;
-    }
-    // 32 columns at a time through shared memory: eight lanes then hold a row's
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      __syncwarp();
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        st_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16, __float_as_uint(v[32 * h + 4 * k] * down), __float_as_uint(v[32 * h + 4 * k + 1] * down),
-                   __float_as_uint(v[32 * h + 4 * k + 2] * down), __float_as_uint(v[32 * h + 4 * k + 3] * down));
-      __syncwarp();
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int rr = 4 * i + lane / 8, r = 128 * tile + 32 * q + rr, c = c0 + 32 * h + 4 * (lane % 8);
-        const float4 x = ld_shared4(buf + rr * 128 + ((lane % 8) ^ (rr & 7)) * 16);
-        if (r >= side || c >= wide) continue;
-        const float z[4] = {x.x, x.y, x.z, x.w};
-        if (m.out) {
-          T* o = static_cast<T*>(m.out) + r * m.ldo + c;
-          if (m.vec_out && c + 4 <= wide) {
-            if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(o) = x;
-            else *reinterpret_cast<uint2*>(o) = make_uint2(bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3]));
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (c + e < wide) o[e] = from_f<T>(z[e]);
-          }
-        }
-        if (m.param) {
-          float* w = m.param + r * m.ldp + c;
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (c + e < wide) w[e] = fmaf(-m.step, z[e], w[e] * p.decay);
-        }
-      }
-    }
+    deliver<T>(p, m, tile, cblk, q, lane, buf, v);
     return;
   }
   char* dst = p.ws + (PHASE == kGram ? m.a : PHASE == kPoly ? m.c : m.x[p.from ^ 1]) + half_block;
@@ -700,6 +715,266 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
   }
 }
 
+// ------------------------------------------------------------ up to 128 rows
+// A matrix whose smaller side is at most 128 and the larger one at most 2048 stays
+// in shared memory for all steps: each of up to eight CTAs of a cluster holds all
+// rows of 256 columns of X (two parts), forms its columns' part of X X^T, and,
+// with the sum of the parts, all of A A and C and its own columns of C X.  The
+// parts are exchanged through the workspace (L2).  One launch for all such
+// matrices of a list.  A step is a chain of three products on one SM, each too
+// short to fill it: its latency is what counts, and launches of their own cost
+// more (200 x 96 fp32: 143 us).
+constexpr int kSmallRows = 128, kSmallCols = 256, kSmallCtas = 8;
+constexpr int kSmallThreads = 256;
+constexpr int kSmallX = 8 * kBlock, kSmallA = 4 * kBlock;             // one part of X, of A or C
+constexpr int kSmallSmem = 1024 + 2 * kSmallX + 2 * kSmallA + 192;
+constexpr int kSmallPart = kSmallRows * kSmallRows * 4;                // of X X^T
+static_assert(kSmallSmem <= 232448, "shared memory per CTA");
+
+// 64 elements of a row, starting at a block's row, as one or two parts of fp16.
+template <int PARTS>
+__device__ __forceinline__ void put_row(uint32_t at, uint32_t part, int row, float (&v)[64]) {
+#pragma unroll
+  for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const uint4 w = take_half8(v + 8 * k);
+      st_shared4(at + q * part + row * 128 + (k ^ (row & 7)) * 16, w.x, w.y, w.z, w.w);
+    }
+}
+
+template <int PARTS, typename T>
+__global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThreads, 1) ortho_small_k(const __grid_constant__ OrthoParams p, int steps) {
+  extern __shared__ char smem_raw[];
+  char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, t = threadIdx.x;
+  const Item& m = p.item[blockIdx.x / kSmallCtas];
+  const int me = blockIdx.x % kSmallCtas;
+  const int rows = m.transposed ? m.cols : m.rows, cols = m.transposed ? m.rows : m.cols;      // rows <= cols
+  const int ctas = (cols + kSmallCols - 1) / kSmallCols, col0 = me * kSmallCols;
+  if (me >= ctas) return;
+  const int blocks = (min(cols - col0, kSmallCols) + 63) / 64;       // of 64 columns, here
+  const uint32_t sx = smem_u32(smem), sa = sx + 2 * kSmallX;
+  uint64_t* bar = reinterpret_cast<uint64_t*>(smem + 2 * kSmallX + 2 * kSmallA);
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(bar + 1);
+  float4* box = reinterpret_cast<float4*>(bar + 4);
+  if (t == 0) {
+    mbar_init(bar, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tslot)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tslot;
+  pdl_trigger();                     // this block holds its tensor memory
+  pdl_wait();
+  Waits wait(&g_err);
+
+  // the norm, over all columns
+  {
+    float mid = 0.f, big = 0.f, small = 0.f;
+    const int here = min(cols - col0, kSmallCols);
+    const int n_rows = m.transposed ? here : rows, per_row = ((m.transposed ? rows : here) + 7) / 8;
+    const int first_row = m.transposed ? col0 : 0, first_col = m.transposed ? 0 : col0;
+    for (int e = t; e < n_rows * per_row; e += kSmallThreads) {
+      const int r = e / per_row, c = e - r * per_row;
+      float v[8];
+      update8<T, true>(p, m, first_row + r, first_col + 8 * c, v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float x = v[k], a = fabsf(x);
+        if (a > 0x1p40f) big = fmaf(x * 0x1p-80f, x * 0x1p-80f, big);
+        else if (a < 0x1p-40f) small = fmaf(x * 0x1p80f, x * 0x1p80f, small);
+        else mid = fmaf(x, x, mid);         // NaN too
+      }
+    }
+    mid = warp_sum(mid);
+    big = warp_sum(big);
+    small = warp_sum(small);
+    if (lane == 0) box[warp] = make_float4(mid, big, small, 0.f);
+    __syncthreads();
+    if (t == 0) {
+      for (int w = 1; w < 8; ++w) {
+        mid += box[w].x;
+        big += box[w].y;
+        small += box[w].z;
+      }
+      const double s = double(mid) + double(big) * 0x1p160 + double(small) * 0x1p-160;
+      reinterpret_cast<double*>(p.ws + m.a)[me] = s;
+    }
+    if (ctas > 1) cluster_sync_all();
+    if (t == 0) {
+      double s = 0.0;
+      for (int i = 0; i < ctas; ++i) s += __ldcg(reinterpret_cast<const double*>(p.ws + m.a) + i);
+      const float2 f = scale_of(s, p.eps);
+      box[1] = make_float4(f.x, f.y, 0.f, 0.f);
+    }
+    __syncthreads();
+  }
+  const float s1 = box[1].x, s2 = box[1].y;
+  // X: units of eight columns of a row (or of eight rows of a column)
+  if (!m.transposed) {
+    for (int e = t; e < kSmallRows * 8 * blocks; e += kSmallThreads) {
+      const int r = e / (8 * blocks), u = e - r * 8 * blocks;
+      float v[8];
+      update8<T, false>(p, m, r, col0 + 8 * u, v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = v[k] * s1 * s2;
+      const uint32_t at = sx + (u / 8) * 2 * kBlock + r * 128 + ((u % 8) ^ (r & 7)) * 16;
+      uint4 w = take_half8(v);
+      st_shared4(at, w.x, w.y, w.z, w.w);
+      w = take_half8(v);
+      st_shared4(at + kSmallX, w.x, w.y, w.z, w.w);
+    }
+  } else {
+    for (int e = t; e < 16 * 64 * blocks; e += kSmallThreads) {      // lanes along the columns
+      const int c = e % (64 * blocks), r = e / (64 * blocks) * 8;
+      float v[8];
+      update8<T, false>(p, m, col0 + c, r, v);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float x = v[k] * s1 * s2;
+        const __half hi = __float2half_rn(x), lo = __float2half_rn(x - __half2float(hi));
+        char* at = smem + (c / 64) * 2 * kBlock + (r + k) * 128 + ((c % 64 / 8) ^ k) * 16 + c % 8 * 2;
+        *reinterpret_cast<__half*>(at) = hi;
+        *reinterpret_cast<__half*>(at + kSmallX) = lo;
+      }
+    }
+  }
+
+  // products: [128 x 64] . [N x 64] or . [64 x N] of one block of terms, the small ones first
+  constexpr uint32_t id = (1u << 4) | (128u >> 4) << 24;
+  auto product = [&](uint32_t d, uint32_t a, uint32_t a_part, uint32_t b, uint32_t b_part, int n, bool flip) {
+    constexpr uint32_t hi = (1024u >> 4) | (1u << 14) | (2u << 29);      // stride 1024, version 1, 128-byte swizzle
+    const uint32_t idesc = id | uint32_t(n >> 3) << 17 | uint32_t(flip) << 16, bs = flip ? 2048u : 32u;
+    const uint32_t bl = (flip ? uint32_t(2 * kBlock) : 16u) >> 4 << 16;
+    auto desc = [&](uint32_t at, uint32_t lbo) { return uint64_t((at & 0x3ffff) >> 4 | lbo) | uint64_t(hi) << 32; };
+    if (PARTS == 2) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        mma_ss(d, desc(a + 32 * k, 1u << 16), desc(b + b_part + bs * k, bl), idesc, k > 0 ? 1u : 0u);
+        mma_ss(d, desc(a + a_part + 32 * k, 1u << 16), desc(b + bs * k, bl), idesc, 1u);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      mma_ss(d, desc(a + 32 * k, 1u << 16), desc(b + bs * k, bl), idesc, PARTS == 2 || k > 0 ? 1u : 0u);
+  };
+  uint32_t phase = 0;
+  auto begin = [&] {                 // what the warps wrote is there for the products
+    fence_proxy_async_smem();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+  };
+  auto finished = [&] {
+    wait.on_lanes(bar, phase, 68);
+    phase ^= 1;
+    tc_fence_after();
+  };
+  const int q = warp % 4, half = warp / 4, row = 32 * q + lane;
+  const uint32_t lanes = tmem + (uint32_t(32 * q) << 16);
+  const uint32_t a_row = sa + half * 2 * kBlock;       // rows of A and C: all of a block column's 128 lie behind one another
+  for (int step = 0; step < steps; ++step) {
+    begin();
+    if (warp == 0) {
+      for (int c = 0; c < blocks; ++c) {
+        const uint32_t x = sx + c * 2 * kBlock;
+        product(tmem + 128 * c, x, kSmallX, x, kSmallX, 128, false);
+      }
+      commit_to(bar);
+    }
+    finished();
+    float v[64];
+#pragma unroll
+    for (int e = 0; e < 64; ++e) v[e] = 0.f;
+    auto sum = [&](uint32_t from, int n, uint32_t step_cols) {
+      for (int c = 0; c < n; ++c)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t r[32];
+          tmem_ld32(from + step_cols * c + 32 * h, r);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[32 * h + e] += __uint_as_float(r[e]);
+        }
+    };
+    sum(lanes + 64 * half, blocks, 128);
+    if (ctas > 1) {
+      // [step parity][CTA][16][thread] of four
+      float4* parts = reinterpret_cast<float4*>(p.ws + m.x[step & 1]);
+#pragma unroll
+      for (int k = 0; k < 16; ++k)
+        __stcg(parts + (me * 16 + k) * kSmallThreads + t, make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
+      cluster_sync_all();
+#pragma unroll
+      for (int e = 0; e < 64; ++e) v[e] = 0.f;
+      for (int i = 0; i < ctas; ++i)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const float4 z = __ldcg(parts + (i * 16 + k) * kSmallThreads + t);
+          v[4 * k] += z.x;
+          v[4 * k + 1] += z.y;
+          v[4 * k + 2] += z.z;
+          v[4 * k + 3] += z.w;
+        }
+    }
+    float A[64];
+#pragma unroll
+    for (int e = 0; e < 64; ++e) A[e] = v[e] *= kUpA / (kUpX * kUpX);
+    put_row<PARTS>(a_row, kSmallA, row, v);
+    begin();
+    if (warp == 0) {
+      for (int c = 0; c < 2; ++c) product(tmem + 128 * c, sa + c * 2 * kBlock, kSmallA, sa + c * 2 * kBlock, kSmallA, 128, false);
+      commit_to(bar);
+    }
+    finished();
+#pragma unroll
+    for (int e = 0; e < 64; ++e) v[e] = 0.f;
+    sum(lanes + 64 * half, 2, 128);
+#pragma unroll
+    for (int e = 0; e < 64; ++e) v[e] = fmaf(p.cc / kUpA, v[e], p.cb * A[e]);
+    put_row<PARTS>(a_row, kSmallA, row, v);
+    begin();
+    if (warp == 0) {
+      for (int c = 0; c < 2; ++c)
+        product(tmem + 256 * c, sa + c * 2 * kBlock, kSmallA, sx + c * kBlock, kSmallX, 64 * blocks, true);
+      commit_to(bar);
+    }
+    finished();
+    for (int b = half; b < blocks; b += 2) {
+#pragma unroll
+      for (int e = 0; e < 64; ++e) v[e] = 0.f;
+      sum(lanes + 64 * b, 2, 256);
+      const uint32_t x_row = sx + b * 2 * kBlock + row * 128;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int off = (k ^ (row & 7)) * 16;
+        const float4 hi = ld_shared4(x_row + off), lo = ld_shared4(x_row + kSmallX + off);
+        const float zh[4] = {hi.x, hi.y, hi.z, hi.w}, zl[4] = {lo.x, lo.y, lo.z, lo.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 fh = of_pair(__float_as_uint(zh[e])), fl = of_pair(__float_as_uint(zl[e]));
+          float &x = v[8 * k + 2 * e], &y = v[8 * k + 2 * e + 1];
+          x = fmaf(p.ca, fh.x, fmaf(p.ca, fl.x, x * (1.f / kUpA)));
+          y = fmaf(p.ca, fh.y, fmaf(p.ca, fl.y, y * (1.f / kUpA)));
+        }
+      }
+      if (step + 1 < steps) put_row<2>(sx + b * 2 * kBlock, kSmallX, row, v);
+      else deliver<T>(p, m, 0, col0 / 64 + b, q, lane, sa + warp * 4096, v);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
 // ---------------------------------------------------------------------- host
 int bad(const std::string& why) { return report_error(FO_ERR_ARG, "orthogonalize: " + why); }
 int done(cudaError_t e) { return e == cudaSuccess ? FO_OK : report_error(FO_ERR_CUDA, cudaGetErrorString(e)); }
@@ -713,8 +988,14 @@ int check_items(const fo_matrix_update* m, int count, int dtype) {
   }
   return FO_OK;
 }
+bool is_small(const fo_matrix_update& m) {
+  const int64_t lo = m.rows < m.cols ? m.rows : m.cols, hi = m.rows < m.cols ? m.cols : m.rows;
+  return lo <= kSmallRows && hi <= kSmallCols * kSmallCtas;
+}
+// Small matrices: parts of X X^T of even and odd steps, and of the norm.
 int64_t item_bytes(const fo_matrix_update& m, int parts) {
   if (m.rows == 0 || m.cols == 0) return 0;
+  if (is_small(m)) return 2 * kSmallCtas * kSmallPart + 256;
   const int64_t r = (m.rows + 127) / 128, c = (m.cols + 127) / 128, mt = r < c ? r : c, nt = r < c ? c : r;
   return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + (kMaxSums + 1) * 8;
 }
@@ -768,6 +1049,14 @@ cudaError_t product(OrthoParams& p, int pairs, cudaStream_t st) {
   return launch_product<PARTS, 128, PHASE, T>(p, pairs, st);
 }
 
+template <typename T>
+cudaError_t orthogonalize_small(const OrthoParams& p, int steps, cudaStream_t st) {
+  auto k = ortho_small_k<sizeof(T) == 4 ? 2 : 1, T>;
+  static std::atomic<bool> allowed[kMaxDevices];
+  const cudaError_t e = allow_smem(k, allowed);
+  if (e != cudaSuccess) return e;
+  return launch_k(k, dim3(kSmallCtas * unsigned(p.count)), dim3(kSmallThreads), kSmallSmem, st, p, steps);
+}
 template <typename T>
 cudaError_t orthogonalize(OrthoParams& p, int steps, cudaStream_t st) {
   constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
@@ -848,7 +1137,8 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
     return bad("the workspace is missing, misaligned or too small");
   const int parts = dtype == FO_DTYPE_F32 ? 2 : 1;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  for (int first = 0; first < count; first += kItems) {
+  for (int first = 0; first < count; first += kItems)
+   for (const bool small : {true, false}) {
     OrthoParams p = {};
     p.ws = static_cast<char*>(workspace);
     p.ca = float(coefficients[0]);
@@ -866,7 +1156,7 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
     };
     for (int i = first; i < count && i < first + kItems; ++i) {
       const fo_matrix_update& m = items[i];
-      if (m.rows == 0 || m.cols == 0) continue;
+      if (m.rows == 0 || m.cols == 0 || is_small(m) != small) continue;
       Item& it = p.item[p.count++];
       it.g = m.grad;
       it.mom = m.momentum;
@@ -882,9 +1172,14 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
       const int64_t r = (m.rows + 127) / 128, c = (m.cols + 127) / 128;
       it.mt = int(r < c ? r : c);
       it.nt = int(r < c ? c : r);
-      for (int k = 0; k < 2; ++k) it.x[k] = take(int64_t(it.mt) * it.nt * 4 * kBlock * 2);
-      it.a = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
-      it.c = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
+      if (small) {
+        for (int k = 0; k < 2; ++k) it.x[k] = take(kSmallCtas * kSmallPart);
+        it.a = take(256);
+      } else {
+        for (int k = 0; k < 2; ++k) it.x[k] = take(int64_t(it.mt) * it.nt * 4 * kBlock * 2);
+        it.a = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
+        it.c = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
+      }
       const int64_t per = dtype == FO_DTYPE_F32 ? 4 : 8;
       it.vec_in = aligned16(m.grad) && (m.rows == 1 || m.grad_stride % per == 0) &&
                   (!m.momentum || (aligned16(m.momentum) && (m.rows == 1 || m.momentum_stride % 4 == 0)));
@@ -896,7 +1191,8 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
     if (p.count == 0) continue;
     p.sums = reinterpret_cast<double*>(p.ws + at);
     p.scale = reinterpret_cast<float2*>(p.sums + p.count * kMaxSums);
-    const cudaError_t e = dtype == FO_DTYPE_F32 ? orthogonalize<float>(p, steps, st) : orthogonalize<bf16>(p, steps, st);
+    const cudaError_t e = small ? (dtype == FO_DTYPE_F32 ? orthogonalize_small<float>(p, steps, st) : orthogonalize_small<bf16>(p, steps, st))
+                          : dtype == FO_DTYPE_F32 ? orthogonalize<float>(p, steps, st) : orthogonalize<bf16>(p, steps, st);
     if (e != cudaSuccess) return done(e);
   }
   return FO_OK;
