@@ -70,12 +70,12 @@ struct OrthoParams {
   int start[kItems + 1];    // first unit of work of each matrix in this launch
   uint8_t order[kItems];    // the matrices in the order of their units
   char* ws;
-  double* sums;
+  float4* sums;
   float2* scale;            // of each matrix: the two factors that make X of U
   int count, from, last;    // from: which X is read; last: X goes to the caller
   float ca, cb, cc, mu, decay;
   bool nesterov;
-  double eps;
+  float eps;
 };
 
 __device__ __forceinline__ int slot_of(const OrthoParams& p, int unit) {
@@ -124,8 +124,50 @@ __device__ __forceinline__ void update8(const OrthoParams& p, const Item& it, in
   }
 }
 
-// Sums of squares.  fp32 squares leave its range beyond 2^+-64; elements far
-// from 1 are squared in units of 2^80 or 2^-80 and summed apart.
+// X = U (kUpX / (|U| + eps)), |U| = root 2^unit: the factor as a power of two,
+// which goes first, and a rest near kUpX, so that neither leaves fp32's range.
+// (fp32 throughout: double arithmetic takes microseconds here.)
+__device__ __forceinline__ float2 factors(float root, int unit, float eps) {
+  const float n = root + scalbnf(eps, -unit);
+  if (!(n < INFINITY)) return make_float2(1.f / n, 1.f);
+  const int k = ilogbf(n);
+  return make_float2(scalbnf(1.f, min(127, -(unit + k))), kUpX / scalbnf(n, -k));
+}
+// Sums of squares of elements within 2^-40 .. 2^40, above (in units of 2^160) and
+// below (2^-160).
+struct Squares {
+  float mid, big, small;
+  __device__ __forceinline__ void add(float x) {
+    const float a = fabsf(x);
+    if (a > 0x1p40f) big = fmaf(x * 0x1p-80f, x * 0x1p-80f, big);
+    else if (a < 0x1p-40f) small = fmaf(x * 0x1p80f, x * 0x1p80f, small);
+    else mid = fmaf(x, x, mid);         // NaN too
+  }
+  __device__ __forceinline__ void add(const float4& o) {
+    mid += o.x;
+    big += o.y;
+    small += o.z;
+  }
+  // The sums over a block, in its first thread.
+  __device__ __forceinline__ float4 over_block(float4* box) {
+    mid = warp_sum(mid);
+    big = warp_sum(big);
+    small = warp_sum(small);
+    if (threadIdx.x % 32 == 0) box[threadIdx.x / 32] = make_float4(mid, big, small, 0.f);
+    __syncthreads();
+    if (threadIdx.x == 0)
+      for (unsigned w = 1; w < blockDim.x / 32; ++w) add(box[w]);
+    return make_float4(mid, big, small, 0.f);
+  }
+  // Root of the sum and its unit, a power of two.
+  __device__ __forceinline__ float root(int& unit) const {
+    unit = big > 0.f ? 40 : mid > 0.f ? 0 : -80;
+    const float r = big > 0.f ? hypotf(sqrtf(big) * 0x1p40f, sqrtf(mid) * 0x1p-40f)
+                              : mid > 0.f ? hypotf(sqrtf(mid), sqrtf(small) * 0x1p-80f) : sqrtf(small);
+    return r + (mid + big + small) * 0.f;        // NaN and infinity stay
+  }
+};
+
 template <typename T>
 __global__ void __launch_bounds__(256) ortho_sums_k(const __grid_constant__ OrthoParams p) {
   __shared__ float4 box[8];
@@ -139,13 +181,7 @@ __global__ void __launch_bounds__(256) ortho_sums_k(const __grid_constant__ Orth
   uint32_t col = uint32_t(e - row * per_row);
   const int64_t down = stride / per_row;
   const uint32_t right = uint32_t(stride - down * per_row);
-  float mid = 0.f, big = 0.f, small = 0.f;
-  auto add = [&](float x) {
-    const float a = fabsf(x);
-    if (a > 0x1p40f) big = fmaf(x * 0x1p-80f, x * 0x1p-80f, big);
-    else if (a < 0x1p-40f) small = fmaf(x * 0x1p80f, x * 0x1p80f, small);
-    else mid = fmaf(x, x, mid);         // NaN too
-  };
+  Squares sum = {};
   auto next = [&] {
     row += down;
     col += right;
@@ -166,7 +202,7 @@ __global__ void __launch_bounds__(256) ortho_sums_k(const __grid_constant__ Orth
         float v[8];
         raw[u].get(v);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) add(v[k]);
+        for (int k = 0; k < 8; ++k) sum.add(v[k]);
       }
     }
   } else {
@@ -174,51 +210,29 @@ __global__ void __launch_bounds__(256) ortho_sums_k(const __grid_constant__ Orth
       float v[8];
       update8<T, true>(p, it, row, 8 * int(col), v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) add(v[k]);
+      for (int k = 0; k < 8; ++k) sum.add(v[k]);
       next();
     }
   }
-  mid = warp_sum(mid);
-  big = warp_sum(big);
-  small = warp_sum(small);
-  if (threadIdx.x % 32 == 0) box[threadIdx.x / 32] = make_float4(mid, big, small, 0.f);
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < 8; ++w) {
-      mid += box[w].x;
-      big += box[w].y;
-      small += box[w].z;
-    }
-    p.sums[n * kMaxSums + part] = double(mid) + double(big) * 0x1p160 + double(small) * 0x1p-160;
-  }
+  const float4 all = sum.over_block(box);
+  if (threadIdx.x == 0) p.sums[n * kMaxSums + part] = all;
 }
 
-// X = U (kUpX / (|U| + eps)), |U|^2 = s: the factor as a power of two, which goes
-// first, and a rest near kUpX, so that neither leaves fp32's range.
-__device__ __forceinline__ float2 scale_of(double s, double eps) {
-  const double norm = sqrt(s) + eps;
-  int k = 0;
-  const double part = frexp(norm, &k);        // norm = part 2^k
-  return isfinite(norm) ? make_float2(ldexpf(1.f, min(127, -k)), float(double(kUpX) / part)) : make_float2(float(1.0 / norm), 1.f);
-}
-// A kernel of its own: double arithmetic in every block of the next one cost more
-// than a launch.
-__global__ void __launch_bounds__(128) ortho_scale_k(const __grid_constant__ OrthoParams p) {
-  __shared__ double box[4];
+__global__ void __launch_bounds__(256) ortho_scale_k(const __grid_constant__ OrthoParams p) {
+  __shared__ float4 box[8];
   pdl_wait();
   pdl_trigger();
   const int n = blockIdx.x;
-  const double* from = p.sums + n * kMaxSums;
-  double s = 0.0;
+  Squares sum = {};
 #pragma unroll
-  for (int i = 0; i < kMaxSums / 128; ++i) s += int(threadIdx.x) + 128 * i < p.item[n].nsums ? from[threadIdx.x + 128 * i] : 0.0;
-#pragma unroll
-  for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  if (threadIdx.x % 32 == 0) box[threadIdx.x / 32] = s;
-  __syncthreads();
-  if (threadIdx.x) return;
-  for (int w = 1; w < 4; ++w) s += box[w];
-  p.scale[n] = scale_of(s, p.eps);
+  for (int i = 0; i < kMaxSums / 256; ++i)
+    if (int(threadIdx.x) + 256 * i < p.item[n].nsums) sum.add(p.sums[n * kMaxSums + threadIdx.x + 256 * i]);
+  sum.over_block(box);
+  if (threadIdx.x == 0) {
+    int unit;
+    const float root = sum.root(unit);
+    p.scale[n] = factors(root, unit, p.eps);
+  }
 }
 
 __device__ __forceinline__ uint32_t half_pair(float a, float b) {
@@ -349,62 +363,57 @@ __device__ __forceinline__ void commit_pair(uint64_t* bar) {     // the barrier 
       : "memory");
 }
 
-// 64 elements of kUpX X, row 128 tile + 32 q + lane and columns 64 cblk .., to the caller.
+// 32 elements of kUpX X, row 128 tile + 32 q + lane and columns c0 .., to the caller.
 template <typename T>
-__device__ __forceinline__ void deliver(const OrthoParams& p, const Item& m, int tile, int cblk, int q, int lane, uint32_t buf, float (&v)[64]) {
-  const int row = 128 * tile + 32 * q + lane, c0 = 64 * cblk;
+__device__ __forceinline__ void deliver(const OrthoParams& p, const Item& m, int tile, int c0, int q, int lane, uint32_t buf, const float* v) {
+  const int row = 128 * tile + 32 * q + lane;
   constexpr float down = 1.f / kUpX;
   const int side = m.transposed ? m.cols : m.rows, wide = m.transposed ? m.rows : m.cols;
-#pragma unroll
-  for (int e = 0; e < 64; ++e) v[e] *= down;
   if (m.transposed) {       // a row here is a column there: lanes are neighbours
     if (row >= side) return;
     if (m.out) {
       T* o = static_cast<T*>(m.out) + c0 * m.ldo + row;
 #pragma unroll
-      for (int e = 0; e < 64; ++e, o += m.ldo)
-        if (c0 + e < wide) *o = from_f<T>(v[e]);
+      for (int e = 0; e < 32; ++e, o += m.ldo)
+        if (c0 + e < wide) *o = from_f<T>(v[e] * down);
     }
     if (m.param) {
       float* w = m.param + c0 * m.ldp + row;
 #pragma unroll
-      for (int e = 0; e < 64; ++e, w += m.ldp)
-        if (c0 + e < wide) *w = fmaf(-m.step, v[e], *w * p.decay);
+      for (int e = 0; e < 32; ++e, w += m.ldp)
+        if (c0 + e < wide) *w = fmaf(-m.step, v[e] * down, *w * p.decay);
     }
     return;
   }
-  // 32 columns at a time through shared memory: eight lanes then hold a row's
+  // through shared memory: eight lanes then hold a row's
+  __syncwarp();
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    __syncwarp();
+  for (int k = 0; k < 8; ++k)
+    st_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16, __float_as_uint(v[4 * k] * down), __float_as_uint(v[4 * k + 1] * down),
+               __float_as_uint(v[4 * k + 2] * down), __float_as_uint(v[4 * k + 3] * down));
+  __syncwarp();
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      st_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16, __float_as_uint(v[32 * h + 4 * k]), __float_as_uint(v[32 * h + 4 * k + 1]),
-                 __float_as_uint(v[32 * h + 4 * k + 2]), __float_as_uint(v[32 * h + 4 * k + 3]));
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int rr = 4 * i + lane / 8, r = 128 * tile + 32 * q + rr, c = c0 + 32 * h + 4 * (lane % 8);
-      const float4 x = ld_shared4(buf + rr * 128 + ((lane % 8) ^ (rr & 7)) * 16);
-      if (r >= side || c >= wide) continue;
-      const float z[4] = {x.x, x.y, x.z, x.w};
-      if (m.out) {
-        T* o = static_cast<T*>(m.out) + r * m.ldo + c;
-        if (m.vec_out && c + 4 <= wide) {
-          if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(o) = x;
-          else *reinterpret_cast<uint2*>(o) = make_uint2(bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3]));
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (c + e < wide) o[e] = from_f<T>(z[e]);
-        }
-      }
-      if (m.param) {
-        float* w = m.param + r * m.ldp + c;
+  for (int i = 0; i < 8; ++i) {
+    const int rr = 4 * i + lane / 8, r = 128 * tile + 32 * q + rr, c = c0 + 4 * (lane % 8);
+    const float4 x = ld_shared4(buf + rr * 128 + ((lane % 8) ^ (rr & 7)) * 16);
+    if (r >= side || c >= wide) continue;
+    const float z[4] = {x.x, x.y, x.z, x.w};
+    if (m.out) {
+      T* o = static_cast<T*>(m.out) + r * m.ldo + c;
+      if (m.vec_out && c + 4 <= wide) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(o) = x;
+        else *reinterpret_cast<uint2*>(o) = make_uint2(bf16_pair(z[0], z[1]), bf16_pair(z[2], z[3]));
+      } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (c + e < wide) w[e] = fmaf(-m.step, z[e], w[e] * p.decay);
+          if (c + e < wide) o[e] = from_f<T>(z[e]);
       }
+    }
+    if (m.param) {
+      float* w = m.param + r * m.ldp + c;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (c + e < wide) w[e] = fmaf(-m.step, z[e], w[e] * p.decay);
     }
   }
   __syncwarp();
@@ -454,7 +463,8 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
     __syncwarp();
   }
   if (PHASE == kApply && p.last) {
-    deliver<T>(p, m, tile, cblk, q, lane, buf, v);
+    deliver<T>(p, m, tile, 64 * cblk, q, lane, buf, v);
+    deliver<T>(p, m, tile, 64 * cblk + 32, q, lane, buf, v + 32);
     return;
   }
   char* dst = p.ws + (PHASE == kGram ? m.a : PHASE == kPoly ? m.c : m.x[p.from ^ 1]) + half_block;
@@ -725,21 +735,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
 // short to fill it: its latency is what counts, and launches of their own cost
 // more (200 x 96 fp32: 143 us).
 constexpr int kSmallRows = 128, kSmallCols = 256, kSmallCtas = 8;
-constexpr int kSmallThreads = 256;
+constexpr int kSmallThreads = 512, kSmallUnits = kSmallRows * kSmallCols / 8 / kSmallThreads;
 constexpr int kSmallX = 8 * kBlock, kSmallA = 4 * kBlock;             // one part of X, of A or C
-constexpr int kSmallSmem = 1024 + 2 * kSmallX + 2 * kSmallA + 192;
+constexpr int kSmallSmem = 1024 + 2 * kSmallX + 2 * kSmallA + 32 + 16 * 16;
 constexpr int kSmallPart = kSmallRows * kSmallRows * 4;                // of X X^T
 static_assert(kSmallSmem <= 232448, "shared memory per CTA");
 
-// 64 elements of a row, starting at a block's row, as one or two parts of fp16.
+// 32 elements of a row of a block, from unit `first` of eight on, as one or two
+// parts of fp16.
 template <int PARTS>
-__device__ __forceinline__ void put_row(uint32_t at, uint32_t part, int row, float (&v)[64]) {
+__device__ __forceinline__ void put_row(uint32_t at, uint32_t part, int row, int first, float (&v)[32]) {
 #pragma unroll
   for (int q = 0; q < PARTS; ++q)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < 4; ++k) {
       const uint4 w = take_half8(v + 8 * k);
-      st_shared4(at + q * part + row * 128 + (k ^ (row & 7)) * 16, w.x, w.y, w.z, w.w);
+      st_shared4(at + q * part + row * 128 + ((first + k) ^ (row & 7)) * 16, w.x, w.y, w.z, w.w);
     }
 }
 
@@ -774,74 +785,89 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
   pdl_wait();
   Waits wait(&g_err);
 
-  // the norm, over all columns
-  {
-    float mid = 0.f, big = 0.f, small = 0.f;
-    const int here = min(cols - col0, kSmallCols);
-    const int n_rows = m.transposed ? here : rows, per_row = ((m.transposed ? rows : here) + 7) / 8;
-    const int first_row = m.transposed ? col0 : 0, first_col = m.transposed ? 0 : col0;
-    for (int e = t; e < n_rows * per_row; e += kSmallThreads) {
-      const int r = e / per_row, c = e - r * per_row;
-      float v[8];
-      update8<T, true>(p, m, first_row + r, first_col + 8 * c, v);
+  // U: units of eight columns of a row, or (transposed, lanes along the columns)
+  // of eight rows of a column; a thread's units stay in its registers until the
+  // norm, over all columns, is known
+  const int units = kSmallUnits / 4 * blocks, line = m.transposed ? 64 * blocks : 8 * blocks;
+  float u[kSmallUnits][8];
+  if (m.vec_in && !m.mom && m.cols % 8 == 0) {
+    Raw8<T> raw[kSmallUnits];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float x = v[k], a = fabsf(x);
-        if (a > 0x1p40f) big = fmaf(x * 0x1p-80f, x * 0x1p-80f, big);
-        else if (a < 0x1p-40f) small = fmaf(x * 0x1p80f, x * 0x1p80f, small);
-        else mid = fmaf(x, x, mid);         // NaN too
-      }
+    for (int i = 0; i < kSmallUnits; ++i) {
+      const int e = t + kSmallThreads * i, hi = e / line, lo = e - hi * line;
+      const int r = m.transposed ? col0 + lo : hi, c = m.transposed ? 8 * hi : col0 + 8 * lo;
+      raw[i].zero();
+      if (i < units && r < m.rows && c < m.cols) raw[i].load(static_cast<const T*>(m.g) + r * m.ldg + c);
     }
-    mid = warp_sum(mid);
-    big = warp_sum(big);
-    small = warp_sum(small);
-    if (lane == 0) box[warp] = make_float4(mid, big, small, 0.f);
-    __syncthreads();
-    if (t == 0) {
-      for (int w = 1; w < 8; ++w) {
-        mid += box[w].x;
-        big += box[w].y;
-        small += box[w].z;
-      }
-      const double s = double(mid) + double(big) * 0x1p160 + double(small) * 0x1p-160;
-      reinterpret_cast<double*>(p.ws + m.a)[me] = s;
-    }
-    if (ctas > 1) cluster_sync_all();
-    if (t == 0) {
-      double s = 0.0;
-      for (int i = 0; i < ctas; ++i) s += __ldcg(reinterpret_cast<const double*>(p.ws + m.a) + i);
-      const float2 f = scale_of(s, p.eps);
-      box[1] = make_float4(f.x, f.y, 0.f, 0.f);
-    }
-    __syncthreads();
-  }
-  const float s1 = box[1].x, s2 = box[1].y;
-  // X: units of eight columns of a row (or of eight rows of a column)
-  if (!m.transposed) {
-    for (int e = t; e < kSmallRows * 8 * blocks; e += kSmallThreads) {
-      const int r = e / (8 * blocks), u = e - r * 8 * blocks;
-      float v[8];
-      update8<T, false>(p, m, r, col0 + 8 * u, v);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = v[k] * s1 * s2;
-      const uint32_t at = sx + (u / 8) * 2 * kBlock + r * 128 + ((u % 8) ^ (r & 7)) * 16;
-      uint4 w = take_half8(v);
-      st_shared4(at, w.x, w.y, w.z, w.w);
-      w = take_half8(v);
-      st_shared4(at + kSmallX, w.x, w.y, w.z, w.w);
-    }
+    for (int i = 0; i < kSmallUnits; ++i) raw[i].get(u[i]);
   } else {
-    for (int e = t; e < 16 * 64 * blocks; e += kSmallThreads) {      // lanes along the columns
-      const int c = e % (64 * blocks), r = e / (64 * blocks) * 8;
-      float v[8];
-      update8<T, false>(p, m, col0 + c, r, v);
+#pragma unroll
+    for (int i = 0; i < kSmallUnits; ++i) {
+      const int e = t + kSmallThreads * i, hi = e / line, lo = e - hi * line;
+      if (i < units) update8<T, true>(p, m, m.transposed ? col0 + lo : hi, m.transposed ? 8 * hi : col0 + 8 * lo, u[i]);
+      else
+#pragma unroll
+        for (int k = 0; k < 8; ++k) u[i][k] = 0.f;
+    }
+  }
+  // the sum of squares in units of the block's largest exponent
+  float top = 0.f, sum2 = 0.f;
+#pragma unroll
+  for (int i = 0; i < kSmallUnits; ++i)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) top = fmaxf(top, fabsf(u[i][k]));
+  top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
+  if (lane == 0) box[warp].x = top;
+  __syncthreads();
+  for (int w = 0; w < kSmallThreads / 32; ++w) top = fmaxf(top, box[w].x);
+  const int exponent = min(max(int(__float_as_uint(top) >> 23), 1), 253);
+  const float down = __uint_as_float(uint32_t(254 - exponent) << 23);
+#pragma unroll
+  for (int i = 0; i < kSmallUnits; ++i)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum2 = fmaf(u[i][k] * down, u[i][k] * down, sum2);
+  sum2 = warp_sum(sum2);
+  if (lane == 0) box[warp].y = sum2;
+  __syncthreads();
+  sum2 = 0.f;
+  for (int w = 0; w < kSmallThreads / 32; ++w) sum2 += box[w].y;
+  int unit = exponent - 127;
+  if (ctas > 1) {
+    float2* all = reinterpret_cast<float2*>(p.ws + m.a);
+    if (t == 0) __stcg(all + me, make_float2(sum2, float(unit)));
+    cluster_sync_all();
+    float2 part[kSmallCtas];
+#pragma unroll
+    for (int i = 0; i < kSmallCtas; ++i) part[i] = i < ctas ? __ldcg(all + i) : make_float2(0.f, -1000.f);
+    float most = part[0].y;
+#pragma unroll
+    for (int i = 1; i < kSmallCtas; ++i) most = fmaxf(most, part[i].y);
+    sum2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < kSmallCtas; ++i) sum2 += scalbnf(part[i].x, 2 * int(part[i].y - most));
+    unit = int(most);
+  }
+  const float2 scale = factors(sqrtf(sum2), unit, p.eps);
+#pragma unroll
+  for (int i = 0; i < kSmallUnits; ++i) {
+    if (i >= units) break;
+    const int e = t + kSmallThreads * i, hi = e / line, lo = e - hi * line;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) u[i][k] = u[i][k] * scale.x * scale.y;
+    if (!m.transposed) {
+      const uint32_t at = sx + (lo / 8) * 2 * kBlock + hi * 128 + ((lo % 8) ^ (hi & 7)) * 16;
+      uint4 w = take_half8(u[i]);
+      st_shared4(at, w.x, w.y, w.z, w.w);
+      w = take_half8(u[i]);
+      st_shared4(at + kSmallX, w.x, w.y, w.z, w.w);
+    } else {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float x = v[k] * s1 * s2;
-        const __half hi = __float2half_rn(x), lo = __float2half_rn(x - __half2float(hi));
-        char* at = smem + (c / 64) * 2 * kBlock + (r + k) * 128 + ((c % 64 / 8) ^ k) * 16 + c % 8 * 2;
-        *reinterpret_cast<__half*>(at) = hi;
-        *reinterpret_cast<__half*>(at + kSmallX) = lo;
+        const __half h = __float2half_rn(u[i][k]), l = __float2half_rn(u[i][k] - __half2float(h));
+        char* at = smem + (lo / 64) * 2 * kBlock + (8 * hi + k) * 128 + ((lo % 64 / 8) ^ k) * 16 + lo % 8 * 2;
+        *reinterpret_cast<__half*>(at) = h;
+        *reinterpret_cast<__half*>(at + kSmallX) = l;
       }
     }
   }
@@ -876,9 +902,21 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
     phase ^= 1;
     tc_fence_after();
   };
-  const int q = warp % 4, half = warp / 4, row = 32 * q + lane;
+  // warp: 32 rows and 32 columns of A and C, and 64 columns of X
+  const int q = warp % 4, quarter = warp / 4, row = 32 * q + lane;
   const uint32_t lanes = tmem + (uint32_t(32 * q) << 16);
-  const uint32_t a_row = sa + half * 2 * kBlock;       // rows of A and C: all of a block column's 128 lie behind one another
+  const uint32_t a_block = sa + quarter / 2 * 2 * kBlock;       // a block column's 128 rows lie behind one another
+  float v[32];
+  auto sum = [&](uint32_t from, int n, uint32_t step_cols) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e) v[e] = 0.f;
+    for (int c = 0; c < n; ++c) {
+      uint32_t r[32];
+      tmem_ld32(from + step_cols * c, r);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) v[e] += __uint_as_float(r[e]);
+    }
+  };
   for (int step = 0; step < steps; ++step) {
     begin();
     if (warp == 0) {
@@ -889,55 +927,40 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
       commit_to(bar);
     }
     finished();
-    float v[64];
-#pragma unroll
-    for (int e = 0; e < 64; ++e) v[e] = 0.f;
-    auto sum = [&](uint32_t from, int n, uint32_t step_cols) {
-      for (int c = 0; c < n; ++c)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t r[32];
-          tmem_ld32(from + step_cols * c + 32 * h, r);
-#pragma unroll
-          for (int e = 0; e < 32; ++e) v[32 * h + e] += __uint_as_float(r[e]);
-        }
-    };
-    sum(lanes + 64 * half, blocks, 128);
+    sum(lanes + 32 * quarter, blocks, 128);
     if (ctas > 1) {
-      // [step parity][CTA][16][thread] of four
+      // [step parity][CTA][8][thread] of four
       float4* parts = reinterpret_cast<float4*>(p.ws + m.x[step & 1]);
 #pragma unroll
-      for (int k = 0; k < 16; ++k)
-        __stcg(parts + (me * 16 + k) * kSmallThreads + t, make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
+      for (int k = 0; k < 8; ++k)
+        __stcg(parts + (me * 8 + k) * kSmallThreads + t, make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
       cluster_sync_all();
 #pragma unroll
-      for (int e = 0; e < 64; ++e) v[e] = 0.f;
+      for (int e = 0; e < 32; ++e) v[e] = 0.f;
       for (int i = 0; i < ctas; ++i)
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-          const float4 z = __ldcg(parts + (i * 16 + k) * kSmallThreads + t);
+        for (int k = 0; k < 8; ++k) {
+          const float4 z = __ldcg(parts + (i * 8 + k) * kSmallThreads + t);
           v[4 * k] += z.x;
           v[4 * k + 1] += z.y;
           v[4 * k + 2] += z.z;
           v[4 * k + 3] += z.w;
         }
     }
-    float A[64];
+    float A[32];
 #pragma unroll
-    for (int e = 0; e < 64; ++e) A[e] = v[e] *= kUpA / (kUpX * kUpX);
-    put_row<PARTS>(a_row, kSmallA, row, v);
+    for (int e = 0; e < 32; ++e) A[e] = v[e] *= kUpA / (kUpX * kUpX);
+    put_row<PARTS>(a_block, kSmallA, row, quarter % 2 * 4, v);
     begin();
     if (warp == 0) {
       for (int c = 0; c < 2; ++c) product(tmem + 128 * c, sa + c * 2 * kBlock, kSmallA, sa + c * 2 * kBlock, kSmallA, 128, false);
       commit_to(bar);
     }
     finished();
+    sum(lanes + 32 * quarter, 2, 128);
 #pragma unroll
-    for (int e = 0; e < 64; ++e) v[e] = 0.f;
-    sum(lanes + 64 * half, 2, 128);
-#pragma unroll
-    for (int e = 0; e < 64; ++e) v[e] = fmaf(p.cc / kUpA, v[e], p.cb * A[e]);
-    put_row<PARTS>(a_row, kSmallA, row, v);
+    for (int e = 0; e < 32; ++e) v[e] = fmaf(p.cc / kUpA, v[e], p.cb * A[e]);
+    put_row<PARTS>(a_block, kSmallA, row, quarter % 2 * 4, v);
     begin();
     if (warp == 0) {
       for (int c = 0; c < 2; ++c)
@@ -945,26 +968,27 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
       commit_to(bar);
     }
     finished();
-    for (int b = half; b < blocks; b += 2) {
+    if (quarter < blocks) {
+      const uint32_t x_block = sx + quarter * 2 * kBlock;
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        sum(lanes + 64 * quarter + 32 * h, 2, 256);
 #pragma unroll
-      for (int e = 0; e < 64; ++e) v[e] = 0.f;
-      sum(lanes + 64 * b, 2, 256);
-      const uint32_t x_row = sx + b * 2 * kBlock + row * 128;
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t at = x_block + row * 128 + ((4 * h + k) ^ (row & 7)) * 16;
+          const float4 hi = ld_shared4(at), lo = ld_shared4(at + kSmallX);
+          const float zh[4] = {hi.x, hi.y, hi.z, hi.w}, zl[4] = {lo.x, lo.y, lo.z, lo.w};
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int off = (k ^ (row & 7)) * 16;
-        const float4 hi = ld_shared4(x_row + off), lo = ld_shared4(x_row + kSmallX + off);
-        const float zh[4] = {hi.x, hi.y, hi.z, hi.w}, zl[4] = {lo.x, lo.y, lo.z, lo.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 fh = of_pair(__float_as_uint(zh[e])), fl = of_pair(__float_as_uint(zl[e]));
-          float &x = v[8 * k + 2 * e], &y = v[8 * k + 2 * e + 1];
-          x = fmaf(p.ca, fh.x, fmaf(p.ca, fl.x, x * (1.f / kUpA)));
-          y = fmaf(p.ca, fh.y, fmaf(p.ca, fl.y, y * (1.f / kUpA)));
+          for (int e = 0; e < 4; ++e) {
+            const float2 fh = of_pair(__float_as_uint(zh[e])), fl = of_pair(__float_as_uint(zl[e]));
+            float &x = v[8 * k + 2 * e], &y = v[8 * k + 2 * e + 1];
+            x = fmaf(p.ca, fh.x, fmaf(p.ca, fl.x, x * (1.f / kUpA)));
+            y = fmaf(p.ca, fh.y, fmaf(p.ca, fl.y, y * (1.f / kUpA)));
+          }
         }
+        if (step + 1 < steps) put_row<2>(x_block, kSmallX, row, 4 * h, v);
+        else deliver<T>(p, m, 0, col0 + 64 * quarter + 32 * h, q, lane, sa + warp * 4096, v);
       }
-      if (step + 1 < steps) put_row<2>(sx + b * 2 * kBlock, kSmallX, row, v);
-      else deliver<T>(p, m, 0, col0 / 64 + b, q, lane, sa + warp * 4096, v);
     }
   }
   tc_fence_before();
@@ -997,7 +1021,7 @@ int64_t item_bytes(const fo_matrix_update& m, int parts) {
   if (m.rows == 0 || m.cols == 0) return 0;
   if (is_small(m)) return 2 * kSmallCtas * kSmallPart + 256;
   const int64_t r = (m.rows + 127) / 128, c = (m.cols + 127) / 128, mt = r < c ? r : c, nt = r < c ? c : r;
-  return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + (kMaxSums + 1) * 8;
+  return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + kMaxSums * 16 + 16;
 }
 
 template <int PARTS, int BN, int PHASE, typename T>
@@ -1072,7 +1096,7 @@ cudaError_t orthogonalize(OrthoParams& p, int steps, cudaStream_t st) {
   }
   p.start[p.count] = int(units);
   if ((e = launch_k(ortho_sums_k<T>, dim3(unsigned(units)), dim3(256), 0, st, p)) != cudaSuccess) return e;
-  if ((e = launch_k(ortho_scale_k, dim3(unsigned(p.count)), dim3(128), 0, st, p)) != cudaSuccess) return e;
+  if ((e = launch_k(ortho_scale_k, dim3(unsigned(p.count)), dim3(256), 0, st, p)) != cudaSuccess) return e;
   units = 0;
   for (int i = 0; i < p.count; ++i) {
     p.start[i] = int(units);
@@ -1147,7 +1171,7 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
     p.mu = float(momentum);
     p.decay = float(decay);
     p.nesterov = nesterov != 0;
-    p.eps = eps;
+    p.eps = float(eps);
     int64_t at = 0;
     auto take = [&at](int64_t bytes) {
       const int64_t here = at;
@@ -1189,7 +1213,7 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
       it.step = m.step;
     }
     if (p.count == 0) continue;
-    p.sums = reinterpret_cast<double*>(p.ws + at);
+    p.sums = reinterpret_cast<float4*>(p.ws + at);
     p.scale = reinterpret_cast<float2*>(p.sums + p.count * kMaxSums);
     const cudaError_t e = small ? (dtype == FO_DTYPE_F32 ? orthogonalize_small<float>(p, steps, st) : orthogonalize_small<bf16>(p, steps, st))
                           : dtype == FO_DTYPE_F32 ? orthogonalize<float>(p, steps, st) : orthogonalize<bf16>(p, steps, st);
