@@ -62,7 +62,8 @@ def grad_agrees(got, dout, ids, V, scale, before=None):
 
 @pytest.mark.parametrize("table,dtype", TYPES)
 @pytest.mark.parametrize("T,V,D", [(1, 1, 1), (1, 50, 8), (2, 3, 7), (31, 10, 64), (32, 512, 256), (33, 511, 257), (64, 513, 512),
-                                   (1000, 7, 40), (4096, 30522, 512), (5000, 1000, 777), (20000, 262144, 24), (300, 100, 2056)])
+                                   (1000, 7, 40), (4096, 30522, 512), (5000, 1000, 777), (20000, 262144, 24), (300, 100, 2056),
+                                   (16384, 300, 16), (16385, 300, 16), (5000, 1 << 20, 8), (16384, 40000, 8)])
 def test_values_and_gradients(table, dtype, T, V, D):
     for k, id_type in enumerate((torch.int32, torch.int64)):
         ids, w, dout = make(T, V, D, table, dtype, seed=k, id_type=id_type)
