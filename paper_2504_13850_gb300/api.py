@@ -10,6 +10,7 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import os
+import struct
 from array import array
 
 import numpy as np
@@ -686,15 +687,58 @@ def dropout_grad(dy, p, seed, call, out=None, stream=None):
     return dropout_add(dy, None, p, seed, call, out=out, stream=stream)
 
 
-def _dtype_of(torch, t, name):
-    if t.dtype == torch.bfloat16:
-        return DTYPE_BF16
-    if t.dtype == torch.float32:
-        return DTYPE_F32
-    raise ValueError(f"{name}: bf16 or fp32")
+# The binding of the operators below: what a call needs beyond the library's own
+# work costs more than many a kernel, so checks are few and nothing is entered
+# (device, stream) that is current already.
+
+_codes = {}                     # torch dtype -> DTYPE_*
+_raw_stream = None
 
 
-def _dense_rows(torch, g):
+def _setup(torch):
+    global _raw_stream
+    _codes[torch.float32] = DTYPE_F32
+    _codes[torch.bfloat16] = DTYPE_BF16
+    # the handle of a device's current stream, without an object around it
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+def _code(t, name):
+    try:
+        return _codes[t.dtype]
+    except KeyError:
+        raise ValueError(f"{name}: bf16 or fp32") from None
+
+
+def _run(index, stream, body, *args):
+    """body(torch, stream handle, *args) with device `index` current and what it
+    allocates belonging to the stream."""
+    import torch
+    if not _codes:
+        _setup(torch)
+    if index < 0:
+        raise ValueError("device tensors are wanted")
+    if stream is None and index == torch.cuda.current_device():
+        return body(torch, _raw_stream(index), *args)
+    with torch.cuda.device(index):
+        if stream is None:
+            return body(torch, torch.cuda.current_stream(index).cuda_stream, *args)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=torch.device("cuda", index))):
+            return body(torch, stream, *args)
+
+
+def _like(t, shape, dtype, index, name):
+    """(pointer, row stride) of `t` seen as a matrix [rows, last dimension]."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != index:
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}; wanted {tuple(shape)} {dtype} on the same device as the others")
+    if t.is_contiguous():
+        return t.data_ptr(), shape[-1]
+    if len(shape) == 2 and t.stride(1) == 1:
+        return t.data_ptr(), t.stride(0)
+    raise ValueError(f"{name}: contiguous, or a matrix with innermost stride 1")
+
+
+def _dense(torch, g):
     """`g`, or a contiguous copy where its strides would refuse it: autograd
     hands over gradients broadcast by a sum or a mean."""
     if g.is_contiguous() or g.dim() == 2 and g.stride(1) == 1:
@@ -703,16 +747,15 @@ def _dense_rows(torch, g):
 
 
 def _ids(torch, ids):
-    if not ids.is_cuda or ids.dtype not in (torch.int32, torch.int64) or not ids.is_contiguous():
-        raise ValueError("ids: a contiguous int32 or int64 device tensor")
-    return ids.data_ptr(), 32 if ids.dtype == torch.int32 else 64
-
-
-def _of_tokens(t, ids, width, dtype, name):
-    """(pointer, row stride) of `t`, [*ids.shape, width] of `dtype`."""
-    if t.shape[:-1] != ids.shape or t.shape[-1] != width or t.dtype != dtype or t.get_device() != ids.get_device():
-        raise ValueError(f"{name}: {tuple(ids.shape)} x {width} {dtype} on the ids' device is wanted")
-    return _matrix(t, t, name)
+    if ids.dtype == torch.int32:
+        bits = 32
+    elif ids.dtype == torch.int64:
+        bits = 64
+    else:
+        raise ValueError("ids: int32 or int64")
+    if not ids.is_contiguous():
+        raise ValueError("ids: contiguous")
+    return ids.data_ptr(), bits
 
 
 def embedding(ids, table, scale=1.0, dtype=None, out=None, stream=None):
@@ -720,95 +763,57 @@ def embedding(ids, table, scale=1.0, dtype=None, out=None, stream=None):
     contiguous table [vocab, width]; ids outside of the table (padding) give
     zeros.  `dtype` of the output defaults to the table's (bf16 of an fp32 table
     is the other choice).  Runs on `stream`, by default torch's current stream."""
-    import torch
-    if table.dim() != 2 or not table.is_contiguous() or table.get_device() != ids.get_device():
+    return _run(ids.get_device(), stream, _embedding, ids, table, scale, dtype, out)
+
+
+def _embedding(torch, st, ids, table, scale, dtype, out):
+    index = ids.get_device()
+    if table.dim() != 2 or not table.is_contiguous() or table.get_device() != index:
         raise ValueError("table: a contiguous matrix [vocab, width] on the ids' device")
     ip, bits = _ids(torch, ids)
     vocab, width = table.shape
-    dtype = table.dtype if dtype is None else dtype
-
-    def make():
-        return torch.empty((*ids.shape, width), dtype=dtype, device=ids.device)
-
-    with _device_of(torch, ids):
-        if out is None:
-            y, st = _on_stream(torch, ids, stream, make)
-            yp, ys = y.data_ptr(), width
-        else:
-            y, st = out, torch.cuda.current_stream(ids.get_device()).cuda_stream if stream is None else stream
-            yp, ys = _of_tokens(y, ids, width, dtype, "out")
-        _check(lib().fo_embedding(ip, bits, ids.numel(), table.data_ptr(), _dtype_of(torch, table, "table"), vocab, width,
-                                  scale, yp, ys, _dtype_of(torch, y, "out"), st), "embedding")
-    return y
+    if dtype is None:
+        dtype = table.dtype
+    shape = (*ids.shape, width)
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=ids.device)
+        yp, ys = out.data_ptr(), width
+    else:
+        yp, ys = _like(out, shape, dtype, index, "out")
+    _check(lib().fo_embedding(ip, bits, ids.numel(), table.data_ptr(), _code(table, "table"), vocab, width, scale, yp, ys,
+                              _code(out, "out"), st), "embedding")
+    return out
 
 
 def embedding_grad(dout, ids, vocab, scale=1.0, dtype=None, out=None, accumulate=False, stream=None):
     """fo_embedding_grad: the gradient [vocab, width] of embedding's table, of
     `dtype` (default: dout's), from dout = [*ids.shape, width].  `out` may give
     the tensor to write, or with `accumulate` to add to."""
-    import torch
+    return _run(ids.get_device(), stream, _embedding_grad, dout, ids, vocab, scale, dtype, out, accumulate)
+
+
+def _embedding_grad(torch, st, dout, ids, vocab, scale, dtype, out, accumulate):
     ip, bits = _ids(torch, ids)
-    if accumulate and out is None:
-        raise ValueError("accumulate: out holds what is added to")
-    width = dout.shape[-1]
-    dtype = out.dtype if out is not None else dout.dtype if dtype is None else dtype
-    L_ = lib()
-    need = L_.fo_embedding_workspace(ids.numel(), width)
-
-    def make():
-        d = torch.empty((vocab, width), dtype=dtype, device=ids.device) if out is None else out
-        return _dense_rows(torch, dout), d, torch.empty(need, dtype=torch.uint8, device=ids.device) if need > 0 else None
-
-    with _device_of(torch, ids):
-        (g, d, ws), st = _on_stream(torch, ids, stream, make)
-        gp, gs = _of_tokens(g, ids, width, g.dtype, "dout")
-        if out is not None and (d.shape != (vocab, width) or not d.is_contiguous() or d.get_device() != ids.get_device()):
-            raise ValueError("out: a contiguous matrix [vocab, width] on the ids' device")
-        _check(L_.fo_embedding_grad(gp, gs, _dtype_of(torch, g, "dout"), ip, bits, ids.numel(), d.data_ptr(),
-                                    _dtype_of(torch, d, "out"), vocab, width, scale, 1 if accumulate else 0,
-                                    None if ws is None else ws.data_ptr(), max(need, 0), st), "embedding_grad")
-    return d
+    tokens, width, device, L_ = ids.numel(), dout.shape[-1], ids.device, lib()
+    dout = _dense(torch, dout)
+    gp, gs = _like(dout, (*ids.shape, width), dout.dtype, ids.get_device(), "dout")
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate: out holds what is added to")
+        out = torch.empty((vocab, width), dtype=dout.dtype if dtype is None else dtype, device=device)
+    elif out.shape != (vocab, width) or not out.is_contiguous() or out.get_device() != ids.get_device():
+        raise ValueError("out: a contiguous matrix [vocab, width] on the ids' device")
+    need = L_.fo_embedding_workspace(tokens, width)
+    ws = torch.empty((max(need, 0),), dtype=torch.uint8, device=device)
+    _check(L_.fo_embedding_grad(gp, gs, _code(dout, "dout"), ip, bits, tokens, out.data_ptr(), _code(out, "out"), vocab, width,
+                                scale, 1 if accumulate else 0, ws.data_ptr(), need, st), "embedding_grad")
+    return out
 
 
-def _norm_weight(torch, x, weight):
-    if weight.shape != x.shape[-1:] or weight.get_device() != x.get_device() or not weight.is_contiguous():
+def _norm_weight(x, weight, index):
+    if weight.shape != x.shape[-1:] or weight.get_device() != index or not weight.is_contiguous():
         raise ValueError("weight: a contiguous vector as long as x's last dimension, on x's device")
-    return weight.data_ptr(), _dtype_of(torch, weight, "weight")
-
-
-def _norm(x, residual, weight, eps, out, sum_out, eight, with_y, stream):
-    import torch
-    dtype = _dtype_of(torch, x, "x")
-    if not x.is_cuda or x.dim() < 1:
-        raise ValueError("x: a device tensor of one dimension at least")
-    shape, device = x.shape, x.device
-    cols = shape[-1]
-    rows = x.numel() // cols if cols else 0
-
-    def make():
-        q = scales = y = r = None
-        s = x
-        if residual is not None:
-            s = torch.empty(shape, dtype=x.dtype, device=device) if sum_out is None else sum_out
-        if with_y:
-            y = torch.empty(shape, dtype=x.dtype, device=device) if out is None else out
-            r = torch.empty(shape[:-1], dtype=torch.float32, device=device)
-        if eight:
-            q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device)
-            scales = torch.empty((*shape[:-1], (cols + 31) // 32), dtype=torch.uint8, device=device)
-        return q, scales, s, y, r
-
-    with _device_of(torch, x):
-        (q, scales, s, y, r), st = _on_stream(torch, x, stream, make)
-        xp, xs = _matrix(x, x, "x")
-        rp, rs = (None, 0) if residual is None else _matrix(residual, x, "residual")
-        sp, ss = (None, 0) if residual is None else _matrix(s, x, "sum_out")
-        yp, ys = (None, 0) if y is None else _matrix(y, x, "out")
-        wp, wt = _norm_weight(torch, x, weight)
-        _check(lib().fo_rms_norm(xp, xs, rp, rs, wp, wt, sp, ss, yp, ys, None if q is None else q.data_ptr(),
-                                 None if q is None else scales.data_ptr(), None if r is None else r.data_ptr(), dtype, rows,
-                                 cols, eps, st), "rms_norm")
-    return q, scales, s, y, r
+    return weight.data_ptr(), _code(weight, "weight")
 
 
 def rms_norm(x, residual, weight, eps=1e-6, out=None, sum_out=None, stream=None):
@@ -817,121 +822,157 @@ def rms_norm(x, residual, weight, eps=1e-6, out=None, sum_out=None, stream=None)
     dimension of a bf16 or fp32 device tensor.  weight: x's type or fp32.  `out`
     and `sum_out` may give y and s.  Runs on `stream`, by default torch's
     current stream."""
-    s, y, r = _norm(x, residual, weight, eps, out, sum_out, False, True, stream)[2:]
-    return y, s, r
+    return _run(x.get_device(), stream, _rms_norm, x, residual, weight, eps, out, sum_out, False, True)[2:]
 
 
 def rms_norm_8bit(x, residual, weight, eps=1e-6, with_y=False, stream=None):
     """The norm as 8-bit floats: (q, scales, s), q float8_e4m3fn like x, scales
     uint8 [..., ceil(cols / 32)] (fo_rms_norm has the format), or with `with_y`
-    (q, scales, s, y, r) from the same pass."""
-    q, scales, s, y, r = _norm(x, residual, weight, eps, None, None, True, with_y, stream)
-    return (q, scales, s, y, r) if with_y else (q, scales, s)
+    (q, scales, y, s, r) from the same pass."""
+    got = _run(x.get_device(), stream, _rms_norm, x, residual, weight, eps, None, None, True, with_y)
+    return got if with_y else (got[0], got[1], got[3])
+
+
+def _rms_norm(torch, st, x, residual, weight, eps, out, sum_out, eight, with_y):
+    dtype, index, shape, device, t = _code(x, "x"), x.get_device(), x.shape, x.device, x.dtype
+    if not shape:
+        raise ValueError("x: one dimension at least")
+    cols = shape[-1]
+    wp, wt = _norm_weight(x, weight, index)
+    xp, xs = _like(x, shape, t, index, "x")
+    s, rp, rs, sp, ss = x, None, 0, None, 0
+    if residual is not None:
+        rp, rs = _like(residual, shape, t, index, "residual")
+        if sum_out is None:
+            s = torch.empty(shape, dtype=t, device=device)
+            sp, ss = s.data_ptr(), cols
+        else:
+            s = sum_out
+            sp, ss = _like(s, shape, t, index, "sum_out")
+    q = scales = r = qp = cp = yp = op = None
+    ys = 0
+    if with_y:
+        if out is None:
+            out = torch.empty(shape, dtype=t, device=device)
+            yp, ys = out.data_ptr(), cols
+        else:
+            yp, ys = _like(out, shape, t, index, "out")
+        r = torch.empty(shape[:-1], dtype=torch.float32, device=device)
+        op = r.data_ptr()
+    if eight:
+        q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device)
+        scales = torch.empty((*shape[:-1], (cols + 31) // 32), dtype=torch.uint8, device=device)
+        qp, cp = q.data_ptr(), scales.data_ptr()
+    _check(lib().fo_rms_norm(xp, xs, rp, rs, wp, wt, sp, ss, yp, ys, qp, cp, op, dtype, x.numel() // cols if cols else 0, cols,
+                             eps, st), "rms_norm")
+    return q, scales, out, s, r
 
 
 def rms_norm_grad(dy, ds, s, weight, r, out=None, stream=None):
     """fo_rms_norm_grad: (dx, dweight) of rms_norm, from the gradients dy of y and
     ds of s (None: none), and the call's s, weight and r.  dx is also the
     residual's gradient."""
-    import torch
-    L_ = lib()
-    dtype = _dtype_of(torch, s, "s")
-    shape, device = s.shape, s.device
+    return _run(s.get_device(), stream, _rms_norm_grad, dy, ds, s, weight, r, out)
+
+
+def _rms_norm_grad(torch, st, dy, ds, s, weight, r, out):
+    dtype, index, shape, device, t, L_ = _code(s, "s"), s.get_device(), s.shape, s.device, s.dtype, lib()
+    if not shape:
+        raise ValueError("s: one dimension at least")
     cols = shape[-1]
     rows = s.numel() // cols if cols else 0
+    wp, wt = _norm_weight(s, weight, index)
+    dy = _dense(torch, dy)
+    gp, gs = _like(dy, shape, t, index, "dy")
+    hp, hs = None, 0
+    if ds is not None:
+        ds = _dense(torch, ds)
+        hp, hs = _like(ds, shape, t, index, "ds")
+    sp, ss = _like(s, shape, t, index, "s")
+    rp = _small(r, shape[:-1], torch.float32, s, "r")
+    if out is None:
+        out = torch.empty(shape, dtype=t, device=device)
+        xp, xs = out.data_ptr(), cols
+    else:
+        xp, xs = _like(out, shape, t, index, "out")
+    dw = torch.empty(weight.shape, dtype=weight.dtype, device=device)
     need = L_.fo_rms_norm_workspace(rows, cols)
-
-    def make():
-        return (_dense_rows(torch, dy), None if ds is None else _dense_rows(torch, ds),
-                torch.empty(shape, dtype=s.dtype, device=device) if out is None else out,
-                torch.empty(weight.shape, dtype=weight.dtype, device=device),
-                torch.empty(need, dtype=torch.uint8, device=device) if need > 0 else None)
-
-    with _device_of(torch, s):
-        (g, h, dx, dw, ws), st = _on_stream(torch, s, stream, make)
-        gp, gs = _matrix(g, s, "dy")
-        hp, hs = (None, 0) if h is None else _matrix(h, s, "ds")
-        sp, ss = _matrix(s, s, "s")
-        wp, wt = _norm_weight(torch, s, weight)
-        xp, xs = _matrix(dx, s, "out")
-        _check(L_.fo_rms_norm_grad(gp, gs, hp, hs, sp, ss, wp, wt, _small(r, shape[:-1], torch.float32, s, "r"), xp, xs,
-                                   dw.data_ptr(), dtype, rows, cols, None if ws is None else ws.data_ptr(), max(need, 0), st),
-               "rms_norm_grad")
-    return dx, dw
+    ws = torch.empty((max(need, 0),), dtype=torch.uint8, device=device)
+    _check(L_.fo_rms_norm_grad(gp, gs, hp, hs, sp, ss, wp, wt, rp, xp, xs, dw.data_ptr(), dtype, rows, cols, ws.data_ptr(), need,
+                               st), "rms_norm_grad")
+    return out, dw
 
 
 def decode_8bit(q, scales, dtype=None, out=None, stream=None):
     """fo_decode_8bit: the values of rms_norm_8bit's (q, scales), in `dtype`
     (default: bf16)."""
-    import torch
-    shape, device = q.shape, q.device
-    if not q.is_cuda or q.dtype != torch.float8_e4m3fn or not q.is_contiguous() or q.dim() < 1:
-        raise ValueError("q: a contiguous float8_e4m3fn device tensor")
+    return _run(q.get_device(), stream, _decode_8bit, q, scales, dtype, out)
+
+
+def _decode_8bit(torch, st, q, scales, dtype, out):
+    shape, index = q.shape, q.get_device()
+    if q.dtype != torch.float8_e4m3fn or not q.is_contiguous() or not shape:
+        raise ValueError("q: a contiguous float8_e4m3fn tensor of one dimension at least")
     cols = shape[-1]
     sp = _small(scales, (*shape[:-1], (cols + 31) // 32), torch.uint8, q, "scales")
+    if out is None:
+        out = torch.empty(shape, dtype=torch.bfloat16 if dtype is None else dtype, device=q.device)
+        yp, ys = out.data_ptr(), cols
+    else:
+        yp, ys = _like(out, shape, out.dtype, index, "out")
+    _check(lib().fo_decode_8bit(q.data_ptr(), sp, yp, ys, _code(out, "out"), q.numel() // cols if cols else 0, cols, st),
+           "decode_8bit")
+    return out
 
-    def make():
-        return torch.empty(shape, dtype=torch.bfloat16 if dtype is None else dtype, device=device) if out is None else out
-
-    with _device_of(torch, q):
-        y, st = _on_stream(torch, q, stream, make)
-        if y.shape != shape or y.get_device() != q.get_device():
-            raise ValueError("out: q's shape and device are wanted")
-        yp, ys = _matrix(y, y, "out")
-        _check(lib().fo_decode_8bit(q.data_ptr(), sp, yp, ys, _dtype_of(torch, y, "out"), q.numel() // cols if cols else 0, cols,
-                                    st), "decode_8bit")
-    return y
 
 
 # Coefficients that bring singular values into 0.7 .. 1.2 in five steps.
 QUINTIC = (3.4445, -4.7750, 2.0315)
 
-
-def _matrices(torch, tensors, like, dtype, name):
-    """(pointer, row stride) of each matrix, shaped and placed like `like`'s."""
-    flat = []
-    for t, g in zip(tensors, like, strict=True):
-        if t.dim() != 2 or t.shape != g.shape or t.dtype != dtype or t.get_device() != like[0].get_device() or not t.is_cuda:
-            raise ValueError(f"{name}: {dtype} matrices with the gradients' shapes, on one device")
-        flat.append(_matrix(t, t, name))
-    return flat
+_matrix_update_words = C.sizeof(fo_matrix_update) // 8
 
 
-def _orthogonalize(torch, grads, momenta, outs, params, steps_of, steps, coefficients, eps, mu, nesterov, decay, stream):
-    """fo_orthogonalize on lists of tensors (each of the last three may be None);
-    returns outs, made here where it is True."""
-    L_ = lib()
-    n, first = len(grads), grads[0]
-    dtype = _dtype_of(torch, first, "updates")
-    items = (fo_matrix_update * n)()
-
-    def make():
-        dense = [_dense_rows(torch, g) for g in grads]
-        made = [torch.empty(g.shape, dtype=g.dtype, device=g.device) for g in grads] if outs is True else outs
-        for it, g in zip(items, dense):
-            if g.dim() != 2:
-                raise ValueError("updates: matrices")
-            it.rows, it.cols = g.shape
-        need = L_.fo_orthogonalize_workspace(items, n, dtype)
-        if need < 0:
-            _check(ERR_ARG, "orthogonalize")
-        return dense, made, torch.empty(need, dtype=torch.uint8, device=first.device) if need > 0 else None, need
-
-    with _device_of(torch, first):
-        (dense, outs, ws, need), st = _on_stream(torch, first, stream, make)
-        for name, tensors, t in (("grad", dense, first.dtype), ("momentum", momenta, torch.float32), ("out", outs, first.dtype),
-                                 ("param", params, torch.float32)):
-            if tensors is None:
-                continue
-            for it, (p, ld) in zip(items, _matrices(torch, tensors, dense, t, name)):
-                setattr(it, name, p)
-                setattr(it, name + "_stride", ld)
-        if steps_of is not None:
-            for it, v in zip(items, steps_of, strict=True):
-                it.step = v
-        _check(L_.fo_orthogonalize(items, n, dtype, steps, (C.c_double * 3)(*coefficients), eps, mu, 1 if nesterov else 0, decay,
-                                   None if ws is None else ws.data_ptr(), need, st), "orthogonalize")
-    return outs
+def _orthogonalize(torch, st, grads, momenta, outs, params, steps_of, steps, coefficients, eps, mu, nesterov, decay):
+    """fo_orthogonalize on lists of tensors (momenta, outs and params may be
+    None, outs True to make them); returns outs."""
+    L_, n, first = lib(), len(grads), grads[0]
+    dtype, t, index, device, f32 = _code(first, "updates"), first.dtype, first.get_device(), first.device, torch.float32
+    for name, other in (("momenta", momenta), ("out", outs), ("params", params), ("scales", steps_of)):
+        if other is not None and other is not True and len(other) != n:
+            raise ValueError(f"{name}: as many as updates")
+    make, made = outs is True, []
+    flat = array("q", bytes(8 * _matrix_update_words * n))
+    at, keep = 0, []
+    for i, g in enumerate(grads):
+        if g.dim() != 2:
+            raise ValueError("updates: matrices")
+        if not g.is_contiguous():
+            g = _dense(torch, g)
+            keep.append(g)
+        shape = g.shape
+        gp, gs = _like(g, shape, t, index, "updates")
+        flat[at], flat[at + 1], flat[at + 2], flat[at + 6] = shape[0], shape[1], gp, gs
+        if momenta is not None:
+            flat[at + 3], flat[at + 7] = _like(momenta[i], shape, f32, index, "momenta")
+        if make:
+            o = torch.empty(shape, dtype=t, device=device)
+            made.append(o)
+            flat[at + 4], flat[at + 8] = o.data_ptr(), shape[1]
+        elif outs is not None:
+            flat[at + 4], flat[at + 8] = _like(outs[i], shape, t, index, "out")
+        if params is not None:
+            flat[at + 5], flat[at + 9] = _like(params[i], shape, f32, index, "params")
+            flat[at + 10] = struct.unpack("q", struct.pack("ff", steps_of[i], 0.0))[0]
+        at += _matrix_update_words
+    items = flat.buffer_info()[0]
+    need = L_.fo_orthogonalize_workspace(items, n, dtype)
+    if need < 0:
+        _check(ERR_ARG, "orthogonalize")
+    ws = torch.empty((need,), dtype=torch.uint8, device=device)
+    three = array("d", coefficients)
+    _check(L_.fo_orthogonalize(items, n, dtype, steps, three.buffer_info()[0], eps, mu, 1 if nesterov else 0, decay,
+                               ws.data_ptr(), need, st), "orthogonalize")
+    return made if make else outs
 
 
 def orthogonalize(updates, steps=5, coefficients=QUINTIC, eps=1e-7, out=None, stream=None):
@@ -940,13 +981,14 @@ def orthogonalize(updates, steps=5, coefficients=QUINTIC, eps=1e-7, out=None, st
     of X <- c0 X + (c1 A + c2 A A) X with A = X X^T.  One call for a list shares
     its launches.  `out` may give the tensors to write (the updates too).  Runs
     on `stream`, by default torch's current stream."""
-    import torch
-    if isinstance(updates, torch.Tensor):
+    if hasattr(updates, "data_ptr"):
         return orthogonalize([updates], steps, coefficients, eps, None if out is None else [out], stream)[0]
     if len(updates) == 0:
         return []
-    return _orthogonalize(torch, updates, None, True if out is None else out, None, None, steps, coefficients, eps, 0.0, False, 1.0,
-                          stream)
+    if len(coefficients) != 3:
+        raise ValueError("coefficients: three")
+    return _run(updates[0].get_device(), stream, _orthogonalize, updates, None, True if out is None else out, None, None, steps,
+                coefficients, eps, 0.0, False, 1.0)
 
 
 def muon_step(params, grads, momenta, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scales=None, steps=5,
@@ -955,13 +997,16 @@ def muon_step(params, grads, momenta, lr, momentum=0.95, nesterov=True, weight_d
     place: m <- momentum m + g; X = orthogonalize(g + momentum m, or m without
     nesterov); p <- (1 - lr weight_decay) p - lr scale X.  params and momenta are
     fp32, grads fp32 or bf16; scales default to sqrt(max(1, rows / cols))."""
-    import torch
+    if not len(params) == len(grads) == len(momenta):
+        raise ValueError("params, grads and momenta: as many of each")
     if len(params) == 0:
         return
+    if len(coefficients) != 3:
+        raise ValueError("coefficients: three")
     if scales is None:
         scales = [max(1.0, p.shape[0] / max(1, p.shape[1])) ** 0.5 for p in params]
-    _orthogonalize(torch, grads, momenta, None, params, [lr * s for s in scales], steps, coefficients, eps, momentum, nesterov,
-                   1.0 - lr * weight_decay, stream)
+    _run(grads[0].get_device(), stream, _orthogonalize, grads, momenta, None, params, [lr * s for s in scales], steps,
+         coefficients, eps, momentum, nesterov, 1.0 - lr * weight_decay)
 
 
 def orthogonalize_error(stream=None, device=None):

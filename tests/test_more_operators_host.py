@@ -96,10 +96,18 @@ def test_workspaces():
 
 
 class Stand(Machine):
+    def __init__(self, monkeypatch):
+        super().__init__(monkeypatch)
+        api._setup(torch)
+        monkeypatch.setattr(api, "_raw_stream", lambda index: 0)
+
     def fo_embedding_workspace(self, tokens, width):
         return 256
 
     def fo_rms_norm_workspace(self, rows, cols):
+        return 256
+
+    def fo_orthogonalize_workspace(self, items, count, dtype):
         return 256
 
 
@@ -125,6 +133,7 @@ CALLS = {
     "fo_rms_norm": lambda i, **kw: api.rms_norm(matrix(i), matrix(i), vector(i), **kw),
     "fo_rms_norm_grad": lambda i, **kw: api.rms_norm_grad(matrix(i), matrix(i), matrix(i), vector(i), Tensor((2, 16), torch.float32, i), **kw),
     "fo_decode_8bit": lambda i, **kw: api.decode_8bit(*codes(i), **kw),
+    "fo_orthogonalize": lambda i, **kw: api.orthogonalize([Tensor((9, 5), torch.float32, i)] * 2, **kw),
 }
 
 
@@ -143,7 +152,73 @@ def test_mixed_devices_are_refused(monkeypatch):
     for call in (lambda: api.embedding(ids(0), Tensor((10, 64), torch.float32, 1)), lambda: api.embedding_grad(matrix(1), ids(0), 10),
                  lambda: api.rms_norm(matrix(0), matrix(1), vector(0)), lambda: api.rms_norm(matrix(0), None, vector(1)),
                  lambda: api.rms_norm_grad(matrix(1), None, matrix(0), vector(0), Tensor((2, 16), torch.float32, 0)),
-                 lambda: api.decode_8bit(codes(0)[0], codes(1)[1])):
+                 lambda: api.decode_8bit(codes(0)[0], codes(1)[1]),
+                 lambda: api.orthogonalize([Tensor((9, 5), torch.float32, i) for i in (0, 1)])):
         with pytest.raises(ValueError):
             call()
     assert machine.calls == [] and machine.current == 0
+
+
+def test_matrix_updates_are_laid_out_as_the_library_reads_them(monkeypatch):
+    """The binding fills the items as 64-bit words."""
+    import ctypes as C
+    machine, seen = Stand(monkeypatch), []
+
+    def call(items, n, *rest):
+        seen.extend((api.fo_matrix_update * n).from_address(items))
+        machine.copy = [{f: getattr(m, f) for f, _ in m._fields_} for m in seen]
+        return api.OK
+
+    monkeypatch.setattr(Stand, "fo_orthogonalize", staticmethod(call), raising=False)
+    shapes = [(9, 5), (7, 30)]
+    p, g, m = ([Tensor(s, torch.float32, 0) for s in shapes] for _ in range(3))
+    api.muon_step(p, g, m, lr=0.5, scales=[3.0, -0.25])
+    assert C.sizeof(api.fo_matrix_update) == 88
+    for got, (rows, cols), step in zip(machine.copy, shapes, (1.5, -0.125)):
+        assert got == dict(rows=rows, cols=cols, grad=4096, momentum=4096, out=None, param=4096, grad_stride=cols, momentum_stride=cols,
+                           out_stride=0, param_stride=cols, step=step)
+    for bad in (lambda: api.muon_step(p, g[:1], m, 0.1), lambda: api.muon_step(p, g, m, 0.1, scales=[1.0]),
+                lambda: api.orthogonalize(g, coefficients=(1.0, 2.0))):
+        with pytest.raises(ValueError):
+            bad()
+
+
+def items(*sizes, **over):
+    a = (api.fo_matrix_update * len(sizes))()
+    for it, (r, c) in zip(a, sizes):
+        it.rows, it.cols, it.grad, it.out, it.grad_stride, it.out_stride = r, c, P, P, c, c
+        for k, v in over.items():
+            setattr(it, k, v)
+    return a
+
+
+def orthogonalize(a, **over):
+    import ctypes as C
+    k = dict(dtype=0, steps=5, coefficients=(C.c_double * 3)(3.0, -4.0, 2.0), eps=1e-7, mu=0.9, nesterov=1, decay=1.0, workspace=P, bytes=1 << 40)
+    k.update(over)
+    return api.lib().fo_orthogonalize(a, len(a), *k.values(), None)
+
+
+@pytest.mark.parametrize("sizes,over,what", [
+    ([(-1, 4)], {}, "sides"), ([(32769, 32769)], {}, "sides"), ([(4, (1 << 20) + 1)], {}, "sides"),
+    ([(4, 4)], {"grad": None}, "pointer"), ([(4, 4)], {"grad": P + 2}, "pointer"), ([(4, 4)], {"momentum": P + 2}, "pointer"),
+    ([(4, 4)], {"out": None}, "neither"), ([(4, 4)], {"out_stride": 3}, "stride"), ([(4, 4)], {"grad_stride": -1}, "stride"),
+    ([(4, 4)], {"param": P, "param_stride": 2}, "stride"), ([(4, 4)], {"step": float("nan")}, "step")])
+def test_bad_matrices_are_refused(sizes, over, what):
+    assert orthogonalize(items(*sizes, **over)) == api.ERR_ARG and what in api.last_error()
+
+
+@pytest.mark.parametrize("over,what", [
+    ({"dtype": 2}, "dtype"), ({"steps": 0}, "steps"), ({"steps": 65}, "steps"), ({"coefficients": None}, "coefficients"), ({"eps": 0.0}, "eps"),
+    ({"mu": -0.1}, "momentum"), ({"mu": float("nan")}, "momentum"), ({"decay": float("inf")}, "decay"), ({"workspace": None}, "workspace"),
+    ({"workspace": P + 8}, "workspace"), ({"bytes": 1000}, "workspace")])
+def test_bad_orthogonalisations_are_refused(over, what):
+    assert orthogonalize(items((200, 300)), **over) == api.ERR_ARG and what in api.last_error()
+
+
+def test_orthogonalize_workspaces():
+    L = api.lib()
+    assert L.fo_orthogonalize_workspace(items((0, 5), (5, 0)), 2, 0) == 0 and L.fo_orthogonalize_workspace(None, 0, 0) == 0
+    assert L.fo_orthogonalize_workspace(None, 1, 0) == -1 and L.fo_orthogonalize_workspace(items((1, 1)), 1, 7) == -1
+    one = L.fo_orthogonalize_workspace(items((512, 700)), 1, 0)
+    assert one >= 8 * (512 * 700 + 512 * 512) and L.fo_orthogonalize_workspace(items(*[(512, 700)] * 40), 40, 0) == 32 * one
