@@ -12,12 +12,15 @@
 #include "../../include/fedoptima.h"
 
 #include <cuda_fp8.h>
+#include <atomic>
 #include <string>
 
 namespace fo {
 int report_error(int code, const std::string& msg);
 
 namespace {
+
+constexpr int kMaxDevices = 64;
 
 struct NormParams {
   const void *x, *r, *w;
@@ -138,8 +141,8 @@ __device__ __forceinline__ void store_eight(const NormParams& p, int row, int t,
 }
 
 // One row per warp (WARP) or per block; 8 NV elements per thread.
-template <typename T, typename W, int NV, bool VEC, bool WARP>
-__global__ void __launch_bounds__(WARP ? 256 : 1024) norm_fwd_k(const __grid_constant__ NormParams p) {
+template <typename T, typename W, int NV, bool VEC, bool WARP, int THREADS>
+__global__ void __launch_bounds__(THREADS) norm_fwd_k(const __grid_constant__ NormParams p) {
   __shared__ float box[32];
   pdl_wait();
   pdl_trigger();
@@ -205,27 +208,103 @@ __global__ void __launch_bounds__(1024) norm_fwd_wide_k(const __grid_constant__ 
   }
 }
 
+// Rows on their way into shared memory: each thread copies what it will read
+// itself, so its own copies are all it waits for.  STAGES rows are in flight.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+template <typename T, int NV>
+struct RowRing {
+  static constexpr int kPlanes = 3 * NV * int(sizeof(T)) / 2;      // 16 bytes of each thread: dy, s, ds
+  uint32_t at, stage;                  // this thread's first plane; bytes of a stage
+  __device__ __forceinline__ RowRing(const void* smem, int threads)
+      : at(uint32_t(__cvta_generic_to_shared(smem)) + threadIdx.x * 16), stage(kPlanes * threads * 16) {}
+  // Tensor `which` of a row into stage n.
+  __device__ __forceinline__ void copy(int n, int which, const T* row, int cols, int t, int G, int threads) const {
+    constexpr int kParts = int(sizeof(T)) / 2;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = column<true>(j, 0, t, G);
+      if (c < cols)
+#pragma unroll
+        for (int h = 0; h < kParts; ++h)
+          copy16(at + n * stage + ((which * NV + j) * kParts + h) * threads * 16, reinterpret_cast<const char*>(row + c) + 16 * h);
+    }
+  }
+  __device__ __forceinline__ void get(int n, int which, int cols, int t, int G, int threads, float (&v)[8 * NV]) const {
+    constexpr int kParts = int(sizeof(T)) / 2;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      uint4 w[kParts];
+#pragma unroll
+      for (int h = 0; h < kParts; ++h) {
+        w[h] = make_uint4(0u, 0u, 0u, 0u);
+        if (column<true>(j, 0, t, G) < cols)
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(w[h].x), "=r"(w[h].y), "=r"(w[h].z), "=r"(w[h].w)
+                       : "r"(at + n * stage + ((which * NV + j) * kParts + h) * threads * 16)
+                       : "memory");
+      }
+      if constexpr (kParts == 1) {
+        unpack8(w[0], v + 8 * j);
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          v[8 * j + 4 * h] = __uint_as_float(w[h].x);
+          v[8 * j + 4 * h + 1] = __uint_as_float(w[h].y);
+          v[8 * j + 4 * h + 2] = __uint_as_float(w[h].z);
+          v[8 * j + 4 * h + 3] = __uint_as_float(w[h].w);
+        }
+      }
+    }
+  }
+};
+
 // Each warp or block takes every n-th row and holds its part of dw until the
-// end.
-template <typename T, typename W, int NV, bool VEC, bool WARP>
-__global__ void __launch_bounds__(WARP ? 256 : 1024) norm_bwd_k(const __grid_constant__ NormGradParams p) {
-  extern __shared__ float dw_box[];         // WARP: [warps][cols]
+// end.  With 16-byte rows (VEC) the next STAGES - 1 rows are being copied while
+// one is worked on: a row's sum stands between its loads and its stores, and
+// without them a block waits for memory once per row (32768 x 4096 bf16: 345 us
+// instead of 208, 5.2 TB/s).
+template <typename T, typename W, int NV, bool VEC, bool WARP, int THREADS, int STAGES>
+__global__ void __launch_bounds__(THREADS) norm_bwd_k(const __grid_constant__ NormGradParams p) {
+  extern __shared__ __align__(16) char smem[];         // rows in flight; WARP, at the end: dw of [warps][cols]
   __shared__ float box[2][32];
   pdl_wait();
   pdl_trigger();
   const int G = WARP ? 32 : int(blockDim.x), t = int(threadIdx.x) % G;
   const int warp = int(threadIdx.x) / 32, per = WARP ? int(blockDim.x) / 32 : 1;
+  const int64_t first = int64_t(blockIdx.x) * per + (WARP ? warp : 0), next = int64_t(gridDim.x) * per;
+  const T *dy = static_cast<const T*>(p.dy), *sum = static_cast<const T*>(p.s), *ds = static_cast<const T*>(p.ds);
+  const RowRing<T, NV> ring(smem, THREADS);
+  auto fetch = [&](int64_t row, int n) {
+    if (row < p.rows) {
+      ring.copy(n, 0, dy + row * p.lddy, p.cols, t, G, THREADS);
+      ring.copy(n, 1, sum + row * p.lds, p.cols, t, G, THREADS);
+      if (ds) ring.copy(n, 2, ds + row * p.ldds, p.cols, t, G, THREADS);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if constexpr (VEC)
+#pragma unroll
+    for (int n = 0; n < STAGES - 1; ++n) fetch(first + n * next, n);
   float w[8 * NV], dw[8 * NV];
   load_row<W, VEC, NV>(static_cast<const W*>(p.w), p.cols, t, G, w);
 #pragma unroll
   for (int i = 0; i < 8 * NV; ++i) dw[i] = 0.f;
-  int turn = 0;
-  for (int64_t row = int64_t(blockIdx.x) * per + (WARP ? warp : 0); row < p.rows; row += int64_t(gridDim.x) * per) {
+  int turn = 0, n = 0;
+  for (int64_t row = first; row < p.rows; row += next) {
     float g[8 * NV], s[8 * NV], d[8 * NV];
-    load_row<T, VEC, NV>(static_cast<const T*>(p.dy) + row * p.lddy, p.cols, t, G, g);
-    load_row<T, VEC, NV>(static_cast<const T*>(p.s) + row * p.lds, p.cols, t, G, s);
-    if (p.ds) load_row<T, VEC, NV>(static_cast<const T*>(p.ds) + row * p.ldds, p.cols, t, G, d);
     const float r = p.rstd[row];
+    if constexpr (VEC) {
+      fetch(row + (STAGES - 1) * next, n == 0 ? STAGES - 1 : n - 1);
+      asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+      ring.get(n, 0, p.cols, t, G, THREADS, g);
+      ring.get(n, 1, p.cols, t, G, THREADS, s);
+    } else {
+      load_row<T, VEC, NV>(dy + row * p.lddy, p.cols, t, G, g);
+      load_row<T, VEC, NV>(sum + row * p.lds, p.cols, t, G, s);
+      if (ds) load_row<T, VEC, NV>(ds + row * p.ldds, p.cols, t, G, d);
+    }
     float a = 0.f;
 #pragma unroll
     for (int i = 0; i < 8 * NV; ++i) {
@@ -236,17 +315,22 @@ __global__ void __launch_bounds__(WARP ? 256 : 1024) norm_bwd_k(const __grid_con
     a = WARP ? warp_sum(a) : block_sum(a, box[turn]);
     turn ^= 1;
     const float k = -r * r * r * (a * p.inv_cols);
+    if (VEC && ds) ring.get(n, 2, p.cols, t, G, THREADS, d);
 #pragma unroll
     for (int i = 0; i < 8 * NV; ++i) {
       g[i] = fmaf(g[i], r, s[i] * k);
-      if (p.ds) g[i] += d[i];
+      if (ds) g[i] += d[i];
     }
     store_row<T, VEC, NV>(static_cast<T*>(p.dx) + row * p.lddx, p.cols, t, G, g);
+    n = n + 1 == STAGES ? 0 : n + 1;
   }
   float* out = p.part + int64_t(blockIdx.x) * p.cols;
   if constexpr (!WARP) {
     store_row<float, VEC, NV>(out, p.cols, t, G, dw);
   } else {
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+    float* dw_box = reinterpret_cast<float*>(smem);
     store_row<float, VEC, NV>(dw_box + warp * p.cols, p.cols, t, G, dw);
     __syncthreads();
     for (int c = threadIdx.x; c < p.cols; c += blockDim.x) {
@@ -306,58 +390,82 @@ __global__ void __launch_bounds__(256) norm_dw_k(const float* part, W* dw, int p
   }
 }
 
-// 2^(scale - 127) times the 8-bit floats.
+// 2^(scale - 127); a NaN for 255.
+__device__ __forceinline__ float scale_of(int b) {
+  // 2^-127 is half of the smallest normal number
+  return b == 255 ? __uint_as_float(0x7fc00000u) : b == 0 ? __uint_as_float(0x400000u) : __uint_as_float(uint32_t(b) << 23);
+}
+__device__ __forceinline__ float2 decode_pair(uint32_t two, float up) {
+  const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(__nv_fp8x2_storage_t(two), __NV_E4M3);     // exact
+  const float2 f = __half22float2(__half2(h));
+  return make_float2(f.x * up, f.y * up);
+}
+
+// The scale times the 8-bit floats.  A thread's U vectors of eight are loaded
+// before the first is used (16384 x 2048: 20.5 us with one, 5.0 TB/s).
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) decode_k(const uint8_t* q, const uint8_t* scales, T* y, int64_t ldy, int64_t items,
                                                 int cols) {
   pdl_wait();
   pdl_trigger();
+  constexpr int U = VEC ? 4 : 1;
   const int per = VEC ? cols / 8 : cols, blocks = (cols + 31) / 32;
   const int64_t step = int64_t(gridDim.x) * blockDim.x;
-  for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < items; i += step) {
-    const int64_t row = i / per;
-    const int c = int(i - row * per) * (VEC ? 8 : 1);
-    const int b = scales[row * blocks + c / 32];
-    // 2^-127 is half of the smallest normal number
-    const float up = b == 255 ? __uint_as_float(0x7fc00000u) : b == 0 ? __uint_as_float(0x400000u) : __uint_as_float(uint32_t(b) << 23);
-    auto value = [&](uint32_t byte) {
-      __nv_fp8_e4m3 f;
-      f.__x = __nv_fp8_storage_t(byte);
-      return float(f) * up;
-    };
+  for (int64_t i0 = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i0 < items; i0 += U * step) {
     if constexpr (VEC) {
-      const uint2 w = *reinterpret_cast<const uint2*>(q + row * cols + c);
-      float v[8];
+      uint2 w[U];
+      int b[U];
+      T* to[U];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        v[e] = value(w.x >> (8 * e) & 0xffu);
-        v[4 + e] = value(w.y >> (8 * e) & 0xffu);
+      for (int u = 0; u < U; ++u) {
+        const int64_t i = i0 + u * step;
+        to[u] = nullptr;
+        if (i >= items) continue;
+        const int64_t row = i / per;
+        const int c = int(i - row * per) * 8;
+        w[u] = *reinterpret_cast<const uint2*>(q + row * cols + c);
+        b[u] = scales[row * blocks + c / 32];
+        to[u] = y + row * ldy + c;
       }
-      store8(y + row * ldy + c, v);
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (!to[u]) continue;
+        const float up = scale_of(b[u]);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float2 f = decode_pair((e < 2 ? w[u].x : w[u].y) >> (16 * (e % 2)) & 0xffffu, up);
+          v[2 * e] = f.x;
+          v[2 * e + 1] = f.y;
+        }
+        store8(to[u], v);
+      }
     } else {
-      y[row * ldy + c] = from_f<T>(value(q[row * cols + c]));
+      const int64_t row = i0 / per;
+      const int c = int(i0 - row * per);
+      y[row * ldy + c] = from_f<T>(decode_pair(q[row * cols + c], scale_of(scales[row * blocks + c / 32])).x);
     }
   }
 }
 
-// Threads of a row: a warp up to 1024 columns, above a block with 16 elements
-// per thread (32 above 16384 columns).
+// Threads of a row: a warp up to 1024 columns, above a block with up to 16
+// elements per thread.
 struct RowShape {
   bool warp;
-  int nv, threads;
+  int threads;
 };
 RowShape row_shape(int cols) {
-  if (cols <= 256) return {true, 1, 256};
-  if (cols <= 512) return {true, 2, 256};
-  if (cols <= 1024) return {true, 4, 256};
-  if (cols <= 16384) return {false, 2, (cols + 16 * 32 - 1) / (16 * 32) * 32};
-  if (cols <= 32768) return {false, 4, 1024};
-  return {false, 0, 1024};
+  if (cols <= 1024) return {true, 256};
+  if (cols <= 16384) return {false, (cols + 16 * 32 - 1) / (16 * 32) * 32};
+  return {false, 1024};
 }
-constexpr int kGradBlocks = 304;
-int grad_blocks(int rows, const RowShape& a) {
+// Blocks of a gradient: two per SM, or one whose rows in flight fill its shared
+// memory (fewer where there are fewer rows).
+int grad_blocks(int rows, int cols) {
+  const RowShape a = row_shape(cols);
   const int per = a.warp ? a.threads / 32 : 1, want = (rows + per - 1) / per;
-  return want < kGradBlocks ? want : kGradBlocks;
+  const int most = cols <= 4096 ? 2 * 152 : 152;
+  return want < most ? want : most;
 }
 
 template <typename T, typename W, bool VEC>
@@ -365,26 +473,43 @@ cudaError_t forward(const NormParams& p, cudaStream_t st) {
   const RowShape a = row_shape(p.cols);
   const int per = a.warp ? a.threads / 32 : 1;
   const dim3 grid(unsigned((int64_t(p.rows) + per - 1) / per)), block(unsigned(a.threads));
-  if (a.warp) {
-    auto k = a.nv == 1 ? norm_fwd_k<T, W, 1, VEC, true> : a.nv == 2 ? norm_fwd_k<T, W, 2, VEC, true> : norm_fwd_k<T, W, 4, VEC, true>;
-    return launch_k(k, grid, block, 0, st, p);
-  }
-  auto k = a.nv == 2 ? norm_fwd_k<T, W, 2, VEC, false> : a.nv == 4 ? norm_fwd_k<T, W, 4, VEC, false> : norm_fwd_wide_k<T, W>;
+  auto k = p.cols <= 256     ? norm_fwd_k<T, W, 1, VEC, true, 256>
+           : p.cols <= 512   ? norm_fwd_k<T, W, 2, VEC, true, 256>
+           : p.cols <= 1024  ? norm_fwd_k<T, W, 4, VEC, true, 256>
+           : p.cols <= 4096  ? norm_fwd_k<T, W, 2, VEC, false, 256>
+           : p.cols <= 8192  ? norm_fwd_k<T, W, 2, VEC, false, 512>
+           : p.cols <= 16384 ? norm_fwd_k<T, W, 2, VEC, false, 1024>
+                             : norm_fwd_wide_k<T, W>;
   return launch_k(k, grid, block, 0, st, p);
+}
+// The gradient's kernel, launched with its shared memory.
+template <typename T, typename W, int NV, bool VEC, bool WARP, int THREADS, int STAGES>
+cudaError_t backward_rows(const NormGradParams& p, int blocks, cudaStream_t st) {
+  auto k = norm_bwd_k<T, W, NV, VEC, WARP, THREADS, STAGES>;
+  const size_t ring = VEC ? size_t(STAGES) * RowRing<T, NV>::kPlanes * THREADS * 16 : 0;
+  const size_t box = WARP ? size_t(THREADS / 32) * p.cols * sizeof(float) : 0, smem = ring > box ? ring : box;
+  static std::atomic<bool> allowed[kMaxDevices];
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess && smem > 48 * 1024 && !(dev < kMaxDevices && allowed[dev])) {
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem));
+    if (e == cudaSuccess && dev < kMaxDevices) allowed[dev] = true;
+  }
+  if (e != cudaSuccess) return e;
+  return launch_k(k, dim3(unsigned(blocks)), dim3(THREADS), smem, st, p);
 }
 template <typename T, typename W, bool VEC>
 cudaError_t backward(const NormGradParams& p, void* dw, cudaStream_t st) {
-  const RowShape a = row_shape(p.cols);
-  const int blocks = grad_blocks(p.rows, a);
+  const int blocks = grad_blocks(p.rows, p.cols);
+  constexpr int K = sizeof(T) == 2 ? 4 : 2;       // rows in flight: 96 KB per block of 256 threads
   cudaError_t e;
-  if (a.warp) {
-    const size_t smem = size_t(a.threads / 32) * p.cols * sizeof(float);
-    auto k = a.nv == 1 ? norm_bwd_k<T, W, 1, VEC, true> : a.nv == 2 ? norm_bwd_k<T, W, 2, VEC, true> : norm_bwd_k<T, W, 4, VEC, true>;
-    e = launch_k(k, dim3(unsigned(blocks)), dim3(unsigned(a.threads)), smem, st, p);
-  } else {
-    auto k = a.nv == 2 ? norm_bwd_k<T, W, 2, VEC, false> : a.nv == 4 ? norm_bwd_k<T, W, 4, VEC, false> : norm_bwd_wide_k<T, W>;
-    e = launch_k(k, dim3(unsigned(blocks)), dim3(unsigned(a.threads)), 0, st, p);
-  }
+  if (p.cols <= 256) e = backward_rows<T, W, 1, VEC, true, 256, K>(p, blocks, st);
+  else if (p.cols <= 512) e = backward_rows<T, W, 2, VEC, true, 256, K>(p, blocks, st);
+  else if (p.cols <= 1024) e = backward_rows<T, W, 4, VEC, true, 256, 2>(p, blocks, st);
+  else if (p.cols <= 4096) e = backward_rows<T, W, 2, VEC, false, 256, K>(p, blocks, st);
+  else if (p.cols <= 8192) e = backward_rows<T, W, 2, VEC, false, 512, K>(p, blocks, st);
+  else if (p.cols <= 16384) e = backward_rows<T, W, 2, VEC, false, 1024, K / 2>(p, blocks, st);
+  else e = launch_k(norm_bwd_wide_k<T, W>, dim3(unsigned(blocks)), dim3(1024), 0, st, p);
   if (e != cudaSuccess) return e;
   return launch_k(norm_dw_k<W>, dim3(unsigned((p.cols + 31) / 32)), dim3(256), 0, st, (const float*)p.part,
                   static_cast<W*>(dw), blocks, p.cols);
@@ -466,7 +591,7 @@ int fo_rms_norm(const void* x, int64_t x_stride, const void* residual, int64_t r
 
 int64_t fo_rms_norm_workspace(int64_t rows, int64_t cols) {
   if (check_sizes(FO_DTYPE_F32, rows, cols)) return -1;
-  return rows == 0 ? 0 : int64_t(grad_blocks(int(rows), row_shape(int(cols)))) * cols * 4;
+  return rows == 0 ? 0 : int64_t(grad_blocks(int(rows), int(cols))) * cols * 4;
 }
 
 int fo_rms_norm_grad(const void* dy, int64_t dy_stride, const void* ds, int64_t ds_stride, const void* s, int64_t s_stride,
