@@ -1,4 +1,4 @@
-"""Devices that train transformer blocks beside the server.
+"""Devices that train transformer blocks beside the server, in two kinds.
 
 The transformer workload's server trains blocks behind the split (Sec. 3.2); the
 part in front of it, M_dk (an embedding and two blocks, as the workload counts
@@ -10,8 +10,18 @@ torch's.  One event follows Algorithm 1: a local iteration with the local loss
 f_d, then the upload of its split-point activations, which the server trains on
 (Algorithms 2 and 3).
 
-    python -m paper_2504_13850_gb300.sequence
+``RmsDevice`` trains blocks of another kind: a scaled token embedding
+(``api.embedding`` / ``embedding_grad``), root-mean-square norms that take the
+residual's addition with them (``api.rms_norm`` / ``rms_norm_grad``), and weight
+matrices whose momentum is made orthogonal before each step
+(``api.muon_step``).  It uploads its split-point activations in 8 bits
+(``api.rms_norm_8bit``), half of the bytes S_l / b_k of Eq. 5 that bf16 takes;
+the server's side decodes them (``api.decode_8bit``).
+
+    python -m paper_2504_13850_gb300.sequence [--rms]
 """
+import sys
+
 import torch
 from torch.autograd.function import once_differentiable
 
@@ -118,14 +128,147 @@ class SequenceDevice:
         return x.detach(), loss.detach()
 
 
-def run(events=32, devices=4, seed=0, vocab=30522):
+class TokenEmbedding(torch.autograd.Function):
+    """scale * table[ids] in bf16, of an fp32 table; zeros for padding (ids < 0)."""
+
+    @staticmethod
+    def forward(ctx, table, ids, scale):
+        ctx.save_for_backward(ids)
+        ctx.how = table.shape[0], scale
+        return api.embedding(ids, table, scale=scale, dtype=torch.bfloat16)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dx):
+        vocab, scale = ctx.how
+        return api.embedding_grad(dx, *ctx.saved_tensors, vocab, scale=scale, dtype=torch.float32), None, None
+
+
+class Norm(torch.autograd.Function):
+    """Root-mean-square norm of x."""
+
+    @staticmethod
+    def forward(ctx, x, weight):
+        y, _, r = api.rms_norm(x, None, weight)
+        ctx.save_for_backward(x, weight, r)
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, weight, r = ctx.saved_tensors
+        return api.rms_norm_grad(dy, None, x, weight, r)
+
+
+class AddNorm(torch.autograd.Function):
+    """(norm of x + residual, x + residual)."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight):
+        y, s, r = api.rms_norm(x, residual, weight)
+        ctx.save_for_backward(s, weight, r)
+        return y, s
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, ds):
+        dx, dw = api.rms_norm_grad(dy, ds, *ctx.saved_tensors)
+        return dx, dx, dw
+
+
+class UploadNorm(torch.autograd.Function):
+    """The norm of x + residual and its 8-bit form (values, scales), which has no
+    gradient."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight):
+        q, scales, y, s, r = api.rms_norm_8bit(x, residual, weight, with_y=True)
+        ctx.save_for_backward(s, weight, r)
+        ctx.mark_non_differentiable(q, scales)
+        return y, q, scales
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, *_):
+        s, weight, r = ctx.saved_tensors
+        dx, dw = api.rms_norm_grad(dy, None, s, weight, r)
+        return dx, dx, dw
+
+
+class RmsDevice:
+    """One device with root-mean-square norms and orthogonalised updates; bf16
+    compute on fp32 parameters.  The embedding, norms, bias tables and head are
+    trained by SGD with momentum."""
+
+    def __init__(self, seed, vocab=30522, width=512, heads=8, blocks=2, classes=2, lr=0.01, matrix_lr=0.02, momentum=0.9,
+                 weight_decay=0.0):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        self.width, self.heads, self.buckets = width, heads, api.relative_buckets(BUCKETS, REACH)
+        self.matrix_lr, self.momentum, self.weight_decay = matrix_lr, momentum, weight_decay
+
+        def matrix(n, m):
+            return (torch.randn(n, m, device="cuda", generator=g) * m ** -0.5).requires_grad_()
+
+        def ones():
+            return torch.ones(width, device="cuda").requires_grad_()
+
+        self.embedding = (torch.randn(vocab, width, device="cuda", generator=g) * width ** -0.5).requires_grad_()
+        self.blocks = [{"norm1": ones(), "qkv": matrix(3 * width, width),
+                        "table": torch.zeros(heads, BUCKETS, device="cuda").requires_grad_(), "proj": matrix(width, width),
+                        "norm2": ones(), "up": matrix(4 * width, width), "down": matrix(width, 4 * width)} for _ in range(blocks)]
+        self.norm, self.head = ones(), matrix(classes, width)
+        self.matrices = [b[n] for b in self.blocks for n in ("qkv", "proj", "up", "down")]
+        self.momenta = [torch.zeros_like(m) for m in self.matrices]
+        self.others = [self.embedding, self.norm, self.head] + [b[n] for b in self.blocks for n in ("norm1", "table", "norm2")]
+        self.opt = torch.optim.SGD(self.others, lr=lr, momentum=momentum)
+
+    def forward(self, tokens, lengths):
+        """Split-point activations [B, L, width] (bf16) of tokens [B, L], and their 8-bit form."""
+        B, L = tokens.shape
+        valid = torch.arange(L, device=tokens.device) < lengths[:, None]
+        documents = torch.where(valid, 0, -1).to(torch.int32)
+        linear = torch.nn.functional.linear
+        x = TokenEmbedding.apply(self.embedding, torch.where(valid, tokens, -1), self.width ** 0.5)
+        branch = None
+        for b in self.blocks:
+            w = {n: b[n].bfloat16() for n in ("qkv", "table", "proj", "up", "down")}
+            h, x = (Norm.apply(x, b["norm1"]), x) if branch is None else AddNorm.apply(branch, x, b["norm1"])
+            o = PackedAttention.apply(linear(h, w["qkv"]).view(B, L, 3, self.heads, -1), w["table"], self.buckets, documents)
+            h, x = AddNorm.apply(linear(o.reshape(B, L, -1), w["proj"]), x, b["norm2"])
+            branch = linear(torch.nn.functional.gelu(linear(h, w["up"])), w["down"])
+        return UploadNorm.apply(branch, x, self.norm)
+
+    def step(self, tokens, lengths, labels):
+        """One local iteration with the auxiliary head's loss f_d (softmax
+        cross-entropy of the mean over valid tokens): ((8-bit activations, their
+        scales), loss)."""
+        for p in self.matrices:
+            p.grad = None
+        self.opt.zero_grad(set_to_none=True)
+        x, *upload = self.forward(tokens, lengths)
+        valid = (torch.arange(tokens.shape[1], device=tokens.device) < lengths[:, None]).unsqueeze(2)
+        pooled = (x.float() * valid).sum(1) / lengths[:, None]
+        loss = torch.nn.functional.cross_entropy(pooled @ self.head.t(), labels.long())
+        loss.backward()
+        # waits for the step's work; a kernel that gave up a wait ends the step
+        # before it changes a parameter
+        api.attention_error()
+        with torch.no_grad():
+            api.muon_step(self.matrices, [p.grad for p in self.matrices], self.momenta, self.matrix_lr, momentum=self.momentum,
+                          weight_decay=self.weight_decay)
+        self.opt.step()
+        api.orthogonalize_error()
+        return tuple(t.detach() for t in upload), loss.detach()
+
+
+def run(events=32, devices=4, seed=0, vocab=30522, kind=SequenceDevice):
     """Device events and server iterations; returns the local and server losses."""
     cfg = dict(W.CONFIGS["transformer"], K=devices, omega=4 * devices)
     B, L = cfg["batch"], cfg["in_hwc"][0]
     server = api.Server.from_config(cfg)
     server.set_params(W.init_params(cfg))
     g = torch.Generator(device="cuda").manual_seed(seed)
-    parts = [SequenceDevice(seed + k, vocab) for k in range(devices)]
+    parts = [kind(seed + k, vocab) for k in range(devices)]
     data = [(torch.randint(vocab, (B, L), device="cuda", generator=g),
              torch.randint(32, L + 1, (B,), device="cuda", generator=g, dtype=torch.int32),
              torch.randint(2, (B,), device="cuda", generator=g, dtype=torch.int32)) for _ in range(devices)]
@@ -135,6 +278,9 @@ def run(events=32, devices=4, seed=0, vocab=30522):
         tokens, lengths, labels = data[k]
         x, loss = parts[k].step(tokens, lengths, labels)
         local.append(loss)
+        if kind is RmsDevice:                  # what arrived, for the server's slot
+            x = api.decode_8bit(*x)
+            torch.cuda.current_stream().synchronize()
         if server.enqueue_activations(k, x, labels, lengths)[0] == api.OK:
             server.server_step()
     server.synchronize()
@@ -145,6 +291,6 @@ def run(events=32, devices=4, seed=0, vocab=30522):
 
 
 if __name__ == "__main__":
-    local, global_ = run()
+    local, global_ = run(kind=RmsDevice if "--rms" in sys.argv[1:] else SequenceDevice)
     print("device losses", [round(v, 3) for v in local])
     print("server losses", [round(v, 3) for v in global_])
