@@ -67,20 +67,23 @@ struct Item {
 };
 struct OrthoParams {
   Item item[kItems];
-  int start[kItems + 1];    // first unit of work of each matrix in this launch
-  uint8_t order[kItems];    // the matrices in the order of their units
+  // First unit of work of each matrix: before the steps in start[0], then in each
+  // product; the matrices in the order of their units.
+  int start[3][kItems + 1];
+  uint8_t order[3][kItems];
   char* ws;
   float4* sums;
   float2* scale;            // of each matrix: the two factors that make X of U
-  int count, from, last;    // from: which X is read; last: X goes to the caller
+  unsigned* done;           // of each matrix: how many of its units' warps are done, over all steps
+  int count, steps;
   float ca, cb, cc, mu, decay;
   bool nesterov;
   float eps;
 };
 
-__device__ __forceinline__ int slot_of(const OrthoParams& p, int unit) {
+__device__ __forceinline__ int slot_of(const OrthoParams& p, int unit, int which = 0) {
   int n = 0;
-  while (n + 1 < p.count && unit >= p.start[n + 1]) ++n;
+  while (n + 1 < p.count && unit >= p.start[which][n + 1]) ++n;
   return n;
 }
 
@@ -173,7 +176,7 @@ __global__ void __launch_bounds__(256) ortho_sums_k(const __grid_constant__ Orth
   __shared__ float4 box[8];
   pdl_wait();
   pdl_trigger();
-  const int n = slot_of(p, blockIdx.x), part = int(blockIdx.x) - p.start[n];
+  const int n = slot_of(p, blockIdx.x), part = int(blockIdx.x) - p.start[0][n];
   const Item& it = p.item[n];
   const uint32_t per_row = uint32_t(it.cols + 7) / 8;               // vectors of eight
   const int64_t total = int64_t(it.rows) * per_row, stride = int64_t(it.nsums) * 256;
@@ -232,6 +235,7 @@ __global__ void __launch_bounds__(256) ortho_scale_k(const __grid_constant__ Ort
     int unit;
     const float root = sum.root(unit);
     p.scale[n] = factors(root, unit, p.eps);
+    p.done[n] = 0;
   }
 }
 
@@ -263,7 +267,7 @@ __global__ void __launch_bounds__(256) ortho_pack_k(const __grid_constant__ Orth
   pdl_trigger();
   const int n = slot_of(p, blockIdx.x);
   const Item& it = p.item[n];
-  const int blk = int(blockIdx.x) - p.start[n], rows = 2 * it.mt;
+  const int blk = int(blockIdx.x) - p.start[0][n], rows = 2 * it.mt;
   const int rb = blk % rows, cb = blk / rows, t = threadIdx.x, row = t / 4;
   // the user's matrix: two groups of eight of one row
   const int r0 = 64 * (it.transposed ? cb : rb), c0 = 64 * (it.transposed ? rb : cb);
@@ -299,26 +303,37 @@ constexpr int kThreads = 320;                 // copies, products, eight warps o
 template <int PARTS, int BN>
 struct Tiles {
   static constexpr int kA = 2 * kBlock, kB = BN / 128 * kBlock;
-  static constexpr int kStage = PARTS * (kA + kB), kStages = 196608 / kStage;
-  static constexpr int kOut = 8 * 4096;       // 4 KB per warp of arithmetic
+  static constexpr int kStage = PARTS * (kA + kB), kStages = 163840 / kStage;
+  static constexpr int kOut = 8 * 8192;       // two parts of 32 x 64 elements per warp of arithmetic
   static constexpr int kSumsAt = 512 / BN;    // tiles' sums in tensor memory
-  static constexpr int kBars = 3 * kStages + 2 * kSumsAt + 1;
+  static constexpr int kBars = 3 * kStages + 2 * kSumsAt + 9;
   static constexpr int kSmem = 1024 + kStages * kStage + kOut + 8 * kBars + 16;
 };
 static_assert(Tiles<1, 256>::kSmem <= 232448 && Tiles<1, 128>::kSmem <= 232448 && Tiles<2, 128>::kSmem <= 232448, "shared memory per CTA");
 
 struct Place {
-  int item, i, j, kb;       // rows 256 i, columns BN j, blocks of 64 terms (none: nothing to do)
+  int item, phase, step;
+  int i, j, kb;             // rows 256 i, columns BN j, blocks of 64 terms (none: nothing to do)
+  unsigned need;            // warps of this matrix that are done with what this unit reads
 };
-template <int PHASE, int BN>
+template <int BN>
 __device__ __forceinline__ Place place_of(const OrthoParams& p, int unit) {
   Place a;
-  const int n = slot_of(p, unit);
-  a.item = p.order[n];
+  const int n0 = p.start[kGram][p.count], n1 = p.start[kPoly][p.count], n2 = p.start[kApply][p.count];
+  a.step = unit / (n0 + n1 + n2);
+  int t = unit - a.step * (n0 + n1 + n2);
+  a.phase = t < n0 ? kGram : t < n0 + n1 ? kPoly : kApply;
+  t -= a.phase == kGram ? 0 : a.phase == kPoly ? n0 : n0 + n1;
+  const int n = slot_of(p, t, a.phase);
+  a.item = p.order[a.phase][n];
   const Item& it = p.item[a.item];
-  const int t = unit - p.start[n];
-  const int h = (it.mt + 1) / 2, cols = PHASE == kApply ? it.nt : it.mt;
-  if (PHASE == kApply) {
+  t -= p.start[a.phase][n];
+  const int h = (it.mt + 1) / 2, cols = a.phase == kApply ? it.nt : it.mt;
+  // units that have something to do (an odd last column's second half has not)
+  const unsigned triangle = BN == 256 ? h * (h + 1) / 2 : h * (h + 1) - (it.mt & 1 ? h : 0);
+  const unsigned all = 2 * triangle + h * ((it.nt + BN / 128 - 1) / (BN / 128));
+  a.need = 16 * (a.step * all + a.phase * triangle);
+  if (a.phase == kApply) {
     a.i = t % h;
     a.j = t / h;
   } else {                  // 256 x 256 on and above the diagonal, column by column
@@ -329,8 +344,25 @@ __device__ __forceinline__ Place place_of(const OrthoParams& p, int unit) {
     a.i = u - j * (j + 1) / 2;
     a.j = BN == 256 ? j : 2 * j + t % 2;
   }
-  a.kb = a.j * (BN / 128) < cols ? 2 * (PHASE == kGram ? it.nt : it.mt) : 0;
+  a.kb = a.j * (BN / 128) < cols ? 2 * (a.phase == kGram ? it.nt : it.mt) : 0;
   return a;
+}
+// Before copies of what other blocks have stored: `need` of their warps have said so.
+__device__ __forceinline__ void wait_for(Waits& w, const unsigned* done, unsigned need, int code) {
+  if (w.dead || need == 0) return;
+  const uint64_t t0 = global_ns();
+  while (true) {
+    for (int i = 0; i < 64; ++i) {
+      unsigned now;
+      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(now) : "l"(done) : "memory");
+      if (now >= need) {
+        asm volatile("fence.proxy.async;" ::: "memory");
+        return;
+      }
+    }
+    if (global_ns() - t0 > w.limit) break;
+  }
+  w.give_up(code);
 }
 // A symmetric matrix holds its 128 x 128 tiles (i, j) with i / 2 <= j / 2.  Rows
 // 128 i .. of block column kb lie there as rows, or mirrored, as columns of block
@@ -419,37 +451,45 @@ __device__ __forceinline__ void deliver(const OrthoParams& p, const Item& m, int
   __syncwarp();
 }
 
+// A warp's 32 rows of a block of A, C or X: 4 KB per part, in the block's order.
+__device__ __forceinline__ int64_t rows_at(const Item& m, int tile, int cblk, int q) {
+  return (int64_t(cblk) * 2 * m.mt + 2 * tile + q / 2) * kBlock + (q & 1) * 4096;
+}
+// What the sums of these rows are added to (A or X) is on its way into the warp's
+// buffer while the products run.
+template <int PARTS, int PHASE>
+__device__ __forceinline__ void fetch(const OrthoParams& p, const Item& m, int step, int tile, int cblk, int q, int lane, char* buf, uint64_t* bar) {
+  if (PHASE == kGram || lane != 0) return;
+  const char* src = p.ws + (PHASE == kPoly ? m.a : m.x[step & 1]) + rows_at(m, tile, cblk, q);
+  constexpr int kParts = PHASE == kPoly ? PARTS : 2;
+  bulk_wait_read<0>();                // the last stores have read the buffer
+  mbar_expect_tx(bar, kParts * 4096);
+#pragma unroll
+  for (int part = 0; part < kParts; ++part)
+    bulk_g2s(buf + part * 4096, src + part * (int64_t(m.mt) * (PHASE == kPoly ? m.mt : m.nt) * 4 * kBlock), 4096, bar);
+}
+
 // 64 sums of one row, columns 64 cblk .., become elements of A, C or X.
 template <int PARTS, int PHASE, typename T>
-__device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int tile, int cblk, int q, int lane, uint32_t buf, float (&v)[64]) {
-  const int64_t block = int64_t(cblk) * 2 * m.mt + 2 * tile + q / 2;
-  const int64_t half_block = block * kBlock + (q & 1) * 4096;       // this warp's 32 rows
-  const int64_t xi = int64_t(m.mt) * m.nt * 4 * kBlock, si = int64_t(m.mt) * m.mt * 4 * kBlock;
+__device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int step, int tile, int cblk, int q, int lane, char* buf_ptr, uint64_t* bar,
+                                       uint32_t& phase, Waits& wait, float (&v)[64]) {
+  const uint32_t buf = smem_u32(buf_ptr), mine = buf + lane * 128;       // a lane reads and writes its own row
   if (PHASE == kGram) {
 #pragma unroll
     for (int e = 0; e < 64; ++e) v[e] *= kUpA / (kUpX * kUpX);
+    if (lane == 0) bulk_wait_read<0>();       // the last stores have read the buffer
+    __syncwarp();
   } else {
     // C = b A + c A A, or a X + C X
     const float linear = PHASE == kPoly ? p.cb : p.ca, other = (PHASE == kPoly ? p.cc : 1.f) / kUpA;
-    // the warp's 4 KB are read as they lie, and handed out by rows through shared memory
-    const uint4* src = reinterpret_cast<const uint4*>(p.ws + (PHASE == kPoly ? m.a : m.x[p.from]) + half_block) + lane;
     constexpr int kParts = PHASE == kPoly ? PARTS : 2;
-    const int64_t image = (PHASE == kPoly ? si : xi) / 16;
-    uint4 w[kParts][8];
+    wait.on_lanes(bar, phase, 69);
+    phase ^= 1;
 #pragma unroll
-    for (int part = 0; part < kParts; ++part)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) w[part][k] = src[part * image + 32 * k];
-    if (lane == 0) bulk_wait_read<0>();       // the last store has read the buffer
-#pragma unroll
-    for (int part = kParts - 1; part >= 0; --part) {
-      __syncwarp();
-#pragma unroll
-      for (int k = 0; k < 8; ++k) st_shared4(buf + (32 * k + lane) * 16, w[part][k].x, w[part][k].y, w[part][k].z, w[part][k].w);
-      __syncwarp();
+    for (int part = kParts - 1; part >= 0; --part)
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float4 u = ld_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16);
+        const float4 u = ld_shared4(mine + part * 4096 + (k ^ (lane & 7)) * 16);
         const float z[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -459,46 +499,57 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
           y = fmaf(linear, f.y, part == kParts - 1 ? y * other : y);
         }
       }
-    }
-    __syncwarp();
   }
-  if (PHASE == kApply && p.last) {
+  if (PHASE == kApply && step + 1 == p.steps) {
     deliver<T>(p, m, tile, 64 * cblk, q, lane, buf, v);
     deliver<T>(p, m, tile, 64 * cblk + 32, q, lane, buf, v + 32);
+    fence_proxy_async_smem();                 // before the next copy into the buffer
+    __syncwarp();
     return;
   }
-  char* dst = p.ws + (PHASE == kGram ? m.a : PHASE == kPoly ? m.c : m.x[p.from ^ 1]) + half_block;
-  const int64_t image = PHASE == kApply ? xi : si;
+  constexpr int kParts = PHASE == kApply ? 2 : PARTS;
 #pragma unroll
-  for (int part = 0; part < (PHASE == kApply ? 2 : PARTS); ++part) {
-    if (lane == 0) bulk_wait_read<0>();       // the last store has read the buffer
-    __syncwarp();
+  for (int part = 0; part < kParts; ++part)
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const uint4 w = take_half8(v + 8 * k);
-      st_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16, w.x, w.y, w.z, w.w);
+      st_shared4(mine + part * 4096 + (k ^ (lane & 7)) * 16, w.x, w.y, w.z, w.w);
     }
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) {
-      asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 4096;" ::"l"(dst + part * image), "r"(buf) : "memory");
-      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-    }
+  fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0) {
+    char* dst = p.ws + (PHASE == kGram ? m.a : PHASE == kPoly ? m.c : m.x[step & 1 ^ 1]) + rows_at(m, tile, cblk, q);
+#pragma unroll
+    for (int part = 0; part < kParts; ++part)
+      asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 4096;" ::"l"(
+                       dst + part * (int64_t(m.mt) * (PHASE == kApply ? m.nt : m.mt) * 4 * kBlock)),
+                   "r"(buf + part * 4096)
+                   : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
   }
 }
 
-template <int PARTS, int BN, int PHASE, typename T>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_product_k(const __grid_constant__ OrthoParams p) {
+// All steps of all matrices in one launch.  Units of work (a tile of one of the
+// three products of a step of a matrix) have an order, and pairs take them in
+// turn; a unit's copies start when the units of the matrix before it are done,
+// which every warp that has stored its part says in the matrix's counter.  So
+// the products of one matrix fill the gaps of another's, and between two products
+// of one lie 2 us instead of a launch's 7 (its blocks fill an SM's shared memory,
+// so they cannot start while the last launch's run).  Units wait for earlier ones
+// only and all blocks run at the same time (a cooperative launch).
+template <int PARTS, int BN, typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_steps_k(const __grid_constant__ OrthoParams p) {
   using S = Tiles<PARTS, BN>;
   extern __shared__ char smem_raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   char* stage_out = smem + S::kStages * S::kStage;
   uint64_t* full = reinterpret_cast<uint64_t*>(stage_out + S::kOut);
   uint64_t *peer = full + S::kStages, *empty = peer + S::kStages, *acc_full = empty + S::kStages, *acc_empty = acc_full + S::kSumsAt,
-           *done = acc_empty + S::kSumsAt;
-  uint32_t* tslot = reinterpret_cast<uint32_t*>(done + 1);
+           *done = acc_empty + S::kSumsAt, *fetched = done + 1;
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(fetched + 8);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int units = p.start[p.count], pair = int(blockIdx.x) / 2, pairs = int(gridDim.x) / 2, me = int(blockIdx.x) % 2;
+  const int units = p.steps * (p.start[kGram][p.count] + p.start[kPoly][p.count] + p.start[kApply][p.count]);
+  const int pair = int(blockIdx.x) / 2, pairs = int(gridDim.x) / 2, me = int(blockIdx.x) % 2;
 
   if (threadIdx.x == 0) {
     for (int e = 0; e < S::kStages; ++e) {
@@ -511,6 +562,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
       mbar_init(&acc_empty[e], 16);        // one arrival per warp of arithmetic, of both CTAs
     }
     mbar_init(done, 1);
+    for (int e = 0; e < 8; ++e) mbar_init(&fetched[e], 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -523,8 +575,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
   cluster_sync_all();                // both CTAs' barriers are there
   tc_fence_after();
   const uint32_t tmem = *tslot;      // sum s: columns BN s
-  pdl_trigger();                     // this block holds its tensor memory
-  pdl_wait();
   Waits wait(&g_err);
 
   if (warp == 0) {
@@ -532,16 +582,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
       Ring<S::kStages> at;
       int it = 0;
       for (int u = pair; u < units && !wait.dead; u += pairs) {
-        const Place a = place_of<PHASE, BN>(p, u);
+        const Place a = place_of<BN>(p, u);
         const Item& m = p.item[a.item];
-        const char* x = p.ws + m.x[p.from];
-        const char* sym = p.ws + (PHASE == kPoly ? m.a : m.c);
+        const char* x = p.ws + m.x[a.step & 1];
+        const char* sym = p.ws + (a.phase == kPoly ? m.a : m.c);
         const int64_t xi = int64_t(m.mt) * m.nt * 4 * kBlock, si = int64_t(m.mt) * m.mt * 4 * kBlock;
-        const int cols = PHASE == kApply ? m.nt : m.mt;       // tiles of 128
+        const int cols = a.phase == kApply ? m.nt : m.mt;     // tiles of 128
         const int ta = 2 * a.i + me, tb = BN == 256 ? 2 * a.j + me : a.j;
         const bool has_a = ta < m.mt, has_b = tb < cols;
         const uint32_t bytes = PARTS * ((has_a ? S::kA : 0) + (has_b ? S::kB : 0));
         const int64_t wide = int64_t(2 * m.mt) * kBlock;      // from one block column to the next
+        if (a.kb) wait_for(wait, p.done + a.item, a.need, 60);
         for (int kb = 0; kb < a.kb; ++kb, ++it) {
           if (it >= S::kStages) wait.on(&empty[at.at], at.phase ^ 1, 61);
           if (wait.dead) break;
@@ -552,8 +603,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
           for (int q = 0; q < PARTS; ++q) {
             if (has_a) {
               char* d = s + q * S::kA;
-              const char* src = PHASE == kGram ? x + q * xi : sym + q * si;
-              if (PHASE == kGram || !mirrored(ta, kb)) {
+              const char* src = a.phase == kGram ? x + q * xi : sym + q * si;
+              if (a.phase == kGram || !mirrored(ta, kb)) {
                 bulk_g2s(d, src + kb * wide + int64_t(2 * ta) * kBlock, 2 * kBlock, bar);
               } else {
                 src += 2 * ta * wide + int64_t(kb) * kBlock;
@@ -563,9 +614,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
             }
             if (has_b) {
               char* d = s + PARTS * S::kA + q * S::kB;
-              const char* src = PHASE == kPoly ? sym + q * si : x + q * xi;
+              const char* src = a.phase == kPoly ? sym + q * si : x + q * xi;
               const int b0 = BN == 256 ? 2 * tb : 2 * tb + me;          // this CTA's first block
-              if (PHASE == kGram || (PHASE == kPoly && !mirrored(tb, kb))) {
+              if (a.phase == kGram || (a.phase == kPoly && !mirrored(tb, kb))) {
                 bulk_g2s(d, src + kb * wide + int64_t(b0) * kBlock, S::kB, bar);
               } else {
                 src += b0 * wide + int64_t(kb) * kBlock;
@@ -585,7 +636,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
     if (lane == 0) {
       Ring<S::kStages> at;
       for (int u = pair; u < units && !wait.dead; u += pairs) {
-        const Place a = place_of<PHASE, BN>(p, u);
+        const Place a = place_of<BN>(p, u);
         for (int kb = 0; kb < a.kb; ++kb) {
           wait.on(&full[at.at], at.phase, 65);
           if (wait.dead) break;
@@ -603,7 +654,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
     const uint32_t ring = smem_u32(smem);
     bool dead = false;
     for (int u = pair; u < units && !dead; u += pairs) {
-      const Place a = place_of<PHASE, BN>(p, u);
+      const Place a = place_of<BN>(p, u);
       const int tb = BN == 256 ? 2 * a.j : a.j;
       for (int kb = 0; kb < a.kb; ++kb) {
         const uint32_t d = tmem + sum.at * BN;
@@ -615,7 +666,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
         tc_fence_after();
         const uint32_t s = ring + at.at * S::kStage;
         // mirrored operands have their rows along the terms
-        const uint32_t am = PHASE != kGram && mirrored(2 * a.i, kb), bm = PHASE == kApply || (PHASE == kPoly && mirrored(tb, kb));
+        const uint32_t am = a.phase != kGram && mirrored(2 * a.i, kb), bm = a.phase == kApply || (a.phase == kPoly && mirrored(tb, kb));
         const uint32_t idesc = id | am << 15 | bm << 16;
         const uint32_t as = am ? 2048u : 32u, bs = bm ? 2048u : 32u;
         const uint32_t al = (am ? uint32_t(kBlock) : 16u) >> 4 << 16, bl = (bm ? uint32_t(kBlock) : 16u) >> 4 << 16;
@@ -655,27 +706,40 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
     const int q = warp % 4, half = (warp - 2) / 4;
     constexpr int NB = BN / 128;
     const uint32_t col = tmem + (uint32_t(32 * q) << 16) + (BN / 2) * half;
-    const uint32_t buf = smem_u32(stage_out) + uint32_t(warp - 2) * 4096u;
+    char* buf = stage_out + (warp - 2) * 8192;
+    uint64_t* in = &fetched[warp - 2];
+    uint32_t in_phase = 0;
     Ring<S::kSumsAt> sum;
     bool dead = false;
     for (int u = pair; u < units && !dead; u += pairs) {
-      const Place a = place_of<PHASE, BN>(p, u);
-      if (a.kb == 0) continue;
+      const Place a = place_of<BN>(p, u);
       const Item& m = p.item[a.item];
-      const int tile = 2 * a.i + me, cblk = a.j * (BN / 64) + half * NB, cols = 2 * (PHASE == kApply ? m.nt : m.mt);
-      float v[PARTS == 2 ? NB : 1][64];
+      const int tile = 2 * a.i + me, cblk = a.j * (BN / 64) + half * NB, cols = 2 * (a.phase == kApply ? m.nt : m.mt);
+      float v[64];
+      auto get = [&](int b) {
+        if (a.phase == kPoly) fetch<PARTS, kPoly>(p, m, a.step, tile, cblk + b, q, lane, buf, in);
+        else fetch<PARTS, kApply>(p, m, a.step, tile, cblk + b, q, lane, buf, in);
+      };
+      auto end = [&](int b) {
+        if (a.phase == kGram) finish<PARTS, kGram, T>(p, m, a.step, tile, cblk + b, q, lane, buf, in, in_phase, wait, v);
+        else if (a.phase == kPoly) finish<PARTS, kPoly, T>(p, m, a.step, tile, cblk + b, q, lane, buf, in, in_phase, wait, v);
+        else finish<PARTS, kApply, T>(p, m, a.step, tile, cblk + b, q, lane, buf, in, in_phase, wait, v);
+      };
+      bool here = a.kb > 0 && tile < m.mt && cblk < cols;        // the first block of columns
       if (PARTS == 2) {
         for (int kb = 0; kb < a.kb; ++kb) {
           wait.on(&acc_full[sum.at], sum.phase, 64);
           __syncwarp();
           tc_fence_after();
+          // the first sum tells that what the unit reads is there
+          if (kb == 0 && here && a.phase != kGram) get(0);
 #pragma unroll
-          for (int h = 0; h < 2 * NB; ++h) {
+          for (int h = 0; h < 2; ++h) {
             uint32_t r[32];
             tmem_ld32(col + sum.at * BN + 32 * h, r);
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-              float& x = v[h / 2][32 * (h % 2) + e];
+              float& x = v[32 * h + e];
               x = (kb > 0 ? x : 0.f) + __uint_as_float(r[e]);
             }
           }
@@ -686,14 +750,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
         }
         dead = __any_sync(0xffffffffu, wait.dead);
         if (dead) break;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-          if (tile < m.mt && cblk + b < cols) finish<PARTS, PHASE, T>(p, m, tile, cblk + b, q, lane, buf, v[b]);
-      } else {
+        static_assert(PARTS == 1 || NB == 1, "one block of columns");
+        if (here) end(0);
+      } else if (a.kb > 0) {
         wait.on(&acc_full[sum.at], sum.phase, 64);
         __syncwarp();
         tc_fence_after();
         dead = __any_sync(0xffffffffu, wait.dead);
+        if (here && a.phase != kGram) get(0);
 #pragma unroll 1
         for (int b = 0; b < NB; ++b) {
 #pragma unroll
@@ -701,19 +765,32 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_p
             uint32_t r[32];
             tmem_ld32(col + sum.at * BN + 64 * b + 32 * h, r);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[0][32 * h + e] = __uint_as_float(r[e]);
+            for (int e = 0; e < 32; ++e) v[32 * h + e] = __uint_as_float(r[e]);
           }
           if (b == NB - 1) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) arrive_leader(&acc_empty[sum.at]);
           }
-          if (!dead && tile < m.mt && cblk + b < cols) finish<PARTS, PHASE, T>(p, m, tile, cblk + b, q, lane, buf, v[0]);
+          if (dead || !here) continue;
+          end(b);
+          here = b + 1 < NB && cblk + b + 1 < cols;
+          if (here && a.phase != kGram) get(b + 1);
         }
         sum.step();
       }
+      // this warp's part is stored: units that read it may start
+      if (lane == 0 && a.kb > 0 && !(a.phase == kApply && a.step + 1 == p.steps)) {
+        bulk_wait_all();
+        asm volatile("fence.proxy.async;" ::: "memory");
+        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.done + a.item) : "memory");
+      }
+      __syncwarp();
     }
-    if (lane == 0) bulk_wait_all();
+    if (lane == 0) {
+      bulk_wait_all();
+      if (dead) mbar_wait(in, in_phase);         // no copy is on its way into the buffer
+    }
     __syncwarp();
   }
   tc_fence_before();
@@ -755,13 +832,13 @@ __device__ __forceinline__ void put_row(uint32_t at, uint32_t part, int row, int
 }
 
 template <int PARTS, typename T>
-__global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThreads, 1) ortho_small_k(const __grid_constant__ OrthoParams p, int steps) {
+__global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThreads, 1) ortho_small_k(const __grid_constant__ OrthoParams p) {
   extern __shared__ char smem_raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, t = threadIdx.x;
   const Item& m = p.item[blockIdx.x / kSmallCtas];
   const int me = blockIdx.x % kSmallCtas;
-  const int rows = m.transposed ? m.cols : m.rows, cols = m.transposed ? m.rows : m.cols;      // rows <= cols
+  const int cols = m.transposed ? m.rows : m.cols;      // the larger side
   const int ctas = (cols + kSmallCols - 1) / kSmallCols, col0 = me * kSmallCols;
   if (me >= ctas) return;
   const int blocks = (min(cols - col0, kSmallCols) + 63) / 64;       // of 64 columns, here
@@ -917,7 +994,7 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
       for (int e = 0; e < 32; ++e) v[e] += __uint_as_float(r[e]);
     }
   };
-  for (int step = 0; step < steps; ++step) {
+  for (int step = 0; step < p.steps; ++step) {
     begin();
     if (warp == 0) {
       for (int c = 0; c < blocks; ++c) {
@@ -986,7 +1063,7 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
             y = fmaf(p.ca, fh.y, fmaf(p.ca, fl.y, y * (1.f / kUpA)));
           }
         }
-        if (step + 1 < steps) put_row<2>(x_block, kSmallX, row, 4 * h, v);
+        if (step + 1 < p.steps) put_row<2>(x_block, kSmallX, row, 4 * h, v);
         else deliver<T>(p, m, 0, col0 + 64 * quarter + 32 * h, q, lane, sa + warp * 4096, v);
       }
     }
@@ -1024,94 +1101,97 @@ int64_t item_bytes(const fo_matrix_update& m, int parts) {
   return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + kMaxSums * 16 + 16;
 }
 
-template <int PARTS, int BN, int PHASE, typename T>
-cudaError_t launch_product(const OrthoParams& p, int pairs, cudaStream_t st) {
-  auto k = ortho_product_k<PARTS, BN, PHASE, T>;
-  static std::atomic<bool> allowed[kMaxDevices];
-  const cudaError_t e = allow_smem(k, allowed);
-  if (e != cudaSuccess) return e;
-  const int units = p.start[p.count];
-  return launch_k(k, dim3(2 * unsigned(units < pairs ? units : pairs)), dim3(kThreads), Tiles<PARTS, BN>::kSmem, st, p);
-}
-
-// Units of each matrix, those with the longest sums first.
+// Units of each matrix in one of the products, those with the longest sums first.
 template <int PHASE, int BN>
 int64_t plan(OrthoParams& p) {
   auto length = [&p](int i) { return PHASE == kGram ? p.item[i].nt : p.item[i].mt; };
+  uint8_t* order = p.order[PHASE];
   for (int i = 0; i < p.count; ++i) {
     int at = i;
-    for (; at > 0 && length(p.order[at - 1]) < length(i); --at) p.order[at] = p.order[at - 1];
-    p.order[at] = uint8_t(i);
+    for (; at > 0 && length(order[at - 1]) < length(i); --at) order[at] = order[at - 1];
+    order[at] = uint8_t(i);
   }
   int64_t units = 0;
   for (int i = 0; i < p.count; ++i) {
-    p.start[i] = int(units);
-    const Item& m = p.item[p.order[i]];
+    p.start[PHASE][i] = int(units);
+    const Item& m = p.item[order[i]];
     const int64_t h = (m.mt + 1) / 2;
     if (PHASE == kApply) units += h * (BN == 256 ? (m.nt + 1) / 2 : m.nt);
     else units += h * (h + 1) / 2 * (256 / BN);
   }
-  p.start[p.count] = int(units);
+  p.start[PHASE][p.count] = int(units);
   return units;
 }
 
-template <int PARTS, int PHASE, typename T>
-cudaError_t product(OrthoParams& p, int pairs, cudaStream_t st) {
-  // Wide tiles load fewer bytes per product and take 1.7 times as long as narrow
-  // ones; narrow ones divide the work into twice as many.  fp32 matrices, whose
-  // products are three, load few enough with narrow ones, and a wide tile's sums
-  // would not fit into the registers.
-  if constexpr (PARTS == 1) {
-    const int64_t wide = plan<PHASE, 256>(p), narrow = plan<PHASE, 128>(p);
-    if (17 * ((wide + pairs - 1) / pairs) <= 10 * ((narrow + pairs - 1) / pairs)) {
-      plan<PHASE, 256>(p);
-      return launch_product<PARTS, 256, PHASE, T>(p, pairs, st);
-    }
-  } else {
-    plan<PHASE, 128>(p);
+template <int PARTS, int BN, typename T>
+cudaError_t launch_steps(OrthoParams& p, int dev, cudaStream_t st) {
+  auto k = ortho_steps_k<PARTS, BN, T>;
+  static std::atomic<bool> allowed[kMaxDevices];
+  static std::atomic<int> resident[kMaxDevices];      // pairs that run at the same time
+  cudaError_t e = allow_smem(k, allowed);
+  if (e != cudaSuccess) return e;
+  const int64_t units = plan<kGram, BN>(p) + plan<kPoly, BN>(p) + plan<kApply, BN>(p);
+  if (units * p.steps >= int64_t(1) << 31) return cudaErrorInvalidValue;      // sides are limited: not reached
+  cudaLaunchConfig_t cfg = {};
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Tiles<PARTS, BN>::kSmem;
+  cfg.stream = st;
+  cfg.gridDim = dim3(2);
+  int pairs = dev < kMaxDevices ? resident[dev].load() : 0;
+  if (pairs == 0) {
+    if ((e = cudaOccupancyMaxActiveClusters(&pairs, k, &cfg)) != cudaSuccess) return e;
+    if (pairs < 1) return cudaErrorCooperativeLaunchTooLarge;
+    if (dev < kMaxDevices) resident[dev].store(pairs);
   }
-  return launch_product<PARTS, 128, PHASE, T>(p, pairs, st);
+  cfg.gridDim = dim3(2 * unsigned(units < pairs ? units : pairs));
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeCooperative;
+  attr[0].val.cooperative = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, k, static_cast<const OrthoParams&>(p));
 }
 
 template <typename T>
-cudaError_t orthogonalize_small(const OrthoParams& p, int steps, cudaStream_t st) {
+cudaError_t orthogonalize_small(const OrthoParams& p, cudaStream_t st) {
   auto k = ortho_small_k<sizeof(T) == 4 ? 2 : 1, T>;
   static std::atomic<bool> allowed[kMaxDevices];
   const cudaError_t e = allow_smem(k, allowed);
   if (e != cudaSuccess) return e;
-  return launch_k(k, dim3(kSmallCtas * unsigned(p.count)), dim3(kSmallThreads), kSmallSmem, st, p, steps);
+  return launch_k(k, dim3(kSmallCtas * unsigned(p.count)), dim3(kSmallThreads), kSmallSmem, st, p);
 }
 template <typename T>
-cudaError_t orthogonalize(OrthoParams& p, int steps, cudaStream_t st) {
-  constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
+cudaError_t orthogonalize(OrthoParams& p, cudaStream_t st) {
   int dev = 0, sms = 1;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
-  const int pairs = sms > 1 ? sms / 2 : 1;
   int64_t units = 0;
   for (int i = 0; i < p.count; ++i) {
-    p.start[i] = int(units);
+    p.start[0][i] = int(units);
     units += p.item[i].nsums;
   }
-  p.start[p.count] = int(units);
+  p.start[0][p.count] = int(units);
   if ((e = launch_k(ortho_sums_k<T>, dim3(unsigned(units)), dim3(256), 0, st, p)) != cudaSuccess) return e;
   if ((e = launch_k(ortho_scale_k, dim3(unsigned(p.count)), dim3(256), 0, st, p)) != cudaSuccess) return e;
   units = 0;
   for (int i = 0; i < p.count; ++i) {
-    p.start[i] = int(units);
+    p.start[0][i] = int(units);
     units += 4 * int64_t(p.item[i].mt) * p.item[i].nt;
   }
-  p.start[p.count] = int(units);
+  p.start[0][p.count] = int(units);
   if ((e = launch_k(ortho_pack_k<T>, dim3(unsigned(units)), dim3(256), 0, st, p)) != cudaSuccess) return e;
-  for (int s = 0; s < steps; ++s) {
-    p.from = s & 1;
-    p.last = s + 1 == steps;
-    if ((e = product<PARTS, kGram, T>(p, pairs, st)) != cudaSuccess) return e;
-    if ((e = product<PARTS, kPoly, T>(p, pairs, st)) != cudaSuccess) return e;
-    if ((e = product<PARTS, kApply, T>(p, pairs, st)) != cudaSuccess) return e;
+  // Wide tiles load fewer bytes per product and take 1.7 times as long as narrow
+  // ones, which divide the work into twice as many: they are taken where a product
+  // has fewer than two rounds of wide ones.  fp32 matrices, whose products are
+  // three, load few enough with narrow ones, and a wide tile's sums would not fit
+  // into the registers.
+  if constexpr (sizeof(T) == 2) {
+    if (plan<kApply, 256>(p) >= sms) return launch_steps<1, 256, T>(p, dev, st);
+    return launch_steps<1, 128, T>(p, dev, st);
+  } else {
+    return launch_steps<2, 128, T>(p, dev, st);
   }
-  return cudaSuccess;
 }
 
 }  // namespace
@@ -1165,6 +1245,7 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
    for (const bool small : {true, false}) {
     OrthoParams p = {};
     p.ws = static_cast<char*>(workspace);
+    p.steps = steps;
     p.ca = float(coefficients[0]);
     p.cb = float(coefficients[1]);
     p.cc = float(coefficients[2]);
@@ -1215,8 +1296,9 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
     if (p.count == 0) continue;
     p.sums = reinterpret_cast<float4*>(p.ws + at);
     p.scale = reinterpret_cast<float2*>(p.sums + p.count * kMaxSums);
-    const cudaError_t e = small ? (dtype == FO_DTYPE_F32 ? orthogonalize_small<float>(p, steps, st) : orthogonalize_small<bf16>(p, steps, st))
-                          : dtype == FO_DTYPE_F32 ? orthogonalize<float>(p, steps, st) : orthogonalize<bf16>(p, steps, st);
+    p.done = reinterpret_cast<unsigned*>(p.scale + p.count);
+    const cudaError_t e = small ? (dtype == FO_DTYPE_F32 ? orthogonalize_small<float>(p, st) : orthogonalize_small<bf16>(p, st))
+                          : dtype == FO_DTYPE_F32 ? orthogonalize<float>(p, st) : orthogonalize<bf16>(p, st);
     if (e != cudaSuccess) return done(e);
   }
   return FO_OK;
