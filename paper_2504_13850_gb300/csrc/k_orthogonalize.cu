@@ -38,6 +38,7 @@
 #include "fo_vec8.cuh"
 #include "../../include/fedoptima.h"
 
+#include <algorithm>
 #include <atomic>
 #include <cmath>
 #include <string>
@@ -52,6 +53,7 @@ __device__ GaveUp g_err;
 constexpr int kItems = 32;                    // matrices per launch
 constexpr int kBlock = 8192;                  // bytes of a 64 x 64 block
 constexpr int kMaxSums = 1024;                // partial sums of squares per matrix
+constexpr int kMaxShared = 64;                // tiles of A whose sums are shared, per matrix
 constexpr float kUpX = 1024.f, kUpA = 256.f;  // what X, and A and C, are multiplied by as fp16
 
 struct Item {
@@ -60,8 +62,10 @@ struct Item {
   void* out;
   int64_t ldg, ldm, ldp, ldo;
   int64_t x[2], a, c;       // byte offsets in the workspace
+  int64_t parts;            // of A's sums that are shared, [tile][split][CTA][warp] of 8 KB
   int rows, cols, mt, nt;   // mt, nt: tiles of 128 of the smaller and the larger side
   int nsums;                // partial sums of squares, at kMaxSums times its index
+  int split;                // units that share one of A's sums
   bool transposed, vec_in, vec_out;
   float step;
 };
@@ -75,6 +79,7 @@ struct OrthoParams {
   float4* sums;
   float2* scale;            // of each matrix: the two factors that make X of U
   unsigned* done;           // of each matrix: how many of its units' warps are done, over all steps
+  unsigned* shared;         // the same of each tile of A whose sums are shared, kMaxShared for each matrix
   int count, steps;
   float ca, cb, cc, mu, decay;
   bool nesterov;
@@ -237,6 +242,7 @@ __global__ void __launch_bounds__(256) ortho_scale_k(const __grid_constant__ Ort
     p.scale[n] = factors(root, unit, p.eps);
     p.done[n] = 0;
   }
+  if (threadIdx.x < kMaxShared) p.shared[n * kMaxShared + threadIdx.x] = 0;
 }
 
 __device__ __forceinline__ uint32_t half_pair(float a, float b) {
@@ -303,8 +309,10 @@ constexpr int kThreads = 320;                 // copies, products, eight warps o
 template <int PARTS, int BN>
 struct Tiles {
   static constexpr int kA = 2 * kBlock, kB = BN / 128 * kBlock;
-  static constexpr int kStage = PARTS * (kA + kB), kStages = 163840 / kStage;
-  static constexpr int kOut = 8 * 8192;       // two parts of 32 x 64 elements per warp of arithmetic
+  // Of 32 x 64 elements per warp of arithmetic: both parts, or with wide tiles,
+  // which want the room for copies in flight, one.
+  static constexpr int kBuffer = BN == 256 ? 4096 : 8192, kOut = 8 * kBuffer;
+  static constexpr int kStage = PARTS * (kA + kB), kStages = (229376 - kOut) / kStage;
   static constexpr int kSumsAt = 512 / BN;    // tiles' sums in tensor memory
   static constexpr int kBars = 3 * kStages + 2 * kSumsAt + 9;
   static constexpr int kSmem = 1024 + kStages * kStage + kOut + 8 * kBars + 16;
@@ -314,6 +322,8 @@ static_assert(Tiles<1, 256>::kSmem <= 232448 && Tiles<1, 128>::kSmem <= 232448 &
 struct Place {
   int item, phase, step;
   int i, j, kb;             // rows 256 i, columns BN j, blocks of 64 terms (none: nothing to do)
+  int k0, split, tile;      // its first block; which of the units that share a sum; the tile's number
+  bool adds;                // it has the last of the shared terms and adds the others' sums, or is alone
   unsigned need;            // warps of this matrix that are done with what this unit reads
 };
 template <int BN>
@@ -333,6 +343,14 @@ __device__ __forceinline__ Place place_of(const OrthoParams& p, int unit) {
   const unsigned triangle = BN == 256 ? h * (h + 1) / 2 : h * (h + 1) - (it.mt & 1 ? h : 0);
   const unsigned all = 2 * triangle + h * ((it.nt + BN / 128 - 1) / (BN / 128));
   a.need = 16 * (a.step * all + a.phase * triangle);
+  a.k0 = a.split = 0;
+  a.adds = true;
+  if (a.phase == kGram) {
+    a.split = t % it.split;
+    t /= it.split;
+    a.adds = a.split + 1 == it.split;
+  }
+  a.tile = t;
   if (a.phase == kApply) {
     a.i = t % h;
     a.j = t / h;
@@ -345,6 +363,10 @@ __device__ __forceinline__ Place place_of(const OrthoParams& p, int unit) {
     a.j = BN == 256 ? j : 2 * j + t % 2;
   }
   a.kb = a.j * (BN / 128) < cols ? 2 * (a.phase == kGram ? it.nt : it.mt) : 0;
+  if (a.phase == kGram && it.split > 1) {
+    a.k0 = a.kb * a.split / it.split;
+    a.kb = a.kb * (a.split + 1) / it.split - a.k0;
+  }
   return a;
 }
 // Before copies of what other blocks have stored: `need` of their warps have said so.
@@ -457,9 +479,9 @@ __device__ __forceinline__ int64_t rows_at(const Item& m, int tile, int cblk, in
 }
 // What the sums of these rows are added to (A or X) is on its way into the warp's
 // buffer while the products run.
-template <int PARTS, int PHASE>
+template <int PARTS, int BN, int PHASE>
 __device__ __forceinline__ void fetch(const OrthoParams& p, const Item& m, int step, int tile, int cblk, int q, int lane, char* buf, uint64_t* bar) {
-  if (PHASE == kGram || lane != 0) return;
+  if (BN == 256 || PHASE == kGram || lane != 0) return;
   const char* src = p.ws + (PHASE == kPoly ? m.a : m.x[step & 1]) + rows_at(m, tile, cblk, q);
   constexpr int kParts = PHASE == kPoly ? PARTS : 2;
   bulk_wait_read<0>();                // the last stores have read the buffer
@@ -469,8 +491,54 @@ __device__ __forceinline__ void fetch(const OrthoParams& p, const Item& m, int s
     bulk_g2s(buf + part * 4096, src + part * (int64_t(m.mt) * (PHASE == kPoly ? m.mt : m.nt) * 4 * kBlock), 4096, bar);
 }
 
+// One of the units that share a tile's sums leaves its own in the workspace, and
+// the last adds the others' in their order: 32 columns at a time of the warp's 32
+// rows (4 KB), every lane its own.
+__device__ __forceinline__ char* shared_at(const OrthoParams& p, const Item& m, const Place& a, int split, int me, int warp) {
+  return p.ws + m.parts + (((int64_t(a.tile) * (m.split - 1) + split) * 2 + me) * 8 + warp) * 8192;
+}
+__device__ __forceinline__ void leave_sums(const OrthoParams& p, const Item& m, const Place& a, int me, int warp, int lane, char* buf, float (&v)[64]) {
+  const uint32_t mine = smem_u32(buf) + lane * 16;
+  char* dst = shared_at(p, m, a, a.split, me, warp);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (lane == 0) bulk_wait_read<0>();
+    __syncwarp();
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      st_shared4(mine + k * 512, __float_as_uint(v[32 * h + 4 * k]), __float_as_uint(v[32 * h + 4 * k + 1]), __float_as_uint(v[32 * h + 4 * k + 2]),
+                 __float_as_uint(v[32 * h + 4 * k + 3]));
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 4096;" ::"l"(dst + h * 4096), "r"(smem_u32(buf)) : "memory");
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    }
+  }
+}
+__device__ __forceinline__ void add_sums(const OrthoParams& p, const Item& m, const Place& a, int me, int warp, int lane, float (&v)[64]) {
+  float own[64];
+#pragma unroll
+  for (int e = 0; e < 64; ++e) own[e] = 0.f;
+  for (int s = 0; s + 1 < m.split; ++s) {
+    const float4* src = reinterpret_cast<const float4*>(shared_at(p, m, a, s, me, warp)) + lane;
+    float4 w[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) w[k] = __ldcg(src + 32 * k);
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      own[4 * k] += w[k].x;
+      own[4 * k + 1] += w[k].y;
+      own[4 * k + 2] += w[k].z;
+      own[4 * k + 3] += w[k].w;
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 64; ++e) v[e] += own[e];
+}
+
 // 64 sums of one row, columns 64 cblk .., become elements of A, C or X.
-template <int PARTS, int PHASE, typename T>
+template <int PARTS, int BN, int PHASE, typename T>
 __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int step, int tile, int cblk, int q, int lane, char* buf_ptr, uint64_t* bar,
                                        uint32_t& phase, Waits& wait, float (&v)[64]) {
   const uint32_t buf = smem_u32(buf_ptr), mine = buf + lane * 128;       // a lane reads and writes its own row
@@ -483,13 +551,31 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
     // C = b A + c A A, or a X + C X
     const float linear = PHASE == kPoly ? p.cb : p.ca, other = (PHASE == kPoly ? p.cc : 1.f) / kUpA;
     constexpr int kParts = PHASE == kPoly ? PARTS : 2;
-    wait.on_lanes(bar, phase, 69);
-    phase ^= 1;
+    uint4 w[BN == 256 ? kParts : 1][8];
+    if (BN == 256) {          // the warp's 4 KB are read as they lie, past L1, which may hold an older step's
+      const uint4* src = reinterpret_cast<const uint4*>(p.ws + (PHASE == kPoly ? m.a : m.x[step & 1]) + rows_at(m, tile, cblk, q)) + lane;
 #pragma unroll
-    for (int part = kParts - 1; part >= 0; --part)
+      for (int part = 0; part < kParts; ++part)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) w[part][k] = __ldcg(src + part * (int64_t(m.mt) * (PHASE == kPoly ? m.mt : m.nt) * 4 * kBlock / 16) + 32 * k);
+      if (lane == 0) bulk_wait_read<0>();       // the last stores have read the buffer
+    } else {
+      wait.on_lanes(bar, phase, 69);
+      phase ^= 1;
+    }
+#pragma unroll
+    for (int part = kParts - 1; part >= 0; --part) {
+      if (BN == 256) {        // and handed out by rows
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          st_shared4(buf + (32 * k + lane) * 16, w[BN == 256 ? part : 0][k].x, w[BN == 256 ? part : 0][k].y, w[BN == 256 ? part : 0][k].z,
+                     w[BN == 256 ? part : 0][k].w);
+        __syncwarp();
+      }
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float4 u = ld_shared4(mine + part * 4096 + (k ^ (lane & 7)) * 16);
+        const float4 u = ld_shared4(mine + (BN == 256 ? 0 : part * 4096) + (k ^ (lane & 7)) * 16);
         const float z[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -499,6 +585,8 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
           y = fmaf(linear, f.y, part == kParts - 1 ? y * other : y);
         }
       }
+    }
+    if (BN == 256) __syncwarp();
   }
   if (PHASE == kApply && step + 1 == p.steps) {
     deliver<T>(p, m, tile, 64 * cblk, q, lane, buf, v);
@@ -508,24 +596,32 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
     return;
   }
   constexpr int kParts = PHASE == kApply ? 2 : PARTS;
+  char* dst = p.ws + (PHASE == kGram ? m.a : PHASE == kPoly ? m.c : m.x[step & 1 ^ 1]) + rows_at(m, tile, cblk, q);
 #pragma unroll
-  for (int part = 0; part < kParts; ++part)
+  for (int part = 0; part < kParts; ++part) {
+    const uint32_t at = BN == 256 ? 0 : part * 4096;
+    if (BN == 256 && part > 0) {
+      if (lane == 0) bulk_wait_read<0>();
+      __syncwarp();
+    }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const uint4 w = take_half8(v + 8 * k);
-      st_shared4(mine + part * 4096 + (k ^ (lane & 7)) * 16, w.x, w.y, w.z, w.w);
+      st_shared4(mine + at + (k ^ (lane & 7)) * 16, w.x, w.y, w.z, w.w);
     }
-  fence_proxy_async_smem();
-  __syncwarp();
-  if (lane == 0) {
-    char* dst = p.ws + (PHASE == kGram ? m.a : PHASE == kPoly ? m.c : m.x[step & 1 ^ 1]) + rows_at(m, tile, cblk, q);
+    if (BN == 256 || part + 1 == kParts) {
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) {
 #pragma unroll
-    for (int part = 0; part < kParts; ++part)
-      asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 4096;" ::"l"(
-                       dst + part * (int64_t(m.mt) * (PHASE == kApply ? m.nt : m.mt) * 4 * kBlock)),
-                   "r"(buf + part * 4096)
-                   : "memory");
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        for (int o = BN == 256 ? part : 0; o <= part; ++o)
+          asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 4096;" ::"l"(
+                           dst + o * (int64_t(m.mt) * (PHASE == kApply ? m.nt : m.mt) * 4 * kBlock)),
+                       "r"(buf + (BN == 256 ? 0 : o * 4096))
+                       : "memory");
+        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+      }
+    }
   }
 }
 
@@ -593,7 +689,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
         const uint32_t bytes = PARTS * ((has_a ? S::kA : 0) + (has_b ? S::kB : 0));
         const int64_t wide = int64_t(2 * m.mt) * kBlock;      // from one block column to the next
         if (a.kb) wait_for(wait, p.done + a.item, a.need, 60);
-        for (int kb = 0; kb < a.kb; ++kb, ++it) {
+        for (int kb = a.k0; kb < a.k0 + a.kb; ++kb, ++it) {
           if (it >= S::kStages) wait.on(&empty[at.at], at.phase ^ 1, 61);
           if (wait.dead) break;
           char* s = smem + at.at * S::kStage;
@@ -706,7 +802,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
     const int q = warp % 4, half = (warp - 2) / 4;
     constexpr int NB = BN / 128;
     const uint32_t col = tmem + (uint32_t(32 * q) << 16) + (BN / 2) * half;
-    char* buf = stage_out + (warp - 2) * 8192;
+    char* buf = stage_out + (warp - 2) * S::kBuffer;
     uint64_t* in = &fetched[warp - 2];
     uint32_t in_phase = 0;
     Ring<S::kSumsAt> sum;
@@ -717,13 +813,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
       const int tile = 2 * a.i + me, cblk = a.j * (BN / 64) + half * NB, cols = 2 * (a.phase == kApply ? m.nt : m.mt);
       float v[64];
       auto get = [&](int b) {
-        if (a.phase == kPoly) fetch<PARTS, kPoly>(p, m, a.step, tile, cblk + b, q, lane, buf, in);
-        else fetch<PARTS, kApply>(p, m, a.step, tile, cblk + b, q, lane, buf, in);
+        if (a.phase == kPoly) fetch<PARTS, BN, kPoly>(p, m, a.step, tile, cblk + b, q, lane, buf, in);
+        else fetch<PARTS, BN, kApply>(p, m, a.step, tile, cblk + b, q, lane, buf, in);
       };
       auto end = [&](int b) {
-        if (a.phase == kGram) finish<PARTS, kGram, T>(p, m, a.step, tile, cblk + b, q, lane, buf, in, in_phase, wait, v);
-        else if (a.phase == kPoly) finish<PARTS, kPoly, T>(p, m, a.step, tile, cblk + b, q, lane, buf, in, in_phase, wait, v);
-        else finish<PARTS, kApply, T>(p, m, a.step, tile, cblk + b, q, lane, buf, in, in_phase, wait, v);
+        if (BN == 128 && a.phase == kGram && m.split > 1) {
+          if (!a.adds) {
+            leave_sums(p, m, a, me, warp - 2, lane, buf, v);
+            return;
+          }
+          if (lane == 0) wait_for(wait, p.shared + a.item * kMaxShared + a.tile, 16u * (m.split - 1) * (a.step + 1), 70);
+          __syncwarp();
+          add_sums(p, m, a, me, warp - 2, lane, v);
+        }
+        if (a.phase == kGram) finish<PARTS, BN, kGram, T>(p, m, a.step, tile, cblk + b, q, lane, buf, in, in_phase, wait, v);
+        else if (a.phase == kPoly) finish<PARTS, BN, kPoly, T>(p, m, a.step, tile, cblk + b, q, lane, buf, in, in_phase, wait, v);
+        else finish<PARTS, BN, kApply, T>(p, m, a.step, tile, cblk + b, q, lane, buf, in, in_phase, wait, v);
       };
       bool here = a.kb > 0 && tile < m.mt && cblk < cols;        // the first block of columns
       if (PARTS == 2) {
@@ -783,13 +888,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
       if (lane == 0 && a.kb > 0 && !(a.phase == kApply && a.step + 1 == p.steps)) {
         bulk_wait_all();
         asm volatile("fence.proxy.async;" ::: "memory");
-        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.done + a.item) : "memory");
+        unsigned* count = BN == 256 || a.adds ? p.done + a.item : p.shared + a.item * kMaxShared + a.tile;
+        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(count) : "memory");
       }
       __syncwarp();
     }
     if (lane == 0) {
       bulk_wait_all();
-      if (dead) mbar_wait(in, in_phase);         // no copy is on its way into the buffer
+      if (BN == 128 && dead) mbar_wait(in, in_phase);         // no copy is on its way into the buffer
     }
     __syncwarp();
   }
@@ -1089,6 +1195,15 @@ int check_items(const fo_matrix_update* m, int count, int dtype) {
   }
   return FO_OK;
 }
+// How many units share one of A's sums at most, and what they leave.
+constexpr int kMaxSplit = 8;
+int64_t tiles_of(int mt) { return int64_t((mt + 1) / 2) * ((mt + 1) / 2 + 1); }
+int most_split(int mt, int nt) {
+  const int64_t tiles = tiles_of(mt), most = (152 + tiles - 1) / tiles, want = (2 * nt + 7) / 8;
+  return tiles > kMaxShared ? 1 : int(std::min<int64_t>(std::min(most, want), kMaxSplit));
+}
+int64_t shared_bytes(int mt, int nt) { return tiles_of(mt) * (most_split(mt, nt) - 1) * 16 * 8192; }
+
 bool is_small(const fo_matrix_update& m) {
   const int64_t lo = m.rows < m.cols ? m.rows : m.cols, hi = m.rows < m.cols ? m.cols : m.rows;
   return lo <= kSmallRows && hi <= kSmallCols * kSmallCtas;
@@ -1098,13 +1213,13 @@ int64_t item_bytes(const fo_matrix_update& m, int parts) {
   if (m.rows == 0 || m.cols == 0) return 0;
   if (is_small(m)) return 2 * kSmallCtas * kSmallPart + 256;
   const int64_t r = (m.rows + 127) / 128, c = (m.cols + 127) / 128, mt = r < c ? r : c, nt = r < c ? c : r;
-  return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + kMaxSums * 16 + 16;
+  return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + shared_bytes(int(mt), int(nt)) + kMaxSums * 16 + kMaxShared * 4 + 16;
 }
 
 // Units of each matrix in one of the products, those with the longest sums first.
 template <int PHASE, int BN>
 int64_t plan(OrthoParams& p) {
-  auto length = [&p](int i) { return PHASE == kGram ? p.item[i].nt : p.item[i].mt; };
+  auto length = [&p](int i) { return PHASE == kGram ? (p.item[i].nt + p.item[i].split - 1) / p.item[i].split : p.item[i].mt; };
   uint8_t* order = p.order[PHASE];
   for (int i = 0; i < p.count; ++i) {
     int at = i;
@@ -1117,10 +1232,25 @@ int64_t plan(OrthoParams& p) {
     const Item& m = p.item[order[i]];
     const int64_t h = (m.mt + 1) / 2;
     if (PHASE == kApply) units += h * (BN == 256 ? (m.nt + 1) / 2 : m.nt);
-    else units += h * (h + 1) / 2 * (256 / BN);
+    else units += h * (h + 1) / 2 * (256 / BN) * (PHASE == kGram ? m.split : 1);
   }
   p.start[PHASE][p.count] = int(units);
   return units;
+}
+
+// How many units share one of A's sums: a sum of X X^T has the larger side's terms,
+// and few tiles; shared by units of 8 blocks of 64 terms, or of an equal part of
+// all where that is longer, the longest chain of a step is as long as the others
+// (2048 x 512: SHARE).
+void share_sums(OrthoParams& p) {
+  int64_t all = 0;
+  for (int i = 0; i < p.count; ++i) all += tiles_of(p.item[i].mt) * 2 * p.item[i].nt;
+  const int64_t part = all / 76 > 8 ? all / 76 : 8;
+  for (int i = 0; i < p.count; ++i) {
+    const int64_t want = (2 * p.item[i].nt + part - 1) / part;
+    const int most = most_split(p.item[i].mt, p.item[i].nt);
+    p.item[i].split = int(want < most ? want : most);
+  }
 }
 
 template <int PARTS, int BN, typename T>
@@ -1130,6 +1260,9 @@ cudaError_t launch_steps(OrthoParams& p, int dev, cudaStream_t st) {
   static std::atomic<int> resident[kMaxDevices];      // pairs that run at the same time
   cudaError_t e = allow_smem(k, allowed);
   if (e != cudaSuccess) return e;
+  // without wide tiles' numbers of units, a long sum's terms are shared
+  for (int i = 0; i < p.count; ++i) p.item[i].split = 1;
+  if (BN == 128) share_sums(p);
   const int64_t units = plan<kGram, BN>(p) + plan<kPoly, BN>(p) + plan<kApply, BN>(p);
   if (units * p.steps >= int64_t(1) << 31) return cudaErrorInvalidValue;      // sides are limited: not reached
   cudaLaunchConfig_t cfg = {};
@@ -1284,6 +1417,7 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
         for (int k = 0; k < 2; ++k) it.x[k] = take(int64_t(it.mt) * it.nt * 4 * kBlock * 2);
         it.a = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
         it.c = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
+        it.parts = take(shared_bytes(it.mt, it.nt));
       }
       const int64_t per = dtype == FO_DTYPE_F32 ? 4 : 8;
       it.vec_in = aligned16(m.grad) && (m.rows == 1 || m.grad_stride % per == 0) &&
@@ -1297,6 +1431,7 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
     p.sums = reinterpret_cast<float4*>(p.ws + at);
     p.scale = reinterpret_cast<float2*>(p.sums + p.count * kMaxSums);
     p.done = reinterpret_cast<unsigned*>(p.scale + p.count);
+    p.shared = p.done + p.count;
     const cudaError_t e = small ? (dtype == FO_DTYPE_F32 ? orthogonalize_small<float>(p, st) : orthogonalize_small<bf16>(p, st))
                           : dtype == FO_DTYPE_F32 ? orthogonalize<float>(p, st) : orthogonalize<bf16>(p, st);
     if (e != cudaSuccess) return done(e);
