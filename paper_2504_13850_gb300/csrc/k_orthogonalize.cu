@@ -53,7 +53,6 @@ __device__ GaveUp g_err;
 constexpr int kItems = 32;                    // matrices per launch
 constexpr int kBlock = 8192;                  // bytes of a 64 x 64 block
 constexpr int kMaxSums = 1024;                // partial sums of squares per matrix
-constexpr int kMaxShared = 64;                // tiles of A whose sums are shared, per matrix
 constexpr float kUpX = 1024.f, kUpA = 256.f;  // what X, and A and C, are multiplied by as fp16
 
 struct Item {
@@ -62,33 +61,28 @@ struct Item {
   void* out;
   int64_t ldg, ldm, ldp, ldo;
   int64_t x[2], a, c;       // byte offsets in the workspace
-  int64_t parts;            // of A's sums that are shared, [tile][split][CTA][warp] of 8 KB
+  int64_t parts;            // of A's shared sums, [tile][split - 1][CTA][warp] of 8 KB
   int rows, cols, mt, nt;   // mt, nt: tiles of 128 of the smaller and the larger side
   int nsums;                // partial sums of squares, at kMaxSums times its index
-  int split;                // units that share one of A's sums
   bool transposed, vec_in, vec_out;
   float step;
 };
 struct OrthoParams {
   Item item[kItems];
-  // First unit of work of each matrix: before the steps in start[0], then in each
-  // product; the matrices in the order of their units.
-  int start[3][kItems + 1];
-  uint8_t order[3][kItems];
+  int start[kItems + 1];    // first unit of work of each matrix in this launch
+  uint8_t order[kItems];    // the matrices in the order of their units
   char* ws;
   float4* sums;
   float2* scale;            // of each matrix: the two factors that make X of U
-  unsigned* done;           // of each matrix: how many of its units' warps are done, over all steps
-  unsigned* shared;         // the same of each tile of A whose sums are shared, kMaxShared for each matrix
-  int count, steps;
+  int count, from, last;    // from: which X is read; last: X goes to the caller
   float ca, cb, cc, mu, decay;
   bool nesterov;
   float eps;
 };
 
-__device__ __forceinline__ int slot_of(const OrthoParams& p, int unit, int which = 0) {
+__device__ __forceinline__ int slot_of(const OrthoParams& p, int unit) {
   int n = 0;
-  while (n + 1 < p.count && unit >= p.start[which][n + 1]) ++n;
+  while (n + 1 < p.count && unit >= p.start[n + 1]) ++n;
   return n;
 }
 
@@ -181,7 +175,7 @@ __global__ void __launch_bounds__(256) ortho_sums_k(const __grid_constant__ Orth
   __shared__ float4 box[8];
   pdl_wait();
   pdl_trigger();
-  const int n = slot_of(p, blockIdx.x), part = int(blockIdx.x) - p.start[0][n];
+  const int n = slot_of(p, blockIdx.x), part = int(blockIdx.x) - p.start[n];
   const Item& it = p.item[n];
   const uint32_t per_row = uint32_t(it.cols + 7) / 8;               // vectors of eight
   const int64_t total = int64_t(it.rows) * per_row, stride = int64_t(it.nsums) * 256;
@@ -240,9 +234,7 @@ __global__ void __launch_bounds__(256) ortho_scale_k(const __grid_constant__ Ort
     int unit;
     const float root = sum.root(unit);
     p.scale[n] = factors(root, unit, p.eps);
-    p.done[n] = 0;
   }
-  if (threadIdx.x < kMaxShared) p.shared[n * kMaxShared + threadIdx.x] = 0;
 }
 
 __device__ __forceinline__ uint32_t half_pair(float a, float b) {
@@ -273,7 +265,7 @@ __global__ void __launch_bounds__(256) ortho_pack_k(const __grid_constant__ Orth
   pdl_trigger();
   const int n = slot_of(p, blockIdx.x);
   const Item& it = p.item[n];
-  const int blk = int(blockIdx.x) - p.start[0][n], rows = 2 * it.mt;
+  const int blk = int(blockIdx.x) - p.start[n], rows = 2 * it.mt;
   const int rb = blk % rows, cb = blk / rows, t = threadIdx.x, row = t / 4;
   // the user's matrix: two groups of eight of one row
   const int r0 = 64 * (it.transposed ? cb : rb), c0 = 64 * (it.transposed ? rb : cb);
@@ -309,10 +301,8 @@ constexpr int kThreads = 320;                 // copies, products, eight warps o
 template <int PARTS, int BN>
 struct Tiles {
   static constexpr int kA = 2 * kBlock, kB = BN / 128 * kBlock;
-  // Of 32 x 64 elements per warp of arithmetic: both parts, or with wide tiles,
-  // which want the room for copies in flight, one.
-  static constexpr int kBuffer = BN == 256 ? 4096 : 8192, kOut = 8 * kBuffer;
-  static constexpr int kStage = PARTS * (kA + kB), kStages = (229376 - kOut) / kStage;
+  static constexpr int kStage = PARTS * (kA + kB), kStages = 196608 / kStage;
+  static constexpr int kOut = 8 * 4096;       // 4 KB per warp of arithmetic
   static constexpr int kSumsAt = 512 / BN;    // tiles' sums in tensor memory
   static constexpr int kBars = 3 * kStages + 2 * kSumsAt + 9;
   static constexpr int kSmem = 1024 + kStages * kStage + kOut + 8 * kBars + 16;
@@ -320,38 +310,21 @@ struct Tiles {
 static_assert(Tiles<1, 256>::kSmem <= 232448 && Tiles<1, 128>::kSmem <= 232448 && Tiles<2, 128>::kSmem <= 232448, "shared memory per CTA");
 
 struct Place {
-  int item, phase, step;
-  int i, j, kb;             // rows 256 i, columns BN j, blocks of 64 terms (none: nothing to do)
-  int k0, split, tile;      // its first block; which of the units that share a sum; the tile's number
-  bool adds;                // it has the last of the shared terms and adds the others' sums, or is alone
-  unsigned need;            // warps of this matrix that are done with what this unit reads
+  int item, tile;           // the tile's number among the matrix's
+  int i, j;                 // rows 256 i, columns BN j
+  int k0, kb;               // first block of 64 terms, and how many (none: nothing to do)
 };
-template <int BN>
-__device__ __forceinline__ Place place_of(const OrthoParams& p, int unit) {
+// `share` of `shares` of the terms.
+template <int PHASE, int BN>
+__device__ __forceinline__ Place place_of(const OrthoParams& p, int unit, int share, int shares) {
   Place a;
-  const int n0 = p.start[kGram][p.count], n1 = p.start[kPoly][p.count], n2 = p.start[kApply][p.count];
-  a.step = unit / (n0 + n1 + n2);
-  int t = unit - a.step * (n0 + n1 + n2);
-  a.phase = t < n0 ? kGram : t < n0 + n1 ? kPoly : kApply;
-  t -= a.phase == kGram ? 0 : a.phase == kPoly ? n0 : n0 + n1;
-  const int n = slot_of(p, t, a.phase);
-  a.item = p.order[a.phase][n];
+  const int n = slot_of(p, unit);
+  a.item = p.order[n];
   const Item& it = p.item[a.item];
-  t -= p.start[a.phase][n];
-  const int h = (it.mt + 1) / 2, cols = a.phase == kApply ? it.nt : it.mt;
-  // units that have something to do (an odd last column's second half has not)
-  const unsigned triangle = BN == 256 ? h * (h + 1) / 2 : h * (h + 1) - (it.mt & 1 ? h : 0);
-  const unsigned all = 2 * triangle + h * ((it.nt + BN / 128 - 1) / (BN / 128));
-  a.need = 16 * (a.step * all + a.phase * triangle);
-  a.k0 = a.split = 0;
-  a.adds = true;
-  if (a.phase == kGram) {
-    a.split = t % it.split;
-    t /= it.split;
-    a.adds = a.split + 1 == it.split;
-  }
+  const int t = unit - p.start[n];
   a.tile = t;
-  if (a.phase == kApply) {
+  const int h = (it.mt + 1) / 2, cols = PHASE == kApply ? it.nt : it.mt;
+  if (PHASE == kApply) {
     a.i = t % h;
     a.j = t / h;
   } else {                  // 256 x 256 on and above the diagonal, column by column
@@ -362,29 +335,10 @@ __device__ __forceinline__ Place place_of(const OrthoParams& p, int unit) {
     a.i = u - j * (j + 1) / 2;
     a.j = BN == 256 ? j : 2 * j + t % 2;
   }
-  a.kb = a.j * (BN / 128) < cols ? 2 * (a.phase == kGram ? it.nt : it.mt) : 0;
-  if (a.phase == kGram && it.split > 1) {
-    a.k0 = a.kb * a.split / it.split;
-    a.kb = a.kb * (a.split + 1) / it.split - a.k0;
-  }
+  const int all = a.j * (BN / 128) < cols ? 2 * (PHASE == kGram ? it.nt : it.mt) : 0;
+  a.k0 = all * share / shares;
+  a.kb = all * (share + 1) / shares - a.k0;
   return a;
-}
-// Before copies of what other blocks have stored: `need` of their warps have said so.
-__device__ __forceinline__ void wait_for(Waits& w, const unsigned* done, unsigned need, int code) {
-  if (w.dead || need == 0) return;
-  const uint64_t t0 = global_ns();
-  while (true) {
-    for (int i = 0; i < 64; ++i) {
-      unsigned now;
-      asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(now) : "l"(done) : "memory");
-      if (now >= need) {
-        asm volatile("fence.proxy.async;" ::: "memory");
-        return;
-      }
-    }
-    if (global_ns() - t0 > w.limit) break;
-  }
-  w.give_up(code);
 }
 // A symmetric matrix holds its 128 x 128 tiles (i, j) with i / 2 <= j / 2.  Rows
 // 128 i .. of block column kb lie there as rows, or mirrored, as columns of block
@@ -396,10 +350,11 @@ __device__ __forceinline__ bool mirrored(int i, int kb) { return i / 2 > kb / 4;
 // took 1 us (4096 x 4096: 2361 us).  Copies are plain ones to this CTA's barrier,
 // of which a warp tells the leader; tensor copies that complete on the leader's
 // barrier themselves were 10% slower on 256 x 256 tiles (rows of 128 bytes).
-__device__ __forceinline__ void arrive_leader(uint64_t* bar) {
+__device__ __forceinline__ void arrive_at(uint64_t* bar, uint32_t rank) {
   asm volatile(
-      "{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, 0;\n mbarrier.arrive.shared::cluster.b64 _, [r];\n}\n" ::"r"(
-          smem_u32(bar))
+      "{\n .reg .b32 r;\n mapa.shared::cluster.u32 r, %0, %1;\n mbarrier.arrive.shared::cluster.b64 _, [r];\n}\n" ::"r"(
+          smem_u32(bar)),
+      "r"(rank)
       : "memory");
 }
 __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
@@ -409,11 +364,11 @@ __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uin
       "l"(a), "l"(b), "r"(idesc), "r"(acc)
       : "memory");
 }
-__device__ __forceinline__ void commit_pair(uint64_t* bar) {     // the barrier of both CTAs
+__device__ __forceinline__ void commit_pair(uint64_t* bar, uint32_t leader) {     // the barrier of both CTAs
   asm volatile(
       "{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n"
       " @q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}\n" ::"r"(smem_u32(bar)),
-      "h"(uint16_t(3))
+      "h"(uint16_t(3u << leader))
       : "memory");
 }
 
@@ -473,109 +428,60 @@ __device__ __forceinline__ void deliver(const OrthoParams& p, const Item& m, int
   __syncwarp();
 }
 
-// A warp's 32 rows of a block of A, C or X: 4 KB per part, in the block's order.
-__device__ __forceinline__ int64_t rows_at(const Item& m, int tile, int cblk, int q) {
-  return (int64_t(cblk) * 2 * m.mt + 2 * tile + q / 2) * kBlock + (q & 1) * 4096;
+// Several pairs of a cluster share a tile's terms: the others leave their sums in
+// the workspace, and the first adds them in their order.  Every lane its own, 16
+// bytes beside its neighbours'.
+__device__ __forceinline__ float4* shared_at(const OrthoParams& p, const Item& m, int tile, int share, int shares, int me, int warp) {
+  return reinterpret_cast<float4*>(p.ws + m.parts + (((int64_t(tile) * (shares - 1) + share - 1) * 2 + me) * 8 + warp) * 8192);
 }
-// What the sums of these rows are added to (A or X) is on its way into the warp's
-// buffer while the products run.
-template <int PARTS, int BN, int PHASE>
-__device__ __forceinline__ void fetch(const OrthoParams& p, const Item& m, int step, int tile, int cblk, int q, int lane, char* buf, uint64_t* bar) {
-  if (BN == 256 || PHASE == kGram || lane != 0) return;
-  const char* src = p.ws + (PHASE == kPoly ? m.a : m.x[step & 1]) + rows_at(m, tile, cblk, q);
-  constexpr int kParts = PHASE == kPoly ? PARTS : 2;
-  bulk_wait_read<0>();                // the last stores have read the buffer
-  mbar_expect_tx(bar, kParts * 4096);
+__device__ __forceinline__ void leave_sums(float4* to, int lane, const float (&v)[64]) {
 #pragma unroll
-  for (int part = 0; part < kParts; ++part)
-    bulk_g2s(buf + part * 4096, src + part * (int64_t(m.mt) * (PHASE == kPoly ? m.mt : m.nt) * 4 * kBlock), 4096, bar);
+  for (int k = 0; k < 16; ++k) __stcg(to + 32 * k + lane, make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]));
 }
-
-// One of the units that share a tile's sums leaves its own in the workspace, and
-// the last adds the others' in their order: 32 columns at a time of the warp's 32
-// rows (4 KB), every lane its own.
-__device__ __forceinline__ char* shared_at(const OrthoParams& p, const Item& m, const Place& a, int split, int me, int warp) {
-  return p.ws + m.parts + (((int64_t(a.tile) * (m.split - 1) + split) * 2 + me) * 8 + warp) * 8192;
-}
-__device__ __forceinline__ void leave_sums(const OrthoParams& p, const Item& m, const Place& a, int me, int warp, int lane, char* buf, float (&v)[64]) {
-  const uint32_t mine = smem_u32(buf) + lane * 16;
-  char* dst = shared_at(p, m, a, a.split, me, warp);
+__device__ __forceinline__ void add_sums(const float4* from, int lane, float (&v)[64]) {
+  float4 w[16];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if (lane == 0) bulk_wait_read<0>();
-    __syncwarp();
+  for (int k = 0; k < 16; ++k) w[k] = __ldcg(from + 32 * k + lane);
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      st_shared4(mine + k * 512, __float_as_uint(v[32 * h + 4 * k]), __float_as_uint(v[32 * h + 4 * k + 1]), __float_as_uint(v[32 * h + 4 * k + 2]),
-                 __float_as_uint(v[32 * h + 4 * k + 3]));
-    fence_proxy_async_smem();
-    __syncwarp();
-    if (lane == 0) {
-      asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 4096;" ::"l"(dst + h * 4096), "r"(smem_u32(buf)) : "memory");
-      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-    }
+  for (int k = 0; k < 16; ++k) {
+    v[4 * k] += w[k].x;
+    v[4 * k + 1] += w[k].y;
+    v[4 * k + 2] += w[k].z;
+    v[4 * k + 3] += w[k].w;
   }
-}
-__device__ __forceinline__ void add_sums(const OrthoParams& p, const Item& m, const Place& a, int me, int warp, int lane, float (&v)[64]) {
-  float own[64];
-#pragma unroll
-  for (int e = 0; e < 64; ++e) own[e] = 0.f;
-  for (int s = 0; s + 1 < m.split; ++s) {
-    const float4* src = reinterpret_cast<const float4*>(shared_at(p, m, a, s, me, warp)) + lane;
-    float4 w[16];
-#pragma unroll
-    for (int k = 0; k < 16; ++k) w[k] = __ldcg(src + 32 * k);
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-      own[4 * k] += w[k].x;
-      own[4 * k + 1] += w[k].y;
-      own[4 * k + 2] += w[k].z;
-      own[4 * k + 3] += w[k].w;
-    }
-  }
-#pragma unroll
-  for (int e = 0; e < 64; ++e) v[e] += own[e];
 }
 
 // 64 sums of one row, columns 64 cblk .., become elements of A, C or X.
-template <int PARTS, int BN, int PHASE, typename T>
-__device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int step, int tile, int cblk, int q, int lane, char* buf_ptr, uint64_t* bar,
-                                       uint32_t& phase, Waits& wait, float (&v)[64]) {
-  const uint32_t buf = smem_u32(buf_ptr), mine = buf + lane * 128;       // a lane reads and writes its own row
+template <int PARTS, int PHASE, typename T>
+__device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int tile, int cblk, int q, int lane, uint32_t buf, float (&v)[64]) {
+  const int64_t block = int64_t(cblk) * 2 * m.mt + 2 * tile + q / 2;
+  const int64_t half_block = block * kBlock + (q & 1) * 4096;       // this warp's 32 rows
+  const int64_t xi = int64_t(m.mt) * m.nt * 4 * kBlock, si = int64_t(m.mt) * m.mt * 4 * kBlock;
   if (PHASE == kGram) {
 #pragma unroll
     for (int e = 0; e < 64; ++e) v[e] *= kUpA / (kUpX * kUpX);
-    if (lane == 0) bulk_wait_read<0>();       // the last stores have read the buffer
-    __syncwarp();
   } else {
     // C = b A + c A A, or a X + C X
     const float linear = PHASE == kPoly ? p.cb : p.ca, other = (PHASE == kPoly ? p.cc : 1.f) / kUpA;
+    // the warp's 4 KB are read as they lie, and handed out by rows through shared memory
+    const uint4* src = reinterpret_cast<const uint4*>(p.ws + (PHASE == kPoly ? m.a : m.x[p.from]) + half_block) + lane;
     constexpr int kParts = PHASE == kPoly ? PARTS : 2;
-    uint4 w[BN == 256 ? kParts : 1][8];
-    if (BN == 256) {          // the warp's 4 KB are read as they lie, past L1, which may hold an older step's
-      const uint4* src = reinterpret_cast<const uint4*>(p.ws + (PHASE == kPoly ? m.a : m.x[step & 1]) + rows_at(m, tile, cblk, q)) + lane;
+    const int64_t image = (PHASE == kPoly ? si : xi) / 16;
+    uint4 w[kParts][8];
 #pragma unroll
-      for (int part = 0; part < kParts; ++part)
+    for (int part = 0; part < kParts; ++part)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) w[part][k] = __ldcg(src + part * (int64_t(m.mt) * (PHASE == kPoly ? m.mt : m.nt) * 4 * kBlock / 16) + 32 * k);
-      if (lane == 0) bulk_wait_read<0>();       // the last stores have read the buffer
-    } else {
-      wait.on_lanes(bar, phase, 69);
-      phase ^= 1;
-    }
+      for (int k = 0; k < 8; ++k) w[part][k] = src[part * image + 32 * k];
+    if (lane == 0) bulk_wait_read<0>();       // the last store has read the buffer
 #pragma unroll
     for (int part = kParts - 1; part >= 0; --part) {
-      if (BN == 256) {        // and handed out by rows
-        __syncwarp();
+      __syncwarp();
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-          st_shared4(buf + (32 * k + lane) * 16, w[BN == 256 ? part : 0][k].x, w[BN == 256 ? part : 0][k].y, w[BN == 256 ? part : 0][k].z,
-                     w[BN == 256 ? part : 0][k].w);
-        __syncwarp();
-      }
+      for (int k = 0; k < 8; ++k) st_shared4(buf + (32 * k + lane) * 16, w[part][k].x, w[part][k].y, w[part][k].z, w[part][k].w);
+      __syncwarp();
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const float4 u = ld_shared4(mine + (BN == 256 ? 0 : part * 4096) + (k ^ (lane & 7)) * 16);
+        const float4 u = ld_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16);
         const float z[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -586,66 +492,48 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
         }
       }
     }
-    if (BN == 256) __syncwarp();
+    __syncwarp();
   }
-  if (PHASE == kApply && step + 1 == p.steps) {
+  if (PHASE == kApply && p.last) {
     deliver<T>(p, m, tile, 64 * cblk, q, lane, buf, v);
     deliver<T>(p, m, tile, 64 * cblk + 32, q, lane, buf, v + 32);
-    fence_proxy_async_smem();                 // before the next copy into the buffer
-    __syncwarp();
     return;
   }
-  constexpr int kParts = PHASE == kApply ? 2 : PARTS;
-  char* dst = p.ws + (PHASE == kGram ? m.a : PHASE == kPoly ? m.c : m.x[step & 1 ^ 1]) + rows_at(m, tile, cblk, q);
+  char* dst = p.ws + (PHASE == kGram ? m.a : PHASE == kPoly ? m.c : m.x[p.from ^ 1]) + half_block;
+  const int64_t image = PHASE == kApply ? xi : si;
 #pragma unroll
-  for (int part = 0; part < kParts; ++part) {
-    const uint32_t at = BN == 256 ? 0 : part * 4096;
-    if (BN == 256 && part > 0) {
-      if (lane == 0) bulk_wait_read<0>();
-      __syncwarp();
-    }
+  for (int part = 0; part < (PHASE == kApply ? 2 : PARTS); ++part) {
+    if (lane == 0) bulk_wait_read<0>();       // the last store has read the buffer
+    __syncwarp();
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       const uint4 w = take_half8(v + 8 * k);
-      st_shared4(mine + at + (k ^ (lane & 7)) * 16, w.x, w.y, w.z, w.w);
+      st_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16, w.x, w.y, w.z, w.w);
     }
-    if (BN == 256 || part + 1 == kParts) {
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-#pragma unroll
-        for (int o = BN == 256 ? part : 0; o <= part; ++o)
-          asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 4096;" ::"l"(
-                           dst + o * (int64_t(m.mt) * (PHASE == kApply ? m.nt : m.mt) * 4 * kBlock)),
-                       "r"(buf + (BN == 256 ? 0 : o * 4096))
-                       : "memory");
-        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-      }
+    fence_proxy_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], 4096;" ::"l"(dst + part * image), "r"(buf) : "memory");
+      asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     }
   }
 }
 
-// All steps of all matrices in one launch.  Units of work (a tile of one of the
-// three products of a step of a matrix) have an order, and pairs take them in
-// turn; a unit's copies start when the units of the matrix before it are done,
-// which every warp that has stored its part says in the matrix's counter.  So
-// the products of one matrix fill the gaps of another's, and between two products
-// of one lie 2 us instead of a launch's 7 (its blocks fill an SM's shared memory,
-// so they cannot start while the last launch's run).  Units wait for earlier ones
-// only and all blocks run at the same time (a cooperative launch).
-template <int PARTS, int BN, typename T>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_steps_k(const __grid_constant__ OrthoParams p) {
+template <int PARTS, int BN, int PHASE, bool SHARED, typename T>
+__device__ __forceinline__ void product_tiles(const OrthoParams& p, int pairs_of_tile) {
   using S = Tiles<PARTS, BN>;
   extern __shared__ char smem_raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   char* stage_out = smem + S::kStages * S::kStage;
   uint64_t* full = reinterpret_cast<uint64_t*>(stage_out + S::kOut);
   uint64_t *peer = full + S::kStages, *empty = peer + S::kStages, *acc_full = empty + S::kStages, *acc_empty = acc_full + S::kSumsAt,
-           *done = acc_empty + S::kSumsAt, *fetched = done + 1;
-  uint32_t* tslot = reinterpret_cast<uint32_t*>(fetched + 8);
+           *done = acc_empty + S::kSumsAt, *left = done + 1;       // left: a warp's sums of the cluster's other pairs
+  uint32_t* tslot = reinterpret_cast<uint32_t*>(left + 8);
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  const int units = p.steps * (p.start[kGram][p.count] + p.start[kPoly][p.count] + p.start[kApply][p.count]);
-  const int pair = int(blockIdx.x) / 2, pairs = int(gridDim.x) / 2, me = int(blockIdx.x) % 2;
+  // a cluster of 2 * shares CTAs takes a tile
+  const int shares = SHARED ? pairs_of_tile : 1;
+  const int units = p.start[p.count], pair = int(blockIdx.x) / (2 * shares), pairs = int(gridDim.x) / (2 * shares);
+  const int rank = int(blockIdx.x) % (2 * shares), me = rank % 2, leader = rank - me, share = rank / 2;
 
   if (threadIdx.x == 0) {
     for (int e = 0; e < S::kStages; ++e) {
@@ -658,7 +546,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
       mbar_init(&acc_empty[e], 16);        // one arrival per warp of arithmetic, of both CTAs
     }
     mbar_init(done, 1);
-    for (int e = 0; e < 8; ++e) mbar_init(&fetched[e], 1);
+    for (int e = 0; e < 8; ++e) mbar_init(&left[e], shares > 1 ? shares - 1 : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -671,6 +559,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
   cluster_sync_all();                // both CTAs' barriers are there
   tc_fence_after();
   const uint32_t tmem = *tslot;      // sum s: columns BN s
+  pdl_trigger();                     // this block holds its tensor memory
+  pdl_wait();
   Waits wait(&g_err);
 
   if (warp == 0) {
@@ -678,17 +568,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
       Ring<S::kStages> at;
       int it = 0;
       for (int u = pair; u < units && !wait.dead; u += pairs) {
-        const Place a = place_of<BN>(p, u);
+        const Place a = place_of<PHASE, BN>(p, u, share, shares);
         const Item& m = p.item[a.item];
-        const char* x = p.ws + m.x[a.step & 1];
-        const char* sym = p.ws + (a.phase == kPoly ? m.a : m.c);
+        const char* x = p.ws + m.x[p.from];
+        const char* sym = p.ws + (PHASE == kPoly ? m.a : m.c);
         const int64_t xi = int64_t(m.mt) * m.nt * 4 * kBlock, si = int64_t(m.mt) * m.mt * 4 * kBlock;
-        const int cols = a.phase == kApply ? m.nt : m.mt;     // tiles of 128
+        const int cols = PHASE == kApply ? m.nt : m.mt;       // tiles of 128
         const int ta = 2 * a.i + me, tb = BN == 256 ? 2 * a.j + me : a.j;
         const bool has_a = ta < m.mt, has_b = tb < cols;
         const uint32_t bytes = PARTS * ((has_a ? S::kA : 0) + (has_b ? S::kB : 0));
         const int64_t wide = int64_t(2 * m.mt) * kBlock;      // from one block column to the next
-        if (a.kb) wait_for(wait, p.done + a.item, a.need, 60);
         for (int kb = a.k0; kb < a.k0 + a.kb; ++kb, ++it) {
           if (it >= S::kStages) wait.on(&empty[at.at], at.phase ^ 1, 61);
           if (wait.dead) break;
@@ -699,8 +588,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
           for (int q = 0; q < PARTS; ++q) {
             if (has_a) {
               char* d = s + q * S::kA;
-              const char* src = a.phase == kGram ? x + q * xi : sym + q * si;
-              if (a.phase == kGram || !mirrored(ta, kb)) {
+              const char* src = PHASE == kGram ? x + q * xi : sym + q * si;
+              if (PHASE == kGram || !mirrored(ta, kb)) {
                 bulk_g2s(d, src + kb * wide + int64_t(2 * ta) * kBlock, 2 * kBlock, bar);
               } else {
                 src += 2 * ta * wide + int64_t(kb) * kBlock;
@@ -710,9 +599,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
             }
             if (has_b) {
               char* d = s + PARTS * S::kA + q * S::kB;
-              const char* src = a.phase == kPoly ? sym + q * si : x + q * xi;
+              const char* src = PHASE == kPoly ? sym + q * si : x + q * xi;
               const int b0 = BN == 256 ? 2 * tb : 2 * tb + me;          // this CTA's first block
-              if (a.phase == kGram || (a.phase == kPoly && !mirrored(tb, kb))) {
+              if (PHASE == kGram || (PHASE == kPoly && !mirrored(tb, kb))) {
                 bulk_g2s(d, src + kb * wide + int64_t(b0) * kBlock, S::kB, bar);
               } else {
                 src += b0 * wide + int64_t(kb) * kBlock;
@@ -732,11 +621,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
     if (lane == 0) {
       Ring<S::kStages> at;
       for (int u = pair; u < units && !wait.dead; u += pairs) {
-        const Place a = place_of<BN>(p, u);
+        const Place a = place_of<PHASE, BN>(p, u, share, shares);
         for (int kb = 0; kb < a.kb; ++kb) {
           wait.on(&full[at.at], at.phase, 65);
           if (wait.dead) break;
-          arrive_leader(&peer[at.at]);
+          arrive_at(&peer[at.at], leader);
           at.step();
         }
       }
@@ -750,7 +639,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
     const uint32_t ring = smem_u32(smem);
     bool dead = false;
     for (int u = pair; u < units && !dead; u += pairs) {
-      const Place a = place_of<BN>(p, u);
+      const Place a = place_of<PHASE, BN>(p, u, share, shares);
       const int tb = BN == 256 ? 2 * a.j : a.j;
       for (int kb = 0; kb < a.kb; ++kb) {
         const uint32_t d = tmem + sum.at * BN;
@@ -762,7 +651,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
         tc_fence_after();
         const uint32_t s = ring + at.at * S::kStage;
         // mirrored operands have their rows along the terms
-        const uint32_t am = a.phase != kGram && mirrored(2 * a.i, kb), bm = a.phase == kApply || (a.phase == kPoly && mirrored(tb, kb));
+        const uint32_t am = PHASE != kGram && mirrored(2 * a.i, kb), bm = PHASE == kApply || (PHASE == kPoly && mirrored(tb, kb));
         const uint32_t idesc = id | am << 15 | bm << 16;
         const uint32_t as = am ? 2048u : 32u, bs = bm ? 2048u : 32u;
         const uint32_t al = (am ? uint32_t(kBlock) : 16u) >> 4 << 16, bl = (bm ? uint32_t(kBlock) : 16u) >> 4 << 16;
@@ -779,10 +668,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
 #pragma unroll
         for (int k = 0; k < 4; ++k)
           mma_pair(d, desc(k * as, al), desc(b0 + k * bs, bl), idesc, PARTS == 2 || kb > 0 || k > 0 ? 1u : 0u);
-        commit_pair(&empty[at.at]);
+        commit_pair(&empty[at.at], leader);
         at.step();
         if (PARTS == 2 || kb + 1 == a.kb) {
-          commit_pair(&acc_full[sum.at]);
+          commit_pair(&acc_full[sum.at], leader);
           sum.step();
         }
         // off the waits' path; what was issued after one gave up is void anyway
@@ -802,67 +691,65 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
     const int q = warp % 4, half = (warp - 2) / 4;
     constexpr int NB = BN / 128;
     const uint32_t col = tmem + (uint32_t(32 * q) << 16) + (BN / 2) * half;
-    char* buf = stage_out + (warp - 2) * S::kBuffer;
-    uint64_t* in = &fetched[warp - 2];
-    uint32_t in_phase = 0;
+    const uint32_t buf = smem_u32(stage_out) + uint32_t(warp - 2) * 4096u;
     Ring<S::kSumsAt> sum;
+    uint32_t turn = 0;
+    // before the end of a tile of which the cluster's pairs have shared the terms: whether this pair finishes it
+    auto shared = [&](const Item& m, int tile, float (&v)[64]) {
+      if (!SHARED) return true;
+      if (share > 0) {
+        leave_sums(shared_at(p, m, tile, share, shares, me, warp - 2), lane, v);
+        __syncwarp();
+        if (lane == 0) {
+          asm volatile("fence.acq_rel.cluster;" ::: "memory");
+          arrive_at(&left[warp - 2], me);
+        }
+        __syncwarp();
+        return false;
+      }
+      wait.on_lanes(&left[warp - 2], turn, 72);
+      turn ^= 1;
+      asm volatile("fence.acq_rel.cluster;" ::: "memory");
+      for (int s = 1; s < shares; ++s) add_sums(shared_at(p, m, tile, s, shares, me, warp - 2), lane, v);
+      return true;
+    };
     bool dead = false;
     for (int u = pair; u < units && !dead; u += pairs) {
-      const Place a = place_of<BN>(p, u);
+      const Place a = place_of<PHASE, BN>(p, u, share, shares);
+      if (a.kb == 0) continue;
       const Item& m = p.item[a.item];
-      const int tile = 2 * a.i + me, cblk = a.j * (BN / 64) + half * NB, cols = 2 * (a.phase == kApply ? m.nt : m.mt);
-      float v[64];
-      auto get = [&](int b) {
-        if (a.phase == kPoly) fetch<PARTS, BN, kPoly>(p, m, a.step, tile, cblk + b, q, lane, buf, in);
-        else fetch<PARTS, BN, kApply>(p, m, a.step, tile, cblk + b, q, lane, buf, in);
-      };
-      auto end = [&](int b) {
-        if (BN == 128 && a.phase == kGram && m.split > 1) {
-          if (!a.adds) {
-            leave_sums(p, m, a, me, warp - 2, lane, buf, v);
-            return;
-          }
-          if (lane == 0) wait_for(wait, p.shared + a.item * kMaxShared + a.tile, 16u * (m.split - 1) * (a.step + 1), 70);
-          __syncwarp();
-          add_sums(p, m, a, me, warp - 2, lane, v);
-        }
-        if (a.phase == kGram) finish<PARTS, BN, kGram, T>(p, m, a.step, tile, cblk + b, q, lane, buf, in, in_phase, wait, v);
-        else if (a.phase == kPoly) finish<PARTS, BN, kPoly, T>(p, m, a.step, tile, cblk + b, q, lane, buf, in, in_phase, wait, v);
-        else finish<PARTS, BN, kApply, T>(p, m, a.step, tile, cblk + b, q, lane, buf, in, in_phase, wait, v);
-      };
-      bool here = a.kb > 0 && tile < m.mt && cblk < cols;        // the first block of columns
+      const int tile = 2 * a.i + me, cblk = a.j * (BN / 64) + half * NB, cols = 2 * (PHASE == kApply ? m.nt : m.mt);
+      float v[PARTS == 2 ? NB : 1][64];
       if (PARTS == 2) {
         for (int kb = 0; kb < a.kb; ++kb) {
           wait.on(&acc_full[sum.at], sum.phase, 64);
           __syncwarp();
           tc_fence_after();
-          // the first sum tells that what the unit reads is there
-          if (kb == 0 && here && a.phase != kGram) get(0);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
+          for (int h = 0; h < 2 * NB; ++h) {
             uint32_t r[32];
             tmem_ld32(col + sum.at * BN + 32 * h, r);
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
-              float& x = v[32 * h + e];
+              float& x = v[h / 2][32 * (h % 2) + e];
               x = (kb > 0 ? x : 0.f) + __uint_as_float(r[e]);
             }
           }
           tc_fence_before();
           __syncwarp();
-          if (lane == 0) arrive_leader(&acc_empty[sum.at]);
+          if (lane == 0) arrive_at(&acc_empty[sum.at], leader);
           sum.step();
         }
         dead = __any_sync(0xffffffffu, wait.dead);
         if (dead) break;
-        static_assert(PARTS == 1 || NB == 1, "one block of columns");
-        if (here) end(0);
-      } else if (a.kb > 0) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          if (tile < m.mt && cblk + b < cols && shared(m, a.tile, v[b])) finish<PARTS, PHASE, T>(p, m, tile, cblk + b, q, lane, buf, v[b]);
+      } else {
         wait.on(&acc_full[sum.at], sum.phase, 64);
         __syncwarp();
         tc_fence_after();
         dead = __any_sync(0xffffffffu, wait.dead);
-        if (here && a.phase != kGram) get(0);
 #pragma unroll 1
         for (int b = 0; b < NB; ++b) {
 #pragma unroll
@@ -870,33 +757,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
             uint32_t r[32];
             tmem_ld32(col + sum.at * BN + 64 * b + 32 * h, r);
 #pragma unroll
-            for (int e = 0; e < 32; ++e) v[32 * h + e] = __uint_as_float(r[e]);
+            for (int e = 0; e < 32; ++e) v[0][32 * h + e] = __uint_as_float(r[e]);
           }
           if (b == NB - 1) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) arrive_leader(&acc_empty[sum.at]);
+            if (lane == 0) arrive_at(&acc_empty[sum.at], leader);
           }
-          if (dead || !here) continue;
-          end(b);
-          here = b + 1 < NB && cblk + b + 1 < cols;
-          if (here && a.phase != kGram) get(b + 1);
+          if (!dead && tile < m.mt && cblk + b < cols && shared(m, a.tile, v[0])) finish<PARTS, PHASE, T>(p, m, tile, cblk + b, q, lane, buf, v[0]);
         }
         sum.step();
       }
-      // this warp's part is stored: units that read it may start
-      if (lane == 0 && a.kb > 0 && !(a.phase == kApply && a.step + 1 == p.steps)) {
-        bulk_wait_all();
-        asm volatile("fence.proxy.async;" ::: "memory");
-        unsigned* count = BN == 256 || a.adds ? p.done + a.item : p.shared + a.item * kMaxShared + a.tile;
-        asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(count) : "memory");
-      }
-      __syncwarp();
     }
-    if (lane == 0) {
-      bulk_wait_all();
-      if (BN == 128 && dead) mbar_wait(in, in_phase);         // no copy is on its way into the buffer
-    }
+    if (lane == 0) bulk_wait_all();
     __syncwarp();
   }
   tc_fence_before();
@@ -906,6 +779,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_s
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
+}
+
+// Pairs, and clusters of `shares` pairs.
+template <int PARTS, int BN, int PHASE, typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1) ortho_product_k(const __grid_constant__ OrthoParams p) {
+  product_tiles<PARTS, BN, PHASE, false, T>(p, 1);
+}
+template <int PARTS, typename T>
+__global__ void __launch_bounds__(kThreads, 1) ortho_shared_k(const __grid_constant__ OrthoParams p, int shares) {
+  product_tiles<PARTS, 128, kGram, true, T>(p, shares);
 }
 
 // ------------------------------------------------------------ up to 128 rows
@@ -938,7 +821,7 @@ __device__ __forceinline__ void put_row(uint32_t at, uint32_t part, int row, int
 }
 
 template <int PARTS, typename T>
-__global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThreads, 1) ortho_small_k(const __grid_constant__ OrthoParams p) {
+__global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThreads, 1) ortho_small_k(const __grid_constant__ OrthoParams p, int steps) {
   extern __shared__ char smem_raw[];
   char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, t = threadIdx.x;
@@ -1100,7 +983,7 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
       for (int e = 0; e < 32; ++e) v[e] += __uint_as_float(r[e]);
     }
   };
-  for (int step = 0; step < p.steps; ++step) {
+  for (int step = 0; step < steps; ++step) {
     begin();
     if (warp == 0) {
       for (int c = 0; c < blocks; ++c) {
@@ -1169,7 +1052,7 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
             y = fmaf(p.ca, fh.y, fmaf(p.ca, fl.y, y * (1.f / kUpA)));
           }
         }
-        if (step + 1 < p.steps) put_row<2>(x_block, kSmallX, row, 4 * h, v);
+        if (step + 1 < steps) put_row<2>(x_block, kSmallX, row, 4 * h, v);
         else deliver<T>(p, m, 0, col0 + 64 * quarter + 32 * h, q, lane, sa + warp * 4096, v);
       }
     }
@@ -1195,14 +1078,12 @@ int check_items(const fo_matrix_update* m, int count, int dtype) {
   }
   return FO_OK;
 }
-// How many units share one of A's sums at most, and what they leave.
-constexpr int kMaxSplit = 8;
-int64_t tiles_of(int mt) { return int64_t((mt + 1) / 2) * ((mt + 1) / 2 + 1); }
-int most_split(int mt, int nt) {
-  const int64_t tiles = tiles_of(mt), most = (152 + tiles - 1) / tiles, want = (2 * nt + 7) / 8;
-  return tiles > kMaxShared ? 1 : int(std::min<int64_t>(std::min(most, want), kMaxSplit));
-}
-int64_t shared_bytes(int mt, int nt) { return tiles_of(mt) * (most_split(mt, nt) - 1) * 16 * 8192; }
+// How many pairs share one of A's sums at most (clusters of eight CTAs), and what
+// all but the first of them leave.
+constexpr int kMaxShares = 4;
+int64_t tiles_of(int64_t mt) { return (mt + 1) / 2 * ((mt + 1) / 2 + 1); }
+int most_shares(int64_t mt) { return tiles_of(mt) <= 38 ? kMaxShares : 1; }
+int64_t shared_bytes(int64_t mt) { return tiles_of(mt) * (most_shares(mt) - 1) * 16 * 8192; }
 
 bool is_small(const fo_matrix_update& m) {
   const int64_t lo = m.rows < m.cols ? m.rows : m.cols, hi = m.rows < m.cols ? m.cols : m.rows;
@@ -1213,118 +1094,132 @@ int64_t item_bytes(const fo_matrix_update& m, int parts) {
   if (m.rows == 0 || m.cols == 0) return 0;
   if (is_small(m)) return 2 * kSmallCtas * kSmallPart + 256;
   const int64_t r = (m.rows + 127) / 128, c = (m.cols + 127) / 128, mt = r < c ? r : c, nt = r < c ? c : r;
-  return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + shared_bytes(int(mt), int(nt)) + kMaxSums * 16 + kMaxShared * 4 + 16;
+  return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + shared_bytes(mt) + kMaxSums * 16 + 16;
 }
 
-// Units of each matrix in one of the products, those with the longest sums first.
+template <int PARTS, int BN, int PHASE, typename T>
+cudaError_t launch_product(const OrthoParams& p, int pairs, cudaStream_t st) {
+  auto k = ortho_product_k<PARTS, BN, PHASE, T>;
+  static std::atomic<bool> allowed[kMaxDevices];
+  const cudaError_t e = allow_smem(k, allowed);
+  if (e != cudaSuccess) return e;
+  const int units = p.start[p.count];
+  return launch_k(k, dim3(2 * unsigned(std::min(units, pairs))), dim3(kThreads), Tiles<PARTS, BN>::kSmem, st, p);
+}
+template <int PARTS, typename T>
+cudaError_t launch_shared(const OrthoParams& p, int shares, cudaStream_t st) {
+  auto k = ortho_shared_k<PARTS, T>;
+  static std::atomic<bool> allowed[kMaxDevices];
+  const cudaError_t e = allow_smem(k, allowed);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(2 * unsigned(shares * p.start[p.count]));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = Tiles<PARTS, 128>::kSmem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = unsigned(2 * shares);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, k, p, shares);
+}
+
+// Units of each matrix, those with the longest sums first.
 template <int PHASE, int BN>
 int64_t plan(OrthoParams& p) {
-  auto length = [&p](int i) { return PHASE == kGram ? (p.item[i].nt + p.item[i].split - 1) / p.item[i].split : p.item[i].mt; };
-  uint8_t* order = p.order[PHASE];
+  auto length = [&p](int i) { return PHASE == kGram ? p.item[i].nt : p.item[i].mt; };
   for (int i = 0; i < p.count; ++i) {
     int at = i;
-    for (; at > 0 && length(order[at - 1]) < length(i); --at) order[at] = order[at - 1];
-    order[at] = uint8_t(i);
+    for (; at > 0 && length(p.order[at - 1]) < length(i); --at) p.order[at] = p.order[at - 1];
+    p.order[at] = uint8_t(i);
   }
   int64_t units = 0;
   for (int i = 0; i < p.count; ++i) {
-    p.start[PHASE][i] = int(units);
-    const Item& m = p.item[order[i]];
+    p.start[i] = int(units);
+    const Item& m = p.item[p.order[i]];
     const int64_t h = (m.mt + 1) / 2;
     if (PHASE == kApply) units += h * (BN == 256 ? (m.nt + 1) / 2 : m.nt);
-    else units += h * (h + 1) / 2 * (256 / BN) * (PHASE == kGram ? m.split : 1);
+    else units += h * (h + 1) / 2 * (256 / BN);
   }
-  p.start[PHASE][p.count] = int(units);
+  p.start[p.count] = int(units);
   return units;
 }
 
-// How many units share one of A's sums: a sum of X X^T has the larger side's terms,
-// and few tiles; shared by units of 8 blocks of 64 terms, or of an equal part of
-// all where that is longer, the longest chain of a step is as long as the others
-// (2048 x 512: SHARE).
-void share_sums(OrthoParams& p) {
-  int64_t all = 0;
-  for (int i = 0; i < p.count; ++i) all += tiles_of(p.item[i].mt) * 2 * p.item[i].nt;
-  const int64_t part = all / 76 > 8 ? all / 76 : 8;
-  for (int i = 0; i < p.count; ++i) {
-    const int64_t want = (2 * p.item[i].nt + part - 1) / part;
-    const int most = most_split(p.item[i].mt, p.item[i].nt);
-    p.item[i].split = int(want < most ? want : most);
+template <int PARTS, int PHASE, typename T>
+cudaError_t product(OrthoParams& p, int pairs, cudaStream_t st) {
+  // Wide tiles load fewer bytes per product and take 1.7 times as long as narrow
+  // ones; narrow ones divide the work into twice as many.  fp32 matrices, whose
+  // products are three, load few enough with narrow ones, and a wide tile's sums
+  // would not fit into the registers.
+  if constexpr (PARTS == 1) {
+    const int64_t wide = plan<PHASE, 256>(p), narrow = plan<PHASE, 128>(p);
+    if (17 * ((wide + pairs - 1) / pairs) <= 10 * ((narrow + pairs - 1) / pairs)) {
+      plan<PHASE, 256>(p);
+      return launch_product<PARTS, 256, PHASE, T>(p, pairs, st);
+    }
+  } else {
+    plan<PHASE, 128>(p);
   }
-}
-
-template <int PARTS, int BN, typename T>
-cudaError_t launch_steps(OrthoParams& p, int dev, cudaStream_t st) {
-  auto k = ortho_steps_k<PARTS, BN, T>;
-  static std::atomic<bool> allowed[kMaxDevices];
-  static std::atomic<int> resident[kMaxDevices];      // pairs that run at the same time
-  cudaError_t e = allow_smem(k, allowed);
-  if (e != cudaSuccess) return e;
-  // without wide tiles' numbers of units, a long sum's terms are shared
-  for (int i = 0; i < p.count; ++i) p.item[i].split = 1;
-  if (BN == 128) share_sums(p);
-  const int64_t units = plan<kGram, BN>(p) + plan<kPoly, BN>(p) + plan<kApply, BN>(p);
-  if (units * p.steps >= int64_t(1) << 31) return cudaErrorInvalidValue;      // sides are limited: not reached
-  cudaLaunchConfig_t cfg = {};
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Tiles<PARTS, BN>::kSmem;
-  cfg.stream = st;
-  cfg.gridDim = dim3(2);
-  int pairs = dev < kMaxDevices ? resident[dev].load() : 0;
-  if (pairs == 0) {
-    if ((e = cudaOccupancyMaxActiveClusters(&pairs, k, &cfg)) != cudaSuccess) return e;
-    if (pairs < 1) return cudaErrorCooperativeLaunchTooLarge;
-    if (dev < kMaxDevices) resident[dev].store(pairs);
+  // A sum of X X^T has the larger side's terms, and few tiles where the smaller side
+  // is short: pairs that would have no tile take a part of them, as long as a part
+  // is not shorter than 8 blocks of 64 (512 x 2048 fp32: 240 -> 190 us).
+  if constexpr (PHASE == kGram) {
+    const int64_t units = p.start[p.count];
+    int longest = 0, shares = 1;
+    bool room = true;
+    for (int i = 0; i < p.count; ++i) {
+      longest = std::max(longest, 2 * p.item[i].nt);
+      room = room && most_shares(p.item[i].mt) == kMaxShares;
+    }
+    while (room && shares < kMaxShares && 2 * shares * units <= pairs && longest / (2 * shares) >= 8) shares *= 2;
+    if (shares > 1) return launch_shared<PARTS, T>(p, shares, st);
   }
-  cfg.gridDim = dim3(2 * unsigned(units < pairs ? units : pairs));
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeCooperative;
-  attr[0].val.cooperative = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, k, static_cast<const OrthoParams&>(p));
+  return launch_product<PARTS, 128, PHASE, T>(p, pairs, st);
 }
 
 template <typename T>
-cudaError_t orthogonalize_small(const OrthoParams& p, cudaStream_t st) {
+cudaError_t orthogonalize_small(const OrthoParams& p, int steps, cudaStream_t st) {
   auto k = ortho_small_k<sizeof(T) == 4 ? 2 : 1, T>;
   static std::atomic<bool> allowed[kMaxDevices];
   const cudaError_t e = allow_smem(k, allowed);
   if (e != cudaSuccess) return e;
-  return launch_k(k, dim3(kSmallCtas * unsigned(p.count)), dim3(kSmallThreads), kSmallSmem, st, p);
+  return launch_k(k, dim3(kSmallCtas * unsigned(p.count)), dim3(kSmallThreads), kSmallSmem, st, p, steps);
 }
 template <typename T>
-cudaError_t orthogonalize(OrthoParams& p, cudaStream_t st) {
+cudaError_t orthogonalize(OrthoParams& p, int steps, cudaStream_t st) {
+  constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
   int dev = 0, sms = 1;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
+  const int pairs = sms > 1 ? sms / 2 : 1;
   int64_t units = 0;
   for (int i = 0; i < p.count; ++i) {
-    p.start[0][i] = int(units);
+    p.start[i] = int(units);
     units += p.item[i].nsums;
   }
-  p.start[0][p.count] = int(units);
+  p.start[p.count] = int(units);
   if ((e = launch_k(ortho_sums_k<T>, dim3(unsigned(units)), dim3(256), 0, st, p)) != cudaSuccess) return e;
   if ((e = launch_k(ortho_scale_k, dim3(unsigned(p.count)), dim3(256), 0, st, p)) != cudaSuccess) return e;
   units = 0;
   for (int i = 0; i < p.count; ++i) {
-    p.start[0][i] = int(units);
+    p.start[i] = int(units);
     units += 4 * int64_t(p.item[i].mt) * p.item[i].nt;
   }
-  p.start[0][p.count] = int(units);
+  p.start[p.count] = int(units);
   if ((e = launch_k(ortho_pack_k<T>, dim3(unsigned(units)), dim3(256), 0, st, p)) != cudaSuccess) return e;
-  // Wide tiles load fewer bytes per product and take 1.7 times as long as narrow
-  // ones, which divide the work into twice as many: they are taken where a product
-  // has fewer than two rounds of wide ones.  fp32 matrices, whose products are
-  // three, load few enough with narrow ones, and a wide tile's sums would not fit
-  // into the registers.
-  if constexpr (sizeof(T) == 2) {
-    if (plan<kApply, 256>(p) >= sms) return launch_steps<1, 256, T>(p, dev, st);
-    return launch_steps<1, 128, T>(p, dev, st);
-  } else {
-    return launch_steps<2, 128, T>(p, dev, st);
+  for (int s = 0; s < steps; ++s) {
+    p.from = s & 1;
+    p.last = s + 1 == steps;
+    if ((e = product<PARTS, kGram, T>(p, pairs, st)) != cudaSuccess) return e;
+    if ((e = product<PARTS, kPoly, T>(p, pairs, st)) != cudaSuccess) return e;
+    if ((e = product<PARTS, kApply, T>(p, pairs, st)) != cudaSuccess) return e;
   }
+  return cudaSuccess;
 }
 
 }  // namespace
@@ -1378,7 +1273,6 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
    for (const bool small : {true, false}) {
     OrthoParams p = {};
     p.ws = static_cast<char*>(workspace);
-    p.steps = steps;
     p.ca = float(coefficients[0]);
     p.cb = float(coefficients[1]);
     p.cc = float(coefficients[2]);
@@ -1417,7 +1311,7 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
         for (int k = 0; k < 2; ++k) it.x[k] = take(int64_t(it.mt) * it.nt * 4 * kBlock * 2);
         it.a = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
         it.c = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
-        it.parts = take(shared_bytes(it.mt, it.nt));
+        it.parts = take(shared_bytes(it.mt));
       }
       const int64_t per = dtype == FO_DTYPE_F32 ? 4 : 8;
       it.vec_in = aligned16(m.grad) && (m.rows == 1 || m.grad_stride % per == 0) &&
@@ -1430,10 +1324,8 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
     if (p.count == 0) continue;
     p.sums = reinterpret_cast<float4*>(p.ws + at);
     p.scale = reinterpret_cast<float2*>(p.sums + p.count * kMaxSums);
-    p.done = reinterpret_cast<unsigned*>(p.scale + p.count);
-    p.shared = p.done + p.count;
-    const cudaError_t e = small ? (dtype == FO_DTYPE_F32 ? orthogonalize_small<float>(p, st) : orthogonalize_small<bf16>(p, st))
-                          : dtype == FO_DTYPE_F32 ? orthogonalize<float>(p, st) : orthogonalize<bf16>(p, st);
+    const cudaError_t e = small ? (dtype == FO_DTYPE_F32 ? orthogonalize_small<float>(p, steps, st) : orthogonalize_small<bf16>(p, steps, st))
+                          : dtype == FO_DTYPE_F32 ? orthogonalize<float>(p, steps, st) : orthogonalize<bf16>(p, steps, st);
     if (e != cudaSuccess) return done(e);
   }
   return FO_OK;
