@@ -14,10 +14,13 @@
 // Operands are fp16, not bf16: singular values stay below about 1.3, so the
 // range is known and held in the middle of fp16's by powers of two, and each
 // rounding costs 2^-12 instead of 2^-9.  X itself is kept as the sum of two fp16
-// numbers (22 bits), and a X is added from both: what the roundings of the
-// products' operands leave in the weak directions, which each step multiplies by
-// up to a, is then proportional to C, which is small there (off by 0.5 to 0.8e-3
-// for bf16 matrices instead of 2e-3 with a in the product).  For fp32 matrices
+// numbers (22 bits), and what the product's operands would round most is added
+// without them: a X, and for bf16 matrices also the diagonal of C times X, in
+// fp32.  The roundings that are left fall on the rest of C, which is small in the
+// weak directions that each step multiplies by up to a, and small once the rows
+// are orthogonal (errors before the result's rounding: 512 x 512 2.2e-3 with all
+// of it in the product, 0.7e-3 without a, 0.5e-3 without the diagonal; 16 x 300
+// 2.1, 1.4 and 0.6e-3).  For fp32 matrices
 // all operands are such pairs, and each product three (hi lo, lo hi, hi hi, in
 // this order; the fourth is below fp32's rounding).  Sums are fp32 in tensor
 // memory; because the tensor cores truncate, those of fp32 matrices are moved to
@@ -60,7 +63,7 @@ struct Item {
   float *mom, *param;
   void* out;
   int64_t ldg, ldm, ldp, ldo;
-  int64_t x[2], a, c;       // byte offsets in the workspace
+  int64_t x[2], a, c, d;    // byte offsets in the workspace; d: the diagonal of C
   int64_t parts;            // of A's shared sums, [tile][split - 1][CTA][warp] of 8 KB
   int rows, cols, mt, nt;   // mt, nt: tiles of 128 of the smaller and the larger side
   int nsums;                // partial sums of squares, at kMaxSums times its index
@@ -462,7 +465,9 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
     for (int e = 0; e < 64; ++e) v[e] *= kUpA / (kUpX * kUpX);
   } else {
     // C = b A + c A A, or a X + C X
-    const float linear = PHASE == kPoly ? p.cb : p.ca, other = (PHASE == kPoly ? p.cc : 1.f) / kUpA;
+    const float other = (PHASE == kPoly ? p.cc : 1.f) / kUpA;
+    float linear = p.cb;
+    if (PHASE == kApply) linear = PARTS == 2 ? p.ca : fmaf(1.f / kUpA, reinterpret_cast<const float*>(p.ws + m.d)[128 * tile + 32 * q + lane], p.ca);
     // the warp's 4 KB are read as they lie, and handed out by rows through shared memory
     const uint4* src = reinterpret_cast<const uint4*>(p.ws + (PHASE == kPoly ? m.a : m.x[p.from]) + half_block) + lane;
     constexpr int kParts = PHASE == kPoly ? PARTS : 2;
@@ -493,6 +498,17 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
       }
     }
     __syncwarp();
+  }
+  if (PARTS == 1 && PHASE == kPoly && 2 * tile + q / 2 == cblk) {      // the diagonal goes its own way
+    float diagonal = 0.f;
+    const uint32_t bit = 1u << lane;       // a mask, not an index, which would move v to memory
+#pragma unroll
+    for (int e = 0; e < 64; ++e) {
+      const bool here = (bit >> e % 32 & 1u) && e / 32 == q % 2;
+      diagonal += here ? v[e] : 0.f;
+      v[e] = here ? 0.f : v[e];
+    }
+    reinterpret_cast<float*>(p.ws + m.d)[128 * tile + 32 * q + lane] = diagonal;
   }
   if (PHASE == kApply && p.last) {
     deliver<T>(p, m, tile, 64 * cblk, q, lane, buf, v);
@@ -803,7 +819,7 @@ __global__ void __launch_bounds__(kThreads, 1) ortho_shared_k(const __grid_const
 constexpr int kSmallRows = 128, kSmallCols = 256, kSmallCtas = 8;
 constexpr int kSmallThreads = 512, kSmallUnits = kSmallRows * kSmallCols / 8 / kSmallThreads;
 constexpr int kSmallX = 8 * kBlock, kSmallA = 4 * kBlock;             // one part of X, of A or C
-constexpr int kSmallSmem = 1024 + 2 * kSmallX + 2 * kSmallA + 32 + 16 * 16;
+constexpr int kSmallSmem = 1024 + 2 * kSmallX + 2 * kSmallA + 32 + 16 * 16 + kSmallRows * 4;
 constexpr int kSmallPart = kSmallRows * kSmallRows * 4;                // of X X^T
 static_assert(kSmallSmem <= 232448, "shared memory per CTA");
 
@@ -835,6 +851,7 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
   uint64_t* bar = reinterpret_cast<uint64_t*>(smem + 2 * kSmallX + 2 * kSmallA);
   uint32_t* tslot = reinterpret_cast<uint32_t*>(bar + 1);
   float4* box = reinterpret_cast<float4*>(bar + 4);
+  float* diagonal = reinterpret_cast<float*>(box + 16);        // of C
   if (t == 0) {
     mbar_init(bar, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -1017,6 +1034,10 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
 #pragma unroll
     for (int e = 0; e < 32; ++e) A[e] = v[e] *= kUpA / (kUpX * kUpX);
     put_row<PARTS>(a_block, kSmallA, row, quarter % 2 * 4, v);
+    // b A of the rounded A, as A A has it: near a singular value of 1 the two
+    // errors cancel (b + 2 c = -0.7)
+#pragma unroll
+    for (int e = 0; e < 32; ++e) A[e] -= v[e];
     begin();
     if (warp == 0) {
       for (int c = 0; c < 2; ++c) product(tmem + 128 * c, sa + c * 2 * kBlock, kSmallA, sa + c * 2 * kBlock, kSmallA, 128, false);
@@ -1026,6 +1047,17 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
     sum(lanes + 32 * quarter, 2, 128);
 #pragma unroll
     for (int e = 0; e < 32; ++e) v[e] = fmaf(p.cc / kUpA, v[e], p.cb * A[e]);
+    if (PARTS == 1 && q == quarter) {         // the diagonal goes its own way
+      float own = 0.f;
+      const uint32_t bit = 1u << lane;        // a mask, not an index, which would move v to memory
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        const bool here = bit >> e & 1u;
+        own += here ? v[e] : 0.f;
+        v[e] = here ? 0.f : v[e];
+      }
+      diagonal[row] = own;
+    }
     put_row<PARTS>(a_block, kSmallA, row, quarter % 2 * 4, v);
     begin();
     if (warp == 0) {
@@ -1035,6 +1067,7 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
     }
     finished();
     if (quarter < blocks) {
+      const float linear = PARTS == 2 ? p.ca : fmaf(1.f / kUpA, diagonal[row], p.ca);
       const uint32_t x_block = sx + quarter * 2 * kBlock;
 #pragma unroll 1
       for (int h = 0; h < 2; ++h) {
@@ -1048,8 +1081,8 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
           for (int e = 0; e < 4; ++e) {
             const float2 fh = of_pair(__float_as_uint(zh[e])), fl = of_pair(__float_as_uint(zl[e]));
             float &x = v[8 * k + 2 * e], &y = v[8 * k + 2 * e + 1];
-            x = fmaf(p.ca, fh.x, fmaf(p.ca, fl.x, x * (1.f / kUpA)));
-            y = fmaf(p.ca, fh.y, fmaf(p.ca, fl.y, y * (1.f / kUpA)));
+            x = fmaf(linear, fh.x, fmaf(linear, fl.x, x * (1.f / kUpA)));
+            y = fmaf(linear, fh.y, fmaf(linear, fl.y, y * (1.f / kUpA)));
           }
         }
         if (step + 1 < steps) put_row<2>(x_block, kSmallX, row, 4 * h, v);
@@ -1094,7 +1127,7 @@ int64_t item_bytes(const fo_matrix_update& m, int parts) {
   if (m.rows == 0 || m.cols == 0) return 0;
   if (is_small(m)) return 2 * kSmallCtas * kSmallPart + 256;
   const int64_t r = (m.rows + 127) / 128, c = (m.cols + 127) / 128, mt = r < c ? r : c, nt = r < c ? c : r;
-  return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + shared_bytes(mt) + kMaxSums * 16 + 16;
+  return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + shared_bytes(mt) + mt * 512 + kMaxSums * 16 + 16;
 }
 
 template <int PARTS, int BN, int PHASE, typename T>
@@ -1312,6 +1345,7 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
         it.a = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
         it.c = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
         it.parts = take(shared_bytes(it.mt));
+        it.d = take(int64_t(it.mt) * 512);
       }
       const int64_t per = dtype == FO_DTYPE_F32 ? 4 : 8;
       it.vec_in = aligned16(m.grad) && (m.rows == 1 || m.grad_stride % per == 0) &&
