@@ -569,9 +569,10 @@ FO_API int fo_decode_8bit(const uint8_t* q, const uint8_t* scales, void* y, int6
  * Coefficients such as (3.4445, -4.7750, 2.0315) bring the singular values into
  * 0.7 .. 1.2 in five steps.  The products run on the tensor cores, on fp16
  * operands for bf16 matrices (roundings of 2^-12) and on pairs of them for fp32
- * ones (2^-22), with fp32 sums; singular values that exceed 64 on the way
- * overflow.  An infinity or NaN in U makes all of X NaN.  The order of all sums
- * is fixed.  Sides of 0 to 32768 (the smaller) and 2^20.
+ * ones (2^-22), with fp32 sums; a singular value t above 16 on the way, or
+ * c1 t^2 + c2 t^4 beyond +-255, overflows.  An infinity or NaN in U makes all of X NaN.  The order of all sums
+ * is fixed.  Sides of 0 to 32768 (the smaller) and 2^20.  What one matrix writes
+ * is none of another's tensors (equal addresses are refused).
  * ---------------------------------------------------------------------- */
 typedef struct fo_matrix_update {
   int64_t rows, cols;

@@ -1296,6 +1296,10 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
                        (m.param && m.param_stride < m.cols)))
       return bad("bad row stride");
     if (!(std::fabs(m.step) <= 1e30f)) return bad("bad step");
+    // matrices of one launch are worked on at the same time
+    for (int k = i / kItems * kItems; k < i; ++k)
+      if ((m.out && m.out == items[k].out) || (m.momentum && m.momentum == items[k].momentum) || (m.param && m.param == items[k].param))
+        return bad("a tensor to write stands twice in the list");
   }
   const int64_t need = fo_orthogonalize_workspace(items, count, dtype);
   if (need > 0 && (!workspace || odd(workspace, 256) || workspace_bytes < need))

@@ -188,6 +188,19 @@ def test_row_strides(dtype, cols, pad, skip):
     assert gradient_agrees(api.rms_norm_grad(loose, None, s, w, got[2]), loose, None, s, w, got[2])
 
 
+@pytest.mark.parametrize("cols,pad", [(64, 8), (64, 3), (45, 2), (2048, 16)])
+def test_eight_bits_of_and_into_strided_rows(cols, pad):
+    big = [torch.randn(21, cols + pad, device="cuda").bfloat16() for _ in range(3)]
+    x, r, y = (t[:, :cols] for t in big)
+    w, before = torch.randn(cols, device="cuda"), big[2].clone()
+    q, scales, s = api.rms_norm_8bit(x, r, w)
+    assert eight_agrees(q, scales, forward(x, r, w)[1], cols) and torch.equal(s, forward(x, r, w)[0])
+    assert api.decode_8bit(q, scales, out=y).data_ptr() == y.data_ptr()
+    before[:, :cols] = api.decode_8bit(q, scales)
+    assert torch.equal(before, big[2])
+    assert torch.equal(api.decode_8bit(q.view(3, 7, cols), scales.view(3, 7, -1)), y.reshape(3, 7, cols))
+
+
 @pytest.mark.parametrize("cols", [96, 2048, 40000])
 def test_in_place(cols):
     x, r, w, dy, ds = make(5, cols, F32, F32)

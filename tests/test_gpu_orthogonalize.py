@@ -47,10 +47,10 @@ def reference(u, dtype, steps=5, coefficients=api.QUINTIC, eps=1e-7):
     e = (100 * U) * float(X.norm())
     m, k = X.shape
     for _ in range(steps):
-        S, F = float(torch.linalg.matrix_norm(X, 2)), float(X.norm())
+        A = X @ X.t()
+        S, F = float(torch.linalg.eigvalsh(A)[-1].clamp(min=0).sqrt()), float(X.norm())
         s = torch.linspace(0, 1.05 * S + 1e-3, 2000, dtype=torch.float64)
         L = float((a + 3 * b * s ** 2 + 5 * c * s ** 4).abs().max())
-        A = X @ X.t()
         B = a * torch.eye(m, dtype=X.dtype, device=X.device) + b * A + c * A @ A
         new = B @ X
         gram = d * float(A.norm()) + sums_loss(dtype, k) * float((X.abs() @ X.abs().t()).norm())
@@ -74,8 +74,10 @@ def make(rows, cols, dtype, seed=0):
     return (u @ torch.randn(k, cols, device="cuda", generator=g) + 0.2 * torch.randn(rows, cols, device="cuda", generator=g)).to(dtype)
 
 
+# up to 128 x 2048 in shared memory; above, tiles of pairs, and clusters that share the long sums of few tiles
 SHAPES = [(1, 1), (1, 9), (8, 1), (3, 5), (64, 64), (63, 65), (128, 128), (129, 127), (96, 200), (200, 96), (256, 130), (130, 384), (512, 513),
-          (1000, 77), (40, 3000), (512, 2048), (1536, 512), (700, 1100)]
+          (1000, 77), (40, 3000), (512, 2048), (1536, 512), (700, 1100), (128, 2048),
+          (100, 2049), (1300, 128), (140, 4096), (300, 2500), (1920, 2100)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF])

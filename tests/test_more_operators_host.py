@@ -208,6 +208,15 @@ def test_bad_matrices_are_refused(sizes, over, what):
     assert orthogonalize(items(*sizes, **over)) == api.ERR_ARG and what in api.last_error()
 
 
+@pytest.mark.parametrize("field", ["out", "momentum", "param"])
+def test_a_tensor_to_write_twice_is_refused(field):
+    a = items((4, 4), (4, 4), out_stride=4, momentum_stride=4, param_stride=4)
+    for k, it in enumerate(a):
+        it.out, it.momentum, it.param = P + 4096 * k, P + 65536 * (1 + k), P + 1048576 * (1 + k)
+    setattr(a[1], field, getattr(a[0], field))
+    assert orthogonalize(a) == api.ERR_ARG and "twice" in api.last_error()
+
+
 @pytest.mark.parametrize("over,what", [
     ({"dtype": 2}, "dtype"), ({"steps": 0}, "steps"), ({"steps": 65}, "steps"), ({"coefficients": None}, "coefficients"), ({"eps": 0.0}, "eps"),
     ({"mu": -0.1}, "momentum"), ({"mu": float("nan")}, "momentum"), ({"decay": float("inf")}, "decay"), ({"workspace": None}, "workspace"),
