@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_place_k(const __grid_consta
 // word, its key above its number.  The other blocks of the launch meanwhile clear
 // the rows of the table that no token has: each marks the ids in its range of
 // rows in a bitmap.
-constexpr int kOneThreads = 1024, kOneWarps = kOneThreads / 32, kOneTokens = 16384, kOneDigit = 10;
+constexpr int kOneThreads = 1024, kOneWarps = kOneThreads / 32, kOneTokens = 16384, kOneDigit = 9;
 constexpr int kClearRows = 32768;             // rows of a bitmap
 struct OneParams {
   const void* ids;
@@ -214,10 +214,10 @@ __device__ __forceinline__ uint32_t id_key(const OneParams& p, uint32_t i) {
 }
 
 __global__ void __launch_bounds__(kOneThreads) sort_one_k(const __grid_constant__ OneParams p) {
-  extern __shared__ uint32_t words[];         // [2][n] and [warps][bins] of 16 bits
+  extern __shared__ uint32_t words[];         // [2][n], and of 16 bits [warps][bins] and [n]
   __shared__ uint32_t base[1 << kOneDigit];
   __shared__ uint32_t box[kOneWarps];
-  static_assert(kOneThreads == 1 << kOneDigit, "one bin per thread");
+  static_assert(kOneThreads >= 1 << kOneDigit, "one bin per thread");
   pdl_wait();
   pdl_trigger();
   const int t = threadIdx.x, lane = t % 32, warp = t / 32;
@@ -254,6 +254,7 @@ __global__ void __launch_bounds__(kOneThreads) sort_one_k(const __grid_constant_
   uint32_t *from = words, *to = words + p.n;
   uint16_t* counts = reinterpret_cast<uint16_t*>(words + 2 * p.n);
   const int bins = 1 << p.digit;
+  uint16_t* ranks = counts + kOneWarps * bins;          // of a token among its warp's of its digit
   const uint32_t per = (p.n + 32 * kOneWarps - 1) / (32 * kOneWarps) * 32;       // a warp's neighbouring tokens
   const uint32_t first = min(p.n, warp * per), end = min(p.n, first + per);
   for (uint32_t i = first + lane; i < end; i += 32) from[i] = id_key(p, i) << p.token_bits | i;
@@ -261,21 +262,22 @@ __global__ void __launch_bounds__(kOneThreads) sort_one_k(const __grid_constant_
     for (int i = t; i < kOneWarps * bins / 2; i += kOneThreads) reinterpret_cast<uint32_t*>(counts)[i] = 0;
     __syncthreads();
     uint16_t* own = counts + warp * bins;
-    uint32_t ranks[kOneTokens / kOneThreads / 2];          // of the tokens that this thread holds, two to a word
-#pragma unroll
-    for (int j = 0; j < kOneTokens / kOneThreads; ++j) {
-      const uint32_t i = first + 32 * j + lane;
-      if (first + 32 * j >= end) break;
+    // not unrolled: a block's first pass through long code waits for instructions
+    // (5000 tokens: 12 us with both loops unrolled)
+#pragma unroll 1
+    for (uint32_t i0 = first; i0 < end; i0 += 32) {
+      const uint32_t i = i0 + lane;
       const bool in = i < end;
       const uint32_t digit = in ? from[i] >> (p.token_bits + shift) & uint32_t(bins - 1) : 0u;
       const uint32_t peers = __match_any_sync(0xffffffffu, in ? digit : uint32_t(bins));
       const uint32_t before = in ? own[digit] : 0u;
       __syncwarp();
       const uint32_t lower = __popc(peers & ((1u << lane) - 1u));
-      if (in && lower == 0) own[digit] = uint16_t(before + __popc(peers));
+      if (in) {
+        if (lower == 0) own[digit] = uint16_t(before + __popc(peers));
+        ranks[i] = uint16_t(before + lower);
+      }
       __syncwarp();
-      if (j % 2 == 0) ranks[j / 2] = before + lower;
-      else ranks[j / 2] |= (before + lower) << 16;
     }
     __syncthreads();
     uint32_t all = 0;                         // of bin t, before each warp
@@ -290,12 +292,10 @@ __global__ void __launch_bounds__(kOneThreads) sort_one_k(const __grid_constant_
     if (t < bins) base[t] = at;
     __syncthreads();
     const bool last = shift + p.digit >= p.bits;
-#pragma unroll
-    for (int j = 0; j < kOneTokens / kOneThreads; ++j) {
-      const uint32_t i = first + 32 * j + lane;
-      if (i >= end) break;
+#pragma unroll 2
+    for (uint32_t i = first + lane; i < end; i += 32) {
       const uint32_t v = from[i], digit = v >> (p.token_bits + shift) & uint32_t(bins - 1);
-      const uint32_t place = base[digit] + own[digit] + (ranks[j / 2] >> (j % 2 * 16) & 0xffffu);
+      const uint32_t place = base[digit] + own[digit] + ranks[i];
       if (last) {
         p.key_out[place] = v >> p.token_bits;
         p.token_out[place] = v & ((1u << p.token_bits) - 1u);
@@ -621,7 +621,7 @@ int bits_of(int64_t v) {
   while (v >> n) ++n;
   return n;
 }
-constexpr int kOneSmem = 2 * kOneTokens * 4 + (kOneWarps << kOneDigit) * 2;
+constexpr int kOneSmem = 2 * kOneTokens * 4 + (kOneWarps << kOneDigit) * 2 + kOneTokens * 2;
 cudaError_t sort_one(const OneParams& o, bool accumulate, cudaStream_t st) {
   static std::atomic<bool> allowed[kMaxDevices];
   int dev = 0;
@@ -631,7 +631,7 @@ cudaError_t sort_one(const OneParams& o, bool accumulate, cudaStream_t st) {
     if (e == cudaSuccess && dev < kMaxDevices) allowed[dev] = true;
   }
   if (e != cudaSuccess) return e;
-  const int64_t sort = 8 * int64_t(o.n) + (int64_t(kOneWarps) << o.digit) * 2, clear = kClearRows / 8;
+  const int64_t sort = 10 * int64_t(o.n) + (int64_t(kOneWarps) << o.digit) * 2, clear = kClearRows / 8;
   // as many blocks as fit at once, of 64 rows at least
   const int most = elementwise_blocks(INT64_MAX / 2, 256) / 8 - 1, want = int((int64_t(o.vocab) + 63) / 64);
   const int blocks = accumulate ? 1 : 1 + (want < most ? want : most > 1 ? most : 1);
