@@ -10,7 +10,6 @@ from __future__ import annotations
 import contextlib
 import ctypes as C
 import os
-import struct
 from array import array
 
 import numpy as np
@@ -687,75 +686,25 @@ def dropout_grad(dy, p, seed, call, out=None, stream=None):
     return dropout_add(dy, None, p, seed, call, out=out, stream=stream)
 
 
-# The binding of the operators below: what a call needs beyond the library's own
-# work costs more than many a kernel, so checks are few and nothing is entered
-# (device, stream) that is current already.
+# The operators below are short on the GPU, so their checks, allocations and calls
+# are compiled (csrc/fo_binding.cpp); what stands here is their interface.
 
-_codes = {}                     # torch dtype -> DTYPE_*
-_raw_stream = None
+_compiled = None
 
 
-def _setup(torch):
-    global _raw_stream
-    _codes[torch.float32] = DTYPE_F32
-    _codes[torch.bfloat16] = DTYPE_BF16
-    # the handle of a device's current stream, without an object around it
-    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
-
-
-def _code(t, name):
-    try:
-        return _codes[t.dtype]
-    except KeyError:
-        raise ValueError(f"{name}: bf16 or fp32") from None
-
-
-def _run(index, stream, body, *args):
-    """body(torch, stream handle, *args) with device `index` current and what it
-    allocates belonging to the stream."""
-    import torch
-    if not _codes:
-        _setup(torch)
-    if index < 0:
-        raise ValueError("device tensors are wanted")
-    if stream is None and index == torch.cuda.current_device():
-        return body(torch, _raw_stream(index), *args)
-    with torch.cuda.device(index):
-        if stream is None:
-            return body(torch, torch.cuda.current_stream(index).cuda_stream, *args)
-        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=torch.device("cuda", index))):
-            return body(torch, stream, *args)
-
-
-def _like(t, shape, dtype, index, name):
-    """(pointer, row stride) of `t` seen as a matrix [rows, last dimension]."""
-    if t.shape != shape or t.dtype != dtype or t.get_device() != index:
-        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}; wanted {tuple(shape)} {dtype} on the same device as the others")
-    if t.is_contiguous():
-        return t.data_ptr(), shape[-1]
-    if len(shape) == 2 and t.stride(1) == 1:
-        return t.data_ptr(), t.stride(0)
-    raise ValueError(f"{name}: contiguous, or a matrix with innermost stride 1")
-
-
-def _dense(torch, g):
-    """`g`, or a contiguous copy where its strides would refuse it: autograd
-    hands over gradients broadcast by a sum or a mean."""
-    if g.is_contiguous() or g.dim() == 2 and g.stride(1) == 1:
-        return g
-    return g.clone(memory_format=torch.contiguous_format)
-
-
-def _ids(torch, ids):
-    if ids.dtype == torch.int32:
-        bits = 32
-    elif ids.dtype == torch.int64:
-        bits = 64
-    else:
-        raise ValueError("ids: int32 or int64")
-    if not ids.is_contiguous():
-        raise ValueError("ids: contiguous")
-    return ids.data_ptr(), bits
+def _binding():
+    """The compiled binding (raises if it has not been built)."""
+    global _compiled
+    if _compiled is None:
+        lib()
+        import torch  # noqa: F401  (its libraries come first)
+        try:
+            from . import _binding as module
+        except ImportError as e:
+            raise FedOptimaError(f"the compiled binding is missing: build it with paper_2504_13850_gb300.build.build() ({e})") from e
+        module.set_error(FedOptimaError)
+        _compiled = module
+    return _compiled
 
 
 def embedding(ids, table, scale=1.0, dtype=None, out=None, stream=None):
@@ -763,57 +712,14 @@ def embedding(ids, table, scale=1.0, dtype=None, out=None, stream=None):
     contiguous table [vocab, width]; ids outside of the table (padding) give
     zeros.  `dtype` of the output defaults to the table's (bf16 of an fp32 table
     is the other choice).  Runs on `stream`, by default torch's current stream."""
-    return _run(ids.get_device(), stream, _embedding, ids, table, scale, dtype, out)
-
-
-def _embedding(torch, st, ids, table, scale, dtype, out):
-    index = ids.get_device()
-    if table.dim() != 2 or not table.is_contiguous() or table.get_device() != index:
-        raise ValueError("table: a contiguous matrix [vocab, width] on the ids' device")
-    ip, bits = _ids(torch, ids)
-    vocab, width = table.shape
-    if dtype is None:
-        dtype = table.dtype
-    shape = (*ids.shape, width)
-    if out is None:
-        out = torch.empty(shape, dtype=dtype, device=ids.device)
-        yp, ys = out.data_ptr(), width
-    else:
-        yp, ys = _like(out, shape, dtype, index, "out")
-    _check(lib().fo_embedding(ip, bits, ids.numel(), table.data_ptr(), _code(table, "table"), vocab, width, scale, yp, ys,
-                              _code(out, "out"), st), "embedding")
-    return out
+    return (_compiled or _binding()).embedding(ids, table, scale, dtype, out, stream)
 
 
 def embedding_grad(dout, ids, vocab, scale=1.0, dtype=None, out=None, accumulate=False, stream=None):
     """fo_embedding_grad: the gradient [vocab, width] of embedding's table, of
     `dtype` (default: dout's), from dout = [*ids.shape, width].  `out` may give
     the tensor to write, or with `accumulate` to add to."""
-    return _run(ids.get_device(), stream, _embedding_grad, dout, ids, vocab, scale, dtype, out, accumulate)
-
-
-def _embedding_grad(torch, st, dout, ids, vocab, scale, dtype, out, accumulate):
-    ip, bits = _ids(torch, ids)
-    tokens, width, device, L_ = ids.numel(), dout.shape[-1], ids.device, lib()
-    dout = _dense(torch, dout)
-    gp, gs = _like(dout, (*ids.shape, width), dout.dtype, ids.get_device(), "dout")
-    if out is None:
-        if accumulate:
-            raise ValueError("accumulate: out holds what is added to")
-        out = torch.empty((vocab, width), dtype=dout.dtype if dtype is None else dtype, device=device)
-    elif out.shape != (vocab, width) or not out.is_contiguous() or out.get_device() != ids.get_device():
-        raise ValueError("out: a contiguous matrix [vocab, width] on the ids' device")
-    need = L_.fo_embedding_workspace(tokens, width)
-    ws = torch.empty((max(need, 0),), dtype=torch.uint8, device=device)
-    _check(L_.fo_embedding_grad(gp, gs, _code(dout, "dout"), ip, bits, tokens, out.data_ptr(), _code(out, "out"), vocab, width,
-                                scale, 1 if accumulate else 0, ws.data_ptr(), need, st), "embedding_grad")
-    return out
-
-
-def _norm_weight(x, weight, index):
-    if weight.shape != x.shape[-1:] or weight.get_device() != index or not weight.is_contiguous():
-        raise ValueError("weight: a contiguous vector as long as x's last dimension, on x's device")
-    return weight.data_ptr(), _code(weight, "weight")
+    return (_compiled or _binding()).embedding_grad(dout, ids, vocab, scale, dtype, out, accumulate, stream)
 
 
 def rms_norm(x, residual, weight, eps=1e-6, out=None, sum_out=None, stream=None):
@@ -822,157 +728,31 @@ def rms_norm(x, residual, weight, eps=1e-6, out=None, sum_out=None, stream=None)
     dimension of a bf16 or fp32 device tensor.  weight: x's type or fp32.  `out`
     and `sum_out` may give y and s.  Runs on `stream`, by default torch's
     current stream."""
-    return _run(x.get_device(), stream, _rms_norm, x, residual, weight, eps, out, sum_out, False, True)[2:]
+    return (_compiled or _binding()).rms_norm(x, residual, weight, eps, out, sum_out, stream)
 
 
 def rms_norm_8bit(x, residual, weight, eps=1e-6, with_y=False, stream=None):
     """The norm as 8-bit floats: (q, scales, s), q float8_e4m3fn like x, scales
     uint8 [..., ceil(cols / 32)] (fo_rms_norm has the format), or with `with_y`
     (q, scales, y, s, r) from the same pass."""
-    got = _run(x.get_device(), stream, _rms_norm, x, residual, weight, eps, None, None, True, with_y)
-    return got if with_y else (got[0], got[1], got[3])
-
-
-def _rms_norm(torch, st, x, residual, weight, eps, out, sum_out, eight, with_y):
-    dtype, index, shape, device, t = _code(x, "x"), x.get_device(), x.shape, x.device, x.dtype
-    if not shape:
-        raise ValueError("x: one dimension at least")
-    cols = shape[-1]
-    wp, wt = _norm_weight(x, weight, index)
-    xp, xs = _like(x, shape, t, index, "x")
-    s, rp, rs, sp, ss = x, None, 0, None, 0
-    if residual is not None:
-        rp, rs = _like(residual, shape, t, index, "residual")
-        if sum_out is None:
-            s = torch.empty(shape, dtype=t, device=device)
-            sp, ss = s.data_ptr(), cols
-        else:
-            s = sum_out
-            sp, ss = _like(s, shape, t, index, "sum_out")
-    q = scales = r = qp = cp = yp = op = None
-    ys = 0
-    if with_y:
-        if out is None:
-            out = torch.empty(shape, dtype=t, device=device)
-            yp, ys = out.data_ptr(), cols
-        else:
-            yp, ys = _like(out, shape, t, index, "out")
-        r = torch.empty(shape[:-1], dtype=torch.float32, device=device)
-        op = r.data_ptr()
-    if eight:
-        q = torch.empty(shape, dtype=torch.float8_e4m3fn, device=device)
-        scales = torch.empty((*shape[:-1], (cols + 31) // 32), dtype=torch.uint8, device=device)
-        qp, cp = q.data_ptr(), scales.data_ptr()
-    _check(lib().fo_rms_norm(xp, xs, rp, rs, wp, wt, sp, ss, yp, ys, qp, cp, op, dtype, x.numel() // cols if cols else 0, cols,
-                             eps, st), "rms_norm")
-    return q, scales, out, s, r
+    return (_compiled or _binding()).rms_norm_8bit(x, residual, weight, eps, with_y, stream)
 
 
 def rms_norm_grad(dy, ds, s, weight, r, out=None, stream=None):
     """fo_rms_norm_grad: (dx, dweight) of rms_norm, from the gradients dy of y and
     ds of s (None: none), and the call's s, weight and r.  dx is also the
     residual's gradient."""
-    return _run(s.get_device(), stream, _rms_norm_grad, dy, ds, s, weight, r, out)
-
-
-def _rms_norm_grad(torch, st, dy, ds, s, weight, r, out):
-    dtype, index, shape, device, t, L_ = _code(s, "s"), s.get_device(), s.shape, s.device, s.dtype, lib()
-    if not shape:
-        raise ValueError("s: one dimension at least")
-    cols = shape[-1]
-    rows = s.numel() // cols if cols else 0
-    wp, wt = _norm_weight(s, weight, index)
-    dy = _dense(torch, dy)
-    gp, gs = _like(dy, shape, t, index, "dy")
-    hp, hs = None, 0
-    if ds is not None:
-        ds = _dense(torch, ds)
-        hp, hs = _like(ds, shape, t, index, "ds")
-    sp, ss = _like(s, shape, t, index, "s")
-    rp = _small(r, shape[:-1], torch.float32, s, "r")
-    if out is None:
-        out = torch.empty(shape, dtype=t, device=device)
-        xp, xs = out.data_ptr(), cols
-    else:
-        xp, xs = _like(out, shape, t, index, "out")
-    dw = torch.empty(weight.shape, dtype=weight.dtype, device=device)
-    need = L_.fo_rms_norm_workspace(rows, cols)
-    ws = torch.empty((max(need, 0),), dtype=torch.uint8, device=device)
-    _check(L_.fo_rms_norm_grad(gp, gs, hp, hs, sp, ss, wp, wt, rp, xp, xs, dw.data_ptr(), dtype, rows, cols, ws.data_ptr(), need,
-                               st), "rms_norm_grad")
-    return out, dw
+    return (_compiled or _binding()).rms_norm_grad(dy, ds, s, weight, r, out, stream)
 
 
 def decode_8bit(q, scales, dtype=None, out=None, stream=None):
     """fo_decode_8bit: the values of rms_norm_8bit's (q, scales), in `dtype`
     (default: bf16)."""
-    return _run(q.get_device(), stream, _decode_8bit, q, scales, dtype, out)
-
-
-def _decode_8bit(torch, st, q, scales, dtype, out):
-    shape, index = q.shape, q.get_device()
-    if q.dtype != torch.float8_e4m3fn or not q.is_contiguous() or not shape:
-        raise ValueError("q: a contiguous float8_e4m3fn tensor of one dimension at least")
-    cols = shape[-1]
-    sp = _small(scales, (*shape[:-1], (cols + 31) // 32), torch.uint8, q, "scales")
-    if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16 if dtype is None else dtype, device=q.device)
-        yp, ys = out.data_ptr(), cols
-    else:
-        yp, ys = _like(out, shape, out.dtype, index, "out")
-    _check(lib().fo_decode_8bit(q.data_ptr(), sp, yp, ys, _code(out, "out"), q.numel() // cols if cols else 0, cols, st),
-           "decode_8bit")
-    return out
-
+    return (_compiled or _binding()).decode_8bit(q, scales, dtype, out, stream)
 
 
 # Coefficients that bring singular values into 0.7 .. 1.2 in five steps.
 QUINTIC = (3.4445, -4.7750, 2.0315)
-
-_matrix_update_words = C.sizeof(fo_matrix_update) // 8
-
-
-def _orthogonalize(torch, st, grads, momenta, outs, params, steps_of, steps, coefficients, eps, mu, nesterov, decay):
-    """fo_orthogonalize on lists of tensors (momenta, outs and params may be
-    None, outs True to make them); returns outs."""
-    L_, n, first = lib(), len(grads), grads[0]
-    dtype, t, index, device, f32 = _code(first, "updates"), first.dtype, first.get_device(), first.device, torch.float32
-    for name, other in (("momenta", momenta), ("out", outs), ("params", params), ("scales", steps_of)):
-        if other is not None and other is not True and len(other) != n:
-            raise ValueError(f"{name}: as many as updates")
-    make, made = outs is True, []
-    flat = array("q", bytes(8 * _matrix_update_words * n))
-    at, keep = 0, []
-    for i, g in enumerate(grads):
-        if g.dim() != 2:
-            raise ValueError("updates: matrices")
-        if not g.is_contiguous():
-            g = _dense(torch, g)
-            keep.append(g)
-        shape = g.shape
-        gp, gs = _like(g, shape, t, index, "updates")
-        flat[at], flat[at + 1], flat[at + 2], flat[at + 6] = shape[0], shape[1], gp, gs
-        if momenta is not None:
-            flat[at + 3], flat[at + 7] = _like(momenta[i], shape, f32, index, "momenta")
-        if make:
-            o = torch.empty(shape, dtype=t, device=device)
-            made.append(o)
-            flat[at + 4], flat[at + 8] = o.data_ptr(), shape[1]
-        elif outs is not None:
-            flat[at + 4], flat[at + 8] = _like(outs[i], shape, t, index, "out")
-        if params is not None:
-            flat[at + 5], flat[at + 9] = _like(params[i], shape, f32, index, "params")
-            flat[at + 10] = struct.unpack("q", struct.pack("ff", steps_of[i], 0.0))[0]
-        at += _matrix_update_words
-    items = flat.buffer_info()[0]
-    need = L_.fo_orthogonalize_workspace(items, n, dtype)
-    if need < 0:
-        _check(ERR_ARG, "orthogonalize")
-    ws = torch.empty((need,), dtype=torch.uint8, device=device)
-    three = array("d", coefficients)
-    _check(L_.fo_orthogonalize(items, n, dtype, steps, three.buffer_info()[0], eps, mu, 1 if nesterov else 0, decay,
-                               ws.data_ptr(), need, st), "orthogonalize")
-    return made if make else outs
 
 
 def orthogonalize(updates, steps=5, coefficients=QUINTIC, eps=1e-7, out=None, stream=None):
@@ -985,10 +765,9 @@ def orthogonalize(updates, steps=5, coefficients=QUINTIC, eps=1e-7, out=None, st
         return orthogonalize([updates], steps, coefficients, eps, None if out is None else [out], stream)[0]
     if len(updates) == 0:
         return []
-    if len(coefficients) != 3:
-        raise ValueError("coefficients: three")
-    return _run(updates[0].get_device(), stream, _orthogonalize, updates, None, True if out is None else out, None, None, steps,
-                coefficients, eps, 0.0, False, 1.0)
+    made = (_compiled or _binding()).orthogonalize(updates, None, True if out is None else out, None, None, steps, coefficients, eps, 0.0,
+                                                   False, 1.0, stream)
+    return made if out is None else out
 
 
 def muon_step(params, grads, momenta, lr, momentum=0.95, nesterov=True, weight_decay=0.0, scales=None, steps=5,
@@ -1001,12 +780,10 @@ def muon_step(params, grads, momenta, lr, momentum=0.95, nesterov=True, weight_d
         raise ValueError("params, grads and momenta: as many of each")
     if len(params) == 0:
         return
-    if len(coefficients) != 3:
-        raise ValueError("coefficients: three")
     if scales is None:
         scales = [max(1.0, p.shape[0] / max(1, p.shape[1])) ** 0.5 for p in params]
-    _run(grads[0].get_device(), stream, _orthogonalize, grads, momenta, None, params, [lr * s for s in scales], steps,
-         coefficients, eps, momentum, nesterov, 1.0 - lr * weight_decay)
+    (_compiled or _binding()).orthogonalize(grads, momenta, None, params, [lr * s for s in scales], steps, coefficients, eps, momentum,
+                                            nesterov, 1.0 - lr * weight_decay, stream)
 
 
 def orthogonalize_error(stream=None, device=None):

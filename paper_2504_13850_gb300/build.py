@@ -1,5 +1,6 @@
 """Build the C-ABI shared library libfedoptima.so in-tree with nvcc for
-sm_103a (GB300).  Sources compile in parallel; objects go to _build/.
+sm_103a (GB300), and _binding.so, the compiled part of its Python binding, with
+g++ against torch's headers.  Sources compile in parallel; objects go to _build/.
 
 Several processes may call build() at once (one per rank under torchrun):
 an exclusive file lock serialises them, and every object and the library
@@ -9,15 +10,18 @@ from __future__ import annotations
 
 import concurrent.futures as cf
 import fcntl
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libfedoptima.so")
 BUILD = os.path.join(HERE, "_build")
+BINDING = os.path.join(HERE, "_binding.so")
 
 SOURCES = ["fo_server.cu", "k_elementwise.cu", "k_simt_conv.cu", "k_attention.cu", "k_tc_gemm.cu", "k_tc_gemm_fwd.cu", "k_tc_gemm_dgrad.cu", "k_tc_gemm_wgrad.cu", "k_head.cu", "k_vec.cu", "fo_noalloc.cu", "k_attention_tc.cu", "fo_preproc.cu", "k_mobile.cu", "k_scored.cu", "k_scored_fwd.cu", "k_scored_bwd.cu", "k_dropout.cu", "k_embedding.cu", "k_norm.cu", "k_orthogonalize.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -32,7 +36,47 @@ def nvcc():
     raise RuntimeError("nvcc not found")
 
 
+def _torch():
+    """torch's folder, without importing it."""
+    return importlib.util.find_spec("torch").submodule_search_locations[0]
+
+
+def _run(cmd, what, tmp):
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        if os.path.exists(tmp):
+            os.remove(tmp)
+        raise RuntimeError(f"{what}:\n{r.stdout}\n{r.stderr}")
+    return r.stderr
+
+
+def _compile_binding():
+    obj, src = os.path.join(BUILD, "fo_binding.o"), os.path.join(CSRC, "fo_binding.cpp")
+    include = os.path.join(_torch(), "include")
+    deps = [src, os.path.join(HERE, "..", "include", "fedoptima.h"), os.path.join(include, "torch", "csrc", "autograd", "python_variable.h")]
+    if os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps):
+        return obj, ""
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc()))), "include")
+    tmp = f"{obj}.{os.getpid()}.tmp"
+    log = _run(["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I" + sysconfig.get_paths()["include"], "-isystem", include,
+                "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-isystem", cuda, "-c", src, "-o", tmp],
+               "g++ failed for fo_binding.cpp", tmp)
+    os.replace(tmp, obj)
+    return obj, log
+
+
+def _link_binding(obj):
+    if os.path.exists(BINDING) and os.path.getmtime(BINDING) >= max(os.path.getmtime(obj), os.path.getmtime(OUT)):
+        return
+    tmp = f"{BINDING}.{os.getpid()}.tmp"
+    _run(["g++", "-shared", "-o", tmp, obj, "-L" + HERE, "-l:" + os.path.basename(OUT), "-Wl,-rpath,$ORIGIN", "-L" + os.path.join(_torch(), "lib"),
+          "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"], "link of _binding.so failed", tmp)
+    os.replace(tmp, BINDING)
+
+
 def _compile(src, extra):
+    if src.endswith(".cpp"):
+        return _compile_binding()
     obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
     srcp = os.path.join(CSRC, src)
     deps = [srcp] + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".hpp", ".cuh"))]
@@ -40,14 +84,9 @@ def _compile(src, extra):
     if os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps):
         return obj, ""
     tmp = f"{obj}.{os.getpid()}.tmp"
-    cmd = [nvcc(), *ARCH, *FLAGS, *extra, "-c", srcp, "-o", tmp]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        if os.path.exists(tmp):
-            os.remove(tmp)
-        raise RuntimeError(f"nvcc failed for {src}:\n{r.stdout}\n{r.stderr}")
+    log = _run([nvcc(), *ARCH, *FLAGS, *extra, "-c", srcp, "-o", tmp], f"nvcc failed for {src}", tmp)
     os.replace(tmp, obj)
-    return obj, r.stderr
+    return obj, log
 
 
 def build(verbose=False, extra=()):
@@ -58,8 +97,9 @@ def build(verbose=False, extra=()):
         except OSError:                       # a filesystem without locks: build unserialised
             pass
         with cf.ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 4)) as ex:
-            results = list(ex.map(lambda s: _compile(s, list(extra)), SOURCES))
+            results = list(ex.map(lambda s: _compile(s, list(extra)), SOURCES + ["fo_binding.cpp"]))
         objs = [o for o, _ in results]
+        binding = objs.pop()
         if verbose:
             for _, log in results:
                 if log:
@@ -67,13 +107,9 @@ def build(verbose=False, extra=()):
         newest = max(os.path.getmtime(o) for o in objs)
         if not os.path.exists(OUT) or os.path.getmtime(OUT) < newest:
             tmp = f"{OUT}.{os.getpid()}.tmp"
-            cmd = [nvcc(), *ARCH, "-shared", "-o", tmp, *objs]
-            r = subprocess.run(cmd, capture_output=True, text=True)
-            if r.returncode != 0:
-                if os.path.exists(tmp):
-                    os.remove(tmp)
-                raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
+            _run([nvcc(), *ARCH, "-shared", "-o", tmp, *objs], "link failed", tmp)
             os.replace(tmp, OUT)
+        _link_binding(binding)
     return OUT
 
 

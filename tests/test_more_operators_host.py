@@ -1,10 +1,9 @@
 """The host side of embedding and norm, without a GPU: refusals of the C ABI and
-workspace sizes, and the tensors' device made current by the binding."""
+workspace sizes, and of the compiled binding."""
 import pytest
 import torch
 
 from paper_2504_13850_gb300 import api, build
-from test_operators_device import Machine, Tensor
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -95,92 +94,27 @@ def test_workspaces():
     assert L.fo_rms_norm_workspace(1, 100) >= 400
 
 
-class Stand(Machine):
-    def __init__(self, monkeypatch):
-        super().__init__(monkeypatch)
-        api._setup(torch)
-        monkeypatch.setattr(api, "_raw_stream", lambda index: 0)
-
-    def fo_embedding_workspace(self, tokens, width):
-        return 256
-
-    def fo_rms_norm_workspace(self, rows, cols):
-        return 256
-
-    def fo_orthogonalize_workspace(self, items, count, dtype):
-        return 256
-
-
-def ids(index):
-    return Tensor((2, 16), torch.int32, index)
-
-
-def matrix(index, dtype=torch.bfloat16):
-    return Tensor((2, 16, 64), dtype, index)
-
-
-def vector(index):
-    return Tensor((64,), torch.float32, index)
-
-
-def codes(index):
-    return Tensor((2, 16, 64), torch.float8_e4m3fn, index), Tensor((2, 16, 2), torch.uint8, index)
-
-
-CALLS = {
-    "fo_embedding": lambda i, **kw: api.embedding(ids(i), Tensor((10, 64), torch.float32, i), dtype=torch.bfloat16, **kw),
-    "fo_embedding_grad": lambda i, **kw: api.embedding_grad(matrix(i), ids(i), 10, dtype=torch.float32, **kw),
-    "fo_rms_norm": lambda i, **kw: api.rms_norm(matrix(i), matrix(i), vector(i), **kw),
-    "fo_rms_norm_grad": lambda i, **kw: api.rms_norm_grad(matrix(i), matrix(i), matrix(i), vector(i), Tensor((2, 16), torch.float32, i), **kw),
-    "fo_decode_8bit": lambda i, **kw: api.decode_8bit(*codes(i), **kw),
-    "fo_orthogonalize": lambda i, **kw: api.orthogonalize([Tensor((9, 5), torch.float32, i)] * 2, **kw),
-}
-
-
-@pytest.mark.parametrize("name", CALLS)
-@pytest.mark.parametrize("index", [0, 1])
-@pytest.mark.parametrize("stream", [None, 77])
-def test_the_tensors_device_is_current(monkeypatch, name, index, stream):
-    machine = Stand(monkeypatch)
-    CALLS[name](index, stream=stream)
-    assert machine.calls == [(name, index, stream or 0)]
-    assert set(machine.allocated) == {index} and machine.current == 0
-
-
-def test_mixed_devices_are_refused(monkeypatch):
-    machine = Stand(monkeypatch)
-    for call in (lambda: api.embedding(ids(0), Tensor((10, 64), torch.float32, 1)), lambda: api.embedding_grad(matrix(1), ids(0), 10),
-                 lambda: api.rms_norm(matrix(0), matrix(1), vector(0)), lambda: api.rms_norm(matrix(0), None, vector(1)),
-                 lambda: api.rms_norm_grad(matrix(1), None, matrix(0), vector(0), Tensor((2, 16), torch.float32, 0)),
-                 lambda: api.decode_8bit(codes(0)[0], codes(1)[1]),
-                 lambda: api.orthogonalize([Tensor((9, 5), torch.float32, i) for i in (0, 1)])):
+def test_the_compiled_binding_refuses_what_is_no_device_tensor():
+    """Checks that come before any call of the library."""
+    x, ids, w = torch.ones(2, 4), torch.zeros(2, dtype=torch.int32), torch.ones(4)
+    q = torch.zeros(2, 4, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    for call in (lambda: api.embedding(ids, x), lambda: api.embedding_grad(x, ids, 3), lambda: api.rms_norm(x, None, w),
+                 lambda: api.rms_norm(x.half(), None, w), lambda: api.rms_norm_8bit(x, None, w), lambda: api.rms_norm_grad(x, None, x, w, w),
+                 lambda: api.decode_8bit(q, ids), lambda: api.orthogonalize(x), lambda: api.orthogonalize([x], out=[x, x]),
+                 lambda: api.orthogonalize([x], coefficients=(1.0, 2.0)), lambda: api.muon_step([x], [x, x], [x], 0.1),
+                 lambda: api.muon_step([x], [x], [x], 0.1, scales=[1.0, 2.0])):
         with pytest.raises(ValueError):
             call()
-    assert machine.calls == [] and machine.current == 0
+    for call in (lambda: api.embedding(3, x), lambda: api.rms_norm("x", None, w), lambda: api.orthogonalize([1.0]),
+                 lambda: api.orthogonalize([x], steps="5", eps=None)):
+        with pytest.raises((TypeError, ValueError)):
+            call()
+    assert api.orthogonalize([]) == [] and api.muon_step([], [], [], 0.1) is None
 
 
-def test_matrix_updates_are_laid_out_as_the_library_reads_them(monkeypatch):
-    """The binding fills the items as 64-bit words."""
+def test_matrix_updates_have_the_headers_layout():
     import ctypes as C
-    machine, seen = Stand(monkeypatch), []
-
-    def call(items, n, *rest):
-        seen.extend((api.fo_matrix_update * n).from_address(items))
-        machine.copy = [{f: getattr(m, f) for f, _ in m._fields_} for m in seen]
-        return api.OK
-
-    monkeypatch.setattr(Stand, "fo_orthogonalize", staticmethod(call), raising=False)
-    shapes = [(9, 5), (7, 30)]
-    p, g, m = ([Tensor(s, torch.float32, 0) for s in shapes] for _ in range(3))
-    api.muon_step(p, g, m, lr=0.5, scales=[3.0, -0.25])
-    assert C.sizeof(api.fo_matrix_update) == 88
-    for got, (rows, cols), step in zip(machine.copy, shapes, (1.5, -0.125)):
-        assert got == dict(rows=rows, cols=cols, grad=4096, momentum=4096, out=None, param=4096, grad_stride=cols, momentum_stride=cols,
-                           out_stride=0, param_stride=cols, step=step)
-    for bad in (lambda: api.muon_step(p, g[:1], m, 0.1), lambda: api.muon_step(p, g, m, 0.1, scales=[1.0]),
-                lambda: api.orthogonalize(g, coefficients=(1.0, 2.0))):
-        with pytest.raises(ValueError):
-            bad()
+    assert C.sizeof(api.fo_matrix_update) == 88 and api.fo_matrix_update.grad.offset == 16 and api.fo_matrix_update.step.offset == 80
 
 
 def items(*sizes, **over):
