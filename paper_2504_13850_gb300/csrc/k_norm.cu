@@ -316,7 +316,7 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_k(const __grid_constant__ No
     }
     a = WARP ? warp_sum(a) : block_sum(a, box[turn]);
     turn ^= 1;
-    const float k = -r * r * r * (a * p.inv_cols);
+    const float k = -r * r * (a * r * p.inv_cols);     // r^3 alone leaves fp32 where its products do not
     if (VEC && ds) ring.get(n, 2, p.cols, t, G, THREADS, d);
 #pragma unroll
     for (int i = 0; i < 8 * NV; ++i) {
@@ -363,7 +363,7 @@ __global__ void __launch_bounds__(1024) norm_bwd_wide_k(const __grid_constant__ 
       out[c] = fmaf(g, z * r, out[c]);
       a = fmaf(g * to_f(w[c]), z, a);
     }
-    const float k = -r * r * r * (block_sum(a, box[turn]) * p.inv_cols);
+    const float k = -r * r * (block_sum(a, box[turn]) * r * p.inv_cols);
     turn ^= 1;
     for (int c = t; c < p.cols; c += G) {
       float g = fmaf(to_f(dy[c]) * to_f(w[c]), r, to_f(s[c]) * k);

@@ -167,6 +167,22 @@ def test_rows_without_size_and_not_finite():
 
 
 @pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("cols", [40, 45, 512, 2048, 17000])
+def test_magnitudes_whose_r_cubed_leaves_fp32(dtype, cols):
+    """Rows of 1e-16, 1e15 and zeros: r^3 is up to 1e51 and down to 1e-45, the
+    gradient's terms are all within fp32."""
+    x, r, w, dy, ds = make(9, cols, dtype, dtype)
+    for rows, size in ((slice(0, 3), 1e-16), (slice(3, 6), 1e15), (slice(6, 7), 0.0)):
+        x[rows] *= size
+        r[rows] *= size
+        ds[rows] /= size or 1.0
+    got = api.rms_norm(x, r, w, eps=1e-34)
+    assert forward_agrees(got, x, r, w, eps=1e-34)
+    for h in (ds, None):
+        assert gradient_agrees(api.rms_norm_grad(dy, h, got[1], w, got[2]), dy, h, got[1], w, got[2])
+
+
+@pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("cols,pad,skip", [(64, 8, 0), (64, 8, 8), (64, 3, 1), (13, 5, 2), (2048, 8, 0), (2048, 1, 1)])
 def test_row_strides(dtype, cols, pad, skip):
     rows = 37
