@@ -572,7 +572,8 @@ FO_API int fo_decode_8bit(const uint8_t* q, const uint8_t* scales, void* y, int6
  * ones (2^-22), with fp32 sums; a singular value t above 16 on the way, or
  * c1 t^2 + c2 t^4 beyond +-255, overflows.  An infinity or NaN in U makes all of X NaN.  The order of all sums
  * is fixed.  Sides of 0 to 32768 (the smaller) and 2^20.  What one matrix writes
- * is none of another's tensors (equal addresses are refused).
+ * is none of another's tensors, and out, momentum and param are three (equal
+ * addresses are refused, but for out and the same matrix's grad).
  * ---------------------------------------------------------------------- */
 typedef struct fo_matrix_update {
   int64_t rows, cols;

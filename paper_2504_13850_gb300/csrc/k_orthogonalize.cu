@@ -44,7 +44,10 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <functional>
+#include <new>
 #include <string>
+#include <vector>
 
 namespace fo {
 int report_error(int code, const std::string& msg);
@@ -1118,6 +1121,27 @@ int64_t tiles_of(int64_t mt) { return (mt + 1) / 2 * ((mt + 1) / 2 + 1); }
 int most_shares(int64_t mt) { return tiles_of(mt) <= 38 ? kMaxShares : 1; }
 int64_t shared_bytes(int64_t mt) { return tiles_of(mt) * (most_shares(mt) - 1) * 16 * 8192; }
 
+// Matrices are worked on at the same time, and a gradient is read twice, around
+// the momentum's update: every written address is there once, and no gradient
+// but its own matrix's out is one.
+bool apart(const fo_matrix_update* items, int count) {
+  std::vector<const void*> written;
+  written.reserve(size_t(count) * 3);
+  auto there = [](const fo_matrix_update& m) { return m.rows > 0 && m.cols > 0; };
+  for (int i = 0; i < count; ++i)
+    if (there(items[i]))
+      for (const void* w : {static_cast<const void*>(items[i].out), static_cast<const void*>(items[i].momentum),
+                            static_cast<const void*>(items[i].param)})
+        if (w) written.push_back(w);
+  std::sort(written.begin(), written.end(), std::less<const void*>());
+  if (std::adjacent_find(written.begin(), written.end()) != written.end()) return false;
+  for (int i = 0; i < count; ++i)
+    if (there(items[i]) && items[i].grad != items[i].out &&
+        std::binary_search(written.begin(), written.end(), items[i].grad, std::less<const void*>()))
+      return false;
+  return true;
+}
+
 bool is_small(const fo_matrix_update& m) {
   const int64_t lo = m.rows < m.cols ? m.rows : m.cols, hi = m.rows < m.cols ? m.cols : m.rows;
   return lo <= kSmallRows && hi <= kSmallCols * kSmallCtas;
@@ -1296,10 +1320,11 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
                        (m.param && m.param_stride < m.cols)))
       return bad("bad row stride");
     if (!(std::fabs(m.step) <= 1e30f)) return bad("bad step");
-    // matrices of one launch are worked on at the same time
-    for (int k = i / kItems * kItems; k < i; ++k)
-      if ((m.out && m.out == items[k].out) || (m.momentum && m.momentum == items[k].momentum) || (m.param && m.param == items[k].param))
-        return bad("a tensor to write stands twice in the list");
+  }
+  try {
+    if (!apart(items, count)) return bad("a tensor to write stands twice in the list, or is another's gradient");
+  } catch (const std::bad_alloc&) {
+    return report_error(FO_ERR_OOM, "orthogonalize: no host memory");
   }
   const int64_t need = fo_orthogonalize_workspace(items, count, dtype);
   if (need > 0 && (!workspace || odd(workspace, 256) || workspace_bytes < need))

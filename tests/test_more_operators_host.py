@@ -151,6 +151,20 @@ def test_a_tensor_to_write_twice_is_refused(field):
     assert orthogonalize(a) == api.ERR_ARG and "twice" in api.last_error()
 
 
+@pytest.mark.parametrize("to,name,what", [(39, "out", 0), (39, "grad", 0), (0, "grad", 39), (5, "momentum", 5), (7, "param", 7), (7, "param", 30)])
+def test_tensors_written_by_another_place_of_the_list_are_refused(to, name, what):
+    """out of matrix `what` as `name` of matrix `to`, launches apart or the same; a
+    matrix's own grad may be its out."""
+    a = items(*[(4, 4)] * 40, out_stride=4, momentum_stride=4, param_stride=4)
+    for k, it in enumerate(a):
+        it.grad, it.out, it.momentum, it.param = (P + 4096 * (4 * k + j) for j in range(4))
+    assert orthogonalize(a, workspace=None) == api.ERR_ARG and "workspace" in api.last_error()
+    a[3].out = a[3].grad
+    assert orthogonalize(a, workspace=None) == api.ERR_ARG and "workspace" in api.last_error()
+    setattr(a[to], name, a[what].out)
+    assert orthogonalize(a, workspace=None) == api.ERR_ARG and "twice" in api.last_error()
+
+
 @pytest.mark.parametrize("over,what", [
     ({"dtype": 2}, "dtype"), ({"steps": 0}, "steps"), ({"steps": 65}, "steps"), ({"coefficients": None}, "coefficients"), ({"eps": 0.0}, "eps"),
     ({"mu": -0.1}, "momentum"), ({"mu": float("nan")}, "momentum"), ({"decay": float("inf")}, "decay"), ({"workspace": None}, "workspace"),
