@@ -87,6 +87,24 @@ def test_values(dtype, rows, cols):
     assert agrees(api.orthogonalize(u), u)
 
 
+@pytest.mark.parametrize("rows,cols", [(2400, 2400), (2600, 2500), (2900, 2900)])
+def test_more_tiles_than_pairs(rows, cols):
+    """100, 110 and (of X X^T) 78 tiles of 256 x 256 for 76 pairs, some of them
+    beyond the matrix's edge by half."""
+    u = make(rows, cols, BF)
+    assert agrees(api.orthogonalize(u), u)
+
+
+def test_more_tiles_than_pairs_of_several_matrices():
+    """96 tiles of C X.  The second's and third's sums of X X^T are shared by several
+    pairs where they have the device to themselves (12 and 20 tiles of 128 columns
+    for 76 pairs), and are taken in another order here."""
+    us = [make(r, c, BF, seed=k) for k, (r, c) in enumerate([(1500, 1700), (700, 2400), (1300, 1000), (40, 50)])]
+    for k, (u, x) in enumerate(zip(us, api.orthogonalize(us))):
+        assert agrees(x, u)
+        assert k in (1, 2) or torch.equal(x, api.orthogonalize(u))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF])
 @pytest.mark.parametrize("rows,cols", [(300, 300), (260, 700), (700, 260)])
 def test_places(dtype, rows, cols):
