@@ -154,6 +154,46 @@ def test_equal_calls_give_equal_bits_and_tokens_order_is_kept():
         assert torch.equal(api.embedding_grad(dout, ids, 50), first)
 
 
+def test_sorts_give_equal_bits():
+    """8192 tokens are sorted by one block where an id and a token's number fit 32
+    bits, else by launches: the same order, so the same sums."""
+    ids, w, dout = make(8192, 300, 24, F32, F32)
+    small, large = api.embedding_grad(dout, ids, 300), api.embedding_grad(dout, ids, 1 << 19)
+    assert torch.equal(large[:300], small) and float(large[300:].abs().max()) == 0
+
+
+@pytest.mark.parametrize("table,dtype", TYPES)
+@pytest.mark.parametrize("T,V,D", [(8192, 3000, 16), (8193, 3000, 16), (16385, 1, 8), (17000, 40, 9), (24576, 511, 32), (40000, 512, 8), (65536, 100000, 40), (131071, 3000, 16),
+                                   (131072, 30522, 8), (131073, 30522, 8), (300000, 700, 17), (300, 1 << 26, 1), (1, (1 << 27) + 1, 2)])
+def test_many_tokens_and_rows(table, dtype, T, V, D):
+    """More tokens, or larger ids, than one block sorts."""
+    ids, w, dout = make(T, V, D, table, dtype, id_type=torch.int64 if V % 2 else torch.int32)
+    over = torch.full((V, D), float("nan"), device="cuda", dtype=table)
+    got = api.embedding_grad(dout, ids, V, scale=0.5, out=over)
+    if V > 1 << 20:                                      # few rows have tokens: only those in 64 bits
+        rows, back = ids.clamp(min=0).long().unique(return_inverse=True)
+        part = torch.where(ids < 0, -1, back)
+        assert grad_agrees(got[rows], dout, part, len(rows), 0.5)
+        got[rows] = 0
+        assert float(got.abs().max()) == 0
+        return
+    assert grad_agrees(got, dout, ids, V, 0.5)
+    before = torch.randn(V, D, device="cuda").to(table)
+    got = api.embedding_grad(dout, ids, V, scale=0.5, out=before.clone(), accumulate=True)
+    assert grad_agrees(got, dout, ids, V, 0.5, before)
+
+
+@pytest.mark.parametrize("T", [20000, 140000])
+@pytest.mark.parametrize("case", ["one id", "runs of 33", "all padding", "ends", "descending", "bad ids"])
+def test_ids_that_fill_large_batches(case, T):
+    V, at = 700, torch.arange(T, device="cuda")
+    ids = {"one id": torch.full((T,), 5, device="cuda"), "runs of 33": at // 33, "all padding": torch.full((T,), -1, device="cuda"),
+           "ends": torch.where(at % 2 == 0, 0, V - 1), "descending": (T - 1 - at) * V // T,
+           "bad ids": torch.where(at % 3 == 0, V + at, torch.where(at % 3 == 1, -at - 1, at % V))}[case]
+    ids, w, dout = make(T, V, 24, F32, F32, ids=ids, id_type=torch.int64)
+    assert grad_agrees(api.embedding_grad(dout, ids, V), dout, ids, V, 1.0)
+
+
 def test_capture_and_other_streams():
     """Captured and replayed on new inputs, beside calls on two other streams."""
     ids, w, dout = make(3000, 500, 96, F32, BF)
