@@ -533,8 +533,9 @@ FO_API int fo_embedding_grad(const void* dout, int64_t dout_stride, int dtype, c
  * columns share the smallest power of two 2^e, -127 <= e <= 127, for which
  * max|y| / 2^e <= 448; scales [rows][ceil(cols / 32)] holds e + 127, q
  * [rows][cols] y / 2^e rounded to 4 exponent and 3 mantissa bits (e4m3).  Its y
- * is not rounded to dtype before.  A group that holds an infinity or NaN has
- * scale 255 and decodes to NaN.
+ * is not rounded to dtype before, and off from the formula's by little more than
+ * fp32's one rounding (infinite weights give NaN in this form's y).  A group that
+ * holds an infinity or NaN has scale 255 and decodes to NaN.
  * rows < 2^31, cols <= 2^20.
  * ---------------------------------------------------------------------- */
 FO_API int fo_rms_norm(const void* x, int64_t x_stride, const void* residual, int64_t residual_stride, const void* weight,

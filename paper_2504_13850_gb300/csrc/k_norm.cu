@@ -29,7 +29,7 @@ struct NormParams {
   float* rstd;
   int64_t ldx, ldr, lds, ldy;
   int rows, cols;
-  float eps, inv_cols;
+  float eps, inv_cols, inv_rest;       // 1 / cols, and what its rounding left
 };
 struct NormGradParams {
   const void *dy, *ds, *s, *w;
@@ -97,6 +97,80 @@ __device__ __forceinline__ float up_by(int biased) {   // 2^-(biased - 127)
 }
 __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// The 8-bit form rounds y where its neighbours are 2^-4 apart, and an error of fp32's
+// size on the way would now and then round it to the other side (two or three of the
+// 33 million elements of 16384 x 2048).  For it y is rounded once, and the joined sum
+// of squares and r are held as two numbers, the second what rounding left of the first
+// (the products and sums whose rounding is asked for are not to be contracted): 45
+// instead of 41 us.  The threads' and warps' own sums stay single, their errors are
+// many and of either sign; with them in two numbers it takes 59 us.
+struct Two {
+  float hi, lo;
+  __device__ __forceinline__ void add(float x) {
+    const float s = __fadd_rn(hi, x), b = __fsub_rn(s, hi);
+    lo += __fsub_rn(hi, __fsub_rn(s, b)) + __fsub_rn(x, b);
+    hi = s;
+  }
+  __device__ __forceinline__ void over_warp() {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) {
+      const float h = __shfl_xor_sync(0xffffffffu, hi, o), l = __shfl_xor_sync(0xffffffffu, lo, o);
+      lo += l;             // the same in both lanes, as what add() adds is
+      add(h);
+    }
+  }
+  __device__ __forceinline__ void over_block(float* box) {
+    const float mine = warp_sum(hi + lo);
+    if (threadIdx.x % 32 == 0) box[threadIdx.x / 32] = mine;
+    __syncthreads();
+    hi = box[0];
+    lo = 0.f;
+    // not unrolled: 48 us
+#pragma unroll 1
+    for (unsigned w = 1; w < blockDim.x / 32; ++w) add(box[w]);
+  }
+};
+__device__ __forceinline__ float finite_or_zero(float x) { return fabsf(x) < INFINITY ? x : 0.f; }
+// (sum / cols + eps)^(-1/2)
+__device__ __forceinline__ Two root_of(Two sum, float inv_cols, float inv_rest, float eps) {
+  sum.lo = finite_or_zero(sum.lo);       // beside an infinity
+  Two m = {__fmul_rn(sum.hi, inv_cols), 0.f};
+  m.lo = fmaf(sum.hi, inv_cols, -m.hi) + fmaf(sum.lo, inv_cols, sum.hi * inv_rest);
+  m.add(eps);
+  const float r = __frsqrt_rn(m.hi), q = __fmul_rn(r, r);
+  const float off = fmaf(-m.hi, q, 1.f) - fmaf(m.hi, fmaf(r, r, -q), m.lo * q);
+  return {r, finite_or_zero(0.5f * r * off)};
+}
+// Two products or sums in one instruction.
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+  uint64_t p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(a), "f"(b));
+  return p;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t p;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(p) : "l"(a), "l"(b));
+  return p;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t p;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(p) : "l"(a), "l"(b), "l"(c));
+  return p;
+}
+// v r w of two elements, rounded once: v r as h + l.  An infinite weight gives NaN.
+__device__ __forceinline__ void scale_pair(float* v, const Two& r, const float* w) {
+  const uint64_t x = pair_of(v[0], v[1]), m = pair_of(w[0], w[1]), hi = pair_of(r.hi, r.hi);
+  const uint64_t h = mul2(x, hi), minus = mul2(x, pair_of(-r.hi, -r.hi));
+  const uint64_t l = fma2(x, pair_of(r.lo, r.lo), fma2(x, hi, minus)), y = fma2(h, m, mul2(l, m));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(v[0]), "=f"(v[1]) : "l"(y));
+}
+__device__ __forceinline__ float scaled(float v, const Two& r, float w) {
+  float x[2] = {v, 0.f};
+  const float m[2] = {w, 0.f};
+  scale_pair(x, r, m);
+  return x[0];
+}
+
 // y of one row as 8-bit floats.  The 32 columns of a block are four
 // neighbouring lanes' chunk (VEC) or one element of each lane of a warp.
 template <bool VEC, int NV>
@@ -141,7 +215,7 @@ __device__ __forceinline__ void store_eight(const NormParams& p, int row, int t,
 }
 
 // One row per warp (WARP) or per block; 8 NV elements per thread.
-template <typename T, typename W, int NV, bool VEC, bool WARP, int THREADS>
+template <typename T, typename W, int NV, bool VEC, bool WARP, int THREADS, bool EIGHT>
 __global__ void __launch_bounds__(THREADS) norm_fwd_k(const __grid_constant__ NormParams p) {
   __shared__ float box[32];
   pdl_wait();
@@ -158,18 +232,32 @@ __global__ void __launch_bounds__(THREADS) norm_fwd_k(const __grid_constant__ No
     for (int i = 0; i < 8 * NV; ++i) v[i] = to_f(from_f<T>(v[i] + z[i]));
   }
   if (p.s) store_row<T, VEC, NV>(static_cast<T*>(p.s) + row * p.lds, p.cols, t, G, v);
-  float a = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8 * NV; ++i) a = fmaf(v[i], v[i], a);
-  a = WARP ? warp_sum(a) : block_sum(a, box);
-  const float r = __frsqrt_rn(fmaf(a, p.inv_cols, p.eps));
-  if (p.rstd && t == 0) p.rstd[row] = r;
   float w[8 * NV];
-  load_row<W, VEC, NV>(static_cast<const W*>(p.w), p.cols, t, G, w);
+  if constexpr (EIGHT) {
+    float a[4] = {};
 #pragma unroll
-  for (int i = 0; i < 8 * NV; ++i) v[i] = v[i] * r * w[i];
+    for (int i = 0; i < 8 * NV; ++i) a[i % 4] = fmaf(v[i], v[i], a[i % 4]);
+    Two sum = {(a[0] + a[1]) + (a[2] + a[3]), 0.f};
+    if (WARP) sum.over_warp();
+    else sum.over_block(box);
+    const Two r = root_of(sum, p.inv_cols, p.inv_rest, p.eps);
+    if (p.rstd && t == 0) p.rstd[row] = r.hi;
+    load_row<W, VEC, NV>(static_cast<const W*>(p.w), p.cols, t, G, w);
+#pragma unroll
+    for (int i = 0; i < 8 * NV; i += 2) scale_pair(v + i, r, w + i);
+  } else {
+    float a = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8 * NV; ++i) a = fmaf(v[i], v[i], a);
+    a = WARP ? warp_sum(a) : block_sum(a, box);
+    const float r = __frsqrt_rn(fmaf(a, p.inv_cols, p.eps));
+    if (p.rstd && t == 0) p.rstd[row] = r;
+    load_row<W, VEC, NV>(static_cast<const W*>(p.w), p.cols, t, G, w);
+#pragma unroll
+    for (int i = 0; i < 8 * NV; ++i) v[i] = v[i] * r * w[i];
+  }
   if (p.y) store_row<T, VEC, NV>(static_cast<T*>(p.y) + row * p.ldy, p.cols, t, G, v);
-  if (p.q) store_eight<VEC, NV>(p, row, t, G, v);
+  if constexpr (EIGHT) store_eight<VEC, NV>(p, row, t, G, v);
 }
 
 // Rows wider than the registers of a block: two passes over each row.
@@ -184,19 +272,20 @@ __global__ void __launch_bounds__(1024) norm_fwd_wide_k(const __grid_constant__ 
   T *s = static_cast<T*>(p.s), *y = static_cast<T*>(p.y);
   if (s) s += row * p.lds;
   if (y) y += row * p.ldy;
-  float a = 0.f;
+  Two sum = {};
   for (int c = t; c < p.cols; c += G) {
     float v = to_f(x[c]);
     if (res) v = to_f(from_f<T>(v + to_f(res[c])));
     if (s) s[c] = from_f<T>(v);
-    a = fmaf(v, v, a);
+    sum.add(v * v);
   }
-  const float r = __frsqrt_rn(fmaf(block_sum(a, box), p.inv_cols, p.eps));
-  if (p.rstd && t == 0) p.rstd[row] = r;
+  sum.over_block(box);
+  const Two r = root_of(sum, p.inv_cols, p.inv_rest, p.eps);
+  if (p.rstd && t == 0) p.rstd[row] = r.hi;
   const T* from = s ? s : x;        // each thread reads what it wrote
   const int blocks = (p.cols + 31) / 32;
   for (int c = t; c < 32 * blocks; c += G) {     // whole warps
-    const float v = c < p.cols ? to_f(from[c]) * r * to_f(static_cast<const W*>(p.w)[c]) : 0.f;
+    const float v = c < p.cols ? scaled(to_f(from[c]), r, to_f(static_cast<const W*>(p.w)[c])) : 0.f;
     if (y && c < p.cols) y[c] = from_f<T>(v);
     if (p.q) {
       const int b = block_exponent(__reduce_max_sync(0xffffffffu, magnitude(v)));
@@ -468,19 +557,23 @@ int grad_blocks(int rows, int cols) {
   return want < most ? want : most;
 }
 
-template <typename T, typename W, bool VEC>
-cudaError_t forward(const NormParams& p, cudaStream_t st) {
+template <typename T, typename W, bool VEC, bool EIGHT>
+cudaError_t forward_rows(const NormParams& p, cudaStream_t st) {
   const RowShape a = row_shape(p.cols);
   const int per = a.warp ? a.threads / 32 : 1;
   const dim3 grid(unsigned((int64_t(p.rows) + per - 1) / per)), block(unsigned(a.threads));
-  auto k = p.cols <= 256     ? norm_fwd_k<T, W, 1, VEC, true, 256>
-           : p.cols <= 512   ? norm_fwd_k<T, W, 2, VEC, true, 256>
-           : p.cols <= 1024  ? norm_fwd_k<T, W, 4, VEC, true, 256>
-           : p.cols <= 4096  ? norm_fwd_k<T, W, 2, VEC, false, 256>
-           : p.cols <= 8192  ? norm_fwd_k<T, W, 2, VEC, false, 512>
-           : p.cols <= 16384 ? norm_fwd_k<T, W, 2, VEC, false, 1024>
+  auto k = p.cols <= 256     ? norm_fwd_k<T, W, 1, VEC, true, 256, EIGHT>
+           : p.cols <= 512   ? norm_fwd_k<T, W, 2, VEC, true, 256, EIGHT>
+           : p.cols <= 1024  ? norm_fwd_k<T, W, 4, VEC, true, 256, EIGHT>
+           : p.cols <= 4096  ? norm_fwd_k<T, W, 2, VEC, false, 256, EIGHT>
+           : p.cols <= 8192  ? norm_fwd_k<T, W, 2, VEC, false, 512, EIGHT>
+           : p.cols <= 16384 ? norm_fwd_k<T, W, 2, VEC, false, 1024, EIGHT>
                              : norm_fwd_wide_k<T, W>;
   return launch_k(k, grid, block, 0, st, p);
+}
+template <typename T, typename W, bool VEC>
+cudaError_t forward(const NormParams& p, cudaStream_t st) {
+  return p.q ? forward_rows<T, W, VEC, true>(p, st) : forward_rows<T, W, VEC, false>(p, st);
 }
 // The gradient's kernel, launched with its shared memory.
 template <typename T, typename W, int NV, bool VEC, bool WARP, int THREADS, int STAGES>
@@ -579,6 +672,7 @@ int fo_rms_norm(const void* x, int64_t x_stride, const void* residual, int64_t r
   p.cols = int(cols);
   p.eps = float(eps);
   p.inv_cols = float(1.0 / double(cols));
+  p.inv_rest = float(1.0 / double(cols) - double(p.inv_cols));
   const bool vec = cols % 8 == 0 && wide_rows(x, x_stride, dtype, rows) && aligned16(weight) &&
                    (!residual || wide_rows(residual, residual_stride, dtype, rows)) &&
                    (!sum || wide_rows(sum, sum_stride, dtype, rows)) && (!y || wide_rows(y, y_stride, dtype, rows)) &&

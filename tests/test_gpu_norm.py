@@ -121,6 +121,28 @@ def test_eight_bits(dtype, weight, rows, cols):
         assert torch.equal(api.decode_8bit(q, scales, dtype=t), (q.float().double() * unit).to(t))
 
 
+@pytest.mark.parametrize("dtype,weight", TYPES)
+@pytest.mark.parametrize("rows,cols", [(4000, 512), (3000, 777), (1000, 2048), (700, 1536), (100, 20000)])
+def test_eight_bits_round_as_64_bits_do(dtype, weight, rows, cols):
+    """The sum of squares has at most 11 roundings one after another (10 in a thread of a
+    warp's row; 4 and 2 in a thread and 5 in a warp of a block's; one and 5 in a wide
+    row's), all of one sign, the rest is exact to less than 2^-24, and y is rounded once:
+    y is off by (11 / 2 + 2) 2^-24, and its code is one of those at either end."""
+    x, r, w, _, _ = make(rows, cols, dtype, weight, seed=11)
+    eps = 2.0 ** -20
+    q, scales, _ = api.rms_norm_8bit(x, r, w, eps=eps)
+    Y = forward(x, r, w, eps)[1]
+    pad = torch.nn.functional.pad(Y, (0, -cols % 32)).view(rows, -1, 32)
+    mantissa, k = torch.frexp(pad.abs().amax(2))           # top = mantissa 2^k, mantissa in 0.5 .. 1
+    k = (k - 9 + (mantissa > 0.875).int()).clamp(-127, 127)
+    assert torch.equal(scales, (k + 127).to(torch.uint8))
+    unit = torch.pow(2.0, k.double()).repeat_interleave(32, 1)[:, :cols]
+    e = (11 / 2 + 2) * U
+    ends = [(Y / unit * (1 + sign * e)).float().to(torch.float8_e4m3fn).float() for sign in (-1, 1)]
+    got = q.float()
+    assert bool(((got == ends[0]) | (got == ends[1])).all())
+
+
 def test_eight_bit_limits():
     """Zeros, magnitudes at both ends of the exponents, and groups that hold an
     infinity or NaN."""
