@@ -22,7 +22,13 @@
 // of it in the product, 0.7e-3 without a, 0.5e-3 without the diagonal; 16 x 300
 // 2.1, 1.4 and 0.6e-3).  For fp32 matrices
 // all operands are such pairs, and each product three (hi lo, lo hi, hi hi, in
-// this order; the fourth is below fp32's rounding).  Sums are fp32 in tensor
+// this order; the fourth is below fp32's rounding).  The second number is held
+// 2^11 times its size, or it would be subnormal where the first is small: an
+// element of X is off by 2^-23 of itself or 2^-46, whichever is more (2^-35 without:
+// a row of a 512 x 2048 matrix at 1e-5 of the others was off by 1.9e-3 of itself).
+// The tensor cores take the sum of the two mixed products times 2^-11 as they begin
+// the third.
+// Sums are fp32 in tensor
 // memory; because the tensor cores truncate, those of fp32 matrices are moved to
 // registers and added there, rounded, every 64 terms (512: 7e-6 off instead of
 // 1.5e-6 on matrices of width 512, torch's fp32 products 2.3e-6).
@@ -60,6 +66,8 @@ constexpr int kItems = 32;                    // matrices per launch
 constexpr int kBlock = 8192;                  // bytes of a 64 x 64 block
 constexpr int kMaxSums = 1024;                // partial sums of squares per matrix
 constexpr float kUpX = 1024.f, kUpA = 256.f;  // what X, and A and C, are multiplied by as fp16
+constexpr int kLowBits = 11;                  // and the second number of a pair by 2^11 more
+constexpr float kUpLow = 1 << kLowBits, kDownLow = 1.f / kUpLow;
 
 struct Item {
   const void* g;            // [rows][cols] gradient
@@ -250,15 +258,17 @@ __device__ __forceinline__ uint32_t half_pair(float a, float b) {
 __device__ __forceinline__ float2 of_pair(uint32_t w) {
   return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
-// Eight values as fp16; v keeps what they leave.
+// Eight values' first (PART 0) or second number as fp16; v keeps what it leaves.
+template <int PART>
 __device__ __forceinline__ uint4 take_half8(float* v) {
+  constexpr float up = PART ? kUpLow : 1.f, down = PART ? kDownLow : 1.f;
   uint32_t w[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    w[e] = half_pair(v[2 * e], v[2 * e + 1]);
+    w[e] = half_pair(v[2 * e] * up, v[2 * e + 1] * up);
     const float2 f = of_pair(w[e]);
-    v[2 * e] -= f.x;
-    v[2 * e + 1] -= f.y;
+    v[2 * e] = fmaf(-down, f.x, v[2 * e]);
+    v[2 * e + 1] = fmaf(-down, f.y, v[2 * e + 1]);
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
@@ -293,8 +303,8 @@ __global__ void __launch_bounds__(256) ortho_pack_k(const __grid_constant__ Orth
     float z[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) z[e] = (it.transposed ? tile[8 * u + e][row] : v[h][e]) * scale.x * scale.y;
-    *reinterpret_cast<uint4*>(img + at) = take_half8(z);
-    *reinterpret_cast<uint4*>(img + image + at) = take_half8(z);
+    *reinterpret_cast<uint4*>(img + at) = take_half8<0>(z);
+    *reinterpret_cast<uint4*>(img + image + at) = take_half8<1>(z);
   }
 }
 
@@ -369,6 +379,22 @@ __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uin
       " @q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
       "l"(a), "l"(b), "r"(idesc), "r"(acc)
       : "memory");
+}
+// d <- a b + 2^-kLowBits d, of a pair of CTAs or of one.
+template <int CTAS>
+__device__ __forceinline__ void mma_onto_low(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc) {
+  if constexpr (CTAS == 2)
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.eq.b32 p, 0, 0;\n elect.sync _|q, 0xffffffff;\n"
+        " @q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p, %4;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "n"(kLowBits)
+        : "memory");
+  else
+    asm volatile(
+        "{\n .reg .pred p, q;\n setp.eq.b32 p, 0, 0;\n elect.sync _|q, 0xffffffff;\n"
+        " @q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p, %4;\n}\n" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "n"(kLowBits)
+        : "memory");
 }
 __device__ __forceinline__ void commit_pair(uint64_t* bar, uint32_t leader) {     // the barrier of both CTAs
   asm volatile(
@@ -483,6 +509,7 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
     if (lane == 0) bulk_wait_read<0>();       // the last store has read the buffer
 #pragma unroll
     for (int part = kParts - 1; part >= 0; --part) {
+      const float factor = part ? linear * kDownLow : linear;
       __syncwarp();
 #pragma unroll
       for (int k = 0; k < 8; ++k) st_shared4(buf + (32 * k + lane) * 16, w[part][k].x, w[part][k].y, w[part][k].z, w[part][k].w);
@@ -495,8 +522,8 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
         for (int e = 0; e < 4; ++e) {
           const float2 f = of_pair(__float_as_uint(z[e]));
           float &x = v[8 * k + 2 * e], &y = v[8 * k + 2 * e + 1];
-          x = fmaf(linear, f.x, part == kParts - 1 ? x * other : x);
-          y = fmaf(linear, f.y, part == kParts - 1 ? y * other : y);
+          x = fmaf(factor, f.x, part == kParts - 1 ? x * other : x);
+          y = fmaf(factor, f.y, part == kParts - 1 ? y * other : y);
         }
       }
     }
@@ -526,7 +553,7 @@ __device__ __forceinline__ void finish(const OrthoParams& p, const Item& m, int 
     __syncwarp();
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      const uint4 w = take_half8(v + 8 * k);
+      const uint4 w = part ? take_half8<1>(v + 8 * k) : take_half8<0>(v + 8 * k);
       st_shared4(buf + lane * 128 + (k ^ (lane & 7)) * 16, w.x, w.y, w.z, w.w);
     }
     fence_proxy_async_smem();
@@ -685,8 +712,10 @@ __device__ __forceinline__ void product_tiles(const OrthoParams& p, int pairs_of
           }
         }
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          mma_pair(d, desc(k * as, al), desc(b0 + k * bs, bl), idesc, PARTS == 2 || kb > 0 || k > 0 ? 1u : 0u);
+        for (int k = 0; k < 4; ++k) {
+          if (PARTS == 2 && k == 0) mma_onto_low<2>(d, desc(0, al), desc(b0, bl), idesc);
+          else mma_pair(d, desc(k * as, al), desc(b0 + k * bs, bl), idesc, PARTS == 2 || kb > 0 || k > 0 ? 1u : 0u);
+        }
         commit_pair(&empty[at.at], leader);
         at.step();
         if (PARTS == 2 || kb + 1 == a.kb) {
@@ -834,7 +863,7 @@ __device__ __forceinline__ void put_row(uint32_t at, uint32_t part, int row, int
   for (int q = 0; q < PARTS; ++q)
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const uint4 w = take_half8(v + 8 * k);
+      const uint4 w = q ? take_half8<1>(v + 8 * k) : take_half8<0>(v + 8 * k);
       st_shared4(at + q * part + row * 128 + ((first + k) ^ (row & 7)) * 16, w.x, w.y, w.z, w.w);
     }
 }
@@ -943,14 +972,14 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
     for (int k = 0; k < 8; ++k) u[i][k] = u[i][k] * scale.x * scale.y;
     if (!m.transposed) {
       const uint32_t at = sx + (lo / 8) * 2 * kBlock + hi * 128 + ((lo % 8) ^ (hi & 7)) * 16;
-      uint4 w = take_half8(u[i]);
+      uint4 w = take_half8<0>(u[i]);
       st_shared4(at, w.x, w.y, w.z, w.w);
-      w = take_half8(u[i]);
+      w = take_half8<1>(u[i]);
       st_shared4(at + kSmallX, w.x, w.y, w.z, w.w);
     } else {
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const __half h = __float2half_rn(u[i][k]), l = __float2half_rn(u[i][k] - __half2float(h));
+        const __half h = __float2half_rn(u[i][k]), l = __float2half_rn((u[i][k] - __half2float(h)) * kUpLow);
         char* at = smem + (lo / 64) * 2 * kBlock + (8 * hi + k) * 128 + ((lo % 64 / 8) ^ k) * 16 + lo % 8 * 2;
         *reinterpret_cast<__half*>(at) = h;
         *reinterpret_cast<__half*>(at + kSmallX) = l;
@@ -973,8 +1002,10 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
       }
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k)
-      mma_ss(d, desc(a + 32 * k, 1u << 16), desc(b + bs * k, bl), idesc, PARTS == 2 || k > 0 ? 1u : 0u);
+    for (int k = 0; k < 4; ++k) {
+      if (PARTS == 2 && k == 0) mma_onto_low<1>(d, desc(a, 1u << 16), desc(b, bl), idesc);
+      else mma_ss(d, desc(a + 32 * k, 1u << 16), desc(b + bs * k, bl), idesc, k > 0 ? 1u : 0u);
+    }
   };
   uint32_t phase = 0;
   auto begin = [&] {                 // what the warps wrote is there for the products
@@ -1084,8 +1115,8 @@ __global__ void __cluster_dims__(kSmallCtas, 1, 1) __launch_bounds__(kSmallThrea
           for (int e = 0; e < 4; ++e) {
             const float2 fh = of_pair(__float_as_uint(zh[e])), fl = of_pair(__float_as_uint(zl[e]));
             float &x = v[8 * k + 2 * e], &y = v[8 * k + 2 * e + 1];
-            x = fmaf(linear, fh.x, fmaf(linear, fl.x, x * (1.f / kUpA)));
-            y = fmaf(linear, fh.y, fmaf(linear, fl.y, y * (1.f / kUpA)));
+            x = fmaf(linear, fh.x, fmaf(linear * kDownLow, fl.x, x * (1.f / kUpA)));
+            y = fmaf(linear, fh.y, fmaf(linear * kDownLow, fl.y, y * (1.f / kUpA)));
           }
         }
         if (step + 1 < steps) put_row<2>(x_block, kSmallX, row, 4 * h, v);
