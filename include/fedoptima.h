@@ -569,8 +569,8 @@ FO_API int fo_decode_8bit(const uint8_t* q, const uint8_t* scales, void* y, int6
  *     out = X;  param <- decay param - step X
  * Coefficients such as (3.4445, -4.7750, 2.0315) bring the singular values into
  * 0.7 .. 1.2 in five steps.  The products run on the tensor cores, on fp16
- * operands for bf16 matrices (roundings of 2^-12) and on pairs of them for fp32
- * ones: an element of X, whose norm is 1 at first, is held to 2^-23 of itself or
+ * operands for bf16 matrices without a param (roundings of 2^-12) and on pairs of
+ * them where grad or param is fp32: an element of X, whose norm is 1 at first, is held to 2^-23 of itself or
  * to 2^-46, whichever is more, so that a row (of the shorter side) below about
  * 1e-6 of the others keeps fewer bits than the rest.  Sums are fp32; a singular
  * value t above 16 on the way, or c1 t^2 + c2 t^4 beyond +-255, overflows.  An

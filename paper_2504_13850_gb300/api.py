@@ -775,7 +775,8 @@ def muon_step(params, grads, momenta, lr, momentum=0.95, nesterov=True, weight_d
     """One optimiser step on weight matrices with orthogonalised momentum, in
     place: m <- momentum m + g; X = orthogonalize(g + momentum m, or m without
     nesterov); p <- (1 - lr weight_decay) p - lr scale X.  params and momenta are
-    fp32, grads fp32 or bf16; scales default to sqrt(max(1, rows / cols))."""
+    fp32, grads fp32 or bf16; X is as exact as fp32 products make it for either;
+    scales default to sqrt(max(1, rows / cols))."""
     if not len(params) == len(grads) == len(momenta):
         raise ValueError("params, grads and momenta: as many of each")
     if len(params) == 0:

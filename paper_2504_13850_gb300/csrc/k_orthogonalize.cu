@@ -20,8 +20,8 @@
 // weak directions that each step multiplies by up to a, and small once the rows
 // are orthogonal (errors before the result's rounding: 512 x 512 2.2e-3 with all
 // of it in the product, 0.7e-3 without a, 0.5e-3 without the diagonal; 16 x 300
-// 2.1, 1.4 and 0.6e-3).  For fp32 matrices
-// all operands are such pairs, and each product three (hi lo, lo hi, hi hi, in
+// 2.1, 1.4 and 0.6e-3).  For fp32 matrices,
+// and for bf16 ones that update parameters, all operands are such pairs, and each product three (hi lo, lo hi, hi hi, in
 // this order; the fourth is below fp32's rounding).  The second number is held
 // 2^11 times its size, or it would be subnormal where the first is small: an
 // element of X is off by 2^-23 of itself or 2^-46, whichever is more (2^-35 without:
@@ -1177,9 +1177,14 @@ bool is_small(const fo_matrix_update& m) {
   const int64_t lo = m.rows < m.cols ? m.rows : m.cols, hi = m.rows < m.cols ? m.cols : m.rows;
   return lo <= kSmallRows && hi <= kSmallCols * kSmallCtas;
 }
+// Operands are pairs where X goes anywhere in fp32: the roundings of single ones are
+// small only beside a result's in bf16 (1e-3 and 1.7e-3; 512 x 768 8e-4 of an update
+// of parameters, with pairs 1e-6).
+bool in_pairs(const fo_matrix_update& m, int dtype) { return dtype == FO_DTYPE_F32 || m.param; }
 // Small matrices: parts of X X^T of even and odd steps, and of the norm.
-int64_t item_bytes(const fo_matrix_update& m, int parts) {
+int64_t item_bytes(const fo_matrix_update& m, int dtype) {
   if (m.rows == 0 || m.cols == 0) return 0;
+  const int parts = in_pairs(m, dtype) ? 2 : 1;
   if (is_small(m)) return 2 * kSmallCtas * kSmallPart + 256;
   const int64_t r = (m.rows + 127) / 128, c = (m.cols + 127) / 128, mt = r < c ? r : c, nt = r < c ? c : r;
   return (2 * mt * nt * 2 + 2 * mt * mt * parts) * 4 * kBlock + shared_bytes(mt) + mt * 512 + kMaxSums * 16 + 16;
@@ -1240,7 +1245,7 @@ int64_t plan(OrthoParams& p) {
 template <int PARTS, int PHASE, typename T>
 cudaError_t product(OrthoParams& p, int pairs, cudaStream_t st) {
   // Wide tiles load fewer bytes per product and take 1.7 times as long as narrow
-  // ones; narrow ones divide the work into twice as many.  fp32 matrices, whose
+  // ones; narrow ones divide the work into twice as many.  Operands in pairs, whose
   // products are three, load few enough with narrow ones, and a wide tile's sums
   // would not fit into the registers.
   if constexpr (PARTS == 1) {
@@ -1269,17 +1274,16 @@ cudaError_t product(OrthoParams& p, int pairs, cudaStream_t st) {
   return launch_product<PARTS, 128, PHASE, T>(p, pairs, st);
 }
 
-template <typename T>
+template <int PARTS, typename T>
 cudaError_t orthogonalize_small(const OrthoParams& p, int steps, cudaStream_t st) {
-  auto k = ortho_small_k<sizeof(T) == 4 ? 2 : 1, T>;
+  auto k = ortho_small_k<PARTS, T>;
   static std::atomic<bool> allowed[kMaxDevices];
   const cudaError_t e = allow_smem(k, allowed);
   if (e != cudaSuccess) return e;
   return launch_k(k, dim3(kSmallCtas * unsigned(p.count)), dim3(kSmallThreads), kSmallSmem, st, p, steps);
 }
-template <typename T>
+template <int PARTS, typename T>
 cudaError_t orthogonalize(OrthoParams& p, int steps, cudaStream_t st) {
-  constexpr int PARTS = sizeof(T) == 4 ? 2 : 1;
   int dev = 0, sms = 1;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
@@ -1319,11 +1323,10 @@ extern "C" {
 
 int64_t fo_orthogonalize_workspace(const fo_matrix_update* items, int count, int dtype) {
   if (check_items(items, count, dtype)) return -1;
-  const int parts = dtype == FO_DTYPE_F32 ? 2 : 1;
   int64_t most = 0;
   for (int i = 0; i < count; i += kItems) {
     int64_t sum = 0;
-    for (int k = i; k < count && k < i + kItems; ++k) sum += item_bytes(items[k], parts);
+    for (int k = i; k < count && k < i + kItems; ++k) sum += item_bytes(items[k], dtype);
     if (sum > most) most = sum;
   }
   return most;
@@ -1360,10 +1363,10 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
   const int64_t need = fo_orthogonalize_workspace(items, count, dtype);
   if (need > 0 && (!workspace || odd(workspace, 256) || workspace_bytes < need))
     return bad("the workspace is missing, misaligned or too small");
-  const int parts = dtype == FO_DTYPE_F32 ? 2 : 1;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   for (int first = 0; first < count; first += kItems)
-   for (const bool small : {true, false}) {
+   for (const bool small : {true, false})
+    for (const bool pairs : {true, false}) {
     OrthoParams p = {};
     p.ws = static_cast<char*>(workspace);
     p.ca = float(coefficients[0]);
@@ -1381,7 +1384,7 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
     };
     for (int i = first; i < count && i < first + kItems; ++i) {
       const fo_matrix_update& m = items[i];
-      if (m.rows == 0 || m.cols == 0 || is_small(m) != small) continue;
+      if (m.rows == 0 || m.cols == 0 || is_small(m) != small || in_pairs(m, dtype) != pairs) continue;
       Item& it = p.item[p.count++];
       it.g = m.grad;
       it.mom = m.momentum;
@@ -1402,8 +1405,8 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
         it.a = take(256);
       } else {
         for (int k = 0; k < 2; ++k) it.x[k] = take(int64_t(it.mt) * it.nt * 4 * kBlock * 2);
-        it.a = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
-        it.c = take(int64_t(it.mt) * it.mt * 4 * kBlock * parts);
+        it.a = take(int64_t(it.mt) * it.mt * 4 * kBlock * (pairs ? 2 : 1));
+        it.c = take(int64_t(it.mt) * it.mt * 4 * kBlock * (pairs ? 2 : 1));
         it.parts = take(shared_bytes(it.mt));
         it.d = take(int64_t(it.mt) * 512);
       }
@@ -1418,8 +1421,10 @@ int fo_orthogonalize(const fo_matrix_update* items, int count, int dtype, int st
     if (p.count == 0) continue;
     p.sums = reinterpret_cast<float4*>(p.ws + at);
     p.scale = reinterpret_cast<float2*>(p.sums + p.count * kMaxSums);
-    const cudaError_t e = small ? (dtype == FO_DTYPE_F32 ? orthogonalize_small<float>(p, steps, st) : orthogonalize_small<bf16>(p, steps, st))
-                          : dtype == FO_DTYPE_F32 ? orthogonalize<float>(p, steps, st) : orthogonalize<bf16>(p, steps, st);
+    const cudaError_t e =
+        dtype == FO_DTYPE_F32 ? (small ? orthogonalize_small<2, float>(p, steps, st) : orthogonalize<2, float>(p, steps, st))
+        : pairs               ? (small ? orthogonalize_small<2, bf16>(p, steps, st) : orthogonalize<2, bf16>(p, steps, st))
+                              : (small ? orthogonalize_small<1, bf16>(p, steps, st) : orthogonalize<1, bf16>(p, steps, st));
     if (e != cudaSuccess) return done(e);
   }
   return FO_OK;
