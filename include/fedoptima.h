@@ -528,7 +528,8 @@ FO_API int fo_embedding_grad(const void* dout, int64_t dout_stride, int dtype, c
  * are device matrices [rows][cols] of dtype with row strides in elements (0
  * broadcasts an input's row); weight is a device vector of dtype or fp32; rstd
  * (NULL: not wanted) receives r, fp32 [rows].  y or sum may be x or residual.
- * Sums are fp32: magnitudes above 1e19 / sqrt(cols) overflow them.
+ * Sums are fp32: magnitudes above 1e19 / sqrt(cols) overflow them, and squares of
+ * those below 1e-19 lose bits (r then has them from eps alone, if that is more).
  * 8-bit form (q and scales, both or neither; y may then be NULL): each 32
  * columns share the smallest power of two 2^e, -127 <= e <= 127, for which
  * max|y| / 2^e <= 448; scales [rows][ceil(cols / 32)] holds e + 127, q
@@ -547,6 +548,7 @@ FO_API int64_t fo_rms_norm_workspace(int64_t rows, int64_t cols);
 /* Gradients of a call whose sum and rstd are s and rstd, from dy = dL/dy and
  * the gradient ds that reaches s by the residual stream (NULL: none):
  *     dx = r (w dy - s r^2 mean(w dy s)) + ds (also the residual's);   dweight = sum over rows of dy s r
+ * taken so that only s r, r and products of dy with them have to be within fp32.
  * dx may be dy or ds.  dweight has the weight's type.  Fixed order of sums;
  * the workspace as in fo_embedding_grad (no counterpart in the paper). */
 FO_API int fo_rms_norm_grad(const void* dy, int64_t dy_stride, const void* ds, int64_t ds_stride, const void* s, int64_t s_stride,

@@ -4,6 +4,9 @@
 //   s = x + residual (rounded to the tensors' type);  r = (mean s^2 + eps)^(-1/2);  y = s r w
 //   dx = r (w dy - s r^2 mean(w dy s)) + ds;          dw = sum over rows of dy s r
 //
+// The gradient is taken as r (w dy - z mean(w dy z)) + ds with z = s r: of r^2 and r^3
+// either leaves fp32 where r alone and the result do not.
+//
 // A row's elements stay in registers between the sum of squares and the
 // output, so that each tensor passes once: forward x, residual in, s, y out;
 // backward dy, ds, s in, dx out.  Both are bound by HBM for large inputs and by
@@ -399,18 +402,19 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_k(const __grid_constant__ No
     float a = 0.f;
 #pragma unroll
     for (int i = 0; i < 8 * NV; ++i) {
-      dw[i] = fmaf(g[i], s[i] * r, dw[i]);
+      s[i] *= r;
+      dw[i] = fmaf(g[i], s[i], dw[i]);
       g[i] *= w[i];
       a = fmaf(g[i], s[i], a);
     }
     a = WARP ? warp_sum(a) : block_sum(a, box[turn]);
     turn ^= 1;
-    const float k = -r * r * (a * r * p.inv_cols);     // r^3 alone leaves fp32 where its products do not
+    const float k = -a * p.inv_cols;
     if (VEC && ds) ring.get(n, 2, p.cols, t, G, THREADS, d);
 #pragma unroll
     for (int i = 0; i < 8 * NV; ++i) {
-      g[i] = fmaf(g[i], r, s[i] * k);
-      if (ds) g[i] += d[i];
+      g[i] = fmaf(s[i], k, g[i]);
+      g[i] = ds ? fmaf(g[i], r, d[i]) : g[i] * r;
     }
     store_row<T, VEC, NV>(static_cast<T*>(p.dx) + row * p.lddx, p.cols, t, G, g);
     n = n + 1 == STAGES ? 0 : n + 1;
@@ -448,16 +452,15 @@ __global__ void __launch_bounds__(1024) norm_bwd_wide_k(const __grid_constant__ 
     const float r = p.rstd[row];
     float a = 0.f;
     for (int c = t; c < p.cols; c += G) {
-      const float g = to_f(dy[c]), z = to_f(s[c]);
-      out[c] = fmaf(g, z * r, out[c]);
+      const float g = to_f(dy[c]), z = to_f(s[c]) * r;
+      out[c] = fmaf(g, z, out[c]);
       a = fmaf(g * to_f(w[c]), z, a);
     }
-    const float k = -r * r * (block_sum(a, box[turn]) * r * p.inv_cols);
+    const float k = -block_sum(a, box[turn]) * p.inv_cols;
     turn ^= 1;
     for (int c = t; c < p.cols; c += G) {
-      float g = fmaf(to_f(dy[c]) * to_f(w[c]), r, to_f(s[c]) * k);
-      if (ds) g += to_f(ds[c]);
-      dx[c] = from_f<T>(g);
+      const float g = fmaf(to_f(s[c]) * r, k, to_f(dy[c]) * to_f(w[c]));
+      dx[c] = from_f<T>(ds ? fmaf(g, r, to_f(ds[c])) : g * r);
     }
   }
 }
