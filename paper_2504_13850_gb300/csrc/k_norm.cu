@@ -288,7 +288,11 @@ __global__ void __launch_bounds__(1024) norm_fwd_wide_k(const __grid_constant__ 
   const T* from = s ? s : x;        // each thread reads what it wrote
   const int blocks = (p.cols + 31) / 32;
   for (int c = t; c < 32 * blocks; c += G) {     // whole warps
-    const float v = c < p.cols ? scaled(to_f(from[c]), r, to_f(static_cast<const W*>(p.w)[c])) : 0.f;
+    float v = 0.f;
+    if (c < p.cols) {
+      const float z = to_f(from[c]), w = to_f(static_cast<const W*>(p.w)[c]);
+      v = p.q ? scaled(z, r, w) : z * r.hi * w;       // an infinite weight stays one where y alone is wanted
+    }
     if (y && c < p.cols) y[c] = from_f<T>(v);
     if (p.q) {
       const int b = block_exponent(__reduce_max_sync(0xffffffffu, magnitude(v)));
