@@ -228,8 +228,8 @@ PyObject* norm(PyObject* x_, PyObject* residual_, PyObject* weight_, PyObject* e
   const Rows xr = rows_of(x, shape, type, at.index, "x");
   Rows rr, sr, yr;
   at::Tensor s = x, y, r, q, scales;
-  if (residual_ != Py_None) {
-    rr = rows_of(tensor(residual_, "residual"), shape, type, at.index, "residual");
+  if (residual_ != Py_None) rr = rows_of(tensor(residual_, "residual"), shape, type, at.index, "residual");
+  if (residual_ != Py_None || sum_ != Py_None) {
     s = sum_ == Py_None ? at.empty(shape, type) : tensor(sum_, "sum_out");
     sr = rows_of(s, shape, type, at.index, "sum_out");
   }
