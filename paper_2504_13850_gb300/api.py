@@ -726,7 +726,8 @@ def rms_norm(x, residual, weight, eps=1e-6, out=None, sum_out=None, stream=None)
     """fo_rms_norm: (y, s, r) with s = x + residual (where residual is None, x
     itself, or a copy in `sum_out`), r = (mean s^2 + eps)^(-1/2) in fp32 and
     y = s r weight, over the last dimension of a bf16 or fp32 device tensor.
-    weight: x's type or fp32.  `out` and `sum_out` may give y and s.  Runs on `stream`, by default torch's
+    weight: x's type or fp32.  `out` and `sum_out` may give y and s; `out` may be
+    x where s is not.  Runs on `stream`, by default torch's
     current stream."""
     return (_compiled or _binding()).rms_norm(x, residual, weight, eps, out, sum_out, stream)
 

@@ -237,6 +237,7 @@ PyObject* norm(PyObject* x_, PyObject* residual_, PyObject* weight_, PyObject* e
   if (with_y) {
     y = out_ == Py_None ? at.empty(shape, type) : tensor(out_, "out");
     yr = rows_of(y, shape, type, at.index, "out");
+    if (!sr.data && yr.data == xr.data && rows > 0) refuse(PyExc_ValueError, "out: x is the sum that is returned; sum_out can take it");
     r = at.empty(outer, ScalarType::Float);
   }
   if (eight) {

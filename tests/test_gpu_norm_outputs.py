@@ -30,3 +30,18 @@ def test_sum_out_without_a_residual_holds_x(dtype, cols):
             assert bool(((got - first).double().abs() <= 2.01 * off * first.double().abs()).all())
     with pytest.raises(ValueError):
         api.rms_norm(x, None, w, sum_out=torch.zeros(4, cols, device="cuda", dtype=dtype))
+
+
+@pytest.mark.parametrize("cols", [512, 20000])
+def test_y_in_place_of_x(cols):
+    """Refused where x would be returned as s, which the gradient reads; s elsewhere, y may lie in x's place."""
+    x, w = torch.randn(5, cols, device="cuda"), torch.randn(cols, device="cuda")
+    before, want = x.clone(), api.rms_norm(x, None, w)
+    with pytest.raises(ValueError, match="sum_out"):
+        api.rms_norm(x, None, w, out=x)
+    with pytest.raises(ValueError, match="sum_out"):
+        api.rms_norm(x, None, w, out=x.view(5, cols))
+    assert torch.equal(x, before)
+    y, s, r = api.rms_norm(x, None, w, out=x, sum_out=torch.empty_like(x))
+    assert y is x and torch.equal(s, before) and torch.equal(y, want[0]) and torch.equal(r, want[2])
+    assert api.rms_norm(x[:0], None, w, out=x[:0])[0].shape == (0, cols)
