@@ -253,11 +253,17 @@ class RmsDevice:
         # waits for the step's work; a kernel that gave up a wait ends the step
         # before it changes a parameter
         api.attention_error()
-        with torch.no_grad():
+        changed = [t.detach() for t in (*self.matrices, *self.momenta)]
+        before = [t.clone() for t in changed]
+        try:
             api.muon_step(self.matrices, [p.grad for p in self.matrices], self.momenta, self.matrix_lr, momentum=self.momentum,
                           weight_decay=self.weight_decay)
+            api.orthogonalize_error()
+        except api.FedOptimaError:             # part of them is void
+            for t, b in zip(changed, before):
+                t.copy_(b)
+            raise
         self.opt.step()
-        api.orthogonalize_error()
         return tuple(t.detach() for t in upload), loss.detach()
 
 
