@@ -1,6 +1,8 @@
 """Build the C-ABI shared library libfedoptima.so in-tree with nvcc for
 sm_103a (GB300), and _binding.so, the compiled part of its Python binding, with
 g++ against torch's headers.  Sources compile in parallel; objects go to _build/.
+The library needs nvcc alone: without torch or g++ it is built and the binding
+left out.
 
 Several processes may call build() at once (one per rank under torchrun):
 an exclusive file lock serialises them, and every object and the library
@@ -37,8 +39,19 @@ def nvcc():
 
 
 def _torch():
-    """torch's folder, without importing it."""
-    return importlib.util.find_spec("torch").submodule_search_locations[0]
+    """torch's folder, without importing it, or None."""
+    spec = importlib.util.find_spec("torch")
+    return spec.submodule_search_locations[0] if spec else None
+
+
+def _without_binding():
+    """Why the binding cannot be built here, or None."""
+    root = _torch()
+    if root is None:
+        return "torch is not installed"
+    if not os.path.exists(os.path.join(root, "include", "torch", "csrc", "autograd", "python_variable.h")):
+        return "torch has no headers here"
+    return None if shutil.which("g++") else "g++ was not found"
 
 
 def _run(cmd, what, tmp):
@@ -75,8 +88,6 @@ def _link_binding(obj):
 
 
 def _compile(src, extra):
-    if src.endswith(".cpp"):
-        return _compile_binding()
     obj = os.path.join(BUILD, os.path.splitext(src)[0] + ".o")
     srcp = os.path.join(CSRC, src)
     deps = [srcp] + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".hpp", ".cuh"))]
@@ -97,9 +108,10 @@ def build(verbose=False, extra=()):
         except OSError:                       # a filesystem without locks: build unserialised
             pass
         with cf.ThreadPoolExecutor(max_workers=min(len(SOURCES), os.cpu_count() or 4)) as ex:
-            results = list(ex.map(lambda s: _compile(s, list(extra)), SOURCES + ["fo_binding.cpp"]))
+            why = _without_binding()
+            binding = None if why else ex.submit(_compile_binding)
+            results = list(ex.map(lambda s: _compile(s, list(extra)), SOURCES))
         objs = [o for o, _ in results]
-        binding = objs.pop()
         if verbose:
             for _, log in results:
                 if log:
@@ -109,7 +121,13 @@ def build(verbose=False, extra=()):
             tmp = f"{OUT}.{os.getpid()}.tmp"
             _run([nvcc(), *ARCH, "-shared", "-o", tmp, *objs], "link failed", tmp)
             os.replace(tmp, OUT)
-        _link_binding(binding)
+        if binding is None:
+            sys.stderr.write(f"_binding.so is left out ({why}): embedding, norms and orthogonalised updates have no Python entry points\n")
+        else:
+            obj, log = binding.result()
+            if verbose and log:
+                sys.stderr.write(log)
+            _link_binding(obj)
     return OUT
 
 
