@@ -63,18 +63,43 @@ def _run(cmd, what, tmp):
     return r.stderr
 
 
+def _made_for():
+    """What the binding's binary interface goes by: this Python, and torch's folder, version and revision."""
+    root = _torch()
+    with open(os.path.join(root, "version.py")) as f:
+        return f"{sys.version}\n{root}\n{f.read()}"
+
+
+def _binding_files():
+    return os.path.join(BUILD, "fo_binding.o"), os.path.join(CSRC, "fo_binding.cpp")
+
+
+def _is_current():
+    """Whether the binding's object is of its source and for this torch."""
+    obj, src = _binding_files()
+    try:
+        with open(obj + ".txt") as f:
+            if f.read() != _made_for():
+                return False
+        deps = [src, os.path.join(HERE, "..", "include", "fedoptima.h")]
+        return all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps)
+    except (OSError, TypeError):               # no object, or no torch
+        return False
+
+
 def _compile_binding():
-    obj, src = os.path.join(BUILD, "fo_binding.o"), os.path.join(CSRC, "fo_binding.cpp")
-    include = os.path.join(_torch(), "include")
-    deps = [src, os.path.join(HERE, "..", "include", "fedoptima.h"), os.path.join(include, "torch", "csrc", "autograd", "python_variable.h")]
-    if os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps):
+    obj, src = _binding_files()
+    if _is_current():
         return obj, ""
+    include = os.path.join(_torch(), "include")
     cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc()))), "include")
     tmp = f"{obj}.{os.getpid()}.tmp"
     log = _run(["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I" + sysconfig.get_paths()["include"], "-isystem", include,
                 "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-isystem", cuda, "-c", src, "-o", tmp],
                "g++ failed for fo_binding.cpp", tmp)
     os.replace(tmp, obj)
+    with open(obj + ".txt", "w") as f:        # last: without it the object is made again
+        f.write(_made_for())
     return obj, log
 
 
@@ -122,6 +147,8 @@ def build(verbose=False, extra=()):
             _run([nvcc(), *ARCH, "-shared", "-o", tmp, *objs], "link failed", tmp)
             os.replace(tmp, OUT)
         if binding is None:
+            if os.path.exists(BINDING) and not _is_current():
+                os.remove(BINDING)             # made for another torch, or from another source
             sys.stderr.write(f"_binding.so is left out ({why}): embedding, norms and orthogonalised updates have no Python entry points\n")
         else:
             obj, log = binding.result()

@@ -29,6 +29,8 @@ def test_the_library_needs_no_torch_and_no_compiler_but_nvcc(sources, monkeypatc
     else:
         which = build.shutil.which
         monkeypatch.setattr(build.shutil, "which", lambda name, *a, **kw: None if name == "g++" else which(name, *a, **kw))
+    with open(build.BINDING, "w") as f:
+        f.write("made for another torch")
     assert build.build() == build.OUT and os.path.exists(build.OUT)
     assert not os.path.exists(build.BINDING) and "_binding.so is left out" in capfd.readouterr().err
 
@@ -38,3 +40,19 @@ def test_a_binding_that_does_not_compile_raises_behind_the_library(sources):
     with pytest.raises(RuntimeError, match="not this one"):
         build.build()
     assert os.path.exists(build.OUT)
+
+
+def test_another_torch_gets_another_binding(sources, monkeypatch, tmp_path):
+    """Whatever the dates of its files."""
+    os.makedirs(build.BUILD)
+    root = tmp_path / "torch"
+    (root / "include").mkdir(parents=True)
+    monkeypatch.setattr(build, "_torch", lambda: str(root))
+    said = []
+    run = build._run
+    monkeypatch.setattr(build, "_run", lambda *a: said.append(a[1]) or run(*a))
+    for version, compiled in (("2.9.1", 1), ("2.9.1", 1), ("2.11.0", 2), ("2.11.0", 2), ("2.9.1", 3)):
+        (root / "version.py").write_text(f"__version__ = '{version}'\n")
+        os.utime(root / "version.py", (0, 0))
+        build._compile_binding()
+        assert len(said) == compiled
