@@ -556,12 +556,13 @@ RowShape row_shape(int cols) {
   return {false, 1024};
 }
 // Blocks of a gradient: two per SM, or one whose rows in flight fill its shared
-// memory (fewer where there are fewer rows).
-int grad_blocks(int rows, int cols) {
+// memory (fewer where there are fewer rows).  fp32 rows of 513 to 1024 columns fill
+// it too, and their 304 blocks take two turns.
+int grad_blocks(int64_t rows, int cols) {
   const RowShape a = row_shape(cols);
-  const int per = a.warp ? a.threads / 32 : 1, want = (rows + per - 1) / per;
+  const int64_t per = a.warp ? a.threads / 32 : 1, want = (rows + per - 1) / per;
   const int most = cols <= 4096 ? 2 * 152 : 152;
-  return want < most ? want : most;
+  return want < most ? int(want) : most;
 }
 
 template <typename T, typename W, bool VEC, bool EIGHT>
@@ -692,7 +693,7 @@ int fo_rms_norm(const void* x, int64_t x_stride, const void* residual, int64_t r
 
 int64_t fo_rms_norm_workspace(int64_t rows, int64_t cols) {
   if (check_sizes(FO_DTYPE_F32, rows, cols)) return -1;
-  return rows == 0 ? 0 : int64_t(grad_blocks(int(rows), int(cols))) * cols * 4;
+  return rows == 0 ? 0 : int64_t(grad_blocks(rows, int(cols))) * cols * 4;
 }
 
 int fo_rms_norm_grad(const void* dy, int64_t dy_stride, const void* ds, int64_t ds_stride, const void* s, int64_t s_stride,
