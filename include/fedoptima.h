@@ -569,16 +569,20 @@ FO_API int fo_decode_8bit(const uint8_t* q, const uint8_t* scales, void* y, int6
  *     `steps` times, on X or its transpose, whichever has rows <= columns:
  *         A = X X^T;  X <- c0 X + (c1 A + c2 A A) X
  *     out = X;  param <- decay param - step X
- * Coefficients such as (3.4445, -4.7750, 2.0315) bring the singular values into
- * 0.7 .. 1.2 in five steps.  The products run on the tensor cores, on fp16
+ * The coefficients (3.4445, -4.7750, 2.0315), published with the Muon optimiser
+ * (Jordan and others, 2024), bring singular values from 0.0015 of the norm up into
+ * 0.68 .. 1.21 in five steps; smaller ones grow by up to 485.  The products run on the tensor cores, on fp16
  * operands for bf16 matrices without a param (roundings of 2^-12) and on pairs of
  * them where grad or param is fp32: an element of X, whose norm is 1 at first, is held to 2^-23 of itself or
- * to 2^-46, whichever is more, so that a row (of the shorter side) below about
- * 1e-6 of the others keeps fewer bits than the rest.  Sums are fp32; a singular
+ * to 2^-46, whichever is more, so that a row or column below about 1e-6 of the
+ * others keeps fewer bits than the rest.  Sums are fp32; a singular
  * value t above 16 on the way, or c1 t^2 + c2 t^4 beyond +-255, overflows.  An
- * infinity or NaN in U makes all of X NaN.  The order of all sums is fixed.  Sides of 0 to 32768 (the smaller) and 2^20.  What one matrix writes
- * is none of another's tensors, and out, momentum and param are three (equal
- * addresses are refused, but for out and the same matrix's grad).
+ * infinity or NaN in U makes all of X NaN.  The order of all sums is fixed: equal
+ * calls give equal bits (which other matrices are in the list decides how some sums
+ * are shared, and may move a matrix's last bits).  Sides of 0 to 32768 (the smaller)
+ * and 2^20.  What one matrix writes is none of another's tensors, and out, momentum
+ * and param are three: equal addresses are refused, but for out and the same
+ * matrix's grad; tensors that overlap from different addresses are not noticed.
  * ---------------------------------------------------------------------- */
 typedef struct fo_matrix_update {
   int64_t rows, cols;

@@ -727,8 +727,7 @@ def rms_norm(x, residual, weight, eps=1e-6, out=None, sum_out=None, stream=None)
     itself, or a copy in `sum_out`), r = (mean s^2 + eps)^(-1/2) in fp32 and
     y = s r weight, over the last dimension of a bf16 or fp32 device tensor.
     weight: x's type or fp32.  `out` and `sum_out` may give y and s; `out` may be
-    x where s is not.  Runs on `stream`, by default torch's
-    current stream."""
+    x where s is not.  Runs on `stream`, by default torch's current stream."""
     return (_compiled or _binding()).rms_norm(x, residual, weight, eps, out, sum_out, stream)
 
 
@@ -752,7 +751,8 @@ def decode_8bit(q, scales, dtype=None, out=None, stream=None):
     return (_compiled or _binding()).decode_8bit(q, scales, dtype, out, stream)
 
 
-# Coefficients that bring singular values into 0.7 .. 1.2 in five steps.
+# Coefficients published with the Muon optimiser (Jordan and others, 2024): singular
+# values from 0.0015 of the norm up reach 0.68 .. 1.21 in five steps.
 QUINTIC = (3.4445, -4.7750, 2.0315)
 
 

@@ -620,7 +620,7 @@ SortLayout layout(int64_t tokens, int64_t width) {
   a.blocks = unsigned(want < kMaxSortBlocks ? want : kMaxSortBlocks);
   a.per = unsigned((tokens + a.blocks - 1) / a.blocks);
   a.counts = take(int64_t(a.blocks) * kBins * 4);
-  // shorter pieces where there are few: at least 16 warps per SM
+  // shorter pieces where they and their chunks of columns are few: at least 16 warps per SM
   const int64_t chunks = (width + 255) / 256;
   a.piece = 32;
   while (a.piece > 8 && (tokens + a.piece - 1) / a.piece * chunks < 16 * 152) a.piece /= 2;

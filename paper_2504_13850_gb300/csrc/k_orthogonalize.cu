@@ -20,18 +20,17 @@
 // weak directions that each step multiplies by up to a, and small once the rows
 // are orthogonal (errors before the result's rounding: 512 x 512 2.2e-3 with all
 // of it in the product, 0.7e-3 without a, 0.5e-3 without the diagonal; 16 x 300
-// 2.1, 1.4 and 0.6e-3).  For fp32 matrices,
-// and for bf16 ones that update parameters, all operands are such pairs, and each product three (hi lo, lo hi, hi hi, in
-// this order; the fourth is below fp32's rounding).  The second number is held
-// 2^11 times its size, or it would be subnormal where the first is small: an
+// 2.1, 1.4 and 0.6e-3).  For fp32 matrices, and for bf16 ones that update
+// parameters, all operands are such pairs, and each product three (hi lo, lo hi,
+// hi hi, in this order; the fourth is below fp32's rounding).  The second number is
+// held 2^11 times its size, or it would be subnormal where the first is small: an
 // element of X is off by 2^-23 of itself or 2^-46, whichever is more (2^-35 without:
 // a row of a 512 x 2048 matrix at 1e-5 of the others was off by 1.9e-3 of itself).
 // The tensor cores take the sum of the two mixed products times 2^-11 as they begin
-// the third.
-// Sums are fp32 in tensor
-// memory; because the tensor cores truncate, those of fp32 matrices are moved to
-// registers and added there, rounded, every 64 terms (512: 7e-6 off instead of
-// 1.5e-6 on matrices of width 512, torch's fp32 products 2.3e-6).
+// the third.  Sums are fp32 in tensor memory; because the tensor cores truncate,
+// those of pairs are moved to registers and added there, rounded, every 64 terms
+// (matrices of width 512 are 7e-7 off, moved every 512 terms they were 7e-6;
+// torch's fp32 products 2.3e-6).
 //
 // X, A and C lie in the workspace as blocks of 64 x 64 elements of 8 KB in the
 // image that a 128-byte-swizzled operand has in shared memory, block rows

@@ -14,9 +14,11 @@ f_d, then the upload of its split-point activations, which the server trains on
 (``api.embedding`` / ``embedding_grad``), root-mean-square norms that take the
 residual's addition with them (``api.rms_norm`` / ``rms_norm_grad``), and weight
 matrices whose momentum is made orthogonal before each step
-(``api.muon_step``).  It uploads its split-point activations in 8 bits
-(``api.rms_norm_8bit``), half of the bytes S_l / b_k of Eq. 5 that bf16 takes;
-the server's side decodes them (``api.decode_8bit``).
+(``api.muon_step``).  It hands over its split-point activations in 8 bits
+(``api.rms_norm_8bit``), a form of half the bytes S_l / b_k of Eq. 5 that bf16
+takes.  Here the devices share the server's GPU and no link is crossed:
+``run`` decodes them beside the server (``api.decode_8bit``), whose slots take
+bf16.
 
     python -m paper_2504_13850_gb300.sequence [--rms]
 """
