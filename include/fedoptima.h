@@ -573,7 +573,7 @@ FO_API int fo_decode_8bit(const uint8_t* q, const uint8_t* scales, void* y, int6
  * (Jordan and others, 2024), bring singular values from 0.0015 of the norm up into
  * 0.68 .. 1.21 in five steps; smaller ones grow by up to 485.  The products run on the tensor cores, on fp16
  * operands for bf16 matrices without a param (roundings of 2^-12) and on pairs of
- * them where grad or param is fp32: an element of X, whose norm is 1 at first, is held to 2^-23 of itself or
+ * them where grad or param is fp32 or a side is at most 16: an element of X, whose norm is 1 at first, is held to 2^-23 of itself or
  * to 2^-46, whichever is more, so that a row or column below about 1e-6 of the
  * others keeps fewer bits than the rest.  Sums are fp32; a singular
  * value t above 16 on the way, or c1 t^2 + c2 t^4 beyond +-255, overflows.  An

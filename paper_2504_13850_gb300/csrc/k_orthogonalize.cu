@@ -21,7 +21,7 @@
 // are orthogonal (errors before the result's rounding: 512 x 512 2.2e-3 with all
 // of it in the product, 0.7e-3 without a, 0.5e-3 without the diagonal; 16 x 300
 // 2.1, 1.4 and 0.6e-3).  For fp32 matrices, and for bf16 ones that update
-// parameters, all operands are such pairs, and each product three (hi lo, lo hi,
+// parameters or have a side of up to 16, all operands are such pairs, and each product three (hi lo, lo hi,
 // hi hi, in this order; the fourth is below fp32's rounding).  The second number is
 // held 2^11 times its size, or it would be subnormal where the first is small: an
 // element of X is off by 2^-23 of itself or 2^-46, whichever is more (2^-35 without:
@@ -1178,8 +1178,13 @@ bool is_small(const fo_matrix_update& m) {
 }
 // Operands are pairs where X goes anywhere in fp32: the roundings of single ones are
 // small only beside a result's in bf16 (1e-3 and 1.7e-3; 512 x 768 8e-4 of an update
-// of parameters, with pairs 1e-6).
-bool in_pairs(const fo_matrix_update& m, int dtype) { return dtype == FO_DTYPE_F32 || m.param; }
+// of parameters, with pairs 1e-6).  And where a side has up to 16 elements, whose few
+// roundings do not even out: results were off by up to 1.7 times as much as their own
+// rounding, from 17 on by 1.25 times (20 x 20 22 us, in pairs 33).
+constexpr int kFew = 16;
+bool in_pairs(const fo_matrix_update& m, int dtype) {
+  return dtype == FO_DTYPE_F32 || m.param || m.rows <= kFew || m.cols <= kFew;
+}
 // Small matrices: parts of X X^T of even and odd steps, and of the norm.
 int64_t item_bytes(const fo_matrix_update& m, int dtype) {
   if (m.rows == 0 || m.cols == 0) return 0;
